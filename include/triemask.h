@@ -91,6 +91,10 @@ enum { TRIE_DTYPE_F32 = 0, TRIE_DTYPE_BF16 = 1 };
 
 #define TRIE_STATE_DEAD (-1)
 #define TRIE_STATE_FINISHED (-2)
+/* A row of a batch without a grammar: trie_head_logits, trie_penalize and
+ * trie_sample allow it every token. The other calls take it as they take any
+ * id that is not a node, so the free rows of a mixed batch stay out of them. */
+#define TRIE_STATE_FREE (-3)
 
 /* Build the byte trie of K strings (Sec. 4.1: insert each value character by
  * character, merging shared prefixes; App. G.1 Step 1). Host only: no device
@@ -477,6 +481,110 @@ int fmt_apply_mask(fmt_t f, void *d_logits, int dtype, const int32_t *d_states, 
 
 /* Release the format and its device copy. NULL is a no-op. */
 int fmt_destroy(fmt_t f);
+
+/* ---- From hidden states to the sampled token ----
+ * The calls around a mask in a decode step: the logits head, the penalties and
+ * the sampler. They need no handle. Their grammar is a mask and a state for
+ * each row of the batch, all three optional together (d_mask NULL: every row
+ * is free):
+ *   d_mask     device uint32[mask_rows][ceil(V/32)], as trie_compile_masks,
+ *              fmt_compile_masks or trie_lazy_rows write it
+ *   d_states   device int32[B]: a row of the mask; TRIE_STATE_FREE (no
+ *              grammar: every token); any other value the row {EOS}
+ * Logits are [B, V] with rows `stride` elements apart (stride >= V) and
+ * consecutive elements in a row; what lies between the rows is not touched.
+ * 2 <= V <= 2^31 - 1024; offsets are computed in 64 bits. No call allocates or synchronises; B = 0 is
+ * a no-op. Errors: TRIE_EINVAL, TRIE_ECUDA. */
+
+/* Quantize M rows of D hidden states to e4m3 with a scale for each row and 128
+ * columns: the block's largest magnitude times 1/448, rounded to 32 bits (1 where
+ * that is 0); values are divided by it and rounded to nearest even. A row with a NaN or an infinity
+ * gets NaNs, and NaN logits.
+ *   d_x       device [M] rows of D, `stride` elements apart, dtype
+ *             TRIE_DTYPE_F32 or _BF16
+ *   d_q       device uint8[M][D]
+ *   d_scales  device float[ceil(D/128)][pitch], pitch >= M (a multiple of 4
+ *             for trie_head_logits); row m's scales are column m */
+int trie_head_quantize(const void *d_x, int dtype, int64_t stride, int32_t M, int32_t D, uint8_t *d_q,
+                       float *d_scales, int64_t pitch, cudaStream_t stream);
+
+/* The same for a weight matrix of V rows, with a scale for each block of 128
+ * rows and 128 columns: d_scales device float[ceil(V/128)][ceil(D/128)]. */
+int trie_head_quantize_weight(const void *d_w, int dtype, int64_t stride, int32_t V, int32_t D, uint8_t *d_q,
+                              float *d_scales, cudaStream_t stream);
+
+/* logits = x W^T of quantized hidden states and weights, under a grammar:
+ * logits[m][v] = sum over blocks kb of scales[kb][m] w_scales[v/128][kb] times
+ * the sum of q[m][k] w[v][k] over the block, and -inf where row m's state does
+ * not allow v. Sums are kept in 32 bits and rounded once to the logits' type.
+ * Weights of 128 consecutive tokens that no row of the batch allows are not
+ * read. D a multiple of 16; d_q, d_w and d_scales 16-byte aligned; M <= 2^20. */
+int trie_head_logits(const uint8_t *d_q, const float *d_scales, int64_t pitch, const uint8_t *d_w,
+                     const float *d_w_scales, int32_t M, int32_t V, int32_t D, void *d_logits, int dtype,
+                     int64_t stride, const uint32_t *d_mask, int32_t mask_rows, const int32_t *d_states,
+                     cudaStream_t stream);
+
+/* Penalties, biases and the grammar on a batch of logits, in place. For token t
+ * of a row, with c(t) its occurrences after the prompt:
+ *   l = l > 0 ? l / repetition : l * repetition   where t is in the history
+ *   l = (l - frequency * c(t)) - presence         where c(t) > 0
+ *   l = l + bias(t)                               where the row lists a bias
+ *   l = -inf                                      where the state does not allow t
+ * in 32 bits, each operation rounded to nearest, rounded once to the logits'
+ * type; logits that nothing applies to keep their bits.
+ *   d_history  device int32[B] rows, history_stride apart, of which the first
+ *              d_length[b] tokens count (at most max_length, <= history_stride);
+ *              ids outside [0, V) are skipped. NULL: no history.
+ *   d_prompt   device int32[B]: the first d_prompt[b] tokens of the history are
+ *              the prompt (NULL: none are)
+ *   d_repetition, d_presence, d_frequency  device float[B], each may be NULL
+ *              (1, 0 and 0); repetition > 0
+ *   d_bias_offsets  device int32[B+1]: row b's biases are entries
+ *              d_bias_offsets[b] .. d_bias_offsets[b+1]-1 of d_bias_tokens
+ *              (int32, ids outside [0, V) are skipped) and d_bias_values
+ *              (float); those of a token listed twice are added up in list
+ *              order first. NULL: no biases.
+ * B <= 65535. */
+int trie_penalize(void *d_logits, int dtype, int64_t stride, int32_t B, int32_t V, const int32_t *d_history,
+                  int64_t history_stride, int32_t max_length, const int32_t *d_length, const int32_t *d_prompt,
+                  const float *d_repetition, const float *d_presence, const float *d_frequency,
+                  const int32_t *d_bias_offsets, const int32_t *d_bias_tokens, const float *d_bias_values,
+                  const uint32_t *d_mask, int32_t mask_rows, const int32_t *d_states, cudaStream_t stream);
+
+/* Bytes of device memory that trie_sample needs for its own use (-1 for sizes
+ * out of range). What it holds between calls does not matter; calls that may
+ * run at the same time need one each. */
+int64_t trie_sample_workspace(int32_t B, int32_t V);
+
+/* Sample a token for each row. Of the allowed tokens (logits x, NaN counted as
+ * -inf, M the largest, w = exp((x - M) / temperature)), ordered by x descending
+ * and id ascending: the first top_k are kept; of those each whose predecessors'
+ * weights sum to less than top_p times the weight of the first top_k; of those
+ * the ones with w >= min_p. The first is always kept.
+ * The draw takes the group of 256 consecutive ids with the largest
+ * log(kept weight) + noise(2^31 + group), then of its kept tokens the one with
+ * the largest (x - M) / temperature + noise(id), ties to the lowest id: tokens
+ * are drawn with probabilities proportional to the kept weights. noise(n) is
+ * -log(-log u) with u = (2 i + 1) / 2^24, i the top 23 bits of
+ * splitmix64(seed + (n + 1) 0x9E3779B97F4A7C15): the same seed gives the same
+ * token, so a row needs a new seed for every step.
+ *   d_seeds        device int64[B]
+ *   d_temperature  device float[B]; not above 0: the largest logit, lowest id
+ *   d_top_k        device int32[B]; <= 0 or >= V: off
+ *   d_top_p        device float[B]; not below 1: off
+ *   d_min_p        device float[B]; not above 0: off
+ *                  each of these four may be NULL (1, off, off, off)
+ *   d_workspace    device, trie_sample_workspace(B, V) bytes, 8-byte aligned
+ *   d_tokens       device int32[B]; -1 where the row has nothing to choose from
+ *                  (trie_advance takes it to DEAD)
+ *   d_logprobs     device float[B] or NULL: the token's log-probability among all
+ *                  allowed tokens at the temperature (at 1 when that is not
+ *                  above 0), before top-k, top-p and min-p; -inf beside -1
+ * B <= 65535. */
+int trie_sample(const void *d_logits, int dtype, int64_t stride, int32_t B, int32_t V, const int64_t *d_seeds,
+                const float *d_temperature, const int32_t *d_top_k, const float *d_top_p, const float *d_min_p,
+                const uint32_t *d_mask, int32_t mask_rows, const int32_t *d_states, void *d_workspace,
+                int32_t *d_tokens, float *d_logprobs, cudaStream_t stream);
 
 /* Release the handle, its host arrays and its device copy of the trie.
  * Synchronises the device first if device memory is held. NULL is a no-op. */

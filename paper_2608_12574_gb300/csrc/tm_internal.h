@@ -29,10 +29,10 @@ __device__ __forceinline__ void pdl_launch_dependents() {
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 template <typename... Params, typename... Args>
-cudaError_t launch_pdl_smem(void (*kernel)(Params...), int64_t grid, int block, size_t smem, cudaStream_t st,
+cudaError_t launch_pdl_grid(void (*kernel)(Params...), dim3 grid, int block, size_t smem, cudaStream_t st,
                             Args... args) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(grid < 1 ? 1 : grid));
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(unsigned(block));
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
@@ -42,6 +42,12 @@ cudaError_t launch_pdl_smem(void (*kernel)(Params...), int64_t grid, int block, 
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+}
+
+template <typename... Params, typename... Args>
+cudaError_t launch_pdl_smem(void (*kernel)(Params...), int64_t grid, int block, size_t smem, cudaStream_t st,
+                            Args... args) {
+    return launch_pdl_grid(kernel, dim3(unsigned(grid < 1 ? 1 : grid)), block, smem, st, args...);
 }
 
 template <typename... Params, typename... Args>

@@ -16,7 +16,7 @@ import numpy as np
 
 TRIE_OK, TRIE_EINVAL, TRIE_ENOMEM, TRIE_ECUDA, TRIE_ESTATE = 0, -1, -2, -3, -4
 TRIE_DTYPE_F32, TRIE_DTYPE_BF16 = 0, 1
-TRIE_STATE_DEAD, TRIE_STATE_FINISHED = -1, -2
+TRIE_STATE_DEAD, TRIE_STATE_FINISHED, TRIE_STATE_FREE = -1, -2, -3
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtriemask.so")
 _lock = threading.Lock()
@@ -62,6 +62,15 @@ SIGNATURES = {
     "fmt_advance": (ctypes.c_int, [_P, _P, _P, _I32, _P, _P]),
     "fmt_apply_mask": (ctypes.c_int, [_P, _P, ctypes.c_int, _P, _I32, _I32, _P]),
     "fmt_destroy": (ctypes.c_int, [_P]),
+    "trie_head_quantize": (ctypes.c_int, [_P, ctypes.c_int, _I64, _I32, _I32, _P, _P, _I64, _P]),
+    "trie_head_quantize_weight": (ctypes.c_int, [_P, ctypes.c_int, _I64, _I32, _I32, _P, _P, _P]),
+    "trie_head_logits": (ctypes.c_int, [_P, _P, _I64, _P, _P, _I32, _I32, _I32, _P, ctypes.c_int, _I64, _P, _I32, _P,
+                                        _P]),
+    "trie_penalize": (ctypes.c_int, [_P, ctypes.c_int, _I64, _I32, _I32, _P, _I64, _I32, _P, _P, _P, _P, _P, _P, _P, _P,
+                                     _P, _I32, _P, _P]),
+    "trie_sample_workspace": (_I64, [_I32, _I32]),
+    "trie_sample": (ctypes.c_int, [_P, ctypes.c_int, _I64, _I32, _I32, _P, _P, _P, _P, _P, _P, _I32, _P, _P, _P, _P,
+                                   _P]),
     "trie_destroy": (ctypes.c_int, [_P]),
     "trie_destroy_async": (ctypes.c_int, [_P, _P]),
     "trie_last_error": (ctypes.c_char_p, []),
@@ -534,6 +543,196 @@ def trie_destroy(h: Trie) -> None:
 
 def trie_destroy_async(h: Trie, stream=None) -> None:
     h.destroy_async(stream)
+
+
+# ------------------------------------------- from hidden states to the token
+
+def _rows(t, dtypes, name: str) -> tuple[int, int]:
+    """(address, elements between rows) of a 2-D CUDA tensor whose rows are contiguous and do not overlap."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must have dtype in {dtypes}, got {t.dtype}")
+    n, m = t.shape
+    if (m > 1 and t.stride(1) != 1) or (n > 1 and t.stride(0) < m):
+        raise ValueError(f"{name} must have contiguous rows that do not overlap")
+    return t.data_ptr(), t.stride(0) if n > 1 else m
+
+
+def _per_row(t, dtype, B: int, name: str, like):
+    """Address of an optional tensor with a value for each row of the batch."""
+    if t is None:
+        return None
+    if t.numel() != B:
+        raise ValueError(f"{name} must have B entries")
+    return _with(like, t, name, _dev(t, (dtype,), name))
+
+
+def _with(like, t, name: str, p):
+    if t.get_device() != like.get_device():
+        raise ValueError(f"{name} is on another device than the logits")
+    return p
+
+
+def _grammar(mask, states, B: int, V: int, like):
+    """(mask, its rows, states) as the library takes them."""
+    import torch
+    if mask is None:
+        if states is not None:
+            raise ValueError("states without a mask")
+        return None, 0, None
+    if states is None:
+        raise ValueError("a mask without states")
+    if mask.dim() != 2 or mask.shape[1] != mask_words(V):
+        raise ValueError("mask must be [rows, ceil(V/32)]")
+    return (_with(like, mask, "mask", _dev(mask, (torch.int32,), "mask")), mask.shape[0],
+            _per_row(states, torch.int32, B, "states", like))
+
+
+def _empty(shape, dtype, device, stream):
+    """A tensor that the call's own stream may use at once and, once it is released, reuse."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _hidden(x, name: str):
+    import torch
+    if x.dim() != 2:
+        raise ValueError(f"{name} must be a matrix")
+    if x.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"{name} must be float32 or bfloat16")
+    dtype = TRIE_DTYPE_BF16 if x.dtype is torch.bfloat16 else TRIE_DTYPE_F32
+    return (*_rows(x, (torch.float32, torch.bfloat16), name), dtype)
+
+
+def trie_head_quantize(x, stream=None):
+    """Hidden states x ([M, D] fp32 or bf16) as (e4m3 [M, D], scales [ceil(D/128), M rounded up to 4]),
+    a scale for each row and 128 columns: column m holds row m's scales."""
+    import torch
+    p, stride, dtype = _hidden(x, "x")
+    M, D = x.shape
+    q = _empty((M, D), torch.float8_e4m3fn, x.device, stream)
+    scales = _empty(((D + 127) // 128, (M + 3) // 4 * 4), torch.float32, x.device, stream)
+    _check(load_library().trie_head_quantize(p, dtype, stride, M, D, q.data_ptr(), scales.data_ptr(), scales.shape[1],
+                                             _stream_of(stream, x)))
+    return q, scales
+
+
+def trie_head_quantize_weight(w, stream=None):
+    """Weights w ([V, D] fp32 or bf16) as (e4m3 [V, D], scales [ceil(V/128), ceil(D/128)]), a scale for
+    each block of 128 x 128."""
+    import torch
+    p, stride, dtype = _hidden(w, "w")
+    V, D = w.shape
+    q = _empty((V, D), torch.float8_e4m3fn, w.device, stream)
+    scales = _empty(((V + 127) // 128, (D + 127) // 128), torch.float32, w.device, stream)
+    _check(load_library().trie_head_quantize_weight(p, dtype, stride, V, D, q.data_ptr(), scales.data_ptr(),
+                                                    _stream_of(stream, w)))
+    return q, scales
+
+
+def trie_head_logits(q, scales, w, w_scales, d_logits, mask=None, states=None, stream=None) -> None:
+    """d_logits ([M, V] fp32 or bf16) = x W^T of the quantized hidden states (q, scales) and weights
+    (w, w_scales), -inf where the row of the mask that states names does not allow the token."""
+    import torch
+    dtype = _logits_dtype(d_logits)
+    M, V = d_logits.shape
+    D = w.shape[1] if w.dim() == 2 else -1
+    if w.shape != (V, D) or q.shape != (M, D):
+        raise ValueError("q must be [M, D] and w [V, D] for logits [M, V]")
+    blocks = (D + 127) // 128
+    if scales.dim() != 2 or scales.shape[0] != blocks or scales.shape[1] < M or scales.shape[1] % 4:
+        raise ValueError("scales must be [ceil(D/128), M rounded up to a multiple of 4]")
+    if w_scales.shape != ((V + 127) // 128, blocks):
+        raise ValueError("w_scales must be [ceil(V/128), ceil(D/128)]")
+    p, stride = _rows(d_logits, (torch.float32, torch.bfloat16), "d_logits")
+    fp8, f32 = (torch.float8_e4m3fn,), (torch.float32,)
+    _check(load_library().trie_head_logits(
+        _with(d_logits, q, "q", _dev(q, fp8, "q")), _with(d_logits, scales, "scales", _dev(scales, f32, "scales")),
+        scales.shape[1], _with(d_logits, w, "w", _dev(w, fp8, "w")),
+        _with(d_logits, w_scales, "w_scales", _dev(w_scales, f32, "w_scales")), M, V, D, p, dtype, stride,
+        *_grammar(mask, states, M, V, d_logits), _stream_of(stream, d_logits)))
+
+
+def trie_penalize(d_logits, history=None, length=None, prompt=None, repetition=None, presence=None, frequency=None,
+                  bias=None, mask=None, states=None, stream=None) -> None:
+    """Penalties for the tokens of the history ([B, H] int32, the first length[b] of row b, of them prompt[b]
+    the prompt), biases ((offsets [B+1], tokens, values)) and the grammar mask, on d_logits ([B, V]) in place."""
+    import torch
+    dtype = _logits_dtype(d_logits)
+    B, V = d_logits.shape
+    p, stride = _rows(d_logits, (torch.float32, torch.bfloat16), "d_logits")
+    ph = h_stride = H = 0
+    if history is not None:
+        if history.dim() != 2 or history.shape[0] != B:
+            raise ValueError("history must be [B, H]")
+        if length is None:
+            raise ValueError("a history without its length")
+        H = history.shape[1]
+        ph, h_stride = _rows(history, (torch.int32,), "history")
+        _with(d_logits, history, "history", ph)
+    elif length is not None or prompt is not None:
+        raise ValueError("length / prompt without a history")
+    off = tok = val = None
+    if bias is not None:
+        off, tok, val = bias
+        if off.numel() != B + 1 or tok.numel() != val.numel():
+            raise ValueError("bias must be (offsets [B+1], tokens [n], values [n])")
+        off = _with(d_logits, off, "bias offsets", _dev(off, (torch.int32,), "bias offsets"))
+        tok = _with(d_logits, tok, "bias tokens", _dev(tok, (torch.int32,), "bias tokens"))
+        val = _with(d_logits, val, "bias values", _dev(val, (torch.float32,), "bias values"))
+        if not bias[1].numel():
+            off = None  # no entries
+    _check(load_library().trie_penalize(
+        p, dtype, stride, B, V, ph if H else None, h_stride, H, _per_row(length, torch.int32, B, "length", d_logits),
+        _per_row(prompt, torch.int32, B, "prompt", d_logits),
+        _per_row(repetition, torch.float32, B, "repetition", d_logits),
+        _per_row(presence, torch.float32, B, "presence", d_logits),
+        _per_row(frequency, torch.float32, B, "frequency", d_logits), off, tok, val,
+        *_grammar(mask, states, B, V, d_logits), _stream_of(stream, d_logits)))
+
+
+def trie_sample(d_logits, seeds, temperature=None, top_k=None, top_p=None, min_p=None, mask=None, states=None,
+                tokens=None, logprobs=None, workspace=None, stream=None):
+    """(tokens int32[B], logprobs fp32[B]) sampled from d_logits ([B, V]) by temperature, top-k, top-p, min-p
+    (tensors of B values, or None) and the grammar; seeds int64[B] make the draw. tokens and logprobs may be
+    given, and a workspace of trie_sample_workspace(B, V) bytes (else taken from torch's allocator)."""
+    import torch
+    lib = load_library()
+    dtype = _logits_dtype(d_logits)
+    B, V = d_logits.shape
+    p, stride = _rows(d_logits, (torch.float32, torch.bfloat16), "d_logits")
+    if seeds is None:
+        raise ValueError("seeds must be given")
+    dev = d_logits.device
+    tokens = _empty(B, torch.int32, dev, stream) if tokens is None else tokens
+    logprobs = _empty(B, torch.float32, dev, stream) if logprobs is None else logprobs
+    need = lib.trie_sample_workspace(B, V)
+    if workspace is None:
+        workspace = _empty(max(need, 0), torch.uint8, dev, stream)
+    elif workspace.numel() * workspace.element_size() < need:
+        raise ValueError(f"workspace must have at least {need} bytes")
+    _check(lib.trie_sample(
+        p, dtype, stride, B, V, _per_row(seeds, torch.int64, B, "seeds", d_logits),
+        _per_row(temperature, torch.float32, B, "temperature", d_logits),
+        _per_row(top_k, torch.int32, B, "top_k", d_logits), _per_row(top_p, torch.float32, B, "top_p", d_logits),
+        _per_row(min_p, torch.float32, B, "min_p", d_logits), *_grammar(mask, states, B, V, d_logits),
+        _with(d_logits, workspace, "workspace", _dev(workspace, (workspace.dtype,), "workspace")),
+        _per_row(tokens, torch.int32, B, "tokens", d_logits),
+        _per_row(logprobs, torch.float32, B, "logprobs", d_logits), _stream_of(stream, d_logits)))
+    return tokens, logprobs
+
+
+def trie_sample_workspace(B: int, V: int) -> int:
+    """Bytes of trie_sample's workspace."""
+    n = load_library().trie_sample_workspace(B, V)
+    if n < 0:
+        raise ValueError("B or V out of range")
+    return n
 
 
 # ------------------------------------------------------------ fixed formats
