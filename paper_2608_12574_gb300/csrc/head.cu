@@ -10,7 +10,7 @@
 //
 //  k_head_quantize         a warp per row and block of 128 columns.
 //  k_head_quantize_weight  a CTA per block of 128 x 128.
-//  k_head_logits           64 tokens x 64 rows a CTA.
+//  k_head_logits           the product on the tensor cores.
 #include <math.h>
 #include <stdint.h>
 #include <stdio.h>
@@ -18,6 +18,7 @@
 #include <cuda_fp8.h>
 #include <cuda_runtime.h>
 
+#include "blackwell.cuh"
 #include "logits.cuh"
 
 namespace tmk {
@@ -27,13 +28,9 @@ namespace {
 constexpr int kBlock = 128;  // columns (and weight rows) that share a scale
 constexpr float kPerMax = 1.0f / 448.0f;  // 448: the largest e4m3 number
 constexpr int kQuantThreads = 256;
-constexpr int kTile = 64;
 
 __device__ __forceinline__ uint8_t to_e4m3(float x) {
     return uint8_t(__nv_cvt_float_to_fp8(x, __NV_SATFINITE, __NV_E4M3));
-}
-__device__ __forceinline__ float from_e4m3(uint8_t x) {
-    return __half2float(__half(__nv_cvt_fp8_to_halfraw(x, __NV_E4M3)));
 }
 
 // NaN does not show in the maximum, but a NaN element becomes a NaN in e4m3 and
@@ -99,63 +96,243 @@ __global__ void __launch_bounds__(kQuantThreads) k_head_quantize_weight(const T 
     if (threadIdx.x == 0) scales[int64_t(vb) * blocks + kb] = s;
 }
 
+// ---- the product
+//
+// The weights are the MMA's rows (128 tokens a tile) and the batch its columns:
+// a full tile whatever the batch, and a token's weight scale is the whole
+// tile's. A CTA computes one tile of 128 tokens by up to 256 rows of the batch:
+// one thread streams blocks of 128 columns of K of both operands (and the rows'
+// scales of that block) into a ring of stages by TMA, one issues the four MMAs
+// of a block into one of several accumulators in tensor memory, and the
+// epilogue warps read each block's sums out and add them, scaled, to sums in
+// registers: a thread holds one token and up to 64 rows.
 struct HeadArgs {
-    const uint8_t *q;      // [M, D]
+    CUtensorMap map_w, map_q;
     const float *s;        // [blocks][pitch]
     int64_t pitch;
-    const uint8_t *w;      // [V, D]
     const float *ws;       // [ceil(V / 128)][blocks]
-    int32_t M, V, D, blocks;
+    int32_t M, V, blocks;
+    int32_t m_tiles, n;    // the batch in m_tiles tiles of n rows (a multiple of 16)
     void *logits;
     int64_t stride;
     Grammar g;
 };
 
+template <int NT>
+struct HeadShape {
+    static constexpr int kColumns = NT < 64 ? NT : 64;        // columns of an epilogue warp
+    static constexpr int kEpilogue = 4 * (NT / kColumns);     // warps
+    static constexpr int kThreads = 64 + 32 * kEpilogue;
+    static constexpr int kAccumulators = NT <= 64 ? 4 : 2;
+    static constexpr int kTmem = NT * kAccumulators < 32 ? 32 : NT * kAccumulators;
+    static constexpr int kCtas = NT <= 128 ? 2 : 1;           // of an SM
+    static constexpr int kStageBytes = (kBlock + NT) * kBlock + 1024;  // weights, rows, scales
+    static constexpr int kStages = (kCtas == 2 ? 112 : 224) * 1024 / kStageBytes;
+    static constexpr int kSmem = kStages * kStageBytes + 1024;         // and room to align
+};
+
+// Writes -inf to rows [m0, m1) of tokens [v0, v1) (at most 128), by all threads.
 template <typename T>
-__global__ void __launch_bounds__(256) k_head_logits(HeadArgs a) {
+__device__ void fill_tile(const HeadArgs &a, int32_t m0, int32_t m1, int32_t v0, int32_t v1) {
+    const int lane = threadIdx.x & 31;
+    const T none = from_f32<T>(-INFINITY);
+    for (int32_t m = m0 + int32_t(threadIdx.x >> 5); m < m1; m += int32_t(blockDim.x >> 5)) {
+        T *out = static_cast<T *>(a.logits) + m * a.stride + v0;
+        if (v1 - v0 == kBlock && (reinterpret_cast<uintptr_t>(out) & (4 * sizeof(T) - 1)) == 0) {
+            if (sizeof(T) == 2) reinterpret_cast<uint2 *>(out)[lane] = make_uint2(0xFF80FF80u, 0xFF80FF80u);
+            else reinterpret_cast<uint4 *>(out)[lane] = make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u);
+        } else {
+            for (int32_t i = lane; i < v1 - v0; i += 32) out[i] = none;
+        }
+    }
+}
+
+template <typename T, int NT>
+__global__ void __launch_bounds__(HeadShape<NT>::kThreads, HeadShape<NT>::kCtas) k_head_logits(const __grid_constant__ HeadArgs a) {
+    using S = HeadShape<NT>;
+    extern __shared__ unsigned char dynamic_smem[];
+    __shared__ uint64_t bars[2 * S::kStages + 2 * S::kAccumulators];
+    __shared__ uint32_t tmem_base;
+    __shared__ int gave_up;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int32_t vt = int32_t(blockIdx.x / unsigned(a.m_tiles)), v0 = vt * kBlock;
+    const int32_t m0 = int32_t(blockIdx.x % unsigned(a.m_tiles)) * a.n, m1 = min(a.M, m0 + a.n);
+    const uint32_t full = smem_addr(bars), empty = full + 8 * S::kStages;
+    const uint32_t ready = empty + 8 * S::kStages, drained = ready + 8 * S::kAccumulators;
+    const uint32_t stages = (smem_addr(dynamic_smem) + 1023u) & ~1023u;
+    if (threadIdx.x == 0) {
+        gave_up = 0;
+        for (int i = 0; i < S::kStages; i++) {
+            bar_init(full + 8 * i, 1);
+            bar_init(empty + 8 * i, 1 + S::kEpilogue);  // the MMAs have read it, and each epilogue warp its scales
+        }
+        for (int i = 0; i < S::kAccumulators; i++) {
+            bar_init(ready + 8 * i, 1);
+            bar_init(drained + 8 * i, S::kEpilogue);
+        }
+        bar_init_fence();
+        tma_prefetch_map(&a.map_w);
+        tma_prefetch_map(&a.map_q);
+    }
     pdl_launch_dependents();
     pdl_wait();
-    __shared__ float ws[kTile][33], xs[kTile][33];
-    const int32_t v0 = blockIdx.x * kTile, m0 = blockIdx.y * kTile;
-    const int tv = threadIdx.x & 15, tm = threadIdx.x >> 4;
-    float acc[4][4] = {};
-    for (int32_t kb = 0; kb < a.blocks; kb++) {
-        float part[4][4] = {};
-        for (int32_t k0 = kb * kBlock; k0 < min(a.D, (kb + 1) * kBlock); k0 += 32) {
-            __syncthreads();
-            for (int i = threadIdx.x; i < kTile * 32; i += 256) {
-                const int r = i >> 5;
-                const int32_t k = k0 + (i & 31);
-                ws[r][i & 31] = v0 + r < a.V && k < a.D ? from_e4m3(a.w[int64_t(v0 + r) * a.D + k]) : 0.0f;
-                xs[r][i & 31] = m0 + r < a.M && k < a.D ? from_e4m3(a.q[int64_t(m0 + r) * a.D + k]) : 0.0f;
+    if (a.g.mask) {
+        // a tile that no row of the batch allows a token of needs no weights
+        bool any = false;
+        const int32_t w0 = v0 >> 5, words = min(4, int32_t(a.g.W) - w0);
+        for (int32_t m = m0 + int32_t(threadIdx.x); m < m1 && !any; m += int32_t(blockDim.x)) {
+            const GrammarRow row = grammar_row(a.g, m);
+            for (int32_t i = 0; i < words; i++) any |= row.word(w0 + i) != 0u;
+        }
+        if (!__syncthreads_or(any)) {
+            fill_tile<T>(a, m0, m1, v0, min(a.V, v0 + kBlock));
+            return;
+        }
+    }
+    if (warp == 1) tmem_alloc(smem_addr(&tmem_base), S::kTmem);
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+    const uint32_t tmem = *static_cast<volatile uint32_t *>(&tmem_base);
+
+    if (warp == 0) {
+        if (lane == 0) {
+            const uint32_t scale_bytes = uint32_t(min(int64_t(a.n), a.pitch - m0)) * 4;
+            int32_t kb = 0;
+            for (; kb < a.blocks; kb++) {
+                const int stage = kb % S::kStages;
+                if (kb >= S::kStages && !bar_wait(empty + 8 * stage, (kb / S::kStages - 1) & 1, &gave_up)) break;
+                const uint32_t at = stages + stage * S::kStageBytes, bar = full + 8 * stage;
+                bar_expect(bar, uint32_t(kBlock + a.n) * kBlock + scale_bytes);
+                tma_load_2d(at, &a.map_w, kb * kBlock, v0, bar);
+                tma_load_2d(at + kBlock * kBlock, &a.map_q, kb * kBlock, m0, bar);
+                bulk_load(at + (kBlock + NT) * kBlock, a.s + kb * a.pitch + m0, scale_bytes, bar);
             }
-            __syncthreads();
-#pragma unroll 8
-            for (int k = 0; k < 32; k++)
-#pragma unroll
-                for (int i = 0; i < 4; i++)
-#pragma unroll
-                    for (int j = 0; j < 4; j++) part[i][j] += xs[tm + 16 * i][k] * ws[tv + 16 * j][k];
+            if (gave_up) {  // copies still write to shared memory: wait for them
+                int none = 0;
+                for (int32_t i = max(0, kb - S::kStages); i < kb; i++) bar_wait(full + 8 * (i % S::kStages), (i / S::kStages) & 1, &none);
+            }
         }
-        const float sw = __ldg(a.ws + int64_t(v0 / kBlock) * a.blocks + kb);
+    } else if (warp == 1) {
+        if (lane == 0) {
+            const uint32_t idesc = mma_idesc_e4m3(kBlock, uint32_t(a.n));
+            for (int32_t kb = 0; kb < a.blocks; kb++) {
+                const int stage = kb % S::kStages, acc = kb % S::kAccumulators;
+                if (kb >= S::kAccumulators && !bar_wait(drained + 8 * acc, (kb / S::kAccumulators - 1) & 1, &gave_up)) break;
+                if (!bar_wait(full + 8 * stage, (kb / S::kStages) & 1, &gave_up)) break;
+                tcgen05_fence_after();
+                const uint32_t at = stages + stage * S::kStageBytes;
+                const uint64_t da = mma_desc(at), db = mma_desc(at + kBlock * kBlock);
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const int32_t m = m0 + tm + 16 * i;
-            const float f = m < a.M ? __ldg(a.s + kb * a.pitch + m) * sw : 0.0f;
+                for (int k = 0; k < kBlock / 32; k++) mma_e4m3(tmem + acc * NT, da + 2 * k, db + 2 * k, idesc, k > 0);
+                mma_commit(empty + 8 * stage);
+                mma_commit(ready + 8 * acc);
+            }
+        }
+    } else {
+        const int quarter = warp & 3, column = (warp - 2) / 4 * S::kColumns;
+        const uint32_t lanes = uint32_t(quarter * 32) << 16;
+        uint64_t sum[S::kColumns / 2];
 #pragma unroll
-            for (int j = 0; j < 4; j++) acc[i][j] += part[i][j] * f;
+        for (int i = 0; i < S::kColumns / 2; i++) sum[i] = 0ull;
+        bool ok = true;
+        const float *ws = a.ws + int64_t(vt) * a.blocks;
+        for (int32_t kb = 0; kb < a.blocks && ok; kb++) {
+            const int stage = kb % S::kStages, acc = kb % S::kAccumulators;
+            const float w = __ldg(ws + kb);
+            const uint64_t w2 = pack2(w, w);
+            ok = bar_wait(full + 8 * stage, (kb / S::kStages) & 1, &gave_up) &&
+                 bar_wait(ready + 8 * acc, (kb / S::kAccumulators) & 1, &gave_up);
+            ok = __all_sync(~0u, ok);
+            if (!ok) break;
+            tcgen05_fence_after();
+            const uint32_t scales = stages + stage * S::kStageBytes + (kBlock + NT) * kBlock + column * 4;
+#pragma unroll
+            for (int c = 0; c < S::kColumns; c += 16) {
+                uint32_t r[16];
+                tmem_load16(tmem + lanes + acc * NT + column + c, r);
+                tmem_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    uint64_t s0, s1;
+                    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(s0), "=l"(s1) : "r"(scales + (c + i) * 4));
+                    sum[(c + i) / 2] = fma2(pack2u(r[i], r[i + 1]), mul2(s0, w2), sum[(c + i) / 2]);
+                    sum[(c + i) / 2 + 1] = fma2(pack2u(r[i + 2], r[i + 3]), mul2(s1, w2), sum[(c + i) / 2 + 1]);
+                }
+            }
+            tcgen05_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                bar_arrive(drained + 8 * acc);
+                bar_arrive(empty + 8 * stage);
+            }
+        }
+        // a tile that gave up waiting has no result: NaN
+        const int32_t v = v0 + quarter * 32 + lane;
+        uint32_t allow[(S::kColumns + 31) / 32];
+#pragma unroll
+        for (int i = 0; i < (S::kColumns + 31) / 32; i++) {
+            const int32_t m = m0 + column + i * 32 + lane;
+            allow[i] = a.g.mask && m < m1 && (v0 >> 5) + quarter < a.g.W ? grammar_row(a.g, m).word((v0 >> 5) + quarter) : ~0u;
+        }
+        T *out = static_cast<T *>(a.logits) + v;
+#pragma unroll
+        for (int i = 0; i < S::kColumns; i++) {
+            const uint32_t word = __shfl_sync(~0u, allow[i / 32], i & 31);
+            const int32_t m = m0 + column + i;
+            float lo, hi;
+            unpack2(sum[i / 2], lo, hi);
+            float x = i & 1 ? hi : lo;
+            if (!ok) x = __int_as_float(0x7FFFFFFF);
+            if (!((word >> lane) & 1u)) x = -INFINITY;
+            if (m < m1 && v < a.V) out[m * a.stride] = from_f32<T>(x);
         }
     }
-    for (int i = 0; i < 4; i++) {
-        const int32_t m = m0 + tm + 16 * i;
-        if (m >= a.M) continue;
-        const GrammarRow row = grammar_row(a.g, m);
-        for (int j = 0; j < 4; j++) {
-            const int32_t v = v0 + tv + 16 * j;
-            if (v < a.V)
-                static_cast<T *>(a.logits)[m * a.stride + v] = from_f32<T>(row.allows(v) ? acc[i][j] : -INFINITY);
+    __syncwarp();
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+    if (warp == 1) tmem_free(tmem, S::kTmem);
+}
+
+// [rows][D] bytes in boxes of box_rows x 128, 128-byte swizzle, zeros outside.
+bool make_map(CUtensorMap *map, const void *base, int64_t rows, int32_t D, int32_t box_rows) {
+    using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static const Encode encode = [] {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult got;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &got) != cudaSuccess ||
+            got != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            f = nullptr;
         }
-    }
+        return reinterpret_cast<Encode>(f);
+    }();
+    if (!encode) return false;
+    const cuuint64_t dims[2] = {cuuint64_t(D), cuuint64_t(rows)}, strides[1] = {cuuint64_t(D)};
+    const cuuint32_t box[2] = {cuuint32_t(kBlock), cuuint32_t(box_rows)}, steps[2] = {1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, steps,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, int NT>
+cudaError_t launch_head(const HeadArgs &a, int64_t grid, cudaStream_t st) {
+    using S = HeadShape<NT>;
+    const cudaError_t e = cudaFuncSetAttribute(k_head_logits<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+    if (e != cudaSuccess) return e;
+    return launch_pdl_smem(k_head_logits<T, NT>, grid, S::kThreads, S::kSmem, st, a);
+}
+
+template <typename T>
+cudaError_t launch_head_type(const HeadArgs &a, int64_t grid, cudaStream_t st) {
+    if (a.n <= 16) return launch_head<T, 16>(a, grid, st);
+    if (a.n <= 32) return launch_head<T, 32>(a, grid, st);
+    if (a.n <= 64) return launch_head<T, 64>(a, grid, st);
+    if (a.n <= 128) return launch_head<T, 128>(a, grid, st);
+    return launch_head<T, 256>(a, grid, st);
 }
 
 const char *check_quantize(const void *x, int dtype, int64_t stride, int32_t rows, int32_t D, const void *q,
@@ -225,22 +402,24 @@ extern "C" int trie_head_logits(const uint8_t *d_q, const float *d_scales, int64
     if (!*bad && M > (1 << 20)) bad = "M must be <= 2^20";
     if (*bad) return set_error(TRIE_EINVAL, bad);
     if (M == 0) return TRIE_OK;
-    HeadArgs a;
-    a.q = d_q;
+    HeadArgs a = {};
     a.s = d_scales;
     a.pitch = pitch;
-    a.w = d_w;
     a.ws = d_w_scales;
     a.M = M;
     a.V = V;
-    a.D = D;
     a.blocks = (D + kBlock - 1) / kBlock;
+    a.m_tiles = (M + 255) / 256;
+    a.n = ((M + a.m_tiles - 1) / a.m_tiles + 15) / 16 * 16;
     a.logits = d_logits;
     a.stride = stride;
     a.g = make_grammar(d_mask, mask_rows, d_states, V);
-    const dim3 grid((unsigned(V) + kTile - 1) / kTile, (unsigned(M) + kTile - 1) / kTile);
-    const cudaError_t e = dtype == TRIE_DTYPE_F32 ? launch_pdl_grid(k_head_logits<float>, grid, 256, 0, stream, a)
-                                                  : launch_pdl_grid(k_head_logits<__nv_bfloat16>, grid, 256, 0, stream, a);
+    if (!make_map(&a.map_w, d_w, V, D, kBlock) || !make_map(&a.map_q, d_q, M, D, a.n))
+        return set_error(TRIE_ECUDA, "cuTensorMapEncodeTiled failed");
+    const int64_t grid = (int64_t(V) + kBlock - 1) / kBlock * a.m_tiles;
+    if (grid > 0x7FFFFFFF) return set_error(TRIE_EINVAL, "M x V is too large");
+    const cudaError_t e = dtype == TRIE_DTYPE_F32 ? launch_head_type<float>(a, grid, stream)
+                                                  : launch_head_type<__nv_bfloat16>(a, grid, stream);
     if (e != cudaSuccess) return fail_launch(e, "head launch");
     return TRIE_OK;
 }
