@@ -574,7 +574,7 @@ int64_t trie_sample_workspace(int32_t B, int32_t V);
  *   d_top_p        device float[B]; not below 1: off
  *   d_min_p        device float[B]; not above 0: off
  *                  each of these four may be NULL (1, off, off, off)
- *   d_workspace    device, trie_sample_workspace(B, V) bytes, 8-byte aligned
+ *   d_workspace    device, trie_sample_workspace(B, V) bytes, 16-byte aligned
  *   d_tokens       device int32[B]; -1 where the row has nothing to choose from
  *                  (trie_advance takes it to DEAD)
  *   d_logprobs     device float[B] or NULL: the token's log-probability among all

@@ -15,16 +15,21 @@
 // how a running sum over the vocabulary is rounded.
 //
 //  k_sample_groups  largest logit and sum of exp((x - largest) / T) of every
-//                   group: the one pass over the logits.
+//                   group: the one pass over the logits. Rows whose top-k or
+//                   top-p set may be large also get a histogram of their logits
+//                   (kBins bins of 1/32, counts and weights in whole numbers so
+//                   that the order of the atomics does not matter), each CTA's
+//                   share stored by itself.
 //  k_sample_pick    one CTA per row: M and the total weight from the groups'
-//                   values; then only groups that can matter are read again.
-//                   The k-th largest group maximum bounds the k-th largest
-//                   logit from below, so the first k (or a first guess at the
-//                   top-p set) come from a few groups into a list in shared
-//                   memory, which is sorted. A row whose kept set does not fit
-//                   the list finds the last kept logit by a radix select over
-//                   the groups, with weights summed in 40-bit fixed point (the
-//                   order of atomic additions then does not matter).
+//                   values, then only groups that can matter are read again.
+//                   top_k <= kSmallK: the k-th largest group maximum bounds the
+//                   k-th largest logit from below, so the first k are in a few
+//                   groups. Otherwise the histogram tells the bin in which the
+//                   kept set ends; one pass over the groups that reach that bin
+//                   adds up what lies above it, exactly, and collects the bin.
+//                   Either way a short list in shared memory is sorted and cut.
+//                   A list that does not fit (many equal logits) leaves the row
+//                   to a radix select over all groups.
 #include <math.h>
 #include <stdint.h>
 #include <stdio.h>
@@ -41,9 +46,11 @@ constexpr int kGroup = 256;
 constexpr int kGroupThreads = 256;  // k_sample_groups
 constexpr int kThreads = 512;       // k_sample_pick
 constexpr int kWarps = kThreads / 32;
-constexpr int kList = 2048;
-constexpr int kListK = 1024;        // largest top-k that goes through the list
-constexpr int kGuess = 64;          // groups of the first guess at a top-p set
+constexpr int kList = 8192;
+constexpr int kSmallK = 64;         // largest top-k that goes without a histogram
+constexpr int kBins = 2048;
+constexpr float kBinsPerUnit = 32.0f;
+constexpr int kChunk = 128;         // most groups of a CTA of k_sample_groups
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr uint32_t kKeyNone = 0x007FFFFFu;  // order_key(-inf)
 constexpr double kFixed = 1099511627776.0;  // 2^40
@@ -58,7 +65,9 @@ struct SampleArgs {
     const int32_t *top_k;
     const float *top_p, *min_p;
     Grammar g;
-    float2 *stats;            // [B][G]
+    float2 *stats;            // [B][G] largest logit, sum of weights (relative to it)
+    uint32_t *hist;           // [B][parts][2][kBins] counts, weights
+    int32_t chunk, parts;     // groups of a CTA, CTAs of a row
     int32_t *tokens;
     float *logprobs;
 };
@@ -85,6 +94,26 @@ __device__ __forceinline__ Way row_way(const SampleArgs &a, int32_t b) {
     if (!(w.min_p > 0.0f)) w.min_p = 0.0f;
     return w;
 }
+
+// Rows that get a histogram: the k-th largest of G group maxima says little
+// where k is large or there are fewer groups.
+__device__ __forceinline__ bool wants_hist(const Way &w, int32_t G) {
+    return !w.greedy && (w.k > min(kSmallK, G) || (w.p < 1.0f && w.k == 0));
+}
+
+// Bins of logits, the largest first: non-increasing in x, so a token of an
+// earlier bin is above every token of a later one. The bins lie around the
+// largest logit of the row's first group, which the row's largest is not below.
+struct Bins {
+    float top;
+    __device__ __forceinline__ explicit Bins(float first) {
+        top = (fabsf(first) <= 3.0e38f ? first : 0.0f) + float(kBins / 2) / kBinsPerUnit;
+    }
+    __device__ __forceinline__ float place(float x) const { return (top - x) * kBinsPerUnit; }
+    __device__ __forceinline__ int32_t bin(float x) const {
+        return int32_t(fminf(fmaxf(place(x), 0.0f), float(kBins - 1)));
+    }
+};
 
 // Unsigned order of floats: a > b as floats iff order_key(a) > order_key(b).
 __device__ __forceinline__ uint32_t order_key(float x) {
@@ -163,13 +192,23 @@ __device__ __forceinline__ float warp_sum(float x) {
 }
 
 struct Shared {
-    unsigned long long list[kList];     // order_key << 32 | ~id
-    float before[kList];                // weights of the list before each entry; then groups' weights
-    uint32_t count[256];
-    unsigned long long mass[256];
+    unsigned long long list[kList];     // order_key << 32 | ~id, or id << 32 | order_key
+    union {
+        float before[kList];            // weights of the list before each entry
+        struct {
+            uint32_t count[kBins];
+            float mass[kBins];
+        } hist;
+        struct {
+            uint32_t count[256];
+            unsigned long long mass[256];
+        } radix;
+    };
     Best best[kWarps];
     float f[kWarps];
+    int32_t i[kWarps];
     int32_t n;
+    int32_t bin[2];
     uint32_t key;
     int32_t ties;
     unsigned long long above, total;
@@ -203,82 +242,247 @@ __device__ float block_sum(Shared &s, float x) {
     return x;
 }
 
+__device__ int32_t block_sum(Shared &s, int32_t x) {
+    x = __reduce_add_sync(~0u, x);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) s.i[threadIdx.x >> 5] = x;
+    __syncthreads();
+    x = s.i[0];
+    for (int i = 1; i < kWarps; i++) x += s.i[i];
+    return x;
+}
+
+// A group's logits, eight a lane: token id(i) of the group in x[i], -inf where
+// not allowed or past the end. Rows on 16-byte boundaries without a grammar are
+// read 16 bytes at a time.
+template <typename T>
+struct GroupLoad {
+    const T *x;
+    GrammarRow allow;
+    int32_t V;
+    bool wide;
+    __device__ __forceinline__ explicit GroupLoad(const Row<T> &row)
+        : x(row.x), allow(row.allow), V(row.V),
+          wide(row.allow.kind == kAllowAll && (reinterpret_cast<uintptr_t>(row.x) & 15) == 0) {}
+    __device__ __forceinline__ int32_t id(int i, int lane) const {
+        if (!wide) return i * 32 + lane;
+        return sizeof(T) == 2 ? lane * 8 + i : (i >> 2) * 128 + lane * 4 + (i & 3);
+    }
+    __device__ __forceinline__ void operator()(int32_t j, int lane, float (&f)[8]) const {
+        const int64_t v0 = int64_t(j) * kGroup;
+        if (wide && v0 + kGroup <= V) {
+            const uint4 *p = reinterpret_cast<const uint4 *>(x + v0) + lane;
+            if (sizeof(T) == 2) {
+                const uint4 q = __ldg(p);
+                const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                for (int i = 0; i < 8; i++) f[i] = __uint_as_float(i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
+            } else {
+                const uint4 q = __ldg(p), r = __ldg(p + 32);
+                const uint32_t w[8] = {q.x, q.y, q.z, q.w, r.x, r.y, r.z, r.w};
+#pragma unroll
+                for (int i = 0; i < 8; i++) f[i] = __uint_as_float(w[i]);
+            }
+        } else if (allow.kind == kAllowAll) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const int64_t v = v0 + id(i, lane);
+                f[i] = v < V ? to_f32(x[v]) : -INFINITY;
+            }
+        } else {
+            const int32_t left = (V - int32_t(v0) + 31) >> 5;  // words of the mask from here on
+            uint32_t words = lane < 8 && lane < left ? allow.word(int32_t(v0 >> 5) + lane) : 0u;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const uint32_t word = __shfl_sync(~0u, words, i);
+                f[i] = -INFINITY;
+                if (word) {  // the whole warp's
+                    const int64_t v = v0 + i * 32 + lane;
+                    if (((word >> lane) & 1u) && v < V) f[i] = to_f32(x[v]);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) f[i] = fmaxf(f[i], -INFINITY);  // NaN counts as -inf
+    }
+};
+
 // ------------------------------------------------------------ the one pass
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 
 template <typename T>
 __global__ void __launch_bounds__(kGroupThreads) k_sample_groups(SampleArgs a) {
+    __shared__ uint32_t hist[2][kBins];
     pdl_launch_dependents();
     pdl_wait();
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int32_t b = blockIdx.y;
     const Way way = row_way(a, b);
-    const Row<T> row = row_at<T>(a, b);
+    const GroupLoad<T> load(row_at<T>(a, b));
     const float c = __fdiv_rn(kLog2e, way.T);
-    for (int32_t j = blockIdx.x * (kGroupThreads / 32) + (threadIdx.x >> 5); j < a.G;
-         j += gridDim.x * (kGroupThreads / 32)) {
-        float x[kGroup / 32], m = -INFINITY;
+    const bool binned = wants_hist(way, a.G);
+    Bins bins(0.0f);
+    if (binned) {
+        for (int i = threadIdx.x; i < 2 * kBins; i += kGroupThreads) hist[0][i] = 0u;
+        float x[8], m = -INFINITY;
+        load(0, lane, x);
 #pragma unroll
-        for (int i = 0; i < kGroup / 32; i++) {
-            const int64_t v = int64_t(j) * kGroup + i * 32 + lane;
-            x[i] = v < a.V ? row(int32_t(v)) : -INFINITY;
-            m = fmaxf(m, x[i]);
-        }
+        for (int i = 0; i < 8; i++) m = fmaxf(m, x[i]);
+        bins = Bins(warp_max(m));
+        __syncthreads();
+    }
+    const int32_t j0 = int32_t(blockIdx.x) * a.chunk, j1 = min(a.G, j0 + a.chunk);
+    for (int32_t j = j0 + warp; j < j1; j += kGroupThreads / 32) {
+        float x[8], m = -INFINITY;
+        load(j, lane, x);
+#pragma unroll
+        for (int i = 0; i < 8; i++) m = fmaxf(m, x[i]);
         m = warp_max(m);
         float sum = 0.0f;
         if (m > -INFINITY) {
 #pragma unroll
-            for (int i = 0; i < kGroup / 32; i++) sum += x[i] == m ? 1.0f : exp2f((x[i] - m) * c);
+            for (int i = 0; i < 8; i++) sum += x[i] == m ? 1.0f : exp2_fast((x[i] - m) * c);
             sum = warp_sum(sum);
+            if (binned) {
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    if (x[i] == -INFINITY) continue;
+                    const float place = bins.place(x[i]);
+                    const int32_t bin = bins.bin(x[i]);
+                    atomicAdd(&hist[0][bin], 1u);
+                    // the weight relative to the bin's upper end: at most 2^16, 2^15 tokens a CTA
+                    const float w = exp2_fast((float(bin) - place) * (c / kBinsPerUnit));
+                    atomicAdd(&hist[1][bin], uint32_t(fminf(w, 1.0f) * 65535.0f + 0.5f));
+                }
+            }
         }
         if (lane == 0) a.stats[int64_t(b) * a.G + j] = make_float2(m, sum);
+    }
+    if (binned) {
+        __syncthreads();
+        uint4 *to = reinterpret_cast<uint4 *>(a.hist + (int64_t(b) * a.parts + blockIdx.x) * 2 * kBins);
+        for (int i = threadIdx.x; i < 2 * kBins / 4; i += kGroupThreads) to[i] = reinterpret_cast<uint4 *>(hist[0])[i];
     }
 }
 
 // ------------------------------------------------------------ one row's draw
 
-// The m-th largest group maximum as a key (kKeyNone when there are fewer).
-__device__ uint32_t nth_group(const float2 *stats, int32_t G, int32_t m) {
-    uint32_t key = 0u;
-    for (int bit = 31; bit >= 0; bit--) {
-        const uint32_t tryit = key | (1u << bit);
-        int32_t n = 0;
-        for (int32_t j0 = 0; j0 < G; j0 += kThreads) {
-            const int32_t j = j0 + int32_t(threadIdx.x);
-            n += __syncthreads_count(j < G && order_key(stats[j].x) >= tryit);
-        }
-        if (n >= m) key = tryit;
+// A lower bound of the m-th largest group maximum (m >= 1), and so of the m-th
+// largest logit, as a key; kKeyNone when fewer groups have a token. `low`: the
+// smallest maximum of those that have.
+__device__ uint32_t nth_group(Shared &s, const float2 *stats, int32_t G, int32_t m, float M, float low) {
+    constexpr int kPer = kBins / kThreads;
+    if (!(M <= 3.0e38f && low >= -3.0e38f) || low == M) return order_key(low);
+    const float per = float(kBins - 1) / (M - low);
+    __syncthreads();
+    for (int i = threadIdx.x; i < kBins; i += kThreads) s.hist.count[i] = 0u;
+    __syncthreads();
+    for (int32_t j = threadIdx.x; j < G; j += kThreads) {
+        const float x = stats[j].x;
+        if (x > -INFINITY) atomicAdd(&s.hist.count[min(kBins - 1, int32_t((M - x) * per))], 1u);
     }
-    return key > kKeyNone ? key : kKeyNone;
+    __syncthreads();
+    int32_t mine = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; i++) mine += int32_t(s.hist.count[threadIdx.x * kPer + i]);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int32_t upto = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int32_t y = __shfl_up_sync(~0u, upto, d);
+        if (lane >= d) upto += y;
+    }
+    if (lane == 31) s.i[warp] = upto;
+    if (threadIdx.x == 0) s.bin[0] = kBins;
+    __syncthreads();
+    for (int i = 0; i < warp; i++) upto += s.i[i];
+    if (upto >= m && upto - mine < m) {
+        int32_t n = upto - mine, bin = int32_t(threadIdx.x) * kPer;
+        while ((n += int32_t(s.hist.count[bin])) < m) bin++;
+        s.bin[0] = bin;
+    }
+    __syncthreads();
+    const int32_t bin = s.bin[0];
+    if (bin >= kBins) return kKeyNone;
+    // every logit of the bin or an earlier one is above this (a unit of rounding further down)
+    const float edge = M - float(bin + 1) / per;
+    return order_key(fmaxf(low, edge - 1e-6f * (fabsf(M) + fabsf(low))));
+}
+
+// Appends the tokens of group j whose bit of `in` is set to s.list (x: the
+// lane's eight logits); s.n counts on past kList.
+template <typename T>
+__device__ __forceinline__ void append(Shared &s, const GroupLoad<T> &load, int32_t j, const float (&x)[8], uint32_t in,
+                                       int lane) {
+    if (!__any_sync(~0u, in)) return;
+    const int32_t mine = __popc(in);
+    int32_t upto = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int32_t y = __shfl_up_sync(~0u, upto, d);
+        if (lane >= d) upto += y;
+    }
+    int32_t at = 0;
+    if (lane == 31) at = atomicAdd(&s.n, upto);
+    at = __shfl_sync(~0u, at, 31) + upto - mine;
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+        if ((in >> i) & 1u) {
+            if (at < kList)
+                s.list[at] = (uint64_t(order_key(x[i] + 0.0f)) << 32) | uint32_t(~uint32_t(j * kGroup + load.id(i, lane)));
+            at++;
+        }
 }
 
 // Collects every allowed token with order_key >= key into s.list; returns how
 // many there are (more than kList: only that many were stored).
 template <typename T>
-__device__ int32_t collect(Shared &s, const Row<T> &row, const float2 *stats, int32_t G, uint32_t key) {
+__device__ int32_t collect(Shared &s, const GroupLoad<T> &load, const float2 *stats, int32_t G, uint32_t key) {
     const int lane = threadIdx.x & 31;
     __syncthreads();
     if (threadIdx.x == 0) s.n = 0;
     __syncthreads();
-    for (int32_t j = threadIdx.x >> 5; j < G; j += kWarps) {
-        if (order_key(stats[j].x) < key) continue;
-        for (int i = 0; i < kGroup / 32; i++) {
-            const int64_t v = int64_t(j) * kGroup + i * 32 + lane;
-            const uint32_t k = v < row.V ? order_key(row(int32_t(v))) : 0u;
-            const bool in = k >= key && k > kKeyNone;
-            const uint32_t m = __ballot_sync(~0u, in);
-            if (!m) continue;
-            int32_t at = 0;
-            if (lane == 0) at = atomicAdd(&s.n, __popc(m));
-            at = __shfl_sync(~0u, at, 0) + __popc(m & ((1u << lane) - 1u));
-            if (in && at < kList) s.list[at] = (uint64_t(k) << 32) | uint32_t(~uint32_t(v));
+    // a warp looks at 32 groups' maxima at a time
+    for (int32_t j0 = int32_t(threadIdx.x >> 5); j0 * 32 < G; j0 += kWarps) {
+        const int32_t mine = j0 * 32 + lane;
+        uint32_t todo = __ballot_sync(~0u, mine < G && order_key(stats[mine].x) >= key);
+        while (todo) {
+            const int32_t j = j0 * 32 + __ffs(todo) - 1;
+            todo &= todo - 1;
+            float x[8];
+            load(j, lane, x);
+            uint32_t in = 0;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const uint32_t k = order_key(x[i] + 0.0f);
+                in |= uint32_t(k >= key && k > kKeyNone) << i;
+            }
+            append(s, load, j, x, in, lane);
         }
     }
     __syncthreads();
     return s.n;
 }
 
-// Sorts s.list[0, n) in descending order (a bitonic network over the next power of two).
+// Sorts s.list[0, n) in descending order: by each entry's rank where few, else
+// by a bitonic network over the next power of two.
 __device__ void sort_list(Shared &s, int32_t n) {
+    if (n <= kThreads) {
+        __syncthreads();
+        const unsigned long long mine = int32_t(threadIdx.x) < n ? s.list[threadIdx.x] : 0ull;
+        int32_t rank = 0;
+        if (int32_t(threadIdx.x) < n)
+            for (int32_t i = 0; i < n; i++) rank += s.list[i] > mine;
+        __syncthreads();
+        if (int32_t(threadIdx.x) < n) s.list[rank] = mine;
+        __syncthreads();
+        return;
+    }
     int32_t size = 2;
     while (size < n) size <<= 1;
     for (int32_t i = n + int32_t(threadIdx.x); i < size; i += kThreads) s.list[i] = 0ull;
@@ -286,7 +490,7 @@ __device__ void sort_list(Shared &s, int32_t n) {
         for (int32_t d = k >> 1; d; d >>= 1) {
             __syncthreads();
             for (int32_t i = threadIdx.x; i < size / 2; i += kThreads) {
-                const int32_t lo = (i / d) * 2 * d + i % d, hi = lo + d;
+                const int32_t lo = ((i & ~(d - 1)) << 1) | (i & (d - 1)), hi = lo + d;
                 const unsigned long long x = s.list[lo], y = s.list[hi];
                 if (((lo & k) == 0) == (x < y)) {
                     s.list[lo] = y;
@@ -298,27 +502,23 @@ __device__ void sort_list(Shared &s, int32_t n) {
     __syncthreads();
 }
 
-__device__ __forceinline__ int32_t list_id(unsigned long long e) { return int32_t(~uint32_t(e)); }
 __device__ __forceinline__ float list_value(unsigned long long e) { return key_value(uint32_t(e >> 32)); }
 
 // s.before[i] = weight of s.list[0, i); returns the whole list's weight. One
 // thread's share is consecutive entries, so the sums' order is fixed.
 __device__ float scan_list(Shared &s, int32_t n, float M, float T) {
-    constexpr int kPer = kList / kThreads;
+    const int32_t per = (n + kThreads - 1) / kThreads, first = int32_t(threadIdx.x) * per;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    float w[kPer], sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kPer; i++) {
-        const int32_t at = int32_t(threadIdx.x) * kPer + i;
-        w[i] = at < n ? weight(list_value(s.list[at]), M, T) : 0.0f;
-        sum += w[i];
-    }
+    float sum = 0.0f;
+    for (int32_t i = first; i < min(n, first + per); i++) sum += weight(list_value(s.list[i]), M, T);
     float upto = sum;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
         const float y = __shfl_up_sync(~0u, upto, d);
         if (lane >= d) upto += y;
     }
+    float before = __shfl_up_sync(~0u, upto, 1);
+    if (lane == 0) before = 0.0f;
     __syncthreads();
     if (lane == 31) s.f[warp] = upto;
     __syncthreads();
@@ -327,37 +527,181 @@ __device__ float scan_list(Shared &s, int32_t n, float M, float T) {
         if (i < warp) base += s.f[i];
         total += s.f[i];
     }
-    float at = base + (upto - sum);
-    if (lane == 0) at = base;
-#pragma unroll
-    for (int i = 0; i < kPer; i++) {
-        const int32_t p = int32_t(threadIdx.x) * kPer + i;
-        if (p < n) s.before[p] = at;
-        at += w[i];
+    before += base;
+    for (int32_t i = first; i < min(n, first + per); i++) {
+        s.before[i] = before;
+        before += weight(list_value(s.list[i]), M, T);
     }
     __syncthreads();
     return total;
 }
 
-// Draws from the first n entries of the sorted list.
-__device__ int32_t draw_list(Shared &s, int32_t n, float M, float T, int64_t seed) {
-    for (int32_t i = threadIdx.x; i < n; i += kThreads) s.before[i] = weight(list_value(s.list[i]), M, T);
+// How many of the first n entries of the sorted, scanned list are kept: those
+// before which the weight, `above` included, is below target, with w >= min_p.
+__device__ int32_t cut_list(Shared &s, int32_t n, float above, float target, const Way &way, float M) {
     __syncthreads();
+    if (threadIdx.x == 0) s.n = 0;
+    __syncthreads();
+    int32_t last = 0;
+    for (int32_t i = threadIdx.x; i < n; i += kThreads)
+        if (above + s.before[i] < target && weight(list_value(s.list[i]), M, way.T) >= way.min_p) last = i + 1;
+    if (last) atomicMax(&s.n, last);
+    __syncthreads();
+    n = s.n;
+    __syncthreads();
+    return n;
+}
+
+// The group drawn: of the first n entries of the list and, when `above`, what
+// stats[j].y holds of each group's weight besides. Reorders the n entries by
+// ascending id, as id << 32 | order_key.
+__device__ int32_t draw_group(Shared &s, int32_t n, bool above, const float2 *stats, int32_t G, float M, float T,
+                              int64_t seed) {
+    __syncthreads();
+    for (int32_t i = threadIdx.x; i < n; i += kThreads) s.list[i] = (s.list[i] << 32) | (s.list[i] >> 32);
+    __syncthreads();
+    sort_list(s, n);  // ~id descending
     Best best = {-INFINITY, -1};
     for (int32_t i = threadIdx.x; i < n; i += kThreads) {
-        const int32_t group = list_id(s.list[i]) / kGroup;
-        float mass = 0.0f;
-        for (int32_t j = 0; j < n; j++)
-            if (list_id(s.list[j]) / kGroup == group) mass += s.before[j];
+        const int32_t group = int32_t(~uint32_t(s.list[i] >> 32)) / kGroup;
+        if (i > 0 && int32_t(~uint32_t(s.list[i - 1] >> 32)) / kGroup == group) continue;
+        float mass = above ? stats[group].y : 0.0f;
+        for (int32_t k = i; k < n && int32_t(~uint32_t(s.list[k] >> 32)) / kGroup == group; k++)
+            mass += weight(key_value(uint32_t(s.list[k])), M, T);
         best = better(best, {logf(mass) + gumbel(seed, 0x80000000ull + uint32_t(group)), group});
     }
-    const int32_t group = block_best(s, best).id;
-    best = {-INFINITY, -1};
-    for (int32_t i = threadIdx.x; i < n; i += kThreads) {
-        const int32_t v = list_id(s.list[i]);
-        if (v / kGroup == group) best = better(best, {scaled(list_value(s.list[i]), M, T) + gumbel(seed, uint32_t(v)), v});
-    }
+    if (above)  // groups without an entry (one with entries scores more above than it does here)
+        for (int32_t j = threadIdx.x; j < G; j += kThreads) {
+            const float mass = stats[j].y;
+            if (mass > 0.0f) best = better(best, {logf(mass) + gumbel(seed, 0x80000000ull + uint32_t(j)), j});
+        }
     return block_best(s, best).id;
+}
+
+// One pass over the groups that reach bin `last`: s.list gets the tokens of bins
+// [first, last], stats[j].y the weight of each group's tokens of earlier bins
+// with w >= min_p, *n and *mass the number and weight of all of those. Returns
+// the list's length.
+template <typename T>
+__device__ int32_t split_at(Shared &s, const GroupLoad<T> &load, float2 *stats, int32_t G, const Bins &bins, int32_t first,
+                            int32_t last, const Way &way, float M, int32_t *n, float *mass) {
+    const int lane = threadIdx.x & 31;
+    const float c = __fdiv_rn(kLog2e, way.T);
+    __syncthreads();
+    if (threadIdx.x == 0) s.n = 0;
+    __syncthreads();
+    int32_t count = 0;
+    float sum = 0.0f;
+    for (int32_t j0 = int32_t(threadIdx.x >> 5); j0 * 32 < G; j0 += kWarps) {
+        const int32_t mine = j0 * 32 + lane;
+        const float top = mine < G ? stats[mine].x : -INFINITY;
+        uint32_t todo = __ballot_sync(~0u, top > -INFINITY && bins.bin(top) <= last);
+        float kept = 0.0f;  // of group `mine`
+        while (todo) {
+            const int at = __ffs(todo) - 1;
+            const int32_t j = j0 * 32 + at;
+            todo &= todo - 1;
+            float x[8], all = 0.0f, of = 0.0f;
+            load(j, lane, x);
+            uint32_t in = 0;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const int32_t bin = bins.bin(x[i]);
+                if (x[i] > -INFINITY && bin <= last) {
+                    if (bin >= first) {
+                        in |= 1u << i;
+                    } else {
+                        const float w = x[i] == M ? 1.0f : exp2_fast((x[i] - M) * c);
+                        count++;
+                        all += w;
+                        if (w >= way.min_p) of += w;
+                    }
+                }
+            }
+            sum += all;
+            of = warp_sum(of);
+            if (lane == at) kept = of;
+            append(s, load, j, x, in, lane);
+        }
+        if (mine < G) stats[mine].y = kept;
+    }
+    *n = block_sum(s, count);
+    *mass = block_sum(s, sum);
+    return s.n;
+}
+
+// Adds up the row's histograms in s.hist, weights relative to M.
+__device__ void sum_hist(Shared &s, const uint32_t *hist, int32_t parts, const Bins &bins, const Way &way, float M) {
+    constexpr int kPer = kBins / kThreads;
+    static_assert(kPer == 4, "one 16-byte load a thread and part");
+    const float c = __fdiv_rn(kLog2e, way.T);
+    uint32_t count[kPer] = {};
+    float mass[kPer] = {};
+    for (int32_t p = 0; p < parts; p++) {
+        const uint4 *at = reinterpret_cast<const uint4 *>(hist + int64_t(p) * 2 * kBins) + threadIdx.x;
+        const uint4 n = __ldcg(at), w = __ldcg(at + kBins / 4);
+        count[0] += n.x, count[1] += n.y, count[2] += n.z, count[3] += n.w;
+        mass[0] += float(w.x), mass[1] += float(w.y), mass[2] += float(w.z), mass[3] += float(w.w);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kPer; i++) {
+        const int bin = int(threadIdx.x) * kPer + i;
+        const float end = bins.top - float(bin) / kBinsPerUnit;
+        s.hist.count[bin] = count[i];
+        s.hist.mass[bin] = count[i] ? mass[i] / 65535.0f * exp2_fast((end - M) * c) : 0.0f;
+    }
+    __syncthreads();
+}
+
+// The bins [s.bin[0], s.bin[1]] in which the kept set ends: by count exactly, by
+// weight to within the histogram's precision. kBins: none found.
+__device__ void find_bins(Shared &s, bool by_mass, int32_t count, float target) {
+    constexpr int kPer = kBins / kThreads;
+    constexpr float kSlack = 1e-4f;  // weights in the histogram are rounded to 2^-16
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int32_t n = 0;
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kPer; i++) {
+        n += int32_t(s.hist.count[threadIdx.x * kPer + i]);
+        m += s.hist.mass[threadIdx.x * kPer + i];
+    }
+    int32_t n_upto = n;
+    float m_upto = m;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int32_t y = __shfl_up_sync(~0u, n_upto, d);
+        const float z = __shfl_up_sync(~0u, m_upto, d);
+        if (lane >= d) n_upto += y, m_upto += z;
+    }
+    __syncthreads();
+    if (lane == 31) s.i[warp] = n_upto, s.f[warp] = m_upto;
+    if (threadIdx.x == 0) s.bin[0] = s.bin[1] = kBins;
+    __syncthreads();
+    for (int i = 0; i < warp; i++) n_upto += s.i[i], m_upto += s.f[i];
+    n_upto -= n;
+    m_upto -= m;
+    int32_t lo = kBins, hi = kBins;
+#pragma unroll
+    for (int i = 0; i < kPer; i++) {
+        const int bin = int(threadIdx.x) * kPer + i;
+        n_upto += int32_t(s.hist.count[bin]);
+        m_upto += s.hist.mass[bin];
+        if (by_mass) {
+            if (lo == kBins && m_upto * (1.0f + kSlack) >= target) lo = bin;
+            if (hi == kBins && m_upto * (1.0f - kSlack) >= target) hi = bin;
+        } else if (lo == kBins && n_upto >= count) {
+            lo = hi = bin;
+        }
+    }
+    lo = __reduce_min_sync(~0u, lo);
+    hi = __reduce_min_sync(~0u, hi);
+    if (lane == 0) {
+        atomicMin(&s.bin[0], lo);
+        atomicMin(&s.bin[1], hi);
+    }
+    __syncthreads();
 }
 
 // The last kept token of a prefix of the order: every token above key is kept,
@@ -379,8 +723,8 @@ __device__ Cut radix_cut(Shared &s, const Row<T> &row, const float2 *stats, int3
     for (int shift = 24; shift >= 0; shift -= 8) {
         __syncthreads();
         for (int i = threadIdx.x; i < 256; i += kThreads) {
-            s.count[i] = 0u;
-            s.mass[i] = 0ull;
+            s.radix.count[i] = 0u;
+            s.radix.mass[i] = 0ull;
         }
         __syncthreads();
         for (int32_t j = threadIdx.x >> 5; j < G; j += kWarps) {
@@ -390,9 +734,24 @@ __device__ Cut radix_cut(Shared &s, const Row<T> &row, const float2 *stats, int3
                 const int64_t v = int64_t(j) * kGroup + i * 32 + lane;
                 const float x = v < row.V ? row(int32_t(v)) : -INFINITY;
                 const uint32_t k = order_key(x);
-                if (x > -INFINITY && (shift == 24 || (k >> (shift + 8)) == (key >> (shift + 8)))) {
-                    atomicAdd(&s.count[(k >> shift) & 255u], 1u);
-                    atomicAdd(&s.mass[(k >> shift) & 255u], (unsigned long long)(double(weight(x, M, T_)) * kFixed));
+                const bool in = x > -INFINITY && (shift == 24 || (k >> (shift + 8)) == (key >> (shift + 8)));
+                const uint32_t who = __ballot_sync(~0u, in);
+                if (!who) continue;
+                // the lanes that share the first one's digit add up in one go: equal logits come in crowds
+                const uint32_t digit = (k >> shift) & 255u, of_first = __shfl_sync(~0u, digit, __ffs(who) - 1);
+                const unsigned long long w = in ? (unsigned long long)(double(weight(x, M, T_)) * kFixed) : 0ull;
+                const bool same = in && digit == of_first;
+                const uint32_t crowd = __ballot_sync(~0u, same);
+                unsigned long long sum = same ? w : 0ull;
+#pragma unroll
+                for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+                if (lane == 0) {
+                    atomicAdd(&s.radix.count[of_first], uint32_t(__popc(crowd)));
+                    atomicAdd(&s.radix.mass[of_first], sum);
+                }
+                if (in && !same) {
+                    atomicAdd(&s.radix.count[digit], 1u);
+                    atomicAdd(&s.radix.mass[digit], w);
                 }
             }
         }
@@ -401,24 +760,24 @@ __device__ Cut radix_cut(Shared &s, const Row<T> &row, const float2 *stats, int3
             int last = -1, stop = -1;
             unsigned long long n = above_n, m = above_mass;
             for (int d = 255; d >= 0 && stop < 0; d--) {
-                if (!s.count[d]) continue;
+                if (!s.radix.count[d]) continue;
                 last = d;
-                if (by_mass ? m + s.mass[d] >= target : n + s.count[d] >= count) {
+                if (by_mass ? m + s.radix.mass[d] >= target : n + s.radix.count[d] >= count) {
                     stop = d;
                 } else {
-                    n += s.count[d];
-                    m += s.mass[d];
+                    n += s.radix.count[d];
+                    m += s.radix.mass[d];
                 }
             }
             if (stop < 0 && last >= 0) {  // fewer than asked for: up to the last one there is
                 stop = last;
-                n -= s.count[last];
-                m -= s.mass[last];
+                n -= s.radix.count[last];
+                m -= s.radix.mass[last];
             }
             s.key = key | (uint32_t(stop < 0 ? 0 : stop) << shift);
             s.above = n;
             s.total = m;
-            s.ties = stop < 0 ? 0 : int32_t(s.count[stop]);
+            s.ties = stop < 0 ? 0 : int32_t(s.radix.count[stop]);
         }
         __syncthreads();
         key = s.key;
@@ -499,18 +858,24 @@ __device__ int32_t last_tie(Shared &s, const Row<T> &row, float2 *stats, int32_t
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) k_sample_pick(SampleArgs a) {
-    __shared__ Shared s;
+__global__ void __launch_bounds__(kThreads, 2) k_sample_pick(SampleArgs a) {
+    extern __shared__ __align__(16) unsigned char dynamic_smem[];
+    Shared &s = *reinterpret_cast<Shared *>(dynamic_smem);
     pdl_launch_dependents();
     pdl_wait();
     const int32_t b = blockIdx.x, G = a.G;
     const int lane = threadIdx.x & 31;
     const Way way = row_way(a, b);
     const Row<T> row = row_at<T>(a, b);
+    const GroupLoad<T> load(row);
     float2 *stats = a.stats + int64_t(b) * G;
-    const int64_t seed = a.seeds ? __ldg(a.seeds + b) : 0;
-    float M = -INFINITY;
-    for (int32_t j = threadIdx.x; j < G; j += kThreads) M = fmaxf(M, stats[j].x);
+    const int64_t seed = __ldg(a.seeds + b);
+    float M = -INFINITY, low = INFINITY;
+    for (int32_t j = threadIdx.x; j < G; j += kThreads) {
+        const float x = stats[j].x;
+        M = fmaxf(M, x);
+        if (x > -INFINITY) low = fminf(low, x);
+    }
     M = block_max(s, M);
     if (M == -INFINITY) {
         if (threadIdx.x == 0) {
@@ -519,6 +884,7 @@ __global__ void __launch_bounds__(kThreads) k_sample_pick(SampleArgs a) {
         }
         return;
     }
+    low = -block_max(s, -low);
     float Z = 0.0f;
     for (int32_t j = threadIdx.x; j < G; j += kThreads) {
         const float2 g = stats[j];
@@ -526,33 +892,73 @@ __global__ void __launch_bounds__(kThreads) k_sample_pick(SampleArgs a) {
     }
     Z = block_sum(s, Z);
 
-    int32_t token = -1;
     const bool by_k = !way.greedy && way.k > 0, by_p = !way.greedy && way.p < 1.0f;
-    if ((by_k && way.k <= kListK) || (by_p && !by_k)) {
-        const uint32_t from = nth_group(stats, G, by_k ? way.k : kGuess);
-        const int32_t n = collect(s, row, stats, G, from);
+    const bool filtered = by_k || by_p || (!way.greedy && way.min_p > 0.0f);
+    int32_t group = -1;         // of the token, once drawn
+    // what is kept, min_p aside: tokens at or above `last` (order_key << 32 | ~id), and those of bins before bins_kept
+    unsigned long long last = 0ull;
+    int32_t bins_kept = 0;
+    const Bins bins(stats[0].x);
+    if (by_k && !wants_hist(way, a.G)) {
+        const uint32_t from = nth_group(s, stats, G, way.k, M, low);
+        const int32_t n = collect(s, load, stats, G, from);
         if (n <= kList) {
             sort_list(s, n);
             const float total = scan_list(s, n, M, way.T);
-            const int32_t first = by_k ? min(way.k, n) : n;
-            const float Zk = by_k ? (first < n ? s.before[first] : total) : Z;
-            const float target = way.p * Zk;
-            // without top-k the list has to hold the whole top-p set, or every token
-            if (by_k || total >= target || from == kKeyNone) {
-                if (threadIdx.x == 0) s.n = 1;
-                __syncthreads();
-                int32_t last = 0;
-                for (int32_t i = threadIdx.x; i < first; i += kThreads)
-                    if ((!by_p || s.before[i] < target) && weight(list_value(s.list[i]), M, way.T) >= way.min_p)
-                        last = i + 1;
-                atomicMax(&s.n, last);
-                __syncthreads();
-                const int32_t kept = s.n;
-                token = draw_list(s, kept, M, way.T, seed);
+            const int32_t first = min(way.k, n);
+            const float target = by_p ? way.p * (first < n ? s.before[first] : total) : INFINITY;
+            const int32_t kept = max(1, cut_list(s, first, 0.0f, target, way, M));
+            last = s.list[kept - 1];
+            group = draw_group(s, kept, false, stats, G, M, way.T, seed);
+        }
+    } else if (wants_hist(way, a.G)) {
+        const uint32_t *hist = a.hist + int64_t(b) * a.parts * 2 * kBins;
+        float target = INFINITY, above = 0.0f, Zk = Z;
+        int32_t first = -1, end = -1, n = 0, n_above = 0, kept = 0;
+        bool done = true;
+        if (by_k) {
+            sum_hist(s, hist, a.parts, bins, way, M);
+            find_bins(s, false, way.k, 0.0f);
+            first = end = s.bin[0];
+            if (first < kBins) {
+                n = split_at(s, load, stats, G, bins, first, end, way, M, &n_above, &above);
+                done = n <= kList;
+                if (done) {
+                    sort_list(s, n);
+                    const float total = scan_list(s, n, M, way.T);
+                    kept = min(n, way.k - n_above);
+                    Zk = above + (kept < n ? s.before[kept] : total);
+                    if (!by_p) kept = cut_list(s, kept, 0.0f, INFINITY, way, M);
+                }
+            } else {  // fewer tokens than top_k: all of them
+                done = by_p;
             }
         }
+        if (done && by_p) {
+            target = way.p * Zk;
+            sum_hist(s, hist, a.parts, bins, way, M);
+            find_bins(s, true, 0, target);
+            first = s.bin[0];
+            end = s.bin[1];
+            done = end < kBins;
+            if (done) {
+                n = split_at(s, load, stats, G, bins, first, end, way, M, &n_above, &above);
+                done = n <= kList;
+            }
+            if (done) {
+                sort_list(s, n);
+                const float total = scan_list(s, n, M, way.T);
+                done = above < target && above + total >= target;
+                if (done) kept = cut_list(s, n, above, target, way, M);
+            }
+        }
+        if (done) {
+            bins_kept = first;
+            last = kept > 0 ? s.list[kept - 1] : ~0ull;
+            group = draw_group(s, kept, true, stats, G, M, way.T, seed);
+        }
     }
-    if (token < 0) {
+    if (group < 0) {
         Cut cut = {kKeyNone, 0, Z};
         int32_t last_id = 0x7FFFFFFF;
         if (by_k) cut = radix_cut(s, row, stats, G, M, way.T, false, uint32_t(way.k), 0ull);
@@ -562,8 +968,10 @@ __global__ void __launch_bounds__(kThreads) k_sample_pick(SampleArgs a) {
                                     target > 0.0 ? (unsigned long long)(target) : 0ull);
             if (!by_k || c.key > cut.key || (c.key == cut.key && c.ties < cut.ties)) cut = c;
         }
-        const bool filtered = by_k || by_p || (!way.greedy && way.min_p > 0.0f);
-        if (by_k || by_p) last_id = last_tie(s, row, stats, G, cut);
+        if (by_k || by_p) {
+            last_id = last_tie(s, row, stats, G, cut);
+            last = (uint64_t(cut.key) << 32) | uint32_t(~uint32_t(last_id));
+        }
         Best best = {-INFINITY, -1};
         if (!filtered) {
             for (int32_t j = threadIdx.x; j < G; j += kThreads) {
@@ -576,37 +984,63 @@ __global__ void __launch_bounds__(kThreads) k_sample_pick(SampleArgs a) {
             for (int32_t j = threadIdx.x >> 5; j < G; j += kWarps) {
                 const uint32_t top = order_key(stats[j].x);
                 if (top < cut.key || top <= kKeyNone || weight(stats[j].x, M, way.T) < way.min_p) continue;
-                float mass = 0.0f;
-                for (int i = 0; i < kGroup / 32; i++) {
-                    const int64_t v = int64_t(j) * kGroup + i * 32 + lane;
-                    const float x = v < a.V ? row(int32_t(v)) : -INFINITY;
-                    const uint32_t k = order_key(x);
-                    const float w = weight(x, M, way.T);
-                    if (x > -INFINITY && (k > cut.key || (k == cut.key && v <= last_id)) && (x == M || w >= way.min_p)) mass += w;
+                float x[8], mass = 0.0f;
+                load(j, lane, x);
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const uint32_t k = order_key(x[i] + 0.0f);
+                    const int32_t v = j * kGroup + load.id(i, lane);
+                    const float w = weight(x[i], M, way.T);
+                    if (x[i] > -INFINITY && (k > cut.key || (k == cut.key && v <= last_id)) && w >= way.min_p) mass += w;
                 }
                 mass = warp_sum(mass);
                 if (mass > 0.0f) best = better(best, {logf(mass) + gumbel(seed, 0x80000000ull + uint32_t(j)), j});
             }
         }
-        const int32_t group = block_best(s, best).id;
-        best = {-INFINITY, -1};
-        if (threadIdx.x < kGroup) {
-            const int64_t v = int64_t(group) * kGroup + threadIdx.x;
-            const float x = v < a.V ? row(int32_t(v)) : -INFINITY;
-            const uint32_t k = order_key(x);
-            if (x > -INFINITY) {
-                if (way.greedy) best = {x, int32_t(v)};
-                else if (!filtered || ((k > cut.key || (k == cut.key && v <= last_id)) &&
-                                       (x == M || weight(x, M, way.T) >= way.min_p)))
-                    best = {scaled(x, M, way.T) + gumbel(seed, uint32_t(v)), int32_t(v)};
-            }
-        }
-        token = block_best(s, best).id;
+        group = block_best(s, best).id;
     }
+    Best best = {-INFINITY, -1};
+    if (threadIdx.x < kGroup) {
+        const int64_t v = int64_t(group) * kGroup + threadIdx.x;
+        const float x = v < a.V ? row(int32_t(v)) : -INFINITY;
+        if (x > -INFINITY) {
+            const unsigned long long entry = (uint64_t(order_key(x)) << 32) | uint32_t(~uint32_t(v));
+            const bool kept = !filtered || ((entry >= last || bins.bin(x) < bins_kept) &&
+                                            (x == M || weight(x, M, way.T) >= way.min_p));
+            if (way.greedy) best = {x, int32_t(v)};
+            else if (kept) best = {scaled(x, M, way.T) + gumbel(seed, uint32_t(v)), int32_t(v)};
+        }
+    }
+    const int32_t token = block_best(s, best).id;
     if (threadIdx.x == 0) {
         a.tokens[b] = token;
         if (a.logprobs) a.logprobs[b] = scaled(row(token), M, way.T) - logf(Z);
     }
+}
+
+// How a batch is cut and where its parts of the workspace lie. A CTA of
+// k_sample_groups takes kChunk groups, or fewer where the batch is small, so
+// that there are some four CTAs an SM.
+struct Plan {
+    int32_t G, chunk, parts;
+    int64_t hist_at, bytes;
+    Plan(int32_t B, int32_t V) {
+        G = int32_t((int64_t(V) + kGroup - 1) / kGroup);
+        chunk = kChunk;
+        while (chunk > 16 && int64_t(B) * ((G + chunk - 1) / chunk) < 600) chunk /= 2;
+        parts = (G + chunk - 1) / chunk;
+        hist_at = (int64_t(B) * G * int64_t(sizeof(float2)) + 255) / 256 * 256;
+        bytes = hist_at + int64_t(B) * parts * 2 * kBins * 4;
+    }
+};
+
+template <typename T>
+cudaError_t launch_sample(const SampleArgs &a, int32_t B, cudaStream_t st) {
+    cudaError_t e = launch_pdl_grid(k_sample_groups<T>, dim3(unsigned(a.parts), unsigned(B)), kGroupThreads, 0, st, a);
+    if (e != cudaSuccess) return e;
+    e = cudaFuncSetAttribute(k_sample_pick<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(sizeof(Shared)));
+    if (e != cudaSuccess) return e;
+    return launch_pdl_smem(k_sample_pick<T>, B, kThreads, sizeof(Shared), st, a);
 }
 
 }  // namespace
@@ -614,8 +1048,8 @@ __global__ void __launch_bounds__(kThreads) k_sample_pick(SampleArgs a) {
 }  // namespace tmk
 
 extern "C" int64_t trie_sample_workspace(int32_t B, int32_t V) {
-    if (B < 0 || V < 2 || V > tmk::kMaxV) return -1;
-    return int64_t(B) * ((int64_t(V) + tmk::kGroup - 1) / tmk::kGroup) * int64_t(sizeof(float2));
+    if (B < 0 || B > 65535 || V < 2 || V > tmk::kMaxV) return -1;
+    return tmk::Plan(B, V).bytes;
 }
 
 extern "C" int trie_sample(const void *d_logits, int dtype, int64_t stride, int32_t B, int32_t V, const int64_t *d_seeds,
@@ -627,7 +1061,7 @@ extern "C" int trie_sample(const void *d_logits, int dtype, int64_t stride, int3
     if (!*bad) bad = check_grammar(d_mask, mask_rows, d_states);
     if (!*bad && B > 65535) bad = "B must be <= 65535";
     if (!*bad && B > 0 && (!d_tokens || !d_workspace)) bad = "d_tokens / d_workspace is NULL";
-    if (!*bad && (reinterpret_cast<uintptr_t>(d_workspace) & 7)) bad = "d_workspace is not aligned to 8 bytes";
+    if (!*bad && (reinterpret_cast<uintptr_t>(d_workspace) & 15)) bad = "d_workspace is not aligned to 16 bytes";
     if (!*bad && B > 0 && !d_seeds) bad = "d_seeds is NULL";
     if (*bad) return set_error(TRIE_EINVAL, bad);
     if (B == 0) return TRIE_OK;
@@ -635,7 +1069,10 @@ extern "C" int trie_sample(const void *d_logits, int dtype, int64_t stride, int3
     a.logits = d_logits;
     a.stride = stride;
     a.V = V;
-    a.G = int32_t((int64_t(V) + kGroup - 1) / kGroup);
+    const Plan plan(B, V);
+    a.G = plan.G;
+    a.chunk = plan.chunk;
+    a.parts = plan.parts;
     a.seeds = d_seeds;
     a.temperature = d_temperature;
     a.top_k = d_top_k;
@@ -643,15 +1080,11 @@ extern "C" int trie_sample(const void *d_logits, int dtype, int64_t stride, int3
     a.min_p = d_min_p;
     a.g = make_grammar(d_mask, mask_rows, d_states, V);
     a.stats = static_cast<float2 *>(d_workspace);
+    a.hist = reinterpret_cast<uint32_t *>(static_cast<unsigned char *>(d_workspace) + plan.hist_at);
     a.tokens = d_tokens;
     a.logprobs = d_logprobs;
-    const dim3 grid((unsigned(a.G) + kGroupThreads / 32 - 1) / (kGroupThreads / 32), unsigned(B));
-    const bool f32 = dtype == TRIE_DTYPE_F32;
-    cudaError_t e = f32 ? launch_pdl_grid(k_sample_groups<float>, grid, kGroupThreads, 0, stream, a)
-                        : launch_pdl_grid(k_sample_groups<__nv_bfloat16>, grid, kGroupThreads, 0, stream, a);
-    if (e != cudaSuccess) return fail_launch(e, "sample groups launch");
-    e = f32 ? launch_pdl(k_sample_pick<float>, B, kThreads, stream, a)
-            : launch_pdl(k_sample_pick<__nv_bfloat16>, B, kThreads, stream, a);
-    if (e != cudaSuccess) return fail_launch(e, "sample pick launch");
+    const cudaError_t e = dtype == TRIE_DTYPE_F32 ? launch_sample<float>(a, B, stream)
+                                                  : launch_sample<__nv_bfloat16>(a, B, stream);
+    if (e != cudaSuccess) return fail_launch(e, "sample launch");
     return TRIE_OK;
 }
