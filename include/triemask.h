@@ -533,7 +533,7 @@ int trie_head_logits(const uint8_t *d_q, const float *d_scales, int64_t pitch, c
  * in 32 bits, each operation rounded to nearest, rounded once to the logits'
  * type; logits that nothing applies to keep their bits.
  *   d_history  device int32[B] rows, history_stride apart, of which the first
- *              d_length[b] tokens count (at most max_length, <= history_stride);
+ *              d_length[b] tokens count (at most max_length <= 2^28, <= history_stride);
  *              ids outside [0, V) are skipped. NULL: no history.
  *   d_prompt   device int32[B]: the first d_prompt[b] tokens of the history are
  *              the prompt (NULL: none are)

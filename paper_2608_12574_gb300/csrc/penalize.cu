@@ -10,11 +10,18 @@
 // in 32 bits, each operation rounded to nearest, with one rounding to bf16 at
 // the end. Logits that nothing applies to keep their bits and are not read.
 //
-//  k_penalize  one CTA per row and window of kWindow tokens: the row's history
-//              is counted into a shared-memory table of the window (integer
-//              atomics, so the order does not matter), its biases are added
-//              up in list order, and the window's logits are written where
-//              something applies.
+// k_penalize has CTAs of two kinds, which touch different logits (allowed and
+// not allowed ones) and so need no order among them:
+//   edits  the row's history and biases are entered into a hash table in shared
+//          memory (integer atomics: their order does not matter; a token listed
+//          twice among the biases is added up in list order when it is written),
+//          then each entry's logit is read and written: what is moved is the
+//          history and the touched logits, not the row. A long history is split
+//          over several CTAs by a hash of the token, each of which reads all of
+//          it and keeps its own. Where a table fills up (long bias lists), the
+//          CTA goes over the vocabulary in windows of the table's size instead.
+//   fills  -inf into a segment of a constrained row, 16 bytes at a time where
+//          nothing is allowed; allowed logits are neither read nor written.
 #include <math.h>
 #include <stdint.h>
 #include <stdio.h>
@@ -28,8 +35,17 @@ namespace tmk {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kWindow = 8192;
-constexpr uint32_t kSeen = 0x80000000u;  // beside the count of a table entry
+constexpr int kTable = 4096;             // entries of an edit CTA's table: 48 KB, four CTAs an SM
+constexpr int kTableBits = 12;
+constexpr int kShare = 2400;             // history tokens of one edit CTA: at most 0.6 of the table when all differ
+constexpr int kProbes = 128;             // past this the table counts as full
+constexpr int kSegment = 8192;           // tokens of a fill CTA
+constexpr uint32_t kNoToken = 0xFFFFFFFFu;
+// beside the count of an entry's occurrences in the output:
+constexpr uint32_t kPrompt = 0x80000000u;  // it is in the prompt
+constexpr uint32_t kBiased = 0x40000000u;  // it has a bias
+constexpr uint32_t kAgain = 0x20000000u;   // it has several
+constexpr uint32_t kCount = 0x1FFFFFFFu;
 
 struct PenalizeArgs {
     void *logits;
@@ -43,76 +59,215 @@ struct PenalizeArgs {
     const float *repetition, *presence, *frequency;
     const int32_t *bias_offsets, *bias_tokens;
     const float *bias_values;
+    int32_t shards;          // edit CTAs of a row
     Grammar g;
 };
 
-__device__ __forceinline__ float penalized(float x, uint32_t entry, float r, float p, float f) {
-    if (!entry) return x;
-    x = x > 0.0f ? __fdiv_rn(x, r) : __fmul_rn(x, r);
-    const uint32_t c = entry & ~kSeen;
-    if (c) x = __fsub_rn(__fsub_rn(x, __fmul_rn(f, float(c))), p);
-    return x;
+struct Table {
+    uint32_t token[kTable];
+    uint32_t entry[kTable];
+    float bias[kTable];
+};
+
+__device__ __forceinline__ uint32_t mix(uint32_t t) {
+    t *= 0x9E3779B1u;
+    return t ^ (t >> 15);
+}
+__device__ __forceinline__ bool in_shard(const PenalizeArgs &a, uint32_t t, uint32_t shard) {
+    return a.shards == 1 || __umulhi(t * 0x85EBCA6Bu, uint32_t(a.shards)) == shard;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) k_penalize(PenalizeArgs a) {
-    __shared__ uint32_t count[kWindow];
-    __shared__ float bias[kWindow];
-    const int32_t b = blockIdx.y;
-    const int32_t v0 = blockIdx.x * kWindow, v1 = min(a.V - v0, kWindow) + v0;
-    const uint32_t n = v1 - v0;
-    for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
-        count[i] = 0u;
-        bias[i] = 0.0f;
+// The slot of token t, entered if it is not there; -1: the table is full.
+__device__ __forceinline__ int32_t slot_of(Table &table, uint32_t t) {
+    uint32_t at = (mix(t) * 0xC2B2AE35u) >> (32 - kTableBits);
+    for (int i = 0; i < kProbes; i++) {
+        const uint32_t old = atomicCAS(&table.token[at], kNoToken, t);
+        if (old == kNoToken || old == t) return int32_t(at);
+        at = (at + 1) & (kTable - 1);
     }
-    __syncthreads();
-    pdl_launch_dependents();
-    pdl_wait();
+    return -1;
+}
+
+// Enters the row's history and biases. `base` < 0: into the hash table (false
+// when it is full); else into the window of tokens base .. base + kTable - 1.
+__device__ bool enter(const PenalizeArgs &a, Table &table, int32_t b, uint32_t shard, int64_t base) {
+    bool fits = true;
+    auto find = [&](uint32_t t) -> int32_t {
+        if (t >= uint32_t(a.V) || !in_shard(a, t, shard)) return -2;
+        if (base >= 0) return int64_t(t) >= base && int64_t(t) < base + kTable ? int32_t(int64_t(t) - base) : -2;
+        const int32_t at = slot_of(table, t);
+        fits &= at >= 0;
+        return at;
+    };
     if (a.history) {
         const int32_t len = max(0, min(__ldg(a.length + b), a.H));
         const int32_t prompt = a.prompt ? __ldg(a.prompt + b) : 0;
         const int32_t *h = a.history + b * a.history_stride;
-        for (int32_t i = threadIdx.x; i < len; i += kThreads) {
-            const uint32_t t = uint32_t(__ldg(h + i)) - uint32_t(v0);
-            if (t < n) {
-                if (i >= prompt) atomicAdd(count + t, 1u);
-                atomicOr(count + t, kSeen);
-            }
+        auto say = [&](int32_t i, uint32_t t) {
+            const int32_t at = find(t);
+            if (at < 0) return;
+            if (i >= prompt) atomicAdd(&table.entry[at], 1u);
+            else if (!(*reinterpret_cast<volatile uint32_t *>(&table.entry[at]) & kPrompt)) atomicOr(&table.entry[at], kPrompt);
+        };
+        // to a 16-byte boundary, by fours, and the rest
+        const int32_t head = min(len, int32_t((16 - (reinterpret_cast<uintptr_t>(h) & 15)) & 15) / 4);
+        const int32_t fours = (len - head) / 4, tail = head + fours * 4;
+        if (int32_t(threadIdx.x) < head) say(int32_t(threadIdx.x), uint32_t(__ldg(h + threadIdx.x)));
+        const int4 *q = reinterpret_cast<const int4 *>(h + head);
+        for (int32_t i = threadIdx.x; i < fours && fits; i += 2 * kThreads) {
+            const bool two = i + kThreads < fours;
+            const int4 x = __ldg(q + i), y = two ? __ldg(q + i + kThreads) : make_int4(-1, -1, -1, -1);
+            const int32_t at = head + 4 * i, next = at + 4 * kThreads;
+            say(at, uint32_t(x.x)), say(at + 1, uint32_t(x.y)), say(at + 2, uint32_t(x.z)), say(at + 3, uint32_t(x.w));
+            if (two) say(next, uint32_t(y.x)), say(next + 1, uint32_t(y.y)), say(next + 2, uint32_t(y.z)), say(next + 3, uint32_t(y.w));
         }
+        if (tail + int32_t(threadIdx.x) < len) say(tail + int32_t(threadIdx.x), uint32_t(__ldg(h + tail + threadIdx.x)));
     }
     if (a.bias_offsets) {
         const int32_t lo = __ldg(a.bias_offsets + b), hi = __ldg(a.bias_offsets + b + 1);
-        for (int32_t i = lo + int32_t(threadIdx.x); i < hi; i += kThreads) {
-            const int32_t t = __ldg(a.bias_tokens + i);
-            if (uint32_t(t) - uint32_t(v0) >= n) continue;
-            bool first = true;  // the first of a token's entries adds up all of them, in list order
-            for (int32_t j = lo; j < i && first; j++) first = __ldg(a.bias_tokens + j) != t;
-            if (!first) continue;
-            float sum = __ldg(a.bias_values + i);
-            for (int32_t j = i + 1; j < hi; j++)
-                if (__ldg(a.bias_tokens + j) == t) sum = __fadd_rn(sum, __ldg(a.bias_values + j));
-            bias[t - v0] = sum;
+        for (int32_t i = lo + int32_t(threadIdx.x); i < hi && fits; i += kThreads) {
+            const int32_t at = find(uint32_t(__ldg(a.bias_tokens + i)));
+            if (at < 0) continue;
+            if (atomicOr(&table.entry[at], kBiased) & kBiased) atomicOr(&table.entry[at], kAgain);
+            else table.bias[at] = __ldg(a.bias_values + i);
         }
     }
-    __syncthreads();
-    const float r = a.repetition ? __ldg(a.repetition + b) : 1.0f;
-    const float p = a.presence ? __ldg(a.presence + b) : 0.0f;
-    const float f = a.frequency ? __ldg(a.frequency + b) : 0.0f;
+    return fits;
+}
+
+__device__ __forceinline__ float bias_sum(const PenalizeArgs &a, int32_t b, int32_t t) {
+    const int32_t lo = __ldg(a.bias_offsets + b), hi = __ldg(a.bias_offsets + b + 1);
+    float sum = 0.0f;
+    bool first = true;
+    for (int32_t i = lo; i < hi; i++)
+        if (__ldg(a.bias_tokens + i) == t) {
+            sum = first ? __ldg(a.bias_values + i) : __fadd_rn(sum, __ldg(a.bias_values + i));
+            first = false;
+        }
+    return sum;
+}
+
+struct Rates {
+    float r, p, f;
+};
+
+__device__ __forceinline__ float penalized(float x, uint32_t entry, const Rates &k, float bias) {
+    const uint32_t c = entry & kCount;
+    if (c || (entry & kPrompt)) x = x > 0.0f ? __fdiv_rn(x, k.r) : __fmul_rn(x, k.r);
+    if (c) x = __fsub_rn(__fsub_rn(x, __fmul_rn(k.f, float(c))), k.p);
+    if (entry & kBiased) x = __fadd_rn(x, bias);
+    return x;
+}
+
+// Writes the logits of the table's entries (base >= 0: a window's) and clears it.
+template <typename T>
+__device__ void write_entries(const PenalizeArgs &a, Table &table, int32_t b, T *logits, int64_t base) {
+    Rates k;
+    k.r = a.repetition ? __ldg(a.repetition + b) : 1.0f;
+    k.p = a.presence ? __ldg(a.presence + b) : 0.0f;
+    k.f = a.frequency ? __ldg(a.frequency + b) : 0.0f;
     const GrammarRow row = grammar_row(a.g, b);
-    T *logits = static_cast<T *>(a.logits) + b * a.stride + v0;
-    for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
-        if (!row.allows(v0 + int32_t(i))) {
-            logits[i] = from_f32<T>(-INFINITY);
-            continue;
+    constexpr int kBatch = 4;  // reads in flight a thread
+    for (int s0 = threadIdx.x; s0 < kTable; s0 += kBatch * kThreads) {
+        uint32_t entry[kBatch];
+        int32_t t[kBatch];
+        float x[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; i++) {
+            entry[i] = table.entry[s0 + i * kThreads];
+            t[i] = base >= 0 ? int32_t(base) + s0 + i * kThreads : int32_t(table.token[s0 + i * kThreads]);
+            if (entry[i] && !row.allows(t[i])) entry[i] = 0u;
         }
-        const uint32_t c = count[i];
-        const float add = bias[i];
-        if (c || add != 0.0f) {
-            float x = penalized(to_f32(logits[i]), c, r, p, f);
-            if (add != 0.0f) x = __fadd_rn(x, add);
-            logits[i] = from_f32<T>(x);
+#pragma unroll
+        for (int i = 0; i < kBatch; i++) x[i] = entry[i] ? to_f32(logits[t[i]]) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < kBatch; i++) {
+            if (!entry[i]) continue;
+            const float bias = entry[i] & kAgain ? bias_sum(a, b, t[i]) : table.bias[s0 + i * kThreads];
+            logits[t[i]] = from_f32<T>(penalized(x[i], entry[i], k, bias));
         }
     }
+}
+
+__device__ __forceinline__ void clear(Table &table) {
+    for (int i = threadIdx.x; i < kTable / 4; i += kThreads) {
+        reinterpret_cast<uint4 *>(table.token)[i] = make_uint4(kNoToken, kNoToken, kNoToken, kNoToken);
+        reinterpret_cast<uint4 *>(table.entry)[i] = make_uint4(0u, 0u, 0u, 0u);
+    }
+}
+
+template <typename T>
+__device__ void edit_row(const PenalizeArgs &a, Table &table, int32_t b, uint32_t shard) {
+    T *logits = static_cast<T *>(a.logits) + b * a.stride;
+    const bool fits = enter(a, table, b, shard, -1);
+    if (__syncthreads_and(fits)) {
+        write_entries(a, table, b, logits, -1);
+        return;
+    }
+    for (int64_t base = 0; base < a.V; base += kTable) {
+        clear(table);
+        __syncthreads();
+        enter(a, table, b, shard, base);
+        __syncthreads();
+        write_entries(a, table, b, logits, base);
+        __syncthreads();
+    }
+}
+
+// -inf into the tokens v0 .. v1 - 1 of row b that its state does not allow.
+template <typename T>
+__device__ void fill_segment(const PenalizeArgs &a, int32_t b, int32_t v0, int32_t v1) {
+    constexpr int kVec = 16 / sizeof(T);
+    const GrammarRow row = grammar_row(a.g, b);
+    if (row.kind == kAllowAll) return;
+    T *logits = static_cast<T *>(a.logits) + b * a.stride;
+    const T none = from_f32<T>(-INFINITY);
+    // chunks of 16 bytes by address; the first may begin before v0, the last end past v1
+    const int32_t ahead = int32_t((reinterpret_cast<uintptr_t>(logits + v0) & 15) / sizeof(T));
+    const int32_t last = (a.V - 1) >> 5;
+    const uint32_t pair = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
+    const uint4 fill = make_uint4(pair, pair, pair, pair);
+#pragma unroll 4
+    for (int32_t c = threadIdx.x; c * kVec < v1 - v0 + ahead; c += kThreads) {
+        const int32_t t = v0 - ahead + c * kVec;  // the chunk's first token
+        const int32_t w = t >> 5;
+        const uint32_t lo = w >= 0 ? row.word(w) : 0u, hi = (t & 31) > 32 - kVec && w < last ? row.word(w + 1) : 0u;
+        const uint32_t bits = __funnelshift_r(lo, hi, t & 31) & ((1u << kVec) - 1u);
+        if (bits == 0u && t >= v0 && t + kVec <= v1) {
+            *reinterpret_cast<uint4 *>(logits + t) = fill;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kVec; i++)
+                if (!((bits >> i) & 1u) && t + i >= v0 && t + i < v1) logits[t + i] = none;
+        }
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) k_penalize(PenalizeArgs a) {
+    extern __shared__ __align__(16) unsigned char dynamic_smem[];
+    Table &table = *reinterpret_cast<Table *>(dynamic_smem);
+    const int32_t b = blockIdx.y;
+    const bool edits = blockIdx.x < unsigned(a.shards);
+    if (edits) {
+        clear(table);
+        __syncthreads();
+    }
+    pdl_launch_dependents();
+    pdl_wait();
+    if (edits) {
+        edit_row<T>(a, table, b, blockIdx.x);
+    } else {
+        const int32_t v0 = int32_t(blockIdx.x - unsigned(a.shards)) * kSegment;
+        fill_segment<T>(a, b, v0, v0 + min(kSegment, a.V - v0));
+    }
+}
+
+template <typename T>
+cudaError_t launch_penalize(const PenalizeArgs &a, dim3 grid, cudaStream_t st) {
+    const cudaError_t e = cudaFuncSetAttribute(k_penalize<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(sizeof(Table)));
+    if (e != cudaSuccess) return e;
+    return launch_pdl_grid(k_penalize<T>, grid, kThreads, sizeof(Table), st, a);
 }
 
 }  // namespace
@@ -130,7 +285,7 @@ extern "C" int trie_penalize(void *d_logits, int dtype, int64_t stride, int32_t 
     if (!*bad) bad = check_grammar(d_mask, mask_rows, d_states);
     if (!*bad && d_history) {
         if (!d_length) bad = "d_history without d_length";
-        else if (max_length < 0 || max_length > (1 << 30)) bad = "max_length must be in [0, 2^30]";
+        else if (max_length < 0 || max_length > (1 << 28)) bad = "max_length must be in [0, 2^28]";
         else if (history_stride < max_length) bad = "history_stride must be >= max_length";
     }
     if (!*bad && d_bias_offsets && (!d_bias_tokens || !d_bias_values))
@@ -154,9 +309,12 @@ extern "C" int trie_penalize(void *d_logits, int dtype, int64_t stride, int32_t 
     a.bias_tokens = d_bias_tokens;
     a.bias_values = d_bias_values;
     a.g = make_grammar(d_mask, mask_rows, d_states, V);
-    const dim3 grid((unsigned(V) + kWindow - 1) / kWindow, unsigned(B));
-    const cudaError_t e = dtype == TRIE_DTYPE_F32 ? launch_pdl_grid(k_penalize<float>, grid, kThreads, 0, stream, a)
-                                                  : launch_pdl_grid(k_penalize<__nv_bfloat16>, grid, kThreads, 0, stream, a);
+    const bool any = (d_history && max_length > 0) || d_bias_offsets;
+    a.shards = !any ? 0 : max_length > kShare ? (max_length + kShare - 1) / kShare : 1;
+    const dim3 grid(unsigned(a.shards) + (d_mask ? (unsigned(V) + kSegment - 1) / kSegment : 0u), unsigned(B));
+    if (grid.x == 0) return TRIE_OK;  // nothing applies
+    const cudaError_t e = dtype == TRIE_DTYPE_F32 ? launch_penalize<float>(a, grid, stream)
+                                                  : launch_penalize<__nv_bfloat16>(a, grid, stream);
     if (e != cudaSuccess) return fail_launch(e, "penalize launch");
     return TRIE_OK;
 }

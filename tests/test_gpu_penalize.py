@@ -175,6 +175,22 @@ def test_penalize_crowded_histories(cuda, stride):
     _check(case[0], out, *case[1:])
 
 
+@pytest.mark.parametrize("n", [4090, 20000])
+def test_penalize_long_bias_lists(cuda, n):
+    """Rows with more biased tokens than a table holds, beside rows with few and with none."""
+    rng = np.random.default_rng(n)
+    V, B = 33001, 4
+    case = list(_case(rng, V, B, 500, 5, 4, "f32"))
+    many = [n, 0, 7, 3]
+    off = np.concatenate([[0], np.cumsum(many)]).astype(np.int32)
+    tok = rng.integers(0, V, off[-1]).astype(np.int32)   # some twice
+    tok[:2 * V // 3:3][:n // 3] = rng.permutation(V)[:len(tok[:2 * V // 3:3][:n // 3])]
+    case[7] = (off, tok, rng.normal(0, 3, off[-1]).astype(np.float32))
+    case[9][:] = [FREE, FREE, 1, 3]
+    out = _run(cuda, V, *case)
+    _check(case[0], out, *case[1:])
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_penalize_special_values(cuda, dtype):
     """Infinities, NaN, zeros and the type's lowest value, touched and untouched, allowed and not."""
