@@ -3,6 +3,9 @@
 #pragma once
 
 #include <stdint.h>
+#include <stdio.h>
+
+#include <atomic>
 
 #include <cuda_bf16.h>
 
@@ -91,6 +94,16 @@ inline Grammar make_grammar(const uint32_t *d_mask, int32_t mask_rows, const int
     g.V = V;
     g.W = (int64_t(V) + 31) / 32;
     return g;
+}
+// SMs of the current device (152 on a GB300).
+inline int sm_count() {
+    static std::atomic<int> known[16];
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 16) return 152;
+    if ((n = known[dev].load(std::memory_order_relaxed))) return n;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) return 152;
+    known[dev].store(n, std::memory_order_relaxed);
+    return n;
 }
 // Records a failed CUDA call as the thread's last error.
 inline int fail_launch(cudaError_t e, const char *what) {

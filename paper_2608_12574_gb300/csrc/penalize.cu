@@ -26,6 +26,8 @@
 #include <stdint.h>
 #include <stdio.h>
 
+#include <algorithm>
+
 #include <cuda_runtime.h>
 
 #include "logits.cuh"
@@ -35,11 +37,12 @@ namespace tmk {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTable = 4096;             // entries of an edit CTA's table: 48 KB, four CTAs an SM
-constexpr int kTableBits = 12;
-constexpr int kShare = 2400;             // history tokens of one edit CTA: at most 0.6 of the table when all differ
+constexpr int kTableBits = 12;           // most entries of an edit CTA's table: 48 KB, four CTAs an SM
+constexpr int kLeastBits = 10;           // fewest: room for some hundred biases
+constexpr int kShare = 3000;             // history tokens of one edit CTA: at most 0.73 of the table when all differ
 constexpr int kProbes = 128;             // past this the table counts as full
-constexpr int kSegment = 8192;           // tokens of a fill CTA
+constexpr int kSegment = 16384;          // tokens filled at a time
+constexpr int kCtasPerSm = 4;
 constexpr uint32_t kNoToken = 0xFFFFFFFFu;
 // beside the count of an entry's occurrences in the output:
 constexpr uint32_t kPrompt = 0x80000000u;  // it is in the prompt
@@ -59,14 +62,20 @@ struct PenalizeArgs {
     const float *repetition, *presence, *frequency;
     const int32_t *bias_offsets, *bias_tokens;
     const float *bias_values;
-    int32_t shards;          // edit CTAs of a row
+    int32_t B, shards;       // edit CTAs of a row
+    int32_t bits;            // of the table's size
     Grammar g;
 };
 
 struct Table {
-    uint32_t token[kTable];
-    uint32_t entry[kTable];
-    float bias[kTable];
+    uint32_t *token, *entry;
+    float *bias;
+    int bits, size;
+    __device__ Table(unsigned char *smem, int bits_) : bits(bits_), size(1 << bits_) {
+        token = reinterpret_cast<uint32_t *>(smem);
+        entry = token + size;
+        bias = reinterpret_cast<float *>(entry + size);
+    }
 };
 
 __device__ __forceinline__ uint32_t mix(uint32_t t) {
@@ -77,24 +86,27 @@ __device__ __forceinline__ bool in_shard(const PenalizeArgs &a, uint32_t t, uint
     return a.shards == 1 || __umulhi(t * 0x85EBCA6Bu, uint32_t(a.shards)) == shard;
 }
 
-// The slot of token t, entered if it is not there; -1: the table is full.
-__device__ __forceinline__ int32_t slot_of(Table &table, uint32_t t) {
-    uint32_t at = (mix(t) * 0xC2B2AE35u) >> (32 - kTableBits);
+// The slot of token t, entered if it is not there; -1: the table is full. A slot
+// never changes once it holds a token, so one that is seen to hold t is t's:
+// frequent tokens then cost a read, not an atomic that all lanes queue for.
+__device__ __forceinline__ int32_t slot_of(const Table &table, uint32_t t) {
+    uint32_t at = (mix(t) * 0xC2B2AE35u) >> (32 - table.bits);
     for (int i = 0; i < kProbes; i++) {
-        const uint32_t old = atomicCAS(&table.token[at], kNoToken, t);
+        uint32_t old = *static_cast<volatile uint32_t *>(table.token + at);
+        if (old == kNoToken) old = atomicCAS(table.token + at, kNoToken, t);
         if (old == kNoToken || old == t) return int32_t(at);
-        at = (at + 1) & (kTable - 1);
+        at = (at + 1) & uint32_t(table.size - 1);
     }
     return -1;
 }
 
 // Enters the row's history and biases. `base` < 0: into the hash table (false
-// when it is full); else into the window of tokens base .. base + kTable - 1.
-__device__ bool enter(const PenalizeArgs &a, Table &table, int32_t b, uint32_t shard, int64_t base) {
+// when it is full); else into the window of tokens base .. base + table.size - 1.
+__device__ bool enter(const PenalizeArgs &a, const Table &table, int32_t b, uint32_t shard, int64_t base) {
     bool fits = true;
     auto find = [&](uint32_t t) -> int32_t {
         if (t >= uint32_t(a.V) || !in_shard(a, t, shard)) return -2;
-        if (base >= 0) return int64_t(t) >= base && int64_t(t) < base + kTable ? int32_t(int64_t(t) - base) : -2;
+        if (base >= 0) return int64_t(t) >= base && int64_t(t) < base + table.size ? int32_t(int64_t(t) - base) : -2;
         const int32_t at = slot_of(table, t);
         fits &= at >= 0;
         return at;
@@ -106,8 +118,8 @@ __device__ bool enter(const PenalizeArgs &a, Table &table, int32_t b, uint32_t s
         auto say = [&](int32_t i, uint32_t t) {
             const int32_t at = find(t);
             if (at < 0) return;
-            if (i >= prompt) atomicAdd(&table.entry[at], 1u);
-            else if (!(*reinterpret_cast<volatile uint32_t *>(&table.entry[at]) & kPrompt)) atomicOr(&table.entry[at], kPrompt);
+            if (i >= prompt) atomicAdd(table.entry + at, 1u);
+            else if (!(*static_cast<volatile uint32_t *>(table.entry + at) & kPrompt)) atomicOr(table.entry + at, kPrompt);
         };
         // to a 16-byte boundary, by fours, and the rest
         const int32_t head = min(len, int32_t((16 - (reinterpret_cast<uintptr_t>(h) & 15)) & 15) / 4);
@@ -128,7 +140,7 @@ __device__ bool enter(const PenalizeArgs &a, Table &table, int32_t b, uint32_t s
         for (int32_t i = lo + int32_t(threadIdx.x); i < hi && fits; i += kThreads) {
             const int32_t at = find(uint32_t(__ldg(a.bias_tokens + i)));
             if (at < 0) continue;
-            if (atomicOr(&table.entry[at], kBiased) & kBiased) atomicOr(&table.entry[at], kAgain);
+            if (atomicOr(table.entry + at, kBiased) & kBiased) atomicOr(table.entry + at, kAgain);
             else table.bias[at] = __ldg(a.bias_values + i);
         }
     }
@@ -161,14 +173,14 @@ __device__ __forceinline__ float penalized(float x, uint32_t entry, const Rates 
 
 // Writes the logits of the table's entries (base >= 0: a window's) and clears it.
 template <typename T>
-__device__ void write_entries(const PenalizeArgs &a, Table &table, int32_t b, T *logits, int64_t base) {
+__device__ void write_entries(const PenalizeArgs &a, const Table &table, int32_t b, T *logits, int64_t base) {
     Rates k;
     k.r = a.repetition ? __ldg(a.repetition + b) : 1.0f;
     k.p = a.presence ? __ldg(a.presence + b) : 0.0f;
     k.f = a.frequency ? __ldg(a.frequency + b) : 0.0f;
     const GrammarRow row = grammar_row(a.g, b);
-    constexpr int kBatch = 4;  // reads in flight a thread
-    for (int s0 = threadIdx.x; s0 < kTable; s0 += kBatch * kThreads) {
+    constexpr int kBatch = 4;  // reads in flight a thread; divides the smallest table / kThreads
+    for (int s0 = threadIdx.x; s0 < table.size; s0 += kBatch * kThreads) {
         uint32_t entry[kBatch];
         int32_t t[kBatch];
         float x[kBatch];
@@ -189,22 +201,22 @@ __device__ void write_entries(const PenalizeArgs &a, Table &table, int32_t b, T 
     }
 }
 
-__device__ __forceinline__ void clear(Table &table) {
-    for (int i = threadIdx.x; i < kTable / 4; i += kThreads) {
+__device__ __forceinline__ void clear(const Table &table) {
+    for (int i = threadIdx.x; i < table.size / 4; i += kThreads) {
         reinterpret_cast<uint4 *>(table.token)[i] = make_uint4(kNoToken, kNoToken, kNoToken, kNoToken);
         reinterpret_cast<uint4 *>(table.entry)[i] = make_uint4(0u, 0u, 0u, 0u);
     }
 }
 
 template <typename T>
-__device__ void edit_row(const PenalizeArgs &a, Table &table, int32_t b, uint32_t shard) {
+__device__ void edit_row(const PenalizeArgs &a, const Table &table, int32_t b, uint32_t shard) {
     T *logits = static_cast<T *>(a.logits) + b * a.stride;
     const bool fits = enter(a, table, b, shard, -1);
     if (__syncthreads_and(fits)) {
         write_entries(a, table, b, logits, -1);
         return;
     }
-    for (int64_t base = 0; base < a.V; base += kTable) {
+    for (int64_t base = 0; base < a.V; base += table.size) {
         clear(table);
         __syncthreads();
         enter(a, table, b, shard, base);
@@ -244,30 +256,30 @@ __device__ void fill_segment(const PenalizeArgs &a, int32_t b, int32_t v0, int32
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) k_penalize(PenalizeArgs a) {
+__global__ void __launch_bounds__(kThreads, kCtasPerSm) k_penalize(PenalizeArgs a) {
     extern __shared__ __align__(16) unsigned char dynamic_smem[];
-    Table &table = *reinterpret_cast<Table *>(dynamic_smem);
-    const int32_t b = blockIdx.y;
-    const bool edits = blockIdx.x < unsigned(a.shards);
-    if (edits) {
+    const Table table(dynamic_smem, a.bits);
+    const uint32_t edits = uint32_t(a.B) * uint32_t(a.shards);
+    if (blockIdx.x < edits) {
         clear(table);
         __syncthreads();
     }
     pdl_launch_dependents();
     pdl_wait();
-    if (edits) {
-        edit_row<T>(a, table, b, blockIdx.x);
-    } else {
-        const int32_t v0 = int32_t(blockIdx.x - unsigned(a.shards)) * kSegment;
-        fill_segment<T>(a, b, v0, v0 + min(kSegment, a.V - v0));
+    if (blockIdx.x < edits) {
+        edit_row<T>(a, table, int32_t(blockIdx.x / uint32_t(a.shards)), blockIdx.x % uint32_t(a.shards));
+        return;
+    }
+    const uint32_t segments = (uint32_t(a.V) + kSegment - 1) / kSegment;
+    for (uint64_t i = blockIdx.x - edits; i < uint64_t(a.B) * segments; i += gridDim.x - edits) {
+        const int32_t v0 = int32_t(i % segments) * kSegment;
+        fill_segment<T>(a, int32_t(i / segments), v0, v0 + min(kSegment, a.V - v0));
     }
 }
 
 template <typename T>
-cudaError_t launch_penalize(const PenalizeArgs &a, dim3 grid, cudaStream_t st) {
-    const cudaError_t e = cudaFuncSetAttribute(k_penalize<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(sizeof(Table)));
-    if (e != cudaSuccess) return e;
-    return launch_pdl_grid(k_penalize<T>, grid, kThreads, sizeof(Table), st, a);
+cudaError_t launch_penalize(const PenalizeArgs &a, int64_t grid, cudaStream_t st) {
+    return launch_pdl_smem(k_penalize<T>, grid, kThreads, size_t(12) << a.bits, st, a);
 }
 
 }  // namespace
@@ -310,11 +322,19 @@ extern "C" int trie_penalize(void *d_logits, int dtype, int64_t stride, int32_t 
     a.bias_values = d_bias_values;
     a.g = make_grammar(d_mask, mask_rows, d_states, V);
     const bool any = (d_history && max_length > 0) || d_bias_offsets;
+    a.B = B;
     a.shards = !any ? 0 : max_length > kShare ? (max_length + kShare - 1) / kShare : 1;
-    const dim3 grid(unsigned(a.shards) + (d_mask ? (unsigned(V) + kSegment - 1) / kSegment : 0u), unsigned(B));
-    if (grid.x == 0) return TRIE_OK;  // nothing applies
-    const cudaError_t e = dtype == TRIE_DTYPE_F32 ? launch_penalize<float>(a, grid, stream)
-                                                  : launch_penalize<__nv_bfloat16>(a, grid, stream);
+    a.bits = kLeastBits;
+    while (a.bits < kTableBits && (3 << a.bits) / 4 < max_length) a.bits++;
+    const int64_t edits = int64_t(B) * a.shards;
+    const int64_t segments = d_mask ? (int64_t(V) + kSegment - 1) / kSegment * B : 0;
+    // fill CTAs take the places that the edits leave of one round of CTAs, and half of one at least
+    const int64_t round = int64_t(sm_count()) * kCtasPerSm;
+    const int64_t fills = std::min(segments, std::max(round / 2, round - edits));
+    if (edits + fills == 0) return TRIE_OK;  // nothing applies
+    if (edits + fills > 0x7FFFFFFF) return set_error(TRIE_EINVAL, "B times max_length is too large");
+    const cudaError_t e = dtype == TRIE_DTYPE_F32 ? launch_penalize<float>(a, edits + fills, stream)
+                                                  : launch_penalize<__nv_bfloat16>(a, edits + fills, stream);
     if (e != cudaSuccess) return fail_launch(e, "penalize launch");
     return TRIE_OK;
 }

@@ -86,6 +86,8 @@ class TrieError(RuntimeError):
 def load_library(path: str = LIB_PATH):
     """Load libtriemask.so (raises if it has not been built)."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             if not os.path.exists(path):
@@ -547,35 +549,33 @@ def trie_destroy_async(h: Trie, stream=None) -> None:
 
 # ------------------------------------------- from hidden states to the token
 
-def _rows(t, dtypes, name: str) -> tuple[int, int]:
+# A decode step makes these calls with up to a dozen tensors each: one test of
+# what a good argument has, and the reason looked for only when it fails.
+def _rows(t, name: str) -> tuple[int, int]:
     """(address, elements between rows) of a 2-D CUDA tensor whose rows are contiguous and do not overlap."""
     import torch
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
-    if t.dtype not in dtypes:
-        raise TypeError(f"{name} must have dtype in {dtypes}, got {t.dtype}")
     n, m = t.shape
-    if (m > 1 and t.stride(1) != 1) or (n > 1 and t.stride(0) < m):
+    step, one = t.stride()
+    if (m > 1 and one != 1) or (n > 1 and step < m):
         raise ValueError(f"{name} must have contiguous rows that do not overlap")
-    return t.data_ptr(), t.stride(0) if n > 1 else m
+    return t.data_ptr(), step if n > 1 else m
 
 
-def _per_row(t, dtype, B: int, name: str, like):
-    """Address of an optional tensor with a value for each row of the batch."""
+def _vec(t, dtype, n: int, name: str, device: int):
+    """Address of an optional contiguous tensor of n values on a device."""
     if t is None:
         return None
-    if t.numel() != B:
-        raise ValueError(f"{name} must have B entries")
-    return _with(like, t, name, _dev(t, (dtype,), name))
+    if t.dtype is dtype and t.numel() == n and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
+    _dev(t, (dtype,), name)
+    if t.numel() != n:
+        raise ValueError(f"{name} must have B entries" if name != "bias offsets" else f"{name} must have B + 1 entries")
+    raise ValueError(f"{name} is on another device than the logits")
 
 
-def _with(like, t, name: str, p):
-    if t.get_device() != like.get_device():
-        raise ValueError(f"{name} is on another device than the logits")
-    return p
-
-
-def _grammar(mask, states, B: int, V: int, like):
+def _grammar(mask, states, B: int, V: int, device: int):
     """(mask, its rows, states) as the library takes them."""
     import torch
     if mask is None:
@@ -586,8 +586,8 @@ def _grammar(mask, states, B: int, V: int, like):
         raise ValueError("a mask without states")
     if mask.dim() != 2 or mask.shape[1] != mask_words(V):
         raise ValueError("mask must be [rows, ceil(V/32)]")
-    return (_with(like, mask, "mask", _dev(mask, (torch.int32,), "mask")), mask.shape[0],
-            _per_row(states, torch.int32, B, "states", like))
+    return (_vec(mask, torch.int32, mask.numel(), "mask", device), mask.shape[0],
+            _vec(states, torch.int32, B, "states", device))
 
 
 def _empty(shape, dtype, device, stream):
@@ -605,8 +605,7 @@ def _hidden(x, name: str):
         raise ValueError(f"{name} must be a matrix")
     if x.dtype not in (torch.float32, torch.bfloat16):
         raise TypeError(f"{name} must be float32 or bfloat16")
-    dtype = TRIE_DTYPE_BF16 if x.dtype is torch.bfloat16 else TRIE_DTYPE_F32
-    return (*_rows(x, (torch.float32, torch.bfloat16), name), dtype)
+    return (*_rows(x, name), TRIE_DTYPE_BF16 if x.dtype is torch.bfloat16 else TRIE_DTYPE_F32)
 
 
 def trie_head_quantize(x, stream=None):
@@ -649,13 +648,12 @@ def trie_head_logits(q, scales, w, w_scales, d_logits, mask=None, states=None, s
         raise ValueError("scales must be [ceil(D/128), M rounded up to a multiple of 4]")
     if w_scales.shape != ((V + 127) // 128, blocks):
         raise ValueError("w_scales must be [ceil(V/128), ceil(D/128)]")
-    p, stride = _rows(d_logits, (torch.float32, torch.bfloat16), "d_logits")
-    fp8, f32 = (torch.float8_e4m3fn,), (torch.float32,)
+    p, stride = _rows(d_logits, "d_logits")
+    dev, fp8, f32 = d_logits.get_device(), torch.float8_e4m3fn, torch.float32
     _check(load_library().trie_head_logits(
-        _with(d_logits, q, "q", _dev(q, fp8, "q")), _with(d_logits, scales, "scales", _dev(scales, f32, "scales")),
-        scales.shape[1], _with(d_logits, w, "w", _dev(w, fp8, "w")),
-        _with(d_logits, w_scales, "w_scales", _dev(w_scales, f32, "w_scales")), M, V, D, p, dtype, stride,
-        *_grammar(mask, states, M, V, d_logits), _stream_of(stream, d_logits)))
+        _vec(q, fp8, M * D, "q", dev), _vec(scales, f32, scales.numel(), "scales", dev), scales.shape[1],
+        _vec(w, fp8, V * D, "w", dev), _vec(w_scales, f32, w_scales.numel(), "w_scales", dev), M, V, D, p, dtype, stride,
+        *_grammar(mask, states, M, V, dev), _stream_of(stream, d_logits)))
 
 
 def trie_penalize(d_logits, history=None, length=None, prompt=None, repetition=None, presence=None, frequency=None,
@@ -665,35 +663,35 @@ def trie_penalize(d_logits, history=None, length=None, prompt=None, repetition=N
     import torch
     dtype = _logits_dtype(d_logits)
     B, V = d_logits.shape
-    p, stride = _rows(d_logits, (torch.float32, torch.bfloat16), "d_logits")
-    ph = h_stride = H = 0
+    p, stride = _rows(d_logits, "d_logits")
+    dev, i32, f32 = d_logits.get_device(), torch.int32, torch.float32
+    ph, h_stride, H = None, 0, 0
     if history is not None:
         if history.dim() != 2 or history.shape[0] != B:
             raise ValueError("history must be [B, H]")
         if length is None:
             raise ValueError("a history without its length")
+        if history.dtype is not i32 or history.get_device() != dev:
+            raise TypeError("history must be an int32 tensor on the logits' device")
         H = history.shape[1]
-        ph, h_stride = _rows(history, (torch.int32,), "history")
-        _with(d_logits, history, "history", ph)
+        ph, h_stride = _rows(history, "history")
     elif length is not None or prompt is not None:
         raise ValueError("length / prompt without a history")
     off = tok = val = None
     if bias is not None:
-        off, tok, val = bias
-        if off.numel() != B + 1 or tok.numel() != val.numel():
+        offsets, tokens, values = bias
+        n = tokens.numel()
+        if values.numel() != n:
             raise ValueError("bias must be (offsets [B+1], tokens [n], values [n])")
-        off = _with(d_logits, off, "bias offsets", _dev(off, (torch.int32,), "bias offsets"))
-        tok = _with(d_logits, tok, "bias tokens", _dev(tok, (torch.int32,), "bias tokens"))
-        val = _with(d_logits, val, "bias values", _dev(val, (torch.float32,), "bias values"))
-        if not bias[1].numel():
+        off = _vec(offsets, i32, B + 1, "bias offsets", dev)
+        tok, val = _vec(tokens, i32, n, "bias tokens", dev), _vec(values, f32, n, "bias values", dev)
+        if n == 0:
             off = None  # no entries
     _check(load_library().trie_penalize(
-        p, dtype, stride, B, V, ph if H else None, h_stride, H, _per_row(length, torch.int32, B, "length", d_logits),
-        _per_row(prompt, torch.int32, B, "prompt", d_logits),
-        _per_row(repetition, torch.float32, B, "repetition", d_logits),
-        _per_row(presence, torch.float32, B, "presence", d_logits),
-        _per_row(frequency, torch.float32, B, "frequency", d_logits), off, tok, val,
-        *_grammar(mask, states, B, V, d_logits), _stream_of(stream, d_logits)))
+        p, dtype, stride, B, V, ph if H else None, h_stride, H, _vec(length, i32, B, "length", dev),
+        _vec(prompt, i32, B, "prompt", dev), _vec(repetition, f32, B, "repetition", dev),
+        _vec(presence, f32, B, "presence", dev), _vec(frequency, f32, B, "frequency", dev), off, tok, val,
+        *_grammar(mask, states, B, V, dev), _stream_of(stream, d_logits)))
 
 
 def trie_sample(d_logits, seeds, temperature=None, top_k=None, top_p=None, min_p=None, mask=None, states=None,
@@ -705,25 +703,22 @@ def trie_sample(d_logits, seeds, temperature=None, top_k=None, top_p=None, min_p
     lib = load_library()
     dtype = _logits_dtype(d_logits)
     B, V = d_logits.shape
-    p, stride = _rows(d_logits, (torch.float32, torch.bfloat16), "d_logits")
+    p, stride = _rows(d_logits, "d_logits")
     if seeds is None:
         raise ValueError("seeds must be given")
-    dev = d_logits.device
-    tokens = _empty(B, torch.int32, dev, stream) if tokens is None else tokens
-    logprobs = _empty(B, torch.float32, dev, stream) if logprobs is None else logprobs
+    dev, i32, f32 = d_logits.get_device(), torch.int32, torch.float32
+    tokens = _empty(B, i32, d_logits.device, stream) if tokens is None else tokens
+    logprobs = _empty(B, f32, d_logits.device, stream) if logprobs is None else logprobs
     need = lib.trie_sample_workspace(B, V)
     if workspace is None:
-        workspace = _empty(max(need, 0), torch.uint8, dev, stream)
+        workspace = _empty(max(need, 0), torch.uint8, d_logits.device, stream)
     elif workspace.numel() * workspace.element_size() < need:
         raise ValueError(f"workspace must have at least {need} bytes")
     _check(lib.trie_sample(
-        p, dtype, stride, B, V, _per_row(seeds, torch.int64, B, "seeds", d_logits),
-        _per_row(temperature, torch.float32, B, "temperature", d_logits),
-        _per_row(top_k, torch.int32, B, "top_k", d_logits), _per_row(top_p, torch.float32, B, "top_p", d_logits),
-        _per_row(min_p, torch.float32, B, "min_p", d_logits), *_grammar(mask, states, B, V, d_logits),
-        _with(d_logits, workspace, "workspace", _dev(workspace, (workspace.dtype,), "workspace")),
-        _per_row(tokens, torch.int32, B, "tokens", d_logits),
-        _per_row(logprobs, torch.float32, B, "logprobs", d_logits), _stream_of(stream, d_logits)))
+        p, dtype, stride, B, V, _vec(seeds, torch.int64, B, "seeds", dev), _vec(temperature, f32, B, "temperature", dev),
+        _vec(top_k, i32, B, "top_k", dev), _vec(top_p, f32, B, "top_p", dev), _vec(min_p, f32, B, "min_p", dev),
+        *_grammar(mask, states, B, V, dev), _vec(workspace, workspace.dtype, workspace.numel(), "workspace", dev),
+        _vec(tokens, i32, B, "tokens", dev), _vec(logprobs, f32, B, "logprobs", dev), _stream_of(stream, d_logits)))
     return tokens, logprobs
 
 
