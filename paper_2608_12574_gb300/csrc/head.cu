@@ -15,6 +15,8 @@
 #include <stdint.h>
 #include <stdio.h>
 
+#include <algorithm>
+
 #include <cuda_fp8.h>
 #include <cuda_runtime.h>
 
@@ -98,21 +100,28 @@ __global__ void __launch_bounds__(kQuantThreads) k_head_quantize_weight(const T 
 
 // ---- the product
 //
-// The weights are the MMA's rows (128 tokens a tile) and the batch its columns:
-// a full tile whatever the batch, and a token's weight scale is the whole
-// tile's. A CTA computes one tile of 128 tokens by up to 256 rows of the batch:
-// one thread streams blocks of 128 columns of K of both operands (and the rows'
-// scales of that block) into a ring of stages by TMA, one issues the four MMAs
-// of a block into one of several accumulators in tensor memory, and the
-// epilogue warps read each block's sums out and add them, scaled, to sums in
-// registers: a thread holds one token and up to 64 rows.
+// A tile is up to 128 rows of the batch, the MMA's rows, by NT tokens, its
+// columns; a thread of the epilogue then holds one row, and the scale of a
+// block is one number for it and 64 tokens (a weight scale covers 128). One
+// thread streams blocks of 128 columns of K of both operands into a ring of
+// stages by TMA, one issues a block's four MMAs into one of two accumulators in
+// tensor memory, and the epilogue warps read each block's sums out and add
+// them, scaled, to sums in registers, a warp 32 rows by 64 tokens. Rows that a
+// batch does not have are not loaded (the MMA multiplies what lies there into
+// rows nobody reads), and warps that would have only such rows do nothing.
+constexpr int kRows = 128;
+constexpr int kColumns = 64;       // tokens of an epilogue warp
+constexpr int kMaxStages = 8;
+
 struct HeadArgs {
     CUtensorMap map_w, map_q;
     const float *s;        // [blocks][pitch]
     int64_t pitch;
     const float *ws;       // [ceil(V / 128)][blocks]
     int32_t M, V, blocks;
-    int32_t m_tiles, n;    // the batch in m_tiles tiles of n rows (a multiple of 16)
+    int32_t m_tiles;       // tiles of kRows rows
+    int32_t box_rows;      // rows of a tile that are loaded
+    int32_t stages;        // of the ring
     void *logits;
     int64_t stride;
     Grammar g;
@@ -120,29 +129,63 @@ struct HeadArgs {
 
 template <int NT>
 struct HeadShape {
-    static constexpr int kColumns = NT < 64 ? NT : 64;        // columns of an epilogue warp
-    static constexpr int kEpilogue = 4 * (NT / kColumns);     // warps
+    static constexpr int kEpilogue = 4 * (NT / kColumns);  // warps
     static constexpr int kThreads = 64 + 32 * kEpilogue;
-    static constexpr int kAccumulators = NT <= 64 ? 4 : 2;
-    static constexpr int kTmem = NT * kAccumulators < 32 ? 32 : NT * kAccumulators;
-    static constexpr int kCtas = NT <= 128 ? 2 : 1;           // of an SM
-    static constexpr int kStageBytes = (kBlock + NT) * kBlock + 1024;  // weights, rows, scales
-    static constexpr int kStages = (kCtas == 2 ? 112 : 224) * 1024 / kStageBytes;
-    static constexpr int kSmem = kStages * kStageBytes + 1024;         // and room to align
+    static constexpr int kCtas = NT == 128 ? 2 : 1;        // of an SM
+    static constexpr int kTmem = 2 * NT;
+    static constexpr int kBudget = (kCtas == 2 ? 111 : 222) * 1024;  // bytes of shared memory
+    static constexpr int kWeightBytes = NT * kBlock;
 };
 
-// Writes -inf to rows [m0, m1) of tokens [v0, v1) (at most 128), by all threads.
+// Writes -inf to rows [m0, m1) of tokens [v0, v1) (at most 256), by all threads.
 template <typename T>
 __device__ void fill_tile(const HeadArgs &a, int32_t m0, int32_t m1, int32_t v0, int32_t v1) {
     const int lane = threadIdx.x & 31;
     const T none = from_f32<T>(-INFINITY);
     for (int32_t m = m0 + int32_t(threadIdx.x >> 5); m < m1; m += int32_t(blockDim.x >> 5)) {
         T *out = static_cast<T *>(a.logits) + m * a.stride + v0;
-        if (v1 - v0 == kBlock && (reinterpret_cast<uintptr_t>(out) & (4 * sizeof(T) - 1)) == 0) {
-            if (sizeof(T) == 2) reinterpret_cast<uint2 *>(out)[lane] = make_uint2(0xFF80FF80u, 0xFF80FF80u);
-            else reinterpret_cast<uint4 *>(out)[lane] = make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u);
+        if ((v1 - v0) % 128 == 0 && (reinterpret_cast<uintptr_t>(out) & (4 * sizeof(T) - 1)) == 0) {
+            for (int32_t i = lane; i < (v1 - v0) / 4; i += 32) {
+                if (sizeof(T) == 2) reinterpret_cast<uint2 *>(out)[i] = make_uint2(0xFF80FF80u, 0xFF80FF80u);
+                else reinterpret_cast<uint4 *>(out)[i] = make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u);
+            }
         } else {
             for (int32_t i = lane; i < v1 - v0; i += 32) out[i] = none;
+        }
+    }
+}
+
+// A warp's 32 rows x 64 tokens of sums to memory: turned in shared memory
+// (`turn`: 32 rows of 64 values and 4 bytes, so that neither side has bank
+// conflicts), so that a row's tokens are written side by side.
+template <typename T>
+__device__ __forceinline__ void store_block(const HeadArgs &a, unsigned char *turn, const uint64_t (&sum)[kColumns / 2],
+                                            int32_t m, int32_t m1, int32_t v, int lane) {
+    constexpr int kPitch = kColumns * int(sizeof(T)) / 4 + 1;  // words
+    uint32_t *mine = reinterpret_cast<uint32_t *>(turn) + lane * kPitch;
+#pragma unroll
+    for (int i = 0; i < kColumns / 2; i++) {
+        float lo, hi;
+        unpack2(sum[i], lo, hi);
+        if (sizeof(T) == 2) {
+            const __nv_bfloat162 both = __floats2bfloat162_rn(lo, hi);
+            mine[i] = *reinterpret_cast<const uint32_t *>(&both);
+        } else {
+            mine[2 * i] = __float_as_uint(lo);
+            mine[2 * i + 1] = __float_as_uint(hi);
+        }
+    }
+    __syncwarp();
+    const int32_t rows = min(32, m1 - m), left = a.V - v;  // of this warp, of its tokens
+    T *out = static_cast<T *>(a.logits) + m * a.stride + v;
+    if (sizeof(T) == 2 && left >= kColumns && (reinterpret_cast<uintptr_t>(out) & 3) == 0 && (a.stride & 1) == 0) {
+        for (int32_t r = 0; r < rows; r++)
+            reinterpret_cast<uint32_t *>(out + r * a.stride)[lane] = reinterpret_cast<uint32_t *>(turn)[r * kPitch + lane];
+    } else {
+        for (int32_t r = 0; r < rows; r++) {
+            const T *from = reinterpret_cast<const T *>(reinterpret_cast<uint32_t *>(turn) + r * kPitch);
+            if (lane < left) out[r * a.stride + lane] = from[lane];
+            if (lane + 32 < left) out[r * a.stride + lane + 32] = from[lane + 32];
         }
     }
 }
@@ -151,24 +194,26 @@ template <typename T, int NT>
 __global__ void __launch_bounds__(HeadShape<NT>::kThreads, HeadShape<NT>::kCtas) k_head_logits(const __grid_constant__ HeadArgs a) {
     using S = HeadShape<NT>;
     extern __shared__ unsigned char dynamic_smem[];
-    __shared__ uint64_t bars[2 * S::kStages + 2 * S::kAccumulators];
+    __shared__ uint64_t bars[2 * kMaxStages + 4];
     __shared__ uint32_t tmem_base;
     __shared__ int gave_up;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int32_t vt = int32_t(blockIdx.x / unsigned(a.m_tiles)), v0 = vt * kBlock;
-    const int32_t m0 = int32_t(blockIdx.x % unsigned(a.m_tiles)) * a.n, m1 = min(a.M, m0 + a.n);
-    const uint32_t full = smem_addr(bars), empty = full + 8 * S::kStages;
-    const uint32_t ready = empty + 8 * S::kStages, drained = ready + 8 * S::kAccumulators;
-    const uint32_t stages = (smem_addr(dynamic_smem) + 1023u) & ~1023u;
+    const int32_t vt = int32_t(blockIdx.x / unsigned(a.m_tiles)), v0 = vt * NT;
+    const int32_t m0 = int32_t(blockIdx.x % unsigned(a.m_tiles)) * kRows, m1 = min(a.M, m0 + kRows);
+    const int quarters = (m1 - m0 + 31) / 32;  // warps' rows that there are
+    const uint32_t full = smem_addr(bars), empty = full + 8 * kMaxStages;
+    const uint32_t ready = empty + 8 * kMaxStages, drained = ready + 16;
+    unsigned char *ring = dynamic_smem + ((1024u - (smem_addr(dynamic_smem) & 1023u)) & 1023u);
+    const uint32_t stages = smem_addr(ring), stage_bytes = uint32_t(S::kWeightBytes + a.box_rows * kBlock);
     if (threadIdx.x == 0) {
         gave_up = 0;
-        for (int i = 0; i < S::kStages; i++) {
+        for (int i = 0; i < a.stages; i++) {
             bar_init(full + 8 * i, 1);
-            bar_init(empty + 8 * i, 1 + S::kEpilogue);  // the MMAs have read it, and each epilogue warp its scales
+            bar_init(empty + 8 * i, 1);
         }
-        for (int i = 0; i < S::kAccumulators; i++) {
+        for (int i = 0; i < 2; i++) {
             bar_init(ready + 8 * i, 1);
-            bar_init(drained + 8 * i, S::kEpilogue);
+            bar_init(drained + 8 * i, uint32_t(quarters * (NT / kColumns)));
         }
         bar_init_fence();
         tma_prefetch_map(&a.map_w);
@@ -179,13 +224,13 @@ __global__ void __launch_bounds__(HeadShape<NT>::kThreads, HeadShape<NT>::kCtas)
     if (a.g.mask) {
         // a tile that no row of the batch allows a token of needs no weights
         bool any = false;
-        const int32_t w0 = v0 >> 5, words = min(4, int32_t(a.g.W) - w0);
+        const int32_t w0 = v0 >> 5, words = min(NT / 32, int32_t(a.g.W) - w0);
         for (int32_t m = m0 + int32_t(threadIdx.x); m < m1 && !any; m += int32_t(blockDim.x)) {
             const GrammarRow row = grammar_row(a.g, m);
             for (int32_t i = 0; i < words; i++) any |= row.word(w0 + i) != 0u;
         }
         if (!__syncthreads_or(any)) {
-            fill_tile<T>(a, m0, m1, v0, min(a.V, v0 + kBlock));
+            fill_tile<T>(a, m0, m1, v0, min(a.V, v0 + NT));
             return;
         }
     }
@@ -197,96 +242,98 @@ __global__ void __launch_bounds__(HeadShape<NT>::kThreads, HeadShape<NT>::kCtas)
 
     if (warp == 0) {
         if (lane == 0) {
-            const uint32_t scale_bytes = uint32_t(min(int64_t(a.n), a.pitch - m0)) * 4;
             int32_t kb = 0;
+            int stage = 0;
+            uint32_t phase = 1;  // of the stage's last use: the first time round there is none
             for (; kb < a.blocks; kb++) {
-                const int stage = kb % S::kStages;
-                if (kb >= S::kStages && !bar_wait(empty + 8 * stage, (kb / S::kStages - 1) & 1, &gave_up)) break;
-                const uint32_t at = stages + stage * S::kStageBytes, bar = full + 8 * stage;
-                bar_expect(bar, uint32_t(kBlock + a.n) * kBlock + scale_bytes);
+                const uint32_t at = stages + uint32_t(stage) * stage_bytes, bar = full + 8 * stage;
+                if (!bar_wait(empty + 8 * stage, phase, &gave_up)) break;
+                bar_expect(bar, stage_bytes);
                 tma_load_2d(at, &a.map_w, kb * kBlock, v0, bar);
-                tma_load_2d(at + kBlock * kBlock, &a.map_q, kb * kBlock, m0, bar);
-                bulk_load(at + (kBlock + NT) * kBlock, a.s + kb * a.pitch + m0, scale_bytes, bar);
+                tma_load_2d(at + S::kWeightBytes, &a.map_q, kb * kBlock, m0, bar);
+                if (++stage == a.stages) stage = 0, phase ^= 1;
             }
-            if (gave_up) {  // copies still write to shared memory: wait for them
+            if (gave_up) {  // copies may still write to shared memory: wait for them
                 int none = 0;
-                for (int32_t i = max(0, kb - S::kStages); i < kb; i++) bar_wait(full + 8 * (i % S::kStages), (i / S::kStages) & 1, &none);
+                for (int32_t i = max(0, kb - a.stages); i < kb; i++)
+                    bar_wait(full + 8 * (i % a.stages), (i / a.stages) & 1, &none);
             }
         }
     } else if (warp == 1) {
         if (lane == 0) {
-            const uint32_t idesc = mma_idesc_e4m3(kBlock, uint32_t(a.n));
+            constexpr uint32_t idesc = mma_idesc_e4m3(kRows, NT);
+            int stage = 0;
+            uint32_t phase = 0;
             for (int32_t kb = 0; kb < a.blocks; kb++) {
-                const int stage = kb % S::kStages, acc = kb % S::kAccumulators;
-                if (kb >= S::kAccumulators && !bar_wait(drained + 8 * acc, (kb / S::kAccumulators - 1) & 1, &gave_up)) break;
-                if (!bar_wait(full + 8 * stage, (kb / S::kStages) & 1, &gave_up)) break;
+                const int acc = kb & 1;
+                if (!bar_wait(drained + 8 * acc, ((kb >> 1) & 1) ^ 1, &gave_up)) break;
+                if (!bar_wait(full + 8 * stage, phase, &gave_up)) break;
                 tcgen05_fence_after();
-                const uint32_t at = stages + stage * S::kStageBytes;
-                const uint64_t da = mma_desc(at), db = mma_desc(at + kBlock * kBlock);
+                const uint32_t at = stages + uint32_t(stage) * stage_bytes;
+                const uint64_t dw = mma_desc(at), dq = mma_desc(at + S::kWeightBytes);
 #pragma unroll
-                for (int k = 0; k < kBlock / 32; k++) mma_e4m3(tmem + acc * NT, da + 2 * k, db + 2 * k, idesc, k > 0);
+                for (int k = 0; k < kBlock / 32; k++) mma_e4m3(tmem + acc * NT, dq + 2 * k, dw + 2 * k, idesc, k > 0);
                 mma_commit(empty + 8 * stage);
                 mma_commit(ready + 8 * acc);
+                if (++stage == a.stages) stage = 0, phase ^= 1;
             }
         }
-    } else {
-        const int quarter = warp & 3, column = (warp - 2) / 4 * S::kColumns;
-        const uint32_t lanes = uint32_t(quarter * 32) << 16;
-        uint64_t sum[S::kColumns / 2];
+    } else if ((warp & 3) < quarters) {
+        const int quarter = warp & 3, column = (warp - 2) / 4 * kColumns;
+        const uint32_t from = tmem + (uint32_t(quarter * 32) << 16) + uint32_t(column);
+        const int32_t row = min(m0 + quarter * 32 + lane, a.M - 1), v = v0 + column;
+        uint64_t sum[kColumns / 2];
 #pragma unroll
-        for (int i = 0; i < S::kColumns / 2; i++) sum[i] = 0ull;
+        for (int i = 0; i < kColumns / 2; i++) sum[i] = 0ull;
         bool ok = true;
-        const float *ws = a.ws + int64_t(vt) * a.blocks;
-        for (int32_t kb = 0; kb < a.blocks && ok; kb++) {
-            const int stage = kb % S::kStages, acc = kb % S::kAccumulators;
-            const float w = __ldg(ws + kb);
-            const uint64_t w2 = pack2(w, w);
-            ok = bar_wait(full + 8 * stage, (kb / S::kStages) & 1, &gave_up) &&
-                 bar_wait(ready + 8 * acc, (kb / S::kAccumulators) & 1, &gave_up);
-            ok = __all_sync(~0u, ok);
+        // scales are read two blocks ahead
+        const float *sp = a.s + row, *wp = a.ws + int64_t(min(v, a.V - 1) / kBlock) * a.blocks;
+        float s0 = __ldg(sp) * __ldg(wp), s1 = 0.0f;
+        if (a.blocks > 1) s1 = __ldg(sp + a.pitch) * __ldg(wp + 1);
+        for (int32_t kb = 0; kb < a.blocks; kb++) {
+            const int acc = kb & 1;
+            const uint64_t scale = pack2(s0, s0);
+            s0 = s1;
+            if (kb + 2 < a.blocks) s1 = __ldg(sp + (kb + 2) * a.pitch) * __ldg(wp + kb + 2);
+            ok = __all_sync(~0u, bar_wait(ready + 8 * acc, (kb >> 1) & 1, &gave_up));
             if (!ok) break;
             tcgen05_fence_after();
-            const uint32_t scales = stages + stage * S::kStageBytes + (kBlock + NT) * kBlock + column * 4;
 #pragma unroll
-            for (int c = 0; c < S::kColumns; c += 16) {
+            for (int c = 0; c < kColumns; c += 16) {
                 uint32_t r[16];
-                tmem_load16(tmem + lanes + acc * NT + column + c, r);
+                tmem_load16(from + acc * NT + c, r);
                 tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 16; i += 4) {
-                    uint64_t s0, s1;
-                    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(s0), "=l"(s1) : "r"(scales + (c + i) * 4));
-                    sum[(c + i) / 2] = fma2(pack2u(r[i], r[i + 1]), mul2(s0, w2), sum[(c + i) / 2]);
-                    sum[(c + i) / 2 + 1] = fma2(pack2u(r[i + 2], r[i + 3]), mul2(s1, w2), sum[(c + i) / 2 + 1]);
-                }
+                for (int i = 0; i < 16; i += 2) sum[(c + i) / 2] = fma2(pack2u(r[i], r[i + 1]), scale, sum[(c + i) / 2]);
             }
             tcgen05_fence_before();
             __syncwarp();
-            if (lane == 0) {
-                bar_arrive(drained + 8 * acc);
-                bar_arrive(empty + 8 * stage);
-            }
+            if (lane == 0) bar_arrive(drained + 8 * acc);
         }
         // a tile that gave up waiting has no result: NaN
-        const int32_t v = v0 + quarter * 32 + lane;
-        uint32_t allow[(S::kColumns + 31) / 32];
+        if (!ok) {
 #pragma unroll
-        for (int i = 0; i < (S::kColumns + 31) / 32; i++) {
-            const int32_t m = m0 + column + i * 32 + lane;
-            allow[i] = a.g.mask && m < m1 && (v0 >> 5) + quarter < a.g.W ? grammar_row(a.g, m).word((v0 >> 5) + quarter) : ~0u;
+            for (int i = 0; i < kColumns / 2; i++) sum[i] = 0x7FFFFFFF7FFFFFFFull;
         }
-        T *out = static_cast<T *>(a.logits) + v;
+        if (a.g.mask) {
+            const GrammarRow allow = grammar_row(a.g, row);
 #pragma unroll
-        for (int i = 0; i < S::kColumns; i++) {
-            const uint32_t word = __shfl_sync(~0u, allow[i / 32], i & 31);
-            const int32_t m = m0 + column + i;
-            float lo, hi;
-            unpack2(sum[i / 2], lo, hi);
-            float x = i & 1 ? hi : lo;
-            if (!ok) x = __int_as_float(0x7FFFFFFF);
-            if (!((word >> lane) & 1u)) x = -INFINITY;
-            if (m < m1 && v < a.V) out[m * a.stride] = from_f32<T>(x);
+            for (int c = 0; c < kColumns; c += 32) {
+                const uint32_t word = (v + c) >> 5 < a.g.W ? allow.word((v + c) >> 5) : 0u;
+                if (word == ~0u) continue;
+#pragma unroll
+                for (int i = 0; i < 32; i += 2) {
+                    float lo, hi;
+                    unpack2(sum[(c + i) / 2], lo, hi);
+                    if (!((word >> i) & 1u)) lo = -INFINITY;
+                    if (!((word >> (i + 1)) & 1u)) hi = -INFINITY;
+                    sum[(c + i) / 2] = pack2(lo, hi);
+                }
+            }
         }
+        // every MMA is done (the last `ready`), so the ring is free to turn the block in
+        if (ok && v < a.V)
+            store_block<T>(a, ring + (warp - 2) * 32 * (kColumns * int(sizeof(T)) + 4), sum, m0 + quarter * 32, m1, v, lane);
     }
     __syncwarp();
     tcgen05_fence_before();
@@ -319,20 +366,17 @@ bool make_map(CUtensorMap *map, const void *base, int64_t rows, int32_t D, int32
 }
 
 template <typename T, int NT>
-cudaError_t launch_head(const HeadArgs &a, int64_t grid, cudaStream_t st) {
+cudaError_t launch_head(HeadArgs a, int64_t grid, cudaStream_t st) {
     using S = HeadShape<NT>;
-    const cudaError_t e = cudaFuncSetAttribute(k_head_logits<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+    const int stage = S::kWeightBytes + a.box_rows * kBlock;
+    // the last stage's MMA reads kRows rows, whatever was loaded; and room to align the ring
+    const int beyond = (kRows - a.box_rows) * kBlock + 1024;
+    a.stages = std::min(kMaxStages, (S::kBudget - beyond) / stage);
+    const int turn = S::kEpilogue * 32 * (kColumns * int(sizeof(T)) + 4) + 1024;
+    const int smem = std::max(a.stages * stage + beyond, turn);
+    const cudaError_t e = cudaFuncSetAttribute(k_head_logits<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBudget);
     if (e != cudaSuccess) return e;
-    return launch_pdl_smem(k_head_logits<T, NT>, grid, S::kThreads, S::kSmem, st, a);
-}
-
-template <typename T>
-cudaError_t launch_head_type(const HeadArgs &a, int64_t grid, cudaStream_t st) {
-    if (a.n <= 16) return launch_head<T, 16>(a, grid, st);
-    if (a.n <= 32) return launch_head<T, 32>(a, grid, st);
-    if (a.n <= 64) return launch_head<T, 64>(a, grid, st);
-    if (a.n <= 128) return launch_head<T, 128>(a, grid, st);
-    return launch_head<T, 256>(a, grid, st);
+    return launch_pdl_smem(k_head_logits<T, NT>, grid, S::kThreads, smem, st, a);
 }
 
 const char *check_quantize(const void *x, int dtype, int64_t stride, int32_t rows, int32_t D, const void *q,
@@ -409,17 +453,19 @@ extern "C" int trie_head_logits(const uint8_t *d_q, const float *d_scales, int64
     a.M = M;
     a.V = V;
     a.blocks = (D + kBlock - 1) / kBlock;
-    a.m_tiles = (M + 255) / 256;
-    a.n = ((M + a.m_tiles - 1) / a.m_tiles + 15) / 16 * 16;
+    a.m_tiles = (M + kRows - 1) / kRows;
+    a.box_rows = std::min(kRows, (M + 7) / 8 * 8);
     a.logits = d_logits;
     a.stride = stride;
     a.g = make_grammar(d_mask, mask_rows, d_states, V);
-    if (!make_map(&a.map_w, d_w, V, D, kBlock) || !make_map(&a.map_q, d_q, M, D, a.n))
+    const int nt = M <= 64 ? 128 : 256;
+    if (!make_map(&a.map_w, d_w, V, D, nt) || !make_map(&a.map_q, d_q, M, D, a.box_rows))
         return set_error(TRIE_ECUDA, "cuTensorMapEncodeTiled failed");
-    const int64_t grid = (int64_t(V) + kBlock - 1) / kBlock * a.m_tiles;
+    const int64_t grid = (int64_t(V) + nt - 1) / nt * a.m_tiles;
     if (grid > 0x7FFFFFFF) return set_error(TRIE_EINVAL, "M x V is too large");
-    const cudaError_t e = dtype == TRIE_DTYPE_F32 ? launch_head_type<float>(a, grid, stream)
-                                                  : launch_head_type<__nv_bfloat16>(a, grid, stream);
+    const bool f32 = dtype == TRIE_DTYPE_F32;
+    const cudaError_t e = nt == 128 ? (f32 ? launch_head<float, 128>(a, grid, stream) : launch_head<__nv_bfloat16, 128>(a, grid, stream))
+                                    : (f32 ? launch_head<float, 256>(a, grid, stream) : launch_head<__nv_bfloat16, 256>(a, grid, stream));
     if (e != cudaSuccess) return fail_launch(e, "head launch");
     return TRIE_OK;
 }
