@@ -513,16 +513,25 @@ int trie_head_quantize(const void *d_x, int dtype, int64_t stride, int32_t M, in
 int trie_head_quantize_weight(const void *d_w, int dtype, int64_t stride, int32_t V, int32_t D, uint8_t *d_q,
                               float *d_scales, cudaStream_t stream);
 
+/* Bytes of device memory that trie_head_logits needs for its own use with a
+ * grammar (-1 for sizes out of range). What it holds between calls does not
+ * matter; calls that may run at the same time need one each. */
+int64_t trie_head_workspace(int32_t M, int32_t V);
+
 /* logits = x W^T of quantized hidden states and weights, under a grammar:
  * logits[m][v] = sum over blocks kb of scales[kb][m] w_scales[v/128][kb] times
  * the sum of q[m][k] w[v][k] over the block, and -inf where row m's state does
  * not allow v. Sums are kept in 32 bits and rounded once to the logits' type.
  * Weights of 128 consecutive tokens that no row of the batch allows are not
- * read. D a multiple of 16; d_q, d_w and d_scales 16-byte aligned; M <= 2^20. */
+ * read, and of rows that allow few tokens only those tokens' are, unless a row
+ * nearby is free. D a multiple of 16; d_q, d_w and d_scales 16-byte aligned;
+ * M <= 2^20.
+ *   d_workspace  device, trie_head_workspace(M, V) bytes, 16-byte aligned; may
+ *                be NULL without a mask */
 int trie_head_logits(const uint8_t *d_q, const float *d_scales, int64_t pitch, const uint8_t *d_w,
                      const float *d_w_scales, int32_t M, int32_t V, int32_t D, void *d_logits, int dtype,
                      int64_t stride, const uint32_t *d_mask, int32_t mask_rows, const int32_t *d_states,
-                     cudaStream_t stream);
+                     void *d_workspace, cudaStream_t stream);
 
 /* Penalties, biases and the grammar on a batch of logits, in place. For token t
  * of a row, with c(t) its occurrences after the prompt:

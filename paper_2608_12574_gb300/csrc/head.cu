@@ -10,6 +10,7 @@
 //
 //  k_head_quantize         a warp per row and block of 128 columns.
 //  k_head_quantize_weight  a CTA per block of 128 x 128.
+//  k_head_rows             with a grammar: the logits of rows that allow few tokens.
 //  k_head_logits           the product on the tensor cores.
 #include <math.h>
 #include <stdint.h>
@@ -100,246 +101,455 @@ __global__ void __launch_bounds__(kQuantThreads) k_head_quantize_weight(const T 
 
 // ---- the product
 //
-// A tile is up to 128 rows of the batch, the MMA's rows, by NT tokens, its
-// columns; a thread of the epilogue then holds one row, and the scale of a
-// block is one number for it and 64 tokens (a weight scale covers 128). One
-// thread streams blocks of 128 columns of K of both operands into a ring of
-// stages by TMA, one issues a block's four MMAs into one of two accumulators in
-// tensor memory, and the epilogue warps read each block's sums out and add
-// them, scaled, to sums in registers, a warp 32 rows by 64 tokens. Rows that a
-// batch does not have are not loaded (the MMA multiplies what lies there into
-// rows nobody reads), and warps that would have only such rows do nothing.
-constexpr int kRows = 128;
-constexpr int kColumns = 64;       // tokens of an epilogue warp
+// A tile is 128 rows of the batch, the MMA's rows, by 128 tokens, its columns,
+// on one CTA; or, for more than 128 rows, 256 by 256 on a pair of CTAs, whose
+// MMA reads each CTA's half of either operand, so that a CTA loads 32 KB for
+// twice the products (what limits larger batches is the 64 bytes a cycle that
+// an SM takes in). Either way a thread of the epilogue holds one row, and the
+// scale of a block is one number for it and the 64 or 128 tokens that it has.
+// CTAs stay and go over the tiles: one thread streams blocks of 128 columns of
+// K of both operands into a ring of stages by TMA, one issues a block's four
+// MMAs into one of several accumulators in tensor memory, and the epilogue
+// warps read each block's sums out and add them, scaled, to sums in registers,
+// so that the next tile's weights arrive while this one's logits are written.
+// Rows that a batch does not have are not loaded (the MMA multiplies what lies
+// there into rows nobody reads).
+constexpr int kRows = 128;         // of a CTA's tile
 constexpr int kMaxStages = 8;
+constexpr int kColumns = 64;       // tokens of an epilogue warp
+constexpr int kHeadSmem = 226 * 1024;
+constexpr int kFewMaxD = 32768;    // longest hidden state whose row fits k_head_rows' shared memory
+constexpr int kNeedTiles = 2048;   // tiles of a CTA whose need is looked up ahead
+constexpr int kScaleSlots = 16;    // more than the blocks that can be between the copies and the epilogue
+constexpr int kTurn = 32 * 17;     // words of a warp's block of 16 tokens, turned
 
 struct HeadArgs {
     CUtensorMap map_w, map_q;
+    const uint8_t *q, *w;  // [M][D], [V][D]
     const float *s;        // [blocks][pitch]
     int64_t pitch;
     const float *ws;       // [ceil(V / 128)][blocks]
-    int32_t M, V, blocks;
-    int32_t m_tiles;       // tiles of kRows rows
-    int32_t box_rows;      // rows of a tile that are loaded
+    int32_t M, V, D, blocks;
+    int32_t m_tiles;       // of 128 rows (a pair: 256)
+    int32_t tiles;
+    int32_t box_rows;      // rows of a CTA's tile that are loaded
     int32_t stages;        // of the ring
     void *logits;
     int64_t stride;
     Grammar g;
+    // with a grammar, of each row (k_head_rows):
+    int32_t *count;        // [M] its allowed tokens where they are few (listed, logits computed), else -1
+    uint32_t *used;        // [M][used_words] bit i: it allows one of tokens 128 i .. 128 i + 127
+    int32_t *token;        // [M][kFew] the list
+    float *value;          // [M][kFew] their logits
+    int32_t used_words;
 };
 
-template <int NT>
-struct HeadShape {
-    static constexpr int kEpilogue = 4 * (NT / kColumns);  // warps
-    static constexpr int kThreads = 64 + 32 * kEpilogue;
-    static constexpr int kCtas = NT == 128 ? 2 : 1;        // of an SM
-    static constexpr int kTmem = 2 * NT;
-    static constexpr int kBudget = (kCtas == 2 ? 111 : 222) * 1024;  // bytes of shared memory
-    static constexpr int kWeightBytes = NT * kBlock;
-};
+// ---- rows that allow few tokens
+//
+// A trie's nodes allow a handful of tokens, so a constrained row's logits are a
+// few dot products of its hidden state with rows of the weights that are
+// scattered over the vocabulary: reading whole tiles of weights for them would
+// cost hundreds of times more. A CTA per row counts the row's allowed tokens;
+// where they are at most kFew (and the batch has no free row nearby, whose
+// tiles are multiplied anyway) it lists them and computes their logits, a warp
+// a token, which the tiles' kernel then writes into its -inf.
+constexpr int kFew = 256;
+constexpr int kNear = 256;         // rows among which one free row makes all dense
+constexpr int kRowThreads = 256;
 
-// Writes -inf to rows [m0, m1) of tokens [v0, v1) (at most 256), by all threads.
-template <typename T>
-__device__ void fill_tile(const HeadArgs &a, int32_t m0, int32_t m1, int32_t v0, int32_t v1) {
-    const int lane = threadIdx.x & 31;
-    const T none = from_f32<T>(-INFINITY);
-    for (int32_t m = m0 + int32_t(threadIdx.x >> 5); m < m1; m += int32_t(blockDim.x >> 5)) {
-        T *out = static_cast<T *>(a.logits) + m * a.stride + v0;
-        if ((v1 - v0) % 128 == 0 && (reinterpret_cast<uintptr_t>(out) & (4 * sizeof(T) - 1)) == 0) {
-            for (int32_t i = lane; i < (v1 - v0) / 4; i += 32) {
-                if (sizeof(T) == 2) reinterpret_cast<uint2 *>(out)[i] = make_uint2(0xFF80FF80u, 0xFF80FF80u);
-                else reinterpret_cast<uint4 *>(out)[i] = make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u);
-            }
-        } else {
-            for (int32_t i = lane; i < v1 - v0; i += 32) out[i] = none;
-        }
-    }
-}
-
-// A warp's 32 rows x 64 tokens of sums to memory: turned in shared memory
-// (`turn`: 32 rows of 64 values and 4 bytes, so that neither side has bank
-// conflicts), so that a row's tokens are written side by side.
-template <typename T>
-__device__ __forceinline__ void store_block(const HeadArgs &a, unsigned char *turn, const uint64_t (&sum)[kColumns / 2],
-                                            int32_t m, int32_t m1, int32_t v, int lane) {
-    constexpr int kPitch = kColumns * int(sizeof(T)) / 4 + 1;  // words
-    uint32_t *mine = reinterpret_cast<uint32_t *>(turn) + lane * kPitch;
+// Sum of 16 products of e4m3 numbers (exact in 32 bits but for the additions).
+__device__ __forceinline__ float dot16(const uint4 &x, const uint4 &w) {
+    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ws[4] = {w.x, w.y, w.z, w.w};
+    float sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kColumns / 2; i++) {
-        float lo, hi;
-        unpack2(sum[i], lo, hi);
-        if (sizeof(T) == 2) {
-            const __nv_bfloat162 both = __floats2bfloat162_rn(lo, hi);
-            mine[i] = *reinterpret_cast<const uint32_t *>(&both);
-        } else {
-            mine[2 * i] = __float_as_uint(lo);
-            mine[2 * i + 1] = __float_as_uint(hi);
+    for (int i = 0; i < 4; i++) {
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2(__nv_fp8x2_storage_t(xs[i] >> (16 * h)), __NV_E4M3);
+            const __half2_raw b = __nv_cvt_fp8x2_to_halfraw2(__nv_fp8x2_storage_t(ws[i] >> (16 * h)), __NV_E4M3);
+            const float2 fa = __half22float2(__half2(a)), fb = __half22float2(__half2(b));
+            sum = fmaf(fa.x, fb.x, sum);
+            sum = fmaf(fa.y, fb.y, sum);
         }
     }
-    __syncwarp();
-    const int32_t rows = min(32, m1 - m), left = a.V - v;  // of this warp, of its tokens
-    T *out = static_cast<T *>(a.logits) + m * a.stride + v;
-    if (sizeof(T) == 2 && left >= kColumns && (reinterpret_cast<uintptr_t>(out) & 3) == 0 && (a.stride & 1) == 0) {
-        for (int32_t r = 0; r < rows; r++)
-            reinterpret_cast<uint32_t *>(out + r * a.stride)[lane] = reinterpret_cast<uint32_t *>(turn)[r * kPitch + lane];
-    } else {
-        for (int32_t r = 0; r < rows; r++) {
-            const T *from = reinterpret_cast<const T *>(reinterpret_cast<uint32_t *>(turn) + r * kPitch);
-            if (lane < left) out[r * a.stride + lane] = from[lane];
-            if (lane + 32 < left) out[r * a.stride + lane + 32] = from[lane + 32];
+    return sum;
+}
+
+__global__ void __launch_bounds__(kRowThreads) k_head_rows(HeadArgs a) {
+    extern __shared__ __align__(16) unsigned char dynamic_smem[];
+    __shared__ int32_t part[kRowThreads / 32];
+    __shared__ int32_t few[kFew];
+    __shared__ int32_t n_few;
+    pdl_launch_dependents();
+    pdl_wait();
+    const int32_t m = blockIdx.x;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const GrammarRow row = grammar_row(a.g, m);
+    const int32_t near = m / kNear * kNear + int32_t(threadIdx.x);
+    const bool dense = __syncthreads_or(near < min(a.M, m / kNear * kNear + kNear) && grammar_row(a.g, near).kind == kAllowAll);
+    if (threadIdx.x == 0) n_few = 0;
+    int32_t n = 0;
+    uint32_t *used = a.used + int64_t(m) * a.used_words;
+    const int32_t W = int32_t(a.g.W);
+    for (int32_t w0 = 0; w0 < a.used_words * 128; w0 += kRowThreads) {  // 4 words of the mask a bit
+        const int32_t w = w0 + int32_t(threadIdx.x);
+        const uint32_t word = w < W ? row.word(w) : 0u;
+        n += __popc(word);
+        const uint32_t any = __ballot_sync(~0u, word != 0u);
+        // eight bits a warp: one for each four lanes
+        uint32_t bits = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i++) bits |= uint32_t(((any >> (4 * i)) & 15u) != 0u) << i;
+        if (lane == 0 && w / 128 < a.used_words) reinterpret_cast<uint8_t *>(used)[w / 32] = uint8_t(bits);
+    }
+    n = __reduce_add_sync(~0u, n);
+    if (lane == 0) part[warp] = n;
+    __syncthreads();
+    n = 0;
+    for (int i = 0; i < kRowThreads / 32; i++) n += part[i];
+    if (row.kind == kAllowAll || dense || n > kFew || a.D > kFewMaxD) {
+        if (threadIdx.x == 0) a.count[m] = -1;
+        return;
+    }
+    for (int32_t w = threadIdx.x; w < W; w += kRowThreads)
+        for (uint32_t word = row.word(w); word; word &= word - 1) few[atomicAdd(&n_few, 1)] = w * 32 + __ffs(word) - 1;
+    for (int32_t i = threadIdx.x; i < a.D / 16; i += kRowThreads)
+        reinterpret_cast<uint4 *>(dynamic_smem)[i] = __ldg(reinterpret_cast<const uint4 *>(a.q + int64_t(m) * a.D) + i);
+    __syncthreads();
+    for (int32_t i = warp; i < n; i += kRowThreads / 32) {
+        const int32_t v = few[i];
+        const uint4 *w = reinterpret_cast<const uint4 *>(a.w + int64_t(v) * a.D);
+        const float *ws = a.ws + int64_t(v / kBlock) * a.blocks;
+        float sum = 0.0f;
+#pragma unroll 4
+        for (int32_t c = lane; c < a.D / 16; c += 32) {
+            const int32_t kb = c / (kBlock / 16);
+            const float f = __ldg(a.s + kb * a.pitch + m) * __ldg(ws + kb);
+            sum = fmaf(dot16(reinterpret_cast<const uint4 *>(dynamic_smem)[c], __ldg(w + c)), f, sum);
+        }
+#pragma unroll
+        for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+        if (lane == 0) {
+            a.token[int64_t(m) * kFew + i] = v;
+            a.value[int64_t(m) * kFew + i] = sum;
+        }
+    }
+    if (threadIdx.x == 0) a.count[m] = n;
+}
+
+// Whether row m allows a token of tokens v0 .. v0 + 127 (v0 a multiple of 128).
+__device__ __forceinline__ bool row_uses(const HeadArgs &a, int32_t m, int32_t v0) {
+    return (__ldg(a.used + int64_t(m) * a.used_words + (v0 >> 12)) >> ((v0 >> 7) & 31)) & 1u;
+}
+
+// Writes the listed logits of row m within tokens [v0, v1), as thread `lane` of `lanes`.
+template <typename T>
+__device__ __forceinline__ void patch_row(const HeadArgs &a, int32_t m, int32_t n, int32_t v0, int32_t v1, int lane, int lanes) {
+    T *out = static_cast<T *>(a.logits) + m * a.stride;
+    for (int32_t i = lane; i < n; i += lanes) {
+        const int32_t v = __ldg(a.token + int64_t(m) * kFew + i);
+        if (v >= v0 && v < v1) out[v] = from_f32<T>(__ldg(a.value + int64_t(m) * kFew + i));
+    }
+}
+
+// Rows [m0, m1) of a tile that no dense row allows a token of: -inf, and the
+// listed logits. By the epilogue warps; NT tokens, fewer at the end.
+template <typename T, int NT, int kWarps>
+__device__ void fill_tile(const HeadArgs &a, int32_t m0, int32_t m1, int32_t v0, int warp, int lane) {
+    constexpr int kVec = 16 / int(sizeof(T));
+    const int32_t v1 = min(a.V, v0 + NT);
+    const uint32_t pair = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
+    for (int32_t m = m0 + warp; m < m1; m += kWarps) {
+        T *out = static_cast<T *>(a.logits) + m * a.stride + v0;
+        if (v1 - v0 == NT && (reinterpret_cast<uintptr_t>(out) & 15) == 0) {
+#pragma unroll
+            for (int i = 0; i < NT / kVec; i += 32)
+                if (i + lane < NT / kVec) reinterpret_cast<uint4 *>(out)[i + lane] = make_uint4(pair, pair, pair, pair);
+        } else {
+            for (int32_t i = lane; i < v1 - v0; i += 32) out[i] = from_f32<T>(-INFINITY);
+        }
+        const int32_t n = __ldg(a.count + m);
+        if (n > 0 && (row_uses(a, m, v0) || (NT > 128 && v0 + 128 < a.V && row_uses(a, m, v0 + 128)))) {
+            __syncwarp();
+            patch_row<T>(a, m, n, v0, v1, lane, 32);
         }
     }
 }
 
-template <typename T, int NT>
-__global__ void __launch_bounds__(HeadShape<NT>::kThreads, HeadShape<NT>::kCtas) k_head_logits(const __grid_constant__ HeadArgs a) {
-    using S = HeadShape<NT>;
+// 16 tokens from v on of a warp's 32 rows from m on (of which `rows` are there),
+// a row a thread. Where every row is on a 32-byte boundary a thread writes its
+// own 32 bytes at a time; else the block is turned in shared memory, so that
+// lanes write consecutive tokens.
+template <typename T>
+__device__ __forceinline__ void store16(const HeadArgs &a, float *turn, const uint64_t *sum, int32_t m, int32_t rows, int32_t v,
+                                        int lane, bool wide) {
+    T *out = static_cast<T *>(a.logits) + m * a.stride + v;
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 8; i++) unpack2(sum[i], x[2 * i], x[2 * i + 1]);
+    if (wide && v + 16 <= a.V) {
+        if (lane >= rows) return;
+        T *mine = out + lane * a.stride;
+        uint32_t r[8];
+        if (sizeof(T) == 2) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const __nv_bfloat162 both = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+                r[i] = *reinterpret_cast<const uint32_t *>(&both);
+            }
+            store32(mine, r);
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+#pragma unroll
+                for (int i = 0; i < 8; i++) r[i] = __float_as_uint(x[8 * h + i]);
+                store32(mine + 8 * h, r);
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; i++) turn[lane * 17 + i] = x[i];
+    __syncwarp();
+    const int c = lane & 15;
+    if (v + c < a.V)
+        for (int r = lane >> 4; r < rows; r += 2) out[r * a.stride + c] = from_f32<T>(turn[r * 17 + c]);
+    __syncwarp();
+}
+
+// Epilogue warps: four quarters of the rows, two or four columns of tokens.
+template <bool kPair>
+constexpr int kEpilogueWarps = kPair ? 16 : 8;
+template <bool kPair>
+constexpr int kHeadThreads = 64 + 32 * kEpilogueWarps<kPair>;
+
+template <typename T, bool kPair>
+__global__ void __launch_bounds__(kHeadThreads<kPair>, 1) k_head_logits(const __grid_constant__ HeadArgs a) {
+    constexpr int NT = kPair ? 256 : 128;          // tokens of a tile
+    constexpr int kAccumulators = 512 / NT;
+    constexpr int kEpilogue = kEpilogueWarps<kPair>;
+    constexpr int kCtas = kPair ? 2 : 1;
+    constexpr int kWeightBytes = 128 * kBlock;     // a CTA's part of the weights of a block
     extern __shared__ unsigned char dynamic_smem[];
-    __shared__ uint64_t bars[2 * kMaxStages + 4];
+    __shared__ uint64_t bars[2 * kMaxStages + 2 * kAccumulators + 2 * kScaleSlots];
+    __shared__ __align__(16) float scales[kScaleSlots][kRows];
+    __shared__ float turn[kEpilogue][kTurn];
+    __shared__ uint32_t need[kNeedTiles / 32];
     __shared__ uint32_t tmem_base;
     __shared__ int gave_up;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int32_t vt = int32_t(blockIdx.x / unsigned(a.m_tiles)), v0 = vt * NT;
-    const int32_t m0 = int32_t(blockIdx.x % unsigned(a.m_tiles)) * kRows, m1 = min(a.M, m0 + kRows);
-    const int quarters = (m1 - m0 + 31) / 32;  // warps' rows that there are
+    const int warp = __shfl_sync(~0u, int(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    const int rank = kPair ? int(cluster_rank()) : 0;
+    const int32_t unit = int32_t(blockIdx.x) / kCtas, units = int32_t(gridDim.x) / kCtas;
     const uint32_t full = smem_addr(bars), empty = full + 8 * kMaxStages;
-    const uint32_t ready = empty + 8 * kMaxStages, drained = ready + 16;
-    unsigned char *ring = dynamic_smem + ((1024u - (smem_addr(dynamic_smem) & 1023u)) & 1023u);
-    const uint32_t stages = smem_addr(ring), stage_bytes = uint32_t(S::kWeightBytes + a.box_rows * kBlock);
+    const uint32_t ready = empty + 8 * kMaxStages, drained = ready + 8 * kAccumulators;
+    const uint32_t s_full = drained + 8 * kAccumulators, s_empty = s_full + 8 * kScaleSlots;
+    const uint32_t stages = (smem_addr(dynamic_smem) + 1023u) & ~1023u, stage_bytes = uint32_t(kWeightBytes + a.box_rows * kBlock);
     if (threadIdx.x == 0) {
         gave_up = 0;
         for (int i = 0; i < a.stages; i++) {
             bar_init(full + 8 * i, 1);
             bar_init(empty + 8 * i, 1);
         }
-        for (int i = 0; i < 2; i++) {
+        for (int i = 0; i < kAccumulators; i++) {
             bar_init(ready + 8 * i, 1);
-            bar_init(drained + 8 * i, uint32_t(quarters * (NT / kColumns)));
+            bar_init(drained + 8 * i, kEpilogue * kCtas);
+        }
+        for (int i = 0; i < kScaleSlots; i++) {
+            bar_init(s_full + 8 * i, 1);
+            bar_init(s_empty + 8 * i, kEpilogue);
         }
         bar_init_fence();
         tma_prefetch_map(&a.map_w);
         tma_prefetch_map(&a.map_q);
     }
+    for (int i = threadIdx.x; i < kNeedTiles / 32; i += kHeadThreads<kPair>) need[i] = 0u;
     pdl_launch_dependents();
     pdl_wait();
+    if (warp == 1) tmem_alloc<kPair>(smem_addr(&tmem_base), 512);
+    __syncthreads();
     if (a.g.mask) {
-        // a tile that no row of the batch allows a token of needs no weights
-        bool any = false;
-        const int32_t w0 = v0 >> 5, words = min(NT / 32, int32_t(a.g.W) - w0);
-        for (int32_t m = m0 + int32_t(threadIdx.x); m < m1 && !any; m += int32_t(blockDim.x)) {
-            const GrammarRow row = grammar_row(a.g, m);
-            for (int32_t i = 0; i < words; i++) any |= row.word(w0 + i) != 0u;
-        }
-        if (!__syncthreads_or(any)) {
-            fill_tile<T>(a, m0, m1, v0, min(a.V, v0 + NT));
-            return;
+        // which of this CTA's tiles a dense row allows a token of
+        for (int32_t i = 0, t = unit; t < a.tiles && i < kNeedTiles; i++, t += units) {
+            const int32_t m = t % a.m_tiles * (kRows * kCtas) + int32_t(threadIdx.x), v0 = t / a.m_tiles * NT;
+            bool any = false;
+            if (threadIdx.x < kRows * kCtas && m < a.M && __ldg(a.count + m) < 0)
+                any = row_uses(a, m, v0) || (NT > 128 && v0 + 128 < a.V && row_uses(a, m, v0 + 128));
+            if (__any_sync(~0u, any) && lane == 0) atomicOr(&need[i >> 5], 1u << (i & 31));
         }
     }
-    if (warp == 1) tmem_alloc(smem_addr(&tmem_base), S::kTmem);
     tcgen05_fence_before();
-    __syncthreads();
+    if (kPair) cluster_sync();
+    else __syncthreads();
     tcgen05_fence_after();
     const uint32_t tmem = *static_cast<volatile uint32_t *>(&tmem_base);
+    auto needed = [&](int32_t i) { return !a.g.mask || i >= kNeedTiles || ((need[i >> 5] >> (i & 31)) & 1u); };
 
     if (warp == 0) {
-        if (lane == 0) {
-            int32_t kb = 0;
-            int stage = 0;
-            uint32_t phase = 1;  // of the stage's last use: the first time round there is none
-            for (; kb < a.blocks; kb++) {
-                const uint32_t at = stages + uint32_t(stage) * stage_bytes, bar = full + 8 * stage;
-                if (!bar_wait(empty + 8 * stage, phase, &gave_up)) break;
-                bar_expect(bar, stage_bytes);
-                tma_load_2d(at, &a.map_w, kb * kBlock, v0, bar);
-                tma_load_2d(at + S::kWeightBytes, &a.map_q, kb * kBlock, m0, bar);
+        int stage = 0;
+        uint32_t phase = 1, used = 0;  // phase: of a stage's last use; the first time round there is none
+        uint32_t it = 0;
+        bool ok = true;
+        const uint32_t leader = kPair ? cluster_addr(full, 0) : full;
+        for (int32_t i = 0, t = unit; t < a.tiles && ok; i++, t += units) {
+            if (!needed(i)) continue;
+            const int32_t m = t % a.m_tiles * (kRows * kCtas) + rank * kRows, v = t / a.m_tiles * NT + rank * 128;
+            // a CTA of a pair without rows takes some others' scales
+            const int64_t sm = min(int64_t(m), a.pitch - 4);
+            const uint32_t scale_bytes = uint32_t(min(int64_t(kRows), a.pitch - sm)) * 4;
+            for (int32_t kb = 0; kb < a.blocks; kb++, it++) {
+                const uint32_t at = stages + uint32_t(stage) * stage_bytes, bar = leader + 8 * stage, slot = it % kScaleSlots;
+                ok = bar_wait(empty + 8 * stage, phase, &gave_up) &&
+                     bar_wait(s_empty + 8 * slot, ((it / kScaleSlots) & 1) ^ 1, &gave_up);
+                ok = __all_sync(~0u, ok);
+                if (!ok) break;
+                if (elect_one()) {
+                    bar_expect(s_full + 8 * slot, scale_bytes);
+                    bulk_load(smem_addr(scales[slot]), a.s + kb * a.pitch + sm, scale_bytes, s_full + 8 * slot);
+                    if (kPair) {
+                        // both CTAs' copies count on the first one's barrier
+                        if (rank == 0) bar_expect(full + 8 * stage, 2 * stage_bytes);
+                        tma_load_2d_pair(at, &a.map_w, kb * kBlock, v, bar);
+                        tma_load_2d_pair(at + kWeightBytes, &a.map_q, kb * kBlock, m, bar);
+                    } else {
+                        bar_expect(bar, stage_bytes);
+                        tma_load_2d(at, &a.map_w, kb * kBlock, v, bar);
+                        tma_load_2d(at + kWeightBytes, &a.map_q, kb * kBlock, m, bar);
+                    }
+                }
+                __syncwarp();
+                used = min(used + 1, uint32_t(a.stages));
                 if (++stage == a.stages) stage = 0, phase ^= 1;
             }
-            if (gave_up) {  // copies may still write to shared memory: wait for them
-                int none = 0;
-                for (int32_t i = max(0, kb - a.stages); i < kb; i++)
-                    bar_wait(full + 8 * (i % a.stages), (i / a.stages) & 1, &none);
+        }
+        if (!ok) {  // copies may still write to shared memory: wait for them
+            int none = 0;
+            for (uint32_t i = it > kScaleSlots ? it - kScaleSlots : 0; i < it; i++)
+                bar_wait(s_full + 8 * (i % kScaleSlots), (i / kScaleSlots) & 1, &none);
+            for (uint32_t i = 0; i < used && rank == 0; i++) {
+                if (--stage < 0) stage = a.stages - 1, phase ^= 1;
+                bar_wait(full + 8 * stage, phase ^ 1, &none);
             }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            constexpr uint32_t idesc = mma_idesc_e4m3(kRows, NT);
+        if (rank == 0) {
+            constexpr uint32_t idesc = mma_idesc_e4m3(kRows * kCtas, NT);
             int stage = 0;
-            uint32_t phase = 0;
-            for (int32_t kb = 0; kb < a.blocks; kb++) {
-                const int acc = kb & 1;
-                if (!bar_wait(drained + 8 * acc, ((kb >> 1) & 1) ^ 1, &gave_up)) break;
-                if (!bar_wait(full + 8 * stage, phase, &gave_up)) break;
-                tcgen05_fence_after();
-                const uint32_t at = stages + uint32_t(stage) * stage_bytes;
-                const uint64_t dw = mma_desc(at), dq = mma_desc(at + S::kWeightBytes);
+            uint32_t phase = 0, it = 0;
+            bool ok = true;
+            for (int32_t i = 0, t = unit; t < a.tiles && ok; i++, t += units) {
+                if (!needed(i)) continue;
+                for (int32_t kb = 0; kb < a.blocks; kb++, it++) {
+                    const uint32_t acc = it % kAccumulators;
+                    ok = bar_wait(drained + 8 * acc, ((it / kAccumulators) & 1) ^ 1, &gave_up) &&
+                         bar_wait(full + 8 * stage, phase, &gave_up);
+                    ok = __all_sync(~0u, ok);
+                    if (!ok) break;
+                    tcgen05_fence_after();
+                    const uint32_t at = stages + uint32_t(stage) * stage_bytes;
+                    const uint64_t dw = mma_desc(at), dq = mma_desc(at + kWeightBytes);
+                    if (elect_one()) {
 #pragma unroll
-                for (int k = 0; k < kBlock / 32; k++) mma_e4m3(tmem + acc * NT, dq + 2 * k, dw + 2 * k, idesc, k > 0);
-                mma_commit(empty + 8 * stage);
-                mma_commit(ready + 8 * acc);
-                if (++stage == a.stages) stage = 0, phase ^= 1;
-            }
-        }
-    } else if ((warp & 3) < quarters) {
-        const int quarter = warp & 3, column = (warp - 2) / 4 * kColumns;
-        const uint32_t from = tmem + (uint32_t(quarter * 32) << 16) + uint32_t(column);
-        const int32_t row = min(m0 + quarter * 32 + lane, a.M - 1), v = v0 + column;
-        uint64_t sum[kColumns / 2];
-#pragma unroll
-        for (int i = 0; i < kColumns / 2; i++) sum[i] = 0ull;
-        bool ok = true;
-        // scales are read two blocks ahead
-        const float *sp = a.s + row, *wp = a.ws + int64_t(min(v, a.V - 1) / kBlock) * a.blocks;
-        float s0 = __ldg(sp) * __ldg(wp), s1 = 0.0f;
-        if (a.blocks > 1) s1 = __ldg(sp + a.pitch) * __ldg(wp + 1);
-        for (int32_t kb = 0; kb < a.blocks; kb++) {
-            const int acc = kb & 1;
-            const uint64_t scale = pack2(s0, s0);
-            s0 = s1;
-            if (kb + 2 < a.blocks) s1 = __ldg(sp + (kb + 2) * a.pitch) * __ldg(wp + kb + 2);
-            ok = __all_sync(~0u, bar_wait(ready + 8 * acc, (kb >> 1) & 1, &gave_up));
-            if (!ok) break;
-            tcgen05_fence_after();
-#pragma unroll
-            for (int c = 0; c < kColumns; c += 16) {
-                uint32_t r[16];
-                tmem_load16(from + acc * NT + c, r);
-                tmem_wait_ld();
-#pragma unroll
-                for (int i = 0; i < 16; i += 2) sum[(c + i) / 2] = fma2(pack2u(r[i], r[i + 1]), scale, sum[(c + i) / 2]);
-            }
-            tcgen05_fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(drained + 8 * acc);
-        }
-        // a tile that gave up waiting has no result: NaN
-        if (!ok) {
-#pragma unroll
-            for (int i = 0; i < kColumns / 2; i++) sum[i] = 0x7FFFFFFF7FFFFFFFull;
-        }
-        if (a.g.mask) {
-            const GrammarRow allow = grammar_row(a.g, row);
-#pragma unroll
-            for (int c = 0; c < kColumns; c += 32) {
-                const uint32_t word = (v + c) >> 5 < a.g.W ? allow.word((v + c) >> 5) : 0u;
-                if (word == ~0u) continue;
-#pragma unroll
-                for (int i = 0; i < 32; i += 2) {
-                    float lo, hi;
-                    unpack2(sum[(c + i) / 2], lo, hi);
-                    if (!((word >> i) & 1u)) lo = -INFINITY;
-                    if (!((word >> (i + 1)) & 1u)) hi = -INFINITY;
-                    sum[(c + i) / 2] = pack2(lo, hi);
+                        for (int k = 0; k < kBlock / 32; k++)
+                            mma_e4m3<kPair>(tmem + acc * NT, dq + 2 * k, dw + 2 * k, idesc, k > 0);
+                        mma_commit<kPair>(empty + 8 * stage);
+                        mma_commit<kPair>(ready + 8 * acc);
+                    }
+                    __syncwarp();
+                    if (++stage == a.stages) stage = 0, phase ^= 1;
                 }
             }
         }
-        // every MMA is done (the last `ready`), so the ring is free to turn the block in
-        if (ok && v < a.V)
-            store_block<T>(a, ring + (warp - 2) * 32 * (kColumns * int(sizeof(T)) + 4), sum, m0 + quarter * 32, m1, v, lane);
+    } else {
+        const int quarter = warp & 3, column = (warp - 2) / 4 * kColumns;
+        const uint32_t from = tmem + (uint32_t(quarter * 32) << 16) + uint32_t(column);
+        const uint32_t drain = kPair ? cluster_addr(drained, 0) : drained;
+        const bool wide = ((reinterpret_cast<uintptr_t>(a.logits) | uintptr_t(a.stride * int64_t(sizeof(T)))) & 31) == 0;
+        uint32_t it = 0;
+        bool ok = true;
+        for (int32_t i = 0, t = unit; t < a.tiles; i++, t += units) {
+            const int32_t m0 = t % a.m_tiles * (kRows * kCtas) + rank * kRows, m1 = min(a.M, m0 + kRows);
+            const int32_t v0 = t / a.m_tiles * NT, v = v0 + column;
+            if (!needed(i)) {
+                fill_tile<T, NT, kEpilogue>(a, m0, m1, v0, warp - 2, lane);
+                continue;
+            }
+            const int32_t mine = m0 + quarter * 32, row = min(mine + lane, a.M - 1);
+            const bool there = mine < m1;  // a warp without rows only keeps the barriers going
+            uint64_t sum[kColumns / 2];
+#pragma unroll
+            for (int c = 0; c < kColumns / 2; c++) sum[c] = 0ull;
+            // A block's scale of the row comes through a ring of its own (a read from
+            // global memory would have to be many blocks ahead); the weights' scale is
+            // read two blocks ahead and multiplied where it is used: an instruction
+            // that needs a value on its way, even a move, holds the warp up.
+            const float *wp = a.ws + int64_t(min(v, a.V - 1) / kBlock) * a.blocks;
+            float w[2] = {};
+            auto add_block = [&](int32_t kb, int set) {
+                const uint32_t acc = it % kAccumulators, slot = it % kScaleSlots;
+                ok = ok && __all_sync(~0u, bar_wait(s_full + 8 * slot, (it / kScaleSlots) & 1, &gave_up) &&
+                                               bar_wait(ready + 8 * acc, (it / kAccumulators) & 1, &gave_up));
+                if (!ok) return;
+                tcgen05_fence_after();
+                const float f = scales[slot][quarter * 32 + lane] * w[set];
+                const uint64_t scale = pack2(f, f);
+                if (kb + 2 < a.blocks) w[set] = __ldg(wp + kb + 2);
+                if (there) {
+#pragma unroll
+                    for (int c = 0; c < kColumns; c += 16) {
+                        uint32_t r[16];
+                        tmem_load16(from + acc * NT + c, r);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 16; e += 2) sum[(c + e) / 2] = fma2(pack2u(r[e], r[e + 1]), scale, sum[(c + e) / 2]);
+                    }
+                }
+                tcgen05_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (kPair) bar_arrive_remote(drain + 8 * acc);
+                    else bar_arrive(drain + 8 * acc);
+                    bar_arrive(s_empty + 8 * slot);
+                }
+                it++;
+            };
+            w[0] = __ldg(wp);
+            w[1] = a.blocks > 1 ? __ldg(wp + 1) : 0.0f;
+            for (int32_t kb = 0; kb < a.blocks; kb += 2) {
+                add_block(kb, 0);
+                if (kb + 1 < a.blocks) add_block(kb + 1, 1);
+            }
+            if (!there) continue;
+            const GrammarRow allow = grammar_row(a.g, row);
+            const int32_t few = a.g.mask ? __ldg(a.count + row) : -1;
+#pragma unroll
+            for (int c = 0; c < kColumns; c += 16) {
+                uint32_t bits = ~0u;
+                if (a.g.mask) bits = few < 0 && (v + c) >> 5 < a.g.W ? allow.word((v + c) >> 5) >> (c & 16) : 0u;
+                if (!ok || (bits & 0xFFFFu) != 0xFFFFu) {
+#pragma unroll
+                    for (int e = 0; e < 16; e += 2) {
+                        float lo, hi;
+                        unpack2(sum[(c + e) / 2], lo, hi);
+                        if (!ok) lo = hi = __int_as_float(0x7FFFFFFF);  // gave up waiting: no result
+                        if (!((bits >> e) & 1u)) lo = -INFINITY;
+                        if (!((bits >> (e + 1)) & 1u)) hi = -INFINITY;
+                        sum[(c + e) / 2] = pack2(lo, hi);
+                    }
+                }
+                if (v + c < a.V) store16<T>(a, turn[warp - 2], sum + c / 2, mine, min(32, m1 - mine), v + c, lane, wide);
+            }
+            __syncwarp();
+            if (few > 0 && mine + lane < m1 && v < a.V && row_uses(a, row, v & ~127))
+                patch_row<T>(a, row, few, v, v + kColumns, 0, 1);
+        }
     }
     __syncwarp();
     tcgen05_fence_before();
-    __syncthreads();
+    if (kPair) cluster_sync();
+    else __syncthreads();
     tcgen05_fence_after();
-    if (warp == 1) tmem_free(tmem, S::kTmem);
+    if (warp == 1) tmem_free<kPair>(tmem, 512);
 }
 
 // [rows][D] bytes in boxes of box_rows x 128, 128-byte swizzle, zeros outside.
@@ -365,18 +575,31 @@ bool make_map(CUtensorMap *map, const void *base, int64_t rows, int32_t D, int32
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T, int NT>
-cudaError_t launch_head(HeadArgs a, int64_t grid, cudaStream_t st) {
-    using S = HeadShape<NT>;
-    const int stage = S::kWeightBytes + a.box_rows * kBlock;
+template <typename T, bool kPair>
+cudaError_t launch_head(HeadArgs a, cudaStream_t st) {
+    const int stage = 128 * kBlock + a.box_rows * kBlock;
     // the last stage's MMA reads kRows rows, whatever was loaded; and room to align the ring
     const int beyond = (kRows - a.box_rows) * kBlock + 1024;
-    a.stages = std::min(kMaxStages, (S::kBudget - beyond) / stage);
-    const int turn = S::kEpilogue * 32 * (kColumns * int(sizeof(T)) + 4) + 1024;
-    const int smem = std::max(a.stages * stage + beyond, turn);
-    const cudaError_t e = cudaFuncSetAttribute(k_head_logits<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBudget);
+    const int fixed = int(sizeof(float)) * (kEpilogueWarps<kPair> * kTurn + kScaleSlots * kRows) + 1024;  // declared in the kernel
+    a.stages = std::min(kMaxStages, (kHeadSmem - fixed - beyond) / stage);
+    const int smem = a.stages * stage + beyond;
+    const cudaError_t e = cudaFuncSetAttribute(k_head_logits<T, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadSmem - fixed);
     if (e != cudaSuccess) return e;
-    return launch_pdl_smem(k_head_logits<T, NT>, grid, S::kThreads, smem, st, a);
+    const int ctas = kPair ? 2 : 1, units = std::min(a.tiles, sm_count() / ctas);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(units * ctas));
+    cfg.blockDim = dim3(kHeadThreads<kPair>);
+    cfg.dynamicSmemBytes = size_t(smem);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = unsigned(ctas);
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = kPair ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, k_head_logits<T, kPair>, a);
 }
 
 const char *check_quantize(const void *x, int dtype, int64_t stride, int32_t rows, int32_t D, const void *q,
@@ -429,10 +652,33 @@ extern "C" int trie_head_quantize_weight(const void *d_w, int dtype, int64_t str
     return TRIE_OK;
 }
 
+namespace tmk {
+namespace {
+// Where the parts of the workspace lie.
+struct HeadSpace {
+    int32_t used_words;
+    int64_t count, used, token, value, bytes;
+    HeadSpace(int32_t M, int32_t V) {
+        used_words = int32_t((int64_t(V) + 4095) / 4096);
+        count = 0;
+        used = (int64_t(M) * 4 + 15) / 16 * 16;
+        token = used + (int64_t(M) * used_words * 4 + 15) / 16 * 16;
+        value = token + int64_t(M) * kFew * 4;
+        bytes = value + int64_t(M) * kFew * 4;
+    }
+};
+}  // namespace
+}  // namespace tmk
+
+extern "C" int64_t trie_head_workspace(int32_t M, int32_t V) {
+    if (M < 0 || M > (1 << 20) || V < 2 || V > tmk::kMaxV) return -1;
+    return tmk::HeadSpace(M, V).bytes;
+}
+
 extern "C" int trie_head_logits(const uint8_t *d_q, const float *d_scales, int64_t pitch, const uint8_t *d_w,
                                 const float *d_w_scales, int32_t M, int32_t V, int32_t D, void *d_logits, int dtype,
                                 int64_t stride, const uint32_t *d_mask, int32_t mask_rows, const int32_t *d_states,
-                                cudaStream_t stream) {
+                                void *d_workspace, cudaStream_t stream) {
     using namespace tmk;
     const char *bad = check_logits(d_logits, dtype, stride, M, V);
     if (!*bad) bad = check_grammar(d_mask, mask_rows, d_states);
@@ -444,28 +690,48 @@ extern "C" int trie_head_logits(const uint8_t *d_q, const float *d_scales, int64
         bad = "d_q, d_w and d_scales must be aligned to 16 bytes";
     if (!*bad && (reinterpret_cast<uintptr_t>(d_w_scales) & 3)) bad = "d_w_scales is not aligned to 4 bytes";
     if (!*bad && M > (1 << 20)) bad = "M must be <= 2^20";
+    if (!*bad && M > 0 && d_mask && !d_workspace) bad = "d_mask without d_workspace";
+    if (!*bad && (reinterpret_cast<uintptr_t>(d_workspace) & 15)) bad = "d_workspace is not aligned to 16 bytes";
     if (*bad) return set_error(TRIE_EINVAL, bad);
     if (M == 0) return TRIE_OK;
     HeadArgs a = {};
+    a.q = d_q;
+    a.w = d_w;
     a.s = d_scales;
     a.pitch = pitch;
     a.ws = d_w_scales;
     a.M = M;
     a.V = V;
+    a.D = D;
     a.blocks = (D + kBlock - 1) / kBlock;
-    a.m_tiles = (M + kRows - 1) / kRows;
+    const bool pair = M > kRows;
+    const int side = pair ? 256 : 128;  // of a tile
+    a.m_tiles = (M + side - 1) / side;
     a.box_rows = std::min(kRows, (M + 7) / 8 * 8);
     a.logits = d_logits;
     a.stride = stride;
     a.g = make_grammar(d_mask, mask_rows, d_states, V);
-    const int nt = M <= 64 ? 128 : 256;
-    if (!make_map(&a.map_w, d_w, V, D, nt) || !make_map(&a.map_q, d_q, M, D, a.box_rows))
+    if (!make_map(&a.map_w, d_w, V, D, 128) || !make_map(&a.map_q, d_q, M, D, a.box_rows))
         return set_error(TRIE_ECUDA, "cuTensorMapEncodeTiled failed");
-    const int64_t grid = (int64_t(V) + nt - 1) / nt * a.m_tiles;
-    if (grid > 0x7FFFFFFF) return set_error(TRIE_EINVAL, "M x V is too large");
+    const int64_t tiles = (int64_t(V) + side - 1) / side * a.m_tiles;
+    if (tiles > 0x3FFFFFFF) return set_error(TRIE_EINVAL, "M x V is too large");
+    a.tiles = int32_t(tiles);
+    cudaError_t e;
+    if (d_mask) {
+        const HeadSpace at(M, V);
+        unsigned char *base = static_cast<unsigned char *>(d_workspace);
+        a.count = reinterpret_cast<int32_t *>(base + at.count);
+        a.used = reinterpret_cast<uint32_t *>(base + at.used);
+        a.token = reinterpret_cast<int32_t *>(base + at.token);
+        a.value = reinterpret_cast<float *>(base + at.value);
+        a.used_words = at.used_words;
+        const int smem = D <= kFewMaxD ? D : 0;
+        if ((e = launch_pdl_smem(k_head_rows, M, kRowThreads, smem, stream, a)) != cudaSuccess)
+            return fail_launch(e, "head rows launch");
+    }
     const bool f32 = dtype == TRIE_DTYPE_F32;
-    const cudaError_t e = nt == 128 ? (f32 ? launch_head<float, 128>(a, grid, stream) : launch_head<__nv_bfloat16, 128>(a, grid, stream))
-                                    : (f32 ? launch_head<float, 256>(a, grid, stream) : launch_head<__nv_bfloat16, 256>(a, grid, stream));
+    e = pair ? (f32 ? launch_head<float, true>(a, stream) : launch_head<__nv_bfloat16, true>(a, stream))
+             : (f32 ? launch_head<float, false>(a, stream) : launch_head<__nv_bfloat16, false>(a, stream));
     if (e != cudaSuccess) return fail_launch(e, "head launch");
     return TRIE_OK;
 }

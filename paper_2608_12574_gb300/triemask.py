@@ -65,7 +65,8 @@ SIGNATURES = {
     "trie_head_quantize": (ctypes.c_int, [_P, ctypes.c_int, _I64, _I32, _I32, _P, _P, _I64, _P]),
     "trie_head_quantize_weight": (ctypes.c_int, [_P, ctypes.c_int, _I64, _I32, _I32, _P, _P, _P]),
     "trie_head_logits": (ctypes.c_int, [_P, _P, _I64, _P, _P, _I32, _I32, _I32, _P, ctypes.c_int, _I64, _P, _I32, _P,
-                                        _P]),
+                                        _P, _P]),
+    "trie_head_workspace": (_I64, [_I32, _I32]),
     "trie_penalize": (ctypes.c_int, [_P, ctypes.c_int, _I64, _I32, _I32, _P, _I64, _I32, _P, _P, _P, _P, _P, _P, _P, _P,
                                      _P, _I32, _P, _P]),
     "trie_sample_workspace": (_I64, [_I32, _I32]),
@@ -634,9 +635,28 @@ def trie_head_quantize_weight(w, stream=None):
     return q, scales
 
 
-def trie_head_logits(q, scales, w, w_scales, d_logits, mask=None, states=None, stream=None) -> None:
+def trie_head_workspace(M: int, V: int) -> int:
+    """Bytes of trie_head_logits' workspace (with a grammar)."""
+    n = load_library().trie_head_workspace(M, V)
+    if n < 0:
+        raise ValueError("M or V out of range")
+    return n
+
+
+def _workspace(given, need: int, like, stream):
+    """Address of a workspace of `need` bytes, the caller's or one from torch's allocator, and its owner."""
+    import torch
+    if given is None:
+        given = _empty(max(need, 0), torch.uint8, like.device, stream)
+    elif given.numel() * given.element_size() < need:
+        raise ValueError(f"workspace must have at least {need} bytes")
+    return _vec(given, given.dtype, given.numel(), "workspace", like.get_device()), given
+
+
+def trie_head_logits(q, scales, w, w_scales, d_logits, mask=None, states=None, workspace=None, stream=None) -> None:
     """d_logits ([M, V] fp32 or bf16) = x W^T of the quantized hidden states (q, scales) and weights
-    (w, w_scales), -inf where the row of the mask that states names does not allow the token."""
+    (w, w_scales), -inf where the row of the mask that states names does not allow the token. A workspace
+    of trie_head_workspace(M, V) bytes may be given where there is a mask."""
     import torch
     dtype = _logits_dtype(d_logits)
     M, V = d_logits.shape
@@ -650,10 +670,13 @@ def trie_head_logits(q, scales, w, w_scales, d_logits, mask=None, states=None, s
         raise ValueError("w_scales must be [ceil(V/128), ceil(D/128)]")
     p, stride = _rows(d_logits, "d_logits")
     dev, fp8, f32 = d_logits.get_device(), torch.float8_e4m3fn, torch.float32
-    _check(load_library().trie_head_logits(
+    lib, space, owner = load_library(), None, None
+    if mask is not None:
+        space, owner = _workspace(workspace, lib.trie_head_workspace(M, V), d_logits, stream)
+    _check(lib.trie_head_logits(
         _vec(q, fp8, M * D, "q", dev), _vec(scales, f32, scales.numel(), "scales", dev), scales.shape[1],
         _vec(w, fp8, V * D, "w", dev), _vec(w_scales, f32, w_scales.numel(), "w_scales", dev), M, V, D, p, dtype, stride,
-        *_grammar(mask, states, M, V, dev), _stream_of(stream, d_logits)))
+        *_grammar(mask, states, M, V, dev), space, _stream_of(stream, d_logits)))
 
 
 def trie_penalize(d_logits, history=None, length=None, prompt=None, repetition=None, presence=None, frequency=None,
@@ -709,15 +732,11 @@ def trie_sample(d_logits, seeds, temperature=None, top_k=None, top_p=None, min_p
     dev, i32, f32 = d_logits.get_device(), torch.int32, torch.float32
     tokens = _empty(B, i32, d_logits.device, stream) if tokens is None else tokens
     logprobs = _empty(B, f32, d_logits.device, stream) if logprobs is None else logprobs
-    need = lib.trie_sample_workspace(B, V)
-    if workspace is None:
-        workspace = _empty(max(need, 0), torch.uint8, d_logits.device, stream)
-    elif workspace.numel() * workspace.element_size() < need:
-        raise ValueError(f"workspace must have at least {need} bytes")
+    space, owner = _workspace(workspace, lib.trie_sample_workspace(B, V), d_logits, stream)
     _check(lib.trie_sample(
         p, dtype, stride, B, V, _vec(seeds, torch.int64, B, "seeds", dev), _vec(temperature, f32, B, "temperature", dev),
         _vec(top_k, i32, B, "top_k", dev), _vec(top_p, f32, B, "top_p", dev), _vec(min_p, f32, B, "min_p", dev),
-        *_grammar(mask, states, B, V, dev), _vec(workspace, workspace.dtype, workspace.numel(), "workspace", dev),
+        *_grammar(mask, states, B, V, dev), space,
         _vec(tokens, i32, B, "tokens", dev), _vec(logprobs, f32, B, "logprobs", dev), _stream_of(stream, d_logits)))
     return tokens, logprobs
 

@@ -157,6 +157,32 @@ def test_head_grammar(cuda, M, V, D, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,V,D,few", [(3, 2, 16, 2), (33, 5000, 144, 255), (33, 5000, 144, 256), (33, 5000, 144, 257),
+                                       (130, 9001, 2048, 40), (300, 4100, 272, 72)])
+def test_head_few_tokens(cuda, M, V, D, few, dtype):
+    """Rows that allow up to a list's length of tokens, exactly that, and one more, beside dense ones; a given
+    workspace."""
+    import torch
+    rng = np.random.default_rng([M, V, few])
+    rows = 16
+    x, w = _inputs(rng, M, V, D, dtype, cuda)
+    q, scales = T.trie_head_quantize(x)
+    wq, ws = T.trie_head_quantize_weight(w)
+    allowed = np.zeros((rows, V), bool)
+    for r in range(rows):
+        allowed[r, rng.choice(V, min(V, few if r % 2 else max(1, few - r)), replace=False)] = True
+    allowed[3] = rng.random(V) < 0.6
+    mask = torch.from_numpy(ref.pack(allowed)).to(cuda)
+    work = torch.full((T.trie_head_workspace(M, V) // 4 + 4,), 0x5A5A5A5A, dtype=torch.int32, device=cuda)
+    for choice in ([1, 5, 2], [0, 1, 2, 3, -1, -2]):
+        states = rng.choice(choice, M).astype(np.int32)
+        ok = torch.from_numpy(np.stack([ref.allowed_row(allowed, int(s), V) for s in states])).to(cuda)
+        out = torch.full((M, V), math.nan, dtype=_type(dtype), device=cuda)
+        T.trie_head_logits(q, scales, wq, ws, out, mask, torch.from_numpy(states).to(cuda), workspace=work)
+        _check(q, scales, wq, ws, out, ok)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("offset,pad", [(1, 0), (3, 13), (4, 64), (7, 1)])
 def test_head_strides(cuda, offset, pad, dtype):
     """Rows of logits at any distance and any alignment; what lies between them is not written."""
@@ -240,6 +266,8 @@ def test_head_refusals(cuda):
         (TypeError, lambda: T.trie_head_logits(q, s, wq, ws, out.half())),
         (TypeError, lambda: T.trie_head_logits(q, s.half(), wq, ws, out)),
         (ValueError, lambda: T.trie_head_logits(q, s, wq, ws, out, mask=m)),
+        (ValueError, lambda: T.trie_head_logits(q, s, wq, ws, out, mask=m, states=i, workspace=i)),
+        (ValueError, lambda: T.trie_head_workspace(-1, 5)),
         (ValueError, lambda: T.trie_head_logits(q, s, wq, ws, out, mask=m[:, :6], states=i)),
         (T.TrieError, lambda: T.trie_head_logits(q[:, :24].contiguous(), s[:1], wq[:, :24].contiguous(),
                                                  ws[:, :1].contiguous(), out)),
@@ -249,12 +277,13 @@ def test_head_refusals(cuda):
             call()
     lib = T.load_library()
     args = [q.data_ptr(), s.data_ptr(), 4, wq.data_ptr(), ws.data_ptr(), M, V, D, out.data_ptr(), 0, V, None, 0, None,
-            None]
+            None, None]
     assert lib.trie_head_logits(*args) == T.TRIE_OK
     torch.cuda.synchronize()
     for at, value in [(0, None), (0, q.data_ptr() + 8), (1, None), (1, s.data_ptr() + 4), (2, 2), (2, 6), (3, None),
                       (3, wq.data_ptr() + 4), (4, None), (4, ws.data_ptr() + 2), (5, -1), (6, 1), (7, 0), (7, 24),
-                      (8, None), (8, out.data_ptr() + 2), (9, 5), (10, V - 1), (11, i.data_ptr()), (13, i.data_ptr())]:
+                      (8, None), (8, out.data_ptr() + 2), (9, 5), (10, V - 1), (11, i.data_ptr()), (13, i.data_ptr()),
+                      (14, out.data_ptr() + 4)]:
         wrong = list(args)
         wrong[at] = value
         assert lib.trie_head_logits(*wrong) == T.TRIE_EINVAL, (at, value)
