@@ -120,7 +120,7 @@ constexpr int kColumns = 64;       // tokens of an epilogue warp
 constexpr int kHeadSmem = 226 * 1024;
 constexpr int kFewMaxD = 32768;    // longest hidden state whose row fits k_head_rows' shared memory
 constexpr int kNeedTiles = 2048;   // tiles of a CTA whose need is looked up ahead
-constexpr int kScaleSlots = 16;    // more than the blocks that can be between the copies and the epilogue
+constexpr int kScaleSlots = 8;     // of two blocks' scales: more blocks than can be between the copies and the epilogue
 constexpr int kTurn = 32 * 17;     // words of a warp's block of 16 tokens, turned
 
 struct HeadArgs {
@@ -282,12 +282,9 @@ __device__ void fill_tile(const HeadArgs &a, int32_t m0, int32_t m1, int32_t v0,
 // own 32 bytes at a time; else the block is turned in shared memory, so that
 // lanes write consecutive tokens.
 template <typename T>
-__device__ __forceinline__ void store16(const HeadArgs &a, float *turn, const uint64_t *sum, int32_t m, int32_t rows, int32_t v,
+__device__ __forceinline__ void store16(const HeadArgs &a, float *turn, const float *x, int32_t m, int32_t rows, int32_t v,
                                         int lane, bool wide) {
     T *out = static_cast<T *>(a.logits) + m * a.stride + v;
-    float x[16];
-#pragma unroll
-    for (int i = 0; i < 8; i++) unpack2(sum[i], x[2 * i], x[2 * i + 1]);
     if (wide && v + 16 <= a.V) {
         if (lane >= rows) return;
         T *mine = out + lane * a.stride;
@@ -333,7 +330,7 @@ __global__ void __launch_bounds__(kHeadThreads<kPair>, 1) k_head_logits(const __
     constexpr int kWeightBytes = 128 * kBlock;     // a CTA's part of the weights of a block
     extern __shared__ unsigned char dynamic_smem[];
     __shared__ uint64_t bars[2 * kMaxStages + 2 * kAccumulators + 2 * kScaleSlots];
-    __shared__ __align__(16) float scales[kScaleSlots][kRows];
+    __shared__ __align__(16) float scales[kScaleSlots][2][kRows];
     __shared__ float turn[kEpilogue][kTurn];
     __shared__ uint32_t need[kNeedTiles / 32];
     __shared__ uint32_t tmem_base;
@@ -397,15 +394,19 @@ __global__ void __launch_bounds__(kHeadThreads<kPair>, 1) k_head_logits(const __
             // a CTA of a pair without rows takes some others' scales
             const int64_t sm = min(int64_t(m), a.pitch - 4);
             const uint32_t scale_bytes = uint32_t(min(int64_t(kRows), a.pitch - sm)) * 4;
-            for (int32_t kb = 0; kb < a.blocks; kb++, it++) {
-                const uint32_t at = stages + uint32_t(stage) * stage_bytes, bar = leader + 8 * stage, slot = it % kScaleSlots;
-                ok = bar_wait(empty + 8 * stage, phase, &gave_up) &&
-                     bar_wait(s_empty + 8 * slot, ((it / kScaleSlots) & 1) ^ 1, &gave_up);
+            for (int32_t kb = 0; kb < a.blocks; kb++) {
+                const uint32_t at = stages + uint32_t(stage) * stage_bytes, bar = leader + 8 * stage;
+                const uint32_t slot = it % kScaleSlots, two = kb + 1 < a.blocks ? 2 : 1;
+                ok = bar_wait(empty + 8 * stage, phase, &gave_up);
+                if (!(kb & 1)) ok = ok && bar_wait(s_empty + 8 * slot, ((it / kScaleSlots) & 1) ^ 1, &gave_up);
                 ok = __all_sync(~0u, ok);
                 if (!ok) break;
                 if (elect_one()) {
-                    bar_expect(s_full + 8 * slot, scale_bytes);
-                    bulk_load(smem_addr(scales[slot]), a.s + kb * a.pitch + sm, scale_bytes, s_full + 8 * slot);
+                    if (!(kb & 1)) {
+                        bar_expect(s_full + 8 * slot, scale_bytes * two);
+                        for (uint32_t j = 0; j < two; j++)
+                            bulk_load(smem_addr(scales[slot][j]), a.s + (kb + j) * a.pitch + sm, scale_bytes, s_full + 8 * slot);
+                    }
                     if (kPair) {
                         // both CTAs' copies count on the first one's barrier
                         if (rank == 0) bar_expect(full + 8 * stage, 2 * stage_bytes);
@@ -418,6 +419,7 @@ __global__ void __launch_bounds__(kHeadThreads<kPair>, 1) k_head_logits(const __
                     }
                 }
                 __syncwarp();
+                if (!(kb & 1)) it++;
                 used = min(used + 1, uint32_t(a.stages));
                 if (++stage == a.stages) stage = 0, phase ^= 1;
             }
@@ -465,8 +467,7 @@ __global__ void __launch_bounds__(kHeadThreads<kPair>, 1) k_head_logits(const __
         const uint32_t from = tmem + (uint32_t(quarter * 32) << 16) + uint32_t(column);
         const uint32_t drain = kPair ? cluster_addr(drained, 0) : drained;
         const bool wide = ((reinterpret_cast<uintptr_t>(a.logits) | uintptr_t(a.stride * int64_t(sizeof(T)))) & 31) == 0;
-        uint32_t it = 0;
-        bool ok = true;
+        uint32_t it = 0, slot = 0, slot_phase = 0;
         for (int32_t i = 0, t = unit; t < a.tiles; i++, t += units) {
             const int32_t m0 = t % a.m_tiles * (kRows * kCtas) + rank * kRows, m1 = min(a.M, m0 + kRows);
             const int32_t v0 = t / a.m_tiles * NT, v = v0 + column;
@@ -476,24 +477,20 @@ __global__ void __launch_bounds__(kHeadThreads<kPair>, 1) k_head_logits(const __
             }
             const int32_t mine = m0 + quarter * 32, row = min(mine + lane, a.M - 1);
             const bool there = mine < m1;  // a warp without rows only keeps the barriers going
-            uint64_t sum[kColumns / 2];
+            float sum[kColumns];
 #pragma unroll
-            for (int c = 0; c < kColumns / 2; c++) sum[c] = 0ull;
-            // A block's scale of the row comes through a ring of its own (a read from
-            // global memory would have to be many blocks ahead); the weights' scale is
-            // read two blocks ahead and multiplied where it is used: an instruction
-            // that needs a value on its way, even a move, holds the warp up.
+            for (int c = 0; c < kColumns; c++) sum[c] = 0.0f;
+            // A block's scales of the rows come through a ring of their own, two blocks at
+            // a time; the weights' are read 32 blocks at a time, one a lane. (A read from
+            // global memory for each block would have to be many blocks ahead, and an
+            // instruction that needs a value on its way, even a move, holds the warp up.)
             const float *wp = a.ws + int64_t(min(v, a.V - 1) / kBlock) * a.blocks;
-            float w[2] = {};
-            auto add_block = [&](int32_t kb, int set) {
-                const uint32_t acc = it % kAccumulators, slot = it % kScaleSlots;
-                ok = ok && __all_sync(~0u, bar_wait(s_full + 8 * slot, (it / kScaleSlots) & 1, &gave_up) &&
-                                               bar_wait(ready + 8 * acc, (it / kAccumulators) & 1, &gave_up));
-                if (!ok) return;
+            float w = __ldg(wp + min(lane, a.blocks - 1));
+            auto add_block = [&](int32_t kb, const float *scale_of_rows) {
+                const uint32_t acc = it % kAccumulators;
+                bar_wait(ready + 8 * acc, (it / kAccumulators) & 1, &gave_up);
                 tcgen05_fence_after();
-                const float f = scales[slot][quarter * 32 + lane] * w[set];
-                const uint64_t scale = pack2(f, f);
-                if (kb + 2 < a.blocks) w[set] = __ldg(wp + kb + 2);
+                const float scale = scale_of_rows[quarter * 32 + lane] * __shfl_sync(~0u, w, kb & 31);
                 if (there) {
 #pragma unroll
                     for (int c = 0; c < kColumns; c += 16) {
@@ -501,7 +498,7 @@ __global__ void __launch_bounds__(kHeadThreads<kPair>, 1) k_head_logits(const __
                         tmem_load16(from + acc * NT + c, r);
                         tmem_wait_ld();
 #pragma unroll
-                        for (int e = 0; e < 16; e += 2) sum[(c + e) / 2] = fma2(pack2u(r[e], r[e + 1]), scale, sum[(c + e) / 2]);
+                        for (int e = 0; e < 16; e++) sum[c + e] = fmaf(__uint_as_float(r[e]), scale, sum[c + e]);
                     }
                 }
                 tcgen05_fence_before();
@@ -509,16 +506,18 @@ __global__ void __launch_bounds__(kHeadThreads<kPair>, 1) k_head_logits(const __
                 if (lane == 0) {
                     if (kPair) bar_arrive_remote(drain + 8 * acc);
                     else bar_arrive(drain + 8 * acc);
-                    bar_arrive(s_empty + 8 * slot);
                 }
                 it++;
             };
-            w[0] = __ldg(wp);
-            w[1] = a.blocks > 1 ? __ldg(wp + 1) : 0.0f;
             for (int32_t kb = 0; kb < a.blocks; kb += 2) {
-                add_block(kb, 0);
-                if (kb + 1 < a.blocks) add_block(kb + 1, 1);
+                bar_wait(s_full + 8 * slot, slot_phase, &gave_up);
+                add_block(kb, scales[slot][0]);
+                if (kb + 1 < a.blocks) add_block(kb + 1, scales[slot][1]);
+                if (lane == 0) bar_arrive(s_empty + 8 * slot);
+                if (++slot == kScaleSlots) slot = 0, slot_phase ^= 1;
+                if ((kb & 31) == 30 && kb + 2 < a.blocks) w = __ldg(wp + min(kb + 2 + lane, a.blocks - 1));
             }
+            const bool ok = *static_cast<volatile int *>(&gave_up) == 0;
             if (!there) continue;
             const GrammarRow allow = grammar_row(a.g, row);
             const int32_t few = a.g.mask ? __ldg(a.count + row) : -1;
@@ -528,16 +527,12 @@ __global__ void __launch_bounds__(kHeadThreads<kPair>, 1) k_head_logits(const __
                 if (a.g.mask) bits = few < 0 && (v + c) >> 5 < a.g.W ? allow.word((v + c) >> 5) >> (c & 16) : 0u;
                 if (!ok || (bits & 0xFFFFu) != 0xFFFFu) {
 #pragma unroll
-                    for (int e = 0; e < 16; e += 2) {
-                        float lo, hi;
-                        unpack2(sum[(c + e) / 2], lo, hi);
-                        if (!ok) lo = hi = __int_as_float(0x7FFFFFFF);  // gave up waiting: no result
-                        if (!((bits >> e) & 1u)) lo = -INFINITY;
-                        if (!((bits >> (e + 1)) & 1u)) hi = -INFINITY;
-                        sum[(c + e) / 2] = pack2(lo, hi);
+                    for (int e = 0; e < 16; e++) {
+                        if (!ok) sum[c + e] = __int_as_float(0x7FFFFFFF);  // gave up waiting: no result
+                        if (!((bits >> e) & 1u)) sum[c + e] = -INFINITY;
                     }
                 }
-                if (v + c < a.V) store16<T>(a, turn[warp - 2], sum + c / 2, mine, min(32, m1 - mine), v + c, lane, wide);
+                if (v + c < a.V) store16<T>(a, turn[warp - 2], sum + c, mine, min(32, m1 - mine), v + c, lane, wide);
             }
             __syncwarp();
             if (few > 0 && mine + lane < m1 && v < a.V && row_uses(a, row, v & ~127))
@@ -580,7 +575,7 @@ cudaError_t launch_head(HeadArgs a, cudaStream_t st) {
     const int stage = 128 * kBlock + a.box_rows * kBlock;
     // the last stage's MMA reads kRows rows, whatever was loaded; and room to align the ring
     const int beyond = (kRows - a.box_rows) * kBlock + 1024;
-    const int fixed = int(sizeof(float)) * (kEpilogueWarps<kPair> * kTurn + kScaleSlots * kRows) + 1024;  // declared in the kernel
+    const int fixed = int(sizeof(float)) * (kEpilogueWarps<kPair> * kTurn + kScaleSlots * 2 * kRows) + 1024;  // declared in the kernel
     a.stages = std::min(kMaxStages, (kHeadSmem - fixed - beyond) / stage);
     const int smem = a.stages * stage + beyond;
     const cudaError_t e = cudaFuncSetAttribute(k_head_logits<T, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadSmem - fixed);
