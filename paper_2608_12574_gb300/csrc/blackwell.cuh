@@ -29,6 +29,17 @@ __device__ __forceinline__ bool elect_one() {
     return yes != 0;
 }
 
+// Registers of each thread of this warpgroup from here on (multiples of 8). The
+// sum over the CTA's warpgroups must stay within what it was launched with.
+template <int kRegisters>
+__device__ __forceinline__ void fewer_registers() {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegisters));
+}
+template <int kRegisters>
+__device__ __forceinline__ void more_registers() {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegisters));
+}
+
 // ---- mbarriers
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");

@@ -156,7 +156,7 @@ struct HeadArgs {
 // a token, which the tiles' kernel then writes into its -inf.
 constexpr int kFew = 256;
 constexpr int kNear = 256;         // rows among which one free row makes all dense
-constexpr int kRowThreads = 256;
+constexpr int kRowThreads = 512;
 
 // Sum of 16 products of e4m3 numbers (exact in 32 bits but for the additions).
 __device__ __forceinline__ float dot16(const uint4 &x, const uint4 &w) {
@@ -176,57 +176,74 @@ __device__ __forceinline__ float dot16(const uint4 &x, const uint4 &w) {
     return sum;
 }
 
-__global__ void __launch_bounds__(kRowThreads) k_head_rows(HeadArgs a) {
-    extern __shared__ __align__(16) unsigned char dynamic_smem[];
-    __shared__ int32_t part[kRowThreads / 32];
+__global__ void __launch_bounds__(kRowThreads, 2) k_head_rows(HeadArgs a) {
+    extern __shared__ __align__(16) unsigned char dynamic_smem[];  // the row's values, then its scales
     __shared__ int32_t few[kFew];
     __shared__ int32_t n_few;
     pdl_launch_dependents();
+    if (threadIdx.x == 0) n_few = 0;
+    __syncthreads();
     pdl_wait();
     const int32_t m = blockIdx.x;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const GrammarRow row = grammar_row(a.g, m);
-    const int32_t near = m / kNear * kNear + int32_t(threadIdx.x);
-    const bool dense = __syncthreads_or(near < min(a.M, m / kNear * kNear + kNear) && grammar_row(a.g, near).kind == kAllowAll);
-    if (threadIdx.x == 0) n_few = 0;
-    int32_t n = 0;
-    uint32_t *used = a.used + int64_t(m) * a.used_words;
-    const int32_t W = int32_t(a.g.W);
-    for (int32_t w0 = 0; w0 < a.used_words * 128; w0 += kRowThreads) {  // 4 words of the mask a bit
-        const int32_t w = w0 + int32_t(threadIdx.x);
-        const uint32_t word = w < W ? row.word(w) : 0u;
-        n += __popc(word);
-        const uint32_t any = __ballot_sync(~0u, word != 0u);
-        // eight bits a warp: one for each four lanes
-        uint32_t bits = 0;
+    const int32_t first = m / kNear * kNear, near = first + int32_t(threadIdx.x);
+    const bool free_near = threadIdx.x < kNear && near < a.M && grammar_row(a.g, near).kind == kAllowAll;
+    uint8_t *used = reinterpret_cast<uint8_t *>(a.used + int64_t(m) * a.used_words);
+    const int32_t W = int32_t(a.g.W), all = a.used_words * 128;  // words of the mask, of which four make a bit of `used`
+    constexpr int kBatch = 8;  // reads in flight a thread
+    for (int32_t w0 = int32_t(threadIdx.x); w0 - lane < all; w0 += kBatch * kRowThreads) {
+        uint32_t word[kBatch];
 #pragma unroll
-        for (int i = 0; i < 8; i++) bits |= uint32_t(((any >> (4 * i)) & 15u) != 0u) << i;
-        if (lane == 0 && w / 128 < a.used_words) reinterpret_cast<uint8_t *>(used)[w / 32] = uint8_t(bits);
+        for (int i = 0; i < kBatch; i++) {
+            const int32_t w = w0 + i * kRowThreads;
+            word[i] = w < W ? row.word(w) : 0u;
+        }
+#pragma unroll
+        for (int i = 0; i < kBatch; i++) {
+            const int32_t w = w0 + i * kRowThreads;
+            const uint32_t any = __ballot_sync(~0u, word[i] != 0u);
+            uint32_t bits = 0;
+#pragma unroll
+            for (int b = 0; b < 8; b++) bits |= uint32_t(((any >> (4 * b)) & 15u) != 0u) << b;
+            if (lane == 0 && w < all) used[w / 32] = uint8_t(bits);
+            if (word[i]) {
+                int32_t at = atomicAdd(&n_few, __popc(word[i]));
+                for (uint32_t x = word[i]; x && at < kFew; x &= x - 1) few[at++] = w * 32 + __ffs(x) - 1;
+            }
+        }
     }
-    n = __reduce_add_sync(~0u, n);
-    if (lane == 0) part[warp] = n;
-    __syncthreads();
-    n = 0;
-    for (int i = 0; i < kRowThreads / 32; i++) n += part[i];
+    const bool dense = __syncthreads_or(free_near);
+    const int32_t n = n_few;
     if (row.kind == kAllowAll || dense || n > kFew || a.D > kFewMaxD) {
         if (threadIdx.x == 0) a.count[m] = -1;
         return;
     }
-    for (int32_t w = threadIdx.x; w < W; w += kRowThreads)
-        for (uint32_t word = row.word(w); word; word &= word - 1) few[atomicAdd(&n_few, 1)] = w * 32 + __ffs(word) - 1;
+    float *scales = reinterpret_cast<float *>(dynamic_smem + a.D);
     for (int32_t i = threadIdx.x; i < a.D / 16; i += kRowThreads)
         reinterpret_cast<uint4 *>(dynamic_smem)[i] = __ldg(reinterpret_cast<const uint4 *>(a.q + int64_t(m) * a.D) + i);
+    for (int32_t i = threadIdx.x; i < a.blocks; i += kRowThreads) scales[i] = __ldg(a.s + i * a.pitch + m);
     __syncthreads();
     for (int32_t i = warp; i < n; i += kRowThreads / 32) {
         const int32_t v = few[i];
         const uint4 *w = reinterpret_cast<const uint4 *>(a.w + int64_t(v) * a.D);
         const float *ws = a.ws + int64_t(v / kBlock) * a.blocks;
         float sum = 0.0f;
-#pragma unroll 4
-        for (int32_t c = lane; c < a.D / 16; c += 32) {
-            const int32_t kb = c / (kBlock / 16);
-            const float f = __ldg(a.s + kb * a.pitch + m) * __ldg(ws + kb);
-            sum = fmaf(dot16(reinterpret_cast<const uint4 *>(dynamic_smem)[c], __ldg(w + c)), f, sum);
+        for (int32_t c0 = lane; c0 < a.D / 16; c0 += 32 * kBatch) {
+            uint4 x[kBatch];
+            float f[kBatch];
+#pragma unroll
+            for (int j = 0; j < kBatch; j++) {
+                const int32_t c = c0 + 32 * j;
+                x[j] = c < a.D / 16 ? __ldg(w + c) : make_uint4(0u, 0u, 0u, 0u);
+                f[j] = c < a.D / 16 ? __ldg(ws + c / (kBlock / 16)) : 0.0f;
+            }
+#pragma unroll
+            for (int j = 0; j < kBatch; j++) {
+                const int32_t c = c0 + 32 * j;
+                if (c < a.D / 16)
+                    sum = fmaf(dot16(reinterpret_cast<const uint4 *>(dynamic_smem)[c], x[j]), f[j] * scales[c / (kBlock / 16)], sum);
+            }
         }
 #pragma unroll
         for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
@@ -255,12 +272,21 @@ __device__ __forceinline__ void patch_row(const HeadArgs &a, int32_t m, int32_t 
 
 // Rows [m0, m1) of a tile that no dense row allows a token of: -inf, and the
 // listed logits. By the epilogue warps; NT tokens, fewer at the end.
+// (A call, so that its unrolled stores take no registers from the sums of the other tiles.)
 template <typename T, int NT, int kWarps>
-__device__ void fill_tile(const HeadArgs &a, int32_t m0, int32_t m1, int32_t v0, int warp, int lane) {
-    constexpr int kVec = 16 / int(sizeof(T));
+__device__ __noinline__ void fill_tile(const HeadArgs &a, int32_t m0, int32_t m1, int32_t v0, int warp, int lane) {
+    constexpr int kVec = 16 / int(sizeof(T)), kEach = kRows / kWarps;
     const int32_t v1 = min(a.V, v0 + NT);
     const uint32_t pair = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
-    for (int32_t m = m0 + warp; m < m1; m += kWarps) {
+    // which of the warp's rows have listed logits here: a lane a row, asked for ahead of the stores
+    int32_t listed = 0;
+    const int32_t mine = m0 + warp + lane * kWarps;
+    if (lane < kEach && mine < m1 && (row_uses(a, mine, v0) || (NT > 128 && v0 + 128 < a.V && row_uses(a, mine, v0 + 128))))
+        listed = __ldg(a.count + mine);
+#pragma unroll 4
+    for (int j = 0; j < kEach; j++) {
+        const int32_t m = m0 + warp + j * kWarps;
+        if (m >= m1) break;
         T *out = static_cast<T *>(a.logits) + m * a.stride + v0;
         if (v1 - v0 == NT && (reinterpret_cast<uintptr_t>(out) & 15) == 0) {
 #pragma unroll
@@ -269,11 +295,11 @@ __device__ void fill_tile(const HeadArgs &a, int32_t m0, int32_t m1, int32_t v0,
         } else {
             for (int32_t i = lane; i < v1 - v0; i += 32) out[i] = from_f32<T>(-INFINITY);
         }
-        const int32_t n = __ldg(a.count + m);
-        if (n > 0 && (row_uses(a, m, v0) || (NT > 128 && v0 + 128 < a.V && row_uses(a, m, v0 + 128)))) {
-            __syncwarp();
-            patch_row<T>(a, m, n, v0, v1, lane, 32);
-        }
+    }
+    __syncwarp();
+    for (uint32_t rows = __ballot_sync(~0u, listed > 0); rows; rows &= rows - 1) {
+        const int j = __ffs(rows) - 1;
+        patch_row<T>(a, m0 + warp + j * kWarps, __shfl_sync(~0u, listed, j), v0, v1, lane, 32);
     }
 }
 
@@ -318,14 +344,19 @@ __device__ __forceinline__ void store16(const HeadArgs &a, float *turn, const fl
 // Epilogue warps: four quarters of the rows, two or four columns of tokens.
 template <bool kPair>
 constexpr int kEpilogueWarps = kPair ? 16 : 8;
+// The warps before them: one for the copies, one for the MMAs, and for a pair two
+// more that make up a warpgroup, which leaves registers to the epilogue: launched
+// with 96 a thread (640 threads), 128 threads keep 32 and 512 get 112.
 template <bool kPair>
-constexpr int kHeadThreads = 64 + 32 * kEpilogueWarps<kPair>;
+constexpr int kFirstWarp = kPair ? 4 : 2;
+template <bool kPair>
+constexpr int kHeadThreads = 32 * (kFirstWarp<kPair> + kEpilogueWarps<kPair>);
 
 template <typename T, bool kPair>
 __global__ void __launch_bounds__(kHeadThreads<kPair>, 1) k_head_logits(const __grid_constant__ HeadArgs a) {
     constexpr int NT = kPair ? 256 : 128;          // tokens of a tile
     constexpr int kAccumulators = 512 / NT;
-    constexpr int kEpilogue = kEpilogueWarps<kPair>;
+    constexpr int kEpilogue = kEpilogueWarps<kPair>, kFirst = kFirstWarp<kPair>;
     constexpr int kCtas = kPair ? 2 : 1;
     constexpr int kWeightBytes = 128 * kBlock;     // a CTA's part of the weights of a block
     extern __shared__ unsigned char dynamic_smem[];
@@ -382,88 +413,9 @@ __global__ void __launch_bounds__(kHeadThreads<kPair>, 1) k_head_logits(const __
     const uint32_t tmem = *static_cast<volatile uint32_t *>(&tmem_base);
     auto needed = [&](int32_t i) { return !a.g.mask || i >= kNeedTiles || ((need[i >> 5] >> (i & 31)) & 1u); };
 
-    if (warp == 0) {
-        int stage = 0;
-        uint32_t phase = 1, used = 0;  // phase: of a stage's last use; the first time round there is none
-        uint32_t it = 0;
-        bool ok = true;
-        const uint32_t leader = kPair ? cluster_addr(full, 0) : full;
-        for (int32_t i = 0, t = unit; t < a.tiles && ok; i++, t += units) {
-            if (!needed(i)) continue;
-            const int32_t m = t % a.m_tiles * (kRows * kCtas) + rank * kRows, v = t / a.m_tiles * NT + rank * 128;
-            // a CTA of a pair without rows takes some others' scales
-            const int64_t sm = min(int64_t(m), a.pitch - 4);
-            const uint32_t scale_bytes = uint32_t(min(int64_t(kRows), a.pitch - sm)) * 4;
-            for (int32_t kb = 0; kb < a.blocks; kb++) {
-                const uint32_t at = stages + uint32_t(stage) * stage_bytes, bar = leader + 8 * stage;
-                const uint32_t slot = it % kScaleSlots, two = kb + 1 < a.blocks ? 2 : 1;
-                ok = bar_wait(empty + 8 * stage, phase, &gave_up);
-                if (!(kb & 1)) ok = ok && bar_wait(s_empty + 8 * slot, ((it / kScaleSlots) & 1) ^ 1, &gave_up);
-                ok = __all_sync(~0u, ok);
-                if (!ok) break;
-                if (elect_one()) {
-                    if (!(kb & 1)) {
-                        bar_expect(s_full + 8 * slot, scale_bytes * two);
-                        for (uint32_t j = 0; j < two; j++)
-                            bulk_load(smem_addr(scales[slot][j]), a.s + (kb + j) * a.pitch + sm, scale_bytes, s_full + 8 * slot);
-                    }
-                    if (kPair) {
-                        // both CTAs' copies count on the first one's barrier
-                        if (rank == 0) bar_expect(full + 8 * stage, 2 * stage_bytes);
-                        tma_load_2d_pair(at, &a.map_w, kb * kBlock, v, bar);
-                        tma_load_2d_pair(at + kWeightBytes, &a.map_q, kb * kBlock, m, bar);
-                    } else {
-                        bar_expect(bar, stage_bytes);
-                        tma_load_2d(at, &a.map_w, kb * kBlock, v, bar);
-                        tma_load_2d(at + kWeightBytes, &a.map_q, kb * kBlock, m, bar);
-                    }
-                }
-                __syncwarp();
-                if (!(kb & 1)) it++;
-                used = min(used + 1, uint32_t(a.stages));
-                if (++stage == a.stages) stage = 0, phase ^= 1;
-            }
-        }
-        if (!ok) {  // copies may still write to shared memory: wait for them
-            int none = 0;
-            for (uint32_t i = it > kScaleSlots ? it - kScaleSlots : 0; i < it; i++)
-                bar_wait(s_full + 8 * (i % kScaleSlots), (i / kScaleSlots) & 1, &none);
-            for (uint32_t i = 0; i < used && rank == 0; i++) {
-                if (--stage < 0) stage = a.stages - 1, phase ^= 1;
-                bar_wait(full + 8 * stage, phase ^ 1, &none);
-            }
-        }
-    } else if (warp == 1) {
-        if (rank == 0) {
-            constexpr uint32_t idesc = mma_idesc_e4m3(kRows * kCtas, NT);
-            int stage = 0;
-            uint32_t phase = 0, it = 0;
-            bool ok = true;
-            for (int32_t i = 0, t = unit; t < a.tiles && ok; i++, t += units) {
-                if (!needed(i)) continue;
-                for (int32_t kb = 0; kb < a.blocks; kb++, it++) {
-                    const uint32_t acc = it % kAccumulators;
-                    ok = bar_wait(drained + 8 * acc, ((it / kAccumulators) & 1) ^ 1, &gave_up) &&
-                         bar_wait(full + 8 * stage, phase, &gave_up);
-                    ok = __all_sync(~0u, ok);
-                    if (!ok) break;
-                    tcgen05_fence_after();
-                    const uint32_t at = stages + uint32_t(stage) * stage_bytes;
-                    const uint64_t dw = mma_desc(at), dq = mma_desc(at + kWeightBytes);
-                    if (elect_one()) {
-#pragma unroll
-                        for (int k = 0; k < kBlock / 32; k++)
-                            mma_e4m3<kPair>(tmem + acc * NT, dq + 2 * k, dw + 2 * k, idesc, k > 0);
-                        mma_commit<kPair>(empty + 8 * stage);
-                        mma_commit<kPair>(ready + 8 * acc);
-                    }
-                    __syncwarp();
-                    if (++stage == a.stages) stage = 0, phase ^= 1;
-                }
-            }
-        }
-    } else {
-        const int quarter = warp & 3, column = (warp - 2) / 4 * kColumns;
+    if (warp >= kFirst) {
+        if (kPair) more_registers<112>();
+        const int quarter = warp & 3, column = (warp - kFirst) / 4 * kColumns;
         const uint32_t from = tmem + (uint32_t(quarter * 32) << 16) + uint32_t(column);
         const uint32_t drain = kPair ? cluster_addr(drained, 0) : drained;
         const bool wide = ((reinterpret_cast<uintptr_t>(a.logits) | uintptr_t(a.stride * int64_t(sizeof(T)))) & 31) == 0;
@@ -472,7 +424,7 @@ __global__ void __launch_bounds__(kHeadThreads<kPair>, 1) k_head_logits(const __
             const int32_t m0 = t % a.m_tiles * (kRows * kCtas) + rank * kRows, m1 = min(a.M, m0 + kRows);
             const int32_t v0 = t / a.m_tiles * NT, v = v0 + column;
             if (!needed(i)) {
-                fill_tile<T, NT, kEpilogue>(a, m0, m1, v0, warp - 2, lane);
+                fill_tile<T, NT, kEpilogue>(a, m0, m1, v0, warp - kFirst, lane);
                 continue;
             }
             const int32_t mine = m0 + quarter * 32, row = min(mine + lane, a.M - 1);
@@ -532,11 +484,94 @@ __global__ void __launch_bounds__(kHeadThreads<kPair>, 1) k_head_logits(const __
                         if (!((bits >> e) & 1u)) sum[c + e] = -INFINITY;
                     }
                 }
-                if (v + c < a.V) store16<T>(a, turn[warp - 2], sum + c, mine, min(32, m1 - mine), v + c, lane, wide);
+                if (v + c < a.V) store16<T>(a, turn[warp - kFirst], sum + c, mine, min(32, m1 - mine), v + c, lane, wide);
             }
             __syncwarp();
             if (few > 0 && mine + lane < m1 && v < a.V && row_uses(a, row, v & ~127))
                 patch_row<T>(a, row, few, v, v + kColumns, 0, 1);
+        }
+    } else {
+        if (kPair) fewer_registers<32>();
+        if (warp == 0) {
+            int stage = 0;
+            uint32_t phase = 1, used = 0;  // phase: of a stage's last use; the first time round there is none
+            uint32_t it = 0;
+            bool ok = true;
+            const uint32_t leader = kPair ? cluster_addr(full, 0) : full;
+            for (int32_t i = 0, t = unit; t < a.tiles && ok; i++, t += units) {
+                if (!needed(i)) continue;
+                const int32_t m = t % a.m_tiles * (kRows * kCtas) + rank * kRows, v = t / a.m_tiles * NT + rank * 128;
+                // a CTA of a pair without rows takes some others' scales
+                const int64_t sm = min(int64_t(m), a.pitch - 4);
+                const uint32_t scale_bytes = uint32_t(min(int64_t(kRows), a.pitch - sm)) * 4;
+                for (int32_t kb = 0; kb < a.blocks; kb++) {
+                    const uint32_t at = stages + uint32_t(stage) * stage_bytes, bar = leader + 8 * stage;
+                    const uint32_t slot = it % kScaleSlots, two = kb + 1 < a.blocks ? 2 : 1;
+                    ok = bar_wait(empty + 8 * stage, phase, &gave_up);
+                    if (!(kb & 1)) ok = ok && bar_wait(s_empty + 8 * slot, ((it / kScaleSlots) & 1) ^ 1, &gave_up);
+                    ok = __all_sync(~0u, ok);
+                    if (!ok) break;
+                    if (elect_one()) {
+                        if (!(kb & 1)) {
+                            bar_expect(s_full + 8 * slot, scale_bytes * two);
+                            for (uint32_t j = 0; j < two; j++)
+                                bulk_load(smem_addr(scales[slot][j]), a.s + (kb + j) * a.pitch + sm, scale_bytes, s_full + 8 * slot);
+                        }
+                        if (kPair) {
+                            // both CTAs' copies count on the first one's barrier
+                            if (rank == 0) bar_expect(full + 8 * stage, 2 * stage_bytes);
+                            tma_load_2d_pair(at, &a.map_w, kb * kBlock, v, bar);
+                            tma_load_2d_pair(at + kWeightBytes, &a.map_q, kb * kBlock, m, bar);
+                        } else {
+                            bar_expect(bar, stage_bytes);
+                            tma_load_2d(at, &a.map_w, kb * kBlock, v, bar);
+                            tma_load_2d(at + kWeightBytes, &a.map_q, kb * kBlock, m, bar);
+                        }
+                    }
+                    __syncwarp();
+                    if (!(kb & 1)) it++;
+                    used = min(used + 1, uint32_t(a.stages));
+                    if (++stage == a.stages) stage = 0, phase ^= 1;
+                }
+            }
+            if (!ok) {  // copies may still write to shared memory: wait for them
+                int none = 0;
+                for (uint32_t i = it > kScaleSlots ? it - kScaleSlots : 0; i < it; i++)
+                    bar_wait(s_full + 8 * (i % kScaleSlots), (i / kScaleSlots) & 1, &none);
+                for (uint32_t i = 0; i < used && rank == 0; i++) {
+                    if (--stage < 0) stage = a.stages - 1, phase ^= 1;
+                    bar_wait(full + 8 * stage, phase ^ 1, &none);
+                }
+            }
+        } else if (warp == 1) {
+            if (rank == 0) {
+                constexpr uint32_t idesc = mma_idesc_e4m3(kRows * kCtas, NT);
+                int stage = 0;
+                uint32_t phase = 0, it = 0;
+                bool ok = true;
+                for (int32_t i = 0, t = unit; t < a.tiles && ok; i++, t += units) {
+                    if (!needed(i)) continue;
+                    for (int32_t kb = 0; kb < a.blocks; kb++, it++) {
+                        const uint32_t acc = it % kAccumulators;
+                        ok = bar_wait(drained + 8 * acc, ((it / kAccumulators) & 1) ^ 1, &gave_up) &&
+                             bar_wait(full + 8 * stage, phase, &gave_up);
+                        ok = __all_sync(~0u, ok);
+                        if (!ok) break;
+                        tcgen05_fence_after();
+                        const uint32_t at = stages + uint32_t(stage) * stage_bytes;
+                        const uint64_t dw = mma_desc(at), dq = mma_desc(at + kWeightBytes);
+                        if (elect_one()) {
+#pragma unroll
+                            for (int k = 0; k < kBlock / 32; k++)
+                                mma_e4m3<kPair>(tmem + acc * NT, dq + 2 * k, dw + 2 * k, idesc, k > 0);
+                            mma_commit<kPair>(empty + 8 * stage);
+                            mma_commit<kPair>(ready + 8 * acc);
+                        }
+                        __syncwarp();
+                        if (++stage == a.stages) stage = 0, phase ^= 1;
+                    }
+                }
+            }
         }
     }
     __syncwarp();
@@ -720,7 +755,7 @@ extern "C" int trie_head_logits(const uint8_t *d_q, const float *d_scales, int64
         a.token = reinterpret_cast<int32_t *>(base + at.token);
         a.value = reinterpret_cast<float *>(base + at.value);
         a.used_words = at.used_words;
-        const int smem = D <= kFewMaxD ? D : 0;
+        const int smem = D <= kFewMaxD ? D + a.blocks * 4 : 0;
         if ((e = launch_pdl_smem(k_head_rows, M, kRowThreads, smem, stream, a)) != cudaSuccess)
             return fail_launch(e, "head rows launch");
     }
