@@ -46,11 +46,13 @@ constexpr int kGroup = 256;
 constexpr int kGroupThreads = 256;  // k_sample_groups
 constexpr int kThreads = 512;       // k_sample_pick
 constexpr int kWarps = kThreads / 32;
-constexpr int kList = 8192;
+constexpr int kList = 4096;
 constexpr int kSmallK = 64;         // largest top-k that goes without a histogram
 constexpr int kBins = 2048;
 constexpr float kBinsPerUnit = 32.0f;
 constexpr int kChunk = 128;         // most groups of a CTA of k_sample_groups
+constexpr int kQuad = 4;            // groups that a warp of k_sample_groups takes at a time
+constexpr int kPair = 2;            // of k_sample_pick
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr uint32_t kKeyNone = 0x007FFFFFu;  // order_key(-inf)
 constexpr double kFixed = 1099511627776.0;  // 2^40
@@ -180,11 +182,7 @@ __device__ __forceinline__ Best warp_best(Best x) {
     }
     return x;
 }
-__device__ __forceinline__ float warp_max(float x) {
-#pragma unroll
-    for (int d = 16; d; d >>= 1) x = fmaxf(x, __shfl_xor_sync(~0u, x, d));
-    return x;
-}
+__device__ __forceinline__ float warp_max(float x) { return key_value(__reduce_max_sync(~0u, order_key(x))); }
 __device__ __forceinline__ float warp_sum(float x) {
 #pragma unroll
     for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
@@ -193,6 +191,7 @@ __device__ __forceinline__ float warp_sum(float x) {
 
 struct Shared {
     unsigned long long list[kList];     // order_key << 32 | ~id, or id << 32 | order_key
+    float weight[kList];                // of the list's entries
     union {
         float before[kList];            // weights of the list before each entry
         struct {
@@ -205,7 +204,7 @@ struct Shared {
         } radix;
     };
     Best best[kWarps];
-    float f[kWarps];
+    float f[kWarps], g[kWarps];
     int32_t i[kWarps];
     int32_t n;
     int32_t bin[2];
@@ -214,41 +213,67 @@ struct Shared {
     unsigned long long above, total;
 };
 
-__device__ Best block_best(Shared &s, Best x) {
+// Over the block: every warp reduces the warps' values once more, so that one
+// barrier after they are written is enough (and one before, for the last use).
+static_assert(kWarps == 16, "half a warp reads the warps' values");
+__device__ __forceinline__ Best block_best(Shared &s, Best x) {
     x = warp_best(x);
     __syncthreads();
     if ((threadIdx.x & 31) == 0) s.best[threadIdx.x >> 5] = x;
     __syncthreads();
-    x = s.best[0];
-    for (int i = 1; i < kWarps; i++) x = better(x, s.best[i]);
+    x = s.best[threadIdx.x & 15];
+#pragma unroll
+    for (int d = 8; d; d >>= 1) {
+        Best y;
+        y.score = __shfl_xor_sync(~0u, x.score, d);
+        y.id = __shfl_xor_sync(~0u, x.id, d);
+        x = better(x, y);
+    }
     return x;
 }
-__device__ float block_max(Shared &s, float x) {
-    x = warp_max(x);
+// The largest a and the smallest b.
+__device__ __forceinline__ void block_range(Shared &s, float &a, float &b) {
+    a = warp_max(a);
+    b = -warp_max(-b);
     __syncthreads();
-    if ((threadIdx.x & 31) == 0) s.f[threadIdx.x >> 5] = x;
+    if ((threadIdx.x & 31) == 0) s.f[threadIdx.x >> 5] = a, s.g[threadIdx.x >> 5] = b;
     __syncthreads();
-    x = s.f[0];
-    for (int i = 1; i < kWarps; i++) x = fmaxf(x, s.f[i]);
-    return x;
+    a = s.f[threadIdx.x & 15];
+    b = s.g[threadIdx.x & 15];
+#pragma unroll
+    for (int d = 8; d; d >>= 1) {
+        a = fmaxf(a, __shfl_xor_sync(~0u, a, d));
+        b = fminf(b, __shfl_xor_sync(~0u, b, d));
+    }
 }
-__device__ float block_sum(Shared &s, float x) {
+__device__ __forceinline__ float block_sum(Shared &s, float x) {
     x = warp_sum(x);
     __syncthreads();
     if ((threadIdx.x & 31) == 0) s.f[threadIdx.x >> 5] = x;
     __syncthreads();
-    x = s.f[0];
-    for (int i = 1; i < kWarps; i++) x += s.f[i];
+    x = s.f[threadIdx.x & 15];
+#pragma unroll
+    for (int d = 8; d; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
     return x;
 }
-
-__device__ int32_t block_sum(Shared &s, int32_t x) {
+__device__ __forceinline__ int32_t block_sum(Shared &s, int32_t x) {
     x = __reduce_add_sync(~0u, x);
     __syncthreads();
     if ((threadIdx.x & 31) == 0) s.i[threadIdx.x >> 5] = x;
     __syncthreads();
-    x = s.i[0];
-    for (int i = 1; i < kWarps; i++) x += s.i[i];
+    return __reduce_add_sync(~0u, (threadIdx.x & 31) < kWarps ? s.i[threadIdx.x & 15] : 0);
+}
+
+// The sums over the warp of four values, in six exchanges: every lane ends with
+// that of value quad_of(lane).
+__device__ __forceinline__ int quad_of(int lane) { return (lane >> 3) & 3; }
+__device__ __forceinline__ float warp_sum4(const float (&v)[kQuad], int lane) {
+    const bool high = lane & 16, odd = lane & 8;
+    const float a = (high ? v[2] : v[0]) + __shfl_xor_sync(~0u, high ? v[0] : v[2], 16);
+    const float b = (high ? v[3] : v[1]) + __shfl_xor_sync(~0u, high ? v[1] : v[3], 16);
+    float x = (odd ? b : a) + __shfl_xor_sync(~0u, odd ? a : b, 8);
+#pragma unroll
+    for (int d = 4; d; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
     return x;
 }
 
@@ -317,7 +342,7 @@ __device__ __forceinline__ float exp2_fast(float x) {
 
 template <typename T>
 __global__ void __launch_bounds__(kGroupThreads) k_sample_groups(SampleArgs a) {
-    __shared__ uint32_t hist[2][kBins];
+    __shared__ __align__(16) uint32_t hist[2 * kBins];  // counts, weights
     pdl_launch_dependents();
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -328,7 +353,7 @@ __global__ void __launch_bounds__(kGroupThreads) k_sample_groups(SampleArgs a) {
     const bool binned = wants_hist(way, a.G);
     Bins bins(0.0f);
     if (binned) {
-        for (int i = threadIdx.x; i < 2 * kBins; i += kGroupThreads) hist[0][i] = 0u;
+        for (int i = threadIdx.x; i < 2 * kBins; i += kGroupThreads) hist[i] = 0u;
         float x[8], m = -INFINITY;
         load(0, lane, x);
 #pragma unroll
@@ -337,36 +362,62 @@ __global__ void __launch_bounds__(kGroupThreads) k_sample_groups(SampleArgs a) {
         __syncthreads();
     }
     const int32_t j0 = int32_t(blockIdx.x) * a.chunk, j1 = min(a.G, j0 + a.chunk);
-    for (int32_t j = j0 + warp; j < j1; j += kGroupThreads / 32) {
-        float x[8], m = -INFINITY;
-        load(j, lane, x);
+    float2 *stats = a.stats + int64_t(b) * a.G;
+    for (int32_t j = j0 + warp * kQuad; j < j1; j += kGroupThreads / 32 * kQuad) {
+        float x[kQuad][8], m[kQuad], sum[kQuad];
+        if (load.allow.kind != kAllowAll) {  // most words of a mask are empty: a lane a word of the four groups
+            const int64_t w = int64_t(j) * (kGroup / 32) + lane;
+            if (!__any_sync(~0u, w < a.g.W && load.allow.word(int32_t(w)))) {
+                if (lane < kQuad && j + lane < j1) stats[j + lane] = make_float2(-INFINITY, 0.0f);
+                continue;
+            }
+        }
 #pragma unroll
-        for (int i = 0; i < 8; i++) m = fmaxf(m, x[i]);
-        m = warp_max(m);
-        float sum = 0.0f;
-        if (m > -INFINITY) {
+        for (int g = 0; g < kQuad; g++) load(min(j + g, a.G - 1), lane, x[g]);
 #pragma unroll
-            for (int i = 0; i < 8; i++) sum += x[i] == m ? 1.0f : exp2_fast((x[i] - m) * c);
-            sum = warp_sum(sum);
-            if (binned) {
+        for (int g = 0; g < kQuad; g++) {
+            m[g] = fmaxf(fmaxf(fmaxf(x[g][0], x[g][1]), fmaxf(x[g][2], x[g][3])),
+                         fmaxf(fmaxf(x[g][4], x[g][5]), fmaxf(x[g][6], x[g][7])));
+            m[g] = warp_max(m[g]);
+            sum[g] = 0.0f;
+            if (fabsf(m[g]) <= 3.0e38f) {
+#pragma unroll
+                for (int i = 0; i < 8; i++) sum[g] += exp2_fast((x[g][i] - m[g]) * c);
+            } else if (m[g] > 0.0f) {  // an infinite one: those share the weight
+#pragma unroll
+                for (int i = 0; i < 8; i++) sum[g] += x[g][i] == m[g] ? 1.0f : 0.0f;
+            } else if (m[g] > -INFINITY) {
+#pragma unroll
+                for (int i = 0; i < 8; i++) sum[g] += x[g][i] == m[g] ? 1.0f : exp2_fast((x[g][i] - m[g]) * c);
+            }
+        }
+        const float total = warp_sum4(sum, lane);
+        const int mine = quad_of(lane);
+        if ((lane & 7) == 0 && j + mine < j1)
+            stats[j + mine] = make_float2(mine & 2 ? (mine & 1 ? m[3] : m[2]) : (mine & 1 ? m[1] : m[0]), total);
+        if (binned) {
+#pragma unroll
+            for (int g = 0; g < kQuad; g++) {
+                if (j + g >= j1) break;
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
-                    if (x[i] == -INFINITY) continue;
-                    const float place = bins.place(x[i]);
-                    const int32_t bin = bins.bin(x[i]);
-                    atomicAdd(&hist[0][bin], 1u);
+                    if (x[g][i] == -INFINITY) continue;
+                    const float place = bins.place(x[g][i]);
+                    const int32_t bin = bins.bin(x[g][i]);
+                    if (way.k) atomicAdd(&hist[bin], 1u);
                     // the weight relative to the bin's upper end: at most 2^16, 2^15 tokens a CTA
-                    const float w = exp2_fast((float(bin) - place) * (c / kBinsPerUnit));
-                    atomicAdd(&hist[1][bin], uint32_t(fminf(w, 1.0f) * 65535.0f + 0.5f));
+                    if (way.p < 1.0f) {
+                        const float w = exp2_fast((float(bin) - place) * (c / kBinsPerUnit));
+                        atomicAdd(&hist[kBins + bin], uint32_t(fminf(w, 1.0f) * 65535.0f + 0.5f));
+                    }
                 }
             }
         }
-        if (lane == 0) a.stats[int64_t(b) * a.G + j] = make_float2(m, sum);
     }
     if (binned) {
         __syncthreads();
         uint4 *to = reinterpret_cast<uint4 *>(a.hist + (int64_t(b) * a.parts + blockIdx.x) * 2 * kBins);
-        for (int i = threadIdx.x; i < 2 * kBins / 4; i += kGroupThreads) to[i] = reinterpret_cast<uint4 *>(hist[0])[i];
+        for (int i = threadIdx.x; i < 2 * kBins / 4; i += kGroupThreads) to[i] = reinterpret_cast<uint4 *>(hist)[i];
     }
 }
 
@@ -375,7 +426,7 @@ __global__ void __launch_bounds__(kGroupThreads) k_sample_groups(SampleArgs a) {
 // A lower bound of the m-th largest group maximum (m >= 1), and so of the m-th
 // largest logit, as a key; kKeyNone when fewer groups have a token. `low`: the
 // smallest maximum of those that have.
-__device__ uint32_t nth_group(Shared &s, const float2 *stats, int32_t G, int32_t m, float M, float low) {
+__device__ __forceinline__ uint32_t nth_group(Shared &s, const float2 *stats, int32_t G, int32_t m, float M, float low) {
     constexpr int kPer = kBins / kThreads;
     if (!(M <= 3.0e38f && low >= -3.0e38f) || low == M) return order_key(low);
     const float per = float(kBins - 1) / (M - low);
@@ -414,13 +465,15 @@ __device__ uint32_t nth_group(Shared &s, const float2 *stats, int32_t G, int32_t
     return order_key(fmaxf(low, edge - 1e-6f * (fabsf(M) + fabsf(low))));
 }
 
-// Appends the tokens of group j whose bit of `in` is set to s.list (x: the
-// lane's eight logits); s.n counts on past kList.
+// Appends the tokens of the groups j whose bits of `in` are set to s.list (x: the
+// lane's eight logits of each); s.n counts on past kList.
 template <typename T>
-__device__ __forceinline__ void append(Shared &s, const GroupLoad<T> &load, int32_t j, const float (&x)[8], uint32_t in,
-                                       int lane) {
-    if (!__any_sync(~0u, in)) return;
-    const int32_t mine = __popc(in);
+__device__ __forceinline__ void append(Shared &s, const GroupLoad<T> &load, const int32_t (&j)[kPair],
+                                       const float (&x)[kPair][8], const uint32_t (&in)[kPair], int lane) {
+    int32_t mine = 0;
+#pragma unroll
+    for (int g = 0; g < kPair; g++) mine += __popc(in[g]);
+    if (!__any_sync(~0u, mine)) return;
     int32_t upto = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -430,37 +483,49 @@ __device__ __forceinline__ void append(Shared &s, const GroupLoad<T> &load, int3
     int32_t at = 0;
     if (lane == 31) at = atomicAdd(&s.n, upto);
     at = __shfl_sync(~0u, at, 31) + upto - mine;
+    if (!mine) return;
 #pragma unroll
-    for (int i = 0; i < 8; i++)
-        if ((in >> i) & 1u) {
-            if (at < kList)
-                s.list[at] = (uint64_t(order_key(x[i] + 0.0f)) << 32) | uint32_t(~uint32_t(j * kGroup + load.id(i, lane)));
-            at++;
-        }
+    for (int g = 0; g < kPair; g++)
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            if ((in[g] >> i) & 1u) {
+                if (at < kList)
+                    s.list[at] = (uint64_t(order_key(x[g][i] + 0.0f)) << 32) | uint32_t(~uint32_t(j[g] * kGroup + load.id(i, lane)));
+                at++;
+            }
 }
 
 // Collects every allowed token with order_key >= key into s.list; returns how
 // many there are (more than kList: only that many were stored).
 template <typename T>
-__device__ int32_t collect(Shared &s, const GroupLoad<T> &load, const float2 *stats, int32_t G, uint32_t key) {
-    const int lane = threadIdx.x & 31;
+__device__ __forceinline__ int32_t collect(Shared &s, const GroupLoad<T> &load, const float2 *stats, int32_t G, uint32_t key) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     __syncthreads();
     if (threadIdx.x == 0) s.n = 0;
     __syncthreads();
-    // a warp looks at 32 groups' maxima at a time
-    for (int32_t j0 = int32_t(threadIdx.x >> 5); j0 * 32 < G; j0 += kWarps) {
-        const int32_t mine = j0 * 32 + lane;
+    // a warp looks at 32 groups' maxima at a time, every 16th group so that crowds are shared
+    for (int32_t j0 = 0; j0 < G; j0 += 32 * kWarps) {
+        const int32_t mine = j0 + lane * kWarps + warp;
         uint32_t todo = __ballot_sync(~0u, mine < G && order_key(stats[mine].x) >= key);
         while (todo) {
-            const int32_t j = j0 * 32 + __ffs(todo) - 1;
-            todo &= todo - 1;
-            float x[8];
-            load(j, lane, x);
-            uint32_t in = 0;
+            int32_t j[kPair];
+            float x[kPair][8];
+            uint32_t in[kPair] = {}, left = todo;
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const uint32_t k = order_key(x[i] + 0.0f);
-                in |= uint32_t(k >= key && k > kKeyNone) << i;
+            for (int g = 0; g < kPair; g++) {
+                j[g] = left ? j0 + (__ffs(left) - 1) * kWarps + warp : -1;
+                left &= left - 1;
+                if (j[g] >= 0) load(j[g], lane, x[g]);
+            }
+            todo = left;
+#pragma unroll
+            for (int g = 0; g < kPair; g++) {
+                if (j[g] < 0) continue;
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const uint32_t k = order_key(x[g][i] + 0.0f);
+                    in[g] |= uint32_t(k >= key && k > kKeyNone) << i;
+                }
             }
             append(s, load, j, x, in, lane);
         }
@@ -469,17 +534,21 @@ __device__ int32_t collect(Shared &s, const GroupLoad<T> &load, const float2 *st
     return s.n;
 }
 
-// Sorts s.list[0, n) in descending order: by each entry's rank where few, else
-// by a bitonic network over the next power of two.
-__device__ void sort_list(Shared &s, int32_t n) {
+// Sorts s.list[0, n) in descending order: by each entry's rank where few, with
+// up to 16 threads an entry, else by a bitonic network over the next power of two.
+__device__ __forceinline__ void sort_list(Shared &s, int32_t n) {
     if (n <= kThreads) {
+        int32_t each = 16;  // threads an entry
+        while (each > 1 && n * each > kThreads) each >>= 1;
+        const int32_t at = int32_t(threadIdx.x) / each, part = int32_t(threadIdx.x) & (each - 1);
         __syncthreads();
-        const unsigned long long mine = int32_t(threadIdx.x) < n ? s.list[threadIdx.x] : 0ull;
+        const unsigned long long mine = at < n ? s.list[at] : 0ull;
         int32_t rank = 0;
-        if (int32_t(threadIdx.x) < n)
-            for (int32_t i = 0; i < n; i++) rank += s.list[i] > mine;
+        if (at < n)
+            for (int32_t i = part; i < n; i += each) rank += s.list[i] > mine;
+        for (int32_t d = each >> 1; d; d >>= 1) rank += __shfl_xor_sync(~0u, rank, d);
         __syncthreads();
-        if (int32_t(threadIdx.x) < n) s.list[rank] = mine;
+        if (at < n && part == 0) s.list[rank] = mine;
         __syncthreads();
         return;
     }
@@ -502,15 +571,19 @@ __device__ void sort_list(Shared &s, int32_t n) {
     __syncthreads();
 }
 
+__device__ __forceinline__ int32_t list_id(unsigned long long e) { return int32_t(~uint32_t(e)); }
 __device__ __forceinline__ float list_value(unsigned long long e) { return key_value(uint32_t(e >> 32)); }
 
-// s.before[i] = weight of s.list[0, i); returns the whole list's weight. One
-// thread's share is consecutive entries, so the sums' order is fixed.
-__device__ float scan_list(Shared &s, int32_t n, float M, float T) {
+// s.weight[i] = weight of s.list[i], s.before[i] = that of s.list[0, i); returns
+// the whole list's weight. One thread's share is consecutive entries, so the
+// sums' order is fixed.
+__device__ __forceinline__ float scan_list(Shared &s, int32_t n, float M, float T) {
+    for (int32_t i = threadIdx.x; i < n; i += kThreads) s.weight[i] = weight(list_value(s.list[i]), M, T);
+    __syncthreads();
     const int32_t per = (n + kThreads - 1) / kThreads, first = int32_t(threadIdx.x) * per;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     float sum = 0.0f;
-    for (int32_t i = first; i < min(n, first + per); i++) sum += weight(list_value(s.list[i]), M, T);
+    for (int32_t i = first; i < min(n, first + per); i++) sum += s.weight[i];
     float upto = sum;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -519,18 +592,17 @@ __device__ float scan_list(Shared &s, int32_t n, float M, float T) {
     }
     float before = __shfl_up_sync(~0u, upto, 1);
     if (lane == 0) before = 0.0f;
-    __syncthreads();
     if (lane == 31) s.f[warp] = upto;
     __syncthreads();
-    float base = 0.0f, total = 0.0f;
+    float total = 0.0f;
+#pragma unroll
     for (int i = 0; i < kWarps; i++) {
-        if (i < warp) base += s.f[i];
+        if (i == warp) before += total;
         total += s.f[i];
     }
-    before += base;
     for (int32_t i = first; i < min(n, first + per); i++) {
         s.before[i] = before;
-        before += weight(list_value(s.list[i]), M, T);
+        before += s.weight[i];
     }
     __syncthreads();
     return total;
@@ -538,13 +610,13 @@ __device__ float scan_list(Shared &s, int32_t n, float M, float T) {
 
 // How many of the first n entries of the sorted, scanned list are kept: those
 // before which the weight, `above` included, is below target, with w >= min_p.
-__device__ int32_t cut_list(Shared &s, int32_t n, float above, float target, const Way &way, float M) {
+__device__ __forceinline__ int32_t cut_list(Shared &s, int32_t n, float above, float target, const Way &way) {
     __syncthreads();
     if (threadIdx.x == 0) s.n = 0;
     __syncthreads();
     int32_t last = 0;
     for (int32_t i = threadIdx.x; i < n; i += kThreads)
-        if (above + s.before[i] < target && weight(list_value(s.list[i]), M, way.T) >= way.min_p) last = i + 1;
+        if (above + s.before[i] < target && s.weight[i] >= way.min_p) last = i + 1;
     if (last) atomicMax(&s.n, last);
     __syncthreads();
     n = s.n;
@@ -553,11 +625,21 @@ __device__ int32_t cut_list(Shared &s, int32_t n, float above, float target, con
 }
 
 // The group drawn: of the first n entries of the list and, when `above`, what
-// stats[j].y holds of each group's weight besides. Reorders the n entries by
-// ascending id, as id << 32 | order_key.
-__device__ int32_t draw_group(Shared &s, int32_t n, bool above, const float2 *stats, int32_t G, float M, float T,
+// stats[j].y holds of each group's weight besides. Unless they are few, reorders
+// the n entries by ascending id, as ~id << 32 | order_key.
+__device__ __forceinline__ int32_t draw_group(Shared &s, int32_t n, bool above, const float2 *stats, int32_t G, float M, float T,
                               int64_t seed) {
     __syncthreads();
+    if (n <= kSmallK && !above) {  // few enough to look at all for each
+        Best best = {-INFINITY, -1};
+        if (int32_t(threadIdx.x) < n) {
+            const int32_t group = list_id(s.list[threadIdx.x]) / kGroup;
+            float mass = 0.0f;
+            for (int32_t i = 0; i < n; i++) mass += list_id(s.list[i]) / kGroup == group ? s.weight[i] : 0.0f;
+            best = {logf(mass) + gumbel(seed, 0x80000000ull + uint32_t(group)), group};
+        }
+        return block_best(s, best).id;
+    }
     for (int32_t i = threadIdx.x; i < n; i += kThreads) s.list[i] = (s.list[i] << 32) | (s.list[i] >> 32);
     __syncthreads();
     sort_list(s, n);  // ~id descending
@@ -583,8 +665,8 @@ __device__ int32_t draw_group(Shared &s, int32_t n, bool above, const float2 *st
 // with w >= min_p, *n and *mass the number and weight of all of those. Returns
 // the list's length.
 template <typename T>
-__device__ int32_t split_at(Shared &s, const GroupLoad<T> &load, float2 *stats, int32_t G, const Bins &bins, int32_t first,
-                            int32_t last, const Way &way, float M, int32_t *n, float *mass) {
+__device__ __forceinline__ int32_t split_at(Shared &s, const GroupLoad<T> &load, float2 *stats, int32_t G, const Bins &bins, int32_t first,
+                            int32_t last, const Way &way, float M, int32_t &n, float &mass) {
     const int lane = threadIdx.x & 31;
     const float c = __fdiv_rn(kLog2e, way.T);
     __syncthreads();
@@ -592,46 +674,58 @@ __device__ int32_t split_at(Shared &s, const GroupLoad<T> &load, float2 *stats, 
     __syncthreads();
     int32_t count = 0;
     float sum = 0.0f;
-    for (int32_t j0 = int32_t(threadIdx.x >> 5); j0 * 32 < G; j0 += kWarps) {
-        const int32_t mine = j0 * 32 + lane;
+    const int warp = threadIdx.x >> 5;
+    for (int32_t j0 = 0; j0 < G; j0 += 32 * kWarps) {
+        const int32_t mine = j0 + lane * kWarps + warp;
         const float top = mine < G ? stats[mine].x : -INFINITY;
-        uint32_t todo = __ballot_sync(~0u, top > -INFINITY && bins.bin(top) <= last);
+        // groups that reach neither the bins nor, where nothing but min_p counts, its weight hold nothing
+        uint32_t todo = __ballot_sync(~0u, top > -INFINITY && bins.bin(top) <= last &&
+                                               (first < kBins || top == M || exp2_fast((top - M) * c) >= way.min_p));
         float kept = 0.0f;  // of group `mine`
         while (todo) {
-            const int at = __ffs(todo) - 1;
-            const int32_t j = j0 * 32 + at;
-            todo &= todo - 1;
-            float x[8], all = 0.0f, of = 0.0f;
-            load(j, lane, x);
-            uint32_t in = 0;
+            int32_t j[kPair], at[kPair];
+            float x[kPair][8], of[kPair] = {};
+            uint32_t in[kPair] = {};
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const int32_t bin = bins.bin(x[i]);
-                if (x[i] > -INFINITY && bin <= last) {
+            for (int g = 0; g < kPair; g++) {
+                at[g] = todo ? __ffs(todo) - 1 : -1;
+                j[g] = todo ? j0 + at[g] * kWarps + warp : -1;
+                todo &= todo - 1;
+                if (j[g] >= 0) load(j[g], lane, x[g]);
+            }
+#pragma unroll
+            for (int g = 0; g < kPair; g++) {
+                if (j[g] < 0) continue;
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const int32_t bin = bins.bin(x[g][i]);
+                    if (bin > last || x[g][i] == -INFINITY) continue;
                     if (bin >= first) {
-                        in |= 1u << i;
+                        in[g] |= 1u << i;
                     } else {
-                        const float w = x[i] == M ? 1.0f : exp2_fast((x[i] - M) * c);
+                        const float w = x[g][i] == M ? 1.0f : exp2_fast((x[g][i] - M) * c);
                         count++;
-                        all += w;
-                        if (w >= way.min_p) of += w;
+                        sum += w;
+                        if (w >= way.min_p) of[g] += w;
                     }
                 }
             }
-            sum += all;
-            of = warp_sum(of);
-            if (lane == at) kept = of;
+#pragma unroll
+            for (int g = 0; g < kPair; g++) {
+                const float of_g = warp_sum(of[g]);
+                if (lane == at[g]) kept = of_g;
+            }
             append(s, load, j, x, in, lane);
         }
         if (mine < G) stats[mine].y = kept;
     }
-    *n = block_sum(s, count);
-    *mass = block_sum(s, sum);
+    n = block_sum(s, count);
+    mass = block_sum(s, sum);
     return s.n;
 }
 
 // Adds up the row's histograms in s.hist, weights relative to M.
-__device__ void sum_hist(Shared &s, const uint32_t *hist, int32_t parts, const Bins &bins, const Way &way, float M) {
+__device__ __forceinline__ void sum_hist(Shared &s, const uint32_t *hist, int32_t parts, const Bins &bins, const Way &way, float M) {
     constexpr int kPer = kBins / kThreads;
     static_assert(kPer == 4, "one 16-byte load a thread and part");
     const float c = __fdiv_rn(kLog2e, way.T);
@@ -649,14 +743,14 @@ __device__ void sum_hist(Shared &s, const uint32_t *hist, int32_t parts, const B
         const int bin = int(threadIdx.x) * kPer + i;
         const float end = bins.top - float(bin) / kBinsPerUnit;
         s.hist.count[bin] = count[i];
-        s.hist.mass[bin] = count[i] ? mass[i] / 65535.0f * exp2_fast((end - M) * c) : 0.0f;
+        s.hist.mass[bin] = mass[i] > 0.0f ? mass[i] / 65535.0f * exp2_fast((end - M) * c) : 0.0f;
     }
     __syncthreads();
 }
 
 // The bins [s.bin[0], s.bin[1]] in which the kept set ends: by count exactly, by
 // weight to within the histogram's precision. kBins: none found.
-__device__ void find_bins(Shared &s, bool by_mass, int32_t count, float target) {
+__device__ __forceinline__ void find_bins(Shared &s, bool by_mass, int32_t count, float target) {
     constexpr int kPer = kBins / kThreads;
     constexpr float kSlack = 1e-4f;  // weights in the histogram are rounded to 2^-16
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -715,7 +809,7 @@ struct Cut {
 // The shortest prefix with `count` tokens (by_mass false) or a weight of at
 // least target / 2^40 (by_mass true); everything when there is none.
 template <typename T>
-__device__ Cut radix_cut(Shared &s, const Row<T> &row, const float2 *stats, int32_t G, float M, float T_, bool by_mass,
+__device__ __noinline__ Cut radix_cut(Shared &s, const Row<T> &row, const float2 *stats, int32_t G, float M, float T_, bool by_mass,
                          uint32_t count, unsigned long long target) {
     uint32_t key = 0u;
     unsigned long long above_n = 0ull, above_mass = 0ull;
@@ -807,7 +901,7 @@ __device__ Cut radix_cut(Shared &s, const Row<T> &row, const float2 *stats, int3
 
 // The id of the cut.ties-th token at cut.key.
 template <typename T>
-__device__ int32_t last_tie(Shared &s, const Row<T> &row, float2 *stats, int32_t G, const Cut &cut) {
+__device__ __noinline__ int32_t last_tie(Shared &s, const Row<T> &row, float2 *stats, int32_t G, const Cut &cut) {
     const int lane = threadIdx.x & 31;
     for (int32_t j = threadIdx.x >> 5; j < G; j += kWarps) {
         int32_t n = 0;
@@ -876,7 +970,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_pick(SampleArgs a) {
         M = fmaxf(M, x);
         if (x > -INFINITY) low = fminf(low, x);
     }
-    M = block_max(s, M);
+    block_range(s, M, low);
     if (M == -INFINITY) {
         if (threadIdx.x == 0) {
             a.tokens[b] = -1;
@@ -884,7 +978,6 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_pick(SampleArgs a) {
         }
         return;
     }
-    low = -block_max(s, -low);
     float Z = 0.0f;
     for (int32_t j = threadIdx.x; j < G; j += kThreads) {
         const float2 g = stats[j];
@@ -892,81 +985,63 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_pick(SampleArgs a) {
     }
     Z = block_sum(s, Z);
 
-    const bool by_k = !way.greedy && way.k > 0, by_p = !way.greedy && way.p < 1.0f;
-    const bool filtered = by_k || by_p || (!way.greedy && way.min_p > 0.0f);
+    const bool by_p = !way.greedy && way.p < 1.0f, by_min = !way.greedy && way.min_p > 0.0f;
+    bool by_k = !way.greedy && way.k > 0;
     int32_t group = -1;         // of the token, once drawn
     // what is kept, min_p aside: tokens at or above `last` (order_key << 32 | ~id), and those of bins before bins_kept
     unsigned long long last = 0ull;
     int32_t bins_kept = 0;
     const Bins bins(stats[0].x);
-    if (by_k && !wants_hist(way, a.G)) {
-        const uint32_t from = nth_group(s, stats, G, way.k, M, low);
-        const int32_t n = collect(s, load, stats, G, from);
-        if (n <= kList) {
-            sort_list(s, n);
-            const float total = scan_list(s, n, M, way.T);
-            const int32_t first = min(way.k, n);
-            const float target = by_p ? way.p * (first < n ? s.before[first] : total) : INFINITY;
-            const int32_t kept = max(1, cut_list(s, first, 0.0f, target, way, M));
-            last = s.list[kept - 1];
-            group = draw_group(s, kept, false, stats, G, M, way.T, seed);
-        }
-    } else if (wants_hist(way, a.G)) {
-        const uint32_t *hist = a.hist + int64_t(b) * a.parts * 2 * kBins;
-        float target = INFINITY, above = 0.0f, Zk = Z;
-        int32_t first = -1, end = -1, n = 0, n_above = 0, kept = 0;
-        bool done = true;
-        if (by_k) {
-            sum_hist(s, hist, a.parts, bins, way, M);
-            find_bins(s, false, way.k, 0.0f);
-            first = end = s.bin[0];
-            if (first < kBins) {
-                n = split_at(s, load, stats, G, bins, first, end, way, M, &n_above, &above);
-                done = n <= kList;
-                if (done) {
-                    sort_list(s, n);
-                    const float total = scan_list(s, n, M, way.T);
-                    kept = min(n, way.k - n_above);
-                    Zk = above + (kept < n ? s.before[kept] : total);
-                    if (!by_p) kept = cut_list(s, kept, 0.0f, INFINITY, way, M);
+    enum { kSmall, kCount, kMass, kLeast, kNone };  // how the kept set is found: few by count, by count, by weight, min_p alone
+    float target = way.p * Z;
+    int step = by_k ? (wants_hist(way, G) ? kCount : kSmall) : by_p ? kMass : by_min ? kLeast : kNone;
+    while (step != kNone) {
+        int32_t first = kBins, end = kBins, n = 0, n_above = 0, kept = 0;
+        float above = 0.0f;
+        if (step == kSmall) {
+            n = collect(s, load, stats, G, nth_group(s, stats, G, way.k, M, low));
+        } else {
+            if (step != kLeast) {
+                sum_hist(s, a.hist + int64_t(b) * a.parts * 2 * kBins, a.parts, bins, way, M);
+                find_bins(s, step == kMass, way.k, target);
+                first = s.bin[0];
+                end = s.bin[1];
+                if (end >= kBins) {
+                    if (step == kMass) break;
+                    by_k = false;  // fewer tokens than top_k: it keeps all
+                    step = by_p ? kMass : by_min ? kLeast : kNone;
+                    continue;
                 }
-            } else {  // fewer tokens than top_k: all of them
-                done = by_p;
             }
+            n = split_at(s, load, stats, G, bins, first, end, way, M, n_above, above);
         }
-        if (done && by_p) {
-            target = way.p * Zk;
-            sum_hist(s, hist, a.parts, bins, way, M);
-            find_bins(s, true, 0, target);
-            first = s.bin[0];
-            end = s.bin[1];
-            done = end < kBins;
-            if (done) {
-                n = split_at(s, load, stats, G, bins, first, end, way, M, &n_above, &above);
-                done = n <= kList;
-            }
-            if (done) {
-                sort_list(s, n);
-                const float total = scan_list(s, n, M, way.T);
-                done = above < target && above + total >= target;
-                if (done) kept = cut_list(s, n, above, target, way, M);
-            }
+        if (n > kList) break;
+        sort_list(s, n);
+        const float total = scan_list(s, n, M, way.T);
+        const int32_t wanted = step == kSmall ? min(way.k, n) : step == kCount ? min(n, way.k - n_above) : n;
+        if (step <= kCount) target = by_p ? way.p * (above + (wanted < n ? s.before[wanted] : total)) : INFINITY;
+        if (step == kCount && by_p) {
+            step = kMass;
+            continue;
         }
-        if (done) {
-            bins_kept = first;
-            last = kept > 0 ? s.list[kept - 1] : ~0ull;
-            group = draw_group(s, kept, true, stats, G, M, way.T, seed);
-        }
+        if (step == kMass && !(above < target && above + total >= target)) break;
+        kept = cut_list(s, wanted, step == kCount ? 0.0f : above, target, way);
+        if (step == kSmall) kept = max(kept, 1);
+        bins_kept = step == kSmall ? 0 : first;
+        last = kept > 0 ? s.list[kept - 1] : ~0ull;
+        group = draw_group(s, kept, step != kSmall, stats, G, M, way.T, seed);
+        break;
     }
+    const bool filtered = by_k || by_p || by_min;
     if (group < 0) {
         Cut cut = {kKeyNone, 0, Z};
         int32_t last_id = 0x7FFFFFFF;
-        if (by_k) cut = radix_cut(s, row, stats, G, M, way.T, false, uint32_t(way.k), 0ull);
-        if (by_p) {
-            const double target = double(way.p) * double(cut.mass) * kFixed;
-            const Cut c = radix_cut(s, row, stats, G, M, way.T, true, 0u,
-                                    target > 0.0 ? (unsigned long long)(target) : 0ull);
-            if (!by_k || c.key > cut.key || (c.key == cut.key && c.ties < cut.ties)) cut = c;
+        for (int by = 0; by < 2; by++) {
+            if (by ? !by_p : !by_k) continue;
+            const double to = double(way.p) * double(cut.mass) * kFixed;
+            const Cut c = radix_cut(s, row, stats, G, M, way.T, by == 1, uint32_t(way.k),
+                                    to > 0.0 ? (unsigned long long)(to) : 0ull);
+            if (by == 0 || !by_k || c.key > cut.key || (c.key == cut.key && c.ties < cut.ties)) cut = c;
         }
         if (by_k || by_p) {
             last_id = last_tie(s, row, stats, G, cut);
