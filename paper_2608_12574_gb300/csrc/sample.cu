@@ -51,8 +51,8 @@ constexpr int kSmallK = 64;         // largest top-k that goes without a histogr
 constexpr int kBins = 2048;
 constexpr float kBinsPerUnit = 32.0f;
 constexpr int kChunk = 128;         // most groups of a CTA of k_sample_groups
-constexpr int kQuad = 4;            // groups that a warp of k_sample_groups takes at a time
-constexpr int kPair = 2;            // of k_sample_pick
+constexpr int kPair = 2;            // groups that a warp of k_sample_groups takes at a time
+constexpr int kQuad = 4;            // and of k_sample_pick
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr uint32_t kKeyNone = 0x007FFFFFu;  // order_key(-inf)
 constexpr double kFixed = 1099511627776.0;  // 2^40
@@ -264,51 +264,75 @@ __device__ __forceinline__ int32_t block_sum(Shared &s, int32_t x) {
     return __reduce_add_sync(~0u, (threadIdx.x & 31) < kWarps ? s.i[threadIdx.x & 15] : 0);
 }
 
-// The sums over the warp of four values, in six exchanges: every lane ends with
-// that of value quad_of(lane).
-__device__ __forceinline__ int quad_of(int lane) { return (lane >> 3) & 3; }
-__device__ __forceinline__ float warp_sum4(const float (&v)[kQuad], int lane) {
-    const bool high = lane & 16, odd = lane & 8;
-    const float a = (high ? v[2] : v[0]) + __shfl_xor_sync(~0u, high ? v[0] : v[2], 16);
-    const float b = (high ? v[3] : v[1]) + __shfl_xor_sync(~0u, high ? v[1] : v[3], 16);
-    float x = (odd ? b : a) + __shfl_xor_sync(~0u, odd ? a : b, 8);
+// The sums over the warp of two values, in five exchanges: that of a in lanes 0
+// to 15, that of b in the others.
+__device__ __forceinline__ float warp_sum2(float a, float b, int lane) {
+    const bool high = lane & 16;
+    float x = (high ? b : a) + __shfl_xor_sync(~0u, high ? a : b, 16);
 #pragma unroll
-    for (int d = 4; d; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
+    for (int d = 8; d; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
     return x;
 }
 
 // A group's logits, eight a lane: token id(i) of the group in x[i], -inf where
-// not allowed or past the end. Rows on 16-byte boundaries without a grammar are
-// read 16 bytes at a time.
+// not allowed or past the end. Whole groups of rows without a grammar are read 16
+// bytes at a time: as they lie where the row is on a 16-byte boundary (kWide);
+// bf16 rows on any other boundary as the two aligned blocks that hold a lane's
+// eight logits, shifted (kShifted: each block read holds a logit of the group,
+// so no read leaves the 16-byte blocks of the row). The rest is read by elements.
+enum : int { kByElement = 0, kWide = 1, kShifted = 2 };
 template <typename T>
 struct GroupLoad {
     const T *x;
     GrammarRow allow;
     int32_t V;
-    bool wide;
+    int mode;
+    int shift;  // kShifted: elements from an aligned block's start to the row's
     __device__ __forceinline__ explicit GroupLoad(const Row<T> &row)
-        : x(row.x), allow(row.allow), V(row.V),
-          wide(row.allow.kind == kAllowAll && (reinterpret_cast<uintptr_t>(row.x) & 15) == 0) {}
+        : x(row.x), allow(row.allow), V(row.V), mode(kByElement), shift(int(reinterpret_cast<uintptr_t>(row.x) & 15) / int(sizeof(T))) {
+        if (row.allow.kind == kAllowAll) mode = shift == 0 ? kWide : sizeof(T) == 2 ? kShifted : kByElement;
+    }
     __device__ __forceinline__ int32_t id(int i, int lane) const {
-        if (!wide) return i * 32 + lane;
+        if (mode == kByElement) return i * 32 + lane;
         return sizeof(T) == 2 ? lane * 8 + i : (i >> 2) * 128 + lane * 4 + (i & 3);
     }
-    __device__ __forceinline__ void operator()(int32_t j, int lane, float (&f)[8]) const {
-        const int64_t v0 = int64_t(j) * kGroup;
-        if (wide && v0 + kGroup <= V) {
-            const uint4 *p = reinterpret_cast<const uint4 *>(x + v0) + lane;
-            if (sizeof(T) == 2) {
-                const uint4 q = __ldg(p);
-                const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    __device__ __forceinline__ bool whole(int32_t j) const { return mode != kByElement && int64_t(j + 1) * kGroup <= V; }
+    // A whole group's blocks (kWide bf16 has one).
+    __device__ __forceinline__ void read(int32_t j, int lane, uint4 (&q)[2]) const {
+        const uint4 *p = reinterpret_cast<const uint4 *>(x + int64_t(j) * kGroup - (mode == kShifted ? shift : 0)) + lane;
+        q[0] = __ldg(p);
+        if (sizeof(T) == 4) q[1] = __ldg(p + 32);
+        else if (mode == kShifted) q[1] = __ldg(p + 1);
+    }
+    __device__ __forceinline__ void decode(const uint4 (&q)[2], float (&f)[8]) const {
+        uint32_t w[8] = {q[0].x, q[0].y, q[0].z, q[0].w, q[1].x, q[1].y, q[1].z, q[1].w};
+        if (sizeof(T) == 4) {
 #pragma unroll
-                for (int i = 0; i < 8; i++) f[i] = __uint_as_float(i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
-            } else {
-                const uint4 q = __ldg(p), r = __ldg(p + 32);
-                const uint32_t w[8] = {q.x, q.y, q.z, q.w, r.x, r.y, r.z, r.w};
+            for (int i = 0; i < 8; i++) f[i] = __uint_as_float(w[i]);
+        } else {
+            if (mode == kShifted) {
+                if (shift & 4) {
 #pragma unroll
-                for (int i = 0; i < 8; i++) f[i] = __uint_as_float(w[i]);
+                    for (int i = 0; i < 6; i++) w[i] = w[i + 2];
+                }
+                if (shift & 2) {
+#pragma unroll
+                    for (int i = 0; i < 5; i++) w[i] = w[i + 1];
+                }
+                if (shift & 1) {
+#pragma unroll
+                    for (int i = 0; i < 4; i++) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+                }
             }
-        } else if (allow.kind == kAllowAll) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) f[i] = __uint_as_float(i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) f[i] = fmaxf(f[i], -INFINITY);  // NaN counts as -inf
+    }
+    __device__ __forceinline__ void by_element(int32_t j, int lane, float (&f)[8]) const {
+        const int64_t v0 = int64_t(j) * kGroup;
+        if (allow.kind == kAllowAll) {
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 const int64_t v = v0 + id(i, lane);
@@ -316,7 +340,7 @@ struct GroupLoad {
             }
         } else {
             const int32_t left = (V - int32_t(v0) + 31) >> 5;  // words of the mask from here on
-            uint32_t words = lane < 8 && lane < left ? allow.word(int32_t(v0 >> 5) + lane) : 0u;
+            const uint32_t words = lane < 8 && lane < left ? allow.word(int32_t(v0 >> 5) + lane) : 0u;
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 const uint32_t word = __shfl_sync(~0u, words, i);
@@ -328,7 +352,16 @@ struct GroupLoad {
             }
         }
 #pragma unroll
-        for (int i = 0; i < 8; i++) f[i] = fmaxf(f[i], -INFINITY);  // NaN counts as -inf
+        for (int i = 0; i < 8; i++) f[i] = fmaxf(f[i], -INFINITY);
+    }
+    __device__ __forceinline__ void operator()(int32_t j, int lane, float (&f)[8]) const {
+        if (whole(j)) {
+            uint4 q[2] = {};
+            read(j, lane, q);
+            decode(q, f);
+        } else {
+            by_element(j, lane, f);
+        }
     }
 };
 
@@ -338,6 +371,23 @@ __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+
+// Sum of exp((x - m) c') of a lane's eight logits, c' in powers of two; an
+// infinite m is shared by the logits that are it.
+__device__ __forceinline__ float lane_weight(const float (&x)[8], float m, float c) {
+    float sum = 0.0f;
+    if (fabsf(m) <= 3.0e38f) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) sum += exp2_fast((x[i] - m) * c);
+    } else if (m > -INFINITY) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) sum += x[i] == m ? 1.0f : exp2_fast((x[i] - m) * c);
+    }
+    return sum;
+}
+__device__ __forceinline__ float lane_max(const float (&x)[8]) {
+    return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
 }
 
 template <typename T>
@@ -354,63 +404,74 @@ __global__ void __launch_bounds__(kGroupThreads) k_sample_groups(SampleArgs a) {
     Bins bins(0.0f);
     if (binned) {
         for (int i = threadIdx.x; i < 2 * kBins; i += kGroupThreads) hist[i] = 0u;
-        float x[8], m = -INFINITY;
+        float x[8];
         load(0, lane, x);
-#pragma unroll
-        for (int i = 0; i < 8; i++) m = fmaxf(m, x[i]);
-        bins = Bins(warp_max(m));
+        bins = Bins(warp_max(lane_max(x)));
         __syncthreads();
     }
+    auto add_bins = [&](const float (&x)[8]) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            if (x[i] == -INFINITY) continue;
+            const float place = bins.place(x[i]);
+            const int32_t bin = bins.bin(x[i]);
+            if (way.k) atomicAdd(&hist[bin], 1u);
+            // the weight relative to the bin's upper end: at most 2^16, 2^15 tokens a CTA
+            if (way.p < 1.0f) {
+                const float w = exp2_fast((float(bin) - place) * (c / kBinsPerUnit));
+                atomicAdd(&hist[kBins + bin], uint32_t(fminf(w, 1.0f) * 65535.0f + 0.5f));
+            }
+        }
+    };
     const int32_t j0 = int32_t(blockIdx.x) * a.chunk, j1 = min(a.G, j0 + a.chunk);
     float2 *stats = a.stats + int64_t(b) * a.G;
-    for (int32_t j = j0 + warp * kQuad; j < j1; j += kGroupThreads / 32 * kQuad) {
-        float x[kQuad][8], m[kQuad], sum[kQuad];
-        if (load.allow.kind != kAllowAll) {  // most words of a mask are empty: a lane a word of the four groups
+    if (load.allow.kind != kAllowAll) {
+        // most words of a mask are empty: a lane a word of four groups
+        for (int32_t j = j0 + warp * 4; j < j1; j += kGroupThreads / 32 * 4) {
             const int64_t w = int64_t(j) * (kGroup / 32) + lane;
-            if (!__any_sync(~0u, w < a.g.W && load.allow.word(int32_t(w)))) {
-                if (lane < kQuad && j + lane < j1) stats[j + lane] = make_float2(-INFINITY, 0.0f);
-                continue;
+            const uint32_t any = __ballot_sync(~0u, w < a.g.W && load.allow.word(int32_t(w)));
+            float2 mine = make_float2(-INFINITY, 0.0f);
+#pragma unroll
+            for (int g = 0; g < 4; g++) {
+                if (!((any >> (8 * g)) & 255u) || j + g >= j1) continue;
+                float x[8];
+                load.by_element(j + g, lane, x);
+                const float m = warp_max(lane_max(x));
+                const float sum = warp_sum(lane_weight(x, m, c));
+                if (lane == g) mine = make_float2(m, sum);
+                if (binned) add_bins(x);
             }
+            if (lane < 4 && j + lane < j1) stats[j + lane] = mine;
         }
+    } else {
+        // two groups a warp, the next two asked for before these are worked on
+        constexpr int kStep = kGroupThreads / 32 * kPair;
+        uint4 q[kPair][2] = {};
+        auto read = [&](int32_t j) {
 #pragma unroll
-        for (int g = 0; g < kQuad; g++) load(min(j + g, a.G - 1), lane, x[g]);
+            for (int g = 0; g < kPair; g++)
+                if (j + g < j1 && load.whole(j + g)) load.read(j + g, lane, q[g]);
+        };
+        int32_t j = j0 + warp * kPair;
+        read(j);
+        for (; j < j1; j += kStep) {
+            float x[kPair][8], m[kPair], sum[kPair];
 #pragma unroll
-        for (int g = 0; g < kQuad; g++) {
-            m[g] = fmaxf(fmaxf(fmaxf(x[g][0], x[g][1]), fmaxf(x[g][2], x[g][3])),
-                         fmaxf(fmaxf(x[g][4], x[g][5]), fmaxf(x[g][6], x[g][7])));
-            m[g] = warp_max(m[g]);
-            sum[g] = 0.0f;
-            if (fabsf(m[g]) <= 3.0e38f) {
-#pragma unroll
-                for (int i = 0; i < 8; i++) sum[g] += exp2_fast((x[g][i] - m[g]) * c);
-            } else if (m[g] > 0.0f) {  // an infinite one: those share the weight
-#pragma unroll
-                for (int i = 0; i < 8; i++) sum[g] += x[g][i] == m[g] ? 1.0f : 0.0f;
-            } else if (m[g] > -INFINITY) {
-#pragma unroll
-                for (int i = 0; i < 8; i++) sum[g] += x[g][i] == m[g] ? 1.0f : exp2_fast((x[g][i] - m[g]) * c);
+            for (int g = 0; g < kPair; g++) {
+                if (load.whole(j + g)) load.decode(q[g], x[g]);
+                else load.by_element(min(j + g, a.G - 1), lane, x[g]);
             }
-        }
-        const float total = warp_sum4(sum, lane);
-        const int mine = quad_of(lane);
-        if ((lane & 7) == 0 && j + mine < j1)
-            stats[j + mine] = make_float2(mine & 2 ? (mine & 1 ? m[3] : m[2]) : (mine & 1 ? m[1] : m[0]), total);
-        if (binned) {
+            read(j + kStep);
 #pragma unroll
-            for (int g = 0; g < kQuad; g++) {
-                if (j + g >= j1) break;
-#pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    if (x[g][i] == -INFINITY) continue;
-                    const float place = bins.place(x[g][i]);
-                    const int32_t bin = bins.bin(x[g][i]);
-                    if (way.k) atomicAdd(&hist[bin], 1u);
-                    // the weight relative to the bin's upper end: at most 2^16, 2^15 tokens a CTA
-                    if (way.p < 1.0f) {
-                        const float w = exp2_fast((float(bin) - place) * (c / kBinsPerUnit));
-                        atomicAdd(&hist[kBins + bin], uint32_t(fminf(w, 1.0f) * 65535.0f + 0.5f));
-                    }
-                }
+            for (int g = 0; g < kPair; g++) {
+                m[g] = warp_max(lane_max(x[g]));
+                sum[g] = lane_weight(x[g], m[g], c);
+            }
+            const float total = warp_sum2(sum[0], sum[1], lane);
+            if ((lane & 15) == 0 && j + (lane >> 4) < j1) stats[j + (lane >> 4)] = make_float2(lane ? m[1] : m[0], total);
+            if (binned) {
+                add_bins(x[0]);
+                if (j + 1 < j1) add_bins(x[1]);
             }
         }
     }
@@ -423,12 +484,13 @@ __global__ void __launch_bounds__(kGroupThreads) k_sample_groups(SampleArgs a) {
 
 // ------------------------------------------------------------ one row's draw
 
-// A lower bound of the m-th largest group maximum (m >= 1), and so of the m-th
-// largest logit, as a key; kKeyNone when fewer groups have a token. `low`: the
+// A lower bound, finite, of the m-th largest group maximum (m >= 1), and so of the
+// m-th largest logit; of every logit when fewer groups have a token. `low`: the
 // smallest maximum of those that have.
-__device__ __forceinline__ uint32_t nth_group(Shared &s, const float2 *stats, int32_t G, int32_t m, float M, float low) {
+__device__ __forceinline__ float nth_group(Shared &s, const float2 *stats, int32_t G, int32_t m, float M, float low) {
     constexpr int kPer = kBins / kThreads;
-    if (!(M <= 3.0e38f && low >= -3.0e38f) || low == M) return order_key(low);
+    constexpr float kLowest = -3.4028234663852886e38f;
+    if (!(M <= 3.0e38f && low >= -3.0e38f) || low == M) return fminf(low, -kLowest);
     const float per = float(kBins - 1) / (M - low);
     __syncthreads();
     for (int i = threadIdx.x; i < kBins; i += kThreads) s.hist.count[i] = 0u;
@@ -459,20 +521,18 @@ __device__ __forceinline__ uint32_t nth_group(Shared &s, const float2 *stats, in
     }
     __syncthreads();
     const int32_t bin = s.bin[0];
-    if (bin >= kBins) return kKeyNone;
+    if (bin >= kBins) return kLowest;
     // every logit of the bin or an earlier one is above this (a unit of rounding further down)
     const float edge = M - float(bin + 1) / per;
-    return order_key(fmaxf(low, edge - 1e-6f * (fabsf(M) + fabsf(low))));
+    return fmaxf(low, edge - 1e-6f * (fabsf(M) + fabsf(low)));
 }
 
-// Appends the tokens of the groups j whose bits of `in` are set to s.list (x: the
-// lane's eight logits of each); s.n counts on past kList.
+// Appends the tokens of the groups j whose bits of `in` are set (bits 8 g .. 8 g +
+// 7: the lane's logits x[g]) to s.list; s.n counts on past kList.
 template <typename T>
-__device__ __forceinline__ void append(Shared &s, const GroupLoad<T> &load, const int32_t (&j)[kPair],
-                                       const float (&x)[kPair][8], const uint32_t (&in)[kPair], int lane) {
-    int32_t mine = 0;
-#pragma unroll
-    for (int g = 0; g < kPair; g++) mine += __popc(in[g]);
+__device__ __forceinline__ void append(Shared &s, const GroupLoad<T> &load, const int32_t (&j)[kQuad],
+                                       const float (&x)[kQuad][8], uint32_t in, int lane) {
+    const int32_t mine = __popc(in);
     if (!__any_sync(~0u, mine)) return;
     int32_t upto = mine;
 #pragma unroll
@@ -483,22 +543,43 @@ __device__ __forceinline__ void append(Shared &s, const GroupLoad<T> &load, cons
     int32_t at = 0;
     if (lane == 31) at = atomicAdd(&s.n, upto);
     at = __shfl_sync(~0u, at, 31) + upto - mine;
-    if (!mine) return;
 #pragma unroll
-    for (int g = 0; g < kPair; g++)
+    for (int g = 0; g < kQuad; g++) {
+        if (!((in >> (8 * g)) & 255u)) continue;
 #pragma unroll
         for (int i = 0; i < 8; i++)
-            if ((in[g] >> i) & 1u) {
+            if ((in >> (8 * g + i)) & 1u) {
                 if (at < kList)
                     s.list[at] = (uint64_t(order_key(x[g][i] + 0.0f)) << 32) | uint32_t(~uint32_t(j[g] * kGroup + load.id(i, lane)));
                 at++;
             }
+    }
 }
 
-// Collects every allowed token with order_key >= key into s.list; returns how
-// many there are (more than kList: only that many were stored).
+// The next four groups of a warp's `todo` (bit i: group j0 + 16 i + warp; -1 where
+// there are no more) and their logits, all asked for before the first is used.
 template <typename T>
-__device__ __forceinline__ int32_t collect(Shared &s, const GroupLoad<T> &load, const float2 *stats, int32_t G, uint32_t key) {
+__device__ __forceinline__ void take_quad(const GroupLoad<T> &load, uint32_t &todo, int32_t j0, int warp, int lane,
+                                          int (&at)[kQuad], int32_t (&j)[kQuad], float (&x)[kQuad][8]) {
+    uint4 q[kQuad][2] = {};
+#pragma unroll
+    for (int g = 0; g < kQuad; g++) {
+        at[g] = __ffs(todo) - 1;
+        todo &= todo - 1;
+        j[g] = at[g] < 0 ? -1 : j0 + at[g] * kWarps + warp;
+        if (j[g] >= 0 && load.whole(j[g])) load.read(j[g], lane, q[g]);
+    }
+#pragma unroll
+    for (int g = 0; g < kQuad; g++) {
+        if (j[g] >= 0 && !load.whole(j[g])) load.by_element(j[g], lane, x[g]);
+        else load.decode(q[g], x[g]);
+    }
+}
+
+// Collects every allowed token with a logit of at least `least` (finite) into
+// s.list; returns how many there are (more than kList: only that many were stored).
+template <typename T>
+__device__ __forceinline__ int32_t collect(Shared &s, const GroupLoad<T> &load, const float2 *stats, int32_t G, float least) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     __syncthreads();
     if (threadIdx.x == 0) s.n = 0;
@@ -506,27 +587,17 @@ __device__ __forceinline__ int32_t collect(Shared &s, const GroupLoad<T> &load, 
     // a warp looks at 32 groups' maxima at a time, every 16th group so that crowds are shared
     for (int32_t j0 = 0; j0 < G; j0 += 32 * kWarps) {
         const int32_t mine = j0 + lane * kWarps + warp;
-        uint32_t todo = __ballot_sync(~0u, mine < G && order_key(stats[mine].x) >= key);
+        uint32_t todo = __ballot_sync(~0u, mine < G && stats[mine].x >= least);
         while (todo) {
-            int32_t j[kPair];
-            float x[kPair][8];
-            uint32_t in[kPair] = {}, left = todo;
+            int at[kQuad];
+            int32_t j[kQuad];
+            float x[kQuad][8];
+            take_quad(load, todo, j0, warp, lane, at, j, x);
+            uint32_t in = 0;
 #pragma unroll
-            for (int g = 0; g < kPair; g++) {
-                j[g] = left ? j0 + (__ffs(left) - 1) * kWarps + warp : -1;
-                left &= left - 1;
-                if (j[g] >= 0) load(j[g], lane, x[g]);
-            }
-            todo = left;
+            for (int g = 0; g < kQuad; g++)
 #pragma unroll
-            for (int g = 0; g < kPair; g++) {
-                if (j[g] < 0) continue;
-#pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    const uint32_t k = order_key(x[g][i] + 0.0f);
-                    in[g] |= uint32_t(k >= key && k > kKeyNone) << i;
-                }
-            }
+                for (int i = 0; i < 8; i++) in |= uint32_t(j[g] >= 0 && x[g][i] >= least) << (8 * g + i);
             append(s, load, j, x, in, lane);
         }
     }
@@ -660,60 +731,67 @@ __device__ __forceinline__ int32_t draw_group(Shared &s, int32_t n, bool above, 
     return block_best(s, best).id;
 }
 
+// The smallest finite value whose bin is at most `last` (bin() does not increase
+// with the value): comparing with it costs less than finding each value's bin.
+__device__ __forceinline__ float bin_floor(const Bins &bins, int32_t last) {
+    const uint32_t lowest = order_key(-3.4028234663852886e38f), highest = order_key(3.4028234663852886e38f);
+    if (last >= kBins - 1) return key_value(lowest);
+    uint32_t lo = lowest, hi = highest;  // bin(lo) > last, or lo is the answer; bin(hi) <= last
+    if (bins.bin(key_value(lo)) <= last) return key_value(lo);
+    while (hi - lo > 1) {
+        const uint32_t mid = lo + (hi - lo) / 2;
+        if (bins.bin(key_value(mid)) <= last) hi = mid;
+        else lo = mid;
+    }
+    return key_value(hi);
+}
+
 // One pass over the groups that reach bin `last`: s.list gets the tokens of bins
 // [first, last], stats[j].y the weight of each group's tokens of earlier bins
-// with w >= min_p, *n and *mass the number and weight of all of those. Returns
-// the list's length.
+// with w >= min_p, n and mass the number and weight of all of those. Returns the
+// list's length.
 template <typename T>
-__device__ __forceinline__ int32_t split_at(Shared &s, const GroupLoad<T> &load, float2 *stats, int32_t G, const Bins &bins, int32_t first,
-                            int32_t last, const Way &way, float M, int32_t &n, float &mass) {
-    const int lane = threadIdx.x & 31;
+__device__ __forceinline__ int32_t split_at(Shared &s, const GroupLoad<T> &load, float2 *stats, int32_t G, const Bins &bins,
+                                            int32_t first, int32_t last, const Way &way, float M, int32_t &n, float &mass) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const float c = __fdiv_rn(kLog2e, way.T);
+    const float least = bin_floor(bins, last), above = bin_floor(bins, first - 1);
     __syncthreads();
     if (threadIdx.x == 0) s.n = 0;
     __syncthreads();
     int32_t count = 0;
     float sum = 0.0f;
-    const int warp = threadIdx.x >> 5;
     for (int32_t j0 = 0; j0 < G; j0 += 32 * kWarps) {
         const int32_t mine = j0 + lane * kWarps + warp;
         const float top = mine < G ? stats[mine].x : -INFINITY;
-        // groups that reach neither the bins nor, where nothing but min_p counts, its weight hold nothing
-        uint32_t todo = __ballot_sync(~0u, top > -INFINITY && bins.bin(top) <= last &&
-                                               (first < kBins || top == M || exp2_fast((top - M) * c) >= way.min_p));
+        // where nothing but min_p counts, groups that do not reach its weight hold nothing
+        uint32_t todo = __ballot_sync(~0u, top >= least && (first < kBins || top == M || exp2_fast((top - M) * c) >= way.min_p));
         float kept = 0.0f;  // of group `mine`
         while (todo) {
-            int32_t j[kPair], at[kPair];
-            float x[kPair][8], of[kPair] = {};
-            uint32_t in[kPair] = {};
+            int at[kQuad];
+            int32_t j[kQuad];
+            float x[kQuad][8];
+            take_quad(load, todo, j0, warp, lane, at, j, x);
+            uint32_t in = 0;
 #pragma unroll
-            for (int g = 0; g < kPair; g++) {
-                at[g] = todo ? __ffs(todo) - 1 : -1;
-                j[g] = todo ? j0 + at[g] * kWarps + warp : -1;
-                todo &= todo - 1;
-                if (j[g] >= 0) load(j[g], lane, x[g]);
-            }
-#pragma unroll
-            for (int g = 0; g < kPair; g++) {
+            for (int g = 0; g < kQuad; g++) {
                 if (j[g] < 0) continue;
+                float of = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
-                    const int32_t bin = bins.bin(x[g][i]);
-                    if (bin > last || x[g][i] == -INFINITY) continue;
-                    if (bin >= first) {
-                        in[g] |= 1u << i;
-                    } else {
+                    if (x[g][i] >= above) {
                         const float w = x[g][i] == M ? 1.0f : exp2_fast((x[g][i] - M) * c);
                         count++;
                         sum += w;
-                        if (w >= way.min_p) of[g] += w;
+                        if (w >= way.min_p) of += w;
+                    } else {
+                        in |= uint32_t(x[g][i] >= least) << (8 * g + i);
                     }
                 }
-            }
-#pragma unroll
-            for (int g = 0; g < kPair; g++) {
-                const float of_g = warp_sum(of[g]);
-                if (lane == at[g]) kept = of_g;
+                if (__any_sync(~0u, of > 0.0f)) {
+                    of = warp_sum(of);
+                    if (lane == at[g]) kept = of;
+                }
             }
             append(s, load, j, x, in, lane);
         }
@@ -731,6 +809,7 @@ __device__ __forceinline__ void sum_hist(Shared &s, const uint32_t *hist, int32_
     const float c = __fdiv_rn(kLog2e, way.T);
     uint32_t count[kPer] = {};
     float mass[kPer] = {};
+#pragma unroll 4
     for (int32_t p = 0; p < parts; p++) {
         const uint4 *at = reinterpret_cast<const uint4 *>(hist + int64_t(p) * 2 * kBins) + threadIdx.x;
         const uint4 n = __ldcg(at), w = __ldcg(at + kBins / 4);
