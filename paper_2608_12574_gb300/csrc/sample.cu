@@ -68,6 +68,7 @@ struct SampleArgs {
     const float *top_p, *min_p;
     Grammar g;
     float2 *stats;            // [B][G] largest logit, sum of weights (relative to it)
+    uint32_t *extra;          // [B][G] weight of a group's kept tokens that stats does not have
     uint32_t *hist;           // [B][parts][2][kBins] counts, weights
     int32_t chunk, parts;     // groups of a CTA, CTAs of a row
     int32_t *tokens;
@@ -190,14 +191,20 @@ __device__ __forceinline__ float warp_sum(float x) {
 }
 
 struct Shared {
-    unsigned long long list[kList];     // order_key << 32 | ~id, or id << 32 | order_key
-    float weight[kList];                // of the list's entries
+    unsigned long long list[kList];     // order_key << 32 | ~id
     union {
-        float before[kList];            // weights of the list before each entry
+        struct {
+            float weight[kList];        // of the list's entries
+            float before[kList];        // of those before each entry
+        };
+        unsigned long long sub[kList];  // a part of the list
         struct {
             uint32_t count[kBins];
             float mass[kBins];
         } hist;
+        struct {
+            uint32_t count[kThreads], mass[kThreads];
+        } fine;
         struct {
             uint32_t count[256];
             unsigned long long mass[256];
@@ -262,6 +269,35 @@ __device__ __forceinline__ int32_t block_sum(Shared &s, int32_t x) {
     if ((threadIdx.x & 31) == 0) s.i[threadIdx.x >> 5] = x;
     __syncthreads();
     return __reduce_add_sync(~0u, (threadIdx.x & 31) < kWarps ? s.i[threadIdx.x & 15] : 0);
+}
+
+// Sums over the threads before this one, of a count and a weight.
+__device__ __forceinline__ void block_scan(Shared &s, int32_t &n, float &m) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int32_t n0 = n;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int32_t y = __shfl_up_sync(~0u, n, d);
+        const float z = __shfl_up_sync(~0u, m, d);
+        if (lane >= d) n += y, m += z;
+    }
+    __syncthreads();
+    if (lane == 31) s.i[warp] = n, s.f[warp] = m;
+    __syncthreads();
+    int32_t nw = s.i[lane & 15];
+    float mw = s.f[lane & 15];
+#pragma unroll
+    for (int d = 1; d < 16; d <<= 1) {
+        const int32_t y = __shfl_up_sync(~0u, nw, d);
+        const float z = __shfl_up_sync(~0u, mw, d);
+        if ((lane & 15) >= d) nw += y, mw += z;
+    }
+    nw = __shfl_sync(~0u, nw, (warp + 15) & 15);
+    mw = __shfl_sync(~0u, mw, (warp + 15) & 15);
+    // before this thread within the warp, and the warps before
+    n += (warp ? nw : 0) - n0;
+    const float upto = __shfl_up_sync(~0u, m, 1);
+    m = (lane ? upto : 0.0f) + (warp ? mw : 0.0f);
 }
 
 // The sums over the warp of two values, in five exchanges: that of a in lanes 0
@@ -484,56 +520,44 @@ __global__ void __launch_bounds__(kGroupThreads) k_sample_groups(SampleArgs a) {
 
 // ------------------------------------------------------------ one row's draw
 
+constexpr float kLowest = -3.4028234663852886e38f;
+
 // A lower bound, finite, of the m-th largest group maximum (m >= 1), and so of the
 // m-th largest logit; of every logit when fewer groups have a token. `low`: the
 // smallest maximum of those that have.
 __device__ __forceinline__ float nth_group(Shared &s, const float2 *stats, int32_t G, int32_t m, float M, float low) {
-    constexpr int kPer = kBins / kThreads;
-    constexpr float kLowest = -3.4028234663852886e38f;
     if (!(M <= 3.0e38f && low >= -3.0e38f) || low == M) return fminf(low, -kLowest);
-    const float per = float(kBins - 1) / (M - low);
+    const float per = float(kThreads - 1) / (M - low);
     __syncthreads();
-    for (int i = threadIdx.x; i < kBins; i += kThreads) s.hist.count[i] = 0u;
+    s.fine.count[threadIdx.x] = 0u;
+    if (threadIdx.x == 0) s.bin[0] = kThreads;
     __syncthreads();
     for (int32_t j = threadIdx.x; j < G; j += kThreads) {
         const float x = stats[j].x;
-        if (x > -INFINITY) atomicAdd(&s.hist.count[min(kBins - 1, int32_t((M - x) * per))], 1u);
+        if (x > -INFINITY) atomicAdd(&s.fine.count[min(kThreads - 1, int32_t((M - x) * per))], 1u);
     }
     __syncthreads();
-    int32_t mine = 0;
-#pragma unroll
-    for (int i = 0; i < kPer; i++) mine += int32_t(s.hist.count[threadIdx.x * kPer + i]);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int32_t upto = mine;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const int32_t y = __shfl_up_sync(~0u, upto, d);
-        if (lane >= d) upto += y;
-    }
-    if (lane == 31) s.i[warp] = upto;
-    if (threadIdx.x == 0) s.bin[0] = kBins;
-    __syncthreads();
-    for (int i = 0; i < warp; i++) upto += s.i[i];
-    if (upto >= m && upto - mine < m) {
-        int32_t n = upto - mine, bin = int32_t(threadIdx.x) * kPer;
-        while ((n += int32_t(s.hist.count[bin])) < m) bin++;
-        s.bin[0] = bin;
-    }
+    const int32_t mine = int32_t(s.fine.count[threadIdx.x]);
+    int32_t before = mine;
+    float none = 0.0f;
+    block_scan(s, before, none);
+    if (before < m && before + mine >= m) s.bin[0] = int32_t(threadIdx.x);
     __syncthreads();
     const int32_t bin = s.bin[0];
-    if (bin >= kBins) return kLowest;
-    // every logit of the bin or an earlier one is above this (a unit of rounding further down)
+    if (bin >= kThreads) return kLowest;
+    // every maximum of the bin or an earlier one is above this (a unit of rounding further down)
     const float edge = M - float(bin + 1) / per;
     return fmaxf(low, edge - 1e-6f * (fabsf(M) + fabsf(low)));
 }
 
-// Appends the tokens of the groups j whose bits of `in` are set (bits 8 g .. 8 g +
-// 7: the lane's logits x[g]) to s.list; s.n counts on past kList.
+// Appends the ids of the tokens of the groups j whose bits of `in` are set (bits
+// 8 g .. 8 g + 7: the lane's logits of group j[g]) to s.list; s.n counts on past
+// kList.
 template <typename T>
-__device__ __forceinline__ void append(Shared &s, const GroupLoad<T> &load, const int32_t (&j)[kQuad],
-                                       const float (&x)[kQuad][8], uint32_t in, int lane) {
+__device__ __forceinline__ void append(Shared &s, const GroupLoad<T> &load, const int32_t (&j)[kQuad], uint32_t in, int lane) {
     const int32_t mine = __popc(in);
-    if (!__any_sync(~0u, mine)) return;
+    const uint32_t who = __ballot_sync(~0u, mine);
+    if (!who) return;
     int32_t upto = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -543,16 +567,19 @@ __device__ __forceinline__ void append(Shared &s, const GroupLoad<T> &load, cons
     int32_t at = 0;
     if (lane == 31) at = atomicAdd(&s.n, upto);
     at = __shfl_sync(~0u, at, 31) + upto - mine;
-#pragma unroll
-    for (int g = 0; g < kQuad; g++) {
-        if (!((in >> (8 * g)) & 255u)) continue;
-#pragma unroll
-        for (int i = 0; i < 8; i++)
-            if ((in >> (8 * g + i)) & 1u) {
-                if (at < kList)
-                    s.list[at] = (uint64_t(order_key(x[g][i] + 0.0f)) << 32) | uint32_t(~uint32_t(j[g] * kGroup + load.id(i, lane)));
-                at++;
-            }
+    for (; in; in &= in - 1, at++) {
+        const int bit = __ffs(in) - 1, g = bit >> 3;
+        const int32_t group = g & 2 ? (g & 1 ? j[3] : j[2]) : (g & 1 ? j[1] : j[0]);
+        if (at < kList) s.list[at] = uint32_t(group * kGroup + load.id(bit & 7, lane));
+    }
+}
+
+// The ids in s.list to entries.
+template <typename T>
+__device__ __forceinline__ void fill_list(Shared &s, const Row<T> &row, int32_t n) {
+    for (int32_t i = threadIdx.x; i < n; i += kThreads) {
+        const uint32_t id = uint32_t(s.list[i]);
+        s.list[i] = (uint64_t(order_key(clean(to_f32(row.x[id])))) << 32) | uint32_t(~id);
     }
 }
 
@@ -598,7 +625,7 @@ __device__ __forceinline__ int32_t collect(Shared &s, const GroupLoad<T> &load, 
             for (int g = 0; g < kQuad; g++)
 #pragma unroll
                 for (int i = 0; i < 8; i++) in |= uint32_t(j[g] >= 0 && x[g][i] >= least) << (8 * g + i);
-            append(s, load, j, x, in, lane);
+            append(s, load, j, in, lane);
         }
     }
     __syncthreads();
@@ -695,40 +722,117 @@ __device__ __forceinline__ int32_t cut_list(Shared &s, int32_t n, float above, f
     return n;
 }
 
-// The group drawn: of the first n entries of the list and, when `above`, what
-// stats[j].y holds of each group's weight besides. Unless they are few, reorders
-// the n entries by ascending id, as ~id << 32 | order_key.
-__device__ __forceinline__ int32_t draw_group(Shared &s, int32_t n, bool above, const float2 *stats, int32_t G, float M, float T,
-                              int64_t seed) {
+// The group drawn by stats[j].y and extra (in units of `unit`).
+__device__ __forceinline__ int32_t draw_group(Shared &s, const float2 *stats, const uint32_t *extra, int32_t G, float unit,
+                                              int64_t seed) {
     __syncthreads();
-    if (n <= kSmallK && !above) {  // few enough to look at all for each
-        Best best = {-INFINITY, -1};
-        if (int32_t(threadIdx.x) < n) {
-            const int32_t group = list_id(s.list[threadIdx.x]) / kGroup;
-            float mass = 0.0f;
-            for (int32_t i = 0; i < n; i++) mass += list_id(s.list[i]) / kGroup == group ? s.weight[i] : 0.0f;
-            best = {logf(mass) + gumbel(seed, 0x80000000ull + uint32_t(group)), group};
-        }
-        return block_best(s, best).id;
-    }
-    for (int32_t i = threadIdx.x; i < n; i += kThreads) s.list[i] = (s.list[i] << 32) | (s.list[i] >> 32);
-    __syncthreads();
-    sort_list(s, n);  // ~id descending
     Best best = {-INFINITY, -1};
-    for (int32_t i = threadIdx.x; i < n; i += kThreads) {
-        const int32_t group = int32_t(~uint32_t(s.list[i] >> 32)) / kGroup;
-        if (i > 0 && int32_t(~uint32_t(s.list[i - 1] >> 32)) / kGroup == group) continue;
-        float mass = above ? stats[group].y : 0.0f;
-        for (int32_t k = i; k < n && int32_t(~uint32_t(s.list[k] >> 32)) / kGroup == group; k++)
-            mass += weight(key_value(uint32_t(s.list[k])), M, T);
-        best = better(best, {logf(mass) + gumbel(seed, 0x80000000ull + uint32_t(group)), group});
+    for (int32_t j = threadIdx.x; j < G; j += kThreads) {
+        const float mass = stats[j].y + float(__ldcg(extra + j)) * unit;
+        if (mass > 0.0f) best = better(best, {logf(mass) + gumbel(seed, 0x80000000ull + uint32_t(j)), j});
     }
-    if (above)  // groups without an entry (one with entries scores more above than it does here)
-        for (int32_t j = threadIdx.x; j < G; j += kThreads) {
-            const float mass = stats[j].y;
-            if (mass > 0.0f) best = better(best, {logf(mass) + gumbel(seed, 0x80000000ull + uint32_t(j)), j});
-        }
     return block_best(s, best).id;
+}
+
+// Of the first n (at most kSmallK) entries of the sorted list, by one warp, an
+// entry a lane and the next 32 in the lane's second place: top-p, min_p, the draw.
+__device__ __forceinline__ int32_t draw_small(Shared &s, int32_t n, const Way &way, float M, int64_t seed, int lane) {
+    float w[2], y[2], before[2];
+    int32_t id[2], group[2];
+    float total = 0.0f;
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+        const int32_t at = h * 32 + lane;
+        const unsigned long long e = at < n ? s.list[at] : 0ull;
+        id[h] = list_id(e);
+        group[h] = at < n ? id[h] / kGroup : -1;
+        y[h] = at < n ? scaled(list_value(e), M, way.T) : -INFINITY;
+        w[h] = at < n ? exp2f(y[h] * kLog2e) : 0.0f;
+        float upto = w[h];
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const float z = __shfl_up_sync(~0u, upto, d);
+            if (lane >= d) upto += z;
+        }
+        const float prev = __shfl_up_sync(~0u, upto, 1);
+        before[h] = total + (lane ? prev : 0.0f);
+        total += __shfl_sync(~0u, upto, 31);
+    }
+    const float target = way.p < 1.0f ? way.p * total : INFINITY;
+    // what is kept is a prefix
+    const uint32_t in0 = __ballot_sync(~0u, lane < n && before[0] < target && w[0] >= way.min_p);
+    const uint32_t in1 = __ballot_sync(~0u, lane + 32 < n && before[1] < target && w[1] >= way.min_p);
+    const int32_t kept = max(1, in1 ? 64 - __clz(in1) : 32 - __clz(in0));
+    float mass[2] = {0.0f, 0.0f};
+    for (int32_t i = 0; i < kept; i++) {
+        const float wi = __shfl_sync(~0u, i < 32 ? w[0] : w[1], i & 31);
+        const int32_t gi = __shfl_sync(~0u, i < 32 ? group[0] : group[1], i & 31);
+        if (group[0] == gi) mass[0] += wi;
+        if (group[1] == gi) mass[1] += wi;
+    }
+    Best best = {-INFINITY, -1};
+#pragma unroll
+    for (int h = 0; h < 2; h++)
+        if (h * 32 + lane < kept)
+            best = better(best, {logf(mass[h]) + gumbel(seed, 0x80000000ull + uint32_t(group[h])), group[h]});
+    const int32_t drawn = warp_best(best).id;
+    best = {-INFINITY, -1};
+#pragma unroll
+    for (int h = 0; h < 2; h++)
+        if (h * 32 + lane < kept && group[h] == drawn) best = better(best, {y[h] + gumbel(seed, uint32_t(id[h])), id[h]});
+    return warp_best(best).id;
+}
+
+// Where the list is long: its tokens from `least` to below `above` are counted and
+// weighed (relative to `top`, the weight at `above`) by 512 equal intervals, the
+// one in which the kept set ends becomes the list, tokens before it go to
+// `extra` (in units of top / 2^20) and to n_above and mass. By count, or by weight
+// (count < 0). Returns the list's length.
+__device__ __forceinline__ int32_t narrow(Shared &s, int32_t n, float least, float above, float top, const Way &way, float M,
+                                          int32_t count, float target, uint32_t *extra, int32_t &n_above, float &mass) {
+    const float c = __fdiv_rn(kLog2e, way.T), per = float(kThreads) / (above - least);
+    __syncthreads();
+    s.fine.count[threadIdx.x] = s.fine.mass[threadIdx.x] = 0u;
+    if (threadIdx.x == 0) s.bin[0] = kThreads, s.ties = 0;
+    __syncthreads();
+    auto place = [&](float x) { return max(0, min(kThreads - 1, int32_t((above - x) * per))); };
+    for (int32_t i = threadIdx.x; i < n; i += kThreads) {
+        const float x = list_value(s.list[i]);
+        const int32_t at = place(x);
+        atomicAdd(&s.fine.count[at], 1u);
+        atomicAdd(&s.fine.mass[at], uint32_t(fminf(exp2_fast((x - above) * c), 1.0f) * 524288.0f + 0.5f));  // kList of them fit
+    }
+    __syncthreads();
+    const int32_t mine = int32_t(s.fine.count[threadIdx.x]);
+    const float weighs = float(s.fine.mass[threadIdx.x]) * (top / 524288.0f);
+    int32_t n_before = mine;
+    float m_before = weighs;
+    block_scan(s, n_before, m_before);
+    const bool reached = count >= 0 ? n_above + n_before + mine >= count : mass + (m_before + weighs) >= target;
+    if (mine && reached) atomicMin(&s.bin[0], int32_t(threadIdx.x));
+    if (mine) atomicMax(&s.ties, int32_t(threadIdx.x));
+    __syncthreads();
+    const int32_t bin = s.bin[0] < kThreads ? s.bin[0] : s.ties;
+    if (int32_t(threadIdx.x) == bin) {
+        s.i[0] = n_before;
+        s.f[0] = m_before;
+    }
+    if (threadIdx.x == 0) s.n = 0;
+    __syncthreads();
+    n_above += s.i[0];
+    mass += s.f[0];
+    for (int32_t i = threadIdx.x; i < n; i += kThreads) {
+        const unsigned long long e = s.list[i];
+        const float x = list_value(e), w = exp2_fast((x - M) * c);
+        const int32_t at = place(x);
+        if (at == bin) s.sub[atomicAdd(&s.n, 1)] = e;
+        else if (at < bin && w >= way.min_p) atomicAdd(extra + list_id(e) / kGroup, uint32_t(w / top * 1048576.0f + 0.5f));
+    }
+    __syncthreads();
+    n = s.n;
+    for (int32_t i = threadIdx.x; i < n; i += kThreads) s.list[i] = s.sub[i];
+    __syncthreads();
+    return n;
 }
 
 // The smallest finite value whose bin is at most `last` (bin() does not increase
@@ -736,6 +840,7 @@ __device__ __forceinline__ int32_t draw_group(Shared &s, int32_t n, bool above, 
 __device__ __forceinline__ float bin_floor(const Bins &bins, int32_t last) {
     const uint32_t lowest = order_key(-3.4028234663852886e38f), highest = order_key(3.4028234663852886e38f);
     if (last >= kBins - 1) return key_value(lowest);
+    if (last < 0) return INFINITY;
     uint32_t lo = lowest, hi = highest;  // bin(lo) > last, or lo is the answer; bin(hi) <= last
     if (bins.bin(key_value(lo)) <= last) return key_value(lo);
     while (hi - lo > 1) {
@@ -746,16 +851,16 @@ __device__ __forceinline__ float bin_floor(const Bins &bins, int32_t last) {
     return key_value(hi);
 }
 
-// One pass over the groups that reach bin `last`: s.list gets the tokens of bins
-// [first, last], stats[j].y the weight of each group's tokens of earlier bins
-// with w >= min_p, n and mass the number and weight of all of those. Returns the
-// list's length.
+// One pass over the groups that reach `least`: s.list gets the ids of the tokens
+// from `least` up to below `above`, stats[j].y the weight of each group's tokens
+// at or above `above` with w >= min_p, n and mass the number and weight of all of
+// those; extra is cleared. all_above: there is no list. Returns the list's length.
 template <typename T>
-__device__ __forceinline__ int32_t split_at(Shared &s, const GroupLoad<T> &load, float2 *stats, int32_t G, const Bins &bins,
-                                            int32_t first, int32_t last, const Way &way, float M, int32_t &n, float &mass) {
+__device__ __forceinline__ int32_t split_at(Shared &s, const GroupLoad<T> &load, float2 *stats, int32_t G,
+                                            float least, float above, bool all_above, const Way &way, float M, uint32_t *extra,
+                                            int32_t &n, float &mass) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const float c = __fdiv_rn(kLog2e, way.T);
-    const float least = bin_floor(bins, last), above = bin_floor(bins, first - 1);
     __syncthreads();
     if (threadIdx.x == 0) s.n = 0;
     __syncthreads();
@@ -765,7 +870,7 @@ __device__ __forceinline__ int32_t split_at(Shared &s, const GroupLoad<T> &load,
         const int32_t mine = j0 + lane * kWarps + warp;
         const float top = mine < G ? stats[mine].x : -INFINITY;
         // where nothing but min_p counts, groups that do not reach its weight hold nothing
-        uint32_t todo = __ballot_sync(~0u, top >= least && (first < kBins || top == M || exp2_fast((top - M) * c) >= way.min_p));
+        uint32_t todo = __ballot_sync(~0u, top >= least && (!all_above || top == M || exp2_fast((top - M) * c) >= way.min_p));
         float kept = 0.0f;  // of group `mine`
         while (todo) {
             int at[kQuad];
@@ -775,27 +880,37 @@ __device__ __forceinline__ int32_t split_at(Shared &s, const GroupLoad<T> &load,
             uint32_t in = 0;
 #pragma unroll
             for (int g = 0; g < kQuad; g++) {
-                if (j[g] < 0) continue;
-                float of = 0.0f;
+                float all = 0.0f, of = 0.0f;
+                uint32_t up = 0;
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
-                    if (x[g][i] >= above) {
-                        const float w = x[g][i] == M ? 1.0f : exp2_fast((x[g][i] - M) * c);
-                        count++;
-                        sum += w;
-                        if (w >= way.min_p) of += w;
-                    } else {
-                        in |= uint32_t(x[g][i] >= least) << (8 * g + i);
-                    }
+                    const bool is_above = j[g] >= 0 && x[g][i] >= above;
+                    float w = exp2_fast((x[g][i] - M) * c);
+                    if (!is_above) w = 0.0f;
+                    up += is_above;
+                    all += w;
+                    of += w >= way.min_p ? w : 0.0f;
+                    in |= uint32_t(j[g] >= 0 && !is_above && x[g][i] >= least) << (8 * g + i);
                 }
+                if (M > 3.0e38f) {  // infinite: those that are it share the weight
+                    all = of = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 8; i++) all += j[g] >= 0 && x[g][i] >= above && x[g][i] == M ? 1.0f : 0.0f;
+                    of = way.min_p <= 1.0f ? all : 0.0f;
+                }
+                count += int32_t(up);
+                sum += all;
                 if (__any_sync(~0u, of > 0.0f)) {
                     of = warp_sum(of);
                     if (lane == at[g]) kept = of;
                 }
             }
-            append(s, load, j, x, in, lane);
+            append(s, load, j, in, lane);
         }
-        if (mine < G) stats[mine].y = kept;
+        if (mine < G) {
+            stats[mine].y = kept;
+            extra[mine] = 0u;
+        }
     }
     n = block_sum(s, count);
     mass = block_sum(s, sum);
@@ -832,7 +947,6 @@ __device__ __forceinline__ void sum_hist(Shared &s, const uint32_t *hist, int32_
 __device__ __forceinline__ void find_bins(Shared &s, bool by_mass, int32_t count, float target) {
     constexpr int kPer = kBins / kThreads;
     constexpr float kSlack = 1e-4f;  // weights in the histogram are rounded to 2^-16
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int32_t n = 0;
     float m = 0.0f;
 #pragma unroll
@@ -840,37 +954,24 @@ __device__ __forceinline__ void find_bins(Shared &s, bool by_mass, int32_t count
         n += int32_t(s.hist.count[threadIdx.x * kPer + i]);
         m += s.hist.mass[threadIdx.x * kPer + i];
     }
-    int32_t n_upto = n;
-    float m_upto = m;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const int32_t y = __shfl_up_sync(~0u, n_upto, d);
-        const float z = __shfl_up_sync(~0u, m_upto, d);
-        if (lane >= d) n_upto += y, m_upto += z;
-    }
-    __syncthreads();
-    if (lane == 31) s.i[warp] = n_upto, s.f[warp] = m_upto;
     if (threadIdx.x == 0) s.bin[0] = s.bin[1] = kBins;
-    __syncthreads();
-    for (int i = 0; i < warp; i++) n_upto += s.i[i], m_upto += s.f[i];
-    n_upto -= n;
-    m_upto -= m;
+    block_scan(s, n, m);
     int32_t lo = kBins, hi = kBins;
 #pragma unroll
     for (int i = 0; i < kPer; i++) {
         const int bin = int(threadIdx.x) * kPer + i;
-        n_upto += int32_t(s.hist.count[bin]);
-        m_upto += s.hist.mass[bin];
+        n += int32_t(s.hist.count[bin]);
+        m += s.hist.mass[bin];
         if (by_mass) {
-            if (lo == kBins && m_upto * (1.0f + kSlack) >= target) lo = bin;
-            if (hi == kBins && m_upto * (1.0f - kSlack) >= target) hi = bin;
-        } else if (lo == kBins && n_upto >= count) {
+            if (lo == kBins && m * (1.0f + kSlack) >= target) lo = bin;
+            if (hi == kBins && m * (1.0f - kSlack) >= target) hi = bin;
+        } else if (lo == kBins && n >= count) {
             lo = hi = bin;
         }
     }
     lo = __reduce_min_sync(~0u, lo);
     hi = __reduce_min_sync(~0u, hi);
-    if (lane == 0) {
+    if ((threadIdx.x & 31) == 0) {
         atomicMin(&s.bin[0], lo);
         atomicMin(&s.bin[1], hi);
     }
@@ -1038,17 +1139,17 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_pick(SampleArgs a) {
     pdl_wait();
     const int32_t b = blockIdx.x, G = a.G;
     const int lane = threadIdx.x & 31;
-    const Way way = row_way(a, b);
-    const Row<T> row = row_at<T>(a, b);
-    const GroupLoad<T> load(row);
     float2 *stats = a.stats + int64_t(b) * G;
-    const int64_t seed = __ldg(a.seeds + b);
     float M = -INFINITY, low = INFINITY;
     for (int32_t j = threadIdx.x; j < G; j += kThreads) {
         const float x = stats[j].x;
         M = fmaxf(M, x);
         if (x > -INFINITY) low = fminf(low, x);
     }
+    const Way way = row_way(a, b);
+    const Row<T> row = row_at<T>(a, b);
+    const GroupLoad<T> load(row);
+    const int64_t seed = __ldg(a.seeds + b);
     block_range(s, M, low);
     if (M == -INFINITY) {
         if (threadIdx.x == 0) {
@@ -1057,58 +1158,78 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_pick(SampleArgs a) {
         }
         return;
     }
+    const float c = __fdiv_rn(kLog2e, way.T);
     float Z = 0.0f;
     for (int32_t j = threadIdx.x; j < G; j += kThreads) {
         const float2 g = stats[j];
-        if (g.x > -INFINITY) Z += g.y * weight(g.x, M, way.T);
+        if (g.x > -INFINITY) Z += g.y * (g.x == M ? 1.0f : exp2_fast((g.x - M) * c));
     }
     Z = block_sum(s, Z);
 
     const bool by_p = !way.greedy && way.p < 1.0f, by_min = !way.greedy && way.min_p > 0.0f;
     bool by_k = !way.greedy && way.k > 0;
     int32_t group = -1;         // of the token, once drawn
-    // what is kept, min_p aside: tokens at or above `last` (order_key << 32 | ~id), and those of bins before bins_kept
+    // what is kept, min_p aside: tokens at or above `last` (order_key << 32 | ~id), and those at or above kept_from
     unsigned long long last = 0ull;
-    int32_t bins_kept = 0;
+    float kept_from = INFINITY;
+    uint32_t *extra = a.extra + int64_t(b) * G;
     const Bins bins(stats[0].x);
     enum { kSmall, kCount, kMass, kLeast, kNone };  // how the kept set is found: few by count, by count, by weight, min_p alone
     float target = way.p * Z;
     int step = by_k ? (wants_hist(way, G) ? kCount : kSmall) : by_p ? kMass : by_min ? kLeast : kNone;
     while (step != kNone) {
-        int32_t first = kBins, end = kBins, n = 0, n_above = 0, kept = 0;
-        float above = 0.0f;
+        int32_t n = 0, n_above = 0, kept = 0;
+        float mass = 0.0f, least = kLowest, above = kLowest, top = 1.0f;
         if (step == kSmall) {
             n = collect(s, load, stats, G, nth_group(s, stats, G, way.k, M, low));
         } else {
             if (step != kLeast) {
                 sum_hist(s, a.hist + int64_t(b) * a.parts * 2 * kBins, a.parts, bins, way, M);
                 find_bins(s, step == kMass, way.k, target);
-                first = s.bin[0];
-                end = s.bin[1];
+                const int32_t first = s.bin[0], end = s.bin[1];
                 if (end >= kBins) {
                     if (step == kMass) break;
                     by_k = false;  // fewer tokens than top_k: it keeps all
                     step = by_p ? kMass : by_min ? kLeast : kNone;
                     continue;
                 }
+                least = bin_floor(bins, end);
+                above = bin_floor(bins, first - 1);
+                if (above < M) top = exp2_fast((above - M) * c);
             }
-            n = split_at(s, load, stats, G, bins, first, end, way, M, n_above, above);
+            n = split_at(s, load, stats, G, least, above, step == kLeast, way, M, extra, n_above, mass);
         }
         if (n > kList) break;
+        fill_list(s, row, n);
+        if (n > kThreads && step != kSmall && above < M)
+            n = narrow(s, n, least, above, top, way, M, step == kCount ? way.k : -1, target, extra, n_above, mass);
         sort_list(s, n);
-        const float total = scan_list(s, n, M, way.T);
-        const int32_t wanted = step == kSmall ? min(way.k, n) : step == kCount ? min(n, way.k - n_above) : n;
-        if (step <= kCount) target = by_p ? way.p * (above + (wanted < n ? s.before[wanted] : total)) : INFINITY;
-        if (step == kCount && by_p) {
-            step = kMass;
-            continue;
+        if (step == kSmall) {
+            if (threadIdx.x >= 32) return;  // one warp does the rest
+            const int32_t token = draw_small(s, min(way.k, n), way, M, seed, lane);
+            if (lane == 0) {
+                a.tokens[b] = token;
+                if (a.logprobs) a.logprobs[b] = scaled(row(token), M, way.T) - logf(Z);
+            }
+            return;
         }
-        if (step == kMass && !(above < target && above + total >= target)) break;
-        kept = cut_list(s, wanted, step == kCount ? 0.0f : above, target, way);
-        if (step == kSmall) kept = max(kept, 1);
-        bins_kept = step == kSmall ? 0 : first;
-        last = kept > 0 ? s.list[kept - 1] : ~0ull;
-        group = draw_group(s, kept, step != kSmall, stats, G, M, way.T, seed);
+        const float total = scan_list(s, n, M, way.T);
+        const int32_t wanted = step == kCount ? min(n, way.k - n_above) : n;
+        if (step == kCount) {
+            target = by_p ? way.p * (mass + (wanted < n ? s.before[wanted] : total)) : INFINITY;
+            if (by_p) {
+                step = kMass;
+                continue;
+            }
+        }
+        if (step == kMass && !(mass < target && mass + total >= target)) break;
+        kept = cut_list(s, wanted, step == kCount ? 0.0f : mass, target, way);
+        kept_from = above;
+        // with none kept of the list (min_p), what lies above its largest
+        last = kept > 0 ? s.list[kept - 1] : n > 0 ? s.list[0] + 1 : ~0ull;
+        for (int32_t i = threadIdx.x; i < kept; i += kThreads)
+            atomicAdd(extra + list_id(s.list[i]) / kGroup, uint32_t(s.weight[i] / top * 1048576.0f + 0.5f));
+        group = draw_group(s, stats, extra, G, top / 1048576.0f, seed);
         break;
     }
     const bool filtered = by_k || by_p || by_min;
@@ -1159,7 +1280,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_pick(SampleArgs a) {
         const float x = v < a.V ? row(int32_t(v)) : -INFINITY;
         if (x > -INFINITY) {
             const unsigned long long entry = (uint64_t(order_key(x)) << 32) | uint32_t(~uint32_t(v));
-            const bool kept = !filtered || ((entry >= last || bins.bin(x) < bins_kept) &&
+            const bool kept = !filtered || ((entry >= last || x >= kept_from) &&
                                             (x == M || weight(x, M, way.T) >= way.min_p));
             if (way.greedy) best = {x, int32_t(v)};
             else if (kept) best = {scaled(x, M, way.T) + gumbel(seed, uint32_t(v)), int32_t(v)};
@@ -1177,13 +1298,14 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_pick(SampleArgs a) {
 // that there are some four CTAs an SM.
 struct Plan {
     int32_t G, chunk, parts;
-    int64_t hist_at, bytes;
+    int64_t extra_at, hist_at, bytes;
     Plan(int32_t B, int32_t V) {
         G = int32_t((int64_t(V) + kGroup - 1) / kGroup);
         chunk = kChunk;
         while (chunk > 16 && int64_t(B) * ((G + chunk - 1) / chunk) < 600) chunk /= 2;
         parts = (G + chunk - 1) / chunk;
-        hist_at = (int64_t(B) * G * int64_t(sizeof(float2)) + 255) / 256 * 256;
+        extra_at = (int64_t(B) * G * int64_t(sizeof(float2)) + 255) / 256 * 256;
+        hist_at = extra_at + (int64_t(B) * G * 4 + 255) / 256 * 256;
         bytes = hist_at + int64_t(B) * parts * 2 * kBins * 4;
     }
 };
@@ -1234,6 +1356,7 @@ extern "C" int trie_sample(const void *d_logits, int dtype, int64_t stride, int3
     a.min_p = d_min_p;
     a.g = make_grammar(d_mask, mask_rows, d_states, V);
     a.stats = static_cast<float2 *>(d_workspace);
+    a.extra = reinterpret_cast<uint32_t *>(static_cast<unsigned char *>(d_workspace) + plan.extra_at);
     a.hist = reinterpret_cast<uint32_t *>(static_cast<unsigned char *>(d_workspace) + plan.hist_at);
     a.tokens = d_tokens;
     a.logprobs = d_logprobs;
