@@ -98,6 +98,11 @@ __device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
+// The object of the CTA of rank `rank` that lies where `object` does in this one's.
+template <typename T>
+__device__ __forceinline__ T *cluster_object(T *object, uint32_t rank) {
+    return static_cast<T *>(__cluster_map_shared_rank(object, rank));
+}
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }

@@ -36,6 +36,7 @@
 
 #include <cuda_runtime.h>
 
+#include "blackwell.cuh"
 #include "logits.cuh"
 
 namespace tmk {
@@ -45,6 +46,7 @@ namespace {
 constexpr int kGroup = 256;
 constexpr int kGroupThreads = 256;  // k_sample_groups
 constexpr int kThreads = 512;       // k_sample_pick
+constexpr int kMostCtas = 4;        // of a row in k_sample_pick
 constexpr int kWarps = kThreads / 32;
 constexpr int kList = 4096;
 constexpr int kSmallK = 64;         // largest top-k that goes without a histogram
@@ -54,6 +56,7 @@ constexpr int kChunk = 128;         // most groups of a CTA of k_sample_groups
 constexpr int kPair = 2;            // groups that a warp of k_sample_groups takes at a time
 constexpr int kQuad = 4;            // and of k_sample_pick
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLowest = -3.4028234663852886e38f;
 constexpr uint32_t kKeyNone = 0x007FFFFFu;  // order_key(-inf)
 constexpr double kFixed = 1099511627776.0;  // 2^40
 
@@ -68,9 +71,10 @@ struct SampleArgs {
     const float *top_p, *min_p;
     Grammar g;
     float2 *stats;            // [B][G] largest logit, sum of weights (relative to it)
-    uint32_t *extra;          // [B][G] weight of a group's kept tokens that stats does not have
+    float *bound;             // [B][G] what a group's score in the draw is not above
     uint32_t *hist;           // [B][parts][2][kBins] counts, weights
-    int32_t chunk, parts;     // groups of a CTA, CTAs of a row
+    int32_t chunk, parts;     // groups of a CTA, CTAs of a row in k_sample_groups
+    int32_t ctas;             // of a row in k_sample_pick: a cluster
     int32_t *tokens;
     float *logprobs;
 };
@@ -218,6 +222,10 @@ struct Shared {
     uint32_t key;
     int32_t ties;
     unsigned long long above, total;
+    // what the CTAs of a cluster are to do, and, of the first one's, what the others found
+    float least, upper, largest;
+    int32_t more;  // 0: nothing, 1: the list, 2: and the weight above it
+    float mass[kMostCtas];
 };
 
 // Over the block: every warp reduces the warps' values once more, so that one
@@ -263,14 +271,6 @@ __device__ __forceinline__ float block_sum(Shared &s, float x) {
     for (int d = 8; d; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
     return x;
 }
-__device__ __forceinline__ int32_t block_sum(Shared &s, int32_t x) {
-    x = __reduce_add_sync(~0u, x);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) s.i[threadIdx.x >> 5] = x;
-    __syncthreads();
-    return __reduce_add_sync(~0u, (threadIdx.x & 31) < kWarps ? s.i[threadIdx.x & 15] : 0);
-}
-
 // Sums over the threads before this one, of a count and a weight.
 __device__ __forceinline__ void block_scan(Shared &s, int32_t &n, float &m) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -520,8 +520,6 @@ __global__ void __launch_bounds__(kGroupThreads) k_sample_groups(SampleArgs a) {
 
 // ------------------------------------------------------------ one row's draw
 
-constexpr float kLowest = -3.4028234663852886e38f;
-
 // A lower bound, finite, of the m-th largest group maximum (m >= 1), and so of the
 // m-th largest logit; of every logit when fewer groups have a token. `low`: the
 // smallest maximum of those that have.
@@ -583,17 +581,16 @@ __device__ __forceinline__ void fill_list(Shared &s, const Row<T> &row, int32_t 
     }
 }
 
-// The next four groups of a warp's `todo` (bit i: group j0 + 16 i + warp; -1 where
+// The next four groups of a warp's `todo` (bit i: group j0 + stride i; -1 where
 // there are no more) and their logits, all asked for before the first is used.
 template <typename T>
-__device__ __forceinline__ void take_quad(const GroupLoad<T> &load, uint32_t &todo, int32_t j0, int warp, int lane,
-                                          int (&at)[kQuad], int32_t (&j)[kQuad], float (&x)[kQuad][8]) {
+__device__ __forceinline__ void take_quad(const GroupLoad<T> &load, uint32_t &todo, int32_t j0, int32_t stride, int lane,
+                                          int32_t (&j)[kQuad], float (&x)[kQuad][8]) {
     uint4 q[kQuad][2] = {};
 #pragma unroll
     for (int g = 0; g < kQuad; g++) {
-        at[g] = __ffs(todo) - 1;
+        j[g] = todo ? j0 + (__ffs(todo) - 1) * stride : -1;
         todo &= todo - 1;
-        j[g] = at[g] < 0 ? -1 : j0 + at[g] * kWarps + warp;
         if (j[g] >= 0 && load.whole(j[g])) load.read(j[g], lane, q[g]);
     }
 #pragma unroll
@@ -616,10 +613,9 @@ __device__ __forceinline__ int32_t collect(Shared &s, const GroupLoad<T> &load, 
         const int32_t mine = j0 + lane * kWarps + warp;
         uint32_t todo = __ballot_sync(~0u, mine < G && stats[mine].x >= least);
         while (todo) {
-            int at[kQuad];
             int32_t j[kQuad];
             float x[kQuad][8];
-            take_quad(load, todo, j0, warp, lane, at, j, x);
+            take_quad(load, todo, j0 + warp, kWarps, lane, j, x);
             uint32_t in = 0;
 #pragma unroll
             for (int g = 0; g < kQuad; g++)
@@ -707,14 +703,14 @@ __device__ __forceinline__ float scan_list(Shared &s, int32_t n, float M, float 
 }
 
 // How many of the first n entries of the sorted, scanned list are kept: those
-// before which the weight, `above` included, is below target, with w >= min_p.
-__device__ __forceinline__ int32_t cut_list(Shared &s, int32_t n, float above, float target, const Way &way) {
+// before which the weight, `above` included, is below target.
+__device__ __forceinline__ int32_t cut_list(Shared &s, int32_t n, float above, float target) {
     __syncthreads();
-    if (threadIdx.x == 0) s.n = 0;
+    if (threadIdx.x == 0) s.n = 1;
     __syncthreads();
     int32_t last = 0;
     for (int32_t i = threadIdx.x; i < n; i += kThreads)
-        if (above + s.before[i] < target && s.weight[i] >= way.min_p) last = i + 1;
+        if (above + s.before[i] < target) last = i + 1;
     if (last) atomicMax(&s.n, last);
     __syncthreads();
     n = s.n;
@@ -722,16 +718,45 @@ __device__ __forceinline__ int32_t cut_list(Shared &s, int32_t n, float above, f
     return n;
 }
 
-// The group drawn by stats[j].y and extra (in units of `unit`).
-__device__ __forceinline__ int32_t draw_group(Shared &s, const float2 *stats, const uint32_t *extra, int32_t G, float unit,
-                                              int64_t seed) {
-    __syncthreads();
-    Best best = {-INFINITY, -1};
+// The group drawn where only tokens with entry >= last (order_key << 32 | ~id) and
+// w >= min_p are kept. A group's score is not above what it would be with all its
+// tokens, so the kept weights of a few groups settle the draw: each warp looks at
+// the best bounds of its groups until none is above the best score found.
+template <typename T>
+__device__ __forceinline__ int32_t draw_group(Shared &s, const GroupLoad<T> &load, const float2 *stats, float *bound, int32_t G,
+                                              unsigned long long last, float min_p, float M, float T_, int64_t seed) {
+    constexpr float kRounding = 2e-5f;  // of a score: sums of logarithms and noise below 64 in 24 bits
+    const int lane = threadIdx.x & 31;
+    const float c = __fdiv_rn(kLog2e, T_);
     for (int32_t j = threadIdx.x; j < G; j += kThreads) {
-        const float mass = stats[j].y + float(__ldcg(extra + j)) * unit;
-        if (mass > 0.0f) best = better(best, {logf(mass) + gumbel(seed, 0x80000000ull + uint32_t(j)), j});
+        const float2 g = stats[j];
+        bound[j] = g.x > -INFINITY ? logf(g.y) + scaled(g.x, M, T_) + gumbel(seed, 0x80000000ull + uint32_t(j)) + kRounding
+                                   : -INFINITY;
     }
-    return block_best(s, best).id;
+    Best found = {-INFINITY, -1};
+    for (;;) {
+        Best next = {-INFINITY, -1};  // of this warp's groups: those of its threads
+        for (int32_t j = threadIdx.x; j < G; j += kThreads) next = better(next, {bound[j], j});
+        next = warp_best(next);
+        const bool look = next.score > -INFINITY && next.score >= found.score;
+        Best mine = {-INFINITY, -1};
+        if (look) {
+            float x[8], mass = 0.0f;
+            load(next.id, lane, x);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const unsigned long long entry = (uint64_t(order_key(x[i] + 0.0f)) << 32) |
+                                                 uint32_t(~uint32_t(next.id * kGroup + load.id(i, lane)));
+                const float w = x[i] == M ? 1.0f : exp2_fast((x[i] - M) * c);
+                if (x[i] > -INFINITY && entry >= last && w >= min_p) mass += w;
+            }
+            mass = warp_sum(mass);
+            if (mass > 0.0f) mine = {logf(mass) + gumbel(seed, 0x80000000ull + uint32_t(next.id)), next.id};
+            if ((next.id & 31) == lane) bound[next.id] = -INFINITY;  // its thread's own
+        }
+        found = better(found, block_best(s, mine));
+        if (!__syncthreads_or(look)) return found.id;
+    }
 }
 
 // Of the first n (at most kSmallK) entries of the sorted list, by one warp, an
@@ -784,13 +809,12 @@ __device__ __forceinline__ int32_t draw_small(Shared &s, int32_t n, const Way &w
 }
 
 // Where the list is long: its tokens from `least` to below `above` are counted and
-// weighed (relative to `top`, the weight at `above`) by 512 equal intervals, the
-// one in which the kept set ends becomes the list, tokens before it go to
-// `extra` (in units of top / 2^20) and to n_above and mass. By count, or by weight
-// (count < 0). Returns the list's length.
-__device__ __forceinline__ int32_t narrow(Shared &s, int32_t n, float least, float above, float top, const Way &way, float M,
-                                          int32_t count, float target, uint32_t *extra, int32_t &n_above, float &mass) {
-    const float c = __fdiv_rn(kLog2e, way.T), per = float(kThreads) / (above - least);
+// weighed (relative to `top`, the weight at `above`) by 512 equal intervals, and
+// the one in which the kept set ends becomes the list; n_above and mass grow by
+// what lies before it. By count, or by weight (count < 0). Returns the list's length.
+__device__ __forceinline__ int32_t narrow(Shared &s, int32_t n, float least, float above, float top, float c, int32_t count,
+                                          float target, int32_t &n_above, float &mass) {
+    const float per = float(kThreads) / (above - least);
     __syncthreads();
     s.fine.count[threadIdx.x] = s.fine.mass[threadIdx.x] = 0u;
     if (threadIdx.x == 0) s.bin[0] = kThreads, s.ties = 0;
@@ -823,10 +847,7 @@ __device__ __forceinline__ int32_t narrow(Shared &s, int32_t n, float least, flo
     mass += s.f[0];
     for (int32_t i = threadIdx.x; i < n; i += kThreads) {
         const unsigned long long e = s.list[i];
-        const float x = list_value(e), w = exp2_fast((x - M) * c);
-        const int32_t at = place(x);
-        if (at == bin) s.sub[atomicAdd(&s.n, 1)] = e;
-        else if (at < bin && w >= way.min_p) atomicAdd(extra + list_id(e) / kGroup, uint32_t(w / top * 1048576.0f + 0.5f));
+        if (place(list_value(e)) == bin) s.sub[atomicAdd(&s.n, 1)] = e;
     }
     __syncthreads();
     n = s.n;
@@ -843,78 +864,52 @@ __device__ __forceinline__ float bin_floor(const Bins &bins, int32_t last) {
     if (last < 0) return INFINITY;
     uint32_t lo = lowest, hi = highest;  // bin(lo) > last, or lo is the answer; bin(hi) <= last
     if (bins.bin(key_value(lo)) <= last) return key_value(lo);
-    while (hi - lo > 1) {
-        const uint32_t mid = lo + (hi - lo) / 2;
-        if (bins.bin(key_value(mid)) <= last) hi = mid;
-        else lo = mid;
+    const uint32_t lane = threadIdx.x & 31;
+    while (hi - lo > 1) {  // 33 parts at a time, a lane a border
+        const uint32_t step = max(1u, (hi - lo) / 33), at = min(hi, lo + step * (lane + 1));
+        const uint32_t in = __ballot_sync(~0u, bins.bin(key_value(at)) <= last);
+        const uint32_t first = in ? uint32_t(__ffs(in)) : 33u;  // the borders before it are not in
+        if (first <= 32) hi = min(hi, lo + step * first);
+        lo += step * (first - 1);
     }
     return key_value(hi);
 }
 
-// One pass over the groups that reach `least`: s.list gets the ids of the tokens
-// from `least` up to below `above`, stats[j].y the weight of each group's tokens
-// at or above `above` with w >= min_p, n and mass the number and weight of all of
-// those; extra is cleared. all_above: there is no list. Returns the list's length.
+// One pass over the groups that reach `least`, by CTA `rank` of `ctas`: s.list gets
+// the ids of the tokens from `least` up to below `above`. Returns the weight of
+// those at or above `above` (to thread 0), 0 when it is not asked for.
 template <typename T>
-__device__ __forceinline__ int32_t split_at(Shared &s, const GroupLoad<T> &load, float2 *stats, int32_t G,
-                                            float least, float above, bool all_above, const Way &way, float M, uint32_t *extra,
-                                            int32_t &n, float &mass) {
+__device__ __forceinline__ float split_at(Shared &s, Shared &first, const GroupLoad<T> &load, const float2 *stats, int32_t G,
+                                          float least, float above, bool weigh, float M, float c, int rank, int ctas) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const float c = __fdiv_rn(kLog2e, way.T);
-    __syncthreads();
-    if (threadIdx.x == 0) s.n = 0;
-    __syncthreads();
-    int32_t count = 0;
     float sum = 0.0f;
-    for (int32_t j0 = 0; j0 < G; j0 += 32 * kWarps) {
-        const int32_t mine = j0 + lane * kWarps + warp;
-        const float top = mine < G ? stats[mine].x : -INFINITY;
-        // where nothing but min_p counts, groups that do not reach its weight hold nothing
-        uint32_t todo = __ballot_sync(~0u, top >= least && (!all_above || top == M || exp2_fast((top - M) * c) >= way.min_p));
-        float kept = 0.0f;  // of group `mine`
+    for (int32_t j0 = 0; j0 < G; j0 += ctas * 32 * kWarps) {
+        const int32_t mine = j0 + (lane * kWarps + warp) * ctas + rank;
+        uint32_t todo = __ballot_sync(~0u, mine < G && stats[mine].x >= least);
         while (todo) {
-            int at[kQuad];
             int32_t j[kQuad];
             float x[kQuad][8];
-            take_quad(load, todo, j0, warp, lane, at, j, x);
+            take_quad(load, todo, j0 + warp * ctas + rank, kWarps * ctas, lane, j, x);
             uint32_t in = 0;
 #pragma unroll
             for (int g = 0; g < kQuad; g++) {
-                float all = 0.0f, of = 0.0f;
-                uint32_t up = 0;
+                if (j[g] < 0) continue;
 #pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    const bool is_above = j[g] >= 0 && x[g][i] >= above;
-                    float w = exp2_fast((x[g][i] - M) * c);
-                    if (!is_above) w = 0.0f;
-                    up += is_above;
-                    all += w;
-                    of += w >= way.min_p ? w : 0.0f;
-                    in |= uint32_t(j[g] >= 0 && !is_above && x[g][i] >= least) << (8 * g + i);
-                }
-                if (M > 3.0e38f) {  // infinite: those that are it share the weight
-                    all = of = 0.0f;
+                for (int i = 0; i < 8; i++) in |= uint32_t(x[g][i] >= least && x[g][i] < above) << (8 * g + i);
+                if (weigh) {
+                    float part = 0.0f;
 #pragma unroll
-                    for (int i = 0; i < 8; i++) all += j[g] >= 0 && x[g][i] >= above && x[g][i] == M ? 1.0f : 0.0f;
-                    of = way.min_p <= 1.0f ? all : 0.0f;
-                }
-                count += int32_t(up);
-                sum += all;
-                if (__any_sync(~0u, of > 0.0f)) {
-                    of = warp_sum(of);
-                    if (lane == at[g]) kept = of;
+                    for (int i = 0; i < 8; i++) {
+                        const float w = exp2_fast((x[g][i] - M) * c);
+                        part += x[g][i] >= above ? w : 0.0f;
+                    }
+                    sum += part;
                 }
             }
-            append(s, load, j, in, lane);
-        }
-        if (mine < G) {
-            stats[mine].y = kept;
-            extra[mine] = 0u;
+            append(first, load, j, in, lane);
         }
     }
-    n = block_sum(s, count);
-    mass = block_sum(s, sum);
-    return s.n;
+    return block_sum(s, sum);
 }
 
 // Adds up the row's histograms in s.hist, weights relative to M.
@@ -942,8 +937,9 @@ __device__ __forceinline__ void sum_hist(Shared &s, const uint32_t *hist, int32_
     __syncthreads();
 }
 
-// The bins [s.bin[0], s.bin[1]] in which the kept set ends: by count exactly, by
-// weight to within the histogram's precision. kBins: none found.
+// The bins [s.bin[0], s.bin[1]] in which the kept set ends: by count exactly (and
+// s.ties tokens are in the bins before), by weight to within the histogram's
+// precision. kBins: none found.
 __device__ __forceinline__ void find_bins(Shared &s, bool by_mass, int32_t count, float target) {
     constexpr int kPer = kBins / kThreads;
     constexpr float kSlack = 1e-4f;  // weights in the histogram are rounded to 2^-16
@@ -967,6 +963,7 @@ __device__ __forceinline__ void find_bins(Shared &s, bool by_mass, int32_t count
             if (hi == kBins && m * (1.0f - kSlack) >= target) hi = bin;
         } else if (lo == kBins && n >= count) {
             lo = hi = bin;
+            if (n - int32_t(s.hist.count[bin]) < count) s.ties = n - int32_t(s.hist.count[bin]);
         }
     }
     lo = __reduce_min_sync(~0u, lo);
@@ -1081,7 +1078,7 @@ __device__ __noinline__ Cut radix_cut(Shared &s, const Row<T> &row, const float2
 
 // The id of the cut.ties-th token at cut.key.
 template <typename T>
-__device__ __noinline__ int32_t last_tie(Shared &s, const Row<T> &row, float2 *stats, int32_t G, const Cut &cut) {
+__device__ __noinline__ int32_t last_tie(Shared &s, const Row<T> &row, const float2 *stats, float *scratch, int32_t G, const Cut &cut) {
     const int lane = threadIdx.x & 31;
     for (int32_t j = threadIdx.x >> 5; j < G; j += kWarps) {
         int32_t n = 0;
@@ -1090,13 +1087,13 @@ __device__ __noinline__ int32_t last_tie(Shared &s, const Row<T> &row, float2 *s
                 const int64_t v = int64_t(j) * kGroup + i * 32 + lane;
                 n += __popc(__ballot_sync(~0u, v < row.V && order_key(row(int32_t(v))) == cut.key));
             }
-        if (lane == 0) stats[j].y = __int_as_float(n);  // the sums of the groups are not needed any more
+        if (lane == 0) scratch[j] = __int_as_float(n);
     }
     __syncthreads();
     if (threadIdx.x < 32) {
         int32_t left = cut.ties, group = G - 1;
         for (int32_t j0 = 0; j0 < G; j0 += 32) {
-            const int32_t n = j0 + lane < G ? __float_as_int(stats[j0 + lane].y) : 0;
+            const int32_t n = j0 + lane < G ? __float_as_int(scratch[j0 + lane]) : 0;
             int32_t upto = n;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
@@ -1137,28 +1134,59 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_pick(SampleArgs a) {
     Shared &s = *reinterpret_cast<Shared *>(dynamic_smem);
     pdl_launch_dependents();
     pdl_wait();
-    const int32_t b = blockIdx.x, G = a.G;
+    const int ctas = a.ctas, rank = ctas > 1 ? int(cluster_rank()) : 0;
+    const int32_t b = int32_t(blockIdx.x) / ctas, G = a.G;
     const int lane = threadIdx.x & 31;
-    float2 *stats = a.stats + int64_t(b) * G;
+    const float2 *stats = a.stats + int64_t(b) * G;
+    const Way way = row_way(a, b);
+    const Row<T> row = row_at<T>(a, b);
+    const GroupLoad<T> load(row);
+    const float c = __fdiv_rn(kLog2e, way.T);
+    // rows whose kept set may be large have the cluster's CTAs share the pass over the groups
+    const bool shared = ctas > 1 && wants_hist(way, G);
+    if (rank > 0) {
+        if (!shared) return;
+        Shared &first = *cluster_object(&s, 0);
+        for (;;) {
+            cluster_sync();  // what is to be done is in this CTA's memory
+            if (!s.more) return;
+            const float mass = split_at(s, first, load, stats, G, s.least, s.upper, s.more > 1, s.largest, c, rank, ctas);
+            if (threadIdx.x == 0) first.mass[rank] = mass;
+            cluster_sync();  // and it is done
+        }
+    }
+    auto tell = [&](int32_t more, float least, float above, float largest) {
+        __syncthreads();
+        if (threadIdx.x == 0) s.n = 0;
+        if (shared) {
+            if (int(threadIdx.x) < ctas) {
+                Shared &other = *cluster_object(&s, threadIdx.x);
+                other.least = least;
+                other.upper = above;
+                other.largest = largest;
+                other.more = more;
+            }
+            cluster_sync();
+        } else {
+            __syncthreads();
+        }
+    };
     float M = -INFINITY, low = INFINITY;
     for (int32_t j = threadIdx.x; j < G; j += kThreads) {
         const float x = stats[j].x;
         M = fmaxf(M, x);
         if (x > -INFINITY) low = fminf(low, x);
     }
-    const Way way = row_way(a, b);
-    const Row<T> row = row_at<T>(a, b);
-    const GroupLoad<T> load(row);
     const int64_t seed = __ldg(a.seeds + b);
     block_range(s, M, low);
     if (M == -INFINITY) {
+        if (shared) tell(0, 0.0f, 0.0f, 0.0f);
         if (threadIdx.x == 0) {
             a.tokens[b] = -1;
             if (a.logprobs) a.logprobs[b] = -INFINITY;
         }
         return;
     }
-    const float c = __fdiv_rn(kLog2e, way.T);
     float Z = 0.0f;
     for (int32_t j = threadIdx.x; j < G; j += kThreads) {
         const float2 g = stats[j];
@@ -1168,125 +1196,105 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_pick(SampleArgs a) {
 
     const bool by_p = !way.greedy && way.p < 1.0f, by_min = !way.greedy && way.min_p > 0.0f;
     bool by_k = !way.greedy && way.k > 0;
-    int32_t group = -1;         // of the token, once drawn
-    // what is kept, min_p aside: tokens at or above `last` (order_key << 32 | ~id), and those at or above kept_from
-    unsigned long long last = 0ull;
-    float kept_from = INFINITY;
-    uint32_t *extra = a.extra + int64_t(b) * G;
+    int32_t token = -1;
+    unsigned long long last = 0ull;  // tokens below this entry (order_key << 32 | ~id) are not kept
     const Bins bins(stats[0].x);
-    enum { kSmall, kCount, kMass, kLeast, kNone };  // how the kept set is found: few by count, by count, by weight, min_p alone
+    enum { kSmall, kCount, kMass, kNone };  // how the kept set is found: few by count, by count, by weight
     float target = way.p * Z;
-    int step = by_k ? (wants_hist(way, G) ? kCount : kSmall) : by_p ? kMass : by_min ? kLeast : kNone;
+    int step = by_k ? (wants_hist(way, G) ? kCount : kSmall) : by_p ? kMass : kNone;
     while (step != kNone) {
-        int32_t n = 0, n_above = 0, kept = 0;
-        float mass = 0.0f, least = kLowest, above = kLowest, top = 1.0f;
+        int32_t n = 0, n_above = 0;
+        float mass = 0.0f, least = kLowest, above = INFINITY, top = 1.0f;
         if (step == kSmall) {
             n = collect(s, load, stats, G, nth_group(s, stats, G, way.k, M, low));
         } else {
-            if (step != kLeast) {
-                sum_hist(s, a.hist + int64_t(b) * a.parts * 2 * kBins, a.parts, bins, way, M);
-                find_bins(s, step == kMass, way.k, target);
-                const int32_t first = s.bin[0], end = s.bin[1];
-                if (end >= kBins) {
-                    if (step == kMass) break;
-                    by_k = false;  // fewer tokens than top_k: it keeps all
-                    step = by_p ? kMass : by_min ? kLeast : kNone;
-                    continue;
-                }
-                least = bin_floor(bins, end);
-                above = bin_floor(bins, first - 1);
-                if (above < M) top = exp2_fast((above - M) * c);
+            sum_hist(s, a.hist + int64_t(b) * a.parts * 2 * kBins, a.parts, bins, way, M);
+            find_bins(s, step == kMass, way.k, target);
+            const int32_t begin = s.bin[0], end = s.bin[1];
+            if (end >= kBins) {
+                if (step == kMass) break;
+                by_k = false;  // fewer tokens than top_k: it keeps all
+                step = by_p ? kMass : kNone;
+                continue;
             }
-            n = split_at(s, load, stats, G, least, above, step == kLeast, way, M, extra, n_above, mass);
+            n_above = s.ties;  // by count; by weight it is not used
+            least = bin_floor(bins, end);
+            above = bin_floor(bins, begin - 1);
+            if (above < M) top = exp2_fast((above - M) * c);
+            tell(by_p ? 2 : 1, least, above, M);
+            mass = split_at(s, s, load, stats, G, least, above, by_p, M, c, 0, ctas);
+            if (shared) {
+                cluster_sync();
+                for (int r = 1; r < ctas; r++) mass += s.mass[r];
+            } else {
+                __syncthreads();
+            }
+            n = s.n;
         }
         if (n > kList) break;
         fill_list(s, row, n);
         if (n > kThreads && step != kSmall && above < M)
-            n = narrow(s, n, least, above, top, way, M, step == kCount ? way.k : -1, target, extra, n_above, mass);
+            n = narrow(s, n, least, above, top, c, step == kCount ? way.k : -1, target, n_above, mass);
         sort_list(s, n);
         if (step == kSmall) {
-            if (threadIdx.x >= 32) return;  // one warp does the rest
-            const int32_t token = draw_small(s, min(way.k, n), way, M, seed, lane);
-            if (lane == 0) {
-                a.tokens[b] = token;
-                if (a.logprobs) a.logprobs[b] = scaled(row(token), M, way.T) - logf(Z);
-            }
-            return;
+            if (threadIdx.x >= 32) return;  // one warp does the rest (such a row's cluster shares nothing)
+            token = draw_small(s, min(way.k, n), way, M, seed, lane);
+            break;
+        }
+        const int32_t wanted = min(n, way.k - n_above);
+        if (step == kCount && !by_p) {
+            last = s.list[wanted - 1];
+            break;
         }
         const float total = scan_list(s, n, M, way.T);
-        const int32_t wanted = step == kCount ? min(n, way.k - n_above) : n;
         if (step == kCount) {
-            target = by_p ? way.p * (mass + (wanted < n ? s.before[wanted] : total)) : INFINITY;
-            if (by_p) {
-                step = kMass;
-                continue;
-            }
+            target = way.p * (mass + (wanted < n ? s.before[wanted] : total));
+            step = kMass;
+            continue;
         }
-        if (step == kMass && !(mass < target && mass + total >= target)) break;
-        kept = cut_list(s, wanted, step == kCount ? 0.0f : mass, target, way);
-        kept_from = above;
-        // with none kept of the list (min_p), what lies above its largest
-        last = kept > 0 ? s.list[kept - 1] : n > 0 ? s.list[0] + 1 : ~0ull;
-        for (int32_t i = threadIdx.x; i < kept; i += kThreads)
-            atomicAdd(extra + list_id(s.list[i]) / kGroup, uint32_t(s.weight[i] / top * 1048576.0f + 0.5f));
-        group = draw_group(s, stats, extra, G, top / 1048576.0f, seed);
+        if (mass < target && mass + total >= target) last = s.list[cut_list(s, n, mass, target) - 1];
         break;
     }
-    const bool filtered = by_k || by_p || by_min;
-    if (group < 0) {
-        Cut cut = {kKeyNone, 0, Z};
-        int32_t last_id = 0x7FFFFFFF;
-        for (int by = 0; by < 2; by++) {
-            if (by ? !by_p : !by_k) continue;
-            const double to = double(way.p) * double(cut.mass) * kFixed;
-            const Cut c = radix_cut(s, row, stats, G, M, way.T, by == 1, uint32_t(way.k),
-                                    to > 0.0 ? (unsigned long long)(to) : 0ull);
-            if (by == 0 || !by_k || c.key > cut.key || (c.key == cut.key && c.ties < cut.ties)) cut = c;
+    if (shared) tell(0, 0.0f, 0.0f, 0.0f);
+    if (step != kSmall || token < 0) {
+        const bool filtered = by_k || by_p || by_min;
+        if ((by_k || by_p) && last == 0ull) {
+            Cut cut = {kKeyNone, 0, Z};
+            for (int by = 0; by < 2; by++) {
+                if (by ? !by_p : !by_k) continue;
+                const double to = double(way.p) * double(cut.mass) * kFixed;
+                const Cut found = radix_cut(s, row, stats, G, M, way.T, by == 1, uint32_t(way.k),
+                                            to > 0.0 ? (unsigned long long)(to) : 0ull);
+                if (by == 0 || !by_k || found.key > cut.key || (found.key == cut.key && found.ties < cut.ties)) cut = found;
+            }
+            last = (uint64_t(cut.key) << 32) | uint32_t(~uint32_t(last_tie(s, row, stats, a.bound + int64_t(b) * G, G, cut)));
         }
-        if (by_k || by_p) {
-            last_id = last_tie(s, row, stats, G, cut);
-            last = (uint64_t(cut.key) << 32) | uint32_t(~uint32_t(last_id));
-        }
-        Best best = {-INFINITY, -1};
-        if (!filtered) {
+        int32_t group;
+        if (filtered) {
+            group = draw_group(s, load, stats, a.bound + int64_t(b) * G, G, last, way.min_p, M, way.T, seed);
+        } else {
+            Best best = {-INFINITY, -1};
             for (int32_t j = threadIdx.x; j < G; j += kThreads) {
                 const float2 g = stats[j];
                 if (!(g.x > -INFINITY)) continue;
                 if (way.greedy) best = better(best, {g.x, j});
                 else best = better(best, {logf(g.y) + scaled(g.x, M, way.T) + gumbel(seed, 0x80000000ull + uint32_t(j)), j});
             }
-        } else {
-            for (int32_t j = threadIdx.x >> 5; j < G; j += kWarps) {
-                const uint32_t top = order_key(stats[j].x);
-                if (top < cut.key || top <= kKeyNone || weight(stats[j].x, M, way.T) < way.min_p) continue;
-                float x[8], mass = 0.0f;
-                load(j, lane, x);
-#pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    const uint32_t k = order_key(x[i] + 0.0f);
-                    const int32_t v = j * kGroup + load.id(i, lane);
-                    const float w = weight(x[i], M, way.T);
-                    if (x[i] > -INFINITY && (k > cut.key || (k == cut.key && v <= last_id)) && w >= way.min_p) mass += w;
-                }
-                mass = warp_sum(mass);
-                if (mass > 0.0f) best = better(best, {logf(mass) + gumbel(seed, 0x80000000ull + uint32_t(j)), j});
+            group = block_best(s, best).id;
+        }
+        Best best = {-INFINITY, -1};
+        if (threadIdx.x < kGroup) {
+            const int64_t v = int64_t(group) * kGroup + threadIdx.x;
+            const float x = v < a.V ? row(int32_t(v)) : -INFINITY;
+            if (x > -INFINITY) {
+                const unsigned long long entry = (uint64_t(order_key(x)) << 32) | uint32_t(~uint32_t(v));
+                const bool kept = !filtered || (entry >= last && (x == M || exp2_fast((x - M) * c) >= way.min_p));
+                if (way.greedy) best = {x, int32_t(v)};
+                else if (kept) best = {scaled(x, M, way.T) + gumbel(seed, uint32_t(v)), int32_t(v)};
             }
         }
-        group = block_best(s, best).id;
+        token = block_best(s, best).id;
     }
-    Best best = {-INFINITY, -1};
-    if (threadIdx.x < kGroup) {
-        const int64_t v = int64_t(group) * kGroup + threadIdx.x;
-        const float x = v < a.V ? row(int32_t(v)) : -INFINITY;
-        if (x > -INFINITY) {
-            const unsigned long long entry = (uint64_t(order_key(x)) << 32) | uint32_t(~uint32_t(v));
-            const bool kept = !filtered || ((entry >= last || x >= kept_from) &&
-                                            (x == M || weight(x, M, way.T) >= way.min_p));
-            if (way.greedy) best = {x, int32_t(v)};
-            else if (kept) best = {scaled(x, M, way.T) + gumbel(seed, uint32_t(v)), int32_t(v)};
-        }
-    }
-    const int32_t token = block_best(s, best).id;
     if (threadIdx.x == 0) {
         a.tokens[b] = token;
         if (a.logprobs) a.logprobs[b] = scaled(row(token), M, way.T) - logf(Z);
@@ -1298,14 +1306,14 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_pick(SampleArgs a) {
 // that there are some four CTAs an SM.
 struct Plan {
     int32_t G, chunk, parts;
-    int64_t extra_at, hist_at, bytes;
+    int64_t bound_at, hist_at, bytes;
     Plan(int32_t B, int32_t V) {
         G = int32_t((int64_t(V) + kGroup - 1) / kGroup);
         chunk = kChunk;
         while (chunk > 16 && int64_t(B) * ((G + chunk - 1) / chunk) < 600) chunk /= 2;
         parts = (G + chunk - 1) / chunk;
-        extra_at = (int64_t(B) * G * int64_t(sizeof(float2)) + 255) / 256 * 256;
-        hist_at = extra_at + (int64_t(B) * G * 4 + 255) / 256 * 256;
+        bound_at = (int64_t(B) * G * int64_t(sizeof(float2)) + 255) / 256 * 256;
+        hist_at = bound_at + (int64_t(B) * G * 4 + 255) / 256 * 256;
         bytes = hist_at + int64_t(B) * parts * 2 * kBins * 4;
     }
 };
@@ -1316,7 +1324,20 @@ cudaError_t launch_sample(const SampleArgs &a, int32_t B, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     e = cudaFuncSetAttribute(k_sample_pick<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(sizeof(Shared)));
     if (e != cudaSuccess) return e;
-    return launch_pdl_smem(k_sample_pick<T>, B, kThreads, sizeof(Shared), st, a);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(B) * unsigned(a.ctas));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = sizeof(Shared);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = unsigned(a.ctas);
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = a.ctas > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, k_sample_pick<T>, a);
 }
 
 }  // namespace
@@ -1349,6 +1370,9 @@ extern "C" int trie_sample(const void *d_logits, int dtype, int64_t stride, int3
     a.G = plan.G;
     a.chunk = plan.chunk;
     a.parts = plan.parts;
+    // a cluster for each row while all of them run at once, two CTAs an SM
+    const int round = 2 * sm_count();
+    a.ctas = B * 4 <= round ? 4 : B * 2 <= round ? 2 : 1;
     a.seeds = d_seeds;
     a.temperature = d_temperature;
     a.top_k = d_top_k;
@@ -1356,7 +1380,7 @@ extern "C" int trie_sample(const void *d_logits, int dtype, int64_t stride, int3
     a.min_p = d_min_p;
     a.g = make_grammar(d_mask, mask_rows, d_states, V);
     a.stats = static_cast<float2 *>(d_workspace);
-    a.extra = reinterpret_cast<uint32_t *>(static_cast<unsigned char *>(d_workspace) + plan.extra_at);
+    a.bound = reinterpret_cast<float *>(static_cast<unsigned char *>(d_workspace) + plan.bound_at);
     a.hist = reinterpret_cast<uint32_t *>(static_cast<unsigned char *>(d_workspace) + plan.hist_at);
     a.tokens = d_tokens;
     a.logprobs = d_logprobs;
