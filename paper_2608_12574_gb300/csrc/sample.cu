@@ -52,9 +52,8 @@ constexpr int kList = 4096;
 constexpr int kSmallK = 64;         // largest top-k that goes without a histogram
 constexpr int kBins = 2048;
 constexpr float kBinsPerUnit = 32.0f;
-constexpr int kChunk = 128;         // most groups of a CTA of k_sample_groups
-constexpr int kPair = 2;            // groups that a warp of k_sample_groups takes at a time
-constexpr int kQuad = 4;            // and of k_sample_pick
+constexpr int kChunk = 256;         // most groups of a CTA of k_sample_groups: 2^16 tokens
+constexpr int kQuad = 4;            // groups that a warp takes at a time
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.4028234663852886e38f;
 constexpr uint32_t kKeyNone = 0x007FFFFFu;  // order_key(-inf)
@@ -169,6 +168,12 @@ __device__ __forceinline__ float gumbel(int64_t seed, uint64_t n) {
 
 // ------------------------------------------------------------- reductions
 
+// Elementwise maximum of two pairs of bf16.
+__device__ __forceinline__ uint32_t max2_bf16(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 m = __hmax2(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&m);
+}
+
 // A score and what it belongs to; the larger score wins, then the smaller id.
 struct Best {
     float score;
@@ -187,7 +192,13 @@ __device__ __forceinline__ Best warp_best(Best x) {
     }
     return x;
 }
-__device__ __forceinline__ float warp_max(float x) { return key_value(__reduce_max_sync(~0u, order_key(x))); }
+// (Floats in the order of signed whole numbers: the lower 31 bits of negative ones turned.)
+__device__ __forceinline__ float warp_max(float x) {
+    int32_t k = __float_as_int(x);
+    k ^= (k >> 31) & 0x7FFFFFFF;
+    k = __reduce_max_sync(~0u, k);
+    return __int_as_float(k ^ ((k >> 31) & 0x7FFFFFFF));
+}
 __device__ __forceinline__ float warp_sum(float x) {
 #pragma unroll
     for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
@@ -300,13 +311,15 @@ __device__ __forceinline__ void block_scan(Shared &s, int32_t &n, float &m) {
     m = (lane ? upto : 0.0f) + (warp ? mw : 0.0f);
 }
 
-// The sums over the warp of two values, in five exchanges: that of a in lanes 0
-// to 15, that of b in the others.
-__device__ __forceinline__ float warp_sum2(float a, float b, int lane) {
-    const bool high = lane & 16;
-    float x = (high ? b : a) + __shfl_xor_sync(~0u, high ? a : b, 16);
+// The sums over the warp of four values, in six exchanges: that of v[g] in lanes
+// 8 g to 8 g + 7.
+__device__ __forceinline__ float warp_sum4(const float (&v)[kQuad], int lane) {
+    const bool high = lane & 16, odd = lane & 8;
+    const float a = (high ? v[2] : v[0]) + __shfl_xor_sync(~0u, high ? v[0] : v[2], 16);
+    const float b = (high ? v[3] : v[1]) + __shfl_xor_sync(~0u, high ? v[1] : v[3], 16);
+    float x = (odd ? b : a) + __shfl_xor_sync(~0u, odd ? a : b, 8);
 #pragma unroll
-    for (int d = 8; d; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
+    for (int d = 4; d; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
     return x;
 }
 
@@ -317,7 +330,8 @@ __device__ __forceinline__ float warp_sum2(float a, float b, int lane) {
 // eight logits, shifted (kShifted: each block read holds a logit of the group,
 // so no read leaves the 16-byte blocks of the row). The rest is read by elements.
 enum : int { kByElement = 0, kWide = 1, kShifted = 2 };
-template <typename T>
+// kAligned: every row of the batch is on a 16-byte boundary.
+template <typename T, bool kAligned = false>
 struct GroupLoad {
     const T *x;
     GrammarRow allow;
@@ -326,7 +340,7 @@ struct GroupLoad {
     int shift;  // kShifted: elements from an aligned block's start to the row's
     __device__ __forceinline__ explicit GroupLoad(const Row<T> &row)
         : x(row.x), allow(row.allow), V(row.V), mode(kByElement), shift(int(reinterpret_cast<uintptr_t>(row.x) & 15) / int(sizeof(T))) {
-        if (row.allow.kind == kAllowAll) mode = shift == 0 ? kWide : sizeof(T) == 2 ? kShifted : kByElement;
+        if (row.allow.kind == kAllowAll) mode = kAligned || shift == 0 ? kWide : sizeof(T) == 2 ? kShifted : kByElement;
     }
     __device__ __forceinline__ int32_t id(int i, int lane) const {
         if (mode == kByElement) return i * 32 + lane;
@@ -335,36 +349,37 @@ struct GroupLoad {
     __device__ __forceinline__ bool whole(int32_t j) const { return mode != kByElement && int64_t(j + 1) * kGroup <= V; }
     // A whole group's blocks (kWide bf16 has one).
     __device__ __forceinline__ void read(int32_t j, int lane, uint4 (&q)[2]) const {
-        const uint4 *p = reinterpret_cast<const uint4 *>(x + int64_t(j) * kGroup - (mode == kShifted ? shift : 0)) + lane;
+        const uint4 *p = reinterpret_cast<const uint4 *>(x + int64_t(j) * kGroup - (!kAligned && mode == kShifted ? shift : 0)) + lane;
         q[0] = __ldg(p);
         if (sizeof(T) == 4) q[1] = __ldg(p + 32);
-        else if (mode == kShifted) q[1] = __ldg(p + 1);
+        else if (!kAligned && mode == kShifted) q[1] = __ldg(p + 1);
+    }
+    // The lane's eight logits as they are stored: eight words, or four of two.
+    __device__ __forceinline__ void words(const uint4 (&q)[2], uint32_t (&w)[8]) const {
+        w[0] = q[0].x, w[1] = q[0].y, w[2] = q[0].z, w[3] = q[0].w, w[4] = q[1].x, w[5] = q[1].y, w[6] = q[1].z, w[7] = q[1].w;
+        if (sizeof(T) == 2 && !kAligned && mode == kShifted) {
+            if (shift & 4) {
+#pragma unroll
+                for (int i = 0; i < 6; i++) w[i] = w[i + 2];
+            }
+            if (shift & 2) {
+#pragma unroll
+                for (int i = 0; i < 5; i++) w[i] = w[i + 1];
+            }
+            if (shift & 1) {
+#pragma unroll
+                for (int i = 0; i < 4; i++) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+            }
+        }
+    }
+    static __device__ __forceinline__ float value(const uint32_t (&w)[8], int i) {
+        return __uint_as_float(sizeof(T) == 4 ? w[i] : i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
     }
     __device__ __forceinline__ void decode(const uint4 (&q)[2], float (&f)[8]) const {
-        uint32_t w[8] = {q[0].x, q[0].y, q[0].z, q[0].w, q[1].x, q[1].y, q[1].z, q[1].w};
-        if (sizeof(T) == 4) {
+        uint32_t w[8];
+        words(q, w);
 #pragma unroll
-            for (int i = 0; i < 8; i++) f[i] = __uint_as_float(w[i]);
-        } else {
-            if (mode == kShifted) {
-                if (shift & 4) {
-#pragma unroll
-                    for (int i = 0; i < 6; i++) w[i] = w[i + 2];
-                }
-                if (shift & 2) {
-#pragma unroll
-                    for (int i = 0; i < 5; i++) w[i] = w[i + 1];
-                }
-                if (shift & 1) {
-#pragma unroll
-                    for (int i = 0; i < 4; i++) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 8; i++) f[i] = __uint_as_float(i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
-        }
-#pragma unroll
-        for (int i = 0; i < 8; i++) f[i] = fmaxf(f[i], -INFINITY);  // NaN counts as -inf
+        for (int i = 0; i < 8; i++) f[i] = fmaxf(value(w, i), -INFINITY);  // NaN counts as -inf
     }
     __device__ __forceinline__ void by_element(int32_t j, int lane, float (&f)[8]) const {
         const int64_t v0 = int64_t(j) * kGroup;
@@ -425,16 +440,39 @@ __device__ __forceinline__ float lane_weight(const float (&x)[8], float m, float
 __device__ __forceinline__ float lane_max(const float (&x)[8]) {
     return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
 }
-
+// The same of words as they are stored (NaN does not show).
 template <typename T>
-__global__ void __launch_bounds__(kGroupThreads) k_sample_groups(SampleArgs a) {
+__device__ __forceinline__ float words_max(const uint32_t (&w)[8]) {
+    if (sizeof(T) == 4) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) x[i] = __uint_as_float(w[i]);
+        return fmaxf(lane_max(x), -INFINITY);
+    }
+    const uint32_t m = max2_bf16(max2_bf16(w[0], w[1]), max2_bf16(w[2], w[3]));
+    return fmaxf(fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u)), -INFINITY);
+}
+
+template <typename T, bool kAligned>
+__global__ void __launch_bounds__(kGroupThreads, sizeof(T) == 2 && kAligned ? 3 : 2) k_sample_groups(SampleArgs a) {
     __shared__ __align__(16) uint32_t hist[2 * kBins];  // counts, weights
     pdl_launch_dependents();
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int32_t b = blockIdx.y;
+    const GroupLoad<T, kAligned> load(row_at<T>(a, b));
+    const int32_t j0 = int32_t(blockIdx.x) * a.chunk, j1 = min(a.G, j0 + a.chunk);
+    // four groups a warp at a time, those of the next turn asked for ahead
+    constexpr int kStep = kGroupThreads / 32 * kQuad;
+    uint4 q[kQuad][2] = {};
+    auto all_whole = [&](int32_t j) { return j + kQuad <= j1 && load.whole(j + kQuad - 1); };
+    auto read = [&](int32_t j) {
+        if (!all_whole(j)) return;
+#pragma unroll
+        for (int g = 0; g < kQuad; g++) load.read(j + g, lane, q[g]);
+    };
+    read(j0 + warp * kQuad);
     const Way way = row_way(a, b);
-    const GroupLoad<T> load(row_at<T>(a, b));
     const float c = __fdiv_rn(kLog2e, way.T);
     const bool binned = wants_hist(way, a.G);
     Bins bins(0.0f);
@@ -452,14 +490,13 @@ __global__ void __launch_bounds__(kGroupThreads) k_sample_groups(SampleArgs a) {
             const float place = bins.place(x[i]);
             const int32_t bin = bins.bin(x[i]);
             if (way.k) atomicAdd(&hist[bin], 1u);
-            // the weight relative to the bin's upper end: at most 2^16, 2^15 tokens a CTA
+            // the weight relative to the bin's upper end: below 2^16, at most 2^16 tokens a CTA
             if (way.p < 1.0f) {
                 const float w = exp2_fast((float(bin) - place) * (c / kBinsPerUnit));
                 atomicAdd(&hist[kBins + bin], uint32_t(fminf(w, 1.0f) * 65535.0f + 0.5f));
             }
         }
     };
-    const int32_t j0 = int32_t(blockIdx.x) * a.chunk, j1 = min(a.G, j0 + a.chunk);
     float2 *stats = a.stats + int64_t(b) * a.G;
     if (load.allow.kind != kAllowAll) {
         // most words of a mask are empty: a lane a word of four groups
@@ -480,35 +517,55 @@ __global__ void __launch_bounds__(kGroupThreads) k_sample_groups(SampleArgs a) {
             if (lane < 4 && j + lane < j1) stats[j + lane] = mine;
         }
     } else {
-        // two groups a warp, the next two asked for before these are worked on
-        constexpr int kStep = kGroupThreads / 32 * kPair;
-        uint4 q[kPair][2] = {};
-        auto read = [&](int32_t j) {
+        for (int32_t j = j0 + warp * kQuad; j < j1; j += kStep) {
+            float m[kQuad], sum[kQuad];
+            uint32_t w[kQuad][8];
+            const bool whole = all_whole(j);
+            if (whole) {
 #pragma unroll
-            for (int g = 0; g < kPair; g++)
-                if (j + g < j1 && load.whole(j + g)) load.read(j + g, lane, q[g]);
-        };
-        int32_t j = j0 + warp * kPair;
-        read(j);
-        for (; j < j1; j += kStep) {
-            float x[kPair][8], m[kPair], sum[kPair];
+                for (int g = 0; g < kQuad; g++) load.words(q[g], w[g]);
+                read(j + kStep);
+                // exp((x - m) / T) as 2^(x c - m c): the product m c is rounded, which its
+                // remainder makes good for the whole group. NaN and infinities make the
+                // sum NaN: it is then taken again with care.
 #pragma unroll
-            for (int g = 0; g < kPair; g++) {
-                if (load.whole(j + g)) load.decode(q[g], x[g]);
-                else load.by_element(min(j + g, a.G - 1), lane, x[g]);
-            }
-            read(j + kStep);
+                for (int g = 0; g < kQuad; g++) {
+                    m[g] = warp_max(words_max<T>(w[g]));
+                    const float mc = m[g] > -INFINITY ? m[g] * c : 0.0f;
+                    float part = 0.0f;
 #pragma unroll
-            for (int g = 0; g < kPair; g++) {
-                m[g] = warp_max(lane_max(x[g]));
-                sum[g] = lane_weight(x[g], m[g], c);
+                    for (int i = 0; i < 8; i++) part += exp2_fast(fmaf(load.value(w[g], i), c, -mc));
+                    sum[g] = m[g] > -INFINITY ? part - part * (fmaf(m[g], c, -mc) * 0.6931471806f) : part;
+                }
+            } else {
+                read(j + kStep);
+#pragma unroll
+                for (int g = 0; g < kQuad; g++) sum[g] = NAN;
             }
-            const float total = warp_sum2(sum[0], sum[1], lane);
-            if ((lane & 15) == 0 && j + (lane >> 4) < j1) stats[j + (lane >> 4)] = make_float2(lane ? m[1] : m[0], total);
-            if (binned) {
-                add_bins(x[0]);
-                if (j + 1 < j1) add_bins(x[1]);
+            float total = warp_sum4(sum, lane);
+            const bool again = __any_sync(~0u, !(total >= 0.0f));
+            if (again || binned) {
+#pragma unroll
+                for (int g = 0; g < kQuad; g++) {
+                    if (j + g >= j1) continue;
+                    float x[8];
+                    if (whole) {
+#pragma unroll
+                        for (int i = 0; i < 8; i++) x[i] = fmaxf(load.value(w[g], i), -INFINITY);
+                    } else {
+                        load(j + g, lane, x);
+                    }
+                    if (again) {
+                        m[g] = warp_max(lane_max(x));
+                        sum[g] = lane_weight(x, m[g], c);
+                    }
+                    if (binned) add_bins(x);
+                }
+                if (again) total = warp_sum4(sum, lane);
             }
+            const int mine = lane >> 3;
+            if ((lane & 7) == 0 && j + mine < j1)
+                stats[j + mine] = make_float2(mine & 2 ? (mine & 1 ? m[3] : m[2]) : (mine & 1 ? m[1] : m[0]), total);
         }
     }
     if (binned) {
@@ -1301,16 +1358,25 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_pick(SampleArgs a) {
     }
 }
 
-// How a batch is cut and where its parts of the workspace lie. A CTA of
-// k_sample_groups takes kChunk groups, or fewer where the batch is small, so
-// that there are some four CTAs an SM.
+// How a batch is cut and where its parts of the workspace lie. A row is cut into
+// the fewest parts of at most kChunk groups (16 in a small batch) whose CTAs fill
+// their rounds to nine tenths, some three an SM running at once.
 struct Plan {
     int32_t G, chunk, parts;
     int64_t bound_at, hist_at, bytes;
     Plan(int32_t B, int32_t V) {
         G = int32_t((int64_t(V) + kGroup - 1) / kGroup);
-        chunk = kChunk;
-        while (chunk > 16 && int64_t(B) * ((G + chunk - 1) / chunk) < 600) chunk /= 2;
+        constexpr int64_t kRound = 3 * 152;
+        const int32_t fewest = (G + kChunk - 1) / kChunk, most = (G + 15) / 16;
+        parts = int64_t(B) * most <= kRound ? most : fewest;
+        double best = 0.0;
+        for (int32_t p = fewest; int64_t(B) * most > kRound && p <= most && p <= fewest + 16 + int32_t(2 * kRound / B); p++) {
+            const int64_t ctas = int64_t(B) * p, rounds = (ctas + kRound - 1) / kRound;
+            const double full = double(ctas) / double(rounds * kRound);
+            if (full > best + 0.02) parts = p, best = full;
+            if (best >= 0.9) break;
+        }
+        chunk = ((G + parts - 1) / parts + 3) / 4 * 4;
         parts = (G + chunk - 1) / chunk;
         bound_at = (int64_t(B) * G * int64_t(sizeof(float2)) + 255) / 256 * 256;
         hist_at = bound_at + (int64_t(B) * G * 4 + 255) / 256 * 256;
@@ -1320,7 +1386,10 @@ struct Plan {
 
 template <typename T>
 cudaError_t launch_sample(const SampleArgs &a, int32_t B, cudaStream_t st) {
-    cudaError_t e = launch_pdl_grid(k_sample_groups<T>, dim3(unsigned(a.parts), unsigned(B)), kGroupThreads, 0, st, a);
+    const bool aligned = ((reinterpret_cast<uintptr_t>(a.logits) | uintptr_t(a.stride * int64_t(sizeof(T)))) & 15) == 0;
+    const dim3 grid(unsigned(a.parts), unsigned(B));
+    cudaError_t e = aligned ? launch_pdl_grid(k_sample_groups<T, true>, grid, kGroupThreads, 0, st, a)
+                            : launch_pdl_grid(k_sample_groups<T, false>, grid, kGroupThreads, 0, st, a);
     if (e != cudaSuccess) return e;
     e = cudaFuncSetAttribute(k_sample_pick<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(sizeof(Shared)));
     if (e != cudaSuccess) return e;
@@ -1372,7 +1441,7 @@ extern "C" int trie_sample(const void *d_logits, int dtype, int64_t stride, int3
     a.parts = plan.parts;
     // a cluster for each row while all of them run at once, two CTAs an SM
     const int round = 2 * sm_count();
-    a.ctas = B * 4 <= round ? 4 : B * 2 <= round ? 2 : 1;
+    a.ctas = B * 4 <= round ? 4 : (B * 2 <= round || (d_mask && B <= round)) ? 2 : 1;
     a.seeds = d_seeds;
     a.temperature = d_temperature;
     a.top_k = d_top_k;
