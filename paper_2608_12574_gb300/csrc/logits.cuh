@@ -40,21 +40,20 @@ struct GrammarRow {
     __device__ __forceinline__ bool allows(int32_t v) const { return (word(v >> 5) >> (v & 31)) & 1u; }
 };
 
-__device__ __forceinline__ GrammarRow grammar_row(const Grammar &g, int32_t b) {
+// What a row in state s allows.
+__device__ __forceinline__ GrammarRow grammar_state(const Grammar &g, int32_t s) {
     GrammarRow r;
     r.V = g.V;
     r.words = nullptr;
-    r.kind = kAllowAll;
-    if (g.mask) {
-        const int32_t s = __ldg(g.states + b);
-        if (s >= 0 && s < g.rows) {
-            r.words = g.mask + int64_t(s) * g.W;
-            r.kind = kAllowRow;
-        } else if (s != TRIE_STATE_FREE) {
-            r.kind = kAllowEos;
-        }
+    r.kind = s == TRIE_STATE_FREE ? kAllowAll : kAllowEos;
+    if (s >= 0 && s < g.rows) {
+        r.words = g.mask + int64_t(s) * g.W;
+        r.kind = kAllowRow;
     }
     return r;
+}
+__device__ __forceinline__ GrammarRow grammar_row(const Grammar &g, int32_t b) {
+    return grammar_state(g, g.mask ? __ldg(g.states + b) : TRIE_STATE_FREE);
 }
 
 __device__ __forceinline__ float to_f32(float x) { return x; }
