@@ -49,6 +49,7 @@ constexpr int kThreads = 512;       // k_sample_pick
 constexpr int kMostCtas = 4;        // of a row in k_sample_pick
 constexpr int kWarps = kThreads / 32;
 constexpr int kList = 4096;
+constexpr int kNarrow = 128;        // a longer list is narrowed before it is sorted
 constexpr int kSmallK = 64;         // largest top-k that goes without a histogram
 constexpr int kBins = 2048;
 constexpr float kBinsPerUnit = 32.0f;
@@ -846,9 +847,16 @@ __device__ __forceinline__ int32_t draw_small(Shared &s, int32_t n, const Way &w
     const uint32_t in1 = __ballot_sync(~0u, lane + 32 < n && before[1] < target && w[1] >= way.min_p);
     const int32_t kept = max(1, in1 ? 64 - __clz(in1) : 32 - __clz(in0));
     float mass[2] = {0.0f, 0.0f};
-    for (int32_t i = 0; i < kept; i++) {
-        const float wi = __shfl_sync(~0u, i < 32 ? w[0] : w[1], i & 31);
-        const int32_t gi = __shfl_sync(~0u, i < 32 ? group[0] : group[1], i & 31);
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+        s.weight[h * 32 + lane] = w[h];
+        s.before[h * 32 + lane] = __int_as_float(h * 32 + lane < kept ? group[h] : -2);
+    }
+    __syncwarp();
+#pragma unroll 8
+    for (int32_t i = 0; i < (kept + 7 & ~7); i++) {  // (a -2 is no entry's group)
+        const float wi = s.weight[i];
+        const int32_t gi = __float_as_int(s.before[i]);
         if (group[0] == gi) mass[0] += wi;
         if (group[1] == gi) mass[1] += wi;
     }
@@ -869,23 +877,26 @@ __device__ __forceinline__ int32_t draw_small(Shared &s, int32_t n, const Way &w
 // weighed (relative to `top`, the weight at `above`) by 512 equal intervals, and
 // the one in which the kept set ends becomes the list; n_above and mass grow by
 // what lies before it. By count, or by weight (count < 0). Returns the list's length.
+// width > 0: the tokens are all equal, of weight `top`, and go by `width` ids.
 __device__ __forceinline__ int32_t narrow(Shared &s, int32_t n, float least, float above, float top, float c, int32_t count,
-                                          float target, int32_t &n_above, float &mass) {
+                                          float target, int32_t width, int32_t &n_above, float &mass) {
     const float per = float(kThreads) / (above - least);
     __syncthreads();
     s.fine.count[threadIdx.x] = s.fine.mass[threadIdx.x] = 0u;
     if (threadIdx.x == 0) s.bin[0] = kThreads, s.ties = 0;
     __syncthreads();
-    auto place = [&](float x) { return max(0, min(kThreads - 1, int32_t((above - x) * per))); };
+    auto place = [&](unsigned long long e) {
+        return width ? list_id(e) / width : max(0, min(kThreads - 1, int32_t((above - list_value(e)) * per)));
+    };
     for (int32_t i = threadIdx.x; i < n; i += kThreads) {
         const float x = list_value(s.list[i]);
-        const int32_t at = place(x);
+        const int32_t at = place(s.list[i]);
         atomicAdd(&s.fine.count[at], 1u);
-        atomicAdd(&s.fine.mass[at], uint32_t(fminf(exp2_fast((x - above) * c), 1.0f) * 524288.0f + 0.5f));  // kList of them fit
+        if (!width) atomicAdd(&s.fine.mass[at], uint32_t(fminf(exp2_fast((x - above) * c), 1.0f) * 524288.0f + 0.5f));  // kList of them fit
     }
     __syncthreads();
     const int32_t mine = int32_t(s.fine.count[threadIdx.x]);
-    const float weighs = float(s.fine.mass[threadIdx.x]) * (top / 524288.0f);
+    const float weighs = width ? float(mine) * top : float(s.fine.mass[threadIdx.x]) * (top / 524288.0f);
     int32_t n_before = mine;
     float m_before = weighs;
     block_scan(s, n_before, m_before);
@@ -904,7 +915,7 @@ __device__ __forceinline__ int32_t narrow(Shared &s, int32_t n, float least, flo
     mass += s.f[0];
     for (int32_t i = threadIdx.x; i < n; i += kThreads) {
         const unsigned long long e = s.list[i];
-        if (place(list_value(e)) == bin) s.sub[atomicAdd(&s.n, 1)] = e;
+        if (place(e) == bin) s.sub[atomicAdd(&s.n, 1)] = e;
     }
     __syncthreads();
     n = s.n;
@@ -921,6 +932,9 @@ __device__ __forceinline__ float bin_floor(const Bins &bins, int32_t last) {
     if (last < 0) return INFINITY;
     uint32_t lo = lowest, hi = highest;  // bin(lo) > last, or lo is the answer; bin(hi) <= last
     if (bins.bin(key_value(lo)) <= last) return key_value(lo);
+    // it is most likely where the arithmetic says, give or take its rounding
+    const float about = bins.top - float(last + 1) / kBinsPerUnit, off = 4e-7f * (fabsf(bins.top) + fabsf(about));
+    if (bins.bin(about - off) > last && bins.bin(about + off) <= last) lo = order_key(about - off), hi = order_key(about + off);
     const uint32_t lane = threadIdx.x & 31;
     while (hi - lo > 1) {  // 33 parts at a time, a lane a border
         const uint32_t step = max(1u, (hi - lo) / 33), at = min(hi, lo + step * (lane + 1));
@@ -930,6 +944,19 @@ __device__ __forceinline__ float bin_floor(const Bins &bins, int32_t last) {
         lo += step * (first - 1);
     }
     return key_value(hi);
+}
+
+// Bit i: x[i] is at least `least` (finite) and below `above` (not NaN). By the signs of the
+// differences (a difference is zero only between equal numbers, and +inf - +inf has
+// no sign bit): two instructions a comparison, where a flag turned into a bit takes three.
+__device__ __forceinline__ uint32_t inside(const float (&x)[8], float least, float above) {
+    uint32_t under = 0u, over = 0u;
+#pragma unroll
+    for (int i = 7; i >= 0; i--) {
+        under = __funnelshift_l(__float_as_uint(__fsub_rn(x[i], least)), under, 1);
+        over = __funnelshift_l(__float_as_uint(__fsub_rn(x[i], above)), over, 1);
+    }
+    return ~under & over & 255u;
 }
 
 // One pass over the groups that reach `least`, by CTA `rank` of `ctas`: s.list gets
@@ -951,8 +978,7 @@ __device__ __forceinline__ float split_at(Shared &s, Shared &first, const GroupL
 #pragma unroll
             for (int g = 0; g < kQuad; g++) {
                 if (j[g] < 0) continue;
-#pragma unroll
-                for (int i = 0; i < 8; i++) in |= uint32_t(x[g][i] >= least && x[g][i] < above) << (8 * g + i);
+                in |= inside(x[g], least, above) << (8 * g);
                 if (weigh) {
                     float part = 0.0f;
 #pragma unroll
@@ -1290,11 +1316,21 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_pick(SampleArgs a) {
         }
         if (n > kList) break;
         fill_list(s, row, n);
-        if (n > kThreads && step != kSmall && above < M)
-            n = narrow(s, n, least, above, top, c, step == kCount ? way.k : -1, target, n_above, mass);
+        for (int by_id = above < M ? 0 : 1; step != kSmall && by_id < 2 && n > kNarrow; by_id++) {
+            if (by_id) {  // bf16 logits of one value come by the thousand
+                __syncthreads();
+                const uint32_t key = uint32_t(s.list[0] >> 32);
+                bool same = true;
+                for (int32_t i = threadIdx.x; i < n; i += kThreads) same &= uint32_t(s.list[i] >> 32) == key;
+                if (!__syncthreads_and(same)) break;
+                top = weight(key_value(key), M, way.T);
+            }
+            n = narrow(s, n, least, above, top, c, step == kCount ? way.k : -1, target, by_id ? (a.V + kThreads - 1) / kThreads : 0,
+                       n_above, mass);
+        }
         sort_list(s, n);
         if (step == kSmall) {
-            if (threadIdx.x >= 32) return;  // one warp does the rest (such a row's cluster shares nothing)
+            if (__shfl_sync(~0u, threadIdx.x >> 5, 0)) return;  // one warp does the rest (such a row's cluster shares nothing)
             token = draw_small(s, min(way.k, n), way, M, seed, lane);
             break;
         }
