@@ -312,9 +312,17 @@ __device__ __forceinline__ void block_scan(Shared &s, int32_t &n, float &m) {
     m = (lane ? upto : 0.0f) + (warp ? mw : 0.0f);
 }
 
+// The sums over the warp of two values, that of v[g] in lanes 16 g to 16 g + 15.
+__device__ __forceinline__ float warp_sums(const float (&v)[2], int lane) {
+    const bool high = lane & 16;
+    float x = (high ? v[1] : v[0]) + __shfl_xor_sync(~0u, high ? v[0] : v[1], 16);
+#pragma unroll
+    for (int d = 8; d; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
+    return x;
+}
 // The sums over the warp of four values, in six exchanges: that of v[g] in lanes
 // 8 g to 8 g + 7.
-__device__ __forceinline__ float warp_sum4(const float (&v)[kQuad], int lane) {
+__device__ __forceinline__ float warp_sums(const float (&v)[4], int lane) {
     const bool high = lane & 16, odd = lane & 8;
     const float a = (high ? v[2] : v[0]) + __shfl_xor_sync(~0u, high ? v[0] : v[2], 16);
     const float b = (high ? v[3] : v[1]) + __shfl_xor_sync(~0u, high ? v[1] : v[3], 16);
@@ -455,7 +463,7 @@ __device__ __forceinline__ float words_max(const uint32_t (&w)[8]) {
 }
 
 template <typename T, bool kAligned>
-__global__ void __launch_bounds__(kGroupThreads, sizeof(T) == 2 && kAligned ? 3 : 2) k_sample_groups(SampleArgs a) {
+__global__ void __launch_bounds__(kGroupThreads, 3) k_sample_groups(SampleArgs a) {
     __shared__ __align__(16) uint32_t hist[2 * kBins];  // counts, weights
     pdl_launch_dependents();
     pdl_wait();
@@ -463,16 +471,16 @@ __global__ void __launch_bounds__(kGroupThreads, sizeof(T) == 2 && kAligned ? 3 
     const int32_t b = blockIdx.y;
     const GroupLoad<T, kAligned> load(row_at<T>(a, b));
     const int32_t j0 = int32_t(blockIdx.x) * a.chunk, j1 = min(a.G, j0 + a.chunk);
-    // four groups a warp at a time, those of the next turn asked for ahead
-    constexpr int kStep = kGroupThreads / 32 * kQuad;
-    uint4 q[kQuad][2] = {};
-    auto all_whole = [&](int32_t j) { return j + kQuad <= j1 && load.whole(j + kQuad - 1); };
+    // some groups a warp at a time, those of the next turn asked for ahead
+    constexpr int kTake = sizeof(T) == 2 && kAligned ? 4 : 2, kStep = kGroupThreads / 32 * kTake;
+    uint4 q[kTake][2] = {};
+    auto all_whole = [&](int32_t j) { return j + kTake <= j1 && load.whole(j + kTake - 1); };
     auto read = [&](int32_t j) {
         if (!all_whole(j)) return;
 #pragma unroll
-        for (int g = 0; g < kQuad; g++) load.read(j + g, lane, q[g]);
+        for (int g = 0; g < kTake; g++) load.read(j + g, lane, q[g]);
     };
-    read(j0 + warp * kQuad);
+    read(j0 + warp * kTake);
     const Way way = row_way(a, b);
     const float c = __fdiv_rn(kLog2e, way.T);
     const bool binned = wants_hist(way, a.G);
@@ -518,19 +526,19 @@ __global__ void __launch_bounds__(kGroupThreads, sizeof(T) == 2 && kAligned ? 3 
             if (lane < 4 && j + lane < j1) stats[j + lane] = mine;
         }
     } else {
-        for (int32_t j = j0 + warp * kQuad; j < j1; j += kStep) {
-            float m[kQuad], sum[kQuad];
-            uint32_t w[kQuad][8];
+        for (int32_t j = j0 + warp * kTake; j < j1; j += kStep) {
+            float m[kTake], sum[kTake];
+            uint32_t w[kTake][8];
             const bool whole = all_whole(j);
             if (whole) {
 #pragma unroll
-                for (int g = 0; g < kQuad; g++) load.words(q[g], w[g]);
+                for (int g = 0; g < kTake; g++) load.words(q[g], w[g]);
                 read(j + kStep);
                 // exp((x - m) / T) as 2^(x c - m c): the product m c is rounded, which its
                 // remainder makes good for the whole group. NaN and infinities make the
                 // sum NaN: it is then taken again with care.
 #pragma unroll
-                for (int g = 0; g < kQuad; g++) {
+                for (int g = 0; g < kTake; g++) {
                     m[g] = warp_max(words_max<T>(w[g]));
                     const float mc = m[g] > -INFINITY ? m[g] * c : 0.0f;
                     float part = 0.0f;
@@ -541,13 +549,13 @@ __global__ void __launch_bounds__(kGroupThreads, sizeof(T) == 2 && kAligned ? 3 
             } else {
                 read(j + kStep);
 #pragma unroll
-                for (int g = 0; g < kQuad; g++) sum[g] = NAN;
+                for (int g = 0; g < kTake; g++) sum[g] = NAN;
             }
-            float total = warp_sum4(sum, lane);
+            float total = warp_sums(sum, lane);
             const bool again = __any_sync(~0u, !(total >= 0.0f));
             if (again || binned) {
 #pragma unroll
-                for (int g = 0; g < kQuad; g++) {
+                for (int g = 0; g < kTake; g++) {
                     if (j + g >= j1) continue;
                     float x[8];
                     if (whole) {
@@ -562,11 +570,11 @@ __global__ void __launch_bounds__(kGroupThreads, sizeof(T) == 2 && kAligned ? 3 
                     }
                     if (binned) add_bins(x);
                 }
-                if (again) total = warp_sum4(sum, lane);
+                if (again) total = warp_sums(sum, lane);
             }
-            const int mine = lane >> 3;
-            if ((lane & 7) == 0 && j + mine < j1)
-                stats[j + mine] = make_float2(mine & 2 ? (mine & 1 ? m[3] : m[2]) : (mine & 1 ? m[1] : m[0]), total);
+            const int mine = lane / (32 / kTake);
+            if (lane % (32 / kTake) == 0 && j + mine < j1)
+                stats[j + mine] = make_float2(mine & 2 ? (mine & 1 ? m[kTake - 1] : m[kTake - 2]) : (mine & 1 ? m[1] : m[0]), total);
         }
     }
     if (binned) {
