@@ -120,6 +120,7 @@ constexpr int kColumns = 64;       // tokens of an epilogue warp
 constexpr int kHeadSmem = 226 * 1024;
 constexpr int kFewMaxD = 32768;    // longest hidden state whose row fits k_head_rows' shared memory
 constexpr int kNeedTiles = 2048;   // tiles of a CTA whose need is looked up ahead
+constexpr int kLookRows = 16384;   // largest batch of which every CTA looks whether a row is left to it
 constexpr int kScaleSlots = 8;     // of two blocks' scales: more blocks than can be between the copies and the epilogue
 constexpr int kTurn = 32 * 17;     // words of a warp's block of 16 tokens, turned
 
@@ -138,10 +139,8 @@ struct HeadArgs {
     int64_t stride;
     Grammar g;
     // with a grammar, of each row (k_head_rows):
-    int32_t *count;        // [M] its allowed tokens where they are few (listed, logits computed), else -1
+    int32_t *dense;        // [M] 0: k_head_rows wrote its logits, 1: k_head_logits does
     uint32_t *used;        // [M][used_words] bit i: it allows one of tokens 128 i .. 128 i + 127
-    int32_t *token;        // [M][kFew] the list
-    float *value;          // [M][kFew] their logits
     int32_t used_words;
 };
 
@@ -152,8 +151,9 @@ struct HeadArgs {
 // scattered over the vocabulary: reading whole tiles of weights for them would
 // cost hundreds of times more. A CTA per row counts the row's allowed tokens;
 // where they are at most kFew (and the batch has no free row nearby, whose
-// tiles are multiplied anyway) it lists them and computes their logits, a warp
-// a token, which the tiles' kernel then writes into its -inf.
+// tiles are multiplied anyway) it asks for their weights, writes -inf over the
+// row while those arrive, computes their logits, a warp a token, and writes
+// them: the tiles' kernel leaves such a row out.
 constexpr int kFew = 256;
 constexpr int kNear = 256;         // rows among which one free row makes all dense
 constexpr int kRowThreads = 512;
@@ -176,6 +176,7 @@ __device__ __forceinline__ float dot16(const uint4 &x, const uint4 &w) {
     return sum;
 }
 
+template <typename T>
 __global__ void __launch_bounds__(kRowThreads, 2) k_head_rows(HeadArgs a) {
     extern __shared__ __align__(16) unsigned char dynamic_smem[];  // the row's values, then its scales
     __shared__ int32_t few[kFew];
@@ -198,6 +199,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_head_rows(HeadArgs a) {
         for (int i = 0; i < kBatch; i++) {
             const int32_t w = w0 + i * kRowThreads;
             word[i] = w < W ? row.word(w) : 0u;
+            if (w == W - 1 && a.V & 31) word[i] &= (1u << (a.V & 31)) - 1u;  // bits past V are nobody's
         }
 #pragma unroll
         for (int i = 0; i < kBatch; i++) {
@@ -216,14 +218,27 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_head_rows(HeadArgs a) {
     const bool dense = __syncthreads_or(free_near);
     const int32_t n = n_few;
     if (row.kind == kAllowAll || dense || n > kFew || a.D > kFewMaxD) {
-        if (threadIdx.x == 0) a.count[m] = -1;
+        if (threadIdx.x == 0) a.dense[m] = 1;
         return;
     }
+    if (threadIdx.x == 0) a.dense[m] = 0;
+    for (int32_t i = warp; i < n; i += kRowThreads / 32)
+        for (int32_t c = lane * 128; c < a.D; c += 32 * 128) prefetch_l2(a.w + int64_t(few[i]) * a.D + c);
     float *scales = reinterpret_cast<float *>(dynamic_smem + a.D);
     for (int32_t i = threadIdx.x; i < a.D / 16; i += kRowThreads)
         reinterpret_cast<uint4 *>(dynamic_smem)[i] = __ldg(reinterpret_cast<const uint4 *>(a.q + int64_t(m) * a.D) + i);
     for (int32_t i = threadIdx.x; i < a.blocks; i += kRowThreads) scales[i] = __ldg(a.s + i * a.pitch + m);
-    __syncthreads();
+    // -inf: to a 16-byte boundary, 16 bytes at a time, and the rest
+    T *out = static_cast<T *>(a.logits) + m * a.stride;
+    constexpr int kVec = 16 / int(sizeof(T));
+    const int32_t ahead = int32_t((16 - (reinterpret_cast<uintptr_t>(out) & 15)) & 15) / int32_t(sizeof(T)), head = min(ahead, a.V);
+    const int32_t body = (a.V - head) / kVec, tail = head + body * kVec;
+    const uint32_t pair = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
+    if (int32_t(threadIdx.x) < head) out[threadIdx.x] = from_f32<T>(-INFINITY);
+    for (int32_t i = threadIdx.x; i < body; i += kRowThreads)
+        reinterpret_cast<uint4 *>(out + head)[i] = make_uint4(pair, pair, pair, pair);
+    if (tail + int32_t(threadIdx.x) < a.V) out[tail + threadIdx.x] = from_f32<T>(-INFINITY);
+    __syncthreads();  // before the logits, too
     for (int32_t i = warp; i < n; i += kRowThreads / 32) {
         const int32_t v = few[i];
         const uint4 *w = reinterpret_cast<const uint4 *>(a.w + int64_t(v) * a.D);
@@ -247,12 +262,8 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_head_rows(HeadArgs a) {
         }
 #pragma unroll
         for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
-        if (lane == 0) {
-            a.token[int64_t(m) * kFew + i] = v;
-            a.value[int64_t(m) * kFew + i] = sum;
-        }
+        if (lane == 0) out[v] = from_f32<T>(sum);
     }
-    if (threadIdx.x == 0) a.count[m] = n;
 }
 
 // Whether row m allows a token of tokens v0 .. v0 + 127 (v0 a multiple of 128).
@@ -260,34 +271,20 @@ __device__ __forceinline__ bool row_uses(const HeadArgs &a, int32_t m, int32_t v
     return (__ldg(a.used + int64_t(m) * a.used_words + (v0 >> 12)) >> ((v0 >> 7) & 31)) & 1u;
 }
 
-// Writes the listed logits of row m within tokens [v0, v1), as thread `lane` of `lanes`.
-template <typename T>
-__device__ __forceinline__ void patch_row(const HeadArgs &a, int32_t m, int32_t n, int32_t v0, int32_t v1, int lane, int lanes) {
-    T *out = static_cast<T *>(a.logits) + m * a.stride;
-    for (int32_t i = lane; i < n; i += lanes) {
-        const int32_t v = __ldg(a.token + int64_t(m) * kFew + i);
-        if (v >= v0 && v < v1) out[v] = from_f32<T>(__ldg(a.value + int64_t(m) * kFew + i));
-    }
-}
-
-// Rows [m0, m1) of a tile that no dense row allows a token of: -inf, and the
-// listed logits. By the epilogue warps; NT tokens, fewer at the end.
+// The dense rows of [m0, m1) in a tile that none of them allows a token of: -inf.
+// By the epilogue warps; NT tokens, fewer at the end.
 // (A call, so that its unrolled stores take no registers from the sums of the other tiles.)
 template <typename T, int NT, int kWarps>
 __device__ __noinline__ void fill_tile(const HeadArgs &a, int32_t m0, int32_t m1, int32_t v0, int warp, int lane) {
     constexpr int kVec = 16 / int(sizeof(T)), kEach = kRows / kWarps;
     const int32_t v1 = min(a.V, v0 + NT);
     const uint32_t pair = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
-    // which of the warp's rows have listed logits here: a lane a row, asked for ahead of the stores
-    int32_t listed = 0;
-    const int32_t mine = m0 + warp + lane * kWarps;
-    if (lane < kEach && mine < m1 && (row_uses(a, mine, v0) || (NT > 128 && v0 + 128 < a.V && row_uses(a, mine, v0 + 128))))
-        listed = __ldg(a.count + mine);
+    const int32_t mine = m0 + warp + lane * kWarps;  // a lane a row
+    const uint32_t dense = __ballot_sync(~0u, lane < kEach && mine < m1 && __ldg(a.dense + mine));
 #pragma unroll 4
     for (int j = 0; j < kEach; j++) {
-        const int32_t m = m0 + warp + j * kWarps;
-        if (m >= m1) break;
-        T *out = static_cast<T *>(a.logits) + m * a.stride + v0;
+        if (!((dense >> j) & 1u)) continue;
+        T *out = static_cast<T *>(a.logits) + (m0 + warp + j * kWarps) * a.stride + v0;
         if (v1 - v0 == NT && (reinterpret_cast<uintptr_t>(out) & 15) == 0) {
 #pragma unroll
             for (int i = 0; i < NT / kVec; i += 32)
@@ -296,23 +293,19 @@ __device__ __noinline__ void fill_tile(const HeadArgs &a, int32_t m0, int32_t m1
             for (int32_t i = lane; i < v1 - v0; i += 32) out[i] = from_f32<T>(-INFINITY);
         }
     }
-    __syncwarp();
-    for (uint32_t rows = __ballot_sync(~0u, listed > 0); rows; rows &= rows - 1) {
-        const int j = __ffs(rows) - 1;
-        patch_row<T>(a, m0 + warp + j * kWarps, __shfl_sync(~0u, listed, j), v0, v1, lane, 32);
-    }
 }
 
-// 16 tokens from v on of a warp's 32 rows from m on (of which `rows` are there),
-// a row a thread. Where every row is on a 32-byte boundary a thread writes its
-// own 32 bytes at a time; else the block is turned in shared memory, so that
-// lanes write consecutive tokens.
-template <typename T>
-__device__ __forceinline__ void store16(const HeadArgs &a, float *turn, const float *x, int32_t m, int32_t rows, int32_t v,
-                                        int lane, bool wide) {
+// 16 tokens from v on of a warp's 32 rows from m on (of which `rows` are there, and
+// with kSome those whose bit of `some` is set), a row a thread. Where every row is
+// on a 32-byte boundary a thread writes its own 32 bytes at a time; else the block
+// is turned in shared memory, so that lanes write consecutive tokens. (One test
+// more for each store, in kSome only, costs 64 unaligned rows 6 us of 101.)
+template <typename T, bool kSome>
+__device__ __forceinline__ void store16(const HeadArgs &a, float *turn, const float *x, int32_t m, int32_t rows, uint32_t some,
+                                        int32_t v, int lane, bool wide) {
     T *out = static_cast<T *>(a.logits) + m * a.stride + v;
     if (wide && v + 16 <= a.V) {
-        if (lane >= rows) return;
+        if (lane >= rows || (kSome && !((some >> lane) & 1u))) return;
         T *mine = out + lane * a.stride;
         uint32_t r[8];
         if (sizeof(T) == 2) {
@@ -337,7 +330,8 @@ __device__ __forceinline__ void store16(const HeadArgs &a, float *turn, const fl
     __syncwarp();
     const int c = lane & 15;
     if (v + c < a.V)
-        for (int r = lane >> 4; r < rows; r += 2) out[r * a.stride + c] = from_f32<T>(turn[r * 17 + c]);
+        for (int r = lane >> 4; r < rows; r += 2)
+            if (!kSome || ((some >> r) & 1u)) out[r * a.stride + c] = from_f32<T>(turn[r * 17 + c]);
     __syncwarp();
 }
 
@@ -394,6 +388,11 @@ __global__ void __launch_bounds__(kHeadThreads<kPair>, 1) k_head_logits(const __
     for (int i = threadIdx.x; i < kNeedTiles / 32; i += kHeadThreads<kPair>) need[i] = 0u;
     pdl_launch_dependents();
     pdl_wait();
+    if (a.g.mask && a.M <= kLookRows) {  // k_head_rows may have left nothing to do (the same answer in all CTAs)
+        bool any = false;
+        for (int32_t m = threadIdx.x; m < a.M; m += kHeadThreads<kPair>) any |= __ldg(a.dense + m) != 0;
+        if (!__syncthreads_or(any)) return;
+    }
     if (warp == 1) tmem_alloc<kPair>(smem_addr(&tmem_base), 512);
     __syncthreads();
     if (a.g.mask) {
@@ -401,7 +400,7 @@ __global__ void __launch_bounds__(kHeadThreads<kPair>, 1) k_head_logits(const __
         for (int32_t i = 0, t = unit; t < a.tiles && i < kNeedTiles; i++, t += units) {
             const int32_t m = t % a.m_tiles * (kRows * kCtas) + int32_t(threadIdx.x), v0 = t / a.m_tiles * NT;
             bool any = false;
-            if (threadIdx.x < kRows * kCtas && m < a.M && __ldg(a.count + m) < 0)
+            if (threadIdx.x < kRows * kCtas && m < a.M && __ldg(a.dense + m))
                 any = row_uses(a, m, v0) || (NT > 128 && v0 + 128 < a.V && row_uses(a, m, v0 + 128));
             if (__any_sync(~0u, any) && lane == 0) atomicOr(&need[i >> 5], 1u << (i & 31));
         }
@@ -472,11 +471,13 @@ __global__ void __launch_bounds__(kHeadThreads<kPair>, 1) k_head_logits(const __
             const bool ok = *static_cast<volatile int *>(&gave_up) == 0;
             if (!there) continue;
             const GrammarRow allow = grammar_row(a.g, row);
-            const int32_t few = a.g.mask ? __ldg(a.count + row) : -1;
+            const int32_t rows = min(32, m1 - mine);
+            uint32_t some = ~0u;
+            if (a.g.mask) some = __ballot_sync(~0u, __ldg(a.dense + row) != 0);
 #pragma unroll
             for (int c = 0; c < kColumns; c += 16) {
                 uint32_t bits = ~0u;
-                if (a.g.mask) bits = few < 0 && (v + c) >> 5 < a.g.W ? allow.word((v + c) >> 5) >> (c & 16) : 0u;
+                if (a.g.mask) bits = (v + c) >> 5 < a.g.W ? allow.word((v + c) >> 5) >> (c & 16) : 0u;
                 if (!ok || (bits & 0xFFFFu) != 0xFFFFu) {
 #pragma unroll
                     for (int e = 0; e < 16; e++) {
@@ -484,11 +485,10 @@ __global__ void __launch_bounds__(kHeadThreads<kPair>, 1) k_head_logits(const __
                         if (!((bits >> e) & 1u)) sum[c + e] = -INFINITY;
                     }
                 }
-                if (v + c < a.V) store16<T>(a, turn[warp - kFirst], sum + c, mine, min(32, m1 - mine), v + c, lane, wide);
+                if (v + c >= a.V) continue;
+                if (some == ~0u) store16<T, false>(a, turn[warp - kFirst], sum + c, mine, rows, some, v + c, lane, wide);
+                else store16<T, true>(a, turn[warp - kFirst], sum + c, mine, rows, some, v + c, lane, wide);
             }
-            __syncwarp();
-            if (few > 0 && mine + lane < m1 && v < a.V && row_uses(a, row, v & ~127))
-                patch_row<T>(a, row, few, v, v + kColumns, 0, 1);
         }
     } else {
         if (kPair) fewer_registers<32>();
@@ -687,14 +687,12 @@ namespace {
 // Where the parts of the workspace lie.
 struct HeadSpace {
     int32_t used_words;
-    int64_t count, used, token, value, bytes;
+    int64_t dense, used, bytes;
     HeadSpace(int32_t M, int32_t V) {
         used_words = int32_t((int64_t(V) + 4095) / 4096);
-        count = 0;
+        dense = 0;
         used = (int64_t(M) * 4 + 15) / 16 * 16;
-        token = used + (int64_t(M) * used_words * 4 + 15) / 16 * 16;
-        value = token + int64_t(M) * kFew * 4;
-        bytes = value + int64_t(M) * kFew * 4;
+        bytes = used + int64_t(M) * used_words * 4;
     }
 };
 }  // namespace
@@ -746,20 +744,19 @@ extern "C" int trie_head_logits(const uint8_t *d_q, const float *d_scales, int64
     const int64_t tiles = (int64_t(V) + side - 1) / side * a.m_tiles;
     if (tiles > 0x3FFFFFFF) return set_error(TRIE_EINVAL, "M x V is too large");
     a.tiles = int32_t(tiles);
+    const bool f32 = dtype == TRIE_DTYPE_F32;
     cudaError_t e;
     if (d_mask) {
         const HeadSpace at(M, V);
         unsigned char *base = static_cast<unsigned char *>(d_workspace);
-        a.count = reinterpret_cast<int32_t *>(base + at.count);
+        a.dense = reinterpret_cast<int32_t *>(base + at.dense);
         a.used = reinterpret_cast<uint32_t *>(base + at.used);
-        a.token = reinterpret_cast<int32_t *>(base + at.token);
-        a.value = reinterpret_cast<float *>(base + at.value);
         a.used_words = at.used_words;
         const int smem = D <= kFewMaxD ? D + a.blocks * 4 : 0;
-        if ((e = launch_pdl_smem(k_head_rows, M, kRowThreads, smem, stream, a)) != cudaSuccess)
-            return fail_launch(e, "head rows launch");
+        e = f32 ? launch_pdl_smem(k_head_rows<float>, M, kRowThreads, smem, stream, a)
+                : launch_pdl_smem(k_head_rows<__nv_bfloat16>, M, kRowThreads, smem, stream, a);
+        if (e != cudaSuccess) return fail_launch(e, "head rows launch");
     }
-    const bool f32 = dtype == TRIE_DTYPE_F32;
     e = pair ? (f32 ? launch_head<float, true>(a, stream) : launch_head<__nv_bfloat16, true>(a, stream))
              : (f32 ? launch_head<float, false>(a, stream) : launch_head<__nv_bfloat16, false>(a, stream));
     if (e != cudaSuccess) return fail_launch(e, "head launch");

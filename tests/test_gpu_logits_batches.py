@@ -11,6 +11,7 @@ import pytest
 import logits_ref as ref
 import test_gpu_penalize as penalize
 import test_gpu_sample as sample
+from paper_2608_12574_gb300 import triemask as T
 
 pytestmark = pytest.mark.gpu
 cuda = sample.cuda
@@ -60,3 +61,35 @@ def test_penalize_batches(cuda, V, B, H, n_bias, rows, dtype):
     case = penalize._case(rng, V, B, H, n_bias, rows, dtype)
     out = penalize._run(cuda, V, *case)
     penalize._check(case[0][:, :V], out, *case[1:])
+
+
+@pytest.mark.parametrize("V", [33, 257, 1001, 5003])
+def test_mask_bits_past_the_vocabulary(cuda, V):
+    """A mask's last word may have bits past V: they name no token."""
+    import torch
+    rng = np.random.default_rng(V)
+    B, D = 6, 64
+    allowed = rng.random((4, V)) < np.array([0.0, 3 / V, 0.5, 1.0])[:, None]
+    states = torch.tensor([0, 1, 2, 3, 1, ref.FINISHED], dtype=torch.int32, device=cuda)
+    clean = torch.from_numpy(ref.pack(allowed)).to(cuda)
+    dirty = clean.clone()
+    dirty[:, -1] |= torch.tensor(np.uint32((0xFFFFFFFF << (V % 32)) & 0xFFFFFFFF).view(np.int32).item(), device=cuda)
+    w, ws = T.trie_head_quantize_weight(torch.from_numpy(rng.normal(0, 0.1, (V, D)).astype(np.float32)).to(cuda))
+    q, s = T.trie_head_quantize(torch.from_numpy(rng.normal(0, 1, (B, D)).astype(np.float32)).to(cuda))
+    seeds = torch.arange(B, device=cuda)
+    for rows in (slice(0, B), slice(0, 2), slice(1, 3)):  # with and without rows that allow many
+        got = []
+        for mask in (clean, dirty):
+            n = rows.stop - rows.start
+            whole = torch.full((n + 1, V + 3), 7.0, device=cuda)
+            out = whole[:n, :V]
+            st = states[rows].contiguous()
+            qn, sn = T.trie_head_quantize(torch.from_numpy(np.ones((n, D), np.float32)).to(cuda)) if n != B else (q, s)
+            T.trie_head_logits(qn, sn, w, ws, out, mask, st)
+            head = out.clone()
+            T.trie_penalize(out, mask=mask, states=st)
+            tok, lp = T.trie_sample(out, seeds[:n], mask=mask, states=st)
+            assert bool((whole[n:] == 7).all()) and bool((whole[:, V:] == 7).all())
+            got.append((head, out.clone(), tok, lp))
+        for a, b in zip(*got):
+            assert torch.equal(a, b)
