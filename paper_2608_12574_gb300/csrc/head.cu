@@ -151,12 +151,13 @@ struct HeadArgs {
 // scattered over the vocabulary: reading whole tiles of weights for them would
 // cost hundreds of times more. A CTA per row counts the row's allowed tokens;
 // where they are at most kFew (and the batch has no free row nearby, whose
-// tiles are multiplied anyway) it asks for their weights, writes -inf over the
-// row while those arrive, computes their logits, a warp a token, and writes
-// them: the tiles' kernel leaves such a row out.
+// tiles are multiplied anyway) it computes their logits, a warp a token, while
+// other warps write -inf over the row, and writes them last: the tiles' kernel
+// leaves such a row out.
 constexpr int kFew = 256;
 constexpr int kNear = 256;         // rows among which one free row makes all dense
 constexpr int kRowThreads = 512;
+static_assert(kFew <= kRowThreads, "a thread writes a logit");
 
 // Sum of 16 products of e4m3 numbers (exact in 32 bits but for the additions).
 __device__ __forceinline__ float dot16(const uint4 &x, const uint4 &w) {
@@ -180,9 +181,10 @@ template <typename T>
 __global__ void __launch_bounds__(kRowThreads, 2) k_head_rows(HeadArgs a) {
     extern __shared__ __align__(16) unsigned char dynamic_smem[];  // the row's values, then its scales
     __shared__ int32_t few[kFew];
-    __shared__ int32_t n_few;
+    __shared__ float value[kFew];
+    __shared__ int32_t n_few, pieces;
     pdl_launch_dependents();
-    if (threadIdx.x == 0) n_few = 0;
+    if (threadIdx.x == 0) n_few = pieces = 0;
     __syncthreads();
     pdl_wait();
     const int32_t m = blockIdx.x;
@@ -228,17 +230,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_head_rows(HeadArgs a) {
     for (int32_t i = threadIdx.x; i < a.D / 16; i += kRowThreads)
         reinterpret_cast<uint4 *>(dynamic_smem)[i] = __ldg(reinterpret_cast<const uint4 *>(a.q + int64_t(m) * a.D) + i);
     for (int32_t i = threadIdx.x; i < a.blocks; i += kRowThreads) scales[i] = __ldg(a.s + i * a.pitch + m);
-    // -inf: to a 16-byte boundary, 16 bytes at a time, and the rest
-    T *out = static_cast<T *>(a.logits) + m * a.stride;
-    constexpr int kVec = 16 / int(sizeof(T));
-    const int32_t ahead = int32_t((16 - (reinterpret_cast<uintptr_t>(out) & 15)) & 15) / int32_t(sizeof(T)), head = min(ahead, a.V);
-    const int32_t body = (a.V - head) / kVec, tail = head + body * kVec;
-    const uint32_t pair = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
-    if (int32_t(threadIdx.x) < head) out[threadIdx.x] = from_f32<T>(-INFINITY);
-    for (int32_t i = threadIdx.x; i < body; i += kRowThreads)
-        reinterpret_cast<uint4 *>(out + head)[i] = make_uint4(pair, pair, pair, pair);
-    if (tail + int32_t(threadIdx.x) < a.V) out[tail + threadIdx.x] = from_f32<T>(-INFINITY);
-    __syncthreads();  // before the logits, too
+    __syncthreads();
     for (int32_t i = warp; i < n; i += kRowThreads / 32) {
         const int32_t v = few[i];
         const uint4 *w = reinterpret_cast<const uint4 *>(a.w + int64_t(v) * a.D);
@@ -262,8 +254,29 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_head_rows(HeadArgs a) {
         }
 #pragma unroll
         for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
-        if (lane == 0) out[v] = from_f32<T>(sum);
+        if (lane == 0) value[i] = sum;
     }
+    // -inf: to a 16-byte boundary, 16 bytes at a time, and the rest; warps without
+    // a token (most of them) come first and take most pieces
+    T *out = static_cast<T *>(a.logits) + m * a.stride;
+    constexpr int kVec = 16 / int(sizeof(T)), kPiece = 8 * 32;
+    const int32_t ahead = int32_t((16 - (reinterpret_cast<uintptr_t>(out) & 15)) & 15) / int32_t(sizeof(T)), head = min(ahead, a.V);
+    const int32_t body = (a.V - head) / kVec, tail = head + body * kVec;
+    const uint32_t pair = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
+    if (int32_t(threadIdx.x) < head) out[threadIdx.x] = from_f32<T>(-INFINITY);
+    if (tail + int32_t(threadIdx.x) < a.V) out[tail + threadIdx.x] = from_f32<T>(-INFINITY);
+    for (;;) {
+        int32_t piece = lane == 0 ? atomicAdd(&pieces, 1) : 0;
+        piece = __shfl_sync(~0u, piece, 0);
+        if (piece > body / kPiece) break;
+#pragma unroll
+        for (int i = 0; i < kPiece / 32; i++) {
+            const int32_t at = piece * kPiece + i * 32 + lane;
+            if (at < body) reinterpret_cast<uint4 *>(out + head)[at] = make_uint4(pair, pair, pair, pair);
+        }
+    }
+    __syncthreads();
+    if (int32_t(threadIdx.x) < n) out[few[threadIdx.x]] = from_f32<T>(value[threadIdx.x]);
 }
 
 // Whether row m allows a token of tokens v0 .. v0 + 127 (v0 a multiple of 128).
