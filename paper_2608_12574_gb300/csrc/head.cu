@@ -12,6 +12,19 @@
 //  k_head_quantize_weight  a CTA per block of 128 x 128.
 //  k_head_rows             with a grammar: the logits of rows that allow few tokens.
 //  k_head_logits           the product on the tensor cores.
+//
+// What bounds it (bf16 hidden states and logits, quantization included; times of
+// calls that follow one another).
+//   1 row, V 32,000, D 2,048: 17 us, 3.9 TB/s of weights; three launch latencies
+//     and the ring's first fill are about half of it.
+//   64 rows, V 128,000, D 4,096: 93 us, 5.8 TB/s; V 128,011: 102, rows that start
+//     at any two bytes are written through shared memory.
+//   256 rows, V 152,064, D 4,096: 148 us, 4.7 TB/s and 2.15 PFLOP/s: reading each
+//     block's sums out of tensor memory and scaling them keeps the epilogue as busy
+//     as the copies and the MMAs are.
+//   1,000 rows, V 128,000, D 4,112, f32: 549 us, 1.92 PFLOP/s: the same.
+//   256 constrained rows (15 tokens each), V 152,064, D 4,096: 35 us, most of it -inf
+//     written to 78 MB behind a chain of waits (mask, list, weights).
 #include <math.h>
 #include <stdint.h>
 #include <stdio.h>
@@ -105,7 +118,9 @@ __global__ void __launch_bounds__(kQuantThreads) k_head_quantize_weight(const T 
 // on one CTA; or, for more than 128 rows, 256 by 256 on a pair of CTAs, whose
 // MMA reads each CTA's half of either operand, so that a CTA loads 32 KB for
 // twice the products (what limits larger batches is the 64 bytes a cycle that
-// an SM takes in). Either way a thread of the epilogue holds one row, and the
+// an SM takes in): 192 rows, V 128,000, D 4,096 126 us on pairs and 169 on single
+// CTAs, 256 rows, V 152,064 148 and 195; but 128 rows, V 128,000 123 and 99,
+// where half of a pair's rows would be nobody's. Either way a thread of the epilogue holds one row, and the
 // scale of a block is one number for it and the 64 or 128 tokens that it has.
 // CTAs stay and go over the tiles: one thread streams blocks of 128 columns of
 // K of both operands into a ring of stages by TMA, one issues a block's four
@@ -120,7 +135,7 @@ constexpr int kColumns = 64;       // tokens of an epilogue warp
 constexpr int kHeadSmem = 226 * 1024;
 constexpr int kFewMaxD = 32768;    // longest hidden state whose row fits k_head_rows' shared memory
 constexpr int kNeedTiles = 2048;   // tiles of a CTA whose need is looked up ahead
-constexpr int kLookRows = 16384;   // largest batch of which every CTA looks whether a row is left to it
+constexpr int kLookRows = 16384;   // largest batch of which every CTA looks whether a row is left to it (64 KB)
 constexpr int kScaleSlots = 8;     // of two blocks' scales: more blocks than can be between the copies and the epilogue
 constexpr int kTurn = 32 * 17;     // words of a warp's block of 16 tokens, turned
 
@@ -153,7 +168,8 @@ struct HeadArgs {
 // where they are at most kFew (and the batch has no free row nearby, whose
 // tiles are multiplied anyway) it computes their logits, a warp a token, while
 // other warps write -inf over the row, and writes them last: the tiles' kernel
-// leaves such a row out.
+// leaves such a row out. 256 constrained rows, V 152,064, D 4,096: 35 us, and 173
+// by tiles. A longer list than kFew would be as much to read, scattered, as tiles are.
 constexpr int kFew = 256;
 constexpr int kNear = 256;         // rows among which one free row makes all dense
 constexpr int kRowThreads = 512;
@@ -311,8 +327,9 @@ __device__ __noinline__ void fill_tile(const HeadArgs &a, int32_t m0, int32_t m1
 // 16 tokens from v on of a warp's 32 rows from m on (of which `rows` are there, and
 // with kSome those whose bit of `some` is set), a row a thread. Where every row is
 // on a 32-byte boundary a thread writes its own 32 bytes at a time; else the block
-// is turned in shared memory, so that lanes write consecutive tokens. (One test
-// more for each store, in kSome only, costs 64 unaligned rows 6 us of 101.)
+// is turned in shared memory, so that lanes write consecutive tokens (256 aligned
+// rows: 148 and 159 us, 64: 93 and 101). One test more for each store, in kSome
+// only, costs 64 unaligned rows 6 us of 101.
 template <typename T, bool kSome>
 __device__ __forceinline__ void store16(const HeadArgs &a, float *turn, const float *x, int32_t m, int32_t rows, uint32_t some,
                                         int32_t v, int lane, bool wide) {
