@@ -93,3 +93,18 @@ def test_mask_bits_past_the_vocabulary(cuda, V):
             got.append((head, out.clone(), tok, lp))
         for a, b in zip(*got):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("offset", [0, 1, 2, 4, 8])
+def test_weights_at_any_boundary(cuda, offset, dtype):
+    """Rows of weights on and off 16-byte boundaries are the same numbers."""
+    import torch
+    rng = np.random.default_rng(offset)
+    V, D = 300, 272
+    w = torch.from_numpy(rng.normal(0, 1, (V, D)).astype(np.float32)).to(getattr(torch, dtype)).to(cuda)
+    want = T.trie_head_quantize_weight(w)
+    wide = torch.zeros(V, D + 16, dtype=w.dtype, device=cuda)
+    wide[:, offset:offset + D] = w
+    got = T.trie_head_quantize_weight(wide[:, offset:offset + D])
+    assert torch.equal(want[0].view(torch.uint8), got[0].view(torch.uint8)) and torch.equal(want[1], got[1])
