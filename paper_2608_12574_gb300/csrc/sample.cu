@@ -112,6 +112,7 @@ __device__ __forceinline__ Way row_way(const SampleArgs &a, int32_t b) {
     if (!(w.p < 1.0f)) w.p = 1.0f;
     w.min_p = a.min_p ? __ldg(a.min_p + b) : 0.0f;
     if (!(w.min_p > 0.0f)) w.min_p = 0.0f;
+    if (w.min_p > 1.0f) w.k = 1, w.min_p = 0.0f;  // above every weight: only the first token, which is always kept
     return w;
 }
 

@@ -1,0 +1,40 @@
+"""trie_sample where its ranges end, against the definition in 64 bits (the rules of test_gpu_sample.py)."""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import pytest
+
+import logits_ref as ref
+from test_gpu_sample import _check, _logits, _run, cuda  # noqa: F401 (cuda: a fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def _full(B, T=1.0, k=0, p=1.0, min_p=0.0):
+    return [np.full(B, v, t) for v, t in ((T, np.float32), (k, np.int32), (p, np.float32), (min_p, np.float32))]
+
+
+def _seeds(rng, B):
+    return rng.integers(-2 ** 63, 2 ** 63 - 1, B)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [700, 40000])
+@pytest.mark.parametrize("min_p", [1.0000001, 1.5, math.inf])
+@pytest.mark.parametrize("k,p", [(0, 1.0), (0, 0.9), (50, 1.0), (300, 0.9)])
+def test_min_p_above_one(cuda, V, k, p, min_p, dtype):  # noqa: F811
+    """No weight reaches min_p: the first token is kept all the same, the lowest id of equal logits."""
+    rng = np.random.default_rng([V, k])
+    B = 6
+    x = _logits(rng, B, V, dtype)
+    x[1] = 0.5
+    x[2, V // 2:] = 40.0
+    allowed = rng.random((3, V)) < 0.01
+    allowed[2] = False
+    states = np.array([ref.FREE, ref.FREE, ref.FREE, 0, 1, 2], np.int32)
+    seeds, ways = _seeds(rng, B), _full(B, 0.7, k, p, min_p)
+    tok, lp = _run(cuda, x.to(cuda), seeds, *ways, allowed, states)
+    _check(x, seeds, *ways, allowed, states, tok, lp)
+    assert tok[1] == 0 and tok[2] == V // 2 and tok[5] == -1
