@@ -578,7 +578,8 @@ int64_t trie_sample_workspace(int32_t B, int32_t V);
  * splitmix64(seed + (n + 1) 0x9E3779B97F4A7C15): the same seed gives the same
  * token, so a row needs a new seed for every step.
  *   d_seeds        device int64[B]
- *   d_temperature  device float[B]; not above 0: the largest logit, lowest id
+ *   d_temperature  device float[B]; not above 0: the largest logit, lowest id;
+ *                  below 2^-126 it counts as that, infinite as the largest number
  *   d_top_k        device int32[B]; <= 0 or >= V: off
  *   d_top_p        device float[B]; not below 1: off
  *   d_min_p        device float[B]; not above 0: off

@@ -106,6 +106,8 @@ __device__ __forceinline__ Way row_way(const SampleArgs &a, int32_t b) {
     w.T = a.temperature ? __ldg(a.temperature + b) : 1.0f;
     w.greedy = !(w.T > 0.0f);
     if (w.greedy) w.T = 1.0f;
+    // to where log2(e) / T is a number above 0: else 0 * inf would make NaNs of weights
+    w.T = fminf(fmaxf(w.T, 0x1p-126f), 0x1.fffffep127f);
     w.k = a.top_k ? __ldg(a.top_k + b) : 0;
     if (w.k < 0 || w.k >= a.V) w.k = 0;
     w.p = a.top_p ? __ldg(a.top_p + b) : 1.0f;

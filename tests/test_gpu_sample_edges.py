@@ -38,3 +38,25 @@ def test_min_p_above_one(cuda, V, k, p, min_p, dtype):  # noqa: F811
     tok, lp = _run(cuda, x.to(cuda), seeds, *ways, allowed, states)
     _check(x, seeds, *ways, allowed, states, tok, lp)
     assert tok[1] == 0 and tok[2] == V // 2 and tok[5] == -1
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [700, 40001])
+@pytest.mark.parametrize("k,p,min_p", [(0, 1.0, 0.0), (50, 1.0, 0.0), (0, 0.9, 0.0), (300, 0.9, 0.2)])
+@pytest.mark.parametrize("temperature", [1e-45, 1e-39, 1e-38, 3e38, math.inf])
+def test_extreme_temperatures(cuda, temperature, V, k, p, min_p, dtype):  # noqa: F811
+    """Next to zero: the largest logits alone have weight. Next to infinity: all that are allowed and finite have
+    the same. Rows with masked, -inf and NaN logits beside free ones."""
+    rng = np.random.default_rng([V, k])
+    B = 6
+    x = _logits(rng, B, V, dtype)
+    x[1, ::3] = -math.inf
+    x[1, 1::3] = math.nan
+    x[2, 5::97] = 41.0
+    allowed = rng.random((3, V)) < 0.03
+    allowed[2, :] = False
+    states = np.array([ref.FREE, ref.FREE, ref.FREE, 0, 1, 2], np.int32)
+    seeds, ways = _seeds(rng, B), _full(B, temperature, k, p, min_p)
+    tok, lp = _run(cuda, x.to(cuda), seeds, *ways, allowed, states)
+    _check(x, seeds, *ways, allowed, states, tok, lp)
+    assert tok[5] == -1 and (tok[:5] >= 0).all()
