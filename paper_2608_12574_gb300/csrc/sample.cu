@@ -1315,6 +1315,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_pick(SampleArgs a) {
     while (step != kNone) {
         int32_t n = 0, n_above = 0;
         float mass = 0.0f, least = kLowest, above = INFINITY, top = 1.0f;
+        if (step != kSmall && M > -kLowest) break;  // infinities have no bin's end above them
         if (step == kSmall) {
             n = collect(s, load, stats, G, nth_group(s, stats, G, way.k, M, low));
         } else {

@@ -60,3 +60,20 @@ def test_extreme_temperatures(cuda, temperature, V, k, p, min_p, dtype):  # noqa
     tok, lp = _run(cuda, x.to(cuda), seeds, *ways, allowed, states)
     _check(x, seeds, *ways, allowed, states, tok, lp)
     assert tok[5] == -1 and (tok[:5] >= 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V,many,k", [(700, 4, 5), (700, 5, 5), (700, 9, 5), (700, 650, 600), (40000, 99, 100), (40000, 100, 100),
+                                      (40000, 230, 100), (40000, 20000, 100), (40000, 230, 50), (40000, 7000, 6000)])
+@pytest.mark.parametrize("p", [1.0, 0.6])
+def test_infinities(cuda, p, V, many, k, dtype):  # noqa: F811
+    """Fewer infinite logits than top_k, as many, and more: the first k in the order of their ids are kept, and finite
+    ones weigh nothing beside them. (0.6 times a number of equal weights that is no whole number of them.)"""
+    rng = np.random.default_rng([V, many, k])
+    B = 8
+    x = _logits(rng, B, V, dtype)
+    for b in range(B):
+        x[b, rng.permutation(V)[:many]] = math.inf
+    seeds, ways = _seeds(rng, B), _full(B, 0.8, k, 0.6 + 1 / 700 if p < 1 else 1.0)
+    tok, lp = _run(cuda, x.to(cuda), seeds, *ways)
+    _check(x, seeds, *ways, None, None, tok, lp)
