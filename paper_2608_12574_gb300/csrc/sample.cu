@@ -1242,9 +1242,13 @@ template <typename T>
 __global__ void __launch_bounds__(kThreads, 2) k_sample_pick(SampleArgs a) {
     extern __shared__ __align__(16) unsigned char dynamic_smem[];
     Shared &s = *reinterpret_cast<Shared *>(dynamic_smem);
+    const int ctas = a.ctas, rank = ctas > 1 ? int(cluster_rank()) : 0;
+    // A CTA's shared memory may be written by the others only once it is known to run: the
+    // cluster meets behind the wait for the pass, which takes longer.
+    if (ctas > 1) cluster_arrive();
     pdl_launch_dependents();
     pdl_wait();
-    const int ctas = a.ctas, rank = ctas > 1 ? int(cluster_rank()) : 0;
+    if (ctas > 1) cluster_wait();
     const int32_t b = int32_t(blockIdx.x) / ctas, G = a.G;
     const int lane = threadIdx.x & 31;
     const float2 *stats = a.stats + int64_t(b) * G;

@@ -77,3 +77,19 @@ def test_infinities(cuda, p, V, many, k, dtype):  # noqa: F811
     seeds, ways = _seeds(rng, B), _full(B, 0.8, k, 0.6 + 1 / 700 if p < 1 else 1.0)
     tok, lp = _run(cuda, x.to(cuda), seeds, *ways)
     _check(x, seeds, *ways, None, None, tok, lp)
+
+
+@pytest.mark.parametrize("B", [1, 5, 76, 120])
+def test_first_word_to_the_cluster(cuda, B):  # noqa: F811
+    """Rows whose CTAs share the pass and that have nothing to choose from, beside rows that have: the first CTA tells
+    the others so as soon as it starts, again and again in a row of calls."""
+    rng = np.random.default_rng(B)
+    V = 300
+    x = _logits(rng, B, V, "f32")
+    x[::2] = -math.inf
+    seeds, ways = _seeds(rng, B), _full(B, 0.9, 0, 0.8)
+    dev = x.to(cuda)
+    for _ in range(20):
+        tok, lp = _run(cuda, dev, seeds, *ways)
+        assert (tok[::2] == -1).all()
+    _check(x, seeds, *ways, None, None, tok, lp)
