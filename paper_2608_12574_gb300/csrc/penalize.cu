@@ -283,6 +283,7 @@ __device__ __forceinline__ void write_entries(const PenalizeArgs &a, const Table
             const uint32_t more_rest = lane + 32 < queued ? queue[kWrites * 32 + 32 + lane] : 0u;
             __syncwarp();
             queue[lane] = rest, queue[lane + 32] = more_rest;
+            __syncwarp();  // before other lanes enter theirs at these places
         }
         if (!more) break;
     }
