@@ -430,6 +430,7 @@ extern "C" int trie_penalize(void *d_logits, int dtype, int64_t stride, int32_t 
     using namespace tmk;
     const char *bad = check_logits(d_logits, dtype, stride, B, V);
     if (!*bad) bad = check_grammar(d_mask, mask_rows, d_states);
+    if (!d_history) max_length = 0;  // of no history
     if (!*bad && d_history) {
         if (!d_length) bad = "d_history without d_length";
         else if (max_length < 0 || max_length > (1 << 28)) bad = "max_length must be in [0, 2^28]";

@@ -24,3 +24,20 @@ def test_full_queues(cuda, H, B):  # noqa: F811
     case[2][:] = H - np.arange(B)
     out = _run(cuda, V, *case)
     _check(case[0], out, *case[1:])
+
+
+@pytest.mark.parametrize("max_length", [-5, 8, 70000, 2 ** 28 + 9, 2 ** 31 - 1])
+def test_no_history(cuda, max_length):  # noqa: F811
+    """Without a history its length says nothing: biases and the grammar as ever."""
+    import torch
+    rng = np.random.default_rng(3)
+    V, B = 20000, 5
+    case = list(_case(rng, V, B, 0, 700, 4, "f32"))
+    x = case[0].to(cuda)
+    off, tok, val, mask, states = (torch.from_numpy(np.ascontiguousarray(a)).to(cuda)
+                                   for a in (*case[7], ref.pack(case[8]), case[9]))
+    rc = T.load_library().trie_penalize(
+        x.data_ptr(), 0, V, B, V, None, 0, max_length, None, None, None, None, None, off.data_ptr(), tok.data_ptr(),
+        val.data_ptr(), mask.data_ptr(), mask.shape[0], states.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    assert rc == T.TRIE_OK, T.trie_last_error()
+    _check(case[0], x.cpu(), None, None, None, None, None, None, *case[7:])
