@@ -78,11 +78,16 @@ inline const char *check_logits(const void *d_logits, int dtype, int64_t stride,
         return "d_logits is not aligned to its element size";
     return "";
 }
+// Whether an address (or several, or-ed) is off a boundary of `size` bytes; NULL is on any.
+template <typename... P>
+inline bool off_boundary(size_t size, const P *...p) {
+    return ((reinterpret_cast<uintptr_t>(p) | ...) & (size - 1)) != 0;
+}
 inline const char *check_grammar(const uint32_t *d_mask, int32_t mask_rows, const int32_t *d_states) {
     if (!d_mask) return d_states ? "d_states without d_mask" : "";
     if (!d_states) return "d_mask without d_states";
     if (mask_rows < 0) return "mask_rows must be >= 0";
-    if (reinterpret_cast<uintptr_t>(d_mask) & 3) return "d_mask is not aligned to 4 bytes";
+    if (off_boundary(4, d_mask, d_states)) return "d_mask / d_states are not aligned to 4 bytes";
     return "";
 }
 inline Grammar make_grammar(const uint32_t *d_mask, int32_t mask_rows, const int32_t *d_states, int32_t V) {

@@ -438,6 +438,9 @@ extern "C" int trie_penalize(void *d_logits, int dtype, int64_t stride, int32_t 
     }
     if (!*bad && d_bias_offsets && (!d_bias_tokens || !d_bias_values))
         bad = "d_bias_offsets without d_bias_tokens and d_bias_values";
+    if (!*bad && off_boundary(4, d_history, d_length, d_prompt, d_repetition, d_presence, d_frequency, d_bias_offsets,
+                              d_bias_tokens, d_bias_values))
+        bad = "an array is not aligned to 4 bytes";
     if (!*bad && B > 65535) bad = "B must be <= 65535";
     if (*bad) return set_error(TRIE_EINVAL, bad);
     if (B == 0) return TRIE_OK;

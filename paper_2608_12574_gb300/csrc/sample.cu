@@ -1497,6 +1497,8 @@ extern "C" int trie_sample(const void *d_logits, int dtype, int64_t stride, int3
     if (!*bad && B > 0 && (!d_tokens || !d_workspace)) bad = "d_tokens / d_workspace is NULL";
     if (!*bad && (reinterpret_cast<uintptr_t>(d_workspace) & 15)) bad = "d_workspace is not aligned to 16 bytes";
     if (!*bad && B > 0 && !d_seeds) bad = "d_seeds is NULL";
+    if (!*bad && (off_boundary(8, d_seeds) || off_boundary(4, d_temperature, d_top_k, d_top_p, d_min_p, d_tokens, d_logprobs)))
+        bad = "an array is not aligned to its elements";
     if (*bad) return set_error(TRIE_EINVAL, bad);
     if (B == 0) return TRIE_OK;
     SampleArgs a;
