@@ -83,7 +83,7 @@ struct SampleArgs {
     const int32_t *top_k;
     const float *top_p, *min_p;
     Grammar g;
-    float2 *stats;            // [B][G] largest logit, sum of weights (relative to it)
+    float2 *stats;            // [B][G] largest logit (never -0), sum of weights (relative to it)
     float *bound;             // [B][G] what a group's score in the draw is not above
     uint32_t *hist;           // [B][parts][2][kBins] counts, weights
     int32_t chunk, parts;     // groups of a CTA, CTAs of a row in k_sample_groups
@@ -539,7 +539,7 @@ __global__ void __launch_bounds__(kGroupThreads, 3) k_sample_groups(SampleArgs a
                 load.by_element(j + g, lane, x);
                 const float m = warp_max(lane_max(x));
                 const float sum = warp_sum(lane_weight(x, m, c));
-                if (lane == g) mine = make_float2(m, sum);
+                if (lane == g) mine = make_float2(m + 0.0f, sum);
                 if (binned) add_bins(x);
             }
             if (lane < 4 && j + lane < j1) stats[j + lane] = mine;
@@ -592,8 +592,10 @@ __global__ void __launch_bounds__(kGroupThreads, 3) k_sample_groups(SampleArgs a
                 if (again) total = warp_sums(sum, lane);
             }
             const int mine = lane / (32 / kTake);
-            if (lane % (32 / kTake) == 0 && j + mine < j1)
-                stats[j + mine] = make_float2(mine & 2 ? (mine & 1 ? m[kTake - 1] : m[kTake - 2]) : (mine & 1 ? m[1] : m[0]), total);
+            if (lane % (32 / kTake) == 0 && j + mine < j1) {
+                const float largest = mine & 2 ? (mine & 1 ? m[kTake - 1] : m[kTake - 2]) : (mine & 1 ? m[1] : m[0]);
+                stats[j + mine] = make_float2(largest + 0.0f, total);
+            }
         }
     }
     if (binned) {

@@ -93,3 +93,24 @@ def test_first_word_to_the_cluster(cuda, B):  # noqa: F811
         tok, lp = _run(cuda, dev, seeds, *ways)
         assert (tok[::2] == -1).all()
     _check(x, seeds, *ways, None, None, tok, lp)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [8192, 50001])
+@pytest.mark.parametrize("k,p", [(40, 1.0), (100, 1.0), (6000, 1.0), (6000, 0.7001), (0, 0.6003)])
+def test_minus_zero(cuda, k, p, V, dtype):  # noqa: F811
+    """-0 is 0, also as the largest logit of its group: the lowest ids are kept."""
+    rng = np.random.default_rng([V, k])
+    B = 8
+    x = _logits(rng, B, V, dtype)
+    x[:4] = -0.0
+    x[1, ::2] = 0.0
+    x[2, ::300] = 0.0
+    x[3, ::7] = -0.5
+    x[4:] = x[4:].clamp(max=-0.0)
+    allowed = np.ones((1, V), bool)
+    allowed[0, 1::5] = False
+    states = np.where(np.arange(B) % 4 == 3, 0, ref.FREE).astype(np.int32)
+    seeds, ways = _seeds(rng, B), _full(B, 1.1, k, p)
+    tok, lp = _run(cuda, x.to(cuda), seeds, *ways, allowed, states)
+    _check(x, seeds, *ways, allowed, states, tok, lp)
