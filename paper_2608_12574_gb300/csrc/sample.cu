@@ -611,7 +611,12 @@ __global__ void __launch_bounds__(kGroupThreads, 3) k_sample_groups(SampleArgs a
 // m-th largest logit; of every logit when fewer groups have a token. `low`: the
 // smallest maximum of those that have.
 __device__ __forceinline__ float nth_group(Shared &s, const float2 *stats, int32_t G, int32_t m, float M, float low) {
-    if (!(M <= 3.0e38f && low >= -3.0e38f) || low == M) return fminf(low, -kLowest);
+    if (!(M <= 3.0e38f && low >= -3.0e38f) || M - low < 1e-30f) {  // no intervals between them: are there m at all?
+        int32_t there = 0;
+        for (int32_t j0 = 0; j0 < G && there < m; j0 += kThreads)
+            there += __syncthreads_count(j0 + int32_t(threadIdx.x) < G && stats[j0 + threadIdx.x].x > -INFINITY);
+        return there < m ? kLowest : fminf(low, -kLowest);
+    }
     const float per = float(kThreads - 1) / (M - low);
     __syncthreads();
     s.fine.count[threadIdx.x] = 0u;

@@ -114,3 +114,38 @@ def test_minus_zero(cuda, k, p, V, dtype):  # noqa: F811
     seeds, ways = _seeds(rng, B), _full(B, 1.1, k, p)
     tok, lp = _run(cuda, x.to(cuda), seeds, *ways, allowed, states)
     _check(x, seeds, *ways, allowed, states, tok, lp)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("k,p,min_p", [(2, 1.0, 0.0), (50, 1.0, 0.0), (64, 0.9, 0.0), (50, 1.0, 0.1)])
+def test_tokens_of_one_group(cuda, k, p, min_p, dtype):  # noqa: F811
+    """All that a row allows lies in one group of 256 ids (ten digits side by side), or in two whose largest logits are
+    equal, or nearly so: fewer groups than top_k. Constrained rows, and free ones masked with -inf; infinite logits
+    beside finite ones."""
+    rng = np.random.default_rng([k, 1])
+    V, B = 16640, 96
+    x = _logits(rng, B, V, dtype)
+    allowed = np.zeros((6, V), bool)
+    allowed[0, 512:522] = True
+    allowed[1, [600, 611, 900, 901]] = True
+    allowed[2, 300:330] = allowed[2, 5000:5042] = True
+    allowed[3, [16639]] = True
+    allowed[4, 1024:1026] = True
+    allowed[5, 256:512:5] = True
+    x[:, [600, 900]] = 1.25
+    x[:, [611, 901]] = 0.75
+    x[:, 300] = x[:, 5000] = 30.0
+    x[1::12, 5000] = 30.25
+    x[:, 1024] = 1e-39
+    x[:, 1025] = 0.0
+    x[2::12, 16000] = math.inf
+    states = (np.arange(B) % 6).astype(np.int32)
+    for b in range(0, B, 4):  # the same by -inf
+        x[b, np.nonzero(~allowed[states[b]])[0]] = -math.inf
+        states[b] = ref.FREE
+    states[2::12] = ref.FREE
+    seeds, ways = _seeds(rng, B), _full(B, 1.3, k, p, min_p)
+    tok, lp = _run(cuda, x.to(cuda), seeds, *ways, allowed, states)
+    _check(x, seeds, *ways, allowed, states, tok, lp)
+    if k == 50 and min_p == 0:
+        assert len(set(tok[states == 0].tolist())) > 2
