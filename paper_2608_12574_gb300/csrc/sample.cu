@@ -554,8 +554,9 @@ __global__ void __launch_bounds__(kGroupThreads, 3) k_sample_groups(SampleArgs a
                 for (int g = 0; g < kTake; g++) load.words(q[g], w[g]);
                 read(j + kStep);
                 // exp((x - m) / T) as 2^(x c - m c): the product m c is rounded, which its
-                // remainder makes good for the whole group. NaN and infinities make the
-                // sum NaN: it is then taken again with care.
+                // remainder, where small (its square is left out: 2^-23 of the sum at 2^-11),
+                // makes good for the whole group. A larger one, NaN and infinities make the sum
+                // NaN: it is then taken again with care.
 #pragma unroll
                 for (int g = 0; g < kTake; g++) {
                     m[g] = warp_max(words_max<T>(w[g]));
@@ -563,7 +564,8 @@ __global__ void __launch_bounds__(kGroupThreads, 3) k_sample_groups(SampleArgs a
                     float part = 0.0f;
 #pragma unroll
                     for (int i = 0; i < 8; i++) part += exp2_fast(fmaf(load.value(w[g], i), c, -mc));
-                    sum[g] = m[g] > -INFINITY ? part - part * (fmaf(m[g], c, -mc) * 0.6931471806f) : part;
+                    const float rest = fmaf(m[g], c, -mc);
+                    sum[g] = !(m[g] > -INFINITY) ? part : fabsf(rest) <= 0x1p-11f ? part - part * (rest * 0.6931471806f) : NAN;
                 }
             } else {
                 read(j + kStep);

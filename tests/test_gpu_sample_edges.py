@@ -149,3 +149,25 @@ def test_tokens_of_one_group(cuda, k, p, min_p, dtype):  # noqa: F811
     _check(x, seeds, *ways, allowed, states, tok, lp)
     if k == 50 and min_p == 0:
         assert len(set(tok[states == 0].tolist())) > 2
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("temperature,offset", [(1e-2, 0.0), (1e-3, 0.0), (1e-4, 0.0), (1e-5, 0.0), (1e-6, 0.0), (1e-7, 0.0),
+                                                (1.0, 1e4), (1.0, -1e5), (0.7, 1e6), (30.0, 3e7)])
+@pytest.mark.parametrize("k,p,min_p", [(0, 1.0, 0.0), (0, 0.7003, 0.0), (50, 0.7003, 0.0), (0, 1.0, 0.5)])
+def test_large_over_temperature(cuda, temperature, offset, k, p, min_p, dtype):  # noqa: F811
+    """Logits that are many temperatures away from 0: five equal largest ones, and others a few
+    temperatures below, which 32 or 16 bits may make equal to them."""
+    import torch
+    rng = np.random.default_rng([int(1e7 * temperature), int(abs(offset))])
+    V, B = 3000, 8
+    x = _logits(rng, B, V, "f32") + offset
+    x[:, 100::700] = 37.3 + offset
+    for b in range(B):
+        x[b, rng.integers(0, V, 50)] = torch.from_numpy((37.3 + offset - temperature * rng.random(50) * 6).astype(np.float32))
+    x[:, 100::700] = 37.3 + offset
+    x = x.to(torch.float32 if dtype == "f32" else torch.bfloat16)
+    seeds, ways = _seeds(rng, B), _full(B, temperature, k, p, min_p)
+    tok, lp = _run(cuda, x.to(cuda), seeds, *ways)
+    _check(x, seeds, *ways, None, None, tok, lp)
+    assert (lp <= 1e-5).all()
