@@ -599,7 +599,12 @@ __global__ void __launch_bounds__(kHeadThreads<kPair>, 1) k_head_logits(const __
                     if (++stage == a.stages) stage = 0, phase ^= 1;
                 }
             }
-            if (!ok) {  // copies may still write to shared memory: wait for them
+            if (ok) {  // the last MMAs' arrivals on this CTA's barriers come before it ends
+                for (int i = 0; i < a.stages; i++) {
+                    bar_wait(empty + 8 * stage, phase, &gave_up);
+                    if (++stage == a.stages) stage = 0, phase ^= 1;
+                }
+            } else {  // copies may still write to shared memory: wait for them
                 int none = 0;
                 for (uint32_t i = it > kScaleSlots ? it - kScaleSlots : 0; i < it; i++)
                     bar_wait(s_full + 8 * (i % kScaleSlots), (i / kScaleSlots) & 1, &none);
