@@ -235,7 +235,7 @@ struct Shared {
             float mass[kBins];
         } hist;
         struct {
-            uint32_t count[kThreads], mass[kThreads];
+            uint32_t count[kThreads], mass[kThreads], rest[kThreads];
         } fine;
         struct {
             uint32_t count[256];
@@ -909,16 +909,20 @@ __device__ __forceinline__ int32_t draw_small(Shared &s, int32_t n, const Way &w
     return warp_best(best).id;
 }
 
-// Where the list is long: its tokens from `least` to below `above` are counted and
-// weighed (relative to `top`, the weight at `above`) by 512 equal intervals, and
-// the one in which the kept set ends becomes the list; n_above and mass grow by
-// what lies before it. By count, or by weight (count < 0). Returns the list's length.
+// Where the list is long: its tokens from `least` to below `above` are counted and,
+// where `weigh`, weighed (relative to `top`, the weight at `above`) by 512 equal
+// intervals, and the one in which the kept set ends becomes the list; n_above and
+// mass grow by what lies before it. By count, or by weight (count < 0). Returns the
+// list's length. Weights are whole numbers of 2^-39 `top`, in two parts, so that the
+// order of the atomics does not matter: of those down to kSpan powers of two below
+// `top` that leaves 27 bits, more than a sum in 32 bits keeps.
 // width > 0: the tokens are all equal, of weight `top`, and go by `width` ids.
-__device__ __forceinline__ int32_t narrow(Shared &s, int32_t n, float least, float above, float top, float c, int32_t count,
-                                          float target, int32_t width, int32_t &n_above, float &mass) {
+constexpr float kSpan = 12.0f;
+__device__ __forceinline__ int32_t narrow(Shared &s, int32_t n, float least, float above, float top, float c, bool weigh,
+                                          int32_t count, float target, int32_t width, int32_t &n_above, float &mass) {
     const float per = float(kThreads) / (above - least);
     __syncthreads();
-    s.fine.count[threadIdx.x] = s.fine.mass[threadIdx.x] = 0u;
+    s.fine.count[threadIdx.x] = s.fine.mass[threadIdx.x] = s.fine.rest[threadIdx.x] = 0u;
     if (threadIdx.x == 0) s.bin[0] = kThreads, s.ties = 0;
     __syncthreads();
     auto place = [&](unsigned long long e) {
@@ -928,11 +932,17 @@ __device__ __forceinline__ int32_t narrow(Shared &s, int32_t n, float least, flo
         const float x = list_value(s.list[i]);
         const int32_t at = place(s.list[i]);
         atomicAdd(&s.fine.count[at], 1u);
-        if (!width) atomicAdd(&s.fine.mass[at], uint32_t(fminf(exp2_fast((x - above) * c), 1.0f) * 524288.0f + 0.5f));  // kList of them fit
+        if (weigh && !width) {  // kList of either part fit
+            const float w = fminf(exp2_fast((x - above) * c), 1.0f) * 0x1p19f;
+            const uint32_t whole = uint32_t(w);
+            atomicAdd(&s.fine.mass[at], whole);
+            atomicAdd(&s.fine.rest[at], uint32_t((w - float(whole)) * 0x1p20f));
+        }
     }
     __syncthreads();
     const int32_t mine = int32_t(s.fine.count[threadIdx.x]);
-    const float weighs = width ? float(mine) * top : float(s.fine.mass[threadIdx.x]) * (top / 524288.0f);
+    const float weighed = (float(s.fine.mass[threadIdx.x]) + float(s.fine.rest[threadIdx.x]) * 0x1p-20f) * (top * 0x1p-19f);
+    const float weighs = width ? float(mine) * top : weighed;
     int32_t n_before = mine;
     float m_before = weighs;
     block_scan(s, n_before, m_before);
@@ -1357,7 +1367,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_pick(SampleArgs a) {
         }
         if (n > kList) break;
         fill_list(s, row, n);
-        for (int by_id = above < M ? 0 : 1; step != kSmall && by_id < 2 && n > kNarrow; by_id++) {
+        // (a list whose weights are too far apart is sorted as it is)
+        const bool by_value = above < M && (!by_p || (above - least) * c <= kSpan);
+        for (int by_id = by_value ? 0 : 1; step != kSmall && by_id < 2 && n > kNarrow; by_id++) {
             if (by_id) {  // bf16 logits of one value come by the thousand
                 __syncthreads();
                 const uint32_t key = uint32_t(s.list[0] >> 32);
@@ -1366,8 +1378,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_pick(SampleArgs a) {
                 if (!__syncthreads_and(same)) break;
                 top = weight(key_value(key), M, way.T);
             }
-            n = narrow(s, n, least, above, top, c, step == kCount ? way.k : -1, target, by_id ? (a.V + kThreads - 1) / kThreads : 0,
-                       n_above, mass);
+            n = narrow(s, n, least, above, top, c, by_p, step == kCount ? way.k : -1, target,
+                       by_id ? (a.V + kThreads - 1) / kThreads : 0, n_above, mass);
         }
         sort_list(s, n);
         if (step == kSmall) {

@@ -171,3 +171,46 @@ def test_large_over_temperature(cuda, temperature, offset, k, p, min_p, dtype): 
     tok, lp = _run(cuda, x.to(cuda), seeds, *ways)
     _check(x, seeds, *ways, None, None, tok, lp)
     assert (lp <= 1e-5).all()
+
+
+LEVELS = {
+    "halves": (np.arange(400, 269, -1) + 0.45) * 2.0 ** -19,  # 19 bits lose nearly half a unit of each
+    "close together": np.linspace(0.33, 0.25, 30),
+    "far apart": np.exp(-np.linspace(4.0, 9.0, 30)),
+}
+
+
+# lift: how many temperatures the largest logit is above the end of the bin
+@pytest.mark.parametrize("temperature,levels,lift,many", [(0.004, "halves", 1.8, 3900), (0.004, "close together", 1.8, 3000),
+                                                          (0.06, "close together", 0.2, 3000), (0.004, "far apart", 1.8, 2500),
+                                                          (1e-3, "far apart", 0.5, 2500)])
+@pytest.mark.parametrize("k", [0, 4500])
+def test_small_weights_of_one_bin(cuda, temperature, levels, lift, many, k):  # noqa: F811
+    """Top-p ends among thousands of tokens of small weights that lie within 1/32 of one another. Over many seeds no
+    token past the cut is drawn, and of those before it as many as their weight says. Sums of weights in 32 bits are
+    within 2^-20 of the whole; chi-square of n degrees of freedom is above n + 6 sqrt(2 n) + 20 with a probability
+    below 1e-7."""
+    import torch
+    rng = np.random.default_rng([many, k])
+    V, B = 6000, 60000
+    x = np.full(V, -5.0, np.float32)
+    at = 300 + rng.permutation(V - 300)[:many]
+    x[at] = 1.0 + temperature * np.log(rng.choice(LEVELS[levels], many))
+    x[3] = 1.0  # the first group's largest logit is where a bin ends
+    x[5000] = 1.0 + lift * temperature
+    ok = np.ones(V, bool)
+    T = float(np.float32(temperature))
+    _, w, _ = ref.kept(x, T, k, 1.0, 0.0, ok)
+    p = float(np.float32((w[0] + w[1] + 0.95 * w[2:many + 2].sum()) / w.sum()))
+    ids, w, _ = ref.kept(x, T, k, p, 0.0, ok)
+    seeds = _seeds(rng, B)
+    tok, _ = _run(cuda, torch.from_numpy(x).to(cuda).repeat(B, 1), seeds, *_full(B, temperature, k, p))
+    near = 2 + int(2.0 ** -20 * w.sum() / w[-1])  # tokens about the cut that rounding may let in or out
+    later, _, _ = ref.kept(x, T, len(ids) + near, 1.0, 0.0, ok)
+    got = np.bincount(tok, minlength=V)
+    assert got.sum() == got[later].sum(), np.setdiff1d(np.nonzero(got)[0], later)
+    part = np.array_split(np.arange(2, max(2, len(ids) - near)), 20)  # in the order of their logits
+    want = np.array([w[i].sum() for i in part]) / w.sum() * B
+    seen = np.array([got[ids[i]].sum() for i in part])
+    chi = ((seen - want) ** 2 / want).sum()
+    assert chi < 20 + 6 * math.sqrt(40) + 20, (chi, seen, want)
