@@ -1331,6 +1331,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_pick(SampleArgs a) {
     bool by_k = !way.greedy && way.k > 0;
     int32_t token = -1;
     unsigned long long last = 0ull;  // tokens below this entry (order_key << 32 | ~id) are not kept
+    unsigned long long kth = 0ull;   // the last of the first top_k, once known
     const Bins bins(stats[0].x);
     enum { kSmall, kCount, kMass, kNone };  // how the kept set is found: few by count, by count, by weight
     float target = way.p * Z;
@@ -1388,8 +1389,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_pick(SampleArgs a) {
             break;
         }
         const int32_t wanted = min(n, way.k - n_above);
+        if (step == kCount) kth = s.list[wanted - 1];
         if (step == kCount && !by_p) {
-            last = s.list[wanted - 1];
+            last = kth;
             break;
         }
         const float total = scan_list(s, n, M, way.T);
@@ -1398,7 +1400,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_pick(SampleArgs a) {
             step = kMass;
             continue;
         }
-        if (mass < target && mass + total >= target) last = s.list[cut_list(s, n, mass, target) - 1];
+        // (top_p next to 1 may let in more than the first top_k where the two lists' sums are rounded differently)
+        if (mass < target && mass + total >= target) last = max(s.list[cut_list(s, n, mass, target) - 1], kth);
         break;
     }
     if (shared) tell(0, 0.0f, 0.0f, 0.0f);

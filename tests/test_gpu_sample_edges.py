@@ -214,3 +214,20 @@ def test_small_weights_of_one_bin(cuda, temperature, levels, lift, many, k):  # 
     seen = np.array([got[ids[i]].sum() for i in part])
     chi = ((seen - want) ** 2 / want).sum()
     assert chi < 20 + 6 * math.sqrt(40) + 20, (chi, seen, want)
+
+
+@pytest.mark.parametrize("seed", range(2))
+def test_top_p_next_to_one(cuda, seed):  # noqa: F811
+    """Top-p just below 1 and top-k at the end of a bin of 1/32: no rounding lets a token past the first k in."""
+    import torch
+    rng = np.random.default_rng(seed)
+    V, B = 2000, 60000
+    x = rng.normal(0, 1, (B, V)).astype(np.float32)
+    edge = x[:, :256].max(axis=1) - (rng.integers(20, 50, B) / 32).astype(np.float32)
+    k = np.maximum(12, (x > edge[:, None]).sum(axis=1) + rng.integers(-1, 2, B)).astype(np.int32)
+    p = (1 - 2.0 ** -24 * rng.integers(1, 4, B)).astype(np.float32)
+    ways = _full(B, 4.0)
+    tok, _ = _run(cuda, torch.from_numpy(x).to(cuda), _seeds(rng, B), ways[0], k, p)
+    drawn = x[np.arange(B), tok][:, None]
+    before = (x > drawn).sum(axis=1) + ((x == drawn) & (np.arange(V) < tok[:, None])).sum(axis=1)
+    assert (before < k).all(), int((before >= k).sum())
