@@ -71,7 +71,6 @@ constexpr int kQuad = 4;            // groups that a warp takes at a time
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.4028234663852886e38f;
 constexpr uint32_t kKeyNone = 0x007FFFFFu;  // order_key(-inf)
-constexpr double kFixed = 1099511627776.0;  // 2^40
 
 struct SampleArgs {
     const void *logits;
@@ -1104,6 +1103,10 @@ __device__ __forceinline__ void find_bins(Shared &s, bool by_mass, int32_t count
     __syncthreads();
 }
 
+// Weights (at most 1) as whole numbers of 2^-40, or more where so many as a row has
+// tokens would not fit 64 bits: V of them stay below 2^63.
+__device__ __forceinline__ double fixed_one(int32_t V) { return double(1ull << min(40, 31 + __clz(V))); }
+
 // The last kept token of a prefix of the order: every token above key is kept,
 // and the first `ties` of those at key, by id.
 struct Cut {
@@ -1113,10 +1116,11 @@ struct Cut {
 };
 
 // The shortest prefix with `count` tokens (by_mass false) or a weight of at
-// least target / 2^40 (by_mass true); everything when there is none.
+// least target / fixed_one (by_mass true); everything when there is none.
 template <typename T>
 __device__ __noinline__ Cut radix_cut(Shared &s, const Row<T> &row, const float2 *stats, int32_t G, float M, float T_, bool by_mass,
                          uint32_t count, unsigned long long target) {
+    const double one = fixed_one(row.V);
     uint32_t key = 0u;
     unsigned long long above_n = 0ull, above_mass = 0ull;
     const int lane = threadIdx.x & 31;
@@ -1139,7 +1143,7 @@ __device__ __noinline__ Cut radix_cut(Shared &s, const Row<T> &row, const float2
                 if (!who) continue;
                 // the lanes that share the first one's digit add up in one go: equal logits come in crowds
                 const uint32_t digit = (k >> shift) & 255u, of_first = __shfl_sync(~0u, digit, __ffs(who) - 1);
-                const unsigned long long w = in ? (unsigned long long)(double(weight(x, M, T_)) * kFixed) : 0ull;
+                const unsigned long long w = in ? (unsigned long long)(double(weight(x, M, T_)) * one) : 0ull;
                 const bool same = in && digit == of_first;
                 const uint32_t crowd = __ballot_sync(~0u, same);
                 unsigned long long sum = same ? w : 0ull;
@@ -1187,7 +1191,7 @@ __device__ __noinline__ Cut radix_cut(Shared &s, const Row<T> &row, const float2
     Cut c;
     c.key = key;
     const int32_t there = s.ties;
-    const unsigned long long each = (unsigned long long)(double(weight(key_value(key), M, T_)) * kFixed);
+    const unsigned long long each = (unsigned long long)(double(weight(key_value(key), M, T_)) * one);
     int32_t ties = there;
     if (by_mass) {
         if (each && target > above_mass) {
@@ -1200,7 +1204,7 @@ __device__ __noinline__ Cut radix_cut(Shared &s, const Row<T> &row, const float2
         ties = int32_t(count - above_n);
     }
     c.ties = ties < 1 ? 1 : ties;
-    c.mass = float((double(above_mass) + double(c.ties) * double(each)) / kFixed);
+    c.mass = float((double(above_mass) + double(c.ties) * double(each)) / one);
     __syncthreads();
     return c;
 }
@@ -1411,7 +1415,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_pick(SampleArgs a) {
             Cut cut = {kKeyNone, 0, Z};
             for (int by = 0; by < 2; by++) {
                 if (by ? !by_p : !by_k) continue;
-                const double to = double(way.p) * double(cut.mass) * kFixed;
+                const double to = double(way.p) * double(cut.mass) * fixed_one(a.V);
                 const Cut found = radix_cut(s, row, stats, G, M, way.T, by == 1, uint32_t(way.k),
                                             to > 0.0 ? (unsigned long long)(to) : 0ull);
                 if (by == 0 || !by_k || found.key > cut.key || (found.key == cut.key && found.ties < cut.ties)) cut = found;

@@ -231,3 +231,33 @@ def test_top_p_next_to_one(cuda, seed):  # noqa: F811
     drawn = x[np.arange(B), tok][:, None]
     before = (x > drawn).sum(axis=1) + ((x == drawn) & (np.arange(V) < tok[:, None])).sum(axis=1)
     assert (before < k).all(), int((before >= k).sum())
+
+
+def _noise(seed, n):
+    """ref.noise of an array of numbers."""
+    with np.errstate(over="ignore"):
+        z = np.uint64(seed % 2 ** 64) + (n.astype(np.uint64) + np.uint64(1)) * np.uint64(0x9E3779B97F4A7C15)
+        z = (z ^ (z >> np.uint64(30))) * np.uint64(0xBF58476D1CE4E5B9)
+        z = (z ^ (z >> np.uint64(27))) * np.uint64(0x94D049BB133111EB)
+        z ^= z >> np.uint64(31)
+    return -np.log(-np.log((2 * (z >> np.uint64(41)).astype(np.float64) + 1) / 2 ** 24))
+
+
+@pytest.mark.parametrize("k,p", [(0, 0.9), (0, 0.3), (20_000_000, 0.95), (17_000_000, 1.0)])
+def test_equal_logits_of_a_huge_vocabulary(cuda, k, p):  # noqa: F811
+    """25 million equal logits: weights of more than 2^24 tokens. A token is one of the first k, or of top-p of them;
+    groups weigh the same, so the draw is the largest noise. (The two largest are about 1 apart; that the rounding of 32
+    bits decides between them is let pass for one row.)"""
+    import torch
+    V, B = 3 << 23, 24
+    x = torch.full((B, V), 0.75, dtype=torch.bfloat16, device=cuda)
+    seeds = np.random.default_rng(7).integers(-2 ** 63, 2 ** 63 - 1, B)
+    tok, lp = _run(cuda, x, seeds, *_full(B, 1.0, k, p))
+    n = math.ceil(float(np.float32(p)) * (k or V)) if p < 1 else k
+    groups = np.arange((n + 255) // 256)
+    same = 0
+    for b in range(B):
+        group = int(np.argmax(np.log(np.minimum(256, n - 256 * groups)) + _noise(int(seeds[b]), groups + 2 ** 31)))
+        ids = np.arange(256 * group, min(n, 256 * group + 256))
+        same += int(ids[np.argmax(_noise(int(seeds[b]), ids))]) == tok[b]
+    assert same >= B - 1 and np.abs(lp + math.log(V)).max() < 1e-4
