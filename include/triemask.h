@@ -495,7 +495,8 @@ int fmt_destroy(fmt_t f);
  * consecutive elements in a row; what lies between the rows is not touched.
  * 2 <= V <= 2^31 - 1024; offsets are computed in 64 bits. No call allocates or synchronises; B = 0 is
  * a no-op. All arrays are aligned to
- * their elements (TRIE_EINVAL). Errors: TRIE_EINVAL, TRIE_ECUDA. */
+ * their elements (TRIE_EINVAL) and lie on the current device, on which the
+ * kernels are launched (not checked). Errors: TRIE_EINVAL, TRIE_ECUDA. */
 
 /* Quantize M rows of D hidden states to e4m3 with a scale for each row and 128
  * columns: the block's largest magnitude times 1/448, rounded to 32 bits (1 where

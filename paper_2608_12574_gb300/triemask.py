@@ -561,6 +561,8 @@ def _rows(t, name: str) -> tuple[int, int]:
     step, one = t.stride()
     if (m > 1 and one != 1) or (n > 1 and step < m):
         raise ValueError(f"{name} must have contiguous rows that do not overlap")
+    if t.get_device() != torch._C._cuda_getDevice():  # these calls have no handle to know their device by
+        raise ValueError(f"{name} is not on the current device")
     return t.data_ptr(), step if n > 1 else m
 
 
