@@ -32,7 +32,7 @@ def _stale() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    deps = sources() + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(INCLUDE, "*.h"))
+    deps = sources() + [h for d in (CSRC, INCLUDE) for ext in ("*.h", "*.cuh") for h in glob.glob(os.path.join(d, ext))]
     return any(os.path.getmtime(d) > t for d in deps)
 
 
