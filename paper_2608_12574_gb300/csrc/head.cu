@@ -19,10 +19,10 @@
 //     and the ring's first fill are about half of it.
 //   64 rows, V 128,000, D 4,096: 93 us, 5.8 TB/s; V 128,011: 102, rows that start
 //     at any two bytes are written through shared memory.
-//   256 rows, V 152,064, D 4,096: 148 us, 4.7 TB/s and 2.15 PFLOP/s: reading each
-//     block's sums out of tensor memory and scaling them keeps the epilogue as busy
-//     as the copies and the MMAs are.
-//   1,000 rows, V 128,000, D 4,112, f32: 549 us, 1.92 PFLOP/s: the same.
+//   256 rows, V 152,064, D 4,096: 148 to 165 us by the box, 4.3 to 4.7 TB/s and 1.94
+//     to 2.15 PFLOP/s. Nothing is full (HBM 57 %, tensor pipe 48 %, issue slots 60 %): the
+//     epilogue waits for each block's sums from tensor memory before it scales them.
+//   1,000 rows, V 128,000, D 4,112, f32: 549 to 567 us, 1.9 PFLOP/s: the same.
 //   256 constrained rows (15 tokens each), V 152,064, D 4,096: 35 us, most of it -inf
 //     written to 78 MB behind a chain of waits (mask, list, weights).
 #include <math.h>

@@ -28,17 +28,17 @@
 //                   kept set ends; one pass over the groups that reach that bin
 //                   adds up what lies above it, exactly, and collects the bin.
 //                   Either way a short list in shared memory is sorted and cut.
-//                   A list that does not fit (many equal logits) leaves the row
-//                   to a radix select over all groups.
+//                   A list that does not fit (many equal logits) and infinite
+//                   logits leave the row to a radix select over all groups.
 //
 // What bounds it (times of calls that follow one another). One row of V 32,000:
 // 11 us, two launches and the chain of block-wide steps of the pick. 256 rows of
-// V 152,064 in bf16, top-k up to 64: 37 us, the pass 20 of it (78 MB at 3.9 TB/s;
+// V 152,064 in bf16, top-k up to 64: 36 us, the pass 20 of it (78 MB at 3.9 TB/s;
 // an exponent, a multiply-add and a sum for each logit are as much to issue), the
-// pick 17. 64 rows of V 262,144 in f32, every kind of filter: 74 us; the pass is 25
+// pick 16. 64 rows of V 262,144 in f32, every kind of filter: 72 us; the pass is 25
 // (the histograms' atomics), the pick 43: large kept sets are read a second time,
 // and a row's steps between wait for one another. 200 rows of V 128,011, three
-// quarters constrained: 69 us, bound by the free rows' pick.
+// quarters constrained: 70 us, bound by the free rows' pick.
 #include <math.h>
 #include <stdint.h>
 #include <stdio.h>
