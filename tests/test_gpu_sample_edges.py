@@ -36,7 +36,8 @@ def test_min_p_above_one(cuda, V, k, p, min_p, dtype):  # noqa: F811
     states = np.array([ref.FREE, ref.FREE, ref.FREE, 0, 1, 2], np.int32)
     seeds, ways = _seeds(rng, B), _full(B, 0.7, k, p, min_p)
     tok, lp = _run(cuda, x.to(cuda), seeds, *ways, allowed, states)
-    _check(x, seeds, *ways, allowed, states, tok, lp)
+    with np.errstate(invalid="ignore"):  # how far weights are from an infinite min_p
+        _check(x, seeds, *ways, allowed, states, tok, lp)
     assert tok[1] == 0 and tok[2] == V // 2 and tok[5] == -1
 
 
