@@ -306,7 +306,7 @@ def _policy(st):
     y = y - torch.log(torch.exp(y).sum(dim=1, keepdim=True))
     token = st["tokens"].clamp(min=0).long()[:, None]
     lp = y.gather(1, token)[:, 0]
-    known = (st["tokens"] >= 0) & (st["tokens"] < V) & (lp > -math.inf)
+    known = (st["tokens"] >= 0) & (st["tokens"] < V) & (lp != -math.inf)
     A, w = st["advantages"], st["weights"]
     rho = torch.exp(lp - st["old"])
     free, held = rho * A, rho.clamp(1.0 - _CLIP[0], 1.0 + _CLIP[1]) * A
