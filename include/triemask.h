@@ -91,8 +91,8 @@ enum { TRIE_DTYPE_F32 = 0, TRIE_DTYPE_BF16 = 1 };
 
 #define TRIE_STATE_DEAD (-1)
 #define TRIE_STATE_FINISHED (-2)
-/* A row of a batch without a grammar: trie_head_logits, trie_penalize and
- * trie_sample allow it every token. The other calls take it as they take any
+/* A row of a batch without a grammar: trie_head_logits, trie_head4_logits,
+ * trie_penalize, trie_sample and trie_policy_loss allow it every token. The other calls take it as they take any
  * id that is not a node, so the free rows of a mixed batch stay out of them. */
 #define TRIE_STATE_FREE (-3)
 
@@ -483,8 +483,9 @@ int fmt_apply_mask(fmt_t f, void *d_logits, int dtype, const int32_t *d_states, 
 int fmt_destroy(fmt_t f);
 
 /* ---- From hidden states to the sampled token ----
- * The calls around a mask in a decode step: the logits head, the penalties and
- * the sampler. They need no handle. Their grammar is a mask and a state for
+ * The calls around a mask in a decode step: the norm in front of the logits
+ * head, the head in 8 or 4 bits, the penalties and the sampler; and, for
+ * training on what was sampled, the policy loss. They need no handle. Their grammar is a mask and a state for
  * each row of the batch, all three optional together (d_mask NULL: every row
  * is free):
  *   d_mask     device uint32[mask_rows][ceil(V/32)], as trie_compile_masks,
@@ -534,6 +535,60 @@ int trie_head_logits(const uint8_t *d_q, const float *d_scales, int64_t pitch, c
                      const float *d_w_scales, int32_t M, int32_t V, int32_t D, void *d_logits, int dtype,
                      int64_t stride, const uint32_t *d_mask, int32_t mask_rows, const int32_t *d_states,
                      void *d_workspace, cudaStream_t stream);
+
+/* The norm in front of the head: with h = x + residual, rounded to the
+ * residual's type and written back to it (h = x without a residual),
+ *   r = 1 / sqrt(mean(h^2) + eps),  y = (h r) gain
+ * with r (from sums kept in more than 32 bits) and both products rounded to 32
+ * bits, and y quantized as trie_head_quantize does it.
+ *   d_x         device [M] rows of D, `stride` elements apart, F32 or BF16
+ *   d_residual  device [M] rows of D, residual_stride elements apart, or NULL;
+ *               apart from d_x
+ *   d_gain      device [D]
+ *   eps         in [1e-30, 1e30]
+ *   d_q, d_scales, pitch  as trie_head_quantize
+ * D <= 2^24. */
+int trie_head_norm_quantize(const void *d_x, int dtype, int64_t stride, void *d_residual, int residual_dtype,
+                            int64_t residual_stride, const void *d_gain, int gain_dtype, double eps, int32_t M,
+                            int32_t D, uint8_t *d_q, float *d_scales, int64_t pitch, cudaStream_t stream);
+
+/* Microscaled 4-bit floating point: rows of hidden states or of weights as e2m1
+ * values with an e4m3 scale for each 16 columns and a 32-bit scale for the row.
+ * In 32 bits, each operation rounded to nearest even:
+ *   S = max(the row's largest magnitude times 1/2688, 2^-100)   (2688 = 6 x 448)
+ *   s = e4m3((the block's largest magnitude / S) times 1/6)
+ *   q = e2m1(x times (1 / (s S))), 0 where s is 0
+ * so that x ~ q s S. The row scale of a row with a NaN or an infinity is NaN (and so are
+ * its logits); its other values mean nothing.
+ *   d_q           device uint8[rows][trie_head4_row_bytes(D)], 16-byte aligned:
+ *                 two codes a byte, the even column's in the low half, 0 behind D
+ *   d_scales      device uint8[trie_head4_scale_bytes(rows, D)], 16-byte aligned:
+ *                 [ceil(rows/128)][ceil(D/64)][32][4][4], the scale of row r and
+ *                 column k at [r/128][k/64][r%32][r%128/32][k%64/16]; 0 behind D,
+ *                 rows behind the last are not written
+ *   d_row_scales  device float[rows]
+ * D <= 2^24. */
+int64_t trie_head4_row_bytes(int32_t D);                   /* -1 for sizes out of range */
+int64_t trie_head4_scale_bytes(int32_t rows, int32_t D);   /* -1 for sizes out of range */
+int trie_head4_quantize(const void *d_x, int dtype, int64_t stride, int32_t rows, int32_t D, uint8_t *d_q,
+                        uint8_t *d_scales, float *d_row_scales, cudaStream_t stream);
+
+/* trie_head_norm_quantize with y quantized as trie_head4_quantize does it. */
+int trie_head4_norm_quantize(const void *d_x, int dtype, int64_t stride, void *d_residual, int residual_dtype,
+                             int64_t residual_stride, const void *d_gain, int gain_dtype, double eps, int32_t M,
+                             int32_t D, uint8_t *d_q, uint8_t *d_scales, float *d_row_scales, cudaStream_t stream);
+
+/* trie_head_logits for hidden states and weights in 4 bits:
+ *   logits[m][v] = S[m] S[v] sum over blocks of 16 columns of s[m] s[v] times
+ *                  the sum of q[m][k] w[v][k]
+ * and -inf where row m's state does not allow v; sums in 32 bits, rounded once to
+ * the logits' type. Any D in [1, 2^24]; M <= 65535.
+ *   d_workspace  device, trie_head_workspace(M, V) bytes, 16-byte aligned; may
+ *                be NULL without a mask */
+int trie_head4_logits(const uint8_t *d_q, const uint8_t *d_scales, const float *d_row_scales, const uint8_t *d_w,
+                      const uint8_t *d_w_scales, const float *d_w_row_scales, int32_t M, int32_t V, int32_t D,
+                      void *d_logits, int dtype, int64_t stride, const uint32_t *d_mask, int32_t mask_rows,
+                      const int32_t *d_states, void *d_workspace, cudaStream_t stream);
 
 /* Penalties, biases and the grammar on a batch of logits, in place. For token t
  * of a row, with c(t) its occurrences after the prompt:
@@ -597,6 +652,36 @@ int trie_sample(const void *d_logits, int dtype, int64_t stride, int32_t B, int3
                 const float *d_temperature, const int32_t *d_top_k, const float *d_top_p, const float *d_min_p,
                 const uint32_t *d_mask, int32_t mask_rows, const int32_t *d_states, void *d_workspace,
                 int32_t *d_tokens, float *d_logprobs, cudaStream_t stream);
+
+/* The clipped policy loss with a KL term of sampled tokens, from the logits that
+ * they are (or would now be) sampled from, and its gradient by these. Of the allowed
+ * tokens of a row, with its token t, log-probabilities at the temperature as
+ * trie_sample gives them:
+ *   lp = log-probability of t,  rho = exp(lp - old),  d = ref - lp
+ *   loss  = weight (kl (exp(d) - d - 1) - min(rho A, clip(rho) A))
+ *   slope = weight (kl (1 - exp(d)) - (rho A <= clip(rho) A ? rho A : 0))
+ *   dloss / dlogit[v] = slope ((v = t) - p[v]) / temperature, 0 where v is not allowed
+ * with A the advantage and clip(rho) in [1 - clip_low, 1 + clip_high]. A row
+ * whose token is outside [0, V), not allowed or of logit -inf has the
+ * log-probability -inf, and like a row of weight 0 the loss 0 and a gradient of
+ * zeros. A row with a NaN or +inf among its allowed logits has NaN; what other tokens'
+ * logits hold does not matter. All in 32 bits; the gradient is rounded once to the logits' type.
+ *   d_tokens        device int32[B]
+ *   d_old_logprobs, d_advantages  device float[B]
+ *   d_ref_logprobs  device float[B] or NULL (no KL term, as for kl = 0)
+ *   d_weights       device float[B] or NULL (1): of the rows' losses in whatever
+ *                   sum the gradient is of
+ *   d_temperature   device float[B] or NULL (1); as in trie_sample, not above 0 is 1
+ *   clip_low        in [0, 1];  clip_high, kl >= 0
+ *   d_losses, d_logprobs  device float[B]
+ *   d_grad          device [B] rows of V, grad_stride elements apart, of the
+ *                   logits' type, or NULL (no gradient); may be d_logits itself
+ *                   (with the same stride), else apart from it */
+int trie_policy_loss(const void *d_logits, int dtype, int64_t stride, int32_t B, int32_t V, const int32_t *d_tokens,
+                     const float *d_old_logprobs, const float *d_advantages, const float *d_ref_logprobs,
+                     const float *d_weights, const float *d_temperature, float clip_low, float clip_high, float kl,
+                     const uint32_t *d_mask, int32_t mask_rows, const int32_t *d_states, float *d_losses,
+                     float *d_logprobs, void *d_grad, int64_t grad_stride, cudaStream_t stream);
 
 /* Release the handle, its host arrays and its device copy of the trie.
  * Synchronises the device first if device memory is held. NULL is a no-op. */

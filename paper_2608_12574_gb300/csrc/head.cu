@@ -31,31 +31,16 @@
 
 #include <algorithm>
 
-#include <cuda_fp8.h>
 #include <cuda_runtime.h>
 
 #include "blackwell.cuh"
-#include "logits.cuh"
+#include "quantize.cuh"
 
 namespace tmk {
 
 namespace {
 
-constexpr int kBlock = 128;  // columns (and weight rows) that share a scale
-constexpr float kPerMax = 1.0f / 448.0f;  // 448: the largest e4m3 number
 constexpr int kQuantThreads = 256;
-
-__device__ __forceinline__ uint8_t to_e4m3(float x) {
-    return uint8_t(__nv_cvt_float_to_fp8(x, __NV_SATFINITE, __NV_E4M3));
-}
-
-// NaN does not show in the maximum, but a NaN element becomes a NaN in e4m3 and
-// an infinite one makes the scale infinite and itself NaN: either way the row's
-// logits are NaN.
-__device__ __forceinline__ float scale_of(float amax) {
-    const float s = __fmul_rn(amax, kPerMax);
-    return s > 0.0f ? s : 1.0f;
-}
 
 template <typename T>
 __global__ void __launch_bounds__(kQuantThreads) k_head_quantize(const T *x, int64_t stride, int32_t M, int32_t D,

@@ -23,7 +23,7 @@ _lock = threading.Lock()
 _lib = None
 
 # every symbol include/triemask.h declares: (restype, argtypes)
-_P, _I32, _I64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+_P, _I32, _I64, _F32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
 SIGNATURES = {
     "trie_build": (ctypes.c_int, [_P, _P, _I32, _P]),
     "trie_build_many": (ctypes.c_int, [_P, _P, _P, _I32, _P]),
@@ -67,11 +67,22 @@ SIGNATURES = {
     "trie_head_logits": (ctypes.c_int, [_P, _P, _I64, _P, _P, _I32, _I32, _I32, _P, ctypes.c_int, _I64, _P, _I32, _P,
                                         _P, _P]),
     "trie_head_workspace": (_I64, [_I32, _I32]),
+    "trie_head_norm_quantize": (ctypes.c_int, [_P, ctypes.c_int, _I64, _P, ctypes.c_int, _I64, _P, ctypes.c_int,
+                                               ctypes.c_double, _I32, _I32, _P, _P, _I64, _P]),
+    "trie_head4_row_bytes": (_I64, [_I32]),
+    "trie_head4_scale_bytes": (_I64, [_I32, _I32]),
+    "trie_head4_quantize": (ctypes.c_int, [_P, ctypes.c_int, _I64, _I32, _I32, _P, _P, _P, _P]),
+    "trie_head4_norm_quantize": (ctypes.c_int, [_P, ctypes.c_int, _I64, _P, ctypes.c_int, _I64, _P, ctypes.c_int,
+                                                ctypes.c_double, _I32, _I32, _P, _P, _P, _P]),
+    "trie_head4_logits": (ctypes.c_int, [_P, _P, _P, _P, _P, _P, _I32, _I32, _I32, _P, ctypes.c_int, _I64, _P, _I32, _P,
+                                         _P, _P]),
     "trie_penalize": (ctypes.c_int, [_P, ctypes.c_int, _I64, _I32, _I32, _P, _I64, _I32, _P, _P, _P, _P, _P, _P, _P, _P,
                                      _P, _I32, _P, _P]),
     "trie_sample_workspace": (_I64, [_I32, _I32]),
     "trie_sample": (ctypes.c_int, [_P, ctypes.c_int, _I64, _I32, _I32, _P, _P, _P, _P, _P, _P, _I32, _P, _P, _P, _P,
                                    _P]),
+    "trie_policy_loss": (ctypes.c_int, [_P, ctypes.c_int, _I64, _I32, _I32, _P, _P, _P, _P, _P, _P, _F32, _F32, _F32, _P,
+                                        _I32, _P, _P, _P, _P, _I64, _P]),
     "trie_destroy": (ctypes.c_int, [_P]),
     "trie_destroy_async": (ctypes.c_int, [_P, _P]),
     "trie_last_error": (ctypes.c_char_p, []),
@@ -681,6 +692,97 @@ def trie_head_logits(q, scales, w, w_scales, d_logits, mask=None, states=None, w
         *_grammar(mask, states, M, V, dev), space, _stream_of(stream, d_logits)))
 
 
+def _normed(x, gain, residual):
+    """The arguments that the norm's calls begin with, up to the gain's type."""
+    import torch
+    p, stride, dtype = _hidden(x, "x")
+    D, f32 = x.shape[1], torch.float32
+    pr, r_dtype, r_stride = None, 0, 0
+    if residual is not None:
+        if residual.shape != x.shape:
+            raise ValueError("residual must be [M, D]")
+        pr, r_stride, r_dtype = _hidden(residual, "residual")
+    if gain.dim() != 1 or gain.shape[0] != D:
+        raise ValueError("gain must have D entries")
+    g_dtype = TRIE_DTYPE_F32 if gain.dtype is f32 else TRIE_DTYPE_BF16
+    pg = _vec(gain, f32 if gain.dtype is f32 else torch.bfloat16, D, "gain", x.get_device())
+    return p, dtype, stride, pr, r_dtype, r_stride, pg, g_dtype
+
+
+def trie_head_norm_quantize(x, gain, residual=None, eps: float = 1e-6, stream=None):
+    """x ([M, D] fp32 or bf16) is added to the residual ([M, D] fp32 or bf16, in place) where there is one, the sum
+    normed by its root mean square and multiplied by gain ([D]), and that quantized as trie_head_quantize does it:
+    (e4m3 [M, D], scales [ceil(D/128), M rounded up to 4])."""
+    import torch
+    normed = _normed(x, gain, residual)
+    M, D = x.shape
+    q = _empty((M, D), torch.float8_e4m3fn, x.device, stream)
+    scales = _empty(((D + 127) // 128, (M + 3) // 4 * 4), torch.float32, x.device, stream)
+    _check(load_library().trie_head_norm_quantize(*normed, eps, M, D, q.data_ptr(), scales.data_ptr(), scales.shape[1],
+                                                  _stream_of(stream, x)))
+    return q, scales
+
+
+def _empty4(x, stream):
+    """(codes, scales, row scales) for rows x in 4 bits."""
+    import torch
+    M, D = x.shape
+    return (_empty((M, (D + 31) // 32 * 16), torch.uint8, x.device, stream),
+            _empty(((M + 127) // 128, (D + 63) // 64, 32, 4, 4), torch.float8_e4m3fn, x.device, stream),
+            _empty((M,), torch.float32, x.device, stream))
+
+
+def trie_head4_quantize(x, stream=None):
+    """Rows of hidden states or weights x ([M, D] fp32 or bf16) in microscaled 4-bit floating point: (codes uint8
+    [M, 16 ceil(D/32)], two e2m1 values a byte; e4m3 scales of 16 columns [ceil(M/128), ceil(D/64), 32, 4, 4], that of
+    row r and column k at [r//128, k//64, r%32, r%128//32, k%64//16]; scales of the rows [M])."""
+    p, stride, dtype = _hidden(x, "x")
+    q, scales, row_scales = _empty4(x, stream)
+    _check(load_library().trie_head4_quantize(p, dtype, stride, *x.shape, q.data_ptr(), scales.data_ptr(),
+                                              row_scales.data_ptr(), _stream_of(stream, x)))
+    return q, scales, row_scales
+
+
+def trie_head4_norm_quantize(x, gain, residual=None, eps: float = 1e-6, stream=None):
+    """trie_head_norm_quantize into 4 bits: (codes, scales, row scales) as trie_head4_quantize gives them."""
+    normed = _normed(x, gain, residual)
+    q, scales, row_scales = _empty4(x, stream)
+    _check(load_library().trie_head4_norm_quantize(*normed, eps, *x.shape, q.data_ptr(), scales.data_ptr(),
+                                                   row_scales.data_ptr(), _stream_of(stream, x)))
+    return q, scales, row_scales
+
+
+def _packed4(q, scales, row_scales, rows: int, bytes_: int, tiles: int, name: str, dev: int):
+    """Addresses of rows in 4 bits."""
+    import torch
+    if q.shape != (rows, bytes_) or scales.shape != ((rows + 127) // 128, tiles, 32, 4, 4) or row_scales.shape != (rows,):
+        raise ValueError(f"{name} must be codes, scales and row scales as trie_head4_quantize gives them for its rows")
+    return (_vec(q, torch.uint8, q.numel(), name, dev),
+            _vec(scales, torch.float8_e4m3fn, scales.numel(), f"{name}'s scales", dev),
+            _vec(row_scales, torch.float32, rows, f"{name}'s row scales", dev))
+
+
+def trie_head4_logits(q, scales, row_scales, w, w_scales, w_row_scales, d_logits, mask=None, states=None, workspace=None,
+                      stream=None) -> None:
+    """trie_head_logits for hidden states and weights in 4 bits (both as trie_head4_quantize gives them). D is known
+    to a multiple of 32 by the codes: what lies behind it is 0."""
+    dtype = _logits_dtype(d_logits)
+    M, V = d_logits.shape
+    bytes_ = w.shape[1] if w.dim() == 2 else -1
+    tiles = w_scales.shape[1] if w_scales.dim() == 5 else -1
+    if bytes_ < 16 or bytes_ % 16 or tiles != (bytes_ + 31) // 32:
+        raise ValueError("w must be codes [V, 16 ceil(D/32)] with scales [ceil(V/128), ceil(D/64), 32, 4, 4]")
+    p, stride = _rows(d_logits, "d_logits")
+    dev = d_logits.get_device()
+    lib, space, owner = load_library(), None, None
+    hidden = _packed4(q, scales, row_scales, M, bytes_, tiles, "q", dev)
+    weight = _packed4(w, w_scales, w_row_scales, V, bytes_, tiles, "w", dev)
+    if mask is not None:
+        space, owner = _workspace(workspace, lib.trie_head_workspace(M, V), d_logits, stream)
+    _check(lib.trie_head4_logits(*hidden, *weight, M, V, bytes_ * 2, p, dtype, stride, *_grammar(mask, states, M, V, dev),
+                                 space, _stream_of(stream, d_logits)))
+
+
 def trie_penalize(d_logits, history=None, length=None, prompt=None, repetition=None, presence=None, frequency=None,
                   bias=None, mask=None, states=None, stream=None) -> None:
     """Penalties for the tokens of the history ([B, H] int32, the first length[b] of row b, of them prompt[b]
@@ -749,6 +851,37 @@ def trie_sample_workspace(B: int, V: int) -> int:
     if n < 0:
         raise ValueError("B or V out of range")
     return n
+
+
+def trie_policy_loss(d_logits, tokens, old_logprobs, advantages, ref_logprobs=None, weights=None, temperature=None,
+                     clip=(0.2, 0.2), kl: float = 0.0, mask=None, states=None, grad=None, losses=None, logprobs=None,
+                     stream=None):
+    """(losses fp32[B], logprobs fp32[B]) of tokens int32[B] sampled from d_logits ([B, V] fp32 or bf16) at the
+    temperature and under the grammar: weight (kl (exp(d) - d - 1) - min(rho A, clip(rho) A)) with rho = exp(logprob -
+    old_logprob) clipped to [1 - clip[0], 1 + clip[1]], A the advantage and d = ref_logprob - logprob. grad ([B, V], of
+    the logits' type, which may be d_logits itself) receives the gradient of the losses' sum by the logits."""
+    import torch
+    dtype = _logits_dtype(d_logits)
+    B, V = d_logits.shape
+    p, stride = _rows(d_logits, "d_logits")
+    if tokens is None or old_logprobs is None or advantages is None:
+        raise ValueError("tokens, old_logprobs and advantages must be given")
+    dev, f32 = d_logits.get_device(), torch.float32
+    pg, g_stride = None, 0
+    if grad is not None:
+        if grad.shape != d_logits.shape or grad.dtype is not d_logits.dtype:
+            raise ValueError("grad must be [B, V] and of the logits' type")
+        pg, g_stride = _rows(grad, "grad")
+    losses = _empty((B,), f32, d_logits.device, stream) if losses is None else losses
+    logprobs = _empty((B,), f32, d_logits.device, stream) if logprobs is None else logprobs
+    _check(load_library().trie_policy_loss(
+        p, dtype, stride, B, V, _vec(tokens, torch.int32, B, "tokens", dev),
+        _vec(old_logprobs, f32, B, "old_logprobs", dev), _vec(advantages, f32, B, "advantages", dev),
+        _vec(ref_logprobs, f32, B, "ref_logprobs", dev), _vec(weights, f32, B, "weights", dev),
+        _vec(temperature, f32, B, "temperature", dev), clip[0], clip[1], kl, *_grammar(mask, states, B, V, dev),
+        _vec(losses, f32, B, "losses", dev), _vec(logprobs, f32, B, "logprobs", dev), pg, g_stride,
+        _stream_of(stream, d_logits)))
+    return losses, logprobs
 
 
 # ------------------------------------------------------------ fixed formats
