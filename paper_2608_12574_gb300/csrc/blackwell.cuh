@@ -121,6 +121,12 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map
         "l"(map), "r"(x), "r"(y), "r"(bar)
         : "memory");
 }
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, int32_t z, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
+}
 // `bytes` and both addresses: multiples of 16.
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
@@ -132,6 +138,14 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap
     asm volatile(
         "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
         "l"(map), "r"(x), "r"(y), "r"(bar)
+        : "memory");
+}
+
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, int32_t z, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+            dst),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
         : "memory");
 }
 
@@ -195,7 +209,39 @@ __device__ __forceinline__ void mma_e4m3(uint32_t d, uint64_t a, uint64_t b, uin
             "l"(a), "l"(b), "r"(idesc), "r"(uint32_t(accumulate))
             : "memory");
 }
-// Arrives on the barrier (of both CTAs of a pair) once all MMAs that this thread
+// e2m1 x e2m1 into fp32 with an e4m3 scale for each row and 16 columns, both
+// operands K-major, an m x n tile.
+__host__ __device__ constexpr uint32_t mma_idesc_e2m1(uint32_t m, uint32_t n) {
+    return (1u << 7) | (1u << 10) | ((n >> 3) << 17) | ((m >> 7) << 27);
+}
+// The scales of 128 rows x 64 columns as they lie in shared memory (512 bytes: lane
+// r % 32's 16 bytes hold rows r % 32 + 0, 32, 64 and 96), into four columns of
+// tensor memory, the same 32 lanes for each of the four quarters; of a pair, in both CTAs.
+template <bool kPair>
+__device__ __forceinline__ void tmem_copy_scales(uint32_t dst, uint32_t src) {
+    const uint64_t desc = uint64_t((src & 0x3FFFFu) >> 4) | (uint64_t(1) << 16) | (uint64_t(128 >> 4) << 32) | (uint64_t(1) << 46);
+    if (kPair) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(dst), "l"(desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(dst), "l"(desc) : "memory");
+}
+// mma_e4m3 for e2m1 operands, over 64 columns of K, with the scales of A's rows
+// and B's rows in tensor memory (of a pair: of its own 128 rows of A and of all of B in each CTA).
+template <bool kPair>
+__device__ __forceinline__ void mma_e2m1(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t a_scales, uint32_t b_scales,
+                                         bool accumulate) {
+    if (kPair)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(a_scales), "r"(b_scales), "r"(uint32_t(accumulate))
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(a_scales), "r"(b_scales), "r"(uint32_t(accumulate))
+            : "memory");
+}
+// Arrives on the barrier (of both CTAs of a pair) once all MMAs (and copies of scales) that this thread
 // has issued are done.
 template <bool kPair>
 __device__ __forceinline__ void mma_commit(uint32_t bar) {

@@ -33,8 +33,7 @@
 
 #include <cuda_runtime.h>
 
-#include "blackwell.cuh"
-#include "quantize.cuh"
+#include "head_tile.cuh"
 
 namespace tmk {
 
@@ -149,51 +148,20 @@ __global__ void __launch_bounds__(kQuantThreads) k_head_quantize_weight(const T 
 // so that the next tile's weights arrive while this one's logits are written.
 // Rows that a batch does not have are not loaded (the MMA multiplies what lies
 // there into rows nobody reads).
-constexpr int kRows = 128;         // of a CTA's tile
-constexpr int kMaxStages = 8;
-constexpr int kColumns = 64;       // tokens of an epilogue warp
-constexpr int kHeadSmem = 226 * 1024;
-constexpr int kFewMaxD = 32768;    // longest hidden state whose row fits k_head_rows' shared memory
-constexpr int kNeedTiles = 2048;   // tiles of a CTA whose need is looked up ahead
-constexpr int kLookRows = 16384;   // largest batch of which every CTA looks whether a row is left to it (64 KB)
 constexpr int kScaleSlots = 8;     // of two blocks' scales: more blocks than can be between the copies and the epilogue
-constexpr int kTurn = 32 * 17;     // words of a warp's block of 16 tokens, turned
 
-struct HeadArgs {
+struct HeadArgs : HeadOut {
     CUtensorMap map_w, map_q;
     const uint8_t *q, *w;  // [M][D], [V][D]
     const float *s;        // [blocks][pitch]
     int64_t pitch;
     const float *ws;       // [ceil(V / 128)][blocks]
-    int32_t M, V, D, blocks;
+    int32_t blocks;
     int32_t m_tiles;       // of 128 rows (a pair: 256)
     int32_t tiles;
     int32_t box_rows;      // rows of a CTA's tile that are loaded
     int32_t stages;        // of the ring
-    void *logits;
-    int64_t stride;
-    Grammar g;
-    // with a grammar, of each row (k_head_rows):
-    int32_t *dense;        // [M] 0: k_head_rows wrote its logits, 1: k_head_logits does
-    uint32_t *used;        // [M][used_words] bit i: it allows one of tokens 128 i .. 128 i + 127
-    int32_t used_words;
 };
-
-// ---- rows that allow few tokens
-//
-// A trie's nodes allow a handful of tokens, so a constrained row's logits are a
-// few dot products of its hidden state with rows of the weights that are
-// scattered over the vocabulary: reading whole tiles of weights for them would
-// cost hundreds of times more. A CTA per row counts the row's allowed tokens;
-// where they are at most kFew (and the batch has no free row nearby, whose
-// tiles are multiplied anyway) it computes their logits, a warp a token, while
-// other warps write -inf over the row, and writes them last: the tiles' kernel
-// leaves such a row out. 256 constrained rows, V 152,064, D 4,096: 35 us, and 173
-// by tiles. A longer list than kFew would be as much to read, scattered, as tiles are.
-constexpr int kFew = 256;
-constexpr int kNear = 256;         // rows among which one free row makes all dense
-constexpr int kRowThreads = 512;
-static_assert(kFew <= kRowThreads, "a thread writes a logit");
 
 // Sum of 16 products of e4m3 numbers (exact in 32 bits but for the additions).
 __device__ __forceinline__ float dot16(const uint4 &x, const uint4 &w) {
@@ -213,177 +181,39 @@ __device__ __forceinline__ float dot16(const uint4 &x, const uint4 &w) {
     return sum;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kRowThreads, 2) k_head_rows(HeadArgs a) {
-    extern __shared__ __align__(16) unsigned char dynamic_smem[];  // the row's values, then its scales
-    __shared__ int32_t few[kFew];
-    __shared__ float value[kFew];
-    __shared__ int32_t n_few, pieces;
-    pdl_launch_dependents();
-    if (threadIdx.x == 0) n_few = pieces = 0;
-    __syncthreads();
-    pdl_wait();
-    const int32_t m = blockIdx.x;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const GrammarRow row = grammar_row(a.g, m);
-    const int32_t first = m / kNear * kNear, near = first + int32_t(threadIdx.x);
-    const bool free_near = threadIdx.x < kNear && near < a.M && grammar_row(a.g, near).kind == kAllowAll;
-    uint8_t *used = reinterpret_cast<uint8_t *>(a.used + int64_t(m) * a.used_words);
-    const int32_t W = int32_t(a.g.W), all = a.used_words * 128;  // words of the mask, of which four make a bit of `used`
-    constexpr int kBatch = 8;  // reads in flight a thread
-    for (int32_t w0 = int32_t(threadIdx.x); w0 - lane < all; w0 += kBatch * kRowThreads) {
-        uint32_t word[kBatch];
-#pragma unroll
-        for (int i = 0; i < kBatch; i++) {
-            const int32_t w = w0 + i * kRowThreads;
-            word[i] = w < W ? row.word(w) : 0u;
-            if (w == W - 1 && a.V & 31) word[i] &= (1u << (a.V & 31)) - 1u;  // bits past V are nobody's
-        }
-#pragma unroll
-        for (int i = 0; i < kBatch; i++) {
-            const int32_t w = w0 + i * kRowThreads;
-            const uint32_t any = __ballot_sync(~0u, word[i] != 0u);
-            uint32_t bits = 0;
-#pragma unroll
-            for (int b = 0; b < 8; b++) bits |= uint32_t(((any >> (4 * b)) & 15u) != 0u) << b;
-            if (lane == 0 && w < all) used[w / 32] = uint8_t(bits);
-            if (word[i]) {
-                int32_t at = atomicAdd(&n_few, __popc(word[i]));
-                for (uint32_t x = word[i]; x && at < kFew; x &= x - 1) few[at++] = w * 32 + __ffs(x) - 1;
-            }
-        }
-    }
-    const bool dense = __syncthreads_or(free_near);
-    const int32_t n = n_few;
-    if (row.kind == kAllowAll || dense || n > kFew || a.D > kFewMaxD) {
-        if (threadIdx.x == 0) a.dense[m] = 1;
-        return;
-    }
-    if (threadIdx.x == 0) a.dense[m] = 0;
-    for (int32_t i = warp; i < n; i += kRowThreads / 32)
-        for (int32_t c = lane * 128; c < a.D; c += 32 * 128) prefetch_l2(a.w + int64_t(few[i]) * a.D + c);
-    float *scales = reinterpret_cast<float *>(dynamic_smem + a.D);
+__device__ __forceinline__ void few_load(const HeadArgs &a, int32_t m, unsigned char *smem) {
+    float *scales = reinterpret_cast<float *>(smem + a.D);
     for (int32_t i = threadIdx.x; i < a.D / 16; i += kRowThreads)
-        reinterpret_cast<uint4 *>(dynamic_smem)[i] = __ldg(reinterpret_cast<const uint4 *>(a.q + int64_t(m) * a.D) + i);
+        reinterpret_cast<uint4 *>(smem)[i] = __ldg(reinterpret_cast<const uint4 *>(a.q + int64_t(m) * a.D) + i);
     for (int32_t i = threadIdx.x; i < a.blocks; i += kRowThreads) scales[i] = __ldg(a.s + i * a.pitch + m);
-    __syncthreads();
-    for (int32_t i = warp; i < n; i += kRowThreads / 32) {
-        const int32_t v = few[i];
-        const uint4 *w = reinterpret_cast<const uint4 *>(a.w + int64_t(v) * a.D);
-        const float *ws = a.ws + int64_t(v / kBlock) * a.blocks;
-        float sum = 0.0f;
-        for (int32_t c0 = lane; c0 < a.D / 16; c0 += 32 * kBatch) {
-            uint4 x[kBatch];
-            float f[kBatch];
+}
+__device__ __forceinline__ void few_ask(const HeadArgs &a, int32_t v, int lane) {
+    for (int32_t c = lane * 128; c < a.D; c += 32 * 128) prefetch_l2(a.w + int64_t(v) * a.D + c);
+}
+__device__ __forceinline__ float few_part(const HeadArgs &a, int32_t v, const unsigned char *smem, int lane) {
+    const float *scales = reinterpret_cast<const float *>(smem + a.D);
+    const uint4 *w = reinterpret_cast<const uint4 *>(a.w + int64_t(v) * a.D);
+    const float *ws = a.ws + int64_t(v / kBlock) * a.blocks;
+    float sum = 0.0f;
+    for (int32_t c0 = lane; c0 < a.D / 16; c0 += 32 * kBatch) {
+        uint4 x[kBatch];
+        float f[kBatch];
 #pragma unroll
-            for (int j = 0; j < kBatch; j++) {
-                const int32_t c = c0 + 32 * j;
-                x[j] = c < a.D / 16 ? __ldg(w + c) : make_uint4(0u, 0u, 0u, 0u);
-                f[j] = c < a.D / 16 ? __ldg(ws + c / (kBlock / 16)) : 0.0f;
-            }
-#pragma unroll
-            for (int j = 0; j < kBatch; j++) {
-                const int32_t c = c0 + 32 * j;
-                if (c < a.D / 16)
-                    sum = fmaf(dot16(reinterpret_cast<const uint4 *>(dynamic_smem)[c], x[j]), f[j] * scales[c / (kBlock / 16)], sum);
-            }
+        for (int j = 0; j < kBatch; j++) {
+            const int32_t c = c0 + 32 * j;
+            x[j] = c < a.D / 16 ? __ldg(w + c) : make_uint4(0u, 0u, 0u, 0u);
+            f[j] = c < a.D / 16 ? __ldg(ws + c / (kBlock / 16)) : 0.0f;
         }
 #pragma unroll
-        for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
-        if (lane == 0) value[i] = sum;
-    }
-    // -inf: to a 16-byte boundary, 16 bytes at a time, and the rest; warps without
-    // a token (most of them) come first and take most pieces
-    T *out = static_cast<T *>(a.logits) + m * a.stride;
-    constexpr int kVec = 16 / int(sizeof(T)), kPiece = 8 * 32;
-    const int32_t ahead = int32_t((16 - (reinterpret_cast<uintptr_t>(out) & 15)) & 15) / int32_t(sizeof(T)), head = min(ahead, a.V);
-    const int32_t body = (a.V - head) / kVec, tail = head + body * kVec;
-    const uint32_t pair = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
-    if (int32_t(threadIdx.x) < head) out[threadIdx.x] = from_f32<T>(-INFINITY);
-    if (tail + int32_t(threadIdx.x) < a.V) out[tail + threadIdx.x] = from_f32<T>(-INFINITY);
-    for (;;) {
-        int32_t piece = lane == 0 ? atomicAdd(&pieces, 1) : 0;
-        piece = __shfl_sync(~0u, piece, 0);
-        if (piece > body / kPiece) break;
-#pragma unroll
-        for (int i = 0; i < kPiece / 32; i++) {
-            const int32_t at = piece * kPiece + i * 32 + lane;
-            if (at < body) reinterpret_cast<uint4 *>(out + head)[at] = make_uint4(pair, pair, pair, pair);
+        for (int j = 0; j < kBatch; j++) {
+            const int32_t c = c0 + 32 * j;
+            if (c < a.D / 16)
+                sum = fmaf(dot16(reinterpret_cast<const uint4 *>(smem)[c], x[j]), f[j] * scales[c / (kBlock / 16)], sum);
         }
     }
-    __syncthreads();
-    if (int32_t(threadIdx.x) < n) out[few[threadIdx.x]] = from_f32<T>(value[threadIdx.x]);
+    return sum;
 }
-
-// Whether row m allows a token of tokens v0 .. v0 + 127 (v0 a multiple of 128).
-__device__ __forceinline__ bool row_uses(const HeadArgs &a, int32_t m, int32_t v0) {
-    return (__ldg(a.used + int64_t(m) * a.used_words + (v0 >> 12)) >> ((v0 >> 7) & 31)) & 1u;
-}
-
-// The dense rows of [m0, m1) in a tile that none of them allows a token of: -inf.
-// By the epilogue warps; NT tokens, fewer at the end.
-// (A call, so that its unrolled stores take no registers from the sums of the other tiles.)
-template <typename T, int NT, int kWarps>
-__device__ __noinline__ void fill_tile(const HeadArgs &a, int32_t m0, int32_t m1, int32_t v0, int warp, int lane) {
-    constexpr int kVec = 16 / int(sizeof(T)), kEach = kRows / kWarps;
-    const int32_t v1 = min(a.V, v0 + NT);
-    const uint32_t pair = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
-    const int32_t mine = m0 + warp + lane * kWarps;  // a lane a row
-    const uint32_t dense = __ballot_sync(~0u, lane < kEach && mine < m1 && __ldg(a.dense + mine));
-#pragma unroll 4
-    for (int j = 0; j < kEach; j++) {
-        if (!((dense >> j) & 1u)) continue;
-        T *out = static_cast<T *>(a.logits) + (m0 + warp + j * kWarps) * a.stride + v0;
-        if (v1 - v0 == NT && (reinterpret_cast<uintptr_t>(out) & 15) == 0) {
-#pragma unroll
-            for (int i = 0; i < NT / kVec; i += 32)
-                if (i + lane < NT / kVec) reinterpret_cast<uint4 *>(out)[i + lane] = make_uint4(pair, pair, pair, pair);
-        } else {
-            for (int32_t i = lane; i < v1 - v0; i += 32) out[i] = from_f32<T>(-INFINITY);
-        }
-    }
-}
-
-// 16 tokens from v on of a warp's 32 rows from m on (of which `rows` are there, and
-// with kSome those whose bit of `some` is set), a row a thread. Where every row is
-// on a 32-byte boundary a thread writes its own 32 bytes at a time; else the block
-// is turned in shared memory, so that lanes write consecutive tokens (256 aligned
-// rows: 148 and 159 us, 64: 93 and 101). One test more for each store, in kSome
-// only, costs 64 unaligned rows 6 us of 101.
-template <typename T, bool kSome>
-__device__ __forceinline__ void store16(const HeadArgs &a, float *turn, const float *x, int32_t m, int32_t rows, uint32_t some,
-                                        int32_t v, int lane, bool wide) {
-    T *out = static_cast<T *>(a.logits) + m * a.stride + v;
-    if (wide && v + 16 <= a.V) {
-        if (lane >= rows || (kSome && !((some >> lane) & 1u))) return;
-        T *mine = out + lane * a.stride;
-        uint32_t r[8];
-        if (sizeof(T) == 2) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const __nv_bfloat162 both = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-                r[i] = *reinterpret_cast<const uint32_t *>(&both);
-            }
-            store32(mine, r);
-        } else {
-#pragma unroll
-            for (int h = 0; h < 2; h++) {
-#pragma unroll
-                for (int i = 0; i < 8; i++) r[i] = __float_as_uint(x[8 * h + i]);
-                store32(mine + 8 * h, r);
-            }
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 16; i++) turn[lane * 17 + i] = x[i];
-    __syncwarp();
-    const int c = lane & 15;
-    if (v + c < a.V)
-        for (int r = lane >> 4; r < rows; r += 2)
-            if (!kSome || ((some >> r) & 1u)) out[r * a.stride + c] = from_f32<T>(turn[r * 17 + c]);
-    __syncwarp();
-}
+__device__ __forceinline__ float few_logit(const HeadArgs &, int32_t, int32_t, float sum) { return sum; }
 
 // Epilogue warps: four quarters of the rows, two or four columns of tokens.
 template <bool kPair>
@@ -406,7 +236,7 @@ __global__ void __launch_bounds__(kHeadThreads<kPair>, 1) k_head_logits(const __
     extern __shared__ unsigned char dynamic_smem[];
     __shared__ uint64_t bars[2 * kMaxStages + 2 * kAccumulators + 2 * kScaleSlots];
     __shared__ __align__(16) float scales[kScaleSlots][2][kRows];
-    __shared__ float turn[kEpilogue][kTurn];
+    __shared__ float turn[kEpilogue][kTurn<float, 16>];
     __shared__ uint32_t need[kNeedTiles / 32];
     __shared__ uint32_t tmem_base;
     __shared__ int gave_up;
@@ -536,8 +366,8 @@ __global__ void __launch_bounds__(kHeadThreads<kPair>, 1) k_head_logits(const __
                     }
                 }
                 if (v + c >= a.V) continue;
-                if (some == ~0u) store16<T, false>(a, turn[warp - kFirst], sum + c, mine, rows, some, v + c, lane, wide);
-                else store16<T, true>(a, turn[warp - kFirst], sum + c, mine, rows, some, v + c, lane, wide);
+                if (some == ~0u) store16<T, false, float, 16>(a, turn[warp - kFirst], sum + c, mine, rows, some, v + c, lane, wide);
+                else store16<T, true, float, 16>(a, turn[warp - kFirst], sum + c, mine, rows, some, v + c, lane, wide);
             }
         }
     } else {
@@ -637,35 +467,12 @@ __global__ void __launch_bounds__(kHeadThreads<kPair>, 1) k_head_logits(const __
     if (warp == 1) tmem_free<kPair>(tmem, 512);
 }
 
-// [rows][D] bytes in boxes of box_rows x 128, 128-byte swizzle, zeros outside.
-bool make_map(CUtensorMap *map, const void *base, int64_t rows, int32_t D, int32_t box_rows) {
-    using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-    static const Encode encode = [] {
-        void *f = nullptr;
-        cudaDriverEntryPointQueryResult got;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &got) != cudaSuccess ||
-            got != cudaDriverEntryPointSuccess) {
-            cudaGetLastError();
-            f = nullptr;
-        }
-        return reinterpret_cast<Encode>(f);
-    }();
-    if (!encode) return false;
-    const cuuint64_t dims[2] = {cuuint64_t(D), cuuint64_t(rows)}, strides[1] = {cuuint64_t(D)};
-    const cuuint32_t box[2] = {cuuint32_t(kBlock), cuuint32_t(box_rows)}, steps[2] = {1, 1};
-    return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, steps,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <typename T, bool kPair>
 cudaError_t launch_head(HeadArgs a, cudaStream_t st) {
     const int stage = 128 * kBlock + a.box_rows * kBlock;
     // the last stage's MMA reads kRows rows, whatever was loaded; and room to align the ring
     const int beyond = (kRows - a.box_rows) * kBlock + 1024;
-    const int fixed = int(sizeof(float)) * (kEpilogueWarps<kPair> * kTurn + kScaleSlots * 2 * kRows) + 1024;  // declared in the kernel
+    const int fixed = int(sizeof(float)) * (kEpilogueWarps<kPair> * kTurn<float, 16> + kScaleSlots * 2 * kRows) + 1024;  // declared in the kernel
     a.stages = std::min(kMaxStages, (kHeadSmem - fixed - beyond) / stage);
     const int smem = a.stages * stage + beyond;
     const cudaError_t e = cudaFuncSetAttribute(k_head_logits<T, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadSmem - fixed);
@@ -737,22 +544,6 @@ extern "C" int trie_head_quantize_weight(const void *d_w, int dtype, int64_t str
     return TRIE_OK;
 }
 
-namespace tmk {
-namespace {
-// Where the parts of the workspace lie.
-struct HeadSpace {
-    int32_t used_words;
-    int64_t dense, used, bytes;
-    HeadSpace(int32_t M, int32_t V) {
-        used_words = int32_t((int64_t(V) + 4095) / 4096);
-        dense = 0;
-        used = (int64_t(M) * 4 + 15) / 16 * 16;
-        bytes = used + int64_t(M) * used_words * 4;
-    }
-};
-}  // namespace
-}  // namespace tmk
-
 extern "C" int64_t trie_head_workspace(int32_t M, int32_t V) {
     if (M < 0 || M > (1 << 20) || V < 2 || V > tmk::kMaxV) return -1;
     return tmk::HeadSpace(M, V).bytes;
@@ -808,8 +599,8 @@ extern "C" int trie_head_logits(const uint8_t *d_q, const float *d_scales, int64
         a.used = reinterpret_cast<uint32_t *>(base + at.used);
         a.used_words = at.used_words;
         const int smem = D <= kFewMaxD ? D + a.blocks * 4 : 0;
-        e = f32 ? launch_pdl_smem(k_head_rows<float>, M, kRowThreads, smem, stream, a)
-                : launch_pdl_smem(k_head_rows<__nv_bfloat16>, M, kRowThreads, smem, stream, a);
+        e = f32 ? launch_pdl_smem(k_head_rows<float, HeadArgs>, M, kRowThreads, smem, stream, a)
+                : launch_pdl_smem(k_head_rows<__nv_bfloat16, HeadArgs>, M, kRowThreads, smem, stream, a);
         if (e != cudaSuccess) return fail_launch(e, "head rows launch");
     }
     e = pair ? (f32 ? launch_head<float, true>(a, stream) : launch_head<__nv_bfloat16, true>(a, stream))

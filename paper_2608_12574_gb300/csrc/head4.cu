@@ -5,60 +5,393 @@
 // and -inf where row m's state does not allow token v: q and w in e2m1, s and t
 // in e4m3 for 16 columns of a row, S and T in 32 bits for a row (quantize.cuh).
 // Sums are kept in 32 bits and rounded once to the logits' type.
+//
+//  k_head_rows   with a grammar: the logits of rows that allow few tokens.
+//  k_head4       the product on the tensor cores.
 #include <math.h>
 #include <stdint.h>
 #include <stdio.h>
 
+#include <algorithm>
+
 #include <cuda_runtime.h>
 
-#include "blackwell.cuh"
-#include "quantize.cuh"
+#include "head_tile.cuh"
 
 namespace tmk {
 
 namespace {
 
-constexpr int kThreads4 = 256;
+// ---- the product
+//
+// Tiles, pairs of CTAs and the ring are as in head.cu: rows of the batch are the
+// MMA's rows, 128 x 128 on a CTA up to 128 rows of the batch, 256 x 256 on a pair
+// beyond. The tensor core applies the blocks' scales itself, so an
+// accumulator takes the whole of K and is read out once a tile: the epilogue
+// holds its 64 tokens a thread in registers and gives the accumulator back before it
+// scales and stores them. A stage is 256 columns, four MMAs deep: 128 bytes of
+// a row of either operand, and 512 bytes of scales for 128 rows and 64 columns,
+// which the MMAs' thread copies from shared to tensor memory in front of them
+// (copies and MMAs of a thread are carried out in order).
+constexpr int kStageColumns = 256;
+constexpr int kSteps = kStageColumns / 64;  // MMAs of a stage
+constexpr int kScaleTile = 512;             // bytes of the scales of 128 rows x 64 columns
 
-struct Head4Args {
-    const uint8_t *q, *s, *w, *ws;
+template <bool kPair>
+constexpr int kTokens = kPair ? 256 : 128;  // of a tile
+template <bool kPair>
+constexpr int kWeightBytes4 = 128 * 128 + kTokens<kPair> / 128 * kSteps * kScaleTile;  // of a stage of a CTA: its 128 rows, all scales
+constexpr int kHiddenScales = kSteps * kScaleTile;
+template <bool kPair>
+constexpr int kEpilogueWarps4 = kPair ? 16 : 8;
+// The warps before them: as in head.cu.
+template <bool kPair>
+constexpr int kFirstWarp4 = kPair ? 4 : 2;
+template <bool kPair>
+constexpr int kThreads4 = 32 * (kFirstWarp4<kPair> + kEpilogueWarps4<kPair>);
+// A warp's block of tokens, turned: 32 bytes of a row at a time.
+template <typename T>
+constexpr int kTurnTokens = 32 / int(sizeof(T));
+
+struct Head4Args : HeadOut {
+    CUtensorMap map_w, map_q, map_ws, map_s;
+    const uint8_t *q, *w, *s, *ws;
     const float *q_rows, *w_rows;
-    int32_t M, V, D;
-    void *logits;
-    int64_t stride;
-    Grammar g;
+    int64_t row_bytes, tiles_k;  // of a row's codes; 64-column tiles of its scales
+    int32_t blocks;              // stages of K
+    int32_t m_tiles, tiles, box_rows, stages;  // as in HeadArgs
 };
 
-__device__ __forceinline__ float2 from_e2m1x2(uint8_t x) {
-    return __half22float2(__half2(__nv_cvt_fp4x2_to_halfraw2(__nv_fp4x2_storage_t(x), __NV_E2M1)));
+// Sum of 32 products and their blocks' scales. e2m1 products are multiples of 1/4 up to 36,
+// so eight of them add up exactly in 16 bits.
+__device__ __forceinline__ float dot32(const uint4 &x, const uint4 &w, const float *xs, uint32_t ws) {
+    const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, ww[4] = {w.x, w.y, w.z, w.w};
+    float sum = 0.0f;
+#pragma unroll
+    for (int b = 0; b < 2; b++) {
+        __half2 part = __float2half2_rn(0.0f);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const __half2 p(__nv_cvt_fp4x2_to_halfraw2(__nv_fp4x2_storage_t(xw[2 * b + i / 4] >> (i % 4 * 8)), __NV_E2M1));
+            const __half2 r(__nv_cvt_fp4x2_to_halfraw2(__nv_fp4x2_storage_t(ww[2 * b + i / 4] >> (i % 4 * 8)), __NV_E2M1));
+            part = __hfma2(p, r, part);
+        }
+        sum = fmaf(__low2float(part) + __high2float(part), xs[b] * from_e4m3(uint8_t(ws >> (8 * b))), sum);
+    }
+    return sum;
+}
+__device__ __forceinline__ void few_load(const Head4Args &a, int32_t m, unsigned char *smem) {
+    float *scales = reinterpret_cast<float *>(smem + a.row_bytes);
+    for (int32_t i = threadIdx.x; i < a.row_bytes / 16; i += kRowThreads)
+        reinterpret_cast<uint4 *>(smem)[i] = __ldg(reinterpret_cast<const uint4 *>(a.q + m * a.row_bytes) + i);
+    for (int32_t i = threadIdx.x; i < a.row_bytes / 8; i += kRowThreads)
+        scales[i] = from_e4m3(__ldg(a.s + scale_word4(m, i / 4, a.tiles_k) + i % 4));
+}
+__device__ __forceinline__ void few_ask(const Head4Args &a, int32_t v, int lane) {
+    for (int32_t c = lane * 128; c < a.row_bytes; c += 32 * 128) prefetch_l2(a.w + v * a.row_bytes + c);
+}
+__device__ __forceinline__ float few_part(const Head4Args &a, int32_t v, const unsigned char *smem, int lane) {
+    const float *scales = reinterpret_cast<const float *>(smem + a.row_bytes);
+    const uint4 *w = reinterpret_cast<const uint4 *>(a.w + v * a.row_bytes);
+    const int32_t n = int32_t(a.row_bytes / 16);
+    float sum = 0.0f;
+    for (int32_t c0 = lane; c0 < n; c0 += 32 * kBatch) {
+        uint4 x[kBatch];
+        uint32_t f[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; j++) {
+            const int32_t c = c0 + 32 * j;
+            x[j] = c < n ? __ldg(w + c) : make_uint4(0u, 0u, 0u, 0u);
+            f[j] = c < n ? __ldg(reinterpret_cast<const uint16_t *>(a.ws + scale_word4(v, c / 2, a.tiles_k) + (c & 1) * 2)) : 0u;
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; j++) {
+            const int32_t c = c0 + 32 * j;
+            if (c < n) sum += dot32(reinterpret_cast<const uint4 *>(smem)[c], x[j], scales + 2 * c, f[j]);
+        }
+    }
+    return sum;
+}
+__device__ __forceinline__ float few_logit(const Head4Args &a, int32_t m, int32_t v, float sum) {
+    return sum * __ldg(a.q_rows + m) * __ldg(a.w_rows + v);
 }
 
-// A thread a logit.
-template <typename T>
-__global__ void __launch_bounds__(kThreads4) k_head4(const Head4Args a) {
+template <typename T, bool kPair>
+__global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_constant__ Head4Args a) {
+    constexpr int NT = kTokens<kPair>;
+    constexpr int kAccumulators = 256 / NT;  // the other 256 columns of tensor memory are for scales
+    constexpr int kEpilogue = kEpilogueWarps4<kPair>, kFirst = kFirstWarp4<kPair>;
+    constexpr int kCtas = kPair ? 2 : 1;
+    constexpr uint32_t kHiddenColumns = kSteps * 4, kSlotColumns = 64;  // of a stage's scales in tensor memory
+    static_assert(kHiddenColumns + kSteps * NT / 32 <= kSlotColumns, "a stage's scales fit a slot");
+    extern __shared__ unsigned char dynamic_smem[];
+    __shared__ uint64_t bars[2 * kMaxStages + 2 * kAccumulators];
+    __shared__ T turn[kEpilogue][kTurn<T, kTurnTokens<T>>];
+    __shared__ __align__(16) float token_scales[kEpilogue][kColumns];
+    __shared__ uint32_t need[kNeedTiles / 32];
+    __shared__ uint32_t tmem_base;
+    __shared__ int gave_up;
+    const int warp = __shfl_sync(~0u, int(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    const int rank = kPair ? int(cluster_rank()) : 0;
+    const int32_t unit = int32_t(blockIdx.x) / kCtas, units = int32_t(gridDim.x) / kCtas;
+    const uint32_t full = smem_addr(bars), empty = full + 8 * kMaxStages;
+    const uint32_t ready = empty + 8 * kMaxStages, drained = ready + 8 * kAccumulators;
+    const uint32_t stages = (smem_addr(dynamic_smem) + 1023u) & ~1023u;
+    const uint32_t stage_bytes = uint32_t(kWeightBytes4<kPair> + kHiddenScales + a.box_rows * 128);
+    if (threadIdx.x == 0) {
+        gave_up = 0;
+        for (int i = 0; i < a.stages; i++) {
+            bar_init(full + 8 * i, 1);
+            bar_init(empty + 8 * i, 1);
+        }
+        for (int i = 0; i < kAccumulators; i++) {
+            bar_init(ready + 8 * i, 1);
+            bar_init(drained + 8 * i, kEpilogue * kCtas);
+        }
+        bar_init_fence();
+        tma_prefetch_map(&a.map_w);
+        tma_prefetch_map(&a.map_q);
+        tma_prefetch_map(&a.map_ws);
+        tma_prefetch_map(&a.map_s);
+    }
+    for (int i = threadIdx.x; i < kNeedTiles / 32; i += kThreads4<kPair>) need[i] = 0u;
     pdl_launch_dependents();
     pdl_wait();
-    const int32_t v = int32_t(blockIdx.x) * kThreads4 + int32_t(threadIdx.x), m = blockIdx.y;
-    if (v >= a.V) return;
-    const int64_t bytes = row_bytes4(a.D), tiles = scale_tiles4(a.D);
-    float sum = -INFINITY;
-    if (grammar_row(a.g, m).allows(v)) {
-        sum = 0.0f;
-        for (int32_t k = 0; k < a.D; k += kGroup4) {
-            const uint8_t *q = a.q + m * bytes + k / 2, *w = a.w + v * bytes + k / 2;
-            float part = 0.0f;
-            for (int i = 0; i < kGroup4 / 2; i++) {
-                const float2 x = from_e2m1x2(__ldg(q + i)), y = from_e2m1x2(__ldg(w + i));
-                part = fmaf(x.x, y.x, part);
-                part = fmaf(x.y, y.y, part);
-            }
-            const int j = k % 64 / kGroup4;
-            sum = fmaf(part, from_e4m3(__ldg(a.s + scale_word4(m, k / 64, tiles) + j)) *
-                                 from_e4m3(__ldg(a.ws + scale_word4(v, k / 64, tiles) + j)), sum);
-        }
-        sum *= __ldg(a.q_rows + m) * __ldg(a.w_rows + v);
+    if (a.g.mask && a.M <= kLookRows) {  // k_head_rows may have left nothing to do (the same answer in all CTAs)
+        bool any = false;
+        for (int32_t m = threadIdx.x; m < a.M; m += kThreads4<kPair>) any |= __ldg(a.dense + m) != 0;
+        if (!__syncthreads_or(any)) return;
     }
-    static_cast<T *>(a.logits)[m * a.stride + v] = from_f32<T>(sum);
+    if (warp == 1) tmem_alloc<kPair>(smem_addr(&tmem_base), 512);
+    __syncthreads();
+    if (a.g.mask) {
+        // which of this CTA's tiles a dense row allows a token of
+        for (int32_t i = 0, t = unit; t < a.tiles && i < kNeedTiles; i++, t += units) {
+            const int32_t m = t % a.m_tiles * (kRows * kCtas) + int32_t(threadIdx.x), v0 = t / a.m_tiles * NT;
+            bool any = false;
+            if (threadIdx.x < kRows * kCtas && m < a.M && __ldg(a.dense + m))
+                any = row_uses(a, m, v0) || (NT > 128 && v0 + 128 < a.V && row_uses(a, m, v0 + 128));
+            if (__any_sync(~0u, any) && lane == 0) atomicOr(&need[i >> 5], 1u << (i & 31));
+        }
+    }
+    tcgen05_fence_before();
+    if (kPair) cluster_sync();
+    else __syncthreads();
+    tcgen05_fence_after();
+    const uint32_t tmem = *static_cast<volatile uint32_t *>(&tmem_base);
+    auto needed = [&](int32_t i) { return !a.g.mask || i >= kNeedTiles || ((need[i >> 5] >> (i & 31)) & 1u); };
+
+    if (warp >= kFirst) {
+        if (kPair) more_registers<112>();
+        const int quarter = warp & 3, column = (warp - kFirst) / 4 * kColumns;
+        const uint32_t from = tmem + (uint32_t(quarter * 32) << 16) + uint32_t(column);
+        const uint32_t drain = kPair ? cluster_addr(drained, 0) : drained;
+        const bool wide = ((reinterpret_cast<uintptr_t>(a.logits) | uintptr_t(a.stride * int64_t(sizeof(T)))) & 31) == 0;
+        float *const tokens = token_scales[warp - kFirst];
+        uint32_t it = 0;
+        for (int32_t i = 0, t = unit; t < a.tiles; i++, t += units) {
+            const int32_t m0 = t % a.m_tiles * (kRows * kCtas) + rank * kRows, m1 = min(a.M, m0 + kRows);
+            const int32_t v0 = t / a.m_tiles * NT, v = v0 + column;
+            if (!needed(i)) {
+                fill_tile<T, NT, kEpilogue>(a, m0, m1, v0, warp - kFirst, lane);
+                continue;
+            }
+            const int32_t mine = m0 + quarter * 32, row = min(mine + lane, a.M - 1);
+            const bool there = mine < m1;  // a warp without rows only keeps the barriers going
+            const float row_scale = __ldg(a.q_rows + row);
+            tokens[lane] = __ldg(a.w_rows + min(v + lane, a.V - 1));
+            tokens[lane + 32] = __ldg(a.w_rows + min(v + lane + 32, a.V - 1));
+            __syncwarp();
+            const uint32_t acc = it % kAccumulators;
+            bar_wait(ready + 8 * acc, (it / kAccumulators) & 1, &gave_up);
+            it++;
+            tcgen05_fence_after();
+            uint32_t raw[kColumns / 16][16];
+            if (there) {
+#pragma unroll
+                for (int c = 0; c < kColumns / 16; c++) tmem_load16(from + acc * NT + 16 * c, raw[c]);
+                tmem_wait_ld();
+            }
+            tcgen05_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (kPair) bar_arrive_remote(drain + 8 * acc);
+                else bar_arrive(drain + 8 * acc);
+            }
+            const bool ok = *static_cast<volatile int *>(&gave_up) == 0;
+            if (there) {
+                const GrammarRow allow = grammar_row(a.g, row);
+                const int32_t rows = min(32, m1 - mine);
+                uint32_t some = ~0u;
+                if (a.g.mask) some = __ballot_sync(~0u, __ldg(a.dense + row) != 0);
+#pragma unroll
+                for (int c = 0; c < kColumns; c += 16) {
+                    float sum[16];
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {
+                        const float4 f = *reinterpret_cast<const float4 *>(tokens + c + e);
+                        sum[e] = __uint_as_float(raw[c / 16][e]) * row_scale * f.x;
+                        sum[e + 1] = __uint_as_float(raw[c / 16][e + 1]) * row_scale * f.y;
+                        sum[e + 2] = __uint_as_float(raw[c / 16][e + 2]) * row_scale * f.z;
+                        sum[e + 3] = __uint_as_float(raw[c / 16][e + 3]) * row_scale * f.w;
+                    }
+                    uint32_t bits = ~0u;
+                    if (a.g.mask) bits = (v + c) >> 5 < a.g.W ? allow.word((v + c) >> 5) >> (c & 16) : 0u;
+                    if (!ok || (bits & 0xFFFFu) != 0xFFFFu) {
+#pragma unroll
+                        for (int e = 0; e < 16; e++) {
+                            if (!ok) sum[e] = __int_as_float(0x7FFFFFFF);  // gave up waiting: no result
+                            if (!((bits >> e) & 1u)) sum[e] = -INFINITY;
+                        }
+                    }
+                    if (v + c >= a.V) continue;
+                    T *const to = turn[warp - kFirst];
+                    if (some == ~0u) store16<T, false, T, kTurnTokens<T>>(a, to, sum, mine, rows, some, v + c, lane, wide);
+                    else store16<T, true, T, kTurnTokens<T>>(a, to, sum, mine, rows, some, v + c, lane, wide);
+                }
+            }
+            __syncwarp();  // the next tile's scales are written where these were read
+        }
+    } else {
+        if (kPair) fewer_registers<32>();
+        if (warp == 0) {
+            int stage = 0;
+            uint32_t phase = 1, used = 0;  // phase: of a stage's last use; the first time round there is none
+            bool ok = true;
+            const uint32_t leader = kPair ? cluster_addr(full, 0) : full;
+            for (int32_t i = 0, t = unit; t < a.tiles && ok; i++, t += units) {
+                if (!needed(i)) continue;
+                const int32_t m = t % a.m_tiles * (kRows * kCtas) + rank * kRows, v0 = t / a.m_tiles * NT;
+                for (int32_t kb = 0; kb < a.blocks; kb++) {
+                    const uint32_t at = stages + uint32_t(stage) * stage_bytes, bar = leader + 8 * stage;
+                    const uint32_t scales = at + 128 * 128, hidden_scales = at + kWeightBytes4<kPair>, hidden = hidden_scales + kHiddenScales;
+                    ok = bar_wait(empty + 8 * stage, phase, &gave_up);
+                    ok = __all_sync(~0u, ok);
+                    if (!ok) break;
+                    if (elect_one()) {
+                        if (kPair) {
+                            // both CTAs' copies count on the first one's barrier
+                            if (rank == 0) bar_expect(full + 8 * stage, 2 * stage_bytes);
+                            tma_load_2d_pair(at, &a.map_w, kb * 128, v0 + rank * 128, bar);
+                            tma_load_3d_pair(scales, &a.map_ws, 0, kb * kSteps, v0 / 128, bar);
+                            tma_load_3d_pair(hidden_scales, &a.map_s, 0, kb * kSteps, m / 128, bar);
+                            tma_load_2d_pair(hidden, &a.map_q, kb * 128, m, bar);
+                        } else {
+                            bar_expect(bar, stage_bytes);
+                            tma_load_2d(at, &a.map_w, kb * 128, v0, bar);
+                            tma_load_3d(scales, &a.map_ws, 0, kb * kSteps, v0 / 128, bar);
+                            tma_load_3d(hidden_scales, &a.map_s, 0, kb * kSteps, m / 128, bar);
+                            tma_load_2d(hidden, &a.map_q, kb * 128, m, bar);
+                        }
+                    }
+                    __syncwarp();
+                    used = min(used + 1, uint32_t(a.stages));
+                    if (++stage == a.stages) stage = 0, phase ^= 1;
+                }
+            }
+            if (ok) {  // the last MMAs' arrivals on this CTA's barriers come before it ends
+                for (int i = 0; i < a.stages; i++) {
+                    bar_wait(empty + 8 * stage, phase, &gave_up);
+                    if (++stage == a.stages) stage = 0, phase ^= 1;
+                }
+            } else {  // copies may still write to shared memory: wait for them
+                int none = 0;
+                for (uint32_t i = 0; i < used && rank == 0; i++) {
+                    if (--stage < 0) stage = a.stages - 1, phase ^= 1;
+                    bar_wait(full + 8 * stage, phase ^ 1, &none);
+                }
+            }
+        } else if (warp == 1) {
+            if (rank == 0) {
+                constexpr uint32_t idesc = mma_idesc_e2m1(kRows * kCtas, NT);
+                int stage = 0;
+                uint32_t phase = 0, it = 0, slot = 0;
+                bool ok = true;
+                for (int32_t i = 0, t = unit; t < a.tiles && ok; i++, t += units) {
+                    if (!needed(i)) continue;
+                    const uint32_t acc = it % kAccumulators;
+                    ok = bar_wait(drained + 8 * acc, ((it / kAccumulators) & 1) ^ 1, &gave_up);
+                    it++;
+                    for (int32_t kb = 0; kb < a.blocks; kb++) {
+                        ok = ok && bar_wait(full + 8 * stage, phase, &gave_up);
+                        ok = __all_sync(~0u, ok);
+                        if (!ok) break;
+                        tcgen05_fence_after();
+                        const uint32_t at = stages + uint32_t(stage) * stage_bytes;
+                        const uint32_t scales = at + 128 * 128, hidden_scales = at + kWeightBytes4<kPair>;
+                        const uint64_t dw = mma_desc(at), dq = mma_desc(hidden_scales + kHiddenScales);
+                        const uint32_t sq = tmem + 256 + slot * kSlotColumns, sw = sq + kHiddenColumns;
+                        const int32_t steps = int32_t(min(int64_t(kSteps), a.tiles_k - int64_t(kb) * kSteps));
+                        if (elect_one()) {
+#pragma unroll
+                            for (int k = 0; k < kSteps; k++) {
+                                if (k >= steps) break;
+                                tmem_copy_scales<kPair>(sq + 4 * k, hidden_scales + k * kScaleTile);
+#pragma unroll
+                                for (int j = 0; j < NT / 128; j++)
+                                    tmem_copy_scales<kPair>(sw + k * (NT / 32) + 4 * j, scales + (j * kSteps + k) * kScaleTile);
+                            }
+#pragma unroll
+                            for (int k = 0; k < kSteps; k++) {
+                                if (k >= steps) break;
+                                mma_e2m1<kPair>(tmem + acc * NT, dq + 2 * k, dw + 2 * k, idesc, sq + 4 * k, sw + k * (NT / 32), kb > 0 || k > 0);
+                            }
+                            mma_commit<kPair>(empty + 8 * stage);
+                            if (kb == a.blocks - 1) mma_commit<kPair>(ready + 8 * acc);
+                        }
+                        __syncwarp();
+                        slot ^= 1;
+                        if (++stage == a.stages) stage = 0, phase ^= 1;
+                    }
+                }
+            }
+        }
+    }
+    __syncwarp();
+    tcgen05_fence_before();
+    if (kPair) cluster_sync();
+    else __syncthreads();
+    tcgen05_fence_after();
+    if (warp == 1) tmem_free<kPair>(tmem, 512);
+}
+
+// [rows / 128][columns / 64][512 bytes] in boxes of `row_blocks` x kSteps x 512 bytes, zeros outside.
+bool make_scale_map(CUtensorMap *map, const void *base, int64_t rows, int64_t tiles, int32_t row_blocks) {
+    const Encode encode = tensor_map_encode();
+    if (!encode) return false;
+    const cuuint64_t dims[3] = {kScaleTile / 4, cuuint64_t(tiles), cuuint64_t((rows + 127) / 128)};
+    const cuuint64_t strides[2] = {kScaleTile, cuuint64_t(tiles) * kScaleTile};
+    const cuuint32_t box[3] = {kScaleTile / 4, kSteps, cuuint32_t(row_blocks)}, steps[3] = {1, 1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<void *>(base), dims, strides, box, steps,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, bool kPair>
+cudaError_t launch_head4(Head4Args a, cudaStream_t st) {
+    const int stage = kWeightBytes4<kPair> + kHiddenScales + a.box_rows * 128;
+    // the last stage's MMA reads kRows rows, whatever was loaded; and room to align the ring
+    const int beyond = (kRows - a.box_rows) * 128 + 1024;
+    const int fixed = kEpilogueWarps4<kPair> * int(sizeof(T) * kTurn<T, kTurnTokens<T>> + sizeof(float) * kColumns) + 1024;  // declared in the kernel
+    a.stages = std::min(kMaxStages, (kHeadSmem - fixed - beyond) / stage);
+    const int smem = a.stages * stage + beyond;
+    const cudaError_t e = cudaFuncSetAttribute(k_head4<T, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadSmem - fixed);
+    if (e != cudaSuccess) return e;
+    const int ctas = kPair ? 2 : 1, units = std::min(a.tiles, sm_count() / ctas);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(units * ctas));
+    cfg.blockDim = dim3(kThreads4<kPair>);
+    cfg.dynamicSmemBytes = size_t(smem);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = unsigned(ctas);
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = kPair ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, k_head4<T, kPair>, a);
 }
 
 }  // namespace
@@ -76,16 +409,52 @@ extern "C" int trie_head4_logits(const uint8_t *d_q, const uint8_t *d_scales, co
     if (!*bad && M > 0 && (!d_q || !d_scales || !d_row_scales || !d_w || !d_w_scales || !d_w_row_scales)) bad = "NULL pointer";
     if (!*bad && off_boundary(16, d_q, d_scales, d_w, d_w_scales)) bad = "d_q, d_w and their scales must be aligned to 16 bytes";
     if (!*bad && off_boundary(4, d_row_scales, d_w_row_scales)) bad = "the row scales are not aligned to 4 bytes";
-    if (!*bad && M > 65535) bad = "M must be <= 65535";
+    if (!*bad && M > (1 << 20)) bad = "M must be <= 2^20";
     if (!*bad && M > 0 && d_mask && !d_workspace) bad = "d_mask without d_workspace";
     if (!*bad && off_boundary(16, static_cast<const char *>(d_workspace))) bad = "d_workspace is not aligned to 16 bytes";
     if (*bad) return set_error(TRIE_EINVAL, bad);
     if (M == 0) return TRIE_OK;
-    Head4Args a = {d_q, d_scales, d_w, d_w_scales, d_row_scales, d_w_row_scales, M, V, D, d_logits, stride,
-                   make_grammar(d_mask, mask_rows, d_states, V)};
-    const dim3 grid(unsigned((int64_t(V) + kThreads4 - 1) / kThreads4), unsigned(M));
-    const cudaError_t e = dtype == TRIE_DTYPE_F32 ? launch_pdl_grid(k_head4<float>, grid, kThreads4, 0, stream, a)
-                                                  : launch_pdl_grid(k_head4<__nv_bfloat16>, grid, kThreads4, 0, stream, a);
+    Head4Args a = {};
+    a.q = d_q;
+    a.s = d_scales;
+    a.q_rows = d_row_scales;
+    a.w = d_w;
+    a.ws = d_w_scales;
+    a.w_rows = d_w_row_scales;
+    a.M = M;
+    a.V = V;
+    a.D = D;
+    a.row_bytes = row_bytes4(D);
+    a.tiles_k = scale_tiles4(D);
+    a.blocks = (D + kStageColumns - 1) / kStageColumns;
+    const bool pair = M > kRows;
+    const int side = pair ? 256 : 128;  // of a tile
+    a.m_tiles = (M + side - 1) / side;
+    a.box_rows = std::min(kRows, (M + 7) / 8 * 8);
+    a.logits = d_logits;
+    a.stride = stride;
+    a.g = make_grammar(d_mask, mask_rows, d_states, V);
+    if (!make_map(&a.map_w, d_w, V, a.row_bytes, 128) || !make_map(&a.map_q, d_q, M, a.row_bytes, a.box_rows) ||
+        !make_scale_map(&a.map_ws, d_w_scales, V, a.tiles_k, side / 128) || !make_scale_map(&a.map_s, d_scales, M, a.tiles_k, 1))
+        return set_error(TRIE_ECUDA, "cuTensorMapEncodeTiled failed");
+    const int64_t tiles = (int64_t(V) + side - 1) / side * a.m_tiles;
+    if (tiles > 0x3FFFFFFF) return set_error(TRIE_EINVAL, "M x V is too large");
+    a.tiles = int32_t(tiles);
+    const bool f32 = dtype == TRIE_DTYPE_F32;
+    cudaError_t e;
+    if (d_mask) {
+        const HeadSpace at(M, V);
+        unsigned char *base = static_cast<unsigned char *>(d_workspace);
+        a.dense = reinterpret_cast<int32_t *>(base + at.dense);
+        a.used = reinterpret_cast<uint32_t *>(base + at.used);
+        a.used_words = at.used_words;
+        const int smem = D <= kFewMaxD ? int(a.row_bytes + a.row_bytes / 8 * 4) : 0;
+        e = f32 ? launch_pdl_smem(k_head_rows<float, Head4Args>, M, kRowThreads, smem, stream, a)
+                : launch_pdl_smem(k_head_rows<__nv_bfloat16, Head4Args>, M, kRowThreads, smem, stream, a);
+        if (e != cudaSuccess) return fail_launch(e, "4-bit head rows launch");
+    }
+    e = pair ? (f32 ? launch_head4<float, true>(a, stream) : launch_head4<__nv_bfloat16, true>(a, stream))
+             : (f32 ? launch_head4<float, false>(a, stream) : launch_head4<__nv_bfloat16, false>(a, stream));
     if (e != cudaSuccess) return fail_launch(e, "4-bit head launch");
     return TRIE_OK;
 }
