@@ -676,7 +676,8 @@ int trie_sample(const void *d_logits, int dtype, int64_t stride, int32_t B, int3
  *   d_losses, d_logprobs  device float[B]
  *   d_grad          device [B] rows of V, grad_stride elements apart, of the
  *                   logits' type, or NULL (no gradient); may be d_logits itself
- *                   (with the same stride), else apart from it */
+ *                   (with the same stride), else apart from it
+ * B <= 2^30. */
 int trie_policy_loss(const void *d_logits, int dtype, int64_t stride, int32_t B, int32_t V, const int32_t *d_tokens,
                      const float *d_old_logprobs, const float *d_advantages, const float *d_ref_logprobs,
                      const float *d_weights, const float *d_temperature, float clip_low, float clip_high, float kl,

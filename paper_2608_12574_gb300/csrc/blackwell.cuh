@@ -55,6 +55,22 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
 __device__ __forceinline__ void bar_arrive_remote(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+// The same, with what this thread wrote to shared memory of the cluster before it visible to
+// who waits for it with bar_wait_cluster.
+__device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool bar_try_cluster(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
@@ -71,9 +87,10 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
 // its CTA has not, returns false with *gave_up set. The clock is looked at once
 // in 256 tries: reading it takes longer than the waits of a full pipeline.
 constexpr uint64_t kWaitLimitNs = 2000000000ull;
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *gave_up) {
+template <bool kCluster>
+__device__ __forceinline__ bool bar_wait_of(uint32_t bar, uint32_t parity, volatile int *gave_up) {
     uint64_t t0 = 0;
-    for (uint32_t n = 1; !bar_try(bar, parity); n++) {
+    for (uint32_t n = 1; !(kCluster ? bar_try_cluster(bar, parity) : bar_try(bar, parity)); n++) {
         if (n & 255u) continue;
         if (*gave_up) return false;
         const uint64_t now = global_ns();
@@ -84,6 +101,12 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
         }
     }
     return true;
+}
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *gave_up) {
+    return bar_wait_of<false>(bar, parity, gave_up);
+}
+__device__ __forceinline__ bool bar_wait_cluster(uint32_t bar, uint32_t parity, volatile int *gave_up) {
+    return bar_wait_of<true>(bar, parity, gave_up);
 }
 
 // ---- clusters

@@ -11,15 +11,24 @@
 #include <stdint.h>
 #include <stdio.h>
 
+#include <algorithm>
+
 #include <cuda_runtime.h>
 
+#include "blackwell.cuh"
 #include "logits.cuh"
 
 namespace tmk {
 
 namespace {
 
-constexpr int kPolicyThreads = 512;
+constexpr int kRowThreads = 1024;       // of k_policy_rows
+constexpr int kSlots = 4;               // shares of rows in shared memory, at most
+constexpr int kRowSmem = 224 * 1024;
+constexpr int kMaxCluster = 16;
+constexpr int kRanks = 4;               // rows whose masses may be on their way
+constexpr int kPolicyThreads = 256;     // of k_policy
+constexpr int kMaxShare = kRowSmem / 3 / 128 * 128;  // bytes of a share of which three fit
 
 struct PolicyArgs {
     const void *logits;
@@ -32,6 +41,9 @@ struct PolicyArgs {
     float *losses, *logprobs;
     void *grad;
     int64_t grad_stride;
+    int32_t ctas;         // of a row
+    int32_t clusters;     // of k_policy_rows
+    int32_t slots, slot_bytes;
 };
 
 __device__ __forceinline__ float exp2_of(float x) {
@@ -52,72 +64,506 @@ struct Mass {
         sum = sum * exp2_of((top - t) * c) + other_sum * exp2_of((other_top - t) * c);
         top = t;
     }
-    __device__ __forceinline__ void add(float x, float c) {
-        if (x > top) {
-            sum = sum * exp2_of((top - x) * c) + 1.0f;
-            top = x;
-        } else if (x != -INFINITY) {
-            sum += exp2_of((x - top) * c);
+};
+
+// 16 bytes of a row.
+template <typename T>
+union Piece {
+    static constexpr int kSize = 16 / int(sizeof(T));
+    uint4 raw;
+    T x[kSize];
+    __device__ Piece() {}
+    __device__ __forceinline__ void clear() {
+        const uint32_t none = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;  // -inf
+        raw = make_uint4(none, none, none, none);
+    }
+};
+// The bits of the tokens from v on.
+__device__ __forceinline__ uint32_t bits_from(const GrammarRow &row, int32_t v, int32_t words) {
+    const int32_t w = v >> 5;
+    const uint32_t next = w + 1 < words ? row.word(w + 1) : 0u;
+    return __funnelshift_r(row.word(w), next, v & 31);
+}
+template <typename T>
+__device__ __forceinline__ void largest(const Piece<T> &p, float &top) {
+    if (sizeof(T) == 2) {
+        const __nv_bfloat162 *pair = reinterpret_cast<const __nv_bfloat162 *>(&p.raw);
+        const __nv_bfloat162 m = __hmax2(__hmax2(pair[0], pair[1]), __hmax2(pair[2], pair[3]));
+        top = fmaxf(top, fmaxf(__low2float(m), __high2float(m)));
+    } else {
+#pragma unroll
+        for (int e = 0; e < Piece<T>::kSize; e++) top = fmaxf(top, to_f32(p.x[e]));
+    }
+}
+__device__ __forceinline__ float temperature_of(const PolicyArgs &a, int32_t b) {
+    const float given = a.temperature ? __ldg(a.temperature + b) : 1.0f;
+    return given > 0.0f ? fminf(fmaxf(given, 1.17549435e-38f), 3.40282347e38f) : 1.0f;
+}
+
+struct RowValues {
+    int32_t token;
+    float old, advantage, ref, weight, temperature;
+    __device__ RowValues(const PolicyArgs &a, int32_t b)
+        : token(__ldg(a.tokens + b)), old(__ldg(a.old + b)), advantage(__ldg(a.advantages + b)), ref(a.ref ? __ldg(a.ref + b) : 0.0f),
+          weight(a.weights ? __ldg(a.weights + b) : 1.0f), temperature(temperature_of(a, b)) {}
+};
+
+// What the gradient of a row needs of it, and its loss (written by one thread).
+struct Slope {
+    float top, c;      // exp2((x - top) c) ..
+    float f;           // .. times this: the gradient of a token
+    float at_token;    // of the row's own
+    int32_t token;     // -1: the gradient is 0 everywhere
+};
+__device__ __forceinline__ Slope finish(const PolicyArgs &a, int32_t b, const Mass &all, float xt, const RowValues &v, bool writes) {
+    float lp = (xt - all.top) / v.temperature - logf(all.sum);
+    if (all.top == INFINITY) lp = __int_as_float(0x7FC00000);
+    if (xt == -INFINITY) lp = -INFINITY;
+    float loss = 0.0f, slope = 0.0f;
+    if (lp != -INFINITY && v.weight != 0.0f) {
+        const float rho = expf(lp - v.old);
+        const float free = rho * v.advantage, held = fminf(fmaxf(rho, a.low), a.high) * v.advantage;
+        loss = -(free > held ? held : free);  // a NaN stays one
+        slope = free > held ? 0.0f : -free;
+        if (a.ref) {
+            const float d = v.ref - lp, e = expm1f(d);
+            loss += a.kl * (e - d);
+            slope -= a.kl * e;
+        }
+        loss *= v.weight;
+        slope *= v.weight;
+    }
+    if (writes) {
+        a.losses[b] = loss;
+        a.logprobs[b] = lp;
+    }
+    const float per = 1.0f / v.temperature;
+    return {all.top, 1.44269504f / v.temperature, -slope / all.sum * per, slope * -expm1f(lp) * per, slope == 0.0f ? -1 : v.token};
+}
+// Of a token that is not allowed (or has no probability, for which it is the same) 0, whatever f is.
+__device__ __forceinline__ float slope_of(const Slope &s, float x) { return x == -INFINITY ? 0.0f : s.f * exp2_of((x - s.top) * s.c); }
+
+// Where the 16-byte pieces of row b lie, and the share of a CTA: pieces [first,
+// last), tokens [lo, hi): what is before the first piece belongs to the first
+// CTA of the row, what is behind the last to the last.
+template <typename T>
+struct Share {
+    const T *x;
+    T *grad;
+    int32_t head, first, last, lo, hi;
+    bool same;  // the gradient's pieces lie as the logits'
+    __device__ Share(const PolicyArgs &a, int32_t b, int32_t rank) {
+        constexpr int kSize = Piece<T>::kSize;
+        x = static_cast<const T *>(a.logits) + b * a.stride;
+        grad = a.grad ? static_cast<T *>(a.grad) + b * a.grad_stride : nullptr;
+        head = min(int32_t((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / int32_t(sizeof(T)), a.V);
+        const int32_t pieces = (a.V - head) / kSize, share = (pieces + a.ctas - 1) / a.ctas;
+        first = min(pieces, rank * share);
+        last = min(pieces, first + share);
+        lo = rank == 0 ? 0 : head + first * kSize;
+        hi = rank == a.ctas - 1 ? a.V : head + last * kSize;
+        same = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(grad)) & 15) == 0;
+    }
+    __device__ __forceinline__ const uint4 *pieces() const { return reinterpret_cast<const uint4 *>(x + head); }
+    // the token of thread i among those outside pieces, -1 for none
+    __device__ __forceinline__ int32_t edge(int32_t i) const {
+        const int32_t from = head + first * Piece<T>::kSize, to = head + last * Piece<T>::kSize, before = from - lo;
+        const int32_t v = i < before ? lo + i : to + i - before;
+        return v < hi ? v : -1;
+    }
+    __device__ __forceinline__ void store(int32_t i, const Piece<T> &g) const {
+        constexpr int kSize = Piece<T>::kSize;
+        if (same) {
+            reinterpret_cast<uint4 *>(grad + head)[i] = g.raw;
+        } else {
+#pragma unroll
+            for (int e = 0; e < kSize; e++) grad[head + i * kSize + e] = g.x[e];
         }
     }
 };
 
+// Rows of which three shares fit a CTA's shared memory: clusters of CTAs stay and
+// go over the rows, a cluster a row. One warp of a CTA, the clerk, asks for a
+// free row's shares by bulk copies rows ahead, reads what else a row has, sends
+// the CTA's mass of a row to the others and makes its slope; the other
+// warps take the masses of a row and then write the gradient of the row before,
+// whose slope has had that long to arrive. Of a constrained row only allowed
+// tokens are read, word by word of its mask, and its gradient is zeros with
+// these put in.
+constexpr int kWorkers = kRowThreads - 32;
+constexpr int kWorkerWarps = kWorkers / 32;
+
+// What the workers need to know of a row, by the clerk.
+struct RowIn {
+    int32_t state, token;
+    float temperature;
+    float edge[16];  // logits outside the pieces
+};
+
+__device__ __forceinline__ bool workers_any(bool p) {
+    uint32_t any;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+        "barrier.cta.red.or.pred q, 1, %2, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(any)
+        : "r"(uint32_t(p)), "n"(kWorkers)
+        : "memory");
+    return any != 0;
+}
+__device__ __forceinline__ void workers_sync() { asm volatile("barrier.cta.sync 1, %0;" ::"n"(kWorkers) : "memory"); }
+
+template <typename T>
+__global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs a) {
+    constexpr int kSize = Piece<T>::kSize;
+    extern __shared__ __align__(128) unsigned char slots[];
+    __shared__ uint64_t bars[2 * kSlots + kRanks + 4];
+    __shared__ Mass parts[2][32];
+    __shared__ Mass ranks[kRanks][kMaxCluster];
+    __shared__ RowIn in[kSlots];
+    __shared__ Slope slopes[2];
+    __shared__ int gave_up;
+    const uint32_t full = smem_addr(bars), freed = full + 8 * kSlots;  // of a slot
+    const uint32_t masses = freed + 8 * kSlots;                         // of a row, of all its CTAs
+    const uint32_t summed = masses + 8 * kRanks, sloped = summed + 8 * 2;
+    const int lane = threadIdx.x & 31, warp = __shfl_sync(~0u, int(threadIdx.x >> 5), 0);
+    const int32_t cluster = int32_t(blockIdx.x) / a.ctas, rank = int32_t(blockIdx.x) % a.ctas, V = a.V;
+    if (threadIdx.x == 0) {
+        gave_up = 0;
+        for (int i = 0; i < kSlots; i++) {
+            bar_init(full + 8 * i, 1);
+            bar_init(freed + 8 * i, kWorkerWarps);
+        }
+        for (int i = 0; i < kRanks; i++) bar_init(masses + 8 * i, a.ctas);
+        for (int i = 0; i < 2; i++) {
+            bar_init(summed + 8 * i, kWorkerWarps);
+            bar_init(sloped + 8 * i, 1);
+        }
+        bar_init_fence();
+    }
+    pdl_launch_dependents();
+    if (a.ctas > 1) cluster_sync();  // every CTA's barriers are there
+    else __syncthreads();
+    pdl_wait();
+
+    if (warp == kWorkerWarps) {
+        // Row number r of this cluster: what there is to know, then its share.
+        auto ask = [&](int32_t r) {
+            const int32_t b = cluster + r * a.clusters, slot = r % a.slots;
+            const Share<T> s(a, b, rank);
+            const GrammarRow row = grammar_row(a.g, b);
+            const int32_t edge = s.edge(lane);
+            const float at_edge = edge >= 0 && row.allows(edge) ? to_f32(s.x[edge]) : -INFINITY;
+            if (lane < 16) in[slot].edge[lane] = at_edge;
+            if (lane == 0) {
+                in[slot].state = a.g.mask ? __ldg(a.g.states + b) : TRIE_STATE_FREE;
+                in[slot].temperature = temperature_of(a, b);
+            }
+            __syncwarp();
+            if (lane == 0) {
+                const uint32_t bytes = row.kind == kAllowAll ? uint32_t(s.last - s.first) * 16u : 0u;
+                bar_expect(full + 8 * slot, bytes);
+                if (bytes) bulk_load(smem_addr(slots + slot * a.slot_bytes), s.pieces() + s.first, bytes, full + 8 * slot);
+            }
+            __syncwarp();
+        };
+        const int32_t rows = (a.B - cluster + a.clusters - 1) / a.clusters;
+        for (int32_t r = 0; r < min(rows, a.slots); r++) ask(r);
+        for (int32_t r = 0; r < rows; r++) {
+            const int32_t b = cluster + r * a.clusters;
+            const RowValues v(a, b);
+            const GrammarRow row = grammar_row(a.g, b);
+            const float xt = v.token >= 0 && v.token < V && row.allows(v.token) ? to_f32(Share<T>(a, b, rank).x[v.token]) : -INFINITY;
+            const float c = 1.44269504f / v.temperature;
+            bool ok = bar_wait(summed + 8 * (r & 1), (r >> 1) & 1, &gave_up);
+            Mass all = {-INFINITY, 0.0f};
+            if (lane < kWorkerWarps) all = parts[r & 1][lane];
+#pragma unroll
+            for (int d = 16; d; d >>= 1) all.join(__shfl_xor_sync(~0u, all.top, d), __shfl_xor_sync(~0u, all.sum, d), c);
+            if (a.ctas > 1) {
+                if (lane < a.ctas) {
+                    *cluster_object(&ranks[r % kRanks][rank], lane) = all;
+                    bar_arrive_cluster(cluster_addr(masses + 8 * (r % kRanks), lane));
+                }
+                __syncwarp();
+                ok = bar_wait_cluster(masses + 8 * (r % kRanks), (r / kRanks) & 1, &gave_up) && ok;
+                all = ranks[r % kRanks][lane & (a.ctas - 1)];
+                for (int d = a.ctas / 2; d; d >>= 1) all.join(__shfl_xor_sync(~0u, all.top, d), __shfl_xor_sync(~0u, all.sum, d), c);
+            }
+            if (!__all_sync(~0u, ok)) all.sum = __int_as_float(0x7FC00000);  // gave up waiting: no result
+            const Slope slope = finish(a, b, all, xt, v, rank == 0 && lane == 0);
+            if (lane == 0) {
+                slopes[r & 1] = slope;
+                bar_arrive(sloped + 8 * (r & 1));
+            }
+            if (r > 0 && r - 1 + a.slots < rows) {
+                ok = bar_wait(freed + 8 * ((r - 1) % a.slots), ((r - 1) / a.slots) & 1, &gave_up);
+                if (__all_sync(~0u, ok)) ask(r - 1 + a.slots);
+            }
+        }
+        return;
+    }
+
+    const int32_t worker = threadIdx.x;
+    auto first_pass = [&](int32_t r) {
+        const int slot = r % a.slots;
+        bool there = bar_wait(full + 8 * slot, (r / a.slots) & 1, &gave_up);
+        const RowIn &i = in[slot];
+        const Share<T> s(a, cluster + r * a.clusters, rank);
+        const GrammarRow row = grammar_state(a.g, i.state);
+        const float c = 1.44269504f / i.temperature;
+        Mass all = {-INFINITY, 0.0f};
+        if (row.kind == kAllowAll) {
+            const float at_edge = worker < 16 ? i.edge[worker] : -INFINITY;
+            const uint4 *held = reinterpret_cast<const uint4 *>(slots + slot * a.slot_bytes);
+            const int32_t n = s.last - s.first;
+            all.top = fmaxf(all.top, at_edge);
+            for (int32_t j = worker; j < n; j += kWorkers) {
+                Piece<T> p;
+                p.raw = held[j];
+                largest(p, all.top);
+            }
+            const float off = all.top == -INFINITY ? 0.0f : all.top;
+            all.sum = exp2_of((at_edge - off) * c);
+            for (int32_t j = worker; j < n; j += kWorkers) {
+                Piece<T> p;
+                p.raw = held[j];
+#pragma unroll
+                for (int e = 0; e < kSize; e++) all.sum += exp2_of((to_f32(p.x[e]) - off) * c);
+            }
+        } else {
+            for (int32_t w = (s.lo >> 5) + worker; w * 32 < s.hi; w += kWorkers) {
+                for (uint32_t bits = row.word(w); bits; bits &= bits - 1) {
+                    const int32_t v = w * 32 + __ffs(bits) - 1;
+                    if (v < s.lo || v >= s.hi) continue;
+                    const float x = to_f32(s.x[v]), top = fmaxf(all.top, x), off = top == -INFINITY ? 0.0f : top;
+                    all.sum = all.sum * exp2_of((all.top - off) * c) + exp2_of((x - off) * c);
+                    all.top = top;
+                }
+            }
+        }
+        if (!there) all.sum = __int_as_float(0x7FC00000);
+#pragma unroll
+        for (int d = 16; d; d >>= 1) all.join(__shfl_xor_sync(~0u, all.top, d), __shfl_xor_sync(~0u, all.sum, d), c);
+        if (lane == 0) {
+            parts[r & 1][warp] = all;
+            bar_arrive(summed + 8 * (r & 1));
+        }
+    };
+    auto second_pass = [&](int32_t r) {
+        const int slot = r % a.slots;
+        bar_wait(sloped + 8 * (r & 1), (r >> 1) & 1, &gave_up);
+        const Slope slope = slopes[r & 1];
+        if (!a.grad) return;
+        const Share<T> s(a, cluster + r * a.clusters, rank);
+        const GrammarRow row = grammar_state(a.g, in[slot].state);
+        const int32_t edge = s.edge(worker), n = s.last - s.first;
+        if (row.kind == kAllowAll && slope.token >= 0) {
+            if (edge >= 0) s.grad[edge] = from_f32<T>(edge == slope.token ? slope.at_token : slope_of(slope, in[slot].edge[worker]));
+            const uint4 *held = reinterpret_cast<const uint4 *>(slots + slot * a.slot_bytes);
+            const int32_t at = (slope.token - s.head) / kSize - s.first;  // the token's piece
+            for (int32_t j = worker; j < n; j += kWorkers) {
+                Piece<T> p, g;
+                p.raw = held[j];
+#pragma unroll
+                for (int e = 0; e < kSize; e++) g.x[e] = from_f32<T>(slope_of(slope, to_f32(p.x[e])));
+                s.store(s.first + j, g);
+                if (j == at && slope.token >= s.head) s.grad[slope.token] = from_f32<T>(slope.at_token);
+            }
+            return;
+        }
+        // in place, the allowed tokens' logits are read before the zeros come
+        constexpr int kFew = 4;
+        float value[kFew];
+        int32_t at[kFew], few = 0;
+        bool more = false;
+        if (slope.token >= 0) {
+            for (int32_t w = (s.lo >> 5) + worker; w * 32 < s.hi; w += kWorkers)
+                for (uint32_t bits = row.word(w); bits; bits &= bits - 1) {
+                    const int32_t v = w * 32 + __ffs(bits) - 1;
+                    if (v < s.lo || v >= s.hi) continue;
+#pragma unroll
+                    for (int k = 0; k < kFew; k++)
+                        if (k == few) at[k] = v, value[k] = v == slope.token ? slope.at_token : slope_of(slope, to_f32(s.x[v]));
+                    more |= few >= kFew;
+                    few++;
+                }
+        }
+        if (!workers_any(more)) {
+            Piece<T> g;
+            g.raw = make_uint4(0u, 0u, 0u, 0u);
+            if (edge >= 0) s.grad[edge] = from_f32<T>(0.0f);
+            for (int32_t j = worker; j < n; j += kWorkers) s.store(s.first + j, g);
+            workers_sync();
+#pragma unroll
+            for (int k = 0; k < kFew; k++)
+                if (k < few) s.grad[at[k]] = from_f32<T>(value[k]);
+        } else {
+            for (int32_t v = s.lo + worker; v < s.hi; v += kWorkers)
+                s.grad[v] = from_f32<T>(!row.allows(v) ? 0.0f : v == slope.token ? slope.at_token : slope_of(slope, to_f32(s.x[v])));
+        }
+    };
+    const int32_t rows = (a.B - cluster + a.clusters - 1) / a.clusters;
+    first_pass(0);
+    for (int32_t r = 0; r < rows; r++) {
+        if (r + 1 < rows) first_pass(r + 1);
+        second_pass(r);
+        __syncwarp();
+        if (lane == 0) bar_arrive(freed + 8 * (r % a.slots));
+    }
+}
+
+// Longer rows: a cluster of CTAs a row, a share of its 16-byte pieces each, which
+// the second pass reads again (from L2, as far as it holds the rows at work).
 template <typename T>
 __global__ void __launch_bounds__(kPolicyThreads) k_policy(const PolicyArgs a) {
+    constexpr int kSize = Piece<T>::kSize;
     __shared__ Mass parts[kPolicyThreads / 32];
+    __shared__ Mass ranks[kMaxCluster];
     pdl_launch_dependents();
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int32_t b = blockIdx.x, V = a.V;
-    const T *x = static_cast<const T *>(a.logits) + b * a.stride;
+    const int32_t b = int32_t(blockIdx.x) / a.ctas, rank = int32_t(blockIdx.x) % a.ctas, V = a.V;
+    if (a.ctas > 1) cluster_arrive();
+    const Share<T> s(a, b, rank);
     const GrammarRow row = grammar_row(a.g, b);
-    const float given = a.temperature ? __ldg(a.temperature + b) : 1.0f;
-    const float temperature = given > 0.0f ? fminf(fmaxf(given, 1.17549435e-38f), 3.40282347e38f) : 1.0f;
-    const float c = 1.44269504f / temperature;
-    Mass all = {-INFINITY, 0.0f};
-    for (int32_t v = threadIdx.x; v < V; v += kPolicyThreads)
-        if (row.allows(v)) all.add(to_f32(x[v]), c);
-    for (int d = 16; d; d >>= 1)
-        all.join(__shfl_xor_sync(~0u, all.top, d), __shfl_xor_sync(~0u, all.sum, d), c);
+    const bool masked = row.kind != kAllowAll;
+    const int32_t words = int32_t(a.g.W);
+    const float c = 1.44269504f / temperature_of(a, b);
+    const int32_t edge = s.edge(threadIdx.x);
+
+    // piece i, -inf where it is not there or a token is not allowed
+    auto load = [&](int32_t i, Piece<T> &p) {
+        const uint32_t bits = i >= s.last ? 0u : masked ? bits_from(row, s.head + i * kSize, words) : ~0u;
+        p.clear();
+        if (bits & ((1u << kSize) - 1u)) p.raw = s.pieces()[i];
+        if (masked) {
+#pragma unroll
+            for (int e = 0; e < kSize; e++)
+                if (!((bits >> e) & 1u)) p.x[e] = from_f32<T>(-INFINITY);
+        }
+    };
+    auto load_edge = [&]() { return edge >= 0 && row.allows(edge) ? to_f32(s.x[edge]) : -INFINITY; };
+
+    Mass all = {load_edge(), 0.0f};
+    if (!(all.top == all.top)) all.top = -INFINITY;  // a NaN shows in the sum
+    all.sum = exp2_of((load_edge() - (all.top == -INFINITY ? 0.0f : all.top)) * c);
+    constexpr int kBatch = 4;
+    for (int32_t i0 = s.first + int32_t(threadIdx.x); i0 < s.last; i0 += kBatch * kPolicyThreads) {
+        Piece<T> p[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; i++) load(i0 + i * kPolicyThreads, p[i]);
+        float top = all.top;
+#pragma unroll
+        for (int i = 0; i < kBatch; i++) largest(p[i], top);
+        const float off = top == -INFINITY ? 0.0f : top;
+        all.sum *= exp2_of((all.top - off) * c);
+        all.top = top;
+#pragma unroll
+        for (int i = 0; i < kBatch; i++)
+#pragma unroll
+            for (int e = 0; e < kSize; e++) all.sum += exp2_of((to_f32(p[i].x[e]) - off) * c);
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) all.join(__shfl_xor_sync(~0u, all.top, d), __shfl_xor_sync(~0u, all.sum, d), c);
     if (lane == 0) parts[warp] = all;
-    const int32_t t = __ldg(a.tokens + b);
-    const float xt = t >= 0 && t < V && row.allows(t) ? to_f32(x[t]) : -INFINITY;
+    const RowValues values(a, b);
+    const int32_t t = values.token;
+    const float xt = t >= 0 && t < V && row.allows(t) ? to_f32(s.x[t]) : -INFINITY;
     __syncthreads();
     all = parts[0];
+#pragma unroll
     for (int i = 1; i < kPolicyThreads / 32; i++) all.join(parts[i].top, parts[i].sum, c);
-    float lp = (xt - all.top) / temperature - logf(all.sum);
-    if (all.top == INFINITY) lp = __int_as_float(0x7FC00000);
-    if (xt == -INFINITY) lp = -INFINITY;
-    const float weight = a.weights ? __ldg(a.weights + b) : 1.0f;
-    float loss = 0.0f, slope = 0.0f;
-    if (lp != -INFINITY && weight != 0.0f) {
-        const float A = __ldg(a.advantages + b), rho = expf(lp - __ldg(a.old + b));
-        const float free = rho * A, held = fminf(fmaxf(rho, a.low), a.high) * A;
-        loss = -(free > held ? held : free);  // a NaN stays one
-        slope = free > held ? 0.0f : -free;
-        if (a.ref) {
-            const float d = __ldg(a.ref + b) - lp, e = expm1f(d);
-            loss += a.kl * (e - d);
-            slope -= a.kl * e;
-        }
-        loss *= weight;
-        slope *= weight;
+    if (a.ctas > 1) {
+        cluster_wait();  // all CTAs of the row are there
+        if (int32_t(threadIdx.x) < a.ctas) *cluster_object(&ranks[rank], threadIdx.x) = all;
+        cluster_sync();
+        all = ranks[0];
+        for (int i = 1; i < a.ctas; i++) all.join(ranks[i].top, ranks[i].sum, c);
     }
-    if (threadIdx.x == 0) {
-        a.losses[b] = loss;
-        a.logprobs[b] = lp;
-    }
+    const Slope slope = finish(a, b, all, xt, values, rank == 0 && threadIdx.x == 0);
     if (!a.grad) return;
-    T *grad = static_cast<T *>(a.grad) + b * a.grad_stride;
-    const float per = 1.0f / temperature, f = -slope / all.sum;
-    for (int32_t v = threadIdx.x; v < V; v += kPolicyThreads) {
-        float g = 0.0f;
-        if (slope != 0.0f && row.allows(v)) {
-            if (v == t) g = slope * -expm1f(lp) * per;
-            else g = f * exp2_of((to_f32(x[v]) - all.top) * c) * per;
-        }
-        grad[v] = from_f32<T>(g);
+    const bool zero = slope.token < 0;
+    if (edge >= 0) s.grad[edge] = from_f32<T>(zero ? 0.0f : slope_of(slope, load_edge()));
+    for (int32_t i = s.first + int32_t(threadIdx.x); i < s.last; i += kPolicyThreads) {
+        Piece<T> p, g;
+        p.clear();
+        if (!zero) load(i, p);
+#pragma unroll
+        for (int e = 0; e < kSize; e++) g.x[e] = from_f32<T>(zero ? 0.0f : slope_of(slope, to_f32(p.x[e])));
+        s.store(i, g);
     }
+    if (zero || t < s.lo || t >= s.hi) return;
+    __syncthreads();
+    if (threadIdx.x == 0) s.grad[t] = from_f32<T>(slope.at_token);
+}
+
+// Launches `kernel` with clusters of a.ctas CTAs.
+template <typename K>
+cudaError_t launch_policy(K kernel, const PolicyArgs &a, int64_t ctas, int threads, int smem, cudaStream_t st) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(ctas));
+    cfg.blockDim = dim3(unsigned(threads));
+    cfg.dynamicSmemBytes = size_t(smem);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = unsigned(a.ctas);
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = a.ctas > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
+// Clusters of k_policy_rows<T> of 1 << log_ctas CTAs that the current device runs at once.
+template <typename T>
+int active_clusters(int log_ctas) {
+    static std::atomic<int> known[16][5];
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 16) return 1;
+    if ((n = known[dev][log_ctas].load(std::memory_order_relaxed))) return n;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(1u << log_ctas);
+    cfg.blockDim = dim3(kRowThreads);
+    cfg.dynamicSmemBytes = size_t(kRowSmem);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 1u << log_ctas;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaFuncSetAttribute(k_policy_rows<T>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+        cudaFuncSetAttribute(k_policy_rows<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowSmem) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, k_policy_rows<T>, &cfg) != cudaSuccess || n < 1) {
+        cudaGetLastError();
+        return 0;
+    }
+    known[dev][log_ctas].store(n, std::memory_order_relaxed);
+    return n;
+}
+
+template <typename T>
+cudaError_t run_policy(PolicyArgs a, cudaStream_t st) {
+    // The fewest CTAs a row of which three shares fit; more where the rows are few.
+    const int64_t pieces = int64_t(a.V) * int64_t(sizeof(T)) / 16;
+    auto share = [&] { return (pieces + a.ctas - 1) / a.ctas * 16; };
+    int log_ctas = 0;
+    while (a.ctas < kMaxCluster && (share() > kMaxShare || (a.ctas < 8 && int64_t(a.B) * a.ctas * 2 <= sm_count() && share() > 16 * kRowThreads))) {
+        a.ctas *= 2;
+        log_ctas++;
+    }
+    a.clusters = share() <= kMaxShare ? std::min(a.B, active_clusters<T>(log_ctas)) : 0;
+    if (a.clusters) {
+        const int rows = (a.B + a.clusters - 1) / a.clusters;
+        a.slot_bytes = std::max(128, int((share() + 127) / 128 * 128));
+        a.slots = std::min(std::min(kSlots, rows), kRowSmem / a.slot_bytes);
+        return launch_policy(k_policy_rows<T>, a, int64_t(a.clusters) * a.ctas, kRowThreads, a.slots * a.slot_bytes, st);
+    }
+    a.ctas = 8;
+    if (int64_t(a.B) * a.ctas > 0x7FFFFFFF) return cudaErrorInvalidValue;
+    return launch_policy(k_policy<T>, a, int64_t(a.B) * a.ctas, kPolicyThreads, 0, st);
 }
 
 }  // namespace
@@ -133,6 +579,7 @@ extern "C" int trie_policy_loss(const void *d_logits, int dtype, int64_t stride,
     const char *bad = check_logits(d_logits, dtype, stride, B, V);
     if (!*bad) bad = check_grammar(d_mask, mask_rows, d_states);
     if (!*bad && B > 0 && (!d_tokens || !d_old_logprobs || !d_advantages || !d_losses || !d_logprobs)) bad = "NULL pointer";
+    if (!*bad && B > (1 << 30)) bad = "B must be <= 2^30";
     if (!*bad && off_boundary(4, d_tokens, d_old_logprobs, d_advantages, d_ref_logprobs, d_weights, d_temperature, d_losses, d_logprobs))
         bad = "an array of the rows is not aligned to 4 bytes";
     if (!*bad && !(clip_low >= 0.0f && clip_low <= 1.0f && clip_high >= 0.0f && clip_high <= 3e38f))
@@ -146,9 +593,8 @@ extern "C" int trie_policy_loss(const void *d_logits, int dtype, int64_t stride,
     if (B == 0) return TRIE_OK;
     PolicyArgs a = {d_logits, stride, B, V, d_tokens, d_old_logprobs, d_advantages, kl > 0.0f ? d_ref_logprobs : nullptr, d_weights,
                     d_temperature, 1.0f - clip_low, 1.0f + clip_high, kl, make_grammar(d_mask, mask_rows, d_states, V),
-                    d_losses, d_logprobs, d_grad, grad_stride};
-    const cudaError_t e = dtype == TRIE_DTYPE_F32 ? launch_pdl(k_policy<float>, B, kPolicyThreads, stream, a)
-                                                  : launch_pdl(k_policy<__nv_bfloat16>, B, kPolicyThreads, stream, a);
+                    d_losses, d_logprobs, d_grad, grad_stride, 1, 0, 0, 0};
+    const cudaError_t e = dtype == TRIE_DTYPE_F32 ? run_policy<float>(a, stream) : run_policy<__nv_bfloat16>(a, stream);
     if (e != cudaSuccess) return fail_launch(e, "policy loss launch");
     return TRIE_OK;
 }

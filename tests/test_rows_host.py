@@ -51,7 +51,7 @@ BAD = {
                           dict(w=AT + 4), dict(scales=AT + 8), dict(w_scales=AT + 1), dict(row_scales=AT + 2),
                           dict(w_row_scales=AT + 1), dict(mask=AT, states=AT, mask_rows=1, space=None),
                           dict(mask=AT, states=AT, mask_rows=1, space=AT + 8)],
-    "trie_policy_loss": [*ON_LOGITS, dict(B=-1), dict(tokens=None), dict(old=None), dict(advantages=None), dict(losses=None),
+    "trie_policy_loss": [*ON_LOGITS, dict(B=-1), dict(B=2 ** 30 + 1), dict(tokens=None), dict(old=None), dict(advantages=None), dict(losses=None),
                          dict(logprobs=None), dict(tokens=AT + 2), dict(old=AT + 1), dict(advantages=AT + 2), dict(ref=AT + 2),
                          dict(weights=AT + 2), dict(temperature=AT + 2), dict(losses=AT + 2), dict(logprobs=AT + 2), dict(low=-0.1),
                          dict(low=1.5), dict(low=math.nan), dict(high=-0.1), dict(high=math.inf), dict(high=math.nan), dict(kl=-1.0),
