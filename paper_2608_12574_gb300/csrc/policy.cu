@@ -66,16 +66,74 @@ struct Mass {
     }
 };
 
+// Two numbers at a time.
+using Two = unsigned long long;
+__device__ __forceinline__ Two two(float x, float y) {
+    Two r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ float2 apart(Two x) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+    return r;
+}
+__device__ __forceinline__ Two add2(Two x, Two y) {
+    Two r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+    return r;
+}
+__device__ __forceinline__ Two mul2(Two x, Two y) {
+    Two r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+    return r;
+}
+// exp2((x - top) c), with -top twice and c twice.
+__device__ __forceinline__ Two exp2_of(Two x, Two minus_top, Two c) {
+    const float2 y = apart(mul2(add2(x, minus_top), c));
+    return two(exp2_of(y.x), exp2_of(y.y));
+}
+
 // 16 bytes of a row.
 template <typename T>
-union Piece {
+struct Piece {
     static constexpr int kSize = 16 / int(sizeof(T));
-    uint4 raw;
-    T x[kSize];
-    __device__ Piece() {}
+    uint32_t w[4];
+    __device__ __forceinline__ void set(const uint4 &v) { w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w; }
+    __device__ __forceinline__ uint4 raw() const { return make_uint4(w[0], w[1], w[2], w[3]); }
     __device__ __forceinline__ void clear() {
         const uint32_t none = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;  // -inf
-        raw = make_uint4(none, none, none, none);
+        set(make_uint4(none, none, none, none));
+    }
+    // -inf where the element's bit is 0
+    __device__ __forceinline__ void keep(uint32_t bits) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            if (sizeof(T) == 2) {
+                if (!(bits >> (2 * i) & 1)) w[i] = (w[i] & 0xFFFF0000u) | 0xFF80u;
+                if (!(bits >> (2 * i) & 2)) w[i] = (w[i] & 0xFFFFu) | 0xFF800000u;
+            } else if (!(bits >> i & 1)) {
+                w[i] = 0xFF800000u;
+            }
+        }
+    }
+    // elements 2 i and 2 i + 1
+    __device__ __forceinline__ Two pair(int i) const {
+        if (sizeof(T) == 2) return two(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+        return two(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+    }
+    __device__ __forceinline__ void set_pair(int i, Two x) {
+        const float2 v = apart(x);
+        if (sizeof(T) == 2) {
+            const __nv_bfloat162 both = __floats2bfloat162_rn(v.x, v.y);
+            w[i] = *reinterpret_cast<const uint32_t *>(&both);
+        } else {
+            w[2 * i] = __float_as_uint(v.x), w[2 * i + 1] = __float_as_uint(v.y);
+        }
+    }
+    __device__ __forceinline__ T element(int i) const {
+        if (sizeof(T) == 2) return from_f32<T>(__uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16));
+        return from_f32<T>(__uint_as_float(w[i]));
     }
 };
 // The bits of the tokens from v on.
@@ -84,16 +142,34 @@ __device__ __forceinline__ uint32_t bits_from(const GrammarRow &row, int32_t v, 
     const uint32_t next = w + 1 < words ? row.word(w + 1) : 0u;
     return __funnelshift_r(row.word(w), next, v & 31);
 }
-template <typename T>
-__device__ __forceinline__ void largest(const Piece<T> &p, float &top) {
+// Adds up kCount pieces. A NaN does not show in the largest value but in the sum.
+template <typename T, int kCount>
+__device__ __forceinline__ void add_pieces(Mass &all, const Piece<T> (&p)[kCount], float c) {
+    float top = all.top;
     if (sizeof(T) == 2) {
-        const __nv_bfloat162 *pair = reinterpret_cast<const __nv_bfloat162 *>(&p.raw);
-        const __nv_bfloat162 m = __hmax2(__hmax2(pair[0], pair[1]), __hmax2(pair[2], pair[3]));
-        top = fmaxf(top, fmaxf(__low2float(m), __high2float(m)));
+        __nv_bfloat162 most = *reinterpret_cast<const __nv_bfloat162 *>(&p[0].w[0]);
+#pragma unroll
+        for (int i = 0; i < kCount; i++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) most = __hmax2(most, *reinterpret_cast<const __nv_bfloat162 *>(&p[i].w[j]));
+        top = fmaxf(top, fmaxf(__low2float(most), __high2float(most)));
     } else {
 #pragma unroll
-        for (int e = 0; e < Piece<T>::kSize; e++) top = fmaxf(top, to_f32(p.x[e]));
+        for (int i = 0; i < kCount; i++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) top = fmaxf(top, __uint_as_float(p[i].w[j]));
     }
+    const float off = top == -INFINITY ? 0.0f : top;
+    all.sum *= exp2_of((all.top - off) * c);
+    all.top = top;
+    const Two minus_top = two(-off, -off), cc = two(c, c);
+    Two sum[2] = {two(0.0f, 0.0f), two(0.0f, 0.0f)};
+#pragma unroll
+    for (int i = 0; i < kCount; i++)
+#pragma unroll
+        for (int j = 0; j < Piece<T>::kSize / 2; j++) sum[j & 1] = add2(sum[j & 1], exp2_of(p[i].pair(j), minus_top, cc));
+    const float2 s = apart(add2(sum[0], sum[1]));
+    all.sum += s.x + s.y;
 }
 __device__ __forceinline__ float temperature_of(const PolicyArgs &a, int32_t b) {
     const float given = a.temperature ? __ldg(a.temperature + b) : 1.0f;
@@ -143,6 +219,24 @@ __device__ __forceinline__ Slope finish(const PolicyArgs &a, int32_t b, const Ma
 // Of a token that is not allowed (or has no probability, for which it is the same) 0, whatever f is.
 __device__ __forceinline__ float slope_of(const Slope &s, float x) { return x == -INFINITY ? 0.0f : s.f * exp2_of((x - s.top) * s.c); }
 
+// Of a piece. f exp2() is 0 where x is -inf, unless f is not a number of its own.
+template <typename T>
+__device__ __forceinline__ Piece<T> slope_of(const Slope &s, const Piece<T> &p) {
+    Piece<T> g;
+    if (fabsf(s.f) <= 3.40282347e38f) {
+        const Two minus_top = two(-s.top, -s.top), c = two(s.c, s.c), f = two(s.f, s.f);
+#pragma unroll
+        for (int j = 0; j < Piece<T>::kSize / 2; j++) g.set_pair(j, mul2(f, exp2_of(p.pair(j), minus_top, c)));
+    } else {
+#pragma unroll
+        for (int j = 0; j < Piece<T>::kSize / 2; j++) {
+            const float2 x = apart(p.pair(j));
+            g.set_pair(j, two(slope_of(s, x.x), slope_of(s, x.y)));
+        }
+    }
+    return g;
+}
+
 // Where the 16-byte pieces of row b lie, and the share of a CTA: pieces [first,
 // last), tokens [lo, hi): what is before the first piece belongs to the first
 // CTA of the row, what is behind the last to the last.
@@ -174,10 +268,10 @@ struct Share {
     __device__ __forceinline__ void store(int32_t i, const Piece<T> &g) const {
         constexpr int kSize = Piece<T>::kSize;
         if (same) {
-            reinterpret_cast<uint4 *>(grad + head)[i] = g.raw;
+            reinterpret_cast<uint4 *>(grad + head)[i] = g.raw();
         } else {
 #pragma unroll
-            for (int e = 0; e < kSize; e++) grad[head + i * kSize + e] = g.x[e];
+            for (int e = 0; e < kSize; e++) grad[head + i * kSize + e] = g.element(e);
         }
     }
 };
@@ -190,8 +284,9 @@ struct Share {
 // whose slope has had that long to arrive. Of a constrained row only allowed
 // tokens are read, word by word of its mask, and its gradient is zeros with
 // these put in.
-constexpr int kWorkers = kRowThreads - 32;
+constexpr int kWorkers = kRowThreads - 64;
 constexpr int kWorkerWarps = kWorkers / 32;
+constexpr int kTogether = 5;  // pieces that a worker adds up at a time
 
 // What the workers need to know of a row, by the clerk.
 struct RowIn {
@@ -246,18 +341,22 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
     else __syncthreads();
     pdl_wait();
 
+    const int32_t rows = (a.B - cluster + a.clusters - 1) / a.clusters;
     if (warp == kWorkerWarps) {
-        // Row number r of this cluster: what there is to know, then its share.
-        auto ask = [&](int32_t r) {
+        // What there is to know of a row, then its share. What does not need the slot comes before the wait for it.
+        for (int32_t r = 0; r < rows; r++) {
             const int32_t b = cluster + r * a.clusters, slot = r % a.slots;
             const Share<T> s(a, b, rank);
-            const GrammarRow row = grammar_row(a.g, b);
-            const int32_t edge = s.edge(lane);
+            const int32_t state = a.g.mask ? __ldg(a.g.states + b) : TRIE_STATE_FREE;
+            const GrammarRow row = grammar_state(a.g, state);
+            const float temperature = temperature_of(a, b);
+            const int32_t edge = lane < 16 ? s.edge(lane) : -1;
             const float at_edge = edge >= 0 && row.allows(edge) ? to_f32(s.x[edge]) : -INFINITY;
+            if (r >= a.slots && !__all_sync(~0u, bar_wait(freed + 8 * slot, (r / a.slots - 1) & 1, &gave_up))) break;
             if (lane < 16) in[slot].edge[lane] = at_edge;
             if (lane == 0) {
-                in[slot].state = a.g.mask ? __ldg(a.g.states + b) : TRIE_STATE_FREE;
-                in[slot].temperature = temperature_of(a, b);
+                in[slot].state = state;
+                in[slot].temperature = temperature;
             }
             __syncwarp();
             if (lane == 0) {
@@ -265,15 +364,25 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
                 bar_expect(full + 8 * slot, bytes);
                 if (bytes) bulk_load(smem_addr(slots + slot * a.slot_bytes), s.pieces() + s.first, bytes, full + 8 * slot);
             }
-            __syncwarp();
+        }
+        return;
+    }
+    if (warp > kWorkerWarps) {
+        // The clerk. The next row's values are read while it waits for this one's masses.
+        auto token_logit = [&](int32_t r, const RowValues &v) {
+            const int32_t b = cluster + r * a.clusters;
+            return v.token >= 0 && v.token < V && grammar_row(a.g, b).allows(v.token) ? to_f32(Share<T>(a, b, rank).x[v.token]) : -INFINITY;
         };
-        const int32_t rows = (a.B - cluster + a.clusters - 1) / a.clusters;
-        for (int32_t r = 0; r < min(rows, a.slots); r++) ask(r);
+        RowValues next(a, cluster);
+        float xt_next = token_logit(0, next);
         for (int32_t r = 0; r < rows; r++) {
             const int32_t b = cluster + r * a.clusters;
-            const RowValues v(a, b);
-            const GrammarRow row = grammar_row(a.g, b);
-            const float xt = v.token >= 0 && v.token < V && row.allows(v.token) ? to_f32(Share<T>(a, b, rank).x[v.token]) : -INFINITY;
+            const RowValues v = next;
+            const float xt = xt_next;
+            if (r + 1 < rows) {
+                next = RowValues(a, b + a.clusters);
+                xt_next = token_logit(r + 1, next);
+            }
             const float c = 1.44269504f / v.temperature;
             bool ok = bar_wait(summed + 8 * (r & 1), (r >> 1) & 1, &gave_up);
             Mass all = {-INFINITY, 0.0f};
@@ -296,10 +405,6 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
                 slopes[r & 1] = slope;
                 bar_arrive(sloped + 8 * (r & 1));
             }
-            if (r > 0 && r - 1 + a.slots < rows) {
-                ok = bar_wait(freed + 8 * ((r - 1) % a.slots), ((r - 1) / a.slots) & 1, &gave_up);
-                if (__all_sync(~0u, ok)) ask(r - 1 + a.slots);
-            }
         }
         return;
     }
@@ -318,18 +423,15 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
             const uint4 *held = reinterpret_cast<const uint4 *>(slots + slot * a.slot_bytes);
             const int32_t n = s.last - s.first;
             all.top = fmaxf(all.top, at_edge);
-            for (int32_t j = worker; j < n; j += kWorkers) {
-                Piece<T> p;
-                p.raw = held[j];
-                largest(p, all.top);
-            }
-            const float off = all.top == -INFINITY ? 0.0f : all.top;
-            all.sum = exp2_of((at_edge - off) * c);
-            for (int32_t j = worker; j < n; j += kWorkers) {
-                Piece<T> p;
-                p.raw = held[j];
+            all.sum = exp2_of((at_edge - (all.top == -INFINITY ? 0.0f : all.top)) * c);
+            for (int32_t j0 = worker; j0 < n; j0 += kTogether * kWorkers) {
+                Piece<T> p[kTogether];
 #pragma unroll
-                for (int e = 0; e < kSize; e++) all.sum += exp2_of((to_f32(p.x[e]) - off) * c);
+                for (int k = 0; k < kTogether; k++) {
+                    p[k].clear();
+                    if (j0 + k * kWorkers < n) p[k].set(held[j0 + k * kWorkers]);
+                }
+                add_pieces(all, p, c);
             }
         } else {
             for (int32_t w = (s.lo >> 5) + worker; w * 32 < s.hi; w += kWorkers) {
@@ -362,12 +464,11 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
             if (edge >= 0) s.grad[edge] = from_f32<T>(edge == slope.token ? slope.at_token : slope_of(slope, in[slot].edge[worker]));
             const uint4 *held = reinterpret_cast<const uint4 *>(slots + slot * a.slot_bytes);
             const int32_t at = (slope.token - s.head) / kSize - s.first;  // the token's piece
+#pragma unroll 2
             for (int32_t j = worker; j < n; j += kWorkers) {
-                Piece<T> p, g;
-                p.raw = held[j];
-#pragma unroll
-                for (int e = 0; e < kSize; e++) g.x[e] = from_f32<T>(slope_of(slope, to_f32(p.x[e])));
-                s.store(s.first + j, g);
+                Piece<T> p;
+                p.set(held[j]);
+                s.store(s.first + j, slope_of(slope, p));
                 if (j == at && slope.token >= s.head) s.grad[slope.token] = from_f32<T>(slope.at_token);
             }
             return;
@@ -391,7 +492,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
         }
         if (!workers_any(more)) {
             Piece<T> g;
-            g.raw = make_uint4(0u, 0u, 0u, 0u);
+            g.set(make_uint4(0u, 0u, 0u, 0u));
             if (edge >= 0) s.grad[edge] = from_f32<T>(0.0f);
             for (int32_t j = worker; j < n; j += kWorkers) s.store(s.first + j, g);
             workers_sync();
@@ -403,7 +504,6 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
                 s.grad[v] = from_f32<T>(!row.allows(v) ? 0.0f : v == slope.token ? slope.at_token : slope_of(slope, to_f32(s.x[v])));
         }
     };
-    const int32_t rows = (a.B - cluster + a.clusters - 1) / a.clusters;
     first_pass(0);
     for (int32_t r = 0; r < rows; r++) {
         if (r + 1 < rows) first_pass(r + 1);
@@ -436,12 +536,8 @@ __global__ void __launch_bounds__(kPolicyThreads) k_policy(const PolicyArgs a) {
     auto load = [&](int32_t i, Piece<T> &p) {
         const uint32_t bits = i >= s.last ? 0u : masked ? bits_from(row, s.head + i * kSize, words) : ~0u;
         p.clear();
-        if (bits & ((1u << kSize) - 1u)) p.raw = s.pieces()[i];
-        if (masked) {
-#pragma unroll
-            for (int e = 0; e < kSize; e++)
-                if (!((bits >> e) & 1u)) p.x[e] = from_f32<T>(-INFINITY);
-        }
+        if (bits & ((1u << kSize) - 1u)) p.set(s.pieces()[i]);
+        if (masked) p.keep(bits);
     };
     auto load_edge = [&]() { return edge >= 0 && row.allows(edge) ? to_f32(s.x[edge]) : -INFINITY; };
 
@@ -453,16 +549,7 @@ __global__ void __launch_bounds__(kPolicyThreads) k_policy(const PolicyArgs a) {
         Piece<T> p[kBatch];
 #pragma unroll
         for (int i = 0; i < kBatch; i++) load(i0 + i * kPolicyThreads, p[i]);
-        float top = all.top;
-#pragma unroll
-        for (int i = 0; i < kBatch; i++) largest(p[i], top);
-        const float off = top == -INFINITY ? 0.0f : top;
-        all.sum *= exp2_of((all.top - off) * c);
-        all.top = top;
-#pragma unroll
-        for (int i = 0; i < kBatch; i++)
-#pragma unroll
-            for (int e = 0; e < kSize; e++) all.sum += exp2_of((to_f32(p[i].x[e]) - off) * c);
+        add_pieces(all, p, c);
     }
 #pragma unroll
     for (int d = 16; d; d >>= 1) all.join(__shfl_xor_sync(~0u, all.top, d), __shfl_xor_sync(~0u, all.sum, d), c);
@@ -486,12 +573,14 @@ __global__ void __launch_bounds__(kPolicyThreads) k_policy(const PolicyArgs a) {
     const bool zero = slope.token < 0;
     if (edge >= 0) s.grad[edge] = from_f32<T>(zero ? 0.0f : slope_of(slope, load_edge()));
     for (int32_t i = s.first + int32_t(threadIdx.x); i < s.last; i += kPolicyThreads) {
-        Piece<T> p, g;
-        p.clear();
-        if (!zero) load(i, p);
-#pragma unroll
-        for (int e = 0; e < kSize; e++) g.x[e] = from_f32<T>(zero ? 0.0f : slope_of(slope, to_f32(p.x[e])));
-        s.store(i, g);
+        Piece<T> p;
+        if (zero) {
+            p.set(make_uint4(0u, 0u, 0u, 0u));
+        } else {
+            load(i, p);
+            p = slope_of(slope, p);
+        }
+        s.store(i, p);
     }
     if (zero || t < s.lo || t >= s.hi) return;
     __syncthreads();
