@@ -177,10 +177,10 @@ __device__ __forceinline__ float temperature_of(const PolicyArgs &a, int32_t b) 
 }
 
 struct RowValues {
-    int32_t token;
+    int32_t token, state;
     float old, advantage, ref, weight, temperature;
     __device__ RowValues(const PolicyArgs &a, int32_t b)
-        : token(__ldg(a.tokens + b)), old(__ldg(a.old + b)), advantage(__ldg(a.advantages + b)), ref(a.ref ? __ldg(a.ref + b) : 0.0f),
+        : token(__ldg(a.tokens + b)), state(a.g.mask ? __ldg(a.g.states + b) : TRIE_STATE_FREE), old(__ldg(a.old + b)), advantage(__ldg(a.advantages + b)), ref(a.ref ? __ldg(a.ref + b) : 0.0f),
           weight(a.weights ? __ldg(a.weights + b) : 1.0f), temperature(temperature_of(a, b)) {}
 };
 
@@ -290,22 +290,16 @@ constexpr int kTogether = 5;  // pieces that a worker adds up at a time
 
 // What the workers need to know of a row, by the clerk.
 struct RowIn {
-    int32_t state, token;
+    int32_t state;
+    int32_t listed;   // of a constrained row: its allowed tokens in this share, whose ids and logits are in the slot
     float temperature;
-    float edge[16];  // logits outside the pieces
+    float edge[16];   // logits outside the pieces
+};
+struct Listed {
+    int32_t token;
+    float x;
 };
 
-__device__ __forceinline__ bool workers_any(bool p) {
-    uint32_t any;
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
-        "barrier.cta.red.or.pred q, 1, %2, p;\n\t"
-        "selp.u32 %0, 1, 0, q;\n\t}"
-        : "=r"(any)
-        : "r"(uint32_t(p)), "n"(kWorkers)
-        : "memory");
-    return any != 0;
-}
 __device__ __forceinline__ void workers_sync() { asm volatile("barrier.cta.sync 1, %0;" ::"n"(kWorkers) : "memory"); }
 
 template <typename T>
@@ -356,6 +350,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
             if (lane < 16) in[slot].edge[lane] = at_edge;
             if (lane == 0) {
                 in[slot].state = state;
+                in[slot].listed = 0;
                 in[slot].temperature = temperature;
             }
             __syncwarp();
@@ -368,21 +363,21 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
         return;
     }
     if (warp > kWorkerWarps) {
-        // The clerk. The next row's values are read while it waits for this one's masses.
+        // The clerk. It reads a row's values two rows ahead, and its token's logit one, so that it waits for none.
         auto token_logit = [&](int32_t r, const RowValues &v) {
             const int32_t b = cluster + r * a.clusters;
-            return v.token >= 0 && v.token < V && grammar_row(a.g, b).allows(v.token) ? to_f32(Share<T>(a, b, rank).x[v.token]) : -INFINITY;
+            return v.token >= 0 && v.token < V && grammar_state(a.g, v.state).allows(v.token) ? to_f32(Share<T>(a, b, rank).x[v.token]) : -INFINITY;
         };
-        RowValues next(a, cluster);
+        auto values = [&](int32_t r) { return RowValues(a, cluster + min(r, rows - 1) * a.clusters); };
+        RowValues next = values(0), after = values(1);
         float xt_next = token_logit(0, next);
         for (int32_t r = 0; r < rows; r++) {
             const int32_t b = cluster + r * a.clusters;
             const RowValues v = next;
             const float xt = xt_next;
-            if (r + 1 < rows) {
-                next = RowValues(a, b + a.clusters);
-                xt_next = token_logit(r + 1, next);
-            }
+            next = after;
+            if (r + 1 < rows) xt_next = token_logit(r + 1, next);
+            after = values(r + 2);
             const float c = 1.44269504f / v.temperature;
             bool ok = bar_wait(summed + 8 * (r & 1), (r >> 1) & 1, &gave_up);
             Mass all = {-INFINITY, 0.0f};
@@ -409,11 +404,11 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
         return;
     }
 
-    const int32_t worker = threadIdx.x;
+    const int32_t worker = threadIdx.x, most = a.slot_bytes / int32_t(sizeof(Listed));
     auto first_pass = [&](int32_t r) {
         const int slot = r % a.slots;
         bool there = bar_wait(full + 8 * slot, (r / a.slots) & 1, &gave_up);
-        const RowIn &i = in[slot];
+        RowIn &i = in[slot];
         const Share<T> s(a, cluster + r * a.clusters, rank);
         const GrammarRow row = grammar_state(a.g, i.state);
         const float c = 1.44269504f / i.temperature;
@@ -434,6 +429,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
                 add_pieces(all, p, c);
             }
         } else {
+            Listed *list = reinterpret_cast<Listed *>(slots + slot * a.slot_bytes);
             for (int32_t w = (s.lo >> 5) + worker; w * 32 < s.hi; w += kWorkers) {
                 for (uint32_t bits = row.word(w); bits; bits &= bits - 1) {
                     const int32_t v = w * 32 + __ffs(bits) - 1;
@@ -441,6 +437,8 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
                     const float x = to_f32(s.x[v]), top = fmaxf(all.top, x), off = top == -INFINITY ? 0.0f : top;
                     all.sum = all.sum * exp2_of((all.top - off) * c) + exp2_of((x - off) * c);
                     all.top = top;
+                    const int32_t at = atomicAdd(&i.listed, 1);
+                    if (at < most) list[at] = {v, x};
                 }
             }
         }
@@ -473,32 +471,18 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
             }
             return;
         }
-        // in place, the allowed tokens' logits are read before the zeros come
-        constexpr int kFew = 4;
-        float value[kFew];
-        int32_t at[kFew], few = 0;
-        bool more = false;
-        if (slope.token >= 0) {
-            for (int32_t w = (s.lo >> 5) + worker; w * 32 < s.hi; w += kWorkers)
-                for (uint32_t bits = row.word(w); bits; bits &= bits - 1) {
-                    const int32_t v = w * 32 + __ffs(bits) - 1;
-                    if (v < s.lo || v >= s.hi) continue;
-#pragma unroll
-                    for (int k = 0; k < kFew; k++)
-                        if (k == few) at[k] = v, value[k] = v == slope.token ? slope.at_token : slope_of(slope, to_f32(s.x[v]));
-                    more |= few >= kFew;
-                    few++;
-                }
-        }
-        if (!workers_any(more)) {
+        const int32_t listed = slope.token >= 0 ? in[slot].listed : 0;
+        if (listed <= most) {
             Piece<T> g;
             g.set(make_uint4(0u, 0u, 0u, 0u));
             if (edge >= 0) s.grad[edge] = from_f32<T>(0.0f);
             for (int32_t j = worker; j < n; j += kWorkers) s.store(s.first + j, g);
             workers_sync();
-#pragma unroll
-            for (int k = 0; k < kFew; k++)
-                if (k < few) s.grad[at[k]] = from_f32<T>(value[k]);
+            const Listed *list = reinterpret_cast<const Listed *>(slots + slot * a.slot_bytes);
+            for (int32_t j = worker; j < listed; j += kWorkers) {
+                const Listed one = list[j];
+                s.grad[one.token] = from_f32<T>(one.token == slope.token ? slope.at_token : slope_of(slope, one.x));
+            }
         } else {
             for (int32_t v = s.lo + worker; v < s.hi; v += kWorkers)
                 s.grad[v] = from_f32<T>(!row.allows(v) ? 0.0f : v == slope.token ? slope.at_token : slope_of(slope, to_f32(s.x[v])));
