@@ -22,7 +22,6 @@ namespace tmk {
 
 namespace {
 
-constexpr int kRowThreads = 1024;       // of k_policy_rows
 constexpr int kSlots = 4;               // shares of rows in shared memory, at most
 constexpr int kRowSmem = 224 * 1024;
 constexpr int kMaxCluster = 16;
@@ -65,6 +64,17 @@ struct Mass {
         top = t;
     }
 };
+
+// Of a warp's masses, in all lanes.
+__device__ __forceinline__ Mass warp_mass(const Mass &mine, float c) {
+    Mass all;
+    asm("redux.sync.max.f32 %0, %1, 0xFFFFFFFF;" : "=f"(all.top) : "f"(mine.top));
+    const float off = all.top == -INFINITY ? 0.0f : all.top;
+    all.sum = mine.sum * exp2_of((mine.top - off) * c);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) all.sum += __shfl_xor_sync(~0u, all.sum, d);
+    return all;
+}
 
 // Two numbers at a time.
 using Two = unsigned long long;
@@ -246,6 +256,7 @@ struct Share {
     T *grad;
     int32_t head, first, last, lo, hi;
     bool same;  // the gradient's pieces lie as the logits'
+    Share() = default;
     __device__ Share(const PolicyArgs &a, int32_t b, int32_t rank) {
         constexpr int kSize = Piece<T>::kSize;
         x = static_cast<const T *>(a.logits) + b * a.stride;
@@ -284,15 +295,18 @@ struct Share {
 // whose slope has had that long to arrive. Of a constrained row only allowed
 // tokens are read, word by word of its mask, and its gradient is zeros with
 // these put in.
-constexpr int kWorkers = kRowThreads - 64;
-constexpr int kWorkerWarps = kWorkers / 32;
+constexpr int kWorkerWarps = 15;
+constexpr int kWorkers = 32 * kWorkerWarps;
+constexpr int kRowThreads = kWorkers + 64;
 constexpr int kTogether = 5;  // pieces that a worker adds up at a time
 
-// What the workers need to know of a row, by the clerk.
+// What the workers need to know of a row.
+template <typename T>
 struct RowIn {
-    int32_t state;
+    Share<T> share;
+    GrammarRow row;
     int32_t listed;   // of a constrained row: its allowed tokens in this share, whose ids and logits are in the slot
-    float temperature;
+    float c;          // log2(e) / temperature
     float edge[16];   // logits outside the pieces
 };
 struct Listed {
@@ -309,7 +323,8 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
     __shared__ uint64_t bars[2 * kSlots + kRanks + 4];
     __shared__ Mass parts[2][32];
     __shared__ Mass ranks[kRanks][kMaxCluster];
-    __shared__ RowIn in[kSlots];
+    __shared__ __align__(16) unsigned char in_bytes[kSlots * sizeof(RowIn<T>)];
+    RowIn<T> *const in = reinterpret_cast<RowIn<T> *>(in_bytes);
     __shared__ Slope slopes[2];
     __shared__ int gave_up;
     const uint32_t full = smem_addr(bars), freed = full + 8 * kSlots;  // of a slot
@@ -343,15 +358,16 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
             const Share<T> s(a, b, rank);
             const int32_t state = a.g.mask ? __ldg(a.g.states + b) : TRIE_STATE_FREE;
             const GrammarRow row = grammar_state(a.g, state);
-            const float temperature = temperature_of(a, b);
+            const float c = 1.44269504f / temperature_of(a, b);
             const int32_t edge = lane < 16 ? s.edge(lane) : -1;
             const float at_edge = edge >= 0 && row.allows(edge) ? to_f32(s.x[edge]) : -INFINITY;
             if (r >= a.slots && !__all_sync(~0u, bar_wait(freed + 8 * slot, (r / a.slots - 1) & 1, &gave_up))) break;
             if (lane < 16) in[slot].edge[lane] = at_edge;
             if (lane == 0) {
-                in[slot].state = state;
+                in[slot].share = s;
+                in[slot].row = row;
                 in[slot].listed = 0;
-                in[slot].temperature = temperature;
+                in[slot].c = c;
             }
             __syncwarp();
             if (lane == 0) {
@@ -382,8 +398,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
             bool ok = bar_wait(summed + 8 * (r & 1), (r >> 1) & 1, &gave_up);
             Mass all = {-INFINITY, 0.0f};
             if (lane < kWorkerWarps) all = parts[r & 1][lane];
-#pragma unroll
-            for (int d = 16; d; d >>= 1) all.join(__shfl_xor_sync(~0u, all.top, d), __shfl_xor_sync(~0u, all.sum, d), c);
+            all = warp_mass(all, c);
             if (a.ctas > 1) {
                 if (lane < a.ctas) {
                     *cluster_object(&ranks[r % kRanks][rank], lane) = all;
@@ -391,8 +406,9 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
                 }
                 __syncwarp();
                 ok = bar_wait_cluster(masses + 8 * (r % kRanks), (r / kRanks) & 1, &gave_up) && ok;
-                all = ranks[r % kRanks][lane & (a.ctas - 1)];
-                for (int d = a.ctas / 2; d; d >>= 1) all.join(__shfl_xor_sync(~0u, all.top, d), __shfl_xor_sync(~0u, all.sum, d), c);
+                all = {-INFINITY, 0.0f};
+                if (lane < a.ctas) all = ranks[r % kRanks][lane];
+                all = warp_mass(all, c);
             }
             if (!__all_sync(~0u, ok)) all.sum = __int_as_float(0x7FC00000);  // gave up waiting: no result
             const Slope slope = finish(a, b, all, xt, v, rank == 0 && lane == 0);
@@ -405,31 +421,33 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
     }
 
     const int32_t worker = threadIdx.x, most = a.slot_bytes / int32_t(sizeof(Listed));
-    auto first_pass = [&](int32_t r) {
-        const int slot = r % a.slots;
-        bool there = bar_wait(full + 8 * slot, (r / a.slots) & 1, &gave_up);
-        RowIn &i = in[slot];
-        const Share<T> s(a, cluster + r * a.clusters, rank);
-        const GrammarRow row = grammar_state(a.g, i.state);
-        const float c = 1.44269504f / i.temperature;
+    auto first_pass = [&](int32_t r, int slot, uint32_t phase) {
+        const bool there = bar_wait(full + 8 * slot, phase, &gave_up);
+        RowIn<T> &i = in[slot];
+        const float c = i.c;
+        unsigned char *const held = slots + slot * a.slot_bytes;
         Mass all = {-INFINITY, 0.0f};
-        if (row.kind == kAllowAll) {
-            const float at_edge = worker < 16 ? i.edge[worker] : -INFINITY;
-            const uint4 *held = reinterpret_cast<const uint4 *>(slots + slot * a.slot_bytes);
-            const int32_t n = s.last - s.first;
-            all.top = fmaxf(all.top, at_edge);
-            all.sum = exp2_of((at_edge - (all.top == -INFINITY ? 0.0f : all.top)) * c);
-            for (int32_t j0 = worker; j0 < n; j0 += kTogether * kWorkers) {
+        if (i.row.kind == kAllowAll) {
+            if (worker < 16) {
+                const float x = i.edge[worker];
+                all.top = fmaxf(all.top, x);
+                all.sum = exp2_of((x - (all.top == -INFINITY ? 0.0f : all.top)) * c);
+            }
+            const uint4 *from = reinterpret_cast<const uint4 *>(held) + worker;
+            for (int32_t left = i.share.last - i.share.first - worker; left > 0; left -= kTogether * kWorkers) {
                 Piece<T> p[kTogether];
 #pragma unroll
                 for (int k = 0; k < kTogether; k++) {
                     p[k].clear();
-                    if (j0 + k * kWorkers < n) p[k].set(held[j0 + k * kWorkers]);
+                    if (left > k * kWorkers) p[k].set(from[k * kWorkers]);
                 }
                 add_pieces(all, p, c);
+                from += kTogether * kWorkers;
             }
         } else {
-            Listed *list = reinterpret_cast<Listed *>(slots + slot * a.slot_bytes);
+            Listed *list = reinterpret_cast<Listed *>(held);
+            const Share<T> s = i.share;
+            const GrammarRow row = i.row;
             for (int32_t w = (s.lo >> 5) + worker; w * 32 < s.hi; w += kWorkers) {
                 for (uint32_t bits = row.word(w); bits; bits &= bits - 1) {
                     const int32_t v = w * 32 + __ffs(bits) - 1;
@@ -443,31 +461,30 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
             }
         }
         if (!there) all.sum = __int_as_float(0x7FC00000);
-#pragma unroll
-        for (int d = 16; d; d >>= 1) all.join(__shfl_xor_sync(~0u, all.top, d), __shfl_xor_sync(~0u, all.sum, d), c);
+        all = warp_mass(all, c);
         if (lane == 0) {
             parts[r & 1][warp] = all;
             bar_arrive(summed + 8 * (r & 1));
         }
     };
-    auto second_pass = [&](int32_t r) {
-        const int slot = r % a.slots;
+    auto second_pass = [&](int32_t r, int slot) {
         bar_wait(sloped + 8 * (r & 1), (r >> 1) & 1, &gave_up);
-        const Slope slope = slopes[r & 1];
         if (!a.grad) return;
-        const Share<T> s(a, cluster + r * a.clusters, rank);
-        const GrammarRow row = grammar_state(a.g, in[slot].state);
-        const int32_t edge = s.edge(worker), n = s.last - s.first;
-        if (row.kind == kAllowAll && slope.token >= 0) {
+        const Slope slope = slopes[r & 1];
+        const Share<T> s = in[slot].share;
+        const int32_t n = s.last - s.first;
+        const unsigned char *const held = slots + slot * a.slot_bytes;
+        const int32_t edge = worker < 16 ? s.edge(worker) : -1;
+        if (in[slot].row.kind == kAllowAll && slope.token >= 0) {
             if (edge >= 0) s.grad[edge] = from_f32<T>(edge == slope.token ? slope.at_token : slope_of(slope, in[slot].edge[worker]));
-            const uint4 *held = reinterpret_cast<const uint4 *>(slots + slot * a.slot_bytes);
-            const int32_t at = (slope.token - s.head) / kSize - s.first;  // the token's piece
-#pragma unroll 2
+            const uint4 *from = reinterpret_cast<const uint4 *>(held);
+            const int32_t at = slope.token < s.head ? -1 : (slope.token - s.head) / kSize - s.first;  // the token's piece
+#pragma unroll 5
             for (int32_t j = worker; j < n; j += kWorkers) {
                 Piece<T> p;
-                p.set(held[j]);
+                p.set(from[j]);
                 s.store(s.first + j, slope_of(slope, p));
-                if (j == at && slope.token >= s.head) s.grad[slope.token] = from_f32<T>(slope.at_token);
+                if (j == at) s.grad[slope.token] = from_f32<T>(slope.at_token);
             }
             return;
         }
@@ -478,22 +495,31 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
             if (edge >= 0) s.grad[edge] = from_f32<T>(0.0f);
             for (int32_t j = worker; j < n; j += kWorkers) s.store(s.first + j, g);
             workers_sync();
-            const Listed *list = reinterpret_cast<const Listed *>(slots + slot * a.slot_bytes);
+            const Listed *list = reinterpret_cast<const Listed *>(held);
             for (int32_t j = worker; j < listed; j += kWorkers) {
                 const Listed one = list[j];
                 s.grad[one.token] = from_f32<T>(one.token == slope.token ? slope.at_token : slope_of(slope, one.x));
             }
         } else {
+            const GrammarRow row = in[slot].row;
             for (int32_t v = s.lo + worker; v < s.hi; v += kWorkers)
                 s.grad[v] = from_f32<T>(!row.allows(v) ? 0.0f : v == slope.token ? slope.at_token : slope_of(slope, to_f32(s.x[v])));
         }
     };
-    first_pass(0);
+    int slot = 0, slot_next = 0;
+    uint32_t phase = 0;  // of slot_next
+    auto step = [&] {
+        if (++slot_next == a.slots) slot_next = 0, phase ^= 1;
+    };
+    first_pass(0, 0, 0);
+    step();
     for (int32_t r = 0; r < rows; r++) {
-        if (r + 1 < rows) first_pass(r + 1);
-        second_pass(r);
+        if (r + 1 < rows) first_pass(r + 1, slot_next, phase);
+        second_pass(r, slot);
         __syncwarp();
-        if (lane == 0) bar_arrive(freed + 8 * (r % a.slots));
+        if (lane == 0) bar_arrive(freed + 8 * slot);
+        slot = slot_next;
+        step();
     }
 }
 
