@@ -23,7 +23,7 @@ namespace tmk {
 namespace {
 
 constexpr int kSlots = 4;               // shares of rows in shared memory, at most
-constexpr int kRowSmem = 224 * 1024;
+constexpr int kRowSmem = 228224;        // beside 4 KB that are declared
 constexpr int kMaxCluster = 16;
 constexpr int kRanks = 4;               // rows whose masses may be on their way
 constexpr int kPolicyThreads = 256;     // of k_policy
@@ -297,7 +297,10 @@ struct Share {
 // these put in.
 constexpr int kWorkerWarps = 15;
 constexpr int kWorkers = 32 * kWorkerWarps;
-constexpr int kRowThreads = kWorkers + 64;
+constexpr int kSender = kWorkerWarps, kFinisher = kSender + 1, kFirstBringer = kFinisher + 1;
+constexpr int kRowThreads = 32 * (kFirstBringer + kSlots);
+constexpr int kListed = 64;   // allowed tokens of a share that are listed, at most
+constexpr int kWordsAhead = 38;  // words of the mask that a lane reads at a time: 38,912 tokens, a share of bf16 logits
 constexpr int kTogether = 5;  // pieces that a worker adds up at a time
 
 // What the workers need to know of a row.
@@ -305,16 +308,17 @@ template <typename T>
 struct RowIn {
     Share<T> share;
     GrammarRow row;
-    int32_t listed;   // of a constrained row: its allowed tokens in this share, whose ids and logits are in the slot
+    int32_t listed;   // >= 0: so many allowed tokens, listed here; -1: the share is in the slot
+    Mass mass;        // of the listed tokens
     float c;          // log2(e) / temperature
     float edge[16];   // logits outside the pieces
-};
-struct Listed {
-    int32_t token;
-    float x;
+    int32_t token[kListed];
+    float x[kListed];
 };
 
 __device__ __forceinline__ void workers_sync() { asm volatile("barrier.cta.sync 1, %0;" ::"n"(kWorkers) : "memory"); }
+
+__device__ __forceinline__ void first_logits_sync() { asm volatile("barrier.cta.sync 2, 64;" ::: "memory"); }
 
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs a) {
@@ -351,117 +355,199 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
     pdl_wait();
 
     const int32_t rows = (a.B - cluster + a.clusters - 1) / a.clusters;
-    if (warp == kWorkerWarps) {
-        // What there is to know of a row, then its share. What does not need the slot comes before the wait for it.
-        for (int32_t r = 0; r < rows; r++) {
-            const int32_t b = cluster + r * a.clusters, slot = r % a.slots;
+    if (warp >= kFirstBringer) {
+        // Brings every a.slots-th row into its slot: what there is to know of it, and its share or the list of its
+        // allowed tokens. What does not need the slot comes before the wait for it.
+        const int slot = warp - kFirstBringer;
+        RowIn<T> &i = in[slot];
+        uint32_t phase = 1;
+        auto state_of = [&](int32_t r) { return a.g.mask && r < rows ? __ldg(a.g.states + cluster + r * a.clusters) : TRIE_STATE_FREE; };
+        int32_t state = state_of(slot);
+        for (int32_t r = slot; r < rows && slot < a.slots; r += a.slots, phase ^= 1) {
+            const int32_t b = cluster + r * a.clusters;
             const Share<T> s(a, b, rank);
-            const int32_t state = a.g.mask ? __ldg(a.g.states + b) : TRIE_STATE_FREE;
             const GrammarRow row = grammar_state(a.g, state);
+            state = state_of(r + a.slots);
             const float c = 1.44269504f / temperature_of(a, b);
             const int32_t edge = lane < 16 ? s.edge(lane) : -1;
             const float at_edge = edge >= 0 && row.allows(edge) ? to_f32(s.x[edge]) : -INFINITY;
-            if (r >= a.slots && !__all_sync(~0u, bar_wait(freed + 8 * slot, (r / a.slots - 1) & 1, &gave_up))) break;
-            if (lane < 16) in[slot].edge[lane] = at_edge;
+            int32_t listed = row.kind == kAllowAll ? -1 : 0, token[kListed / 32];  // token number n: lane n % 32's, n / 32
+#pragma unroll
+            for (int k = 0; k < kListed / 32; k++) token[k] = -1;
+            for (int32_t w0 = s.lo >> 5; listed >= 0 && w0 * 32 < s.hi; w0 += kWordsAhead * 32) {
+                uint32_t word[kWordsAhead];
+                const bool read = row.kind == kAllowRow;
+#pragma unroll
+                for (int k = 0; k < kWordsAhead; k++) {  // all on their way at once
+                    const int32_t w = w0 + 32 * k + lane;
+                    word[k] = read && w * 32 < s.hi ? __ldg(row.words + w) : 0u;
+                }
+#pragma unroll
+                for (int k = 0; k < kWordsAhead; k++) {
+                    const int32_t w = w0 + 32 * k + lane, v = w * 32;
+                    if (!read && w == (V - 1) >> 5) word[k] = row.word(w);
+                    if (v < s.lo) word[k] &= ~0u << (s.lo - v);
+                    if (v + 32 > s.hi) word[k] &= v < s.hi ? (1u << (s.hi - v)) - 1u : 0u;
+                }
+#pragma unroll
+                for (int k = 0; k < kWordsAhead; k++)
+                    for (uint32_t lanes = __ballot_sync(~0u, word[k] != 0u); lanes && listed >= 0; lanes &= lanes - 1) {
+                        const int from = __ffs(lanes) - 1;
+                        const uint32_t bits = __shfl_sync(~0u, word[k], from);
+                        const int32_t at = lane - listed % 32 + (lane < listed % 32 ? 32 : 0);  // which of the word's tokens is this lane's next
+                        const int32_t n = __popc(bits);
+                        if (listed + n > kListed) {
+                            listed = -1;
+                            break;
+                        }
+                        if (at < n) {
+                            const int32_t v = (w0 + 32 * k + from) * 32 + int32_t(__fns(bits, 0, at + 1));
+                            if (listed + at < 32) token[0] = v;
+                            else token[1] = v;
+                        }
+                        listed += n;
+                    }
+            }
+            static_assert(kListed == 64, "two tokens a lane");
+            float x[kListed / 32];
+            Mass mass = {-INFINITY, 0.0f};
+#pragma unroll
+            for (int k = 0; k < kListed / 32; k++) {
+                x[k] = lane + 32 * k < listed ? to_f32(s.x[token[k]]) : -INFINITY;
+                mass.top = fmaxf(mass.top, x[k]);
+            }
+            const float off = mass.top == -INFINITY ? 0.0f : mass.top;
+            mass.sum = exp2_of((x[0] - off) * c) + exp2_of((x[1] - off) * c);
+            mass = warp_mass(mass, c);
+            if (!__all_sync(~0u, bar_wait(freed + 8 * slot, phase, &gave_up))) break;
+            if (lane < 16) i.edge[lane] = at_edge;
+#pragma unroll
+            for (int k = 0; k < kListed / 32; k++) {
+                i.token[lane + 32 * k] = token[k];
+                i.x[lane + 32 * k] = x[k];
+            }
             if (lane == 0) {
-                in[slot].share = s;
-                in[slot].row = row;
-                in[slot].listed = 0;
-                in[slot].c = c;
+                i.share = s;
+                i.row = row;
+                i.listed = listed;
+                i.mass = mass;
+                i.c = c;
             }
             __syncwarp();
             if (lane == 0) {
-                const uint32_t bytes = row.kind == kAllowAll ? uint32_t(s.last - s.first) * 16u : 0u;
+                const uint32_t bytes = listed < 0 ? uint32_t(s.last - s.first) * 16u : 0u;
                 bar_expect(full + 8 * slot, bytes);
                 if (bytes) bulk_load(smem_addr(slots + slot * a.slot_bytes), s.pieces() + s.first, bytes, full + 8 * slot);
             }
         }
         return;
     }
-    if (warp > kWorkerWarps) {
-        // The clerk. It reads a row's values two rows ahead, and its token's logit one, so that it waits for none.
-        auto token_logit = [&](int32_t r, const RowValues &v) {
-            const int32_t b = cluster + r * a.clusters;
-            return v.token >= 0 && v.token < V && grammar_state(a.g, v.state).allows(v.token) ? to_f32(Share<T>(a, b, rank).x[v.token]) : -INFINITY;
-        };
-        auto values = [&](int32_t r) { return RowValues(a, cluster + min(r, rows - 1) * a.clusters); };
-        RowValues next = values(0), after = values(1);
-        float xt_next = token_logit(0, next);
+    if (warp == kSender) {
+        // The CTA's mass of a row, to all CTAs of the cluster; the first once the finisher has its tokens' logits.
+        first_logits_sync();
         for (int32_t r = 0; r < rows; r++) {
-            const int32_t b = cluster + r * a.clusters;
-            const RowValues v = next;
-            const float xt = xt_next;
-            next = after;
-            if (r + 1 < rows) xt_next = token_logit(r + 1, next);
-            after = values(r + 2);
-            const float c = 1.44269504f / v.temperature;
-            bool ok = bar_wait(summed + 8 * (r & 1), (r >> 1) & 1, &gave_up);
+            const float c = 1.44269504f / temperature_of(a, cluster + r * a.clusters);
+            const bool ok = bar_wait(summed + 8 * (r & 1), (r >> 1) & 1, &gave_up);
             Mass all = {-INFINITY, 0.0f};
             if (lane < kWorkerWarps) all = parts[r & 1][lane];
             all = warp_mass(all, c);
-            if (a.ctas > 1) {
-                if (lane < a.ctas) {
-                    *cluster_object(&ranks[r % kRanks][rank], lane) = all;
-                    bar_arrive_cluster(cluster_addr(masses + 8 * (r % kRanks), lane));
-                }
-                __syncwarp();
-                ok = bar_wait_cluster(masses + 8 * (r % kRanks), (r / kRanks) & 1, &gave_up) && ok;
-                all = {-INFINITY, 0.0f};
-                if (lane < a.ctas) all = ranks[r % kRanks][lane];
-                all = warp_mass(all, c);
-            }
             if (!__all_sync(~0u, ok)) all.sum = __int_as_float(0x7FC00000);  // gave up waiting: no result
-            const Slope slope = finish(a, b, all, xt, v, rank == 0 && lane == 0);
-            if (lane == 0) {
-                slopes[r & 1] = slope;
-                bar_arrive(sloped + 8 * (r & 1));
+            if (lane < a.ctas) {
+                *cluster_object(&ranks[r % kRanks][rank], lane) = all;
+                bar_arrive_cluster(cluster_addr(masses + 8 * (r % kRanks), lane));
             }
         }
         return;
     }
+    if (warp == kFinisher) {
+        // A row's slope from all its CTAs' masses. What it needs of a row is read ahead so that it waits for none:
+        // the row's values four rows, the mask's word with its token three, the token's logit two, and the
+        // latter is there before the slope of two rows earlier is, and so before any CTA writes the row's gradient.
+        auto values = [&](int32_t r) { return RowValues(a, cluster + min(r, rows - 1) * a.clusters); };
+        auto mask_word = [&](const RowValues &v) {
+            const GrammarRow row = grammar_state(a.g, v.state);
+            if (v.token < 0 || v.token >= V) return 0u;
+            return row.kind == kAllowRow ? __ldg(row.words + (v.token >> 5)) : row.word(v.token >> 5);
+        };
+        auto token_logit = [&](int32_t r, const RowValues &v, uint32_t word) {
+            return (word >> (v.token & 31)) & 1u ? to_f32(Share<T>(a, cluster + min(r, rows - 1) * a.clusters, rank).x[v.token]) : -INFINITY;
+        };
+        RowValues v0 = values(0), v1 = values(1), v2 = values(2), v3 = values(3);
+        float x0 = token_logit(0, v0, mask_word(v0)), x1 = token_logit(1, v1, mask_word(v1));
+        uint32_t word2 = mask_word(v2);
+        x0 = __shfl_sync(~0u, x0, 0), x1 = __shfl_sync(~0u, x1, 0);
+        first_logits_sync();
+        for (int32_t r = 0; r < rows; r++) {
+            float x2 = token_logit(r + 2, v2, word2);
+            const uint32_t word3 = mask_word(v3);
+            const RowValues v4 = values(r + 4);
+            const float c = 1.44269504f / v0.temperature;
+            const bool ok = bar_wait_cluster(masses + 8 * (r % kRanks), (r / kRanks) & 1, &gave_up);
+            Mass all = {-INFINITY, 0.0f};
+            if (lane < a.ctas) all = ranks[r % kRanks][lane];
+            all = warp_mass(all, c);
+            if (!__all_sync(~0u, ok)) all.sum = __int_as_float(0x7FC00000);
+            const Slope slope = finish(a, cluster + r * a.clusters, all, x0, v0, rank == 0 && lane == 0);
+            x2 = __shfl_sync(~0u, x2, 0);  // it is there
+            if (lane == 0) {
+                slopes[r & 1] = slope;
+                bar_arrive(sloped + 8 * (r & 1));
+            }
+            v0 = v1, v1 = v2, v2 = v3, v3 = v4, x0 = x1, x1 = x2, word2 = word3;
+        }
+        return;
+    }
 
-    const int32_t worker = threadIdx.x, most = a.slot_bytes / int32_t(sizeof(Listed));
+    const int32_t worker = threadIdx.x, words = int32_t(a.g.W);
+    const bool in_place = a.grad == a.logits;
+    auto fill = [&](const Share<T> &s) {  // with zeros
+        const int32_t edge = worker < 16 ? s.edge(worker) : -1;
+        if (edge >= 0) s.grad[edge] = from_f32<T>(0.0f);
+        Piece<T> g;
+        g.set(make_uint4(0u, 0u, 0u, 0u));
+        for (int32_t j = s.first + worker; j < s.last; j += kWorkers) s.store(j, g);
+    };
     auto first_pass = [&](int32_t r, int slot, uint32_t phase) {
         const bool there = bar_wait(full + 8 * slot, phase, &gave_up);
-        RowIn<T> &i = in[slot];
+        const RowIn<T> &i = in[slot];
         const float c = i.c;
-        unsigned char *const held = slots + slot * a.slot_bytes;
         Mass all = {-INFINITY, 0.0f};
-        if (i.row.kind == kAllowAll) {
+        if (i.listed < 0) {
             if (worker < 16) {
                 const float x = i.edge[worker];
                 all.top = fmaxf(all.top, x);
                 all.sum = exp2_of((x - (all.top == -INFINITY ? 0.0f : all.top)) * c);
             }
-            const uint4 *from = reinterpret_cast<const uint4 *>(held) + worker;
+            uint4 *held = reinterpret_cast<uint4 *>(slots + slot * a.slot_bytes) + worker;
+            const bool masked = i.row.kind != kAllowAll;
+            int32_t v = i.share.head + (i.share.first + worker) * kSize;
             for (int32_t left = i.share.last - i.share.first - worker; left > 0; left -= kTogether * kWorkers) {
                 Piece<T> p[kTogether];
 #pragma unroll
                 for (int k = 0; k < kTogether; k++) {
                     p[k].clear();
-                    if (left > k * kWorkers) p[k].set(from[k * kWorkers]);
+                    if (left > k * kWorkers) p[k].set(held[k * kWorkers]);
+                }
+                if (masked) {  // for the second pass too
+#pragma unroll
+                    for (int k = 0; k < kTogether; k++)
+                        if (left > k * kWorkers) {
+                            p[k].keep(bits_from(i.row, v + k * kWorkers * kSize, words));
+                            held[k * kWorkers] = p[k].raw();
+                        }
+                    async_fence();  // a copy writes there next
                 }
                 add_pieces(all, p, c);
-                from += kTogether * kWorkers;
+                held += kTogether * kWorkers;
+                v += kTogether * kWorkers * kSize;
             }
         } else {
-            Listed *list = reinterpret_cast<Listed *>(held);
-            const Share<T> s = i.share;
-            const GrammarRow row = i.row;
-            for (int32_t w = (s.lo >> 5) + worker; w * 32 < s.hi; w += kWorkers) {
-                for (uint32_t bits = row.word(w); bits; bits &= bits - 1) {
-                    const int32_t v = w * 32 + __ffs(bits) - 1;
-                    if (v < s.lo || v >= s.hi) continue;
-                    const float x = to_f32(s.x[v]), top = fmaxf(all.top, x), off = top == -INFINITY ? 0.0f : top;
-                    all.sum = all.sum * exp2_of((all.top - off) * c) + exp2_of((x - off) * c);
-                    all.top = top;
-                    const int32_t at = atomicAdd(&i.listed, 1);
-                    if (at < most) list[at] = {v, x};
-                }
-            }
+            if (worker == 0) all = i.mass;
+            if (a.grad && !in_place) fill(i.share);
         }
         if (!there) all.sum = __int_as_float(0x7FC00000);
         all = warp_mass(all, c);
+        __syncwarp();  // the zeros are written, too
         if (lane == 0) {
             parts[r & 1][warp] = all;
             bar_arrive(summed + 8 * (r & 1));
@@ -475,7 +561,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
         const int32_t n = s.last - s.first;
         const unsigned char *const held = slots + slot * a.slot_bytes;
         const int32_t edge = worker < 16 ? s.edge(worker) : -1;
-        if (in[slot].row.kind == kAllowAll && slope.token >= 0) {
+        if (in[slot].listed < 0 && slope.token >= 0) {
             if (edge >= 0) s.grad[edge] = from_f32<T>(edge == slope.token ? slope.at_token : slope_of(slope, in[slot].edge[worker]));
             const uint4 *from = reinterpret_cast<const uint4 *>(held);
             const int32_t at = slope.token < s.head ? -1 : (slope.token - s.head) / kSize - s.first;  // the token's piece
@@ -488,22 +574,14 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
             }
             return;
         }
-        const int32_t listed = slope.token >= 0 ? in[slot].listed : 0;
-        if (listed <= most) {
-            Piece<T> g;
-            g.set(make_uint4(0u, 0u, 0u, 0u));
-            if (edge >= 0) s.grad[edge] = from_f32<T>(0.0f);
-            for (int32_t j = worker; j < n; j += kWorkers) s.store(s.first + j, g);
+        if (in_place || in[slot].listed < 0) {
+            fill(s);
             workers_sync();
-            const Listed *list = reinterpret_cast<const Listed *>(held);
-            for (int32_t j = worker; j < listed; j += kWorkers) {
-                const Listed one = list[j];
-                s.grad[one.token] = from_f32<T>(one.token == slope.token ? slope.at_token : slope_of(slope, one.x));
-            }
-        } else {
-            const GrammarRow row = in[slot].row;
-            for (int32_t v = s.lo + worker; v < s.hi; v += kWorkers)
-                s.grad[v] = from_f32<T>(!row.allows(v) ? 0.0f : v == slope.token ? slope.at_token : slope_of(slope, to_f32(s.x[v])));
+        }
+        const int32_t listed = slope.token >= 0 ? in[slot].listed : 0;
+        if (worker < listed) {
+            const int32_t v = in[slot].token[worker];
+            s.grad[v] = from_f32<T>(v == slope.token ? slope.at_token : slope_of(slope, in[slot].x[worker]));
         }
     };
     int slot = 0, slot_next = 0;

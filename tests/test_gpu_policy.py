@@ -254,6 +254,52 @@ def test_policy_strides(cuda, offset, pad, g_offset, g_pad, V, dtype):
     assert bool((x[:, V:] == 7).all())
 
 
+@pytest.mark.parametrize("dtype,V", [("bf16", 30011), ("f32", 70001), ("bf16", 700003)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_policy_many_rows(cuda, dtype, V, in_place):
+    """More rows than are at work at a time, free rows and rows that allow few and many tokens one after the other."""
+    import torch
+    rng = np.random.default_rng([V, in_place])
+    B = 700 if V < 100000 else 40
+    allowed = np.zeros((6, V), bool)
+    allowed[0, rng.choice(V, 7, replace=False)] = True
+    allowed[1, rng.choice(V, 500, replace=False)] = True
+    allowed[2, rng.choice(V, 3000, replace=False)] = True
+    allowed[3] = rng.random(V) < 0.7
+    allowed[4, V - 9:] = True
+    allowed[5, :3] = True
+    states = rng.choice([-3, -3, 0, 1, 2, 3, 4, 5, -1], B).astype(np.int32)
+    logits = (torch.from_numpy(rng.normal(0, 2, (64 if B > 64 else B, V)).astype(np.float32)).to(_type(dtype)).to(cuda))
+    logits = logits.repeat((B + len(logits) - 1) // len(logits), 1)[:B].contiguous()
+    ok = torch.from_numpy(np.stack([lref.allowed_row(allowed, s, V) for s in range(-3, 6)])).to(cuda)
+    ok = ok[torch.from_numpy(states).to(cuda).long() + 3]
+    g = torch.Generator(device=cuda)
+    g.manual_seed(V)
+    tokens = torch.where(ok, torch.rand(B, V, generator=g, device=cuda), -1.0).argmax(dim=1)
+    A, weights = torch.randn(B, generator=g, device=cuda), torch.rand(B, generator=g, device=cuda) + 0.5
+    # in 64 bits
+    y = torch.where(ok, logits.double(), -math.inf)
+    y = y - torch.logsumexp(y, dim=1, keepdim=True)
+    lp = y.gather(1, tokens[:, None])[:, 0]
+    old = (lp - 0.1).float()  # rho = exp(0.1): within the clips
+    rho = torch.exp(lp - old.double())
+    want = torch.exp(y) * (weights * A * rho)[:, None]
+    want.scatter_add_(1, tokens[:, None], -(weights * A * rho)[:, None])
+    grad = logits if in_place else torch.full_like(logits, math.nan)
+    losses, logprobs = T.trie_policy_loss(logits, tokens.int(), old, A, weights=weights, clip=(0.5, 0.5), grad=grad,
+                                          mask=torch.from_numpy(lref.pack(allowed)).to(cuda), states=torch.from_numpy(states).to(cuda))
+    # the bounds of _check for |lp| < 20 and |x| < 40
+    off = (60 + 4 * math.log2(V) + V / 128 + 80) * U
+    assert float((logprobs - lp).abs().max()) <= off
+    assert float((losses + weights * A * rho).abs().max()) <= float((weights * A * rho).abs().max()) * (off + 16 * U)
+    assert bool((grad[~ok] == 0).all())
+    half = 2.0 ** -8 if dtype == "bf16" else U
+    reach = (weights * A * rho).abs()[:, None].double()
+    bound = want.abs() * (2 * off + 260 * U + half) + 2.0 ** -133
+    bound.scatter_add_(1, tokens[:, None], reach * off)
+    assert float(((grad.double() - want).abs() - bound).max()) <= 0
+
+
 def test_policy_repeats_and_graphs(cuda):
     """The same bits every time, on a side stream and replayed from a graph on new logits; given outputs."""
     import torch
