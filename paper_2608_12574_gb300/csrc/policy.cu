@@ -362,15 +362,16 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
         RowIn<T> &i = in[slot];
         uint32_t phase = 1;
         auto state_of = [&](int32_t r) { return a.g.mask && r < rows ? __ldg(a.g.states + cluster + r * a.clusters) : TRIE_STATE_FREE; };
+        auto c_of = [&](int32_t r) { return 1.44269504f / temperature_of(a, cluster + min(r, rows - 1) * a.clusters); };
         int32_t state = state_of(slot);
+        float c_next = c_of(slot);
         for (int32_t r = slot; r < rows && slot < a.slots; r += a.slots, phase ^= 1) {
             const int32_t b = cluster + r * a.clusters;
             const Share<T> s(a, b, rank);
             const GrammarRow row = grammar_state(a.g, state);
+            const float c = c_next;
             state = state_of(r + a.slots);
-            const float c = 1.44269504f / temperature_of(a, b);
-            const int32_t edge = lane < 16 ? s.edge(lane) : -1;
-            const float at_edge = edge >= 0 && row.allows(edge) ? to_f32(s.x[edge]) : -INFINITY;
+            c_next = c_of(r + a.slots);
             int32_t listed = row.kind == kAllowAll ? -1 : 0, token[kListed / 32];  // token number n: lane n % 32's, n / 32
 #pragma unroll
             for (int k = 0; k < kListed / 32; k++) token[k] = -1;
@@ -394,19 +395,22 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
                     for (uint32_t lanes = __ballot_sync(~0u, word[k] != 0u); lanes && listed >= 0; lanes &= lanes - 1) {
                         const int from = __ffs(lanes) - 1;
                         const uint32_t bits = __shfl_sync(~0u, word[k], from);
-                        const int32_t at = lane - listed % 32 + (lane < listed % 32 ? 32 : 0);  // which of the word's tokens is this lane's next
-                        const int32_t n = __popc(bits);
-                        if (listed + n > kListed) {
+                        if (listed + __popc(bits) > kListed) {
                             listed = -1;
                             break;
                         }
-                        if (at < n) {
-                            const int32_t v = (w0 + 32 * k + from) * 32 + int32_t(__fns(bits, 0, at + 1));
-                            if (listed + at < 32) token[0] = v;
-                            else token[1] = v;
-                        }
-                        listed += n;
+                        for (uint32_t rest = bits; rest; rest &= rest - 1, listed++)
+                            if (lane == listed % 32) {
+                                const int32_t v = (w0 + 32 * k + from) * 32 + __ffs(rest) - 1;
+                                if (listed < 32) token[0] = v;
+                                else token[1] = v;
+                            }
                     }
+            }
+            float at_edge = -INFINITY;
+            if (listed < 0) {
+                const int32_t edge = lane < 16 ? s.edge(lane) : -1;
+                if (edge >= 0 && row.allows(edge)) at_edge = to_f32(s.x[edge]);
             }
             static_assert(kListed == 64, "two tokens a lane");
             float x[kListed / 32];
