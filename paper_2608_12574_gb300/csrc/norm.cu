@@ -16,16 +16,25 @@
 #include <stdint.h>
 #include <stdio.h>
 
+#include <algorithm>
+#include <type_traits>
+
 #include <cuda_runtime.h>
 
+#include "blackwell.cuh"
 #include "quantize.cuh"
+#include "two.cuh"
 
 namespace tmk {
 
 namespace {
 
-constexpr int kNormThreads = 256;
-constexpr int kEach = 8;  // columns of a thread at a time
+constexpr int kNormThreads = 256;  // where rows are read again
+constexpr int kMaxThreads = 1024;  // of a row of one step a thread
+constexpr int kHoldThreads = 512;  // of more
+constexpr int kStayRows = 1;       // a CTA stays where it has more rows than this
+constexpr size_t kMostSpace = 220 * 1024;  // of an SM's shared memory
+constexpr int kEach = 8;           // columns of a thread at a time
 
 struct NormArgs {
     const void *x;         // [M] rows
@@ -34,9 +43,11 @@ struct NormArgs {
     void *residual;        // [M] rows or NULL
     int64_t residual_stride;
     const void *gain;      // [D]
-    bool residual_f32, gain_f32;
-    bool wide_x, wide_residual, wide_gain, wide_q;  // 16-byte (q: 8-byte) accesses of eight columns
+    bool x_f32, residual_f32, gain_f32;
+    bool wide, wide_q;     // rows can be read (q: written) eight columns at a time
     double eps;
+    int32_t buffers;       // of k_norm_rows: 2 where a CTA takes several rows
+    float eps_32, eps_rest, per_column, per_column_rest;  // eps and 1 / D as pairs
     uint8_t *q;
     float *scales;         // 8 bits: [ceil(D/128)][pitch]
     int64_t pitch;
@@ -44,46 +55,74 @@ struct NormArgs {
     float *row_scales;
 };
 
-// Eight columns from column c of a row of D; zeros behind the end.
-template <typename T>
-__device__ __forceinline__ void load8(const T *row, int32_t c, int32_t D, bool wide, float (&v)[kEach]) {
-    if (wide && c + kEach <= D) {
-        union {
-            uint4 raw[kEach * sizeof(T) / 16];
-            T x[kEach];
-        } u;
-#pragma unroll
-        for (int i = 0; i < int(kEach * sizeof(T) / 16); i++) u.raw[i] = reinterpret_cast<const uint4 *>(row + c)[i];
-#pragma unroll
-        for (int i = 0; i < kEach; i++) v[i] = to_f32(u.x[i]);
+// Eight columns of a row as they were read: with kWide in w[0..3] (bf16) or w[0..7]
+// (f32) as they lie in memory, else an element in each. Nothing is done with
+// them until all of a thread's reads are on their way.
+struct Raw {
+    uint32_t w[kEach];
+};
+template <bool kWide>
+__device__ __forceinline__ Raw load8(const void *row, bool f32, int32_t c, int32_t D) {
+    Raw r;
+    if (kWide) {  // D is a multiple of eight
+        const uint4 *at = reinterpret_cast<const uint4 *>(static_cast<const char *>(row) + int64_t(c) * (f32 ? 4 : 2));
+        uint4 lo = make_uint4(0u, 0u, 0u, 0u), hi = lo;
+        if (c < D) lo = at[0];
+        if (c < D && f32) hi = at[1];
+        r.w[0] = lo.x, r.w[1] = lo.y, r.w[2] = lo.z, r.w[3] = lo.w, r.w[4] = hi.x, r.w[5] = hi.y, r.w[6] = hi.z, r.w[7] = hi.w;
     } else {
 #pragma unroll
-        for (int i = 0; i < kEach; i++) v[i] = c + i < D ? to_f32(row[c + i]) : 0.0f;
+        for (int i = 0; i < kEach; i++) {
+            r.w[i] = 0u;
+            if (f32 && c + i < D) r.w[i] = static_cast<const uint32_t *>(row)[c + i];
+            if (!f32 && c + i < D) r.w[i] = static_cast<const uint16_t *>(row)[c + i];
+        }
+    }
+    return r;
+}
+template <bool kWide>
+__device__ __forceinline__ void values8(const Raw &r, bool f32, Two (&v)[kEach / 2]) {
+#pragma unroll
+    for (int i = 0; i < kEach / 2; i++) {
+        uint32_t x = r.w[2 * i], y = r.w[2 * i + 1];
+        if (!f32) {
+            x = (kWide ? r.w[i] : x) << 16;
+            y = kWide ? r.w[i] & 0xFFFF0000u : y << 16;
+        }
+        v[i] = two(__uint_as_float(x), __uint_as_float(y));
     }
 }
 // Rounds v to the row's type, in it and in v.
-template <typename T>
-__device__ __forceinline__ void store8(T *row, int32_t c, int32_t D, bool wide, float (&v)[kEach]) {
-    union {
-        uint4 raw[kEach * sizeof(T) / 16];
-        T x[kEach];
-    } u;
+template <bool kWide>
+__device__ __forceinline__ void store8(void *row, bool f32, int32_t c, int32_t D, Two (&v)[kEach / 2]) {
+    Raw r;
 #pragma unroll
-    for (int i = 0; i < kEach; i++) {
-        u.x[i] = from_f32<T>(v[i]);
-        v[i] = to_f32(u.x[i]);
+    for (int i = 0; i < kEach / 2; i++) {
+        const float2 f = apart(v[i]);
+        r.w[2 * i] = __float_as_uint(f.x), r.w[2 * i + 1] = __float_as_uint(f.y);
+        if (!f32) {
+            const __nv_bfloat162 both = __floats2bfloat162_rn(f.x, f.y);
+            const uint32_t w = *reinterpret_cast<const uint32_t *>(&both);
+            v[i] = two(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+            if (kWide) r.w[i] = w;
+            else r.w[2 * i] = w & 0xFFFFu, r.w[2 * i + 1] = w >> 16;
+        }
     }
-    if (wide && c + kEach <= D) {
-#pragma unroll
-        for (int i = 0; i < int(kEach * sizeof(T) / 16); i++) reinterpret_cast<uint4 *>(row + c)[i] = u.raw[i];
+    if (kWide) {
+        uint4 *at = reinterpret_cast<uint4 *>(static_cast<char *>(row) + int64_t(c) * (f32 ? 4 : 2));
+        if (c < D) at[0] = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
+        if (c < D && f32) at[1] = make_uint4(r.w[4], r.w[5], r.w[6], r.w[7]);
     } else {
 #pragma unroll
         for (int i = 0; i < kEach; i++)
-            if (c + i < D) row[c + i] = u.x[i];
+            if (c + i < D) {
+                if (f32) static_cast<uint32_t *>(row)[c + i] = r.w[i];
+                else static_cast<uint16_t *>(row)[c + i] = uint16_t(r.w[i]);
+            }
     }
 }
 
-// A sum and what its roundings have left out.
+// A sum and what its roundings have left out (of additions: Knuth's two-sum).
 struct Pair {
     float sum, rest;
     __device__ __forceinline__ void add(float x) {
@@ -91,172 +130,437 @@ struct Pair {
         rest += (sum - (s - b)) + (x - b);
         sum = s;
     }
-    __device__ __forceinline__ void add_square(float x) {
-        const float p = __fmul_rn(x, x);
-        rest += __fmaf_rn(x, x, -p);
-        add(p);
-    }
 };
 
-// 1 / sqrt(mean + eps) of n values, rounded once. In doubles where the squares
-// leave the range that pairs of floats are exact in (the same way in all threads).
-__device__ __forceinline__ bool root_of(const Pair &p, float n, double eps, float *r) {
-    const float mean = __fdiv_rn(p.sum, n);
-    Pair m = {mean, __fdiv_rn(__fmaf_rn(-mean, n, p.sum) + p.rest, n)};
-    const float e = float(eps);
-    m.add(e);
-    m.rest += float(eps - double(e));
-    if (!(m.sum > 8.0779357e-28f && m.sum < 1.3292280e36f)) return false;  // 2^-90, 2^120
+// 1 / sqrt(mean + eps) of the sum of D squares, rounded once: the mean by 1 / D, which
+// is a pair too, and one Newton step. False where the squares leave the range that pairs of
+// floats are exact in (the same way in all threads).
+__device__ __forceinline__ bool root_of(const Pair &p, const NormArgs &a, float *r) {
+    const float mean = __fmul_rn(p.sum, a.per_column);
+    Pair m = {mean, __fmaf_rn(p.sum, a.per_column, -mean) + (p.sum * a.per_column_rest + p.rest * a.per_column)};
+    m.add(a.eps_32);
+    m.rest += a.eps_rest;
+    if (!(m.sum > 0x1p-90f && m.sum < 0x1p120f)) return false;
     const float r0 = rsqrtf(m.sum), s = __fmul_rn(r0, r0), s_rest = __fmaf_rn(r0, r0, -s);
     const float left = __fmaf_rn(-m.sum, s, 1.0f) - (m.sum * s_rest + m.rest * s);  // 1 - m r0^2
     *r = __fmaf_rn(0.5f * r0, left, r0);
     return true;
 }
 
-template <typename TX, bool kNorm, int kBits>
-__global__ void __launch_bounds__(kNormThreads) k_norm_quantize(const NormArgs a) {
-    __shared__ Pair pairs[kNormThreads / 32];
-    __shared__ double doubles[kNormThreads / 32];
-    __shared__ uint32_t maxima[kNormThreads / 32];
-    pdl_launch_dependents();
-    pdl_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int32_t m = blockIdx.x, D = a.D;
-    const TX *x = static_cast<const TX *>(a.x) + m * a.stride;
-    float *residual_f32 = static_cast<float *>(a.residual) + m * a.residual_stride;
-    __nv_bfloat16 *residual_bf16 = static_cast<__nv_bfloat16 *>(a.residual) + m * a.residual_stride;
-    const int32_t end = kBits == 8 ? (D + 127) / 128 * 128 : (D + 63) / 64 * 64;
-    float r = 0.0f;
-
-    // h of eight columns, the first time and again
-    auto first = [&](int32_t c, float (&h)[kEach]) {
-        load8(x, c, D, a.wide_x, h);
-        if (!kNorm || !a.residual) return;
-        float v[kEach];
-        if (a.residual_f32) load8(residual_f32, c, D, a.wide_residual, v);
-        else load8(residual_bf16, c, D, a.wide_residual, v);
+// The sum of squares of a thread's numbers, two at a time: Pair::add of two
+// squares, and what their own rounding left out, which of bf16 numbers (kShort) is
+// nothing. Differences are multiply-adds with -1: one instruction for two numbers, a
+// subtraction is three.
+template <bool kShort>
+struct Squares {
+    Two sum = 0, rest = 0;
+    __device__ __forceinline__ void add(const Two (&h)[kEach / 2]) {
+        const Two minus = two(-1.0f, -1.0f);
 #pragma unroll
-        for (int i = 0; i < kEach; i++) h[i] = __fadd_rn(h[i], v[i]);
-        if (a.residual_f32) store8(residual_f32, c, D, a.wide_residual, h);
-        else store8(residual_bf16, c, D, a.wide_residual, h);
-    };
-    auto again = [&](int32_t c, float (&h)[kEach]) {
-        if (!kNorm || !a.residual) load8(x, c, D, a.wide_x, h);
-        else if (a.residual_f32) load8(residual_f32, c, D, a.wide_residual, h);
-        else load8(residual_bf16, c, D, a.wide_residual, h);
-    };
-    auto norm = [&](int32_t c, float (&h)[kEach]) {
-        if (!kNorm) return;
-        float g[kEach];
-        if (a.gain_f32) load8(static_cast<const float *>(a.gain), c, D, a.wide_gain, g);
-        else load8(static_cast<const __nv_bfloat16 *>(a.gain), c, D, a.wide_gain, g);
-#pragma unroll
-        for (int i = 0; i < kEach; i++) h[i] = c + i < D ? __fmul_rn(__fmul_rn(h[i], r), g[i]) : 0.0f;
-    };
-
-    if (kNorm) {
-        Pair p = {0.0f, 0.0f};
-        for (int32_t c = int32_t(threadIdx.x) * kEach; c < D; c += kNormThreads * kEach) {
-            float h[kEach];
-            first(c, h);
-#pragma unroll
-            for (int i = 0; i < kEach; i++) p.add_square(h[i]);
-        }
-#pragma unroll
-        for (int d = 16; d; d >>= 1) {
-            const float s = __shfl_xor_sync(~0u, p.sum, d), rest = __shfl_xor_sync(~0u, p.rest, d);
-            p.add(s);
-            p.rest += rest;
-        }
-        if (lane == 0) pairs[warp] = p;
-        __syncthreads();
-        Pair all = pairs[0];
-        for (int i = 1; i < kNormThreads / 32; i++) {
-            all.add(pairs[i].sum);
-            all.rest += pairs[i].rest;
-        }
-        if (!root_of(all, float(D), a.eps, &r)) {
-            double s = 0.0;
-            for (int32_t c = int32_t(threadIdx.x) * kEach; c < D; c += kNormThreads * kEach) {
-                float h[kEach];
-                again(c, h);
-                for (int i = 0; i < kEach; i++) s += double(h[i]) * h[i];
+        for (int i = 0; i < kEach / 2; i++) {
+            if (kShort) {
+                const Two p = mul2(h[i], h[i]), s = add2(sum, p), b = fma2(s, minus, sum);  // b: minus what sum grew by
+                rest = add2(rest, add2(fma2(add2(s, b), minus, sum), add2(p, b)));
+                sum = s;
+            } else {
+                const Two p = mul2(mul2(h[i], minus), h[i]);  // minus the square
+                const Two s = fma2(p, minus, sum), b = fma2(s, minus, sum), left = fma2(h[i], h[i], p);
+                rest = add2(rest, add2(add2(fma2(add2(s, b), minus, sum), fma2(p, minus, b)), left));
+                sum = s;
             }
-            for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
-            if (lane == 0) doubles[warp] = s;
-            __syncthreads();
-            s = doubles[0];
-            for (int i = 1; i < kNormThreads / 32; i++) s += doubles[i];
-            r = float(1.0 / sqrt(s / D + a.eps));
         }
     }
+    __device__ __forceinline__ Pair pair() const {
+        const float2 s = apart(sum), left = apart(rest);
+        Pair p = {s.x, left.x + left.y};
+        p.add(s.y);
+        return p;
+    }
+};
+__device__ __forceinline__ double squares_of(const Two (&h)[kEach / 2]) {
+    double s = 0.0;
+    for (int i = 0; i < kEach / 2; i++) {
+        const float2 f = apart(h[i]);
+        s += double(f.x) * f.x + double(f.y) * f.y;
+    }
+    return s;
+}
+// The largest magnitude's bits: NaN above infinity above numbers.
+__device__ __forceinline__ uint32_t largest_of(const Two (&y)[kEach / 2]) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < kEach / 2; i++) most = max(most, max(uint32_t(y[i]) & 0x7FFFFFFFu, uint32_t(y[i] >> 32) & 0x7FFFFFFFu));
+    return most;
+}
 
-    if (kBits == 8) {
-        for (int32_t c = int32_t(threadIdx.x) * kEach; c - lane * kEach < end; c += kNormThreads * kEach) {
-            float y[kEach], amax = 0.0f;
-            again(c, y);
-            norm(c, y);
+__device__ __forceinline__ Pair warp_sum(Pair p, int lanes) {
+    for (int d = lanes / 2; d; d >>= 1) {
+        const float s = __shfl_xor_sync(~0u, p.sum, d), rest = __shfl_xor_sync(~0u, p.rest, d);
+        p.add(s);
+        p.rest += rest;
+    }
+    return p;
+}
+// root_of all threads' sums, in all of them: below 0 where it is false. By one warp, as
+// in all of them it would be half of the kernel's instructions.
+struct RootSpace {
+    Pair pairs[32];
+    float root;
+};
+__device__ __forceinline__ float block_root(const Pair &mine, const NormArgs &a, RootSpace &space) {
+    const int lane = threadIdx.x & 31;
+    Pair p = mine;
 #pragma unroll
-            for (int i = 0; i < kEach; i++) amax = fmaxf(amax, fabsf(y[i]));
+    for (int d = 16; d; d >>= 1) {
+        const float s = __shfl_xor_sync(~0u, p.sum, d), rest = __shfl_xor_sync(~0u, p.rest, d);
+        p.add(s);
+        p.rest += rest;
+    }
+    if (lane == 0) space.pairs[threadIdx.x >> 5] = p;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        const int warps = int(blockDim.x) >> 5;
+        p = {0.0f, 0.0f};
+        if (lane < warps) p = space.pairs[lane];
+        float r = -1.0f;
+        const bool ok = root_of(warp_sum(p, warps <= 8 ? 8 : 32), a, &r);  // lane 0's is of all
+        if (lane == 0) space.root = ok ? r : -1.0f;
+    }
+    __syncthreads();
+    return space.root;
+}
+__device__ __forceinline__ double block_sum(double s, double *doubles) {
+    for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
+    if ((threadIdx.x & 31) == 0) doubles[threadIdx.x >> 5] = s;
+    __syncthreads();
+    s = doubles[0];
+    for (int i = 1; i < int(blockDim.x) >> 5; i++) s += doubles[i];
+    return s;
+}
+__device__ __forceinline__ uint32_t block_max(uint32_t m, uint32_t *maxima) {
+    const int lane = threadIdx.x & 31;
+    m = __reduce_max_sync(~0u, m);
+    if (lane == 0) maxima[threadIdx.x >> 5] = m;
+    __syncthreads();
+    return __reduce_max_sync(~0u, lane < int(blockDim.x) >> 5 ? maxima[lane] : 0u);
+}
+
+// x / s for two numbers, each rounded once: with r = 1 / s rounded once, q = x r is
+// off by a unit of its last place at most, x - q s is a number of 32 bits, and q + (x - q s) r
+// rounds as x / s does (Markstein's theorem), as long as nothing leaves the range. The sign of
+// a 0 is put back.
+__device__ __forceinline__ Two divide2(Two x, Two minus_s, Two r) {
+    const Two q = mul2(x, r);
+    return fma2(fma2(q, minus_s, x), r, q) | (x & 0x8000000080000000ull);
+}
+
+// Eight columns from c on of y as e4m3, with the scale of their block of 128: all
+// of 16 threads' columns.
+__device__ __forceinline__ void put8(const NormArgs &a, int32_t m, int32_t c, const Two (&y)[kEach / 2]) {
+    float v[kEach], amax = 0.0f;
 #pragma unroll
-            for (int d = 8; d; d >>= 1) amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, d));
-            const float s = scale_of(amax);
-            uint32_t out[2] = {0u, 0u};
+    for (int i = 0; i < kEach / 2; i++) {
+        const float2 f = apart(y[i]);
+        v[2 * i] = f.x, v[2 * i + 1] = f.y;
+        amax = fmaxf(amax, fmaxf(fabsf(f.x), fabsf(f.y)));
+    }
 #pragma unroll
-            for (int i = 0; i < kEach; i++) out[i / 4] |= uint32_t(to_e4m3(__fdiv_rn(y[i], s))) << (i % 4 * 8);
-            uint8_t *q = a.q + int64_t(m) * D + c;
-            if (a.wide_q && c + kEach <= D) {
-                *reinterpret_cast<uint2 *>(q) = make_uint2(out[0], out[1]);
-            } else {
+    for (int d = 8; d; d >>= 1) amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, d));
+    const float s = scale_of(amax);
+    if (s > 0x1p-60f && s < 0x1p60f) {
+        const float r = __frcp_rn(s);
 #pragma unroll
-                for (int i = 0; i < kEach; i++)
-                    if (c + i < D) q[i] = uint8_t(out[i / 4] >> (i % 4 * 8));
-            }
-            if ((lane & 15) == 0 && c < end) a.scales[int64_t(c / kBlock) * a.pitch + m] = s;
+        for (int i = 0; i < kEach / 2; i++) {
+            const float2 f = apart(divide2(y[i], two(-s, -s), two(r, r)));
+            v[2 * i] = f.x, v[2 * i + 1] = f.y;
         }
     } else {
-        uint32_t most = 0;  // of the magnitudes' bits: NaN above infinity above numbers
-        for (int32_t c = int32_t(threadIdx.x) * kEach; c < D; c += kNormThreads * kEach) {
-            float y[kEach];
-            again(c, y);
-            norm(c, y);
 #pragma unroll
-            for (int i = 0; i < kEach; i++) most = max(most, __float_as_uint(y[i]) & 0x7FFFFFFFu);
+        for (int i = 0; i < kEach; i++) v[i] = __fdiv_rn(v[i], s);
+    }
+    uint32_t out[2];
+#pragma unroll
+    for (int i = 0; i < 2; i++)
+        out[i] = uint32_t(__nv_cvt_float2_to_fp8x2(make_float2(v[4 * i], v[4 * i + 1]), __NV_SATFINITE, __NV_E4M3)) |
+                 uint32_t(__nv_cvt_float2_to_fp8x2(make_float2(v[4 * i + 2], v[4 * i + 3]), __NV_SATFINITE, __NV_E4M3)) << 16;
+    uint8_t *q = a.q + int64_t(m) * a.D + c;
+    if (a.wide_q && c + kEach <= a.D) {
+        *reinterpret_cast<uint2 *>(q) = make_uint2(out[0], out[1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kEach; i++)
+            if (c + i < a.D) q[i] = uint8_t(out[i / 4] >> (i % 4 * 8));
+    }
+    if ((threadIdx.x & 15) == 0 && c < a.D) a.scales[int64_t(c / kBlock) * a.pitch + m] = s;
+}
+// The same as e2m1; a block of 16 is two threads', a word of scales eight threads'.
+__device__ __forceinline__ void put4(const NormArgs &a, int32_t m, int32_t c, const Two (&y)[kEach / 2], float row_scale, float per_row) {
+    const int lane = threadIdx.x & 31;
+    float amax = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kEach / 2; i++) {
+        const float2 f = apart(y[i]);
+        amax = fmaxf(amax, fmaxf(fabsf(f.x), fabsf(f.y)));
+    }
+    amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 1));
+    const float t = row_scale > 0x1p-60f && row_scale < 0x1p60f ? apart(divide2(two(amax, 0.0f), two(-row_scale, -row_scale), two(per_row, per_row))).x
+                                                                : __fdiv_rn(amax, row_scale);
+    const uint8_t s = to_e4m3(__fmul_rn(t, 1.0f / 6.0f));
+    const float per = per_step4(s, row_scale);
+    uint32_t out = 0;
+#pragma unroll
+    for (int i = 0; i < kEach / 2; i++) {
+        const float2 f = apart(mul2(y[i], two(per, per)));
+        out |= uint32_t(to_e2m1x2(f.x, f.y)) << (8 * i);
+    }
+    if (c < row_bytes4(a.D) * 2) *reinterpret_cast<uint32_t *>(a.q + m * row_bytes4(a.D) + c / 2) = out;
+    uint32_t word = uint32_t(s) << (8 * ((lane >> 1) & 3));
+    word |= __shfl_xor_sync(~0u, word, 2);
+    word |= __shfl_xor_sync(~0u, word, 4);
+    const int64_t tiles = scale_tiles4(a.D);
+    if ((lane & 7) == 0 && c < tiles * 64) *reinterpret_cast<uint32_t *>(a.scales4 + scale_word4(m, c / 64, tiles)) = word;
+}
+
+// Rows of any length and alignment, a CTA a row: read again in each pass (the
+// residual as it was written).
+template <bool kWide, bool kNorm, int kBits>
+__global__ void __launch_bounds__(kNormThreads) k_norm_long(const __grid_constant__ NormArgs a) {
+    __shared__ RootSpace space;
+    __shared__ double doubles[32];
+    __shared__ uint32_t maxima[32];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int lane = threadIdx.x & 31;
+    const int32_t m = blockIdx.x, D = a.D, mine = int32_t(threadIdx.x) * kEach;
+    constexpr int32_t kStride = kNormThreads * kEach;
+    const void *x = static_cast<const char *>(a.x) + m * a.stride * (a.x_f32 ? 4 : 2);
+    void *residual = static_cast<char *>(a.residual) + m * a.residual_stride * (a.residual_f32 ? 4 : 2);
+    const bool has_residual = kNorm && a.residual;
+    float r = 0.0f;
+
+    auto again = [&](int32_t c, Two (&h)[kEach / 2]) {
+        const bool f32 = has_residual ? a.residual_f32 : a.x_f32;
+        values8<kWide>(load8<kWide>(has_residual ? residual : x, f32, c, D), f32, h);
+    };
+    auto normed = [&](int32_t c, Two (&h)[kEach / 2]) {
+        again(c, h);
+        if (!kNorm) return;
+        Two g[kEach / 2];
+        values8<kWide>(load8<kWide>(a.gain, a.gain_f32, c, D), a.gain_f32, g);
+#pragma unroll
+        for (int i = 0; i < kEach / 2; i++) {
+            h[i] = mul2(mul2(h[i], two(r, r)), g[i]);
+            const float2 f = apart(h[i]);  // 0 behind the end, whatever r is
+            h[i] = two(c + 2 * i < D ? f.x : 0.0f, c + 2 * i + 1 < D ? f.y : 0.0f);
         }
-        most = __reduce_max_sync(~0u, most);
-        if (lane == 0) maxima[warp] = most;
-        __syncthreads();
-        for (int i = 0; i < kNormThreads / 32; i++) most = max(most, maxima[i]);
-        const float row_scale = row_scale4(most);
+    };
+    if (kNorm) {
+        Squares<false> all;
+        for (int32_t c = mine; c < D; c += kStride) {
+            Two h[kEach / 2];
+            values8<kWide>(load8<kWide>(x, a.x_f32, c, D), a.x_f32, h);
+            if (has_residual) {
+                Two v[kEach / 2];
+                values8<kWide>(load8<kWide>(residual, a.residual_f32, c, D), a.residual_f32, v);
+#pragma unroll
+                for (int i = 0; i < kEach / 2; i++) h[i] = add2(h[i], v[i]);
+                store8<kWide>(residual, a.residual_f32, c, D, h);
+            }
+            all.add(h);
+        }
+        r = block_root(all.pair(), a, space);
+        if (r < 0.0f) {
+            double wide = 0.0;
+            for (int32_t c = mine; c < D; c += kStride) {
+                Two h[kEach / 2];
+                again(c, h);
+                wide += squares_of(h);
+            }
+            r = float(1.0 / sqrt(block_sum(wide, doubles) / D + a.eps));
+        }
+    }
+    float row_scale = 0.0f, per_row = 0.0f;  // and its reciprocal
+    if (kBits == 4) {
+        uint32_t most = 0;
+        for (int32_t c = mine; c < D; c += kStride) {
+            Two y[kEach / 2];
+            normed(c, y);
+            most = max(most, largest_of(y));
+        }
+        row_scale = row_scale4(block_max(most, maxima));
+        per_row = __frcp_rn(row_scale);
         if (threadIdx.x == 0) a.row_scales[m] = row_scale;
-        const int64_t tiles = scale_tiles4(D);
-        for (int32_t c = int32_t(threadIdx.x) * kEach; c - lane * kEach < end; c += kNormThreads * kEach) {
-            float y[kEach], amax = 0.0f;
-            again(c, y);
-            norm(c, y);
+    }
+    for (int32_t c = mine; c - lane * kEach < (D + 127) / 128 * 128; c += kStride) {
+        Two y[kEach / 2];
+        normed(c, y);
+        if (kBits == 8) put8(a, m, c, y);
+        else put4(a, m, c, y, row_scale, per_row);
+    }
+}
+
+// 16 bytes to shared memory, zeros where `there` is false; asynchronous.
+__device__ __forceinline__ void copy16(uint32_t to, const void *from, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
+
+struct None {};
+template <typename T>
+constexpr int kPieces = std::is_same<T, None>::value ? 0 : int(sizeof(T)) / 2;  // 16-byte pieces of eight columns
+
+// Aligned rows of whole eights of columns that kSteps steps of a CTA's threads
+// hold: CTAs stay and go over the rows, and copy the next row's columns to shared
+// memory while they look at this one's. A thread copies and reads its own columns
+// only. TR: the residual's type, or None.
+template <typename TX, typename TR, bool kNorm, int kBits, int kSteps>
+__global__ void __launch_bounds__(kSteps == 1 ? kMaxThreads : kSteps == 2 ? kHoldThreads : 256, kSteps == 2 ? 2 : kSteps == 4 ? 3 : 1) k_norm_rows(const __grid_constant__ NormArgs a) {
+    constexpr bool kResidual = !std::is_same<TR, None>::value;
+    using R = typename std::conditional<kResidual, TR, float>::type;
+    constexpr int kX = kPieces<TX>, kEachStep = kX + kPieces<TR>;
+    extern __shared__ __align__(16) uint4 space[];  // [a.buffers][kSteps][kEachStep][threads], then the gain as [kSteps][4][threads] pairs
+    __shared__ RootSpace roots[2];
+    __shared__ double doubles[32];
+    __shared__ uint32_t maxima[2][32];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int lane = threadIdx.x & 31, threads = blockDim.x;
+    const int32_t D = a.D, stride = threads * kEach, mine = int32_t(threadIdx.x) * kEach;
+    uint4 *const own = space + threadIdx.x;
+    Two *const gains = reinterpret_cast<Two *>(space + a.buffers * kSteps * kEachStep * threads) + threadIdx.x;
+    const TX *x = static_cast<const TX *>(a.x) + blockIdx.x * a.stride + mine;
+    R *residual = static_cast<R *>(a.residual) + blockIdx.x * a.residual_stride + mine;
+    const int64_t x_step = int64_t(gridDim.x) * a.stride, residual_step = int64_t(gridDim.x) * a.residual_stride;
+    auto ask = [&](int turn, const TX *from, const R *from_residual) {
 #pragma unroll
-            for (int i = 0; i < kEach; i++) amax = fmaxf(amax, fabsf(y[i]));
-            amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 1));
-            const uint8_t s = block_scale4(amax, row_scale);
-            const float per = per_step4(s, row_scale);
-            uint32_t out = 0;
+        for (int i = 0; i < kSteps; i++) {
+            const bool there = mine + i * stride < D;
 #pragma unroll
-            for (int i = 0; i < kEach; i += 2)
-                out |= uint32_t(to_e2m1x2(__fmul_rn(y[i], per), __fmul_rn(y[i + 1], per))) << (4 * i);
-            if (c < row_bytes4(D) * 2) *reinterpret_cast<uint32_t *>(a.q + m * row_bytes4(D) + c / 2) = out;
-            uint32_t word = uint32_t(s) << (8 * ((lane >> 1) & 3));
-            word |= __shfl_xor_sync(~0u, word, 2);
-            word |= __shfl_xor_sync(~0u, word, 4);
-            if ((lane & 7) == 0 && c < end) *reinterpret_cast<uint32_t *>(a.scales4 + scale_word4(m, c / 64, tiles)) = word;
+            for (int k = 0; k < kEachStep; k++) {
+                const void *at = k < kX ? static_cast<const void *>(reinterpret_cast<const uint4 *>(from + (there ? i * stride : 0)) + k)
+                                        : static_cast<const void *>(reinterpret_cast<const uint4 *>(from_residual + (there ? i * stride : 0)) + k - kX);
+                copy16(smem_addr(own + ((turn * kSteps + i) * kEachStep + k) * threads), at, there);
+            }
+        }
+    };
+    auto values = [&](int turn, int i, int k0, bool f32, Two (&v)[kEach / 2]) {
+        const uint4 lo = own[((turn * kSteps + i) * kEachStep + k0) * threads];
+        const uint4 hi = f32 ? own[((turn * kSteps + i) * kEachStep + k0 + 1) * threads] : lo;
+        values8<true>(Raw{{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w}}, f32, v);
+    };
+    ask(0, x, residual);
+    copies_commit();
+    if (kNorm) {
+#pragma unroll
+        for (int i = 0; i < kSteps; i++) {
+            Two g[kEach / 2];
+            values8<true>(load8<true>(a.gain, a.gain_f32, mine + i * stride, D), a.gain_f32, g);
+#pragma unroll
+            for (int k = 0; k < kEach / 2; k++) gains[(i * (kEach / 2) + k) * threads] = g[k];
+        }
+    }
+    int turn = 0;
+    for (int32_t m = blockIdx.x; m < a.M; m += gridDim.x, turn ^= 1) {
+        x += x_step;
+        if (kResidual) residual += residual_step;
+        if (m + int32_t(gridDim.x) < a.M) ask(turn ^ 1, x, residual);
+        copies_commit();
+        copies_wait<1>();
+        Two held[kSteps][kEach / 2];
+#pragma unroll
+        for (int i = 0; i < kSteps; i++) {
+            values(turn, i, 0, kX == 2, held[i]);
+            if (kResidual) {
+                Two v[kEach / 2];
+                values(turn, i, kX, sizeof(R) == 4, v);
+#pragma unroll
+                for (int k = 0; k < kEach / 2; k++) held[i][k] = add2(held[i][k], v[k]);
+                store8<true>(residual - residual_step - mine, sizeof(R) == 4, mine + i * stride, D, held[i]);
+            }
+        }
+        if (kNorm) {
+            Squares<(kResidual ? sizeof(R) : sizeof(TX)) == 2> all;
+#pragma unroll
+            for (int i = 0; i < kSteps; i++) all.add(held[i]);
+            float r = block_root(all.pair(), a, roots[turn]);
+            if (r < 0.0f) {
+                double wide = 0.0;
+                for (int i = 0; i < kSteps; i++) wide += squares_of(held[i]);
+                __syncthreads();  // the row before may still be reading
+                r = float(1.0 / sqrt(block_sum(wide, doubles) / D + a.eps));
+            }
+            const Two rr = two(r, r);  // behind the end both factors are 0 (and where r is a NaN the row is)
+#pragma unroll
+            for (int i = 0; i < kSteps; i++)
+#pragma unroll
+                for (int k = 0; k < kEach / 2; k++) held[i][k] = mul2(mul2(held[i][k], rr), gains[(i * (kEach / 2) + k) * threads]);
+        }
+        float row_scale = 0.0f, per_row = 0.0f;  // and its reciprocal
+        if (kBits == 4) {
+            uint32_t most = 0;
+#pragma unroll
+            for (int i = 0; i < kSteps; i++) most = max(most, largest_of(held[i]));
+            row_scale = row_scale4(block_max(most, maxima[turn]));
+            per_row = __frcp_rn(row_scale);
+            if (threadIdx.x == 0) a.row_scales[m] = row_scale;
+        }
+#pragma unroll
+        for (int i = 0; i < kSteps; i++) {
+            const int32_t c = mine + i * stride;
+            if (c - lane * kEach >= (D + 127) / 128 * 128) break;  // the warp has nothing there
+            if (kBits == 8) put8(a, m, c, held[i]);
+            else put4(a, m, c, held[i], row_scale, per_row);
         }
     }
 }
 
+template <typename TX, typename TR, bool kNorm, int kBits, int kSteps>
+cudaError_t launch_held(NormArgs a, int threads, cudaStream_t st) {
+    auto space = [&](int buffers) {
+        return size_t(threads) * kSteps * (buffers * (kPieces<TX> + kPieces<TR>) * sizeof(uint4) + (kNorm ? kEach * sizeof(float) : 0));
+    };
+    // CTAs that stay, as many as fit an SM by threads (64 registers each; 80 with four
+    // steps) and shared memory; where they would take few rows each, a CTA a row.
+    const int fit = std::max(1, std::min((kSteps == 4 ? 768 : 1024) / threads, int(kMostSpace / (space(2) + 2048))));
+    const int64_t stay = int64_t(sm_count()) * fit;
+    a.buffers = a.M > kStayRows * stay ? 2 : 1;
+    const size_t smem = space(a.buffers);
+    auto kernel = k_norm_rows<TX, TR, kNorm, kBits, kSteps>;
+    if (smem > kMostSpace) return launch_pdl(k_norm_long<true, kNorm, kBits>, a.M, kNormThreads, st, a);
+    if (smem > 40 * 1024) {  // what is declared in the kernel counts towards the 48 KB that need no attribute
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+        if (e != cudaSuccess) return e;
+    }
+    return launch_pdl_smem(kernel, a.buffers == 2 ? stay : int64_t(a.M), threads, smem, st, a);
+}
+
+template <typename TX, typename TR, bool kNorm, int kBits>
+cudaError_t launch_rows(const NormArgs &a, cudaStream_t st) {
+    // Few rows: a step a thread, as many threads as that takes, for the shortest chain. Else
+    // two or four, so that what a warp does for a row is shared by more of its columns.
+    const int32_t eights = int32_t((int64_t(a.D) + 63) / 64 * 64 / kEach);
+    const int steps = eights <= (a.M <= 2 * sm_count() ? kMaxThreads : 64) ? 1 : eights <= 2 * kHoldThreads ? 2 : 4;
+    const int threads = ((eights + steps - 1) / steps + 31) / 32 * 32;
+    if (steps == 1) return launch_held<TX, TR, kNorm, kBits, 1>(a, threads, st);
+    if (steps == 2) return launch_held<TX, TR, kNorm, kBits, 2>(a, threads, st);
+    if (threads <= kNormThreads) return launch_held<TX, TR, kNorm, kBits, 4>(a, threads, st);
+    return launch_pdl(k_norm_long<true, kNorm, kBits>, a.M, kNormThreads, st, a);
+}
+
+template <typename TX, bool kNorm, int kBits>
+cudaError_t launch_typed(const NormArgs &a, cudaStream_t st) {
+    if constexpr (kNorm) {
+        if (a.residual) return a.residual_f32 ? launch_rows<TX, float, kNorm, kBits>(a, st) : launch_rows<TX, __nv_bfloat16, kNorm, kBits>(a, st);
+    }
+    return launch_rows<TX, None, kNorm, kBits>(a, st);
+}
+
 template <bool kNorm, int kBits>
-int launch_norm(const NormArgs &a, int dtype, cudaStream_t st) {
-    const cudaError_t e = dtype == TRIE_DTYPE_F32
-        ? launch_pdl(k_norm_quantize<float, kNorm, kBits>, a.M, kNormThreads, st, a)
-        : launch_pdl(k_norm_quantize<__nv_bfloat16, kNorm, kBits>, a.M, kNormThreads, st, a);
+int launch_norm(const NormArgs &a, cudaStream_t st) {
+    const cudaError_t e = !a.wide ? launch_pdl(k_norm_long<false, kNorm, kBits>, a.M, kNormThreads, st, a)
+                          : a.x_f32 ? launch_typed<float, kNorm, kBits>(a, st) : launch_typed<__nv_bfloat16, kNorm, kBits>(a, st);
     return e == cudaSuccess ? TRIE_OK : fail_launch(e, "norm quantize launch");
 }
 
@@ -305,10 +609,14 @@ NormArgs make_norm(const void *x, int dtype, int64_t stride, int32_t M, int32_t 
     a.gain = gain;
     a.residual_f32 = residual_dtype == TRIE_DTYPE_F32;
     a.gain_f32 = gain_dtype == TRIE_DTYPE_F32;
-    a.wide_x = wide_rows(x, dtype, stride, M);
-    a.wide_residual = residual && wide_rows(residual, residual_dtype, residual_stride, M);
-    a.wide_gain = gain && wide_rows(gain, gain_dtype, 0, 1);
+    a.x_f32 = dtype == TRIE_DTYPE_F32;
+    a.wide = D % 8 == 0 && wide_rows(x, dtype, stride, M) && (!residual || wide_rows(residual, residual_dtype, residual_stride, M)) &&
+             (!gain || wide_rows(gain, gain_dtype, 0, 1));
     a.eps = eps;
+    a.eps_32 = float(eps);
+    a.eps_rest = float(eps - double(a.eps_32));
+    a.per_column = 1.0f / float(D);
+    a.per_column_rest = float(1.0 / D - double(a.per_column));
     return a;
 }
 
@@ -331,7 +639,7 @@ extern "C" int trie_head_norm_quantize(const void *d_x, int dtype, int64_t strid
     a.wide_q = !off_boundary(8, d_q) && D % 8 == 0;
     a.scales = d_scales;
     a.pitch = pitch;
-    return launch_norm<true, 8>(a, dtype, stream);
+    return launch_norm<true, 8>(a, stream);
 }
 
 extern "C" int64_t trie_head4_row_bytes(int32_t D) { return D < 1 || D > (1 << 24) ? -1 : tmk::row_bytes4(D); }
@@ -352,7 +660,7 @@ extern "C" int trie_head4_quantize(const void *d_x, int dtype, int64_t stride, i
     a.q = d_q;
     a.scales4 = d_scales;
     a.row_scales = d_row_scales;
-    return launch_norm<false, 4>(a, dtype, stream);
+    return launch_norm<false, 4>(a, stream);
 }
 
 extern "C" int trie_head4_norm_quantize(const void *d_x, int dtype, int64_t stride, void *d_residual, int residual_dtype,
@@ -368,5 +676,5 @@ extern "C" int trie_head4_norm_quantize(const void *d_x, int dtype, int64_t stri
     a.q = d_q;
     a.scales4 = d_scales;
     a.row_scales = d_row_scales;
-    return launch_norm<true, 4>(a, dtype, stream);
+    return launch_norm<true, 4>(a, stream);
 }

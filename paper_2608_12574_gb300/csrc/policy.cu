@@ -17,6 +17,7 @@
 
 #include "blackwell.cuh"
 #include "logits.cuh"
+#include "two.cuh"
 
 namespace tmk {
 
@@ -76,28 +77,6 @@ __device__ __forceinline__ Mass warp_mass(const Mass &mine, float c) {
     return all;
 }
 
-// Two numbers at a time.
-using Two = unsigned long long;
-__device__ __forceinline__ Two two(float x, float y) {
-    Two r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
-    return r;
-}
-__device__ __forceinline__ float2 apart(Two x) {
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
-    return r;
-}
-__device__ __forceinline__ Two add2(Two x, Two y) {
-    Two r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
-    return r;
-}
-__device__ __forceinline__ Two mul2(Two x, Two y) {
-    Two r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
-    return r;
-}
 // exp2((x - top) c), with -top twice and c twice.
 __device__ __forceinline__ Two exp2_of(Two x, Two minus_top, Two c) {
     const float2 y = apart(mul2(add2(x, minus_top), c));

@@ -39,9 +39,6 @@ __device__ __forceinline__ float row_scale4(uint32_t amax_bits) {
     if (amax_bits >= 0x7F800000u) return __int_as_float(0x7FC00000);
     return fmaxf(__fmul_rn(__uint_as_float(amax_bits), kPerMax4), kTinyRow4);
 }
-__device__ __forceinline__ uint8_t block_scale4(float amax, float row_scale) {
-    return to_e4m3(__fmul_rn(__fdiv_rn(amax, row_scale), 1.0f / 6.0f));
-}
 __device__ __forceinline__ float from_e4m3(uint8_t x) {
     return __half2float(__half(__nv_cvt_fp8_to_halfraw(__nv_fp8_storage_t(x), __NV_E4M3)));
 }
