@@ -148,6 +148,7 @@ __global__ void __launch_bounds__(kQuantThreads) k_head_quantize_weight(const T 
 // so that the next tile's weights arrive while this one's logits are written.
 // Rows that a batch does not have are not loaded (the MMA multiplies what lies
 // there into rows nobody reads).
+constexpr int kTurn = 32 * 17;     // words of a warp's block of 16 tokens, turned
 constexpr int kScaleSlots = 8;     // of two blocks' scales: more blocks than can be between the copies and the epilogue
 
 struct HeadArgs : HeadOut {
@@ -215,6 +216,47 @@ __device__ __forceinline__ float few_part(const HeadArgs &a, int32_t v, const un
 }
 __device__ __forceinline__ float few_logit(const HeadArgs &, int32_t, int32_t, float sum) { return sum; }
 
+// 16 tokens from v on of a warp's 32 rows from m on (of which `rows` are there, and
+// with kSome those whose bit of `some` is set), a row a thread. Where every row is
+// on a 32-byte boundary a thread writes its own 32 bytes at a time; else the block
+// is turned in shared memory, so that lanes write consecutive tokens (256 aligned
+// rows: 148 and 159 us, 64: 93 and 101). One test more for each store, in kSome
+// only, costs 64 unaligned rows 6 us of 101.
+template <typename T, bool kSome>
+__device__ __forceinline__ void store16(const HeadOut &a, float *turn, const float *x, int32_t m, int32_t rows, uint32_t some,
+                                        int32_t v, int lane, bool wide) {
+    T *out = static_cast<T *>(a.logits) + m * a.stride + v;
+    if (wide && v + 16 <= a.V) {
+        if (lane >= rows || (kSome && !((some >> lane) & 1u))) return;
+        T *mine = out + lane * a.stride;
+        uint32_t r[8];
+        if (sizeof(T) == 2) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const __nv_bfloat162 both = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+                r[i] = *reinterpret_cast<const uint32_t *>(&both);
+            }
+            store32(mine, r);
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+#pragma unroll
+                for (int i = 0; i < 8; i++) r[i] = __float_as_uint(x[8 * h + i]);
+                store32(mine + 8 * h, r);
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; i++) turn[lane * 17 + i] = x[i];
+    __syncwarp();
+    const int c = lane & 15;
+    if (v + c < a.V)
+        for (int r = lane >> 4; r < rows; r += 2)
+            if (!kSome || ((some >> r) & 1u)) out[r * a.stride + c] = from_f32<T>(turn[r * 17 + c]);
+    __syncwarp();
+}
+
 // Epilogue warps: four quarters of the rows, two or four columns of tokens.
 template <bool kPair>
 constexpr int kEpilogueWarps = kPair ? 16 : 8;
@@ -236,7 +278,7 @@ __global__ void __launch_bounds__(kHeadThreads<kPair>, 1) k_head_logits(const __
     extern __shared__ unsigned char dynamic_smem[];
     __shared__ uint64_t bars[2 * kMaxStages + 2 * kAccumulators + 2 * kScaleSlots];
     __shared__ __align__(16) float scales[kScaleSlots][2][kRows];
-    __shared__ float turn[kEpilogue][kTurn<float, 16>];
+    __shared__ float turn[kEpilogue][kTurn];
     __shared__ uint32_t need[kNeedTiles / 32];
     __shared__ uint32_t tmem_base;
     __shared__ int gave_up;
@@ -366,8 +408,8 @@ __global__ void __launch_bounds__(kHeadThreads<kPair>, 1) k_head_logits(const __
                     }
                 }
                 if (v + c >= a.V) continue;
-                if (some == ~0u) store16<T, false, float, 16>(a, turn[warp - kFirst], sum + c, mine, rows, some, v + c, lane, wide);
-                else store16<T, true, float, 16>(a, turn[warp - kFirst], sum + c, mine, rows, some, v + c, lane, wide);
+                if (some == ~0u) store16<T, false>(a, turn[warp - kFirst], sum + c, mine, rows, some, v + c, lane, wide);
+                else store16<T, true>(a, turn[warp - kFirst], sum + c, mine, rows, some, v + c, lane, wide);
             }
         }
     } else {
@@ -472,7 +514,7 @@ cudaError_t launch_head(HeadArgs a, cudaStream_t st) {
     const int stage = 128 * kBlock + a.box_rows * kBlock;
     // the last stage's MMA reads kRows rows, whatever was loaded; and room to align the ring
     const int beyond = (kRows - a.box_rows) * kBlock + 1024;
-    const int fixed = int(sizeof(float)) * (kEpilogueWarps<kPair> * kTurn<float, 16> + kScaleSlots * 2 * kRows) + 1024;  // declared in the kernel
+    const int fixed = int(sizeof(float)) * (kEpilogueWarps<kPair> * kTurn + kScaleSlots * 2 * kRows) + 1024;  // declared in the kernel
     a.stages = std::min(kMaxStages, (kHeadSmem - fixed - beyond) / stage);
     const int smem = a.stages * stage + beyond;
     const cudaError_t e = cudaFuncSetAttribute(k_head_logits<T, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadSmem - fixed);

@@ -49,9 +49,8 @@ template <bool kPair>
 constexpr int kFirstWarp4 = kPair ? 4 : 2;
 template <bool kPair>
 constexpr int kThreads4 = 32 * (kFirstWarp4<kPair> + kEpilogueWarps4<kPair>);
-// A warp's block of tokens, turned: 32 bytes of a row at a time.
-template <typename T>
-constexpr int kTurnTokens = 32 / int(sizeof(T));
+// Words of a warp's turned block: 32 rows of 32 words (32 tokens in 32 bits, 64 in bf16), an odd number apart.
+constexpr int kTurnPitch = 33, kTurnWords = 32 * kTurnPitch;
 
 struct Head4Args : HeadOut {
     CUtensorMap map_w, map_q, map_ws, map_s;
@@ -60,6 +59,7 @@ struct Head4Args : HeadOut {
     int64_t row_bytes, tiles_k;  // of a row's codes; 64-column tiles of its scales
     int32_t blocks;              // stages of K
     int32_t m_tiles, tiles, box_rows, stages;  // as in HeadArgs
+    bool wide;                   // every row of logits starts on a 32-byte boundary
 };
 
 // Sum of 32 products and their blocks' scales. e2m1 products are multiples of 1/4 up to 36,
@@ -89,6 +89,7 @@ __device__ __forceinline__ void few_load(const Head4Args &a, int32_t m, unsigned
 }
 __device__ __forceinline__ void few_ask(const Head4Args &a, int32_t v, int lane) {
     for (int32_t c = lane * 128; c < a.row_bytes; c += 32 * 128) prefetch_l2(a.w + v * a.row_bytes + c);
+    for (int32_t t = lane; t < a.tiles_k; t += 32) prefetch_l2(a.ws + scale_word4(v, t, a.tiles_k));
 }
 __device__ __forceinline__ float few_part(const Head4Args &a, int32_t v, const unsigned char *smem, int lane) {
     const float *scales = reinterpret_cast<const float *>(smem + a.row_bytes);
@@ -116,6 +117,63 @@ __device__ __forceinline__ float few_logit(const Head4Args &a, int32_t m, int32_
     return sum * __ldg(a.q_rows + m) * __ldg(a.w_rows + v);
 }
 
+// 16 tokens from v on of a warp's 32 rows from m on (of which `rows` are there, and
+// the bit of `some` is set), a row a thread, 32 bytes at a time.
+template <typename T>
+__device__ __forceinline__ void store16(const HeadOut &a, const float *x, int32_t m, int32_t rows, uint32_t some, int32_t v, int lane) {
+    if (lane >= rows || !((some >> lane) & 1u)) return;
+    T *mine = static_cast<T *>(a.logits) + (m + lane) * a.stride + v;
+    if (v + 16 > a.V) {
+#pragma unroll
+        for (int e = 0; e < 16; e++)
+            if (v + e < a.V) mine[e] = from_f32<T>(x[e]);
+        return;
+    }
+    uint32_t r[8];
+    if (sizeof(T) == 2) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const __nv_bfloat162 both = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+            r[i] = *reinterpret_cast<const uint32_t *>(&both);
+        }
+        store32(mine, r);
+    } else {
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) r[i] = __float_as_uint(x[8 * h + i]);
+            store32(mine + 8 * h, r);
+        }
+    }
+}
+
+// Rows that do not all start on 32-byte boundaries: a warp's tokens from v on (32 in 32
+// bits, 64 in bf16), turned in shared memory, a row an instruction: 1,000 rows, V
+// 128,011, f32 308 us, and 450 with eight tokens of four rows an instruction.
+template <typename T>
+__device__ __forceinline__ void store_turned(const HeadOut &a, const uint32_t *turn, int32_t m, int32_t rows, uint32_t some, int32_t v, int lane) {
+    __syncwarp();
+    T *out = static_cast<T *>(a.logits) + m * a.stride + v;
+    const int32_t n = a.V - v;  // tokens there
+#pragma unroll 4
+    for (int r = 0; r < rows; r++, out += a.stride) {
+        if (!((some >> r) & 1u)) continue;
+        const uint32_t w = turn[r * kTurnPitch + lane];
+        if (sizeof(T) == 4) {
+            if (lane < n) reinterpret_cast<uint32_t *>(out)[lane] = w;
+        } else {
+            uint16_t *to = reinterpret_cast<uint16_t *>(out);
+            const bool odd = reinterpret_cast<uintptr_t>(out) & 2;  // pairs of tokens start at the second
+            const uint32_t next = __shfl_down_sync(~0u, w, 1);
+            const int32_t t = 2 * lane + odd;
+            if (odd && lane == 0 && n > 0) to[0] = uint16_t(w);
+            if (t + 1 < min(n, 64)) *reinterpret_cast<uint32_t *>(to + t) = odd ? __funnelshift_r(w, next, 16) : w;
+            else if (t < min(n, 64)) to[t] = uint16_t(odd ? w >> 16 : w);
+        }
+    }
+    __syncwarp();
+}
+
 template <typename T, bool kPair>
 __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_constant__ Head4Args a) {
     constexpr int NT = kTokens<kPair>;
@@ -126,7 +184,6 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
     static_assert(kHiddenColumns + kSteps * NT / 32 <= kSlotColumns, "a stage's scales fit a slot");
     extern __shared__ unsigned char dynamic_smem[];
     __shared__ uint64_t bars[2 * kMaxStages + 2 * kAccumulators];
-    __shared__ T turn[kEpilogue][kTurn<T, kTurnTokens<T>>];
     __shared__ __align__(16) float token_scales[kEpilogue][kColumns];
     __shared__ uint32_t need[kNeedTiles / 32];
     __shared__ uint32_t tmem_base;
@@ -186,7 +243,8 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
         const int quarter = warp & 3, column = (warp - kFirst) / 4 * kColumns;
         const uint32_t from = tmem + (uint32_t(quarter * 32) << 16) + uint32_t(column);
         const uint32_t drain = kPair ? cluster_addr(drained, 0) : drained;
-        const bool wide = ((reinterpret_cast<uintptr_t>(a.logits) | uintptr_t(a.stride * int64_t(sizeof(T)))) & 31) == 0;
+        uint32_t *const turn = reinterpret_cast<uint32_t *>(dynamic_smem + (stages - smem_addr(dynamic_smem)) + a.stages * stage_bytes +
+                                                            (kRows - a.box_rows) * 128) + (warp - kFirst) * kTurnWords;  // only where not a.wide
         float *const tokens = token_scales[warp - kFirst];
         uint32_t it = 0;
         for (int32_t i = 0, t = unit; t < a.tiles; i++, t += units) {
@@ -244,10 +302,18 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
                             if (!((bits >> e) & 1u)) sum[e] = -INFINITY;
                         }
                     }
-                    if (v + c >= a.V) continue;
-                    T *const to = turn[warp - kFirst];
-                    if (some == ~0u) store16<T, false, T, kTurnTokens<T>>(a, to, sum, mine, rows, some, v + c, lane, wide);
-                    else store16<T, true, T, kTurnTokens<T>>(a, to, sum, mine, rows, some, v + c, lane, wide);
+                    if (a.wide) {
+                        if (v + c < a.V) store16<T>(a, sum, mine, rows, some, v + c, lane);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 16; e += sizeof(T) == 4 ? 1 : 2) {
+                            const __nv_bfloat162 both = __floats2bfloat162_rn(sum[e], sum[e + 1 < 16 ? e + 1 : e]);
+                            if (sizeof(T) == 4) turn[lane * kTurnPitch + c % 32 + e] = __float_as_uint(sum[e]);
+                            else turn[lane * kTurnPitch + (c + e) / 2] = *reinterpret_cast<const uint32_t *>(&both);
+                        }
+                        if (sizeof(T) == 4 ? c % 32 == 16 : c == kColumns - 16)
+                            store_turned<T>(a, turn, mine, rows, some, sizeof(T) == 4 ? v + c - 16 : v, lane);
+                    }
                 }
             }
             __syncwarp();  // the next tile's scales are written where these were read
@@ -372,9 +438,10 @@ cudaError_t launch_head4(Head4Args a, cudaStream_t st) {
     const int stage = kWeightBytes4<kPair> + kHiddenScales + a.box_rows * 128;
     // the last stage's MMA reads kRows rows, whatever was loaded; and room to align the ring
     const int beyond = (kRows - a.box_rows) * 128 + 1024;
-    const int fixed = kEpilogueWarps4<kPair> * int(sizeof(T) * kTurn<T, kTurnTokens<T>> + sizeof(float) * kColumns) + 1024;  // declared in the kernel
-    a.stages = std::min(kMaxStages, (kHeadSmem - fixed - beyond) / stage);
-    const int smem = a.stages * stage + beyond;
+    const int fixed = kEpilogueWarps4<kPair> * int(sizeof(float)) * kColumns + 1024;  // declared in the kernel
+    const int turned = a.wide ? 0 : kEpilogueWarps4<kPair> * kTurnWords * 4;
+    a.stages = std::min(kMaxStages, (kHeadSmem - fixed - beyond - turned) / stage);
+    const int smem = a.stages * stage + beyond + turned;
     const cudaError_t e = cudaFuncSetAttribute(k_head4<T, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadSmem - fixed);
     if (e != cudaSuccess) return e;
     const int ctas = kPair ? 2 : 1, units = std::min(a.tiles, sm_count() / ctas);
@@ -433,6 +500,7 @@ extern "C" int trie_head4_logits(const uint8_t *d_q, const uint8_t *d_scales, co
     a.box_rows = std::min(kRows, (M + 7) / 8 * 8);
     a.logits = d_logits;
     a.stride = stride;
+    a.wide = ((reinterpret_cast<uintptr_t>(d_logits) | uintptr_t(stride * (dtype == TRIE_DTYPE_F32 ? 4 : 2))) & 31) == 0;
     a.g = make_grammar(d_mask, mask_rows, d_states, V);
     if (!make_map(&a.map_w, d_w, V, a.row_bytes, 128) || !make_map(&a.map_q, d_q, M, a.row_bytes, a.box_rows) ||
         !make_scale_map(&a.map_ws, d_w_scales, V, a.tiles_k, side / 128) || !make_scale_map(&a.map_s, d_scales, M, a.tiles_k, 1))

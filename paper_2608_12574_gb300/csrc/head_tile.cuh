@@ -162,54 +162,6 @@ __device__ __noinline__ void fill_tile(const HeadOut &a, int32_t m0, int32_t m1,
     }
 }
 
-// 16 tokens from v on of a warp's 32 rows from m on (of which `rows` are there, and
-// with kSome those whose bit of `some` is set), a row a thread. Where every row is
-// on a 32-byte boundary a thread writes its own 32 bytes at a time; else the block
-// is turned in shared memory, so that lanes write consecutive tokens (256 aligned
-// rows: 148 and 159 us, 64: 93 and 101). One test more for each store, in kSome
-// only, costs 64 unaligned rows 6 us of 101.
-// The turned block is kept in `Turn`, kAcross tokens at a time.
-template <typename Turn, int kAcross>
-constexpr int kTurn = 32 * (kAcross + 4 / int(sizeof(Turn)));  // an odd number of words a row
-template <typename T, bool kSome, typename Turn, int kAcross>
-__device__ __forceinline__ void store16(const HeadOut &a, Turn *turn, const float *x, int32_t m, int32_t rows, uint32_t some,
-                                        int32_t v, int lane, bool wide) {
-    T *out = static_cast<T *>(a.logits) + m * a.stride + v;
-    if (wide && v + 16 <= a.V) {
-        if (lane >= rows || (kSome && !((some >> lane) & 1u))) return;
-        T *mine = out + lane * a.stride;
-        uint32_t r[8];
-        if (sizeof(T) == 2) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const __nv_bfloat162 both = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-                r[i] = *reinterpret_cast<const uint32_t *>(&both);
-            }
-            store32(mine, r);
-        } else {
-#pragma unroll
-            for (int h = 0; h < 2; h++) {
-#pragma unroll
-                for (int i = 0; i < 8; i++) r[i] = __float_as_uint(x[8 * h + i]);
-                store32(mine + 8 * h, r);
-            }
-        }
-        return;
-    }
-    constexpr int kPitch = kTurn<Turn, kAcross> / 32;
-#pragma unroll
-    for (int k = 0; k < 16; k += kAcross) {
-#pragma unroll
-        for (int i = 0; i < kAcross; i++) turn[lane * kPitch + i] = from_f32<Turn>(x[k + i]);
-        __syncwarp();
-        const int c = lane % kAcross;
-        if (v + k + c < a.V)
-            for (int r = lane / kAcross; r < rows; r += 32 / kAcross)
-                if (!kSome || ((some >> r) & 1u)) out[r * a.stride + k + c] = from_f32<T>(to_f32(turn[r * kPitch + c]));
-        __syncwarp();
-    }
-}
-
 // cuTensorMapEncodeTiled, NULL where the driver has none.
 using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
                             const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
