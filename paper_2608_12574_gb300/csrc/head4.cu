@@ -24,17 +24,22 @@ namespace {
 
 // ---- the product
 //
-// Tiles, pairs of CTAs and the ring are as in head.cu: rows of the batch are the
-// MMA's rows, 128 x 128 on a CTA up to 128 rows of the batch, 256 x 256 on a pair
-// beyond. The tensor core applies the blocks' scales itself, so an
-// accumulator takes the whole of K and is read out once a tile: the epilogue
-// holds its 64 tokens a thread in registers and gives the accumulator back before it
-// scales and stores them. A stage is 256 columns, four MMAs deep: 128 bytes of
-// a row of either operand, and 512 bytes of scales for 128 rows and 64 columns,
-// which the MMAs' thread copies from shared to tensor memory in front of them
-// (copies and MMAs of a thread are carried out in order).
+// Tiles and the ring are as in head.cu: rows of the batch are the MMA's rows, 128
+// x 128 on a CTA up to 128 rows of the batch, 256 x 256 on a pair of CTAs beyond.
+// The tensor core applies the blocks' scales itself, so an accumulator takes the
+// whole of K and is read out once a tile: the epilogue holds its 64 tokens a
+// thread in registers and gives the accumulator back before it scales and stores
+// them. A stage is 256 columns, four MMAs deep: 128 bytes of a row of either
+// operand, and 512 bytes of scales for 128 rows and 64 columns, which the
+// MMAs' thread copies from shared to tensor memory in front of them (copies and
+// MMAs of a thread are carried out in order).
+// What bounds large batches is what L2 gives (12 TB/s): two tiles (kShare) of the same rows,
+// side by side in the vocabulary, are a cluster's, whose CTAs load half of the
+// hidden states' stage each and give it to both (TMA multicast), as a pair's
+// CTAs do with the scales of their tokens.
 constexpr int kStageColumns = 256;
 constexpr int kSteps = kStageColumns / 64;  // MMAs of a stage
+constexpr int kShareRows = 32;              // of the batch, from which on two tiles share them
 constexpr int kScaleTile = 512;             // bytes of the scales of 128 rows x 64 columns
 
 template <bool kPair>
@@ -174,12 +179,12 @@ __device__ __forceinline__ void store_turned(const HeadOut &a, const uint32_t *t
     __syncwarp();
 }
 
-template <typename T, bool kPair>
+template <typename T, bool kPair, int kShare>
 __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_constant__ Head4Args a) {
     constexpr int NT = kTokens<kPair>;
     constexpr int kAccumulators = 256 / NT;  // the other 256 columns of tensor memory are for scales
     constexpr int kEpilogue = kEpilogueWarps4<kPair>, kFirst = kFirstWarp4<kPair>;
-    constexpr int kCtas = kPair ? 2 : 1;
+    constexpr int kCtas = kPair ? 2 : 1, kCluster = kCtas * kShare;
     constexpr uint32_t kHiddenColumns = kSteps * 4, kSlotColumns = 64;  // of a stage's scales in tensor memory
     static_assert(kHiddenColumns + kSteps * NT / 32 <= kSlotColumns, "a stage's scales fit a slot");
     extern __shared__ unsigned char dynamic_smem[];
@@ -189,8 +194,9 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
     __shared__ uint32_t tmem_base;
     __shared__ int gave_up;
     const int warp = __shfl_sync(~0u, int(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
-    const int rank = kPair ? int(cluster_rank()) : 0;
-    const int32_t unit = int32_t(blockIdx.x) / kCtas, units = int32_t(gridDim.x) / kCtas;
+    const int cta = kCluster > 1 ? int(cluster_rank()) : 0, rank = cta % kCtas, part = cta / kCtas;  // of a pair; of the tiles
+    const int first_cta = part * kCtas;
+    const int32_t unit = int32_t(blockIdx.x) / kCluster, units = int32_t(gridDim.x) / kCluster;
     const uint32_t full = smem_addr(bars), empty = full + 8 * kMaxStages;
     const uint32_t ready = empty + 8 * kMaxStages, drained = ready + 8 * kAccumulators;
     const uint32_t stages = (smem_addr(dynamic_smem) + 1023u) & ~1023u;
@@ -199,7 +205,7 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
         gave_up = 0;
         for (int i = 0; i < a.stages; i++) {
             bar_init(full + 8 * i, 1);
-            bar_init(empty + 8 * i, 1);
+            bar_init(empty + 8 * i, kShare);
         }
         for (int i = 0; i < kAccumulators; i++) {
             bar_init(ready + 8 * i, 1);
@@ -224,15 +230,15 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
     if (a.g.mask) {
         // which of this CTA's tiles a dense row allows a token of
         for (int32_t i = 0, t = unit; t < a.tiles && i < kNeedTiles; i++, t += units) {
-            const int32_t m = t % a.m_tiles * (kRows * kCtas) + int32_t(threadIdx.x), v0 = t / a.m_tiles * NT;
+            const int32_t m = t % a.m_tiles * (kRows * kCtas) + int32_t(threadIdx.x), v0 = t / a.m_tiles * (NT * kShare);
             bool any = false;
             if (threadIdx.x < kRows * kCtas && m < a.M && __ldg(a.dense + m))
-                any = row_uses(a, m, v0) || (NT > 128 && v0 + 128 < a.V && row_uses(a, m, v0 + 128));
+                for (int32_t v = v0; v < min(a.V, v0 + NT * kShare); v += 128) any |= row_uses(a, m, v);
             if (__any_sync(~0u, any) && lane == 0) atomicOr(&need[i >> 5], 1u << (i & 31));
         }
     }
     tcgen05_fence_before();
-    if (kPair) cluster_sync();
+    if (kCluster > 1) cluster_sync();
     else __syncthreads();
     tcgen05_fence_after();
     const uint32_t tmem = *static_cast<volatile uint32_t *>(&tmem_base);
@@ -242,14 +248,14 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
         if (kPair) more_registers<112>();
         const int quarter = warp & 3, column = (warp - kFirst) / 4 * kColumns;
         const uint32_t from = tmem + (uint32_t(quarter * 32) << 16) + uint32_t(column);
-        const uint32_t drain = kPair ? cluster_addr(drained, 0) : drained;
+        const uint32_t drain = kPair ? cluster_addr(drained, first_cta) : drained;
         uint32_t *const turn = reinterpret_cast<uint32_t *>(dynamic_smem + (stages - smem_addr(dynamic_smem)) + a.stages * stage_bytes +
                                                             (kRows - a.box_rows) * 128) + (warp - kFirst) * kTurnWords;  // only where not a.wide
         float *const tokens = token_scales[warp - kFirst];
         uint32_t it = 0;
         for (int32_t i = 0, t = unit; t < a.tiles; i++, t += units) {
             const int32_t m0 = t % a.m_tiles * (kRows * kCtas) + rank * kRows, m1 = min(a.M, m0 + kRows);
-            const int32_t v0 = t / a.m_tiles * NT, v = v0 + column;
+            const int32_t v0 = (t / a.m_tiles * kShare + part) * NT, v = v0 + column;
             if (!needed(i)) {
                 fill_tile<T, NT, kEpilogue>(a, m0, m1, v0, warp - kFirst, lane);
                 continue;
@@ -324,10 +330,12 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
             int stage = 0;
             uint32_t phase = 1, used = 0;  // phase: of a stage's last use; the first time round there is none
             bool ok = true;
-            const uint32_t leader = kPair ? cluster_addr(full, 0) : full;
+            const uint32_t leader = kPair ? cluster_addr(full, first_cta) : full;
+            const uint16_t same_rows = kShare == 1 ? 1 : kPair ? uint16_t(5 << rank) : 3, same_tokens = uint16_t(3 << first_cta);
+            const int32_t half = a.box_rows / kShare;
             for (int32_t i = 0, t = unit; t < a.tiles && ok; i++, t += units) {
                 if (!needed(i)) continue;
-                const int32_t m = t % a.m_tiles * (kRows * kCtas) + rank * kRows, v0 = t / a.m_tiles * NT;
+                const int32_t m = t % a.m_tiles * (kRows * kCtas) + rank * kRows, v0 = (t / a.m_tiles * kShare + part) * NT;
                 for (int32_t kb = 0; kb < a.blocks; kb++) {
                     const uint32_t at = stages + uint32_t(stage) * stage_bytes, bar = leader + 8 * stage;
                     const uint32_t scales = at + 128 * 128, hidden_scales = at + kWeightBytes4<kPair>, hidden = hidden_scales + kHiddenScales;
@@ -335,17 +343,20 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
                     ok = __all_sync(~0u, ok);
                     if (!ok) break;
                     if (elect_one()) {
+                        // all that comes to a tile's CTAs counts on its first one's barrier
+                        if (rank == 0) bar_expect(full + 8 * stage, kCtas * stage_bytes);
                         if (kPair) {
-                            // both CTAs' copies count on the first one's barrier
-                            if (rank == 0) bar_expect(full + 8 * stage, 2 * stage_bytes);
                             tma_load_2d_pair(at, &a.map_w, kb * 128, v0 + rank * 128, bar);
-                            tma_load_3d_pair(scales, &a.map_ws, 0, kb * kSteps, v0 / 128, bar);
-                            tma_load_3d_pair(hidden_scales, &a.map_s, 0, kb * kSteps, m / 128, bar);
-                            tma_load_2d_pair(hidden, &a.map_q, kb * 128, m, bar);
+                            tma_share_3d<kPair>(scales + rank * kHiddenScales, &a.map_ws, 0, kb * kSteps, v0 / 128 + rank, bar, same_tokens);
                         } else {
-                            bar_expect(bar, stage_bytes);
                             tma_load_2d(at, &a.map_w, kb * 128, v0, bar);
                             tma_load_3d(scales, &a.map_ws, 0, kb * kSteps, v0 / 128, bar);
+                        }
+                        if (kShare > 1) {
+                            tma_share_3d<kPair>(hidden_scales + part * (kHiddenScales / kShare), &a.map_s, 0, kb * kSteps + part * (kSteps / kShare),
+                                                m / 128, bar, same_rows);
+                            tma_share_2d<kPair>(hidden + part * half * 128, &a.map_q, kb * 128, m + part * half, bar, same_rows);
+                        } else {
                             tma_load_3d(hidden_scales, &a.map_s, 0, kb * kSteps, m / 128, bar);
                             tma_load_2d(hidden, &a.map_q, kb * 128, m, bar);
                         }
@@ -402,8 +413,12 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
                                 if (k >= steps) break;
                                 mma_e2m1<kPair>(tmem + acc * NT, dq + 2 * k, dw + 2 * k, idesc, sq + 4 * k, sw + k * (NT / 32), kb > 0 || k > 0);
                             }
-                            mma_commit<kPair>(empty + 8 * stage);
-                            if (kb == a.blocks - 1) mma_commit<kPair>(ready + 8 * acc);
+                            if (kShare > 1) mma_commit_to<kPair>(empty + 8 * stage, uint16_t((1 << kCluster) - 1));
+                            else mma_commit<kPair>(empty + 8 * stage);
+                            if (kb == a.blocks - 1) {
+                                if (kPair) mma_commit_to<kPair>(ready + 8 * acc, uint16_t(3 << first_cta));
+                                else mma_commit<kPair>(ready + 8 * acc);
+                            }
                         }
                         __syncwarp();
                         slot ^= 1;
@@ -415,25 +430,25 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
     }
     __syncwarp();
     tcgen05_fence_before();
-    if (kPair) cluster_sync();
+    if (kCluster > 1) cluster_sync();
     else __syncthreads();
     tcgen05_fence_after();
     if (warp == 1) tmem_free<kPair>(tmem, 512);
 }
 
-// [rows / 128][columns / 64][512 bytes] in boxes of `row_blocks` x kSteps x 512 bytes, zeros outside.
-bool make_scale_map(CUtensorMap *map, const void *base, int64_t rows, int64_t tiles, int32_t row_blocks) {
+// [rows / 128][columns / 64][512 bytes] in boxes of 1 x `box_tiles` x 512 bytes, zeros outside.
+bool make_scale_map(CUtensorMap *map, const void *base, int64_t rows, int64_t tiles, int32_t box_tiles) {
     const Encode encode = tensor_map_encode();
     if (!encode) return false;
     const cuuint64_t dims[3] = {kScaleTile / 4, cuuint64_t(tiles), cuuint64_t((rows + 127) / 128)};
     const cuuint64_t strides[2] = {kScaleTile, cuuint64_t(tiles) * kScaleTile};
-    const cuuint32_t box[3] = {kScaleTile / 4, kSteps, cuuint32_t(row_blocks)}, steps[3] = {1, 1, 1};
+    const cuuint32_t box[3] = {kScaleTile / 4, cuuint32_t(box_tiles), 1}, steps[3] = {1, 1, 1};
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<void *>(base), dims, strides, box, steps,
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T, bool kPair>
+template <typename T, bool kPair, int kShare>
 cudaError_t launch_head4(Head4Args a, cudaStream_t st) {
     const int stage = kWeightBytes4<kPair> + kHiddenScales + a.box_rows * 128;
     // the last stage's MMA reads kRows rows, whatever was loaded; and room to align the ring
@@ -442,11 +457,13 @@ cudaError_t launch_head4(Head4Args a, cudaStream_t st) {
     const int turned = a.wide ? 0 : kEpilogueWarps4<kPair> * kTurnWords * 4;
     a.stages = std::min(kMaxStages, (kHeadSmem - fixed - beyond - turned) / stage);
     const int smem = a.stages * stage + beyond + turned;
-    const cudaError_t e = cudaFuncSetAttribute(k_head4<T, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadSmem - fixed);
+    const cudaError_t e = cudaFuncSetAttribute(k_head4<T, kPair, kShare>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadSmem - fixed);
     if (e != cudaSuccess) return e;
-    const int ctas = kPair ? 2 : 1, units = std::min(a.tiles, sm_count() / ctas);
+    constexpr int kCluster = (kPair ? 2 : 1) * kShare;
+    // clusters of four do not reach every SM (36 of them, 144 CTAs, on 152); what is beyond waits its turn
+    const int units = std::min(a.tiles, sm_count() / kCluster - (kCluster == 4 ? 2 : 0));
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(units * ctas));
+    cfg.gridDim = dim3(unsigned(units * kCluster));
     cfg.blockDim = dim3(kThreads4<kPair>);
     cfg.dynamicSmemBytes = size_t(smem);
     cfg.stream = st;
@@ -454,11 +471,11 @@ cudaError_t launch_head4(Head4Args a, cudaStream_t st) {
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = unsigned(ctas);
+    attr[1].val.clusterDim.x = unsigned(kCluster);
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = kPair ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, k_head4<T, kPair>, a);
+    cfg.numAttrs = kCluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, k_head4<T, kPair, kShare>, a);
 }
 
 }  // namespace
@@ -497,15 +514,16 @@ extern "C" int trie_head4_logits(const uint8_t *d_q, const uint8_t *d_scales, co
     const bool pair = M > kRows;
     const int side = pair ? 256 : 128;  // of a tile
     a.m_tiles = (M + side - 1) / side;
-    a.box_rows = std::min(kRows, (M + 7) / 8 * 8);
+    const int share = M > kShareRows ? 2 : 1;
+    a.box_rows = std::min(kRows, (M + 15) / 16 * 16);
     a.logits = d_logits;
     a.stride = stride;
     a.wide = ((reinterpret_cast<uintptr_t>(d_logits) | uintptr_t(stride * (dtype == TRIE_DTYPE_F32 ? 4 : 2))) & 31) == 0;
     a.g = make_grammar(d_mask, mask_rows, d_states, V);
-    if (!make_map(&a.map_w, d_w, V, a.row_bytes, 128) || !make_map(&a.map_q, d_q, M, a.row_bytes, a.box_rows) ||
-        !make_scale_map(&a.map_ws, d_w_scales, V, a.tiles_k, side / 128) || !make_scale_map(&a.map_s, d_scales, M, a.tiles_k, 1))
+    if (!make_map(&a.map_w, d_w, V, a.row_bytes, 128) || !make_map(&a.map_q, d_q, M, a.row_bytes, a.box_rows / share) ||
+        !make_scale_map(&a.map_ws, d_w_scales, V, a.tiles_k, kSteps) || !make_scale_map(&a.map_s, d_scales, M, a.tiles_k, kSteps / share))
         return set_error(TRIE_ECUDA, "cuTensorMapEncodeTiled failed");
-    const int64_t tiles = (int64_t(V) + side - 1) / side * a.m_tiles;
+    const int64_t tiles = (int64_t(V) + side * share - 1) / (side * share) * a.m_tiles;
     if (tiles > 0x3FFFFFFF) return set_error(TRIE_EINVAL, "M x V is too large");
     a.tiles = int32_t(tiles);
     const bool f32 = dtype == TRIE_DTYPE_F32;
@@ -521,8 +539,9 @@ extern "C" int trie_head4_logits(const uint8_t *d_q, const uint8_t *d_scales, co
                 : launch_pdl_smem(k_head_rows<__nv_bfloat16, Head4Args>, M, kRowThreads, smem, stream, a);
         if (e != cudaSuccess) return fail_launch(e, "4-bit head rows launch");
     }
-    e = pair ? (f32 ? launch_head4<float, true>(a, stream) : launch_head4<__nv_bfloat16, true>(a, stream))
-             : (f32 ? launch_head4<float, false>(a, stream) : launch_head4<__nv_bfloat16, false>(a, stream));
+    if (pair) e = f32 ? launch_head4<float, true, 2>(a, stream) : launch_head4<__nv_bfloat16, true, 2>(a, stream);
+    else if (share == 2) e = f32 ? launch_head4<float, false, 2>(a, stream) : launch_head4<__nv_bfloat16, false, 2>(a, stream);
+    else e = f32 ? launch_head4<float, false, 1>(a, stream) : launch_head4<__nv_bfloat16, false, 1>(a, stream);
     if (e != cudaSuccess) return fail_launch(e, "4-bit head launch");
     return TRIE_OK;
 }
