@@ -150,6 +150,10 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map
         "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
         : "memory");
 }
+// `bytes` (a multiple of 16) from p (on a 16-byte boundary) into L2.
+__device__ __forceinline__ void bulk_prefetch(const void *p, uint32_t bytes) {
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
+}
 // Orders this thread's accesses to shared memory before copies to it that follow.
 __device__ __forceinline__ void async_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 // `bytes` and both addresses: multiples of 16.

@@ -39,6 +39,7 @@ namespace {
 // CTAs do with the scales of their tokens.
 constexpr int kStageColumns = 256;
 constexpr int kSteps = kStageColumns / 64;  // MMAs of a stage
+constexpr int kAskFirst = 256 * 1024, kAskPiece = 16 * 1024;  // bytes of its first tile that a CTA asks for ahead; at a time
 constexpr int kShareRows = 32;              // of the batch, from which on two tiles share them
 constexpr int kScaleTile = 512;             // bytes of the scales of 128 rows x 64 columns
 
@@ -157,23 +158,35 @@ __device__ __forceinline__ void store16(const HeadOut &a, const float *x, int32_
 // 128,011, f32 308 us, and 450 with eight tokens of four rows an instruction.
 template <typename T>
 __device__ __forceinline__ void store_turned(const HeadOut &a, const uint32_t *turn, int32_t m, int32_t rows, uint32_t some, int32_t v, int lane) {
+    constexpr int kAtOnce = 8;  // rows read before the first is written
     __syncwarp();
-    T *out = static_cast<T *>(a.logits) + m * a.stride + v;
-    const int32_t n = a.V - v;  // tokens there
-#pragma unroll 4
-    for (int r = 0; r < rows; r++, out += a.stride) {
-        if (!((some >> r) & 1u)) continue;
-        const uint32_t w = turn[r * kTurnPitch + lane];
-        if (sizeof(T) == 4) {
-            if (lane < n) reinterpret_cast<uint32_t *>(out)[lane] = w;
-        } else {
-            uint16_t *to = reinterpret_cast<uint16_t *>(out);
-            const bool odd = reinterpret_cast<uintptr_t>(out) & 2;  // pairs of tokens start at the second
-            const uint32_t next = __shfl_down_sync(~0u, w, 1);
-            const int32_t t = 2 * lane + odd;
-            if (odd && lane == 0 && n > 0) to[0] = uint16_t(w);
-            if (t + 1 < min(n, 64)) *reinterpret_cast<uint32_t *>(to + t) = odd ? __funnelshift_r(w, next, 16) : w;
-            else if (t < min(n, 64)) to[t] = uint16_t(odd ? w >> 16 : w);
+    const int32_t n = min(a.V - v, 64);  // tokens there
+    if (rows < 32) some &= (1u << rows) - 1u;
+    char *out = static_cast<char *>(a.logits) + (m * a.stride + v) * int64_t(sizeof(T));
+    const int64_t step = a.stride * int64_t(sizeof(T));
+    turn += lane;
+#pragma unroll 1
+    for (int r0 = 0; r0 < rows; r0 += kAtOnce, out += kAtOnce * step, turn += kAtOnce * kTurnPitch) {
+        uint32_t w[kAtOnce];
+#pragma unroll
+        for (int r = 0; r < kAtOnce; r++) w[r] = turn[r * kTurnPitch];
+        const uint32_t mine = some >> r0;
+#pragma unroll
+        for (int r = 0; r < kAtOnce; r++) {
+            T *to = reinterpret_cast<T *>(out + r * step);
+            const bool there = (mine >> r) & 1u;
+            if (sizeof(T) == 4) {
+                if (there && lane < n) reinterpret_cast<uint32_t *>(to)[lane] = w[r];
+            } else {
+                // pairs of tokens from the first or, where a row starts at an odd 2 bytes, the second
+                const bool odd = reinterpret_cast<uintptr_t>(to) & 2;
+                const uint32_t next = __shfl_down_sync(~0u, w[r], 1);
+                const int32_t t = 2 * lane + odd;
+                uint16_t *half = reinterpret_cast<uint16_t *>(to);
+                if (there && odd && lane == 0 && n > 0) half[0] = uint16_t(w[r]);
+                if (there && t + 1 < n) *reinterpret_cast<uint32_t *>(half + t) = odd ? __funnelshift_r(w[r], next, 16) : w[r];
+                else if (there && t < n) half[t] = uint16_t(odd ? w[r] >> 16 : w[r]);
+            }
         }
     }
     __syncwarp();
@@ -219,6 +232,13 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
     }
     for (int i = threadIdx.x; i < kNeedTiles / 32; i += kThreads4<kPair>) need[i] = 0u;
     pdl_launch_dependents();
+    if (warp == 0 && !a.g.mask && unit < a.tiles && elect_one()) {
+        // while the kernel before runs, the first tile's weights come to L2 (where they are in one piece)
+        const int32_t v = (unit / a.m_tiles * kShare + part) * NT + rank * 128;
+        const int64_t all = min(128, a.V - v) * a.row_bytes;
+        for (int64_t at = 0; at < min(all, int64_t(kAskFirst)); at += kAskPiece)
+            bulk_prefetch(a.w + v * a.row_bytes + at, uint32_t(min(int64_t(kAskPiece), all - at)));
+    }
     pdl_wait();
     if (a.g.mask && a.M <= kLookRows) {  // k_head_rows may have left nothing to do (the same answer in all CTAs)
         bool any = false;
@@ -331,7 +351,7 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
             uint32_t phase = 1, used = 0;  // phase: of a stage's last use; the first time round there is none
             bool ok = true;
             const uint32_t leader = kPair ? cluster_addr(full, first_cta) : full;
-            const uint16_t same_rows = kShare == 1 ? 1 : kPair ? uint16_t(5 << rank) : 3, same_tokens = uint16_t(3 << first_cta);
+            const uint16_t same_rows = kShare == 1 ? uint16_t(1 << rank) : kPair ? uint16_t(5 << rank) : 3, same_tokens = uint16_t(3 << first_cta);
             const int32_t half = a.box_rows / kShare;
             for (int32_t i = 0, t = unit; t < a.tiles && ok; i++, t += units) {
                 if (!needed(i)) continue;
@@ -352,7 +372,7 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
                             tma_load_2d(at, &a.map_w, kb * 128, v0, bar);
                             tma_load_3d(scales, &a.map_ws, 0, kb * kSteps, v0 / 128, bar);
                         }
-                        if (kShare > 1) {
+                        if (kPair || kShare > 1) {
                             tma_share_3d<kPair>(hidden_scales + part * (kHiddenScales / kShare), &a.map_s, 0, kb * kSteps + part * (kSteps / kShare),
                                                 m / 128, bar, same_rows);
                             tma_share_2d<kPair>(hidden + part * half * 128, &a.map_q, kb * 128, m + part * half, bar, same_rows);
@@ -461,7 +481,7 @@ cudaError_t launch_head4(Head4Args a, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     constexpr int kCluster = (kPair ? 2 : 1) * kShare;
     // clusters of four do not reach every SM (36 of them, 144 CTAs, on 152); what is beyond waits its turn
-    const int units = std::min(a.tiles, sm_count() / kCluster - (kCluster == 4 ? 2 : 0));
+    const int units = std::min(a.tiles, std::max(1, sm_count() / kCluster - (kCluster == 4 ? 2 : 0)));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(units * kCluster));
     cfg.blockDim = dim3(kThreads4<kPair>);
@@ -514,7 +534,10 @@ extern "C" int trie_head4_logits(const uint8_t *d_q, const uint8_t *d_scales, co
     const bool pair = M > kRows;
     const int side = pair ? 256 : 128;  // of a tile
     a.m_tiles = (M + side - 1) / side;
-    const int share = M > kShareRows ? 2 : 1;
+    // A pair's tiles share their rows where there are several tiles of rows (512 rows, V 128,000,
+    // D 4,112 111 us, and 151 without) or rows of codes start off 128-byte lines (192 rows 65 and
+    // 76); else what more SMs give is worth more (256 rows, V 152,064, D 4,096 76 and 73).
+    const int share = pair ? (M > 256 || row_bytes4(D) % 128 ? 2 : 1) : M > kShareRows ? 2 : 1;
     a.box_rows = std::min(kRows, (M + 15) / 16 * 16);
     a.logits = d_logits;
     a.stride = stride;
@@ -539,7 +562,8 @@ extern "C" int trie_head4_logits(const uint8_t *d_q, const uint8_t *d_scales, co
                 : launch_pdl_smem(k_head_rows<__nv_bfloat16, Head4Args>, M, kRowThreads, smem, stream, a);
         if (e != cudaSuccess) return fail_launch(e, "4-bit head rows launch");
     }
-    if (pair) e = f32 ? launch_head4<float, true, 2>(a, stream) : launch_head4<__nv_bfloat16, true, 2>(a, stream);
+    if (pair && share == 2) e = f32 ? launch_head4<float, true, 2>(a, stream) : launch_head4<__nv_bfloat16, true, 2>(a, stream);
+    else if (pair) e = f32 ? launch_head4<float, true, 1>(a, stream) : launch_head4<__nv_bfloat16, true, 1>(a, stream);
     else if (share == 2) e = f32 ? launch_head4<float, false, 2>(a, stream) : launch_head4<__nv_bfloat16, false, 2>(a, stream);
     else e = f32 ? launch_head4<float, false, 1>(a, stream) : launch_head4<__nv_bfloat16, false, 1>(a, stream);
     if (e != cudaSuccess) return fail_launch(e, "4-bit head launch");
