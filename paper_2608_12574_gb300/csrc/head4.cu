@@ -473,11 +473,11 @@ cudaError_t launch_head4(Head4Args a, cudaStream_t st) {
     const int stage = kWeightBytes4<kPair> + kHiddenScales + a.box_rows * 128;
     // the last stage's MMA reads kRows rows, whatever was loaded; and room to align the ring
     const int beyond = (kRows - a.box_rows) * 128 + 1024;
-    const int fixed = kEpilogueWarps4<kPair> * int(sizeof(float)) * kColumns + 1024;  // declared in the kernel
+    constexpr int fixed = kEpilogueWarps4<kPair> * int(sizeof(float)) * kColumns + 1024;  // declared in the kernel
     const int turned = a.wide ? 0 : kEpilogueWarps4<kPair> * kTurnWords * 4;
     a.stages = std::min(kMaxStages, (kHeadSmem - fixed - beyond - turned) / stage);
     const int smem = a.stages * stage + beyond + turned;
-    const cudaError_t e = cudaFuncSetAttribute(k_head4<T, kPair, kShare>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadSmem - fixed);
+    const cudaError_t e = allow_smem<k_head4<T, kPair, kShare>, kHeadSmem - fixed>();
     if (e != cudaSuccess) return e;
     constexpr int kCluster = (kPair ? 2 : 1) * kShare;
     // clusters of four do not reach every SM (36 of them, 144 CTAs, on 152); what is beyond waits its turn

@@ -527,13 +527,12 @@ cudaError_t launch_held(NormArgs a, int threads, cudaStream_t st) {
     const int64_t stay = int64_t(sm_count()) * fit;
     a.buffers = a.M > kStayRows * stay ? 2 : 1;
     const size_t smem = space(a.buffers);
-    auto kernel = k_norm_rows<TX, TR, kNorm, kBits, kSteps>;
     if (smem > kMostSpace) return launch_pdl(k_norm_long<true, kNorm, kBits>, a.M, kNormThreads, st, a);
-    if (smem > 40 * 1024) {  // what is declared in the kernel counts towards the 48 KB that need no attribute
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+    if (smem > 40 * 1024) {  // what is declared in the kernel counts towards the 48 KB that need no leave
+        const cudaError_t e = allow_smem<k_norm_rows<TX, TR, kNorm, kBits, kSteps>, int(kMostSpace)>();
         if (e != cudaSuccess) return e;
     }
-    return launch_pdl_smem(kernel, a.buffers == 2 ? stay : int64_t(a.M), threads, smem, st, a);
+    return launch_pdl_smem(k_norm_rows<TX, TR, kNorm, kBits, kSteps>, a.buffers == 2 ? stay : int64_t(a.M), threads, smem, st, a);
 }
 
 template <typename TX, typename TR, bool kNorm, int kBits>

@@ -696,17 +696,17 @@ def _normed(x, gain, residual):
     """The arguments that the norm's calls begin with, up to the gain's type."""
     import torch
     p, stride, dtype = _hidden(x, "x")
-    D, f32 = x.shape[1], torch.float32
-    pr, r_dtype, r_stride = None, 0, 0
-    if residual is not None:
+    device = x.get_device()
+    if residual is None:
+        pr, r_stride, r_dtype = None, 0, 0
+    else:
         if residual.shape != x.shape:
             raise ValueError("residual must be [M, D]")
         pr, r_stride, r_dtype = _hidden(residual, "residual")
-    if gain.dim() != 1 or gain.shape[0] != D:
+    g_dtype, g_type = (TRIE_DTYPE_F32, torch.float32) if gain.dtype is torch.float32 else (TRIE_DTYPE_BF16, torch.bfloat16)
+    if gain.dim() != 1 or gain.shape[0] != x.shape[1]:
         raise ValueError("gain must have D entries")
-    g_dtype = TRIE_DTYPE_F32 if gain.dtype is f32 else TRIE_DTYPE_BF16
-    pg = _vec(gain, f32 if gain.dtype is f32 else torch.bfloat16, D, "gain", x.get_device())
-    return p, dtype, stride, pr, r_dtype, r_stride, pg, g_dtype
+    return p, dtype, stride, pr, r_dtype, r_stride, _vec(gain, g_type, x.shape[1], "gain", device), g_dtype
 
 
 def trie_head_norm_quantize(x, gain, residual=None, eps: float = 1e-6, stream=None):
