@@ -7,6 +7,24 @@
 //   loss = weight (kl (exp(d) - d - 1) - min(rho A, clip(rho) A))
 //   slope = dloss / dlp = weight (kl (1 - exp(d)) - [rho A <= clip(rho) A] rho A)
 //   dloss / dx[v] = slope ([v = t] - exp(y[v] - log sum exp y)) / temperature
+// A row is read once: its logits stay in shared memory between the pass that finds
+// its largest and its sum, and the pass that writes its gradient.
+//
+//  k_policy_rows  rows of which three shares fit the shared memory of up to 16 CTAs.
+//  k_policy       longer ones, and long ones without a gradient.
+//
+// What bounds it (times of calls that follow one another).
+//   4,096 rows, V 152,064, bf16, with the gradient: 381 to 393 us, 6.4 to 6.5 TB/s: HBM. (A
+//     CTA a row read twice: 2,210. Clusters with a row in registers, one row each:
+//     1,389. The clusters staying, but with every warp making every row's slope: 885; a warp of its own
+//     for it: 583; two logits an instruction and what a row needs of its scalars read ahead: 470; 15
+//     working warps instead of 30, so that half as many instructions go into a row's own work: 393.)
+//     Without the gradient 219 us, 5.7 TB/s.
+//   1,024 rows, V 128,011, half of them constrained: 94 us, 4.3 TB/s of zeros, gradients
+//     and free rows' logits: a constrained row waits for its mask's words and then for its
+//     tokens' logits, and three rows of a cluster are on their way at a time.
+//   300 rows, V 262,144, f32: 109 us, 5.8 TB/s on the 112 SMs that clusters of 16 reach.
+//   64 rows, V 32,000, f32, no gradient: 5 us, a chain of waits (row, masses, slope).
 #include <math.h>
 #include <stdint.h>
 #include <stdio.h>
@@ -169,7 +187,8 @@ struct RowValues {
     int32_t token, state;
     float old, advantage, ref, weight, temperature;
     __device__ RowValues(const PolicyArgs &a, int32_t b)
-        : token(__ldg(a.tokens + b)), state(a.g.mask ? __ldg(a.g.states + b) : TRIE_STATE_FREE), old(__ldg(a.old + b)), advantage(__ldg(a.advantages + b)), ref(a.ref ? __ldg(a.ref + b) : 0.0f),
+        : token(__ldg(a.tokens + b)), state(a.g.mask ? __ldg(a.g.states + b) : TRIE_STATE_FREE), old(__ldg(a.old + b)),
+          advantage(__ldg(a.advantages + b)), ref(a.ref ? __ldg(a.ref + b) : 0.0f),
           weight(a.weights ? __ldg(a.weights + b) : 1.0f), temperature(temperature_of(a, b)) {}
 };
 
@@ -267,13 +286,15 @@ struct Share {
 };
 
 // Rows of which three shares fit a CTA's shared memory: clusters of CTAs stay and
-// go over the rows, a cluster a row. One warp of a CTA, the clerk, asks for a
-// free row's shares by bulk copies rows ahead, reads what else a row has, sends
-// the CTA's mass of a row to the others and makes its slope; the other
-// warps take the masses of a row and then write the gradient of the row before,
-// whose slope has had that long to arrive. Of a constrained row only allowed
-// tokens are read, word by word of its mask, and its gradient is zeros with
-// these put in.
+// go over the rows, a cluster a row, a share of it a CTA. Warps with a part of their own:
+//   bringers    one for each slot: a free row's share comes to the slot by a bulk copy; of a
+//               constrained row the allowed tokens are listed from its mask, with
+//               their logits, or, if they are many, the share comes as well
+//   workers     the mass of a row's share, then the gradient of the row before, whose
+//               slope has had that long to arrive
+//   the sender  a CTA's mass of a row to all CTAs of the cluster
+//   the finisher  the row's loss and slope from these
+// The gradient of a constrained row is zeros with the listed tokens' put in.
 constexpr int kWorkerWarps = 15;
 constexpr int kWorkers = 32 * kWorkerWarps;
 constexpr int kSender = kWorkerWarps, kFinisher = kSender + 1, kFirstBringer = kFinisher + 1;
@@ -706,11 +727,15 @@ int active_clusters(int log_ctas) {
 
 template <typename T>
 cudaError_t run_policy(PolicyArgs a, cudaStream_t st) {
-    // The fewest CTAs a row of which three shares fit; more where the rows are few.
+    // The fewest CTAs a row of which three shares fit; more where the rows are few (8 rows of 32,000 in 32 bits
+    // with the gradient 5.1 us, and 6.3 with the fewest; 1 row 4.2 and 4.6).
     const int64_t pieces = int64_t(a.V) * int64_t(sizeof(T)) / 16;
     auto share = [&] { return (pieces + a.ctas - 1) / a.ctas * 16; };
+    // Without a gradient a row that would take 16 is read by k_policy, in one pass (300 rows of 200,000 in 32
+    // bits 65 us, and 75 by clusters of 16; with the gradient 138 and 98).
+    const int most = a.grad ? kMaxCluster : kMaxCluster / 2;
     int log_ctas = 0;
-    while (a.ctas < kMaxCluster && (share() > kMaxShare || (a.ctas < 8 && int64_t(a.B) * a.ctas * 2 <= sm_count() && share() > 16 * kRowThreads))) {
+    while (a.ctas < most && (share() > kMaxShare || (a.ctas < 8 && int64_t(a.B) * a.ctas * 2 <= sm_count() && share() > 16 * kRowThreads))) {
         a.ctas *= 2;
         log_ctas++;
     }
