@@ -285,19 +285,31 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
                                                             (kRows - a.box_rows) * 128) + (warp - kFirst) * kTurnWords;  // only where not a.wide
         float *const tokens = token_scales[warp - kFirst];
         uint32_t it = 0;
+        // a tile's scales, read while the tile before is stored
+        float row_next = 0.0f, token_next[2] = {0.0f, 0.0f};
+        auto read_scales = [&](int32_t t) {
+            if (t >= a.tiles) return;
+            const int32_t m = t % a.m_tiles * (kRows * kCtas) + rank * kRows + quarter * 32, v = (t / a.m_tiles * kShare + part) * NT + column;
+            row_next = __ldg(a.q_rows + min(m + lane, a.M - 1));
+            token_next[0] = __ldg(a.w_rows + min(v + lane, a.V - 1));
+            token_next[1] = __ldg(a.w_rows + min(v + lane + 32, a.V - 1));
+        };
+        read_scales(unit);
         for (int32_t i = 0, t = unit; t < a.tiles; i++, t += units) {
             const int32_t m0 = t % a.m_tiles * (kRows * kCtas) + rank * kRows, m1 = min(a.M, m0 + kRows);
             const int32_t v0 = (t / a.m_tiles * kShare + part) * NT, v = v0 + column;
+            const float row_scale = row_next;
+            tokens[lane] = token_next[0];
+            tokens[lane + 32] = token_next[1];
+            read_scales(t + units);
+            __syncwarp();
             if (!needed(i)) {
                 fill_tile<T, NT, kEpilogue>(a, m0, m1, v0, warp - kFirst, lane);
+                __syncwarp();
                 continue;
             }
             const int32_t mine = m0 + quarter * 32, row = min(mine + lane, a.M - 1);
             const bool there = mine < m1;  // a warp without rows only keeps the barriers going
-            const float row_scale = __ldg(a.q_rows + row);
-            tokens[lane] = __ldg(a.w_rows + min(v + lane, a.V - 1));
-            tokens[lane + 32] = __ldg(a.w_rows + min(v + lane + 32, a.V - 1));
-            __syncwarp();
             const uint32_t acc = it % kAccumulators;
             bar_wait(ready + 8 * acc, (it / kAccumulators) & 1, &gave_up);
             it++;
