@@ -17,10 +17,11 @@
 //  k_norm_long  any others: read again in each pass.
 //
 // What bounds it (residual and x in bf16, 8 bits; times of calls that follow one another).
-//   16,384 rows, D 5,120: 112 us, 5.3 TB/s. Instructions: 20 a value, of them five for the
-//     sum's second float and four for the division by the block's scale; with a loop that reads
-//     rows again 175, with each warp adding up all warps' sums 125, with the next row's
-//     copies ahead but in registers, so that fewer CTAs fit, 174. D 4,096: 84 us, 5.6 TB/s.
+//   16,384 rows, D 5,120: 112 us, 5.3 TB/s. 32 instructions a value (11 of them in the
+//     quantization, 9 in the sum of squares and its root), beside HBM: without any one part it is 101
+//     to 107. With a loop that reads rows again 175, with each warp adding up all warps' sums 125,
+//     with the next row's copies ahead but in registers, so that fewer CTAs fit, 174.
+//     D 4,096: 84 us, 5.6 TB/s.
 //   256 rows, D 4,096, the residual in f32: 4.5 us; 1 row 2.6 us: launch and a chain of waits.
 //   1,000 rows, D 4,112, all f32: 17 us, 3.1 TB/s: two CTAs of 288 threads fit an SM's shared memory
 //     with the next rows' copies, and 1,000 rows are three and a third of what they take at a time.

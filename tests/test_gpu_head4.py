@@ -179,6 +179,27 @@ def test_head4_special_values(cuda, M):
     assert bool(out[bad].isnan().all()) and torch.equal(out[~bad], want[~bad]) and bool((out[5][~bad[5]] == 0).all())
 
 
+def test_head4_far_rows(cuda):
+    """Logits more than 2^31 values behind the first, free and under a grammar."""
+    import torch
+    M, V, D = 16500, 131072, 64
+    g = torch.Generator(device=cuda)
+    g.manual_seed(3)
+    x = T.trie_head4_quantize(torch.randn(M, D, generator=g, device=cuda))
+    w = T.trie_head4_quantize(torch.randn(V, D, generator=g, device=cuda))
+    out = torch.empty(M, V, dtype=torch.bfloat16, device=cuda)
+    T.trie_head4_logits(*x, *w, out)
+    first = M // 128 * 128
+    last = (x[0][first:], x[1][first // 128:], x[2][first:])
+    _check(last, w, D, out[first:])
+    allowed = np.zeros((2, V), bool)
+    allowed[0, 5::9999] = True
+    mask = torch.from_numpy(lref.pack(allowed)).to(cuda)
+    states = torch.zeros(M, dtype=torch.int32, device=cuda)
+    T.trie_head4_logits(*x, *w, out, mask, states)
+    _check(last, w, D, out[first:], torch.from_numpy(allowed[0]).to(cuda).expand(M - first, V))
+
+
 def test_head4_repeats_and_graphs(cuda):
     """The same bits every time, alone, on a side stream and replayed from a graph on new hidden states."""
     import torch

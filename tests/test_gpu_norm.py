@@ -75,6 +75,48 @@ def test_norm(cuda, M, D, dtype, residual, bits):
     same(got, y)
 
 
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("dtype,residual", [("bf16", "bf16"), ("bf16", "f32"), ("f32", None)])
+@pytest.mark.parametrize("M,D", [(5000, 64), (3000, 1040), (1500, 4096), (700, 8192), (700, 8200)])
+def test_norm_many_rows(cuda, M, D, dtype, residual, bits):
+    """More rows than CTAs: each goes over several."""
+    import torch
+    rng = np.random.default_rng([M, D, bits])
+    x = _rows(rng, M, D, dtype)
+    res = None if residual is None else _rows(rng, M, D, residual) * 3
+    gain = torch.from_numpy((1 + 0.3 * rng.normal(0, 1, D)).astype(np.float32))
+    y, h = ref.normed(x, res, gain, 1e-6)
+    there = None if res is None else res.to(cuda)
+    f, same = (T.trie_head_norm_quantize, _same8) if bits == 8 else (T.trie_head4_norm_quantize, _same4)
+    got = f(x.to(cuda), gain.to(cuda), there)
+    if res is not None:
+        assert torch.equal(there.cpu(), h)
+    same(got, y)
+
+
+def test_norm_far_rows(cuda):
+    """Rows more than 2^31 values behind the first."""
+    import torch
+    M, D = 526000, 4096
+    x = torch.zeros(M, D, dtype=torch.bfloat16, device=cuda)
+    res = torch.zeros(M, D, dtype=torch.bfloat16, device=cuda)
+    tail, rest = _rows(np.random.default_rng(1), 40, D, "bf16"), _rows(np.random.default_rng(2), 40, D, "bf16")
+    gain = torch.ones(D, device=cuda)
+    y, h = ref.normed(tail, rest, gain.cpu(), 1e-6)
+    for f in (T.trie_head_norm_quantize, T.trie_head4_norm_quantize):
+        x[-40:], res[-40:] = tail.to(cuda), rest.to(cuda)
+        got = f(x, gain, res)
+        assert torch.equal(res[-40:].cpu(), h)
+        if len(got) == 2:
+            _same8((got[0][-40:], got[1][:, M - 40:M]), y)
+        else:
+            code, s, row = ref.rows4(y)
+            assert torch.equal(got[2][-40:].cpu(), row)
+            first = (M - 40) // 128  # whole blocks of 128 rows from here on
+            mine, scales, _ = ref.unpack4(got[0][first * 128:], got[1][first:], got[2], D)
+            assert np.array_equal(mine[-40:], code) and torch.equal(scales[-40:], s)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("M,D", CASES)
 def test_quantize4(cuda, M, D, dtype):

@@ -254,13 +254,13 @@ def test_policy_strides(cuda, offset, pad, g_offset, g_pad, V, dtype):
     assert bool((x[:, V:] == 7).all())
 
 
-@pytest.mark.parametrize("dtype,V", [("bf16", 30011), ("f32", 70001), ("bf16", 700003)])
+@pytest.mark.parametrize("dtype,V", [("bf16", 3100), ("bf16", 30011), ("f32", 70001), ("f32", 280001), ("bf16", 700003)])
 @pytest.mark.parametrize("in_place", [False, True])
 def test_policy_many_rows(cuda, dtype, V, in_place):
     """More rows than are at work at a time, free rows and rows that allow few and many tokens one after the other."""
     import torch
     rng = np.random.default_rng([V, in_place])
-    B = 700 if V < 100000 else 40
+    B = 3000 if V < 4000 else 700 if V < 100000 else 40
     allowed = np.zeros((6, V), bool)
     allowed[0, rng.choice(V, 7, replace=False)] = True
     allowed[1, rng.choice(V, 500, replace=False)] = True
@@ -298,6 +298,26 @@ def test_policy_many_rows(cuda, dtype, V, in_place):
     bound = want.abs() * (2 * off + 260 * U + half) + 2.0 ** -133
     bound.scatter_add_(1, tokens[:, None], reach * off)
     assert float(((grad.double() - want).abs() - bound).max()) <= 0
+
+
+def test_policy_far_rows(cuda):
+    """Logits and gradients more than 2^31 values behind the first."""
+    import torch
+    B, V = 16500, 131072
+    rng = np.random.default_rng(1)
+    n = 24
+    logits = torch.zeros(B, V, dtype=torch.bfloat16, device=cuda)
+    tail = _logits(rng, n, V, "bf16")
+    logits[-n:] = tail.to(cuda)
+    one = np.ones(n, np.float32)
+    ok, tokens, old, refs, A, weights = _rows(rng, tail, one)
+    put = lambda a, fill: torch.cat([torch.full((B - n,), fill, dtype=torch.from_numpy(a).dtype), torch.from_numpy(a)]).to(cuda)  # noqa: E731
+    grad = torch.full_like(logits, math.nan)
+    losses, logprobs = T.trie_policy_loss(logits, put(tokens, 7), put(old, -math.log(V)), put(A, 0.0), ref_logprobs=put(refs, -math.log(V)),
+                                          weights=put(weights, 1.0), kl=0.05, grad=grad)
+    _check(tail.double().numpy(), (losses[-n:], logprobs[-n:]), grad[-n:], ok, tokens, old, refs, A, weights, one, 0.2, 0.2, 0.05)
+    assert float((logprobs[:-n] + math.log(V)).abs().max()) <= 1e-4
+    assert bool(grad[::97].isfinite().all())
 
 
 def test_policy_repeats_and_graphs(cuda):

@@ -140,3 +140,29 @@ def test_chain_captured(cuda):
         s.synchronize()
         for a, b in zip((*out, c.logits, c.grad), ref):
             assert torch.equal(a, b)
+
+
+def test_first_calls_are_captured(cuda):
+    """A process whose first calls are made under capture (what a call asks the runtime once is asked there)."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import sys, torch
+sys.path[:0] = [%r, %r]
+import test_gpu_policy_chain as C
+dev = torch.device("cuda:0")
+c = C.Chain(dev, 20, 2003, 4096, torch.bfloat16, 1)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    out = c.run()
+graph.replay()
+torch.cuda.synchronize()
+got = [t.clone() for t in (*out, c.logits, c.grad)]
+want = [*c.run(), c.logits, c.grad]
+assert all(torch.equal(a, b) for a, b in zip(got, want))
+print("same")
+""" % (os.path.dirname(os.path.dirname(os.path.abspath(__file__))), os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "same" in r.stdout, r.stderr[-2000:]
