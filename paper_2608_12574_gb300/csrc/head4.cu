@@ -15,7 +15,7 @@
 //   256 rows, V 152,064, D 4,096: 73 us, 5.9 TB/s, with the norm in front 75: HBM, whose reads are 128
 //     bytes of each of 128 rows at a time.
 //   1,000 rows, V 128,000, D 4,112: 204 us, 5.2 PFLOP/s; without its stores 183; the MMAs alone take
-//     120. f32 236 (in 8 bits 534), and V 128,011, whose rows start at any four bytes, 297: partial
+//     120. f32 236 (in 8 bits 534), and V 128,011, whose rows start at any four bytes, 288 to 297: partial
 //     sectors at every warp's 32 tokens, and a ring of four stages instead of five.
 //   256 constrained rows (15 tokens each), V 152,064, D 4,096, with the norm: 45 us, -inf to 78 MB behind a
 //     chain of waits, in which a token's scales are 64 sectors of their own.
@@ -167,7 +167,7 @@ __device__ __forceinline__ void store16(const HeadOut &a, const float *x, int32_
 
 // Rows that do not all start on 32-byte boundaries: a warp's tokens from v on (32 in 32
 // bits, 64 in bf16), turned in shared memory, a row an instruction: 1,000 rows, V
-// 128,011, f32 297 us, and 430 to 450 with eight tokens of four rows an instruction.
+// 128,011, f32 288 to 297 us, and 430 to 450 with eight tokens of four rows an instruction.
 template <typename T>
 __device__ __forceinline__ void store_turned(const HeadOut &a, const uint32_t *turn, int32_t m, int32_t rows, uint32_t some, int32_t v, int lane) {
     constexpr int kAtOnce = 8;  // rows read before the first is written
