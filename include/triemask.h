@@ -582,7 +582,8 @@ int trie_head4_norm_quantize(const void *d_x, int dtype, int64_t stride, void *d
  *   logits[m][v] = S[m] S[v] sum over blocks of 16 columns of s[m] s[v] times
  *                  the sum of q[m][k] w[v][k]
  * and -inf where row m's state does not allow v; sums in 32 bits, rounded once to
- * the logits' type. Any D in [1, 2^24]; M <= 65535.
+ * the logits' type. Weights are left out as in trie_head_logits. Any D in [1, 2^24];
+ * codes and scales 16-byte aligned; M <= 2^20.
  *   d_workspace  device, trie_head_workspace(M, V) bytes, 16-byte aligned; may
  *                be NULL without a mask */
 int trie_head4_logits(const uint8_t *d_q, const uint8_t *d_scales, const float *d_row_scales, const uint8_t *d_w,
