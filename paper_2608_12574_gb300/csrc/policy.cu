@@ -20,9 +20,11 @@
 //     for it: 583; two logits an instruction and what a row needs of its scalars read ahead: 470; 15
 //     working warps instead of 30, so that half as many instructions go into a row's own work: 393.)
 //     Without the gradient 219 us, 5.7 TB/s.
-//   1,024 rows, V 128,011, half of them constrained: 94 us, 4.3 TB/s of zeros, gradients
-//     and free rows' logits: a constrained row waits for its mask's words and then for its
-//     tokens' logits, and three rows of a cluster are on their way at a time.
+//   1,024 rows, V 128,011, half of them constrained: 86 us, 4.7 TB/s of zeros, gradients
+//     and free rows' logits (all free 94, 5.6 TB/s: 28 rows a cluster, beside the first one's chain and
+//     the last one's; all constrained 72): a constrained row waits for its mask's words and then for its tokens' logits, behind
+//     what the workers store, and three rows of a cluster are on their way at a time. The next row's
+//     words, asked for behind this row's logits, are 8 us of the 94 that it was.
 //   300 rows, V 262,144, f32: 109 us, 5.8 TB/s on the 112 SMs that clusters of 16 reach.
 //   64 rows, V 32,000, f32, no gradient: 5 us, a chain of waits (row, masses, slope).
 #include <math.h>
@@ -300,7 +302,9 @@ constexpr int kWorkers = 32 * kWorkerWarps;
 constexpr int kSender = kWorkerWarps, kFinisher = kSender + 1, kFirstBringer = kFinisher + 1;
 constexpr int kRowThreads = 32 * (kFirstBringer + kSlots);
 constexpr int kListed = 64;   // allowed tokens of a share that are listed, at most
-constexpr int kWordsAhead = 38;  // words of the mask that a lane reads at a time: 38,912 tokens, a share of bf16 logits
+constexpr int kWordsAhead = 38;  // words of the mask that a lane reads: 38,912 tokens, more than a share of bf16 logits
+constexpr int kWordsTogether = 8;  // of these, how many are looked at one by one if one of them is not 0
+static_assert(kMaxShare / 2 + 16 + 2 * 32 <= kWordsAhead * 32 * 32, "a share's words");
 constexpr int kTogether = 5;  // pieces that a worker adds up at a time
 
 // What the workers need to know of a row.
@@ -357,55 +361,62 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
     const int32_t rows = (a.B - cluster + a.clusters - 1) / a.clusters;
     if (warp >= kFirstBringer) {
         // Brings every a.slots-th row into its slot: what there is to know of it, and its share or the list of its
-        // allowed tokens. What does not need the slot comes before the wait for it.
+        // allowed tokens. What does not need the slot comes before the wait for it, and the next row's mask is on its
+        // way while this row's logits are waited for.
         const int slot = warp - kFirstBringer;
+        if (slot >= a.slots) return;
         RowIn<T> &i = in[slot];
-        uint32_t phase = 1;
+        uint32_t phase = 1, word[kWordsAhead];
         auto state_of = [&](int32_t r) { return a.g.mask && r < rows ? __ldg(a.g.states + cluster + r * a.clusters) : TRIE_STATE_FREE; };
         auto c_of = [&](int32_t r) { return 1.44269504f / temperature_of(a, cluster + min(r, rows - 1) * a.clusters); };
-        int32_t state = state_of(slot);
+        auto share_of = [&](int32_t r) { return Share<T>(a, cluster + min(r, rows - 1) * a.clusters, rank); };
+        auto read_words = [&](const Share<T> &s, const GrammarRow &row) {
+            if (row.kind != kAllowRow) return;
+            const int32_t w = (s.lo >> 5) + lane, n = ((s.hi + 31) >> 5) - w;
+#pragma unroll
+            for (int k = 0; k < kWordsAhead; k++) word[k] = 32 * k < n ? __ldg(row.words + w + 32 * k) : 0u;
+        };
+        int32_t state = state_of(slot), state_next = state_of(slot + a.slots);
         float c_next = c_of(slot);
-        for (int32_t r = slot; r < rows && slot < a.slots; r += a.slots, phase ^= 1) {
-            const int32_t b = cluster + r * a.clusters;
-            const Share<T> s(a, b, rank);
+        read_words(share_of(slot), grammar_state(a.g, state));
+        for (int32_t r = slot; r < rows; r += a.slots, phase ^= 1) {
+            const Share<T> s = share_of(r);
             const GrammarRow row = grammar_state(a.g, state);
             const float c = c_next;
-            state = state_of(r + a.slots);
             c_next = c_of(r + a.slots);
             int32_t listed = row.kind == kAllowAll ? -1 : 0, token[kListed / 32];  // token number n: lane n % 32's, n / 32
 #pragma unroll
             for (int k = 0; k < kListed / 32; k++) token[k] = -1;
-            for (int32_t w0 = s.lo >> 5; listed >= 0 && w0 * 32 < s.hi; w0 += kWordsAhead * 32) {
-                uint32_t word[kWordsAhead];
-                const bool read = row.kind == kAllowRow;
-#pragma unroll
-                for (int k = 0; k < kWordsAhead; k++) {  // all on their way at once
-                    const int32_t w = w0 + 32 * k + lane;
-                    word[k] = read && w * 32 < s.hi ? __ldg(row.words + w) : 0u;
+            auto list = [&](uint32_t bits, int32_t v) {  // of the tokens from v on
+                if (v < s.lo) bits &= ~0u << (s.lo - v);
+                if (v + 32 > s.hi) bits &= v < s.hi ? (1u << (s.hi - v)) - 1u : 0u;
+                if (listed + __popc(bits) > kListed) {
+                    listed = -1;
+                    return;
                 }
-#pragma unroll
-                for (int k = 0; k < kWordsAhead; k++) {
-                    const int32_t w = w0 + 32 * k + lane, v = w * 32;
-                    if (!read && w == (V - 1) >> 5) word[k] = row.word(w);
-                    if (v < s.lo) word[k] &= ~0u << (s.lo - v);
-                    if (v + 32 > s.hi) word[k] &= v < s.hi ? (1u << (s.hi - v)) - 1u : 0u;
-                }
-#pragma unroll
-                for (int k = 0; k < kWordsAhead; k++)
-                    for (uint32_t lanes = __ballot_sync(~0u, word[k] != 0u); lanes && listed >= 0; lanes &= lanes - 1) {
-                        const int from = __ffs(lanes) - 1;
-                        const uint32_t bits = __shfl_sync(~0u, word[k], from);
-                        if (listed + __popc(bits) > kListed) {
-                            listed = -1;
-                            break;
-                        }
-                        for (uint32_t rest = bits; rest; rest &= rest - 1, listed++)
-                            if (lane == listed % 32) {
-                                const int32_t v = (w0 + 32 * k + from) * 32 + __ffs(rest) - 1;
-                                if (listed < 32) token[0] = v;
-                                else token[1] = v;
-                            }
+                for (; bits; bits &= bits - 1, listed++)
+                    if (lane == listed % 32) {
+                        if (listed < 32) token[0] = v + __ffs(bits) - 1;
+                        else token[1] = v + __ffs(bits) - 1;
                     }
+            };
+            if (row.kind == kAllowRow) {
+                const int32_t w0 = s.lo >> 5;
+#pragma unroll
+                for (int k0 = 0; k0 < kWordsAhead; k0 += kWordsTogether) {
+                    uint32_t any = 0;
+#pragma unroll
+                    for (int k = k0; k < min(k0 + kWordsTogether, kWordsAhead); k++) any |= word[k];
+                    if (listed < 0 || !__any_sync(~0u, any != 0u)) continue;
+#pragma unroll
+                    for (int k = k0; k < min(k0 + kWordsTogether, kWordsAhead); k++)
+                        for (uint32_t lanes = __ballot_sync(~0u, word[k] != 0u); lanes && listed >= 0; lanes &= lanes - 1) {
+                            const int from = __ffs(lanes) - 1;
+                            list(__shfl_sync(~0u, word[k], from), (w0 + 32 * k + from) * 32);
+                        }
+                }
+            } else if (row.kind == kAllowEos && s.lo < s.hi && s.hi == V) {
+                list(row.word((V - 1) >> 5), (V - 1) >> 5 << 5);
             }
             float at_edge = -INFINITY;
             if (listed < 0) {
@@ -416,14 +427,20 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
             float x[kListed / 32];
             Mass mass = {-INFINITY, 0.0f};
 #pragma unroll
-            for (int k = 0; k < kListed / 32; k++) {
-                x[k] = lane + 32 * k < listed ? to_f32(s.x[token[k]]) : -INFINITY;
-                mass.top = fmaxf(mass.top, x[k]);
-            }
+            for (int k = 0; k < kListed / 32; k++) x[k] = lane + 32 * k < listed ? to_f32(s.x[token[k]]) : -INFINITY;
+            state = state_next;
+            state_next = state_of(r + 2 * a.slots);
+            read_words(share_of(r + a.slots), grammar_state(a.g, state));
+            mass.top = fmaxf(x[0], x[1]);
             const float off = mass.top == -INFINITY ? 0.0f : mass.top;
             mass.sum = exp2_of((x[0] - off) * c) + exp2_of((x[1] - off) * c);
             mass = warp_mass(mass, c);
             if (!__all_sync(~0u, bar_wait(freed + 8 * slot, phase, &gave_up))) break;
+            if (lane == 0 && listed < 0) {  // first: 4,096 rows 383 us, and 390 with the row's values before it
+                const uint32_t bytes = uint32_t(s.last - s.first) * 16u;
+                bar_expect_bytes(full + 8 * slot, bytes);
+                if (bytes) bulk_load(smem_addr(slots + slot * a.slot_bytes), s.pieces() + s.first, bytes, full + 8 * slot);
+            }
             if (lane < 16) i.edge[lane] = at_edge;
 #pragma unroll
             for (int k = 0; k < kListed / 32; k++) {
@@ -438,11 +455,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
                 i.c = c;
             }
             __syncwarp();
-            if (lane == 0) {
-                const uint32_t bytes = listed < 0 ? uint32_t(s.last - s.first) * 16u : 0u;
-                bar_expect(full + 8 * slot, bytes);
-                if (bytes) bulk_load(smem_addr(slots + slot * a.slot_bytes), s.pieces() + s.first, bytes, full + 8 * slot);
-            }
+            if (lane == 0) bar_arrive(full + 8 * slot);
         }
         return;
     }
