@@ -14,9 +14,8 @@
 //   64 rows, V 128,000, D 4,112: 57 us, 5.5 TB/s; 128 rows 60 (without sharing rows 73).
 //   256 rows, V 152,064, D 4,096: 73 us, 5.9 TB/s, with the norm in front 75: HBM, whose reads are 128
 //     bytes of each of 128 rows at a time.
-//   1,000 rows, V 128,000, D 4,112: 204 us, 5.2 PFLOP/s; without its stores 183; the MMAs alone take
-//     120. f32 236 (in 8 bits 534), and V 128,011, whose rows start at any four bytes, 288 to 297: partial
-//     sectors at every warp's 32 tokens, and a ring of four stages instead of five.
+//   1,000 rows, V 128,000, D 4,112: 202 us, 5.2 PFLOP/s; without its stores 183; the MMAs alone take
+//     120. f32 234 (in 8 bits 534). V 128,011, whose rows start at any two or four bytes: 218, f32 246.
 //   256 constrained rows (15 tokens each), V 152,064, D 4,096, with the norm: 45 us, -inf to 78 MB behind a
 //     chain of waits, in which a token's scales are 64 sectors of their own.
 #include <math.h>
@@ -67,8 +66,6 @@ template <bool kPair>
 constexpr int kFirstWarp4 = kPair ? 4 : 2;
 template <bool kPair>
 constexpr int kThreads4 = 32 * (kFirstWarp4<kPair> + kEpilogueWarps4<kPair>);
-// Words of a warp's turned block: 32 rows of 32 words (32 tokens in 32 bits, 64 in bf16), an odd number apart.
-constexpr int kTurnPitch = 33, kTurnWords = 32 * kTurnPitch;
 
 struct Head4Args : HeadOut {
     CUtensorMap map_w, map_q, map_ws, map_s;
@@ -77,7 +74,6 @@ struct Head4Args : HeadOut {
     int64_t row_bytes, tiles_k;  // of a row's codes; 64-column tiles of its scales
     int32_t blocks;              // stages of K
     int32_t m_tiles, tiles, box_rows, stages;  // as in HeadArgs
-    bool wide;                   // every row of logits starts on a 32-byte boundary
 };
 
 // Sum of 32 products and their blocks' scales. e2m1 products are multiples of 1/4 up to 36,
@@ -137,11 +133,11 @@ __device__ __forceinline__ float few_logit(const Head4Args &a, int32_t m, int32_
 
 // 16 tokens from v on of a warp's 32 rows from m on (of which `rows` are there, and
 // the bit of `some` is set), a row a thread, 32 bytes at a time.
-template <typename T>
+template <typename T, bool kWide>
 __device__ __forceinline__ void store16(const HeadOut &a, const float *x, int32_t m, int32_t rows, uint32_t some, int32_t v, int lane) {
     if (lane >= rows || !((some >> lane) & 1u)) return;
     T *mine = static_cast<T *>(a.logits) + (m + lane) * a.stride + v;
-    if (v + 16 > a.V) {
+    if (v + 16 > a.V || !kWide) {
 #pragma unroll
         for (int e = 0; e < 16; e++)
             if (v + e < a.V) mine[e] = from_f32<T>(x[e]);
@@ -165,46 +161,95 @@ __device__ __forceinline__ void store16(const HeadOut &a, const float *x, int32_
     }
 }
 
-// Rows that do not all start on 32-byte boundaries: a warp's tokens from v on (32 in 32
-// bits, 64 in bf16), turned in shared memory, a row an instruction: 1,000 rows, V
-// 128,011, f32 288 to 297 us, and 430 to 450 with eight tokens of four rows an instruction.
+// The same for rows that do not all start on 32-byte boundaries, 64 tokens of a row a thread: shifted, so that whole 32
+// bytes that lie on such a boundary are written at once; those that reach into the next 64 tokens too, by the thread
+// that has the first of them, where it reads the others (`next`). 1,000 rows, V 128,011, D 4,112: f32 246 us, bf16
+// 218; 278 and 242 without `next`, so that both sides' threads write a part; 290 and 261 turned in shared memory, a row an instruction.
 template <typename T>
-__device__ __forceinline__ void store_turned(const HeadOut &a, const uint32_t *turn, int32_t m, int32_t rows, uint32_t some, int32_t v, int lane) {
-    constexpr int kAtOnce = 8;  // rows read before the first is written
-    __syncwarp();
-    const int32_t n = min(a.V - v, 64);  // tokens there
-    if (rows < 32) some &= (1u << rows) - 1u;
-    char *out = static_cast<char *>(a.logits) + (m * a.stride + v) * int64_t(sizeof(T));
-    const int64_t step = a.stride * int64_t(sizeof(T));
-    turn += lane;
-#pragma unroll 1
-    for (int r0 = 0; r0 < rows; r0 += kAtOnce, out += kAtOnce * step, turn += kAtOnce * kTurnPitch) {
-        uint32_t w[kAtOnce];
+struct Shifted {
+    static constexpr int kPieces = kColumns * int(sizeof(T)) / 32;
+    char *at;              // where the next 32 bytes go
+    uint32_t ahead;        // bytes before the first of them
+    bool there, head, next;
+    uint32_t kept[8];
+    // head: whether the bytes ahead are this thread's
+    __device__ __forceinline__ Shifted(const HeadOut &a, int32_t m, int32_t v, bool there, bool head, bool next) : there(there), head(head), next(next) {
+        at = reinterpret_cast<char *>(static_cast<T *>(a.logits) + m * a.stride + v);
+        ahead = uint32_t(32 - (reinterpret_cast<uintptr_t>(at) & 31)) & 31u;
+        at += ahead;
+    }
+    // x behind the bytes ahead (15 words of it)
+    __device__ __forceinline__ void shift(uint32_t (&x)[16]) const {
+        if (sizeof(T) == 2) {
 #pragma unroll
-        for (int r = 0; r < kAtOnce; r++) w[r] = turn[r * kTurnPitch];
-        const uint32_t mine = some >> r0;
+            for (int i = 0; i < 16; i++) x[i] = ahead & 2u ? __funnelshift_r(x[i], i < 15 ? x[i + 1] : 0u, 16) : x[i];
+        }
 #pragma unroll
-        for (int r = 0; r < kAtOnce; r++) {
-            T *to = reinterpret_cast<T *>(out + r * step);
-            const bool there = (mine >> r) & 1u;
-            if (sizeof(T) == 4) {
-                if (there && lane < n) reinterpret_cast<uint32_t *>(to)[lane] = w[r];
-            } else {
-                // pairs of tokens from the first or, where a row starts at an odd 2 bytes, the second
-                const bool odd = reinterpret_cast<uintptr_t>(to) & 2;
-                const uint32_t next = __shfl_down_sync(~0u, w[r], 1);
-                const int32_t t = 2 * lane + odd;
-                uint16_t *half = reinterpret_cast<uint16_t *>(to);
-                if (there && odd && lane == 0 && n > 0) half[0] = uint16_t(w[r]);
-                if (there && t + 1 < n) *reinterpret_cast<uint32_t *>(half + t) = odd ? __funnelshift_r(w[r], next, 16) : w[r];
-                else if (there && t < n) half[t] = uint16_t(odd ? w[r] >> 16 : w[r]);
+        for (int d = 1; d <= 4; d *= 2)
+#pragma unroll
+            for (int i = 0; i + d < 16; i++) x[i] = ahead & (4u * d) ? x[i + d] : x[i];
+    }
+    // The next eight words, number `piece` of kPieces.
+    __device__ __forceinline__ void put(const uint32_t *w, int piece) {
+        if (piece > 0) {
+            uint32_t x[16];
+#pragma unroll
+            for (int i = 0; i < 16; i++) x[i] = i < 8 ? kept[i] : w[i - 8];
+            shift(x);
+            if (there) store_words(at, x, 8);
+            at += 32;
+            if (piece == kPieces - 1 && there && !next) {
+                if (ahead == 0u) store_words(at, x + 8, 8);
+                else store_few(at, x + 8, 32u - ahead);
             }
+        } else if (head && there) {
+            // `ahead` bytes, up to a boundary, so the smallest first
+            uint32_t x[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) x[i] = w[i];
+            if (sizeof(T) == 2 && (ahead & 2u)) {
+                *reinterpret_cast<uint16_t *>(at - ahead) = uint16_t(x[0]);
+#pragma unroll
+                for (int i = 0; i < 8; i++) x[i] = __funnelshift_r(x[i], i < 7 ? x[i + 1] : 0u, 16);
+            }
+#pragma unroll
+            for (int d = 1; d <= 4; d *= 2)
+                if (ahead & (4u * d)) {
+                    store_words(at - (ahead & ~(4u * d - 1u)), x, d);
+#pragma unroll
+                    for (int i = 0; i + d < 8; i++) x[i] = x[i + d];
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) kept[i] = w[i];
+    }
+    // `bytes` < 32 from a boundary on, so the largest first.
+    __device__ __forceinline__ static void store_few(char *to, uint32_t *x, uint32_t bytes) {
+#pragma unroll
+        for (int d = 4; d >= 1; d /= 2)
+            if (bytes & (4u * d)) {
+                store_words(to, x, d);
+                to += 4 * d;
+#pragma unroll
+                for (int i = 0; i + d < 8; i++) x[i] = x[i + d];
+            }
+        if (sizeof(T) == 2 && (bytes & 2u)) *reinterpret_cast<uint16_t *>(to) = uint16_t(x[0]);
+    }
+    __device__ __forceinline__ static void store_words(char *to, const uint32_t *x, int n) {
+        if (n == 8) {
+            const uint32_t r[8] = {x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]};
+            store32(to, r);
+        } else if (n == 4) {
+            *reinterpret_cast<uint4 *>(to) = make_uint4(x[0], x[1], x[2], x[3]);
+        } else if (n == 2) {
+            *reinterpret_cast<uint2 *>(to) = make_uint2(x[0], x[1]);
+        } else {
+            *reinterpret_cast<uint32_t *>(to) = x[0];
         }
     }
-    __syncwarp();
-}
+};
 
-template <typename T, bool kPair, int kShare>
+template <typename T, bool kPair, int kShare, bool kWide>
 __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_constant__ Head4Args a) {
     constexpr int NT = kTokens<kPair>;
     constexpr int kAccumulators = 256 / NT;  // the other 256 columns of tensor memory are for scales
@@ -214,7 +259,7 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
     static_assert(kHiddenColumns + kSteps * NT / 32 <= kSlotColumns, "a stage's scales fit a slot");
     extern __shared__ unsigned char dynamic_smem[];
     __shared__ uint64_t bars[2 * kMaxStages + 2 * kAccumulators];
-    __shared__ __align__(16) float token_scales[kEpilogue][kColumns];
+    __shared__ __align__(16) float token_scales[kEpilogue][kColumns + 16];  // and of the 16 tokens behind its own
     __shared__ uint32_t need[kNeedTiles / 32];
     __shared__ uint32_t tmem_base;
     __shared__ int gave_up;
@@ -281,18 +326,17 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
         const int quarter = warp & 3, column = (warp - kFirst) / 4 * kColumns;
         const uint32_t from = tmem + (uint32_t(quarter * 32) << 16) + uint32_t(column);
         const uint32_t drain = kPair ? cluster_addr(drained, first_cta) : drained;
-        uint32_t *const turn = reinterpret_cast<uint32_t *>(dynamic_smem + (stages - smem_addr(dynamic_smem)) + a.stages * stage_bytes +
-                                                            (kRows - a.box_rows) * 128) + (warp - kFirst) * kTurnWords;  // only where not a.wide
         float *const tokens = token_scales[warp - kFirst];
         uint32_t it = 0;
         // a tile's scales, read while the tile before is stored
-        float row_next = 0.0f, token_next[2] = {0.0f, 0.0f};
+        float row_next = 0.0f, token_next[3] = {0.0f, 0.0f, 0.0f};
         auto read_scales = [&](int32_t t) {
             if (t >= a.tiles) return;
             const int32_t m = t % a.m_tiles * (kRows * kCtas) + rank * kRows + quarter * 32, v = (t / a.m_tiles * kShare + part) * NT + column;
             row_next = __ldg(a.q_rows + min(m + lane, a.M - 1));
             token_next[0] = __ldg(a.w_rows + min(v + lane, a.V - 1));
             token_next[1] = __ldg(a.w_rows + min(v + lane + 32, a.V - 1));
+            if (!kWide) token_next[2] = __ldg(a.w_rows + min(v + lane + 64, a.V - 1));
         };
         read_scales(unit);
         for (int32_t i = 0, t = unit; t < a.tiles; i++, t += units) {
@@ -301,6 +345,7 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
             const float row_scale = row_next;
             tokens[lane] = token_next[0];
             tokens[lane + 32] = token_next[1];
+            if (!kWide && lane < 16) tokens[lane + 64] = token_next[2];
             read_scales(t + units);
             __syncwarp();
             if (!needed(i)) {
@@ -314,7 +359,43 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
             bar_wait(ready + 8 * acc, (it / kAccumulators) & 1, &gave_up);
             it++;
             tcgen05_fence_after();
-            uint32_t raw[kColumns / 16][16];
+            const bool ok = *static_cast<volatile int *>(&gave_up) == 0;
+            const GrammarRow allow = grammar_row(a.g, row);
+            // 16 tokens from v + c on
+            auto logits = [&](const uint32_t (&sums)[16], int c, float (&x)[16]) {
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    const float4 f = *reinterpret_cast<const float4 *>(tokens + c + e);
+                    x[e] = __uint_as_float(sums[e]) * row_scale * f.x;
+                    x[e + 1] = __uint_as_float(sums[e + 1]) * row_scale * f.y;
+                    x[e + 2] = __uint_as_float(sums[e + 2]) * row_scale * f.z;
+                    x[e + 3] = __uint_as_float(sums[e + 3]) * row_scale * f.w;
+                }
+                uint32_t bits = ~0u;
+                if (a.g.mask) bits = (v + c) >> 5 < a.g.W ? allow.word((v + c) >> 5) >> (c & 16) : 0u;
+                if (!ok || (bits & 0xFFFFu) != 0xFFFFu) {
+#pragma unroll
+                    for (int e = 0; e < 16; e++) {
+                        if (!ok) x[e] = __int_as_float(0x7FFFFFFF);  // gave up waiting: no result
+                        if (!((bits >> e) & 1u)) x[e] = -INFINITY;
+                    }
+                }
+            };
+            auto word = [](const float (&x)[16], int i) {
+                const __nv_bfloat162 both = __floats2bfloat162_rn(x[2 * i % 16], x[2 * i % 16 + 1]);
+                return sizeof(T) == 4 ? __float_as_uint(x[i]) : *reinterpret_cast<const uint32_t *>(&both);
+            };
+            // what this warp needs of the tokens behind its own, where they are all there and it is to write some of them
+            const bool next = !kWide && column + kColumns < NT && v + 2 * kColumns <= a.V;
+            uint32_t raw[kColumns / 16][16], following[8];
+            if (there && next) {
+                tmem_load16(from + acc * NT + kColumns, raw[0]);
+                tmem_wait_ld();
+                float x[16];
+                logits(raw[0], kColumns, x);
+#pragma unroll
+                for (int i = 0; i < 8; i++) following[i] = word(x, i);
+            }
             if (there) {
 #pragma unroll
                 for (int c = 0; c < kColumns / 16; c++) tmem_load16(from + acc * NT + 16 * c, raw[c]);
@@ -326,44 +407,31 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
                 if (kPair) bar_arrive_remote(drain + 8 * acc);
                 else bar_arrive(drain + 8 * acc);
             }
-            const bool ok = *static_cast<volatile int *>(&gave_up) == 0;
             if (there) {
-                const GrammarRow allow = grammar_row(a.g, row);
                 const int32_t rows = min(32, m1 - mine);
                 uint32_t some = ~0u;
                 if (a.g.mask) some = __ballot_sync(~0u, __ldg(a.dense + row) != 0);
+                if (kWide || v + kColumns > a.V) {
 #pragma unroll
-                for (int c = 0; c < kColumns; c += 16) {
-                    float sum[16];
-#pragma unroll
-                    for (int e = 0; e < 16; e += 4) {
-                        const float4 f = *reinterpret_cast<const float4 *>(tokens + c + e);
-                        sum[e] = __uint_as_float(raw[c / 16][e]) * row_scale * f.x;
-                        sum[e + 1] = __uint_as_float(raw[c / 16][e + 1]) * row_scale * f.y;
-                        sum[e + 2] = __uint_as_float(raw[c / 16][e + 2]) * row_scale * f.z;
-                        sum[e + 3] = __uint_as_float(raw[c / 16][e + 3]) * row_scale * f.w;
+                    for (int c = 0; c < kColumns; c += 16) {
+                        float x[16];
+                        logits(raw[c / 16], c, x);
+                        if (v + c < a.V) store16<T, kWide>(a, x, mine, rows, some, v + c, lane);
                     }
-                    uint32_t bits = ~0u;
-                    if (a.g.mask) bits = (v + c) >> 5 < a.g.W ? allow.word((v + c) >> 5) >> (c & 16) : 0u;
-                    if (!ok || (bits & 0xFFFFu) != 0xFFFFu) {
+                } else {
+                    Shifted<T> shifted(a, mine + lane, v, lane < rows && ((some >> lane) & 1u), column == 0, next);
+                    constexpr int kWords = int(sizeof(T)) * 4;  // of 16 tokens
 #pragma unroll
-                        for (int e = 0; e < 16; e++) {
-                            if (!ok) sum[e] = __int_as_float(0x7FFFFFFF);  // gave up waiting: no result
-                            if (!((bits >> e) & 1u)) sum[e] = -INFINITY;
-                        }
-                    }
-                    if (a.wide) {
-                        if (v + c < a.V) store16<T>(a, sum, mine, rows, some, v + c, lane);
-                    } else {
+                    for (int c = 0; c < kColumns; c += 16) {
+                        float x[16];
+                        uint32_t w[kWords];
+                        logits(raw[c / 16], c, x);
 #pragma unroll
-                        for (int e = 0; e < 16; e += sizeof(T) == 4 ? 1 : 2) {
-                            const __nv_bfloat162 both = __floats2bfloat162_rn(sum[e], sum[e + 1 < 16 ? e + 1 : e]);
-                            if (sizeof(T) == 4) turn[lane * kTurnPitch + c % 32 + e] = __float_as_uint(sum[e]);
-                            else turn[lane * kTurnPitch + (c + e) / 2] = *reinterpret_cast<const uint32_t *>(&both);
-                        }
-                        if (sizeof(T) == 4 ? c % 32 == 16 : c == kColumns - 16)
-                            store_turned<T>(a, turn, mine, rows, some, sizeof(T) == 4 ? v + c - 16 : v, lane);
+                        for (int i = 0; i < kWords; i++) w[i] = word(x, i);
+#pragma unroll
+                        for (int i = 0; i < kWords; i += 8) shifted.put(w + i, (c / 16 * kWords + i) / 8);
                     }
+                    if (next) shifted.put(following, Shifted<T>::kPieces);
                 }
             }
             __syncwarp();  // the next tile's scales are written where these were read
@@ -492,16 +560,15 @@ bool make_scale_map(CUtensorMap *map, const void *base, int64_t rows, int64_t ti
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T, bool kPair, int kShare>
+template <typename T, bool kPair, int kShare, bool kWide>
 cudaError_t launch_head4(Head4Args a, cudaStream_t st) {
     const int stage = kWeightBytes4<kPair> + kHiddenScales + a.box_rows * 128;
     // the last stage's MMA reads kRows rows, whatever was loaded; and room to align the ring
     const int beyond = (kRows - a.box_rows) * 128 + 1024;
-    constexpr int fixed = kEpilogueWarps4<kPair> * int(sizeof(float)) * kColumns + 1024;  // declared in the kernel
-    const int turned = a.wide ? 0 : kEpilogueWarps4<kPair> * kTurnWords * 4;
-    a.stages = std::min(kMaxStages, (kHeadSmem - fixed - beyond - turned) / stage);
-    const int smem = a.stages * stage + beyond + turned;
-    const cudaError_t e = allow_smem<k_head4<T, kPair, kShare>, kHeadSmem - fixed>();
+    constexpr int fixed = kEpilogueWarps4<kPair> * int(sizeof(float)) * (kColumns + 16) + 1024;  // declared in the kernel
+    a.stages = std::min(kMaxStages, (kHeadSmem - fixed - beyond) / stage);
+    const int smem = a.stages * stage + beyond;
+    const cudaError_t e = allow_smem<k_head4<T, kPair, kShare, kWide>, kHeadSmem - fixed>();
     if (e != cudaSuccess) return e;
     constexpr int kCluster = (kPair ? 2 : 1) * kShare;
     // clusters of four do not reach every SM (36 of them, 144 CTAs, on 152); what is beyond waits its turn
@@ -519,7 +586,13 @@ cudaError_t launch_head4(Head4Args a, cudaStream_t st) {
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = kCluster > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, k_head4<T, kPair, kShare>, a);
+    return cudaLaunchKernelEx(&cfg, k_head4<T, kPair, kShare, kWide>, a);
+}
+
+template <typename T, bool kWide>
+cudaError_t launch_wide(const Head4Args &a, bool pair, int share, cudaStream_t st) {
+    if (pair) return share == 2 ? launch_head4<T, true, 2, kWide>(a, st) : launch_head4<T, true, 1, kWide>(a, st);
+    return share == 2 ? launch_head4<T, false, 2, kWide>(a, st) : launch_head4<T, false, 1, kWide>(a, st);
 }
 
 }  // namespace
@@ -565,7 +638,7 @@ extern "C" int trie_head4_logits(const uint8_t *d_q, const uint8_t *d_scales, co
     a.box_rows = std::min(kRows, (M + 15) / 16 * 16);
     a.logits = d_logits;
     a.stride = stride;
-    a.wide = ((reinterpret_cast<uintptr_t>(d_logits) | uintptr_t(stride * (dtype == TRIE_DTYPE_F32 ? 4 : 2))) & 31) == 0;
+    const bool wide = ((reinterpret_cast<uintptr_t>(d_logits) | uintptr_t(stride * (dtype == TRIE_DTYPE_F32 ? 4 : 2))) & 31) == 0;
     a.g = make_grammar(d_mask, mask_rows, d_states, V);
     if (!make_map(&a.map_w, d_w, V, a.row_bytes, 128) || !make_map(&a.map_q, d_q, M, a.row_bytes, a.box_rows / share) ||
         !make_scale_map(&a.map_ws, d_w_scales, V, a.tiles_k, kSteps) || !make_scale_map(&a.map_s, d_scales, M, a.tiles_k, kSteps / share))
@@ -586,10 +659,8 @@ extern "C" int trie_head4_logits(const uint8_t *d_q, const uint8_t *d_scales, co
                 : launch_pdl_smem(k_head_rows<__nv_bfloat16, Head4Args>, M, kRowThreads, smem, stream, a);
         if (e != cudaSuccess) return fail_launch(e, "4-bit head rows launch");
     }
-    if (pair && share == 2) e = f32 ? launch_head4<float, true, 2>(a, stream) : launch_head4<__nv_bfloat16, true, 2>(a, stream);
-    else if (pair) e = f32 ? launch_head4<float, true, 1>(a, stream) : launch_head4<__nv_bfloat16, true, 1>(a, stream);
-    else if (share == 2) e = f32 ? launch_head4<float, false, 2>(a, stream) : launch_head4<__nv_bfloat16, false, 2>(a, stream);
-    else e = f32 ? launch_head4<float, false, 1>(a, stream) : launch_head4<__nv_bfloat16, false, 1>(a, stream);
+    if (f32) e = wide ? launch_wide<float, true>(a, pair, share, stream) : launch_wide<float, false>(a, pair, share, stream);
+    else e = wide ? launch_wide<__nv_bfloat16, true>(a, pair, share, stream) : launch_wide<__nv_bfloat16, false>(a, pair, share, stream);
     if (e != cudaSuccess) return fail_launch(e, "4-bit head launch");
     return TRIE_OK;
 }

@@ -154,6 +154,30 @@ def test_head4_strides(cuda, M, offset, pad, dtype):
     assert bool((whole[:, V:] == 7).all()) and bool((buf[:offset] == 7).all()) and bool((buf[-8:] == 7).all())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,V", [(20, 700), (130, 64), (130, 127), (130, 323), (260, 1100)])
+def test_head4_row_starts(cuda, M, V, dtype):
+    """Rows that start anywhere between two 32-byte boundaries are those of aligned ones, with a grammar too, and
+    nothing beside them is written. The sums are the same ones, so all bits are."""
+    import torch
+    rng = np.random.default_rng([M, V])
+    D = 200
+    x, w = _inputs(rng, M, V, D, cuda)
+    # free rows among the others (-3), so that these are not dot products
+    mask = torch.from_numpy(lref.pack(rng.random((4, V)) < 0.7)).to(cuda)
+    states = torch.from_numpy(rng.choice([0, 1, 2, 3, -3], M).astype(np.int32)).to(cuda)
+    stride = (V + 15) // 16 * 16 + 16
+    for extra in ({}, {"mask": mask, "states": states}):
+        want = torch.empty(M, stride, dtype=_type(dtype), device=cuda)[:, :V]
+        T.trie_head4_logits(*x, *w, want, **extra)
+        for start in range(32 // want.element_size()):
+            buf = torch.full((M * stride + 32,), 7.0, dtype=_type(dtype), device=cuda)
+            rows = buf[start:start + M * stride].view(M, stride)
+            T.trie_head4_logits(*x, *w, rows[:, :V], **extra)
+            assert torch.equal(rows[:, :V], want), start
+            assert bool((rows[:, V:] == 7).all()) and bool((buf[:start] == 7).all()) and bool((buf[start + M * stride:] == 7).all())
+
+
 @pytest.mark.parametrize("M", [70, 200])
 def test_head4_special_values(cuda, M):
     """A row, or a token's weights, with NaN or an infinity has NaN logits and leaves the others alone; zeros give
