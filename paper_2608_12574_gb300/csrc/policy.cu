@@ -14,17 +14,18 @@
 //  k_policy       longer ones, and long ones without a gradient.
 //
 // What bounds it (times of calls that follow one another).
-//   4,096 rows, V 152,064, bf16, with the gradient: 381 to 393 us, 6.4 to 6.5 TB/s: HBM. (A
+//   4,096 rows, V 152,064, bf16, with the gradient: 371 us, 6.7 TB/s: HBM. (A
 //     CTA a row read twice: 2,210. Clusters with a row in registers, one row each:
 //     1,389. The clusters staying, but with every warp making every row's slope: 885; a warp of its own
 //     for it: 583; two logits an instruction and what a row needs of its scalars read ahead: 470; 15
-//     working warps instead of 30, so that half as many instructions go into a row's own work: 393.)
-//     Without the gradient 219 us, 5.7 TB/s.
+//     working warps instead of 30, so that half as many instructions go into a row's own work: 393; less unrolled: 371.)
+//     Without the gradient 225 us, 5.5 TB/s.
 //   1,024 rows, V 128,011, half of them constrained: 86 us, 4.7 TB/s of zeros, gradients
 //     and free rows' logits (all free 94, 5.6 TB/s: 28 rows a cluster, beside the first one's chain and
-//     the last one's; all constrained 72): a constrained row waits for its mask's words and then for its tokens' logits, behind
-//     what the workers store, and three rows of a cluster are on their way at a time. The next row's
+//     the last one's; all constrained 69): a constrained row waits for its mask's words and then for its tokens' logits,
+//     behind what the workers store, and three rows of a cluster are on their way at a time. The next row's
 //     words, asked for behind this row's logits, are 8 us of the 94 that it was.
+//   288 rows, V 35,776, all constrained: 11 us. (Words gone through one after the other by the whole warp: 21.)
 //   300 rows, V 262,144, f32: 109 us, 5.8 TB/s on the 112 SMs that clusters of 16 reach.
 //   64 rows, V 32,000, f32, no gradient: 5 us, a chain of waits (row, masses, slope).
 #include <math.h>
@@ -301,9 +302,9 @@ constexpr int kWorkerWarps = 15;
 constexpr int kWorkers = 32 * kWorkerWarps;
 constexpr int kSender = kWorkerWarps, kFinisher = kSender + 1, kFirstBringer = kFinisher + 1;
 constexpr int kRowThreads = 32 * (kFirstBringer + kSlots);
-constexpr int kListed = 64;   // allowed tokens of a share that are listed, at most
+constexpr int kListed = 128;  // allowed tokens of a share that are listed, at most
 constexpr int kWordsAhead = 38;  // words of the mask that a lane reads: 38,912 tokens, more than a share of bf16 logits
-constexpr int kWordsTogether = 8;  // of these, how many are looked at one by one if one of them is not 0
+constexpr int kWordsTogether = 8;  // of these, how many are gone through if one of them is not 0
 static_assert(kMaxShare / 2 + 16 + 2 * 32 <= kWordsAhead * 32 * 32, "a share's words");
 constexpr int kTogether = 5;  // pieces that a worker adds up at a time
 
@@ -312,10 +313,12 @@ template <typename T>
 struct RowIn {
     Share<T> share;
     GrammarRow row;
-    int32_t listed;   // >= 0: so many allowed tokens, listed here; -1: the share is in the slot
+    int32_t listed;   // >= 0: so many allowed tokens are listed in the slot; -1: the share is there
     Mass mass;        // of the listed tokens
     float c;          // log2(e) / temperature
     float edge[16];   // logits outside the pieces
+};
+struct List {
     int32_t token[kListed];
     float x[kListed];
 };
@@ -333,6 +336,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
     __shared__ Mass ranks[kRanks][kMaxCluster];
     __shared__ __align__(16) unsigned char in_bytes[kSlots * sizeof(RowIn<T>)];
     RowIn<T> *const in = reinterpret_cast<RowIn<T> *>(in_bytes);
+    __shared__ int32_t found[kSlots][kListed];  // a bringer's own
     __shared__ Slope slopes[2];
     __shared__ int gave_up;
     const uint32_t full = smem_addr(bars), freed = full + 8 * kSlots;  // of a slot
@@ -384,56 +388,66 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
             const GrammarRow row = grammar_state(a.g, state);
             const float c = c_next;
             c_next = c_of(r + a.slots);
-            int32_t listed = row.kind == kAllowAll ? -1 : 0, token[kListed / 32];  // token number n: lane n % 32's, n / 32
-#pragma unroll
-            for (int k = 0; k < kListed / 32; k++) token[k] = -1;
-            auto list = [&](uint32_t bits, int32_t v) {  // of the tokens from v on
-                if (v < s.lo) bits &= ~0u << (s.lo - v);
-                if (v + 32 > s.hi) bits &= v < s.hi ? (1u << (s.hi - v)) - 1u : 0u;
-                if (listed + __popc(bits) > kListed) {
-                    listed = -1;
-                    return;
-                }
-                for (; bits; bits &= bits - 1, listed++)
-                    if (lane == listed % 32) {
-                        if (listed < 32) token[0] = v + __ffs(bits) - 1;
-                        else token[1] = v + __ffs(bits) - 1;
-                    }
-            };
+            int32_t listed = row.kind == kAllowAll ? -1 : 0;
             if (row.kind == kAllowRow) {
-                const int32_t w0 = s.lo >> 5;
+                // every lane's words' tokens, one lane after the other
+                const int32_t v = ((s.lo >> 5) + lane) * 32, left = s.hi - v;  // left: tokens from its first word on
+                if (v < s.lo) word[0] &= ~0u << (s.lo - v);
+                int32_t mine = 0;
 #pragma unroll
-                for (int k0 = 0; k0 < kWordsAhead; k0 += kWordsTogether) {
-                    uint32_t any = 0;
+                for (int k = 0; k < kWordsAhead; k++) {
+                    const int32_t n = left - 1024 * k;
+                    if (n > 0 && n < 32) word[k] &= (1u << n) - 1u;
+                    mine += __popc(word[k]);
+                }
+                int32_t upto = mine;
 #pragma unroll
-                    for (int k = k0; k < min(k0 + kWordsTogether, kWordsAhead); k++) any |= word[k];
-                    if (listed < 0 || !__any_sync(~0u, any != 0u)) continue;
+                for (int d = 1; d < 32; d *= 2) {
+                    const int32_t before = __shfl_up_sync(~0u, upto, d);
+                    if (lane >= d) upto += before;
+                }
+                listed = __shfl_sync(~0u, upto, 31);
+                if (listed > kListed) {
+                    listed = -1;
+                } else if (mine) {
+                    int32_t *to = found[slot] + upto - mine;
 #pragma unroll
-                    for (int k = k0; k < min(k0 + kWordsTogether, kWordsAhead); k++)
-                        for (uint32_t lanes = __ballot_sync(~0u, word[k] != 0u); lanes && listed >= 0; lanes &= lanes - 1) {
-                            const int from = __ffs(lanes) - 1;
-                            list(__shfl_sync(~0u, word[k], from), (w0 + 32 * k + from) * 32);
-                        }
+                    for (int k0 = 0; k0 < kWordsAhead; k0 += kWordsTogether) {
+                        uint32_t any = 0;
+#pragma unroll
+                        for (int k = k0; k < min(k0 + kWordsTogether, kWordsAhead); k++) any |= word[k];
+                        if (!any) continue;
+#pragma unroll
+                        for (int k = k0; k < min(k0 + kWordsTogether, kWordsAhead); k++)
+                            for (uint32_t bits = word[k]; bits; bits &= bits - 1) *to++ = v + 1024 * k + __ffs(bits) - 1;
+                    }
                 }
             } else if (row.kind == kAllowEos && s.lo < s.hi && s.hi == V) {
-                list(row.word((V - 1) >> 5), (V - 1) >> 5 << 5);
+                listed = 1;
+                if (lane == 0) found[slot][0] = V - 1;
             }
+            __syncwarp();
             float at_edge = -INFINITY;
             if (listed < 0) {
                 const int32_t edge = lane < 16 ? s.edge(lane) : -1;
                 if (edge >= 0 && row.allows(edge)) at_edge = to_f32(s.x[edge]);
             }
-            static_assert(kListed == 64, "two tokens a lane");
+            int32_t token[kListed / 32];
             float x[kListed / 32];
             Mass mass = {-INFINITY, 0.0f};
 #pragma unroll
-            for (int k = 0; k < kListed / 32; k++) x[k] = lane + 32 * k < listed ? to_f32(s.x[token[k]]) : -INFINITY;
+            for (int k = 0; k < kListed / 32; k++) {
+                token[k] = lane + 32 * k < listed ? found[slot][lane + 32 * k] : 0;
+                x[k] = lane + 32 * k < listed ? to_f32(s.x[token[k]]) : -INFINITY;
+            }
             state = state_next;
             state_next = state_of(r + 2 * a.slots);
             read_words(share_of(r + a.slots), grammar_state(a.g, state));
-            mass.top = fmaxf(x[0], x[1]);
+#pragma unroll
+            for (int k = 0; k < kListed / 32; k++) mass.top = fmaxf(mass.top, x[k]);
             const float off = mass.top == -INFINITY ? 0.0f : mass.top;
-            mass.sum = exp2_of((x[0] - off) * c) + exp2_of((x[1] - off) * c);
+#pragma unroll
+            for (int k = 0; k < kListed / 32; k++) mass.sum += exp2_of((x[k] - off) * c);
             mass = warp_mass(mass, c);
             if (!__all_sync(~0u, bar_wait(freed + 8 * slot, phase, &gave_up))) break;
             if (lane == 0 && listed < 0) {  // first: 4,096 rows 383 us, and 390 with the row's values before it
@@ -442,10 +456,14 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
                 if (bytes) bulk_load(smem_addr(slots + slot * a.slot_bytes), s.pieces() + s.first, bytes, full + 8 * slot);
             }
             if (lane < 16) i.edge[lane] = at_edge;
+            if (listed >= 0) {
+                List &list = *reinterpret_cast<List *>(slots + slot * a.slot_bytes);
 #pragma unroll
-            for (int k = 0; k < kListed / 32; k++) {
-                i.token[lane + 32 * k] = token[k];
-                i.x[lane + 32 * k] = x[k];
+                for (int k = 0; k < kListed / 32; k++) {
+                    list.token[lane + 32 * k] = token[k];
+                    list.x[lane + 32 * k] = x[k];
+                }
+                async_fence();  // a copy may write there next
             }
             if (lane == 0) {
                 i.share = s;
@@ -582,7 +600,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
             if (edge >= 0) s.grad[edge] = from_f32<T>(edge == slope.token ? slope.at_token : slope_of(slope, in[slot].edge[worker]));
             const uint4 *from = reinterpret_cast<const uint4 *>(held);
             const int32_t at = slope.token < s.head ? -1 : (slope.token - s.head) / kSize - s.first;  // the token's piece
-#pragma unroll 5
+#pragma unroll 4  // 4,096 rows, V 152,064, bf16 371 us; 5: 392, 10: 485
             for (int32_t j = worker; j < n; j += kWorkers) {
                 Piece<T> p;
                 p.set(from[j]);
@@ -597,8 +615,9 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
         }
         const int32_t listed = slope.token >= 0 ? in[slot].listed : 0;
         if (worker < listed) {
-            const int32_t v = in[slot].token[worker];
-            s.grad[v] = from_f32<T>(v == slope.token ? slope.at_token : slope_of(slope, in[slot].x[worker]));
+            const List &list = *reinterpret_cast<const List *>(held);
+            const int32_t v = list.token[worker];
+            s.grad[v] = from_f32<T>(v == slope.token ? slope.at_token : slope_of(slope, list.x[worker]));
         }
     };
     int slot = 0, slot_next = 0;
@@ -606,13 +625,14 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
     auto step = [&] {
         if (++slot_next == a.slots) slot_next = 0, phase ^= 1;
     };
-    first_pass(0, 0, 0);
-    step();
-    for (int32_t r = 0; r < rows; r++) {
+#pragma unroll 1
+    for (int32_t r = -1; r < rows; r++) {
         if (r + 1 < rows) first_pass(r + 1, slot_next, phase);
-        second_pass(r, slot);
-        __syncwarp();
-        if (lane == 0) bar_arrive(freed + 8 * slot);
+        if (r >= 0) {
+            second_pass(r, slot);
+            __syncwarp();
+            if (lane == 0) bar_arrive(freed + 8 * slot);
+        }
         slot = slot_next;
         step();
     }
@@ -711,20 +731,20 @@ cudaError_t launch_policy(K kernel, const PolicyArgs &a, int64_t ctas, int threa
     return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
-// Clusters of k_policy_rows<T> of 1 << log_ctas CTAs that the current device runs at once.
+// Clusters of k_policy_rows<T> of so many CTAs that the current device runs at once.
 template <typename T>
-int active_clusters(int log_ctas) {
-    static std::atomic<int> known[16][5];
+int active_clusters(int ctas) {
+    static std::atomic<int> known[16][kMaxCluster + 1];
     int dev = 0, n = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 16) return 1;
-    if ((n = known[dev][log_ctas].load(std::memory_order_relaxed))) return n;
+    if ((n = known[dev][ctas].load(std::memory_order_relaxed))) return n;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(1u << log_ctas);
+    cfg.gridDim = dim3(unsigned(ctas));
     cfg.blockDim = dim3(kRowThreads);
     cfg.dynamicSmemBytes = size_t(kRowSmem);
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 1u << log_ctas;
+    attr[0].val.clusterDim.x = unsigned(ctas);
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
@@ -734,28 +754,32 @@ int active_clusters(int log_ctas) {
         cudaGetLastError();
         return 0;
     }
-    known[dev][log_ctas].store(n, std::memory_order_relaxed);
+    known[dev][ctas].store(n, std::memory_order_relaxed);
     return n;
 }
 
 template <typename T>
 cudaError_t run_policy(PolicyArgs a, cudaStream_t st) {
-    // The fewest CTAs a row of which three shares fit; more where the rows are few (8 rows of 32,000 in 32 bits
-    // with the gradient 5.1 us, and 6.3 with the fewest; 1 row 4.2 and 4.6).
     const int64_t pieces = int64_t(a.V) * int64_t(sizeof(T)) / 16;
     auto share = [&] { return (pieces + a.ctas - 1) / a.ctas * 16; };
-    // Without a gradient a row that would take 16 is read by k_policy, in one pass (300 rows of 200,000 in 32
+    // The fewest CTAs a row of which three shares fit, in even numbers: clusters of 5 reach more SMs than of 6 (140, and
+    // 138 of 152), but not all of them fit at once while the call before still holds SMs (1,085 rows of 152,296 in
+    // bf16 119 to 159 us, and 134; 168 by clusters of 8), and of 9 instead of 8 are no gain (500 rows of 150,000
+    // in 32 bits 109 us, and 99). Beyond 10 the largest, 7 of which reach 112 SMs (8 of 12 96): 300 rows of
+    // 220,000 in 32 bits 102 us, and 106.
+    while (a.ctas < kMaxCluster && share() > kMaxShare) a.ctas = a.ctas == 10 ? kMaxCluster : (a.ctas + 2) / 2 * 2;
+    a.clusters = 0;
+    // Without a gradient a row that takes more than 8 is read by k_policy, in one pass (300 rows of 200,000 in 32
     // bits 65 us, and 75 by clusters of 16; with the gradient 138 and 98).
-    const int most = a.grad ? kMaxCluster : kMaxCluster / 2;
-    int log_ctas = 0;
-    while (a.ctas < most && (share() > kMaxShare || (a.ctas < 8 && int64_t(a.B) * a.ctas * 2 <= sm_count() && share() > 16 * kRowThreads))) {
-        a.ctas *= 2;
-        log_ctas++;
+    if (share() <= kMaxShare && (a.grad || a.ctas <= kMaxCluster / 2)) {
+        // More where the rows are few (8 rows of 32,000 in 32 bits with the gradient 5.1 us, and 6.3 with the fewest;
+        // 1 row 4.2 and 4.6).
+        while (a.ctas <= kMaxCluster / 4 && int64_t(a.B) * a.ctas * 2 <= sm_count() && share() > 16 * kRowThreads) a.ctas *= 2;
+        a.clusters = std::min(a.B, active_clusters<T>(a.ctas));
     }
-    a.clusters = share() <= kMaxShare ? std::min(a.B, active_clusters<T>(log_ctas)) : 0;
     if (a.clusters) {
         const int rows = (a.B + a.clusters - 1) / a.clusters;
-        a.slot_bytes = std::max(128, int((share() + 127) / 128 * 128));
+        a.slot_bytes = std::max(int(sizeof(List)), int((share() + 127) / 128 * 128));
         a.slots = std::min(std::min(kSlots, rows), kRowSmem / a.slot_bytes);
         return launch_policy(k_policy_rows<T>, a, int64_t(a.clusters) * a.ctas, kRowThreads, a.slots * a.slot_bytes, st);
     }

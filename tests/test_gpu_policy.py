@@ -168,6 +168,52 @@ def test_policy_grammar(cuda, B, V, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V,in_place", [(2049, False), (4999, True), (36000, False)])
+def test_policy_numbers_of_tokens(cuda, V, in_place, dtype):
+    """Rows of few to several hundred allowed tokens: anywhere, in one piece at either end, 1,024 apart, and every
+    other one, which are all of some words."""
+    import torch
+    rng = np.random.default_rng([V, 7])
+    rows = []
+    for n in (1, 31, 32, 33, 64, 65, 127, 128, 129, 300):
+        for ids in (rng.choice(V, n, replace=False), np.arange(n), np.arange(V - n, V), (np.arange(n) * 1024 + 5) % V, 2 * np.arange(n)):
+            row = np.zeros(V, bool)
+            row[ids] = True
+            rows.append(row)
+    allowed = np.stack(rows)
+    B = len(rows) + 110  # enough for a CTA a row
+    states = np.concatenate([np.arange(len(rows)), rng.integers(-3, len(rows), 110)]).astype(np.int32)
+    logits = _logits(rng, B, V, dtype)
+    temperature = rng.choice([0.7, 1.0], B).astype(np.float32)
+    ok, tokens, old, refs, A, weights = _rows(rng, logits, temperature, allowed, states)
+    there = logits.to(cuda)
+    grad = there if in_place else torch.full_like(there, math.nan)
+    got = _run(cuda, there, tokens, old, refs, A, weights, temperature, grad, kl=0.05,
+               mask=torch.from_numpy(lref.pack(allowed)).to(cuda), states=torch.from_numpy(states).to(cuda))
+    _check(logits.double().numpy(), got, grad, ok, tokens, old, refs, A, weights, temperature, 0.2, 0.2, 0.05)
+
+
+@pytest.mark.parametrize("with_grad", [False, True])
+@pytest.mark.parametrize("B,V,dtype", [(40, 100001, "bf16"), (60, 160001, "bf16"), (40, 240003, "bf16"), (60, 110001, "f32"),
+                                       (30, 190001, "f32"), (20, 220001, "f32")])
+def test_policy_shares(cuda, B, V, dtype, with_grad):
+    """Rows shared by 4, 6, 8, 10 and 16 CTAs, more of them than are at work at once, some constrained."""
+    import torch
+    rng = np.random.default_rng([B, V, 2])
+    allowed = rng.random((4, V)) < np.array([3 / V, 40 / V, 900 / V, 0.5])[:, None]
+    allowed[:, V // 3] = True
+    states = rng.choice([0, 1, 2, 3, -3, -3, -3, -2], B).astype(np.int32)
+    logits = _logits(rng, B, V, dtype)
+    temperature = rng.choice([0.7, 1.0], B).astype(np.float32)
+    ok, tokens, old, refs, A, weights = _rows(rng, logits, temperature, allowed, states)
+    there = logits.to(cuda)
+    grad = torch.full_like(there, math.nan) if with_grad else None
+    got = _run(cuda, there, tokens, old, refs, A, weights, temperature, grad, kl=0.05,
+               mask=torch.from_numpy(lref.pack(allowed)).to(cuda), states=torch.from_numpy(states).to(cuda))
+    _check(logits.double().numpy(), got, grad, ok, tokens, old, refs, A, weights, temperature, 0.2, 0.2, 0.05)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("V", [40, 5003, 300001])
 def test_policy_special_values(cuda, V, dtype):
     """Rows with a NaN, an infinity, only -inf, one token of any weight, the type's ends; weight 0 beside a NaN."""
