@@ -13,18 +13,18 @@
 // a million, so that the 8- and 4-bit values, which lie next to rounding borders
 // by chance, do not depend on the order of the sum.
 //
-//  k_norm_rows  aligned rows: read once, held in registers.
+//  k_norm_rows  aligned rows, few or in bf16: read once, held in registers.
 //  k_norm_long  any others: read again in each pass.
 //
 // What bounds it (residual and x in bf16, 8 bits; times of calls that follow one another).
 //   16,384 rows, D 5,120: 112 us, 5.3 TB/s. 32 instructions a value (11 of them in the
 //     quantization, 9 in the sum of squares and its root), beside HBM: without any one part it is 101
-//     to 107. With a loop that reads rows again 175, with each warp adding up all warps' sums 125,
+//     to 107. With a loop that reads rows again 147, with each warp adding up all warps' sums 125,
 //     with the next row's copies ahead but in registers, so that fewer CTAs fit, 174.
-//     D 4,096: 84 us, 5.6 TB/s.
+//     D 4,096: 84 us, 5.6 TB/s. x and the residual in f32, D 8,192: 12,010 rows read again 211 us, 6.1 TB/s.
 //   256 rows, D 4,096, the residual in f32: 4.5 us; 1 row 2.6 us: launch and a chain of waits.
-//   1,000 rows, D 4,112, all f32: 17 us, 3.1 TB/s: two CTAs of 288 threads fit an SM's shared memory
-//     with the next rows' copies, and 1,000 rows are three and a third of what they take at a time.
+//   1,000 rows, D 4,112, all f32: 12.5 us, 4.3 TB/s: 1,000 CTAs at once, each a chain of three passes.
+//   4,924 rows, D 7,363, all f32: 120 us; a value at a time, as rows of this D lie, 198.
 #include <math.h>
 #include <stdint.h>
 #include <stdio.h>
@@ -42,7 +42,7 @@ namespace tmk {
 
 namespace {
 
-constexpr int kNormThreads = 256;  // where rows are read again
+constexpr int kNormThreads = 192;  // where rows are read again, at most: 16,384 rows, D 5,120, f32 without residual 107 us, and 117 of 256
 constexpr int kMaxThreads = 1024;  // of a row of one step a thread
 constexpr int kHoldThreads = 512;  // of more
 // A CTA stays where it has more rows than this: 16,384 rows, D 5,120 112 us, and 132 by a CTA a row; 4,000 rows 31 and 35.
@@ -84,6 +84,21 @@ __device__ __forceinline__ Raw load8(const void *row, bool f32, int32_t c, int32
         if (c < D) lo = at[0];
         if (c < D && f32) hi = at[1];
         r.w[0] = lo.x, r.w[1] = lo.y, r.w[2] = lo.z, r.w[3] = lo.w, r.w[4] = hi.x, r.w[5] = hi.y, r.w[6] = hi.z, r.w[7] = hi.w;
+    } else if (c >= kEach && c + 2 * kEach <= D) {  // the 16-byte pieces that they lie in are the row's, too
+        const char *from = static_cast<const char *>(row) + int64_t(c) * (f32 ? 4 : 2);
+        const uint32_t off = reinterpret_cast<uintptr_t>(from) & 15u;
+        const uint4 *at = reinterpret_cast<const uint4 *>(from - off);
+        const uint4 p0 = at[0], p1 = at[1], p2 = f32 ? at[2] : p1;
+        uint32_t u[12] = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w, p2.x, p2.y, p2.z, p2.w};
+#pragma unroll
+        for (int d = 1; d <= 2; d *= 2)
+#pragma unroll
+            for (int i = 0; i + d < 12; i++) u[i] = off & (4u * d) ? u[i + d] : u[i];
+#pragma unroll
+        for (int i = 0; i < kEach; i++) {
+            const uint32_t pair = off & 2u ? __funnelshift_r(u[i / 2], u[i / 2 + 1], 16) : u[i / 2];
+            r.w[i] = f32 ? u[i] : i & 1 ? pair >> 16 : pair & 0xFFFFu;
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < kEach; i++) {
@@ -126,6 +141,22 @@ __device__ __forceinline__ void store8(void *row, bool f32, int32_t c, int32_t D
         uint4 *at = reinterpret_cast<uint4 *>(static_cast<char *>(row) + int64_t(c) * (f32 ? 4 : 2));
         if (c < D) at[0] = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
         if (c < D && f32) at[1] = make_uint4(r.w[4], r.w[5], r.w[6], r.w[7]);
+    } else if (c + kEach <= D) {  // in pairs, from the second on where the first lies off a pair's boundary
+        char *to = static_cast<char *>(row) + int64_t(c) * (f32 ? 4 : 2);
+        const bool odd = reinterpret_cast<uintptr_t>(to) & (f32 ? 4u : 2u);
+        if (f32) {
+            if (odd) reinterpret_cast<uint32_t *>(to)[0] = r.w[0], reinterpret_cast<uint32_t *>(to)[7] = r.w[7];
+#pragma unroll
+            for (int i = 0; i < kEach; i += 2)
+                if (!odd) *reinterpret_cast<uint2 *>(to + 4 * i) = make_uint2(r.w[i], r.w[i + 1]);
+                else if (i < 6) *reinterpret_cast<uint2 *>(to + 4 * i + 4) = make_uint2(r.w[i + 1], r.w[i + 2]);
+        } else {
+            if (odd) reinterpret_cast<uint16_t *>(to)[0] = uint16_t(r.w[0]), reinterpret_cast<uint16_t *>(to)[7] = uint16_t(r.w[7]);
+#pragma unroll
+            for (int i = 0; i < kEach; i += 2)
+                if (!odd) *reinterpret_cast<uint32_t *>(to + 2 * i) = r.w[i] | r.w[i + 1] << 16;
+                else if (i < 6) *reinterpret_cast<uint32_t *>(to + 2 * i + 2) = r.w[i + 1] | r.w[i + 2] << 16;
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < kEach; i++)
@@ -300,6 +331,26 @@ __device__ __forceinline__ void put8(const NormArgs &a, int64_t m, int32_t c, co
     uint8_t *q = a.q + m * a.D + c;
     if (a.wide_q && c + kEach <= a.D) {
         *reinterpret_cast<uint2 *>(q) = make_uint2(out[0], out[1]);
+    } else if (c + kEach <= a.D) {  // as large as they can be, the same in all threads of a row
+        const uint32_t off = reinterpret_cast<uintptr_t>(q) & 3u;
+        if (off == 0) {
+            reinterpret_cast<uint32_t *>(q)[0] = out[0];
+            reinterpret_cast<uint32_t *>(q)[1] = out[1];
+        } else if (off == 2) {
+            *reinterpret_cast<uint16_t *>(q) = uint16_t(out[0]);
+            *reinterpret_cast<uint32_t *>(q + 2) = __funnelshift_r(out[0], out[1], 16);
+            *reinterpret_cast<uint16_t *>(q + 6) = uint16_t(out[1] >> 16);
+        } else if (off == 1) {
+            q[0] = uint8_t(out[0]);
+            *reinterpret_cast<uint16_t *>(q + 1) = uint16_t(out[0] >> 8);
+            *reinterpret_cast<uint32_t *>(q + 3) = __funnelshift_r(out[0], out[1], 24);
+            q[7] = uint8_t(out[1] >> 24);
+        } else {
+            q[0] = uint8_t(out[0]);
+            *reinterpret_cast<uint32_t *>(q + 1) = __funnelshift_r(out[0], out[1], 8);
+            *reinterpret_cast<uint16_t *>(q + 5) = uint16_t(out[1] >> 8);
+            q[7] = uint8_t(out[1] >> 24);
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < kEach; i++)
@@ -346,7 +397,7 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_long(const __grid_constan
     pdl_wait();
     const int lane = threadIdx.x & 31;
     const int32_t m = blockIdx.x, D = a.D, mine = int32_t(threadIdx.x) * kEach;
-    constexpr int32_t kStride = kNormThreads * kEach;
+    const int32_t stride = int32_t(blockDim.x) * kEach;
     const void *x = static_cast<const char *>(a.x) + m * a.stride * (a.x_f32 ? 4 : 2);
     void *residual = static_cast<char *>(a.residual) + m * a.residual_stride * (a.residual_f32 ? 4 : 2);
     const bool has_residual = kNorm && a.residual;
@@ -370,7 +421,7 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_long(const __grid_constan
     };
     if (kNorm) {
         Squares<false> all;
-        for (int32_t c = mine; c < D; c += kStride) {
+        for (int32_t c = mine; c < D; c += stride) {
             Two h[kEach / 2];
             values8<kWide>(load8<kWide>(x, a.x_f32, c, D), a.x_f32, h);
             if (has_residual) {
@@ -385,7 +436,7 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_long(const __grid_constan
         r = block_root(all.pair(), a, space);
         if (r < 0.0f) {
             double wide = 0.0;
-            for (int32_t c = mine; c < D; c += kStride) {
+            for (int32_t c = mine; c < D; c += stride) {
                 Two h[kEach / 2];
                 again(c, h);
                 wide += squares_of(h);
@@ -396,7 +447,7 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_long(const __grid_constan
     float row_scale = 0.0f, per_row = 0.0f;  // and its reciprocal
     if (kBits == 4) {
         uint32_t most = 0;
-        for (int32_t c = mine; c < D; c += kStride) {
+        for (int32_t c = mine; c < D; c += stride) {
             Two y[kEach / 2];
             normed(c, y);
             most = max(most, largest_of(y));
@@ -405,7 +456,7 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_long(const __grid_constan
         per_row = __frcp_rn(row_scale);
         if (threadIdx.x == 0) a.row_scales[m] = row_scale;
     }
-    for (int32_t c = mine; c - lane * kEach < (D + 127) / 128 * 128; c += kStride) {
+    for (int32_t c = mine; c - lane * kEach < (D + 127) / 128 * 128; c += stride) {
         Two y[kEach / 2];
         normed(c, y);
         if (kBits == 8) put8(a, m, c, y);
@@ -421,6 +472,13 @@ __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_
 template <int kLeft>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
 
+// Threads such that the rounds they take are about full.
+template <bool kWide, bool kNorm, int kBits>
+cudaError_t launch_long(const NormArgs &a, cudaStream_t st) {
+    const int32_t eights = (a.D + kEach - 1) / kEach, rounds = (eights + kNormThreads - 1) / kNormThreads;
+    return launch_pdl(k_norm_long<kWide, kNorm, kBits>, a.M, ((eights + rounds - 1) / rounds + 31) / 32 * 32, st, a);
+}
+
 struct None {};
 template <typename T>
 constexpr int kPieces = std::is_same<T, None>::value ? 0 : int(sizeof(T)) / 2;  // 16-byte pieces of eight columns
@@ -430,7 +488,7 @@ constexpr int kPieces = std::is_same<T, None>::value ? 0 : int(sizeof(T)) / 2;  
 // memory while they look at this one's. A thread copies and reads its own columns
 // only. TR: the residual's type, or None.
 template <typename TX, typename TR, bool kNorm, int kBits, int kSteps>
-__global__ void __launch_bounds__(kSteps == 1 ? kMaxThreads : kSteps == 2 ? kHoldThreads : 256, kSteps == 2 ? 2 : kSteps == 4 ? 3 : 1)
+__global__ void __launch_bounds__(kSteps == 1 ? kMaxThreads : kHoldThreads, kSteps)
     k_norm_rows(const __grid_constant__ NormArgs a) {
     constexpr bool kResidual = !std::is_same<TR, None>::value;
     using R = typename std::conditional<kResidual, TR, float>::type;
@@ -536,13 +594,13 @@ cudaError_t launch_held(NormArgs a, int threads, cudaStream_t st) {
     auto space = [&](int buffers) {
         return size_t(threads) * kSteps * (buffers * (kPieces<TX> + kPieces<TR>) * sizeof(uint4) + (kNorm ? kEach * sizeof(float) : 0));
     };
-    // CTAs that stay, as many as fit an SM by threads (64 registers each; 80 with four
-    // steps) and shared memory; where they would take few rows each, a CTA a row.
-    const int fit = std::max(1, std::min((kSteps == 4 ? 768 : 1024) / threads, int(kMostSpace / (space(2) + 2048))));
+    // CTAs that stay, as many as fit an SM by threads (64 registers each) and shared
+    // memory; where they would take few rows each, a CTA a row.
+    const int fit = std::max(1, std::min(1024 / threads, int(kMostSpace / (space(2) + 2048))));
     const int64_t stay = int64_t(sm_count()) * fit;
     a.buffers = a.M > kStayRows * stay ? 2 : 1;
     const size_t smem = space(a.buffers);
-    if (smem > kMostSpace) return launch_pdl(k_norm_long<true, kNorm, kBits>, a.M, kNormThreads, st, a);
+    static_assert(size_t(kMaxThreads) * (2 * 4 * sizeof(uint4) + kEach * sizeof(float)) <= kMostSpace, "any row that is held");
     if (smem > 40 * 1024) {  // what is declared in the kernel counts towards the 48 KB that need no leave
         const cudaError_t e = allow_smem<k_norm_rows<TX, TR, kNorm, kBits, kSteps>, int(kMostSpace)>();
         if (e != cudaSuccess) return e;
@@ -556,12 +614,19 @@ cudaError_t launch_rows(const NormArgs &a, cudaStream_t st) {
     // us, and 6.1 in two steps). Else two, or four where two are not enough, so that what a warp does
     // for a row is shared by more of its columns.
     const int32_t eights = int32_t((int64_t(a.D) + 63) / 64 * 64 / kEach);
-    const int steps = eights <= (a.M <= 2 * sm_count() ? kMaxThreads : 64) ? 1 : eights <= 2 * kHoldThreads ? 2 : 4;
-    const int threads = ((eights + steps - 1) / steps + 31) / 32 * 32;
-    if (steps == 1) return launch_held<TX, TR, kNorm, kBits, 1>(a, threads, st);
-    if (steps == 2) return launch_held<TX, TR, kNorm, kBits, 2>(a, threads, st);
-    if (threads <= kNormThreads) return launch_held<TX, TR, kNorm, kBits, 4>(a, threads, st);
-    return launch_pdl(k_norm_long<true, kNorm, kBits>, a.M, kNormThreads, st, a);
+    auto threads = [&](int steps) { return ((eights + steps - 1) / steps + 31) / 32 * 32; };
+    if (a.M <= 2 * sm_count()) {
+        // Few rows: a step a thread, as many threads as that takes, for the shortest chain (256 rows, D 4,096 4.6
+        // us, and 6.1 in two steps).
+        if (eights <= kMaxThreads) return launch_held<TX, TR, kNorm, kBits, 1>(a, threads(1), st);
+    } else if constexpr (kPieces<TX> < 2 && kPieces<TR> < 2) {
+        // Many: two steps, so that what a warp does for a row is shared by more of its columns.
+        if (eights <= 64) return launch_held<TX, TR, kNorm, kBits, 1>(a, threads(1), st);
+        if (eights <= 2 * kHoldThreads) return launch_held<TX, TR, kNorm, kBits, 2>(a, threads(2), st);
+    }
+    // Longer rows; and many with 32-bit values, which take so much shared memory that too few CTAs fit (12,010 rows,
+    // D 8,192, x and the residual in f32 211 us, and 310 in two steps; in bf16 158 and 131).
+    return launch_long<true, kNorm, kBits>(a, st);
 }
 
 template <typename TX, bool kNorm, int kBits>
@@ -574,7 +639,7 @@ cudaError_t launch_typed(const NormArgs &a, cudaStream_t st) {
 
 template <bool kNorm, int kBits>
 int launch_norm(const NormArgs &a, cudaStream_t st) {
-    const cudaError_t e = !a.wide ? launch_pdl(k_norm_long<false, kNorm, kBits>, a.M, kNormThreads, st, a)
+    const cudaError_t e = !a.wide ? launch_long<false, kNorm, kBits>(a, st)
                           : a.x_f32 ? launch_typed<float, kNorm, kBits>(a, st) : launch_typed<__nv_bfloat16, kNorm, kBits>(a, st);
     return e == cudaSuccess ? TRIE_OK : fail_launch(e, "norm quantize launch");
 }
