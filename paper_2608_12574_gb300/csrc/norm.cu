@@ -21,7 +21,7 @@
 //     quantization, 9 in the sum of squares and its root), beside HBM: without any one part it is 101
 //     to 107. With a loop that reads rows again 147, with each warp adding up all warps' sums 125,
 //     with the next row's copies ahead but in registers, so that fewer CTAs fit, 174.
-//     D 4,096: 84 us, 5.6 TB/s. x and the residual in f32, D 8,192: 12,010 rows read again 211 us, 6.1 TB/s.
+//     D 4,096: 84 us, 5.6 TB/s. x and the residual in f32, D 8,192: 12,010 rows read again 205 us, 6.3 TB/s.
 //   256 rows, D 4,096, the residual in f32: 4.5 us; 1 row 2.6 us: launch and a chain of waits.
 //   1,000 rows, D 4,112, all f32: 12.5 us, 4.3 TB/s: 1,000 CTAs at once, each a chain of three passes.
 //   4,924 rows, D 7,363, all f32: 120 us; a value at a time, as rows of this D lie, 198.
@@ -42,7 +42,7 @@ namespace tmk {
 
 namespace {
 
-constexpr int kNormThreads = 192;  // where rows are read again, at most: 16,384 rows, D 5,120, f32 without residual 107 us, and 117 of 256
+constexpr int kNormThreads = 256;  // where many rows are read again, at most
 constexpr int kMaxThreads = 1024;  // of a row of one step a thread
 constexpr int kHoldThreads = 512;  // of more
 // A CTA stays where it has more rows than this: 16,384 rows, D 5,120 112 us, and 132 by a CTA a row; 4,000 rows 31 and 35.
@@ -388,8 +388,8 @@ __device__ __forceinline__ void put4(const NormArgs &a, int64_t m, int32_t c, co
 
 // Rows of any length and alignment, a CTA a row: read again in each pass (the
 // residual as it was written).
-template <bool kWide, bool kNorm, int kBits>
-__global__ void __launch_bounds__(kNormThreads) k_norm_long(const __grid_constant__ NormArgs a) {
+template <bool kWide, bool kFew, bool kNorm, int kBits>
+__global__ void __launch_bounds__(kFew ? kMaxThreads : kNormThreads) k_norm_long(const __grid_constant__ NormArgs a) {
     __shared__ RootSpace space;
     __shared__ double doubles[32];
     __shared__ uint32_t maxima[32];
@@ -472,11 +472,20 @@ __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_
 template <int kLeft>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
 
-// Threads such that the rounds they take are about full.
 template <bool kWide, bool kNorm, int kBits>
 cudaError_t launch_long(const NormArgs &a, cudaStream_t st) {
-    const int32_t eights = (a.D + kEach - 1) / kEach, rounds = (eights + kNormThreads - 1) / kNormThreads;
-    return launch_pdl(k_norm_long<kWide, kNorm, kBits>, a.M, ((eights + rounds - 1) / rounds + 31) / 32 * 32, st, a);
+    const int32_t eights = (a.D + kEach - 1) / kEach;
+    // Few rows: as many threads as there are eights (300 rows, D 7,363, f32 13 us, and 22 in more rounds).
+    if (a.M <= 2 * sm_count())
+        return launch_pdl(k_norm_long<kWide, true, kNorm, kBits>, a.M, std::min(kMaxThreads, (eights + 31) / 32 * 32), st, a);
+    // Many: the number that is idle least in the last round, of two rounds or more where there are so many (16,384
+    // rows, D 5,120, f32 without residual 160 threads 108 us, 256 117).
+    int threads = (std::min(eights, 128) + 31) / 32 * 32, least = (eights + threads - 1) / threads * threads;
+    for (int n = 160; n <= kNormThreads && n < eights; n += 32) {
+        const int32_t all = (eights + n - 1) / n * n;
+        if (all <= least) threads = n, least = all;
+    }
+    return launch_pdl(k_norm_long<kWide, false, kNorm, kBits>, a.M, threads, st, a);
 }
 
 struct None {};
@@ -625,7 +634,7 @@ cudaError_t launch_rows(const NormArgs &a, cudaStream_t st) {
         if (eights <= 2 * kHoldThreads) return launch_held<TX, TR, kNorm, kBits, 2>(a, threads(2), st);
     }
     // Longer rows; and many with 32-bit values, which take so much shared memory that too few CTAs fit (12,010 rows,
-    // D 8,192, x and the residual in f32 211 us, and 310 in two steps; in bf16 158 and 131).
+    // D 8,192, x and the residual in f32 205 us, and 310 in two steps; in bf16 158 and 131).
     return launch_long<true, kNorm, kBits>(a, st);
 }
 

@@ -94,6 +94,25 @@ def test_norm_many_rows(cuda, M, D, dtype, residual, bits):
     same(got, y)
 
 
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("dtype,residual", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16"), ("f32", "f32"), ("bf16", None),
+                                            ("f32", None)])
+@pytest.mark.parametrize("M,D", [(700, 1), (400, 7), (400, 25), (500, 41), (400, 1001), (330, 2050), (320, 4100), (350, 8), (350, 520),
+                                 (310, 6152)])
+def test_norm_many_odd_rows(cuda, M, D, dtype, residual, bits):
+    """More rows than twice the SMs, at every distance from a 16-byte boundary or at none."""
+    rng = np.random.default_rng([M, D])
+    x, res = _rows(rng, M, D, dtype), None if residual is None else _rows(rng, M, D, residual)
+    gain = _rows(rng, 1, D, dtype)[0]
+    y, h = ref.normed(x, res, gain, 1e-6)
+    there = None if res is None else res.to(cuda)
+    f, same = (T.trie_head_norm_quantize, _same8) if bits == 8 else (T.trie_head4_norm_quantize, _same4)
+    same(f(x.to(cuda), gain.to(cuda), there), y)
+    if res is not None:
+        import torch
+        assert torch.equal(there.cpu(), h)
+
+
 def test_norm_far_rows(cuda):
     """Rows more than 2^31 values behind the first."""
     import torch
