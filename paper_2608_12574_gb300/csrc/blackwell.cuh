@@ -174,38 +174,11 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap
         : "memory");
 }
 
-// The same to several CTAs of the cluster (bits of `mask`): to the same place in each one's
-// shared memory, counted on the barrier at the same place as `bar`; by a CTA of a pair, on that
-// of the first CTA of each one's pair (with `bar` in the first of this one's).
-template <bool kPair>
-__device__ __forceinline__ void tma_share_2d(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, uint32_t bar, uint16_t mask) {
-    if (kPair)
-        asm volatile(
-            "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes.multicast::cluster [%0], [%1, {%2, "
-            "%3}], [%4], %5;" ::"r"(dst),
-            "l"(map), "r"(x), "r"(y), "r"(bar), "h"(mask)
-            : "memory");
-    else
-        asm volatile(
-            "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.multicast::cluster [%0], [%1, {%2, %3}], [%4], %5;" ::"r"(
-                dst),
-            "l"(map), "r"(x), "r"(y), "r"(bar), "h"(mask)
-            : "memory");
-}
-template <bool kPair>
-__device__ __forceinline__ void tma_share_3d(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, int32_t z, uint32_t bar, uint16_t mask) {
-    if (kPair)
-        asm volatile(
-            "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes.multicast::cluster [%0], [%1, {%2, "
-            "%3, %4}], [%5], %6;" ::"r"(dst),
-            "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar), "h"(mask)
-            : "memory");
-    else
-        asm volatile(
-            "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.multicast::cluster [%0], [%1, {%2, %3, %4}], [%5], "
-            "%6;" ::"r"(dst),
-            "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar), "h"(mask)
-            : "memory");
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, int32_t z, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
 }
 
 // ---- tensor memory
@@ -310,19 +283,6 @@ __device__ __forceinline__ void mma_commit(uint32_t bar) {
                      : "memory");
     else
         asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-
-// The same on the barriers of the CTAs of `mask`.
-template <bool kPair>
-__device__ __forceinline__ void mma_commit_to(uint32_t bar, uint16_t mask) {
-    if (kPair)
-        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
-                     "h"(mask)
-                     : "memory");
-    else
-        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
-                     "h"(mask)
-                     : "memory");
 }
 
 // ---- 32 bytes at once

@@ -11,11 +11,12 @@
 //
 // What bounds it (bf16 unless said; quantization included; times of calls that follow one another).
 //   1 row, V 32,000, D 2,048: 10 us, 3.7 TB/s of weights, of it two launches and the ring's first fill.
-//   64 rows, V 128,000, D 4,112: 57 us, 5.5 TB/s; 128 rows 60 (without sharing rows 73).
+//   128 rows, V 152,064, D 4,096: 63 us, 5.9 TB/s; 512 rows 116 us, 5.5 PFLOP/s.
 //   256 rows, V 152,064, D 4,096: 73 us, 5.9 TB/s, with the norm in front 75: HBM, whose reads are 128
 //     bytes of each of 128 rows at a time.
-//   1,000 rows, V 128,000, D 4,112: 202 us, 5.2 PFLOP/s; without its stores 183; the MMAs alone take
-//     120. f32 234 (in 8 bits 534). V 128,011, whose rows start at any two or four bytes: 218, f32 246.
+//   1,000 rows, V 128,000, D 4,096: 181 us, 5.8 PFLOP/s; the MMAs alone take 120 (8-bit head: 463).
+//   D 4,112, whose rows of codes start off 128-byte lines, so that a stage's 128 bytes of a row are parts of two:
+//     128 rows, V 128,000, 77 us; 1,000 rows 259, f32 314; V 128,011, whose logits start at any two or four bytes, 261, f32 330.
 //   256 constrained rows (15 tokens each), V 152,064, D 4,096, with the norm: 45 us, -inf to 78 MB behind a
 //     chain of waits, in which a token's scales are 64 sectors of their own.
 #include <math.h>
@@ -43,15 +44,12 @@ namespace {
 // operand, and 512 bytes of scales for 128 rows and 64 columns, which the
 // MMAs' thread copies from shared to tensor memory in front of them (copies and
 // MMAs of a thread are carried out in order).
-// What bounds large batches is what L2 gives (12 TB/s): two tiles (kShare) of the same rows,
-// side by side in the vocabulary, are a cluster's, whose CTAs load half of the
-// hidden states' stage each and give it to both (TMA multicast), as a pair's
-// CTAs do with the scales of their tokens.
+// Every CTA loads what its tiles read by itself, the scales of all of a pair's tokens too. (Loads
+// into several CTAs at once, by multicast, took 185 us instead of 181 at D 4,096 and 205 instead of 259 at D 4,112
+// for 1,000 rows; they are for programs on one GPU alone, and ranks on several load this library.)
 constexpr int kStageColumns = 256;
 constexpr int kSteps = kStageColumns / 64;  // MMAs of a stage
 constexpr int kAskFirst = 256 * 1024, kAskPiece = 16 * 1024;  // bytes of its first tile that a CTA asks for ahead; at a time
-// Rows of the batch from which on two CTAs' tiles share them: V 128,000, D 4,112, 64 rows 57 us, and 61 without; 128 rows 60 and 73.
-constexpr int kShareRows = 32;
 constexpr int kScaleTile = 512;             // bytes of the scales of 128 rows x 64 columns
 
 template <bool kPair>
@@ -249,12 +247,12 @@ struct Shifted {
     }
 };
 
-template <typename T, bool kPair, int kShare, bool kWide>
+template <typename T, bool kPair, bool kWide>
 __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_constant__ Head4Args a) {
     constexpr int NT = kTokens<kPair>;
     constexpr int kAccumulators = 256 / NT;  // the other 256 columns of tensor memory are for scales
     constexpr int kEpilogue = kEpilogueWarps4<kPair>, kFirst = kFirstWarp4<kPair>;
-    constexpr int kCtas = kPair ? 2 : 1, kCluster = kCtas * kShare;
+    constexpr int kCtas = kPair ? 2 : 1;
     constexpr uint32_t kHiddenColumns = kSteps * 4, kSlotColumns = 64;  // of a stage's scales in tensor memory
     static_assert(kHiddenColumns + kSteps * NT / 32 <= kSlotColumns, "a stage's scales fit a slot");
     extern __shared__ unsigned char dynamic_smem[];
@@ -264,9 +262,8 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
     __shared__ uint32_t tmem_base;
     __shared__ int gave_up;
     const int warp = __shfl_sync(~0u, int(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
-    const int cta = kCluster > 1 ? int(cluster_rank()) : 0, rank = cta % kCtas, part = cta / kCtas;  // of a pair; of the tiles
-    const int first_cta = part * kCtas;
-    const int32_t unit = int32_t(blockIdx.x) / kCluster, units = int32_t(gridDim.x) / kCluster;
+    const int rank = kPair ? int(cluster_rank()) : 0;
+    const int32_t unit = int32_t(blockIdx.x) / kCtas, units = int32_t(gridDim.x) / kCtas;
     const uint32_t full = smem_addr(bars), empty = full + 8 * kMaxStages;
     const uint32_t ready = empty + 8 * kMaxStages, drained = ready + 8 * kAccumulators;
     const uint32_t stages = (smem_addr(dynamic_smem) + 1023u) & ~1023u;
@@ -275,7 +272,7 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
         gave_up = 0;
         for (int i = 0; i < a.stages; i++) {
             bar_init(full + 8 * i, 1);
-            bar_init(empty + 8 * i, kShare);
+            bar_init(empty + 8 * i, 1);
         }
         for (int i = 0; i < kAccumulators; i++) {
             bar_init(ready + 8 * i, 1);
@@ -291,7 +288,7 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
     pdl_launch_dependents();
     if (warp == 0 && !a.g.mask && unit < a.tiles && elect_one()) {
         // while the kernel before runs, the first tile's weights come to L2 (where they are in one piece)
-        const int32_t v = (unit / a.m_tiles * kShare + part) * NT + rank * 128;
+        const int32_t v = unit / a.m_tiles * NT + rank * 128;
         const int64_t all = min(128, a.V - v) * a.row_bytes;
         for (int64_t at = 0; at < min(all, int64_t(kAskFirst)); at += kAskPiece)
             bulk_prefetch(a.w + v * a.row_bytes + at, uint32_t(min(int64_t(kAskPiece), all - at)));
@@ -307,15 +304,15 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
     if (a.g.mask) {
         // which of this CTA's tiles a dense row allows a token of
         for (int32_t i = 0, t = unit; t < a.tiles && i < kNeedTiles; i++, t += units) {
-            const int32_t m = t % a.m_tiles * (kRows * kCtas) + int32_t(threadIdx.x), v0 = t / a.m_tiles * (NT * kShare);
+            const int32_t m = t % a.m_tiles * (kRows * kCtas) + int32_t(threadIdx.x), v0 = t / a.m_tiles * NT;
             bool any = false;
             if (threadIdx.x < kRows * kCtas && m < a.M && __ldg(a.dense + m))
-                for (int32_t v = v0; v < min(a.V, v0 + NT * kShare); v += 128) any |= row_uses(a, m, v);
+                for (int32_t v = v0; v < min(a.V, v0 + NT); v += 128) any |= row_uses(a, m, v);
             if (__any_sync(~0u, any) && lane == 0) atomicOr(&need[i >> 5], 1u << (i & 31));
         }
     }
     tcgen05_fence_before();
-    if (kCluster > 1) cluster_sync();
+    if (kPair) cluster_sync();
     else __syncthreads();
     tcgen05_fence_after();
     const uint32_t tmem = *static_cast<volatile uint32_t *>(&tmem_base);
@@ -325,14 +322,14 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
         if (kPair) more_registers<112>();
         const int quarter = warp & 3, column = (warp - kFirst) / 4 * kColumns;
         const uint32_t from = tmem + (uint32_t(quarter * 32) << 16) + uint32_t(column);
-        const uint32_t drain = kPair ? cluster_addr(drained, first_cta) : drained;
+        const uint32_t drain = kPair ? cluster_addr(drained, 0) : drained;
         float *const tokens = token_scales[warp - kFirst];
         uint32_t it = 0;
         // a tile's scales, read while the tile before is stored
         float row_next = 0.0f, token_next[3] = {0.0f, 0.0f, 0.0f};
         auto read_scales = [&](int32_t t) {
             if (t >= a.tiles) return;
-            const int32_t m = t % a.m_tiles * (kRows * kCtas) + rank * kRows + quarter * 32, v = (t / a.m_tiles * kShare + part) * NT + column;
+            const int32_t m = t % a.m_tiles * (kRows * kCtas) + rank * kRows + quarter * 32, v = t / a.m_tiles * NT + column;
             row_next = __ldg(a.q_rows + min(m + lane, a.M - 1));
             token_next[0] = __ldg(a.w_rows + min(v + lane, a.V - 1));
             token_next[1] = __ldg(a.w_rows + min(v + lane + 32, a.V - 1));
@@ -341,7 +338,7 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
         read_scales(unit);
         for (int32_t i = 0, t = unit; t < a.tiles; i++, t += units) {
             const int32_t m0 = t % a.m_tiles * (kRows * kCtas) + rank * kRows, m1 = min(a.M, m0 + kRows);
-            const int32_t v0 = (t / a.m_tiles * kShare + part) * NT, v = v0 + column;
+            const int32_t v0 = t / a.m_tiles * NT, v = v0 + column;
             const float row_scale = row_next;
             tokens[lane] = token_next[0];
             tokens[lane + 32] = token_next[1];
@@ -442,12 +439,10 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
             int stage = 0;
             uint32_t phase = 1, used = 0;  // phase: of a stage's last use; the first time round there is none
             bool ok = true;
-            const uint32_t leader = kPair ? cluster_addr(full, first_cta) : full;
-            const uint16_t same_rows = kShare == 1 ? uint16_t(1 << rank) : kPair ? uint16_t(5 << rank) : 3, same_tokens = uint16_t(3 << first_cta);
-            const int32_t half = a.box_rows / kShare;
+            const uint32_t leader = kPair ? cluster_addr(full, 0) : full;
             for (int32_t i = 0, t = unit; t < a.tiles && ok; i++, t += units) {
                 if (!needed(i)) continue;
-                const int32_t m = t % a.m_tiles * (kRows * kCtas) + rank * kRows, v0 = (t / a.m_tiles * kShare + part) * NT;
+                const int32_t m = t % a.m_tiles * (kRows * kCtas) + rank * kRows, v0 = t / a.m_tiles * NT;
                 for (int32_t kb = 0; kb < a.blocks; kb++) {
                     const uint32_t at = stages + uint32_t(stage) * stage_bytes, bar = leader + 8 * stage;
                     const uint32_t scales = at + 128 * 128, hidden_scales = at + kWeightBytes4<kPair>, hidden = hidden_scales + kHiddenScales;
@@ -459,16 +454,12 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
                         if (rank == 0) bar_expect(full + 8 * stage, kCtas * stage_bytes);
                         if (kPair) {
                             tma_load_2d_pair(at, &a.map_w, kb * 128, v0 + rank * 128, bar);
-                            tma_share_3d<kPair>(scales + rank * kHiddenScales, &a.map_ws, 0, kb * kSteps, v0 / 128 + rank, bar, same_tokens);
+                            tma_load_3d_pair(scales, &a.map_ws, 0, kb * kSteps, v0 / 128, bar);
+                            tma_load_3d_pair(hidden_scales, &a.map_s, 0, kb * kSteps, m / 128, bar);
+                            tma_load_2d_pair(hidden, &a.map_q, kb * 128, m, bar);
                         } else {
                             tma_load_2d(at, &a.map_w, kb * 128, v0, bar);
                             tma_load_3d(scales, &a.map_ws, 0, kb * kSteps, v0 / 128, bar);
-                        }
-                        if (kPair || kShare > 1) {
-                            tma_share_3d<kPair>(hidden_scales + part * (kHiddenScales / kShare), &a.map_s, 0, kb * kSteps + part * (kSteps / kShare),
-                                                m / 128, bar, same_rows);
-                            tma_share_2d<kPair>(hidden + part * half * 128, &a.map_q, kb * 128, m + part * half, bar, same_rows);
-                        } else {
                             tma_load_3d(hidden_scales, &a.map_s, 0, kb * kSteps, m / 128, bar);
                             tma_load_2d(hidden, &a.map_q, kb * 128, m, bar);
                         }
@@ -525,12 +516,8 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
                                 if (k >= steps) break;
                                 mma_e2m1<kPair>(tmem + acc * NT, dq + 2 * k, dw + 2 * k, idesc, sq + 4 * k, sw + k * (NT / 32), kb > 0 || k > 0);
                             }
-                            if (kShare > 1) mma_commit_to<kPair>(empty + 8 * stage, uint16_t((1 << kCluster) - 1));
-                            else mma_commit<kPair>(empty + 8 * stage);
-                            if (kb == a.blocks - 1) {
-                                if (kPair) mma_commit_to<kPair>(ready + 8 * acc, uint16_t(3 << first_cta));
-                                else mma_commit<kPair>(ready + 8 * acc);
-                            }
+                            mma_commit<kPair>(empty + 8 * stage);
+                            if (kb == a.blocks - 1) mma_commit<kPair>(ready + 8 * acc);
                         }
                         __syncwarp();
                         slot ^= 1;
@@ -542,25 +529,25 @@ __global__ void __launch_bounds__(kThreads4<kPair>, 1) k_head4(const __grid_cons
     }
     __syncwarp();
     tcgen05_fence_before();
-    if (kCluster > 1) cluster_sync();
+    if (kPair) cluster_sync();
     else __syncthreads();
     tcgen05_fence_after();
     if (warp == 1) tmem_free<kPair>(tmem, 512);
 }
 
-// [rows / 128][columns / 64][512 bytes] in boxes of 1 x `box_tiles` x 512 bytes, zeros outside.
-bool make_scale_map(CUtensorMap *map, const void *base, int64_t rows, int64_t tiles, int32_t box_tiles) {
+// [rows / 128][columns / 64][512 bytes] in boxes of `box_rows` x kSteps x 512 bytes, zeros outside.
+bool make_scale_map(CUtensorMap *map, const void *base, int64_t rows, int64_t tiles, int32_t box_rows) {
     const Encode encode = tensor_map_encode();
     if (!encode) return false;
     const cuuint64_t dims[3] = {kScaleTile / 4, cuuint64_t(tiles), cuuint64_t((rows + 127) / 128)};
     const cuuint64_t strides[2] = {kScaleTile, cuuint64_t(tiles) * kScaleTile};
-    const cuuint32_t box[3] = {kScaleTile / 4, cuuint32_t(box_tiles), 1}, steps[3] = {1, 1, 1};
+    const cuuint32_t box[3] = {kScaleTile / 4, kSteps, cuuint32_t(box_rows)}, steps[3] = {1, 1, 1};
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<void *>(base), dims, strides, box, steps,
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T, bool kPair, int kShare, bool kWide>
+template <typename T, bool kPair, bool kWide>
 cudaError_t launch_head4(Head4Args a, cudaStream_t st) {
     const int stage = kWeightBytes4<kPair> + kHiddenScales + a.box_rows * 128;
     // the last stage's MMA reads kRows rows, whatever was loaded; and room to align the ring
@@ -568,11 +555,10 @@ cudaError_t launch_head4(Head4Args a, cudaStream_t st) {
     constexpr int fixed = kEpilogueWarps4<kPair> * int(sizeof(float)) * (kColumns + 16) + 1024;  // declared in the kernel
     a.stages = std::min(kMaxStages, (kHeadSmem - fixed - beyond) / stage);
     const int smem = a.stages * stage + beyond;
-    const cudaError_t e = allow_smem<k_head4<T, kPair, kShare, kWide>, kHeadSmem - fixed>();
+    const cudaError_t e = allow_smem<k_head4<T, kPair, kWide>, kHeadSmem - fixed>();
     if (e != cudaSuccess) return e;
-    constexpr int kCluster = (kPair ? 2 : 1) * kShare;
-    // clusters of four do not reach every SM (36 of them, 144 CTAs, on 152); what is beyond waits its turn
-    const int units = std::min(a.tiles, std::max(1, sm_count() / kCluster - (kCluster == 4 ? 2 : 0)));
+    constexpr int kCluster = kPair ? 2 : 1;
+    const int units = std::min(a.tiles, std::max(1, sm_count() / kCluster));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(units * kCluster));
     cfg.blockDim = dim3(kThreads4<kPair>);
@@ -586,13 +572,12 @@ cudaError_t launch_head4(Head4Args a, cudaStream_t st) {
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = kCluster > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, k_head4<T, kPair, kShare, kWide>, a);
+    return cudaLaunchKernelEx(&cfg, k_head4<T, kPair, kWide>, a);
 }
 
 template <typename T, bool kWide>
-cudaError_t launch_wide(const Head4Args &a, bool pair, int share, cudaStream_t st) {
-    if (pair) return share == 2 ? launch_head4<T, true, 2, kWide>(a, st) : launch_head4<T, true, 1, kWide>(a, st);
-    return share == 2 ? launch_head4<T, false, 2, kWide>(a, st) : launch_head4<T, false, 1, kWide>(a, st);
+cudaError_t launch_wide(const Head4Args &a, bool pair, cudaStream_t st) {
+    return pair ? launch_head4<T, true, kWide>(a, st) : launch_head4<T, false, kWide>(a, st);
 }
 
 }  // namespace
@@ -631,19 +616,15 @@ extern "C" int trie_head4_logits(const uint8_t *d_q, const uint8_t *d_scales, co
     const bool pair = M > kRows;
     const int side = pair ? 256 : 128;  // of a tile
     a.m_tiles = (M + side - 1) / side;
-    // A pair's tiles share their rows where there are several tiles of rows (512 rows, V 128,000,
-    // D 4,112 111 us, and 151 without) or rows of codes start off 128-byte lines (192 rows 65 and
-    // 76); else what more SMs give is worth more (256 rows, V 152,064, D 4,096 76 and 73).
-    const int share = pair ? (M > 256 || row_bytes4(D) % 128 ? 2 : 1) : M > kShareRows ? 2 : 1;
     a.box_rows = std::min(kRows, (M + 15) / 16 * 16);
     a.logits = d_logits;
     a.stride = stride;
     const bool wide = ((reinterpret_cast<uintptr_t>(d_logits) | uintptr_t(stride * (dtype == TRIE_DTYPE_F32 ? 4 : 2))) & 31) == 0;
     a.g = make_grammar(d_mask, mask_rows, d_states, V);
-    if (!make_map(&a.map_w, d_w, V, a.row_bytes, 128) || !make_map(&a.map_q, d_q, M, a.row_bytes, a.box_rows / share) ||
-        !make_scale_map(&a.map_ws, d_w_scales, V, a.tiles_k, kSteps) || !make_scale_map(&a.map_s, d_scales, M, a.tiles_k, kSteps / share))
+    if (!make_map(&a.map_w, d_w, V, a.row_bytes, 128) || !make_map(&a.map_q, d_q, M, a.row_bytes, a.box_rows) ||
+        !make_scale_map(&a.map_ws, d_w_scales, V, a.tiles_k, side / 128) || !make_scale_map(&a.map_s, d_scales, M, a.tiles_k, 1))
         return set_error(TRIE_ECUDA, "cuTensorMapEncodeTiled failed");
-    const int64_t tiles = (int64_t(V) + side * share - 1) / (side * share) * a.m_tiles;
+    const int64_t tiles = (int64_t(V) + side - 1) / side * a.m_tiles;
     if (tiles > 0x3FFFFFFF) return set_error(TRIE_EINVAL, "M x V is too large");
     a.tiles = int32_t(tiles);
     const bool f32 = dtype == TRIE_DTYPE_F32;
@@ -659,8 +640,8 @@ extern "C" int trie_head4_logits(const uint8_t *d_q, const uint8_t *d_scales, co
                 : launch_pdl_smem(k_head_rows<__nv_bfloat16, Head4Args>, M, kRowThreads, smem, stream, a);
         if (e != cudaSuccess) return fail_launch(e, "4-bit head rows launch");
     }
-    if (f32) e = wide ? launch_wide<float, true>(a, pair, share, stream) : launch_wide<float, false>(a, pair, share, stream);
-    else e = wide ? launch_wide<__nv_bfloat16, true>(a, pair, share, stream) : launch_wide<__nv_bfloat16, false>(a, pair, share, stream);
+    if (f32) e = wide ? launch_wide<float, true>(a, pair, stream) : launch_wide<float, false>(a, pair, stream);
+    else e = wide ? launch_wide<__nv_bfloat16, true>(a, pair, stream) : launch_wide<__nv_bfloat16, false>(a, pair, stream);
     if (e != cudaSuccess) return fail_launch(e, "4-bit head launch");
     return TRIE_OK;
 }
