@@ -22,7 +22,7 @@
 //     Without the gradient 225 us, 5.5 TB/s.
 //   1,024 rows, V 128,011, half of them constrained: 86 us, 4.7 TB/s of zeros, gradients
 //     and free rows' logits (all free 94, 5.6 TB/s: 28 rows a cluster, beside the first one's chain and
-//     the last one's; all constrained 69): a constrained row waits for its mask's words and then for its tokens' logits,
+//     the last one's; all constrained 70): a constrained row waits for its mask's words and then for its tokens' logits,
 //     behind what the workers store, and three rows of a cluster are on their way at a time. The next row's
 //     words, asked for behind this row's logits, are 8 us of the 94 that it was.
 //   288 rows, V 35,776, all constrained: 11 us. (Words gone through one after the other by the whole warp: 21.)
@@ -298,6 +298,10 @@ struct Share {
 //   the sender  a CTA's mass of a row to all CTAs of the cluster
 //   the finisher  the row's loss and slope from these
 // The gradient of a constrained row is zeros with the listed tokens' put in.
+// A warp whose wait gives up (no wait of a correct program does) goes no further, so that nothing is
+// taken for there that is not, and stays until all other warps of the cluster have ended or given up too:
+// these may still write to its CTA's shared memory. What it has not finished becomes NaN: the workers' gradients and the
+// finisher's losses, from that row on.
 constexpr int kWorkerWarps = 15;
 constexpr int kWorkers = 32 * kWorkerWarps;
 constexpr int kSender = kWorkerWarps, kFinisher = kSender + 1, kFirstBringer = kFinisher + 1;
@@ -323,15 +327,26 @@ struct List {
     float x[kListed];
 };
 
-__device__ __forceinline__ void workers_sync() { asm volatile("barrier.cta.sync 1, %0;" ::"n"(kWorkers) : "memory"); }
-
 __device__ __forceinline__ void first_logits_sync() { asm volatile("barrier.cta.sync 2, 64;" ::: "memory"); }
+
+// Calls, so that they take no room among the instructions of the rows' loop (1,024 rows of 128,011, all of them
+// constrained, 69.5 us, and 70.8 inlined): a warp's wait that is hardly ever one; and a CTA's share of a row's gradient as
+// NaN, by a warp: all of it, as the tokens of the warp's part of a list lie in other warps' pieces.
+__device__ __noinline__ bool ended_apart(uint32_t bar, uint32_t parity, int *gave_up) {
+    return __all_sync(~0u, bar_wait(bar, parity, gave_up));
+}
+template <typename T>
+__device__ __noinline__ void no_gradient(const PolicyArgs &a, int32_t b, int32_t rank) {
+    const Share<T> s(a, b, rank);
+    const T nan = from_f32<T>(__int_as_float(0x7FC00000));
+    for (int32_t v = s.lo + int32_t(threadIdx.x & 31); v < s.hi; v += 32) s.grad[v] = nan;
+}
 
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs a) {
     constexpr int kSize = Piece<T>::kSize;
     extern __shared__ __align__(128) unsigned char slots[];
-    __shared__ uint64_t bars[2 * kSlots + kRanks + 4];
+    __shared__ uint64_t bars[2 * kSlots + kRanks + 5];
     __shared__ Mass parts[2][32];
     __shared__ Mass ranks[kRanks][kMaxCluster];
     __shared__ __align__(16) unsigned char in_bytes[kSlots * sizeof(RowIn<T>)];
@@ -341,7 +356,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
     __shared__ int gave_up;
     const uint32_t full = smem_addr(bars), freed = full + 8 * kSlots;  // of a slot
     const uint32_t masses = freed + 8 * kSlots;                         // of a row, of all its CTAs
-    const uint32_t summed = masses + 8 * kRanks, sloped = summed + 8 * 2;
+    const uint32_t summed = masses + 8 * kRanks, sloped = summed + 8 * 2, filled = sloped + 8 * 2;
     const int lane = threadIdx.x & 31, warp = __shfl_sync(~0u, int(threadIdx.x >> 5), 0);
     const int32_t cluster = int32_t(blockIdx.x) / a.ctas, rank = int32_t(blockIdx.x) % a.ctas, V = a.V;
     if (threadIdx.x == 0) {
@@ -355,6 +370,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
             bar_init(summed + 8 * i, kWorkerWarps);
             bar_init(sloped + 8 * i, 1);
         }
+        bar_init(filled, kWorkerWarps);
         bar_init_fence();
     }
     pdl_launch_dependents();
@@ -363,6 +379,11 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
     pdl_wait();
 
     const int32_t rows = (a.B - cluster + a.clusters - 1) / a.clusters;
+    // A wait by a warp; and what it does once that is false. (The hardware's barrier takes warps that have ended for arrived.)
+    auto ended = [&](uint32_t bar, uint32_t parity) { return __all_sync(~0u, bar_wait(bar, parity, &gave_up)) != 0; };
+    auto leave = [&] {
+        if (a.ctas > 1) cluster_sync();
+    };
     if (warp >= kFirstBringer) {
         // Brings every a.slots-th row into its slot: what there is to know of it, and its share or the list of its
         // allowed tokens. What does not need the slot comes before the wait for it, and the next row's mask is on its
@@ -370,6 +391,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
         const int slot = warp - kFirstBringer;
         if (slot >= a.slots) return;
         RowIn<T> &i = in[slot];
+        bool ok = true;
         uint32_t phase = 1, word[kWordsAhead];
         auto state_of = [&](int32_t r) { return a.g.mask && r < rows ? __ldg(a.g.states + cluster + r * a.clusters) : TRIE_STATE_FREE; };
         auto c_of = [&](int32_t r) { return 1.44269504f / temperature_of(a, cluster + min(r, rows - 1) * a.clusters); };
@@ -449,7 +471,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
 #pragma unroll
             for (int k = 0; k < kListed / 32; k++) mass.sum += exp2_of((x[k] - off) * c);
             mass = warp_mass(mass, c);
-            if (!__all_sync(~0u, bar_wait(freed + 8 * slot, phase, &gave_up))) break;
+            if (!(ok = ended(freed + 8 * slot, phase))) break;
             if (lane == 0 && listed < 0) {  // first: 4,096 rows 383 us, and 390 with the row's values before it
                 const uint32_t bytes = uint32_t(s.last - s.first) * 16u;
                 bar_expect_bytes(full + 8 * slot, bytes);
@@ -475,6 +497,9 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
             __syncwarp();
             if (lane == 0) bar_arrive(full + 8 * slot);
         }
+        int none = 0;
+        if (slot < rows) ended_apart(full + 8 * slot, phase, &none);  // the CTA does not end before its copies have
+        if (!ok) leave();
         return;
     }
     if (warp == kSender) {
@@ -482,11 +507,13 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
         first_logits_sync();
         for (int32_t r = 0; r < rows; r++) {
             const float c = 1.44269504f / temperature_of(a, cluster + r * a.clusters);
-            const bool ok = bar_wait(summed + 8 * (r & 1), (r >> 1) & 1, &gave_up);
+            if (!ended(summed + 8 * (r & 1), (r >> 1) & 1)) {
+                leave();
+                return;
+            }
             Mass all = {-INFINITY, 0.0f};
             if (lane < kWorkerWarps) all = parts[r & 1][lane];
             all = warp_mass(all, c);
-            if (!__all_sync(~0u, ok)) all.sum = __int_as_float(0x7FC00000);  // gave up waiting: no result
             if (lane < a.ctas) {
                 *cluster_object(&ranks[r % kRanks][rank], lane) = all;
                 bar_arrive_cluster(cluster_addr(masses + 8 * (r % kRanks), lane));
@@ -517,11 +544,16 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
             const uint32_t word3 = mask_word(v3);
             const RowValues v4 = values(r + 4);
             const float c = 1.44269504f / v0.temperature;
-            const bool ok = bar_wait_cluster(masses + 8 * (r % kRanks), (r / kRanks) & 1, &gave_up);
+            if (!__all_sync(~0u, bar_wait_cluster(masses + 8 * (r % kRanks), (r / kRanks) & 1, &gave_up))) {
+                for (int32_t q = r + lane; rank == 0 && q < rows; q += 32)
+                    a.losses[cluster + q * a.clusters] = a.logprobs[cluster + q * a.clusters] = __int_as_float(0x7FC00000);
+                __syncwarp();
+                leave();
+                return;
+            }
             Mass all = {-INFINITY, 0.0f};
             if (lane < a.ctas) all = ranks[r % kRanks][lane];
             all = warp_mass(all, c);
-            if (!__all_sync(~0u, ok)) all.sum = __int_as_float(0x7FC00000);
             const Slope slope = finish(a, cluster + r * a.clusters, all, x0, v0, rank == 0 && lane == 0);
             x2 = __shfl_sync(~0u, x2, 0);  // it is there
             if (lane == 0) {
@@ -535,6 +567,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
 
     const int32_t worker = threadIdx.x, words = int32_t(a.g.W);
     const bool in_place = a.grad == a.logits;
+    uint32_t filled_phase = 0;
     auto fill = [&](const Share<T> &s) {  // with zeros
         const int32_t edge = worker < 16 ? s.edge(worker) : -1;
         if (edge >= 0) s.grad[edge] = from_f32<T>(0.0f);
@@ -542,8 +575,9 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
         g.set(make_uint4(0u, 0u, 0u, 0u));
         for (int32_t j = s.first + worker; j < s.last; j += kWorkers) s.store(j, g);
     };
+    // Both are false where a wait gave up.
     auto first_pass = [&](int32_t r, int slot, uint32_t phase) {
-        const bool there = bar_wait(full + 8 * slot, phase, &gave_up);
+        if (!ended(full + 8 * slot, phase)) return false;
         const RowIn<T> &i = in[slot];
         const float c = i.c;
         Mass all = {-INFINITY, 0.0f};
@@ -580,17 +614,17 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
             if (worker == 0) all = i.mass;
             if (a.grad && !in_place) fill(i.share);
         }
-        if (!there) all.sum = __int_as_float(0x7FC00000);
         all = warp_mass(all, c);
         __syncwarp();  // the zeros are written, too
         if (lane == 0) {
             parts[r & 1][warp] = all;
             bar_arrive(summed + 8 * (r & 1));
         }
+        return true;
     };
     auto second_pass = [&](int32_t r, int slot) {
-        bar_wait(sloped + 8 * (r & 1), (r >> 1) & 1, &gave_up);
-        if (!a.grad) return;
+        if (!ended(sloped + 8 * (r & 1), (r >> 1) & 1)) return false;
+        if (!a.grad) return true;
         const Slope slope = slopes[r & 1];
         const Share<T> s = in[slot].share;
         const int32_t n = s.last - s.first;
@@ -607,35 +641,45 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
                 s.store(s.first + j, slope_of(slope, p));
                 if (j == at) s.grad[slope.token] = from_f32<T>(slope.at_token);
             }
-            return;
+            return true;
         }
-        if (in_place || in[slot].listed < 0) {
-            fill(s);
-            workers_sync();
-        }
+        if (in_place || in[slot].listed < 0) fill(s);
         const int32_t listed = slope.token >= 0 ? in[slot].listed : 0;
+        if (in_place && listed > 0) {
+            __syncwarp();
+            if (lane == 0) bar_arrive(filled);
+            if (!ended_apart(filled, filled_phase, &gave_up)) return false;
+            filled_phase ^= 1;
+        }
         if (worker < listed) {
             const List &list = *reinterpret_cast<const List *>(held);
             const int32_t v = list.token[worker];
             s.grad[v] = from_f32<T>(v == slope.token ? slope.at_token : slope_of(slope, list.x[worker]));
         }
+        return true;
     };
     int slot = 0, slot_next = 0;
     uint32_t phase = 0;  // of slot_next
     auto step = [&] {
         if (++slot_next == a.slots) slot_next = 0, phase ^= 1;
     };
+    int32_t r = -1;
 #pragma unroll 1
-    for (int32_t r = -1; r < rows; r++) {
-        if (r + 1 < rows) first_pass(r + 1, slot_next, phase);
+    for (; r < rows; r++) {
+        if (r + 1 < rows && !first_pass(r + 1, slot_next, phase)) break;
         if (r >= 0) {
-            second_pass(r, slot);
+            if (!second_pass(r, slot)) break;
             __syncwarp();
             if (lane == 0) bar_arrive(freed + 8 * slot);
         }
         slot = slot_next;
         step();
     }
+    if (r == rows) return;
+    __syncwarp();
+    leave();
+    if (!a.grad) return;
+    for (r = max(r, 0); r < rows; r++) no_gradient<T>(a, cluster + r * a.clusters, rank);
 }
 
 // Longer rows: a cluster of CTAs a row, a share of its 16-byte pieces each, which
