@@ -780,8 +780,8 @@ template <typename T>
 int active_clusters(int ctas) {
     static std::atomic<int> known[16][kMaxCluster + 1];
     int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 16) return 1;
-    if ((n = known[dev][ctas].load(std::memory_order_relaxed))) return n;
+    const bool listed = cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < 16;  // else asked every time
+    if (listed && (n = known[dev][ctas].load(std::memory_order_relaxed))) return n;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(ctas));
     cfg.blockDim = dim3(kRowThreads);
@@ -798,7 +798,7 @@ int active_clusters(int ctas) {
         cudaGetLastError();
         return 0;
     }
-    known[dev][ctas].store(n, std::memory_order_relaxed);
+    if (listed) known[dev][ctas].store(n, std::memory_order_relaxed);
     return n;
 }
 

@@ -1,5 +1,15 @@
 // The policy loss with waits that give up as they would after two seconds, for test_gpu_policy_give_up.py:
-// one warp's, from a given one on, at once, the others' after 20 ms. All other code is the library's.
+// one warp's, from a given one on, at once, the others' after 20 ms; and with a current device of any
+// number. All other code is the library's.
+#include <cuda_runtime.h>
+
+static int pretended = -1;
+static cudaError_t device_now(int *device) {
+    if (pretended < 0) return cudaGetDevice(device);
+    *device = pretended;
+    return cudaSuccess;
+}
+#define cudaGetDevice device_now
 #include "blackwell.cuh"
 
 namespace tmk {
@@ -38,6 +48,9 @@ int set_error(int code, const char *) { return code; }
 #define bar_wait planned_wait<false>
 #define bar_wait_cluster planned_wait<true>
 #include "policy.cu"
+
+// What the library takes for the current device's number; -1: what it is.
+extern "C" void pretend_device(int device) { pretended = device; }
 
 // The warp whose waits give up from the one of number `after` on; block -1: none.
 extern "C" int plan_give_up(int block, int warp, int after) {

@@ -1,10 +1,12 @@
 """The policy loss where a wait within it gives up (a stalled GPU): what it writes is right or NaN, nothing else is
-written, and it ends. Built from the library's source with waits that a plan ends (policy_give_up.cu)."""
+written, and it ends; and on a device of any number. Built from the library's source with waits that a plan ends
+(policy_give_up.cu)."""
 from __future__ import annotations
 
 import ctypes
 import math
 import os
+import shutil
 import subprocess
 
 import numpy as np
@@ -32,7 +34,11 @@ def planned(cuda, tmp_path_factory):
     out = str(tmp_path_factory.mktemp("policy") / "policy_give_up.so")
     source = os.path.join(os.path.dirname(os.path.abspath(__file__)), "policy_give_up.cu")
     subprocess.run([_build.NVCC, "-shared", "-cudart", "shared", source, "-o", out, "-I", _build.CSRC, *_build.CUDA_FLAGS], check=True)
-    lib = ctypes.CDLL(out)
+    return _load(out)
+
+
+def _load(path):
+    lib = ctypes.CDLL(str(path))
     lib.trie_policy_loss.restype, lib.trie_policy_loss.argtypes = T.SIGNATURES["trie_policy_loss"]
     return lib
 
@@ -72,6 +78,19 @@ class Case:
         assert bool((losses[B:] == 7).all()) and bool((logprobs[B:] == 7).all())
         assert bool((buf[B] == 7).all()) and bool((buf[:, V:] == 7).all())
         return losses[:B], logprobs[:B], buf[:B, :V]
+
+
+def test_any_device(cuda, planned, tmp_path):
+    """A device whose number is beyond the library's tables: in a library of its own, which has not been called before."""
+    import torch
+    c = Case(cuda, 300, 60003, torch.bfloat16, False)
+    assert planned.plan_give_up(-1, 0, 0) == 0
+    want = c.run(planned)
+    lib = _load(shutil.copy(planned._name, tmp_path / "another.so"))
+    lib.pretend_device(16)
+    for _ in range(2):
+        for t, ref in zip(c.run(lib), want):
+            assert torch.equal(t, ref)
 
 
 @pytest.mark.parametrize("in_place", [False, True])
