@@ -666,7 +666,8 @@ int trie_sample(const void *d_logits, int dtype, int64_t stride, int32_t B, int3
  * whose token is outside [0, V), not allowed or of logit -inf has the
  * log-probability -inf, and like a row of weight 0 the loss 0 and a gradient of
  * zeros. A row with a NaN or +inf among its allowed logits has NaN; what other tokens'
- * logits hold does not matter. All in 32 bits; the gradient is rounded once to the logits' type.
+ * logits hold does not matter. All in 32 bits; where a factor that is 0 (A, p[v], or 1 - p[t]) meets one that 32 bits do not
+ * hold, the product is 0. The gradient is rounded once to the logits' type.
  *   d_tokens        device int32[B]
  *   d_old_logprobs, d_advantages  device float[B]
  *   d_ref_logprobs  device float[B] or NULL (no KL term, as for kl = 0)

@@ -209,7 +209,8 @@ __device__ __forceinline__ Slope finish(const PolicyArgs &a, int32_t b, const Ma
     float loss = 0.0f, slope = 0.0f;
     if (lp != -INFINITY && v.weight != 0.0f) {
         const float rho = expf(lp - v.old);
-        const float free = rho * v.advantage, held = fminf(fmaxf(rho, a.low), a.high) * v.advantage;
+        // no advantage, no surrogate, if the ratio is infinite too
+        const float free = v.advantage == 0.0f ? 0.0f : rho * v.advantage, held = fminf(fmaxf(rho, a.low), a.high) * v.advantage;
         loss = -(free > held ? held : free);  // a NaN stays one
         slope = free > held ? 0.0f : -free;
         if (a.ref) {
@@ -224,11 +225,15 @@ __device__ __forceinline__ Slope finish(const PolicyArgs &a, int32_t b, const Ma
         a.losses[b] = loss;
         a.logprobs[b] = lp;
     }
-    const float per = 1.0f / v.temperature;
-    return {all.top, 1.44269504f / v.temperature, -slope / all.sum * per, slope * -expm1f(lp) * per, slope == 0.0f ? -1 : v.token};
+    const float per = 1.0f / v.temperature, others = -expm1f(lp);
+    return {all.top, 1.44269504f / v.temperature, -slope / all.sum * per, others == 0.0f ? 0.0f : slope * others * per,
+            slope == 0.0f ? -1 : v.token};
 }
-// Of a token that is not allowed (or has no probability, for which it is the same) 0, whatever f is.
-__device__ __forceinline__ float slope_of(const Slope &s, float x) { return x == -INFINITY ? 0.0f : s.f * exp2_of((x - s.top) * s.c); }
+// Of a token that is not allowed 0, whatever f is, and of one whose probability is 0 in 32 bits, unless f is a NaN.
+__device__ __forceinline__ float slope_of(const Slope &s, float x) {
+    const float e = exp2_of((x - s.top) * s.c);
+    return x == -INFINITY || (e == 0.0f && fabsf(s.f) == INFINITY) ? 0.0f : s.f * e;
+}
 
 // Of a piece. f exp2() is 0 where x is -inf, unless f is not a number of its own.
 template <typename T>
