@@ -46,7 +46,10 @@ class DecodeLoop:
         def every(value, dtype=torch.float32):
             return torch.full((B,), value, dtype=dtype, device=dev)
         self.gain, self.head_bits = gain, head_bits
-        self.weight = T.trie_head_quantize_weight(weight) if head_bits == 8 else T.trie_head4_quantize(weight)
+        if head_bits == 8:
+            self.w, self.w_scales = T.trie_head_quantize_weight(weight)
+        else:
+            self.w, self.w_scales, self.w_row_scales = T.trie_head4_quantize(weight)
         self.embedding = weight.to(torch.float32) * D ** 0.5
         self.hidden = torch.zeros(B, D, device=dev)
         self.logits = torch.empty(B, V, dtype=torch.bfloat16, device=dev)
@@ -69,6 +72,11 @@ class DecodeLoop:
         free = torch.arange(B + 1, device=dev, dtype=torch.int32) - constrained
         self.bias = (free.clamp_(min=0), every(V - 1, torch.int32), every(-float("inf")))
         self.graph = None
+
+    @property
+    def weight(self):
+        """The head's weights as its call takes them."""
+        return (self.w, self.w_scales) if self.head_bits == 8 else (self.w, self.w_scales, self.w_row_scales)
 
     def head(self) -> None:
         """self.logits of self.hidden under the grammar."""

@@ -60,3 +60,17 @@ def test_decode_loop_refusals():
         decode.DecodeLoop(None, None, w, prompts, 3, 8)
     with pytest.raises(ValueError):
         decode.DecodeLoop(None, None, w, prompts, 0, 3)
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+def test_head_weights(bits):
+    """A loop's quantized weights can be read, and others put in their place."""
+    import torch
+    loop, w, _ = decode.example(4, 2, 4, D=128, head_bits=bits)
+    assert loop.w.shape == (w.V, 128 if bits == 8 else 64) and loop.w_scales.dtype is (torch.float32 if bits == 8 else torch.float8_e4m3fn)
+    assert len(loop.weight) == (2 if bits == 8 else 3) and loop.weight[0] is loop.w and loop.weight[1] is loop.w_scales
+    loop.head()
+    assert bool((loop.logits[2:, :-1] != 0).any())
+    loop.w = torch.zeros_like(loop.w)
+    loop.head()
+    assert bool((loop.logits[2:, :-1] == 0).all())
