@@ -664,9 +664,10 @@ int trie_sample(const void *d_logits, int dtype, int64_t stride, int32_t B, int3
  *   dloss / dlogit[v] = slope ((v = t) - p[v]) / temperature, 0 where v is not allowed
  * with A the advantage and clip(rho) in [1 - clip_low, 1 + clip_high]. A row
  * whose token is outside [0, V), not allowed or of logit -inf has the
- * log-probability -inf, and like a row of weight 0 the loss 0 and a gradient of
- * zeros. A row with a NaN or +inf among its allowed logits has NaN; what other tokens'
- * logits hold does not matter. All in 32 bits; where a factor that is 0 (A, p[v], or 1 - p[t]) meets one that 32 bits do not
+ * log-probability -inf, the loss 0 and a gradient of zeros, whatever its other logits
+ * hold (padding may hold anything). Any other row with a NaN or +inf among its allowed logits has
+ * NaN: log-probability, and unless its weight is 0 the loss and the allowed tokens' gradient. A weight of 0
+ * gives a loss of 0 and a gradient of zeros. What the logits of tokens hold that are not allowed does not matter. All in 32 bits; where a factor that is 0 (A, p[v], or 1 - p[t]) meets one that 32 bits do not
  * hold, the product is 0. The gradient is rounded once to the logits' type.
  *   d_tokens        device int32[B]
  *   d_old_logprobs, d_advantages  device float[B]

@@ -1,4 +1,5 @@
-"""The policy loss where a ratio, a slope or a temperature's reciprocal leaves the range of 32 bits."""
+"""The policy loss where a ratio, a slope or a temperature's reciprocal leaves the range of 32 bits, and rows without a
+token beside a NaN."""
 from __future__ import annotations
 
 import math
@@ -6,6 +7,7 @@ import math
 import numpy as np
 import pytest
 
+import logits_ref as lref
 from paper_2608_12574_gb300 import triemask as T
 from test_gpu_policy import _type, cuda  # noqa: F401
 
@@ -65,3 +67,32 @@ def test_ratio_beyond_32_bits(cuda, V, dtype):  # noqa: F811
         assert float((grad[b].float().cpu() - want).abs().max()) <= abs(slope) * (1e-4 + (2.0 ** -8 if dtype == "bf16" else 0))
     assert grad[2, 0] == math.inf and bool((grad[2, 3::3] == -math.inf).all()) and bool((grad[2, 1::3] == 0).all())
     assert not bool(grad[3].isnan().any())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+@pytest.mark.parametrize("V", SIZES)
+def test_no_token_beside_nan(cuda, V, value, dtype):  # noqa: F811
+    """A row without a token (outside the vocabulary, not allowed, of logit -inf) has the loss 0 and zeros whatever its allowed
+    logits hold; one with a token has NaN, and with weight 0 the log-probability alone."""
+    import torch
+    allowed = np.ones((2, V), bool)
+    allowed[1] = False
+    allowed[1, [3, 9, V - 1]] = True
+    allowed[0, 6] = False
+    tokens = [-1, V, 6, 8, 4, 2 ** 31 - 1, 6, 8, 8, 9, 4, 3]
+    states = [0, 0, 0, 0, -3, 1, 1, 1, 0, 1, -3, 1]
+    weights = [1.0] * 10 + [0.0] * 2
+    x = torch.from_numpy(np.random.default_rng(V).normal(0, 1, (12, V)).astype(np.float32)).to(_type(dtype)).to(cuda)
+    x[:, V - 1] = value
+    x[3, 8] = x[4, 4] = -math.inf
+    x[10, 4] = 1.0
+    losses, lp, grad = _run(cuda, x, tokens, [-3.0] * 12, [1.0] * 12, weights, refs=[-3.0] * 12, kl=0.1,
+                            mask=torch.from_numpy(lref.pack(allowed)).to(cuda), states=torch.tensor(states, dtype=torch.int32, device=cuda))
+    none = [0, 1, 2, 3, 4, 5, 6, 7]
+    assert bool((losses[none] == 0).all()) and bool((lp[none] == -math.inf).all()) and bool((grad[none] == 0).all())
+    assert bool(losses[8:10].isnan().all()) and bool(lp[8:].isnan().all())
+    for b, s in ((8, 0), (9, 1)):
+        ok = torch.from_numpy(allowed[s]).to(cuda)
+        assert bool(grad[b][ok].isnan().all()) and bool((grad[b][~ok] == 0).all())
+    assert bool((losses[10:] == 0).all()) and bool((grad[10:] == 0).all())
