@@ -619,9 +619,6 @@ cudaError_t launch_held(NormArgs a, int threads, cudaStream_t st) {
 
 template <typename TX, typename TR, bool kNorm, int kBits>
 cudaError_t launch_rows(const NormArgs &a, cudaStream_t st) {
-    // Few rows: a step a thread, as many threads as that takes, for the shortest chain (256 rows, D 4,096 4.6
-    // us, and 6.1 in two steps). Else two, or four where two are not enough, so that what a warp does
-    // for a row is shared by more of its columns.
     const int32_t eights = int32_t((int64_t(a.D) + 63) / 64 * 64 / kEach);
     auto threads = [&](int steps) { return ((eights + steps - 1) / steps + 31) / 32 * 32; };
     if (a.M <= 2 * sm_count()) {
