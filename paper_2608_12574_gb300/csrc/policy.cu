@@ -232,7 +232,7 @@ __device__ __forceinline__ Slope finish(const PolicyArgs &a, int32_t b, const Ma
 // Of a token that is not allowed 0, whatever f is, and of one whose probability is 0 in 32 bits, unless f is a NaN.
 __device__ __forceinline__ float slope_of(const Slope &s, float x) {
     const float e = exp2_of((x - s.top) * s.c);
-    return x == -INFINITY || (e == 0.0f && fabsf(s.f) == INFINITY) ? 0.0f : s.f * e;
+    return x == -INFINITY || (e == 0.0f && s.f == s.f) ? 0.0f : s.f * e;
 }
 
 // Of a piece. f exp2() is 0 where x is -inf, unless f is not a number of its own.
@@ -334,9 +334,15 @@ struct List {
 
 __device__ __forceinline__ void first_logits_sync() { asm volatile("barrier.cta.sync 2, 64;" ::: "memory"); }
 
-// Calls, so that they take no room among the instructions of the rows' loop (1,024 rows of 128,011, all of them
-// constrained, 69.5 us, and 70.8 inlined): a warp's wait that is hardly ever one; and a CTA's share of a row's gradient as
-// NaN, by a warp: all of it, as the tokens of the warp's part of a list lie in other warps' pieces.
+// Calls, so that they take no room among the instructions of the rows' loop, and without an address of the kernel's own
+// variables, which it would keep on a stack then (1,024 rows of 128,011, all of them constrained, 69.6 us, and 70.8 inlined;
+// 4,096 rows of 152,064 370 us, and 380 with a stack): a warp's waits that are hardly ever ones; and a CTA's share of a row's
+// gradient as NaN, by a warp: all of it, as the tokens of the warp's part of a list lie in other warps' pieces.
+__device__ __noinline__ void copies_end(uint32_t bar, uint32_t parity) {
+    int none = 0;
+    bar_wait(bar, parity, &none);
+    __syncwarp();
+}
 __device__ __noinline__ bool ended_apart(uint32_t bar, uint32_t parity, int *gave_up) {
     return __all_sync(~0u, bar_wait(bar, parity, gave_up));
 }
@@ -502,8 +508,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
             __syncwarp();
             if (lane == 0) bar_arrive(full + 8 * slot);
         }
-        int none = 0;
-        if (slot < rows) ended_apart(full + 8 * slot, phase, &none);  // the CTA does not end before its copies have
+        if (slot < rows) copies_end(full + 8 * slot, phase);  // the CTA does not before they do
         if (!ok) leave();
         return;
     }
