@@ -14,9 +14,11 @@
 //   128 rows, V 152,064, D 4,096: 63 us, 5.9 TB/s; 512 rows 116 us, 5.5 PFLOP/s.
 //   256 rows, V 152,064, D 4,096: 73 us, 5.9 TB/s, with the norm in front 75: HBM, whose reads are 128
 //     bytes of each of 128 rows at a time.
-//   1,000 rows, V 128,000, D 4,096: 181 us, 5.8 PFLOP/s; the MMAs alone take 120 (8-bit head: 463).
+//   256 rows of which half are constrained: 90 us, all in tiles.
+//   1,000 rows, V 128,000, D 4,096: 181 to 190 us, 5.5 PFLOP/s and more, f32 212; the MMAs alone take 120 (8-bit head: 463).
+//     V 128,011, whose rows of logits start at any two or four bytes: 193, f32 219.
 //   D 4,112, whose rows of codes start off 128-byte lines, so that a stage's 128 bytes of a row are parts of two:
-//     128 rows, V 128,000, 77 us; 1,000 rows 259, f32 314; V 128,011, whose logits start at any two or four bytes, 261, f32 330.
+//     128 rows, V 128,000, 77 us; 1,000 rows 259, f32 314; V 128,011 261 to 270, f32 309 to 335.
 //   256 constrained rows (15 tokens each), V 152,064, D 4,096, with the norm: 45 us, -inf to 78 MB behind a
 //     chain of waits, in which a token's scales are 64 sectors of their own.
 #include <math.h>
@@ -161,8 +163,9 @@ __device__ __forceinline__ void store16(const HeadOut &a, const float *x, int32_
 
 // The same for rows that do not all start on 32-byte boundaries, 64 tokens of a row a thread: shifted, so that whole 32
 // bytes that lie on such a boundary are written at once; those that reach into the next 64 tokens too, by the thread
-// that has the first of them, where it reads the others (`next`). 1,000 rows, V 128,011, D 4,112: f32 246 us, bf16
-// 218; 278 and 242 without `next`, so that both sides' threads write a part; 290 and 261 turned in shared memory, a row an instruction.
+// that has the first of them, where it reads the others (`next`). 1,000 rows, V 128,011, D 4,096: f32 219 us, bf16
+// 193; 250 and 222 without `next`, so that both sides' threads write a part. (Turned in shared memory, a row an instruction,
+// some 44 more than with it, at D 4,112.)
 template <typename T>
 struct Shifted {
     static constexpr int kPieces = kColumns * int(sizeof(T)) / 32;
