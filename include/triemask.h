@@ -668,7 +668,7 @@ int trie_sample(const void *d_logits, int dtype, int64_t stride, int32_t B, int3
  * hold (padding may hold anything). Any other row with a NaN or +inf among its allowed logits has
  * NaN: log-probability, and unless its weight is 0 the loss and the allowed tokens' gradient. A weight of 0
  * gives a loss of 0 and a gradient of zeros. What the logits of tokens hold that are not allowed does not matter. All in 32 bits; where a factor that is 0 (A, p[v], or 1 - p[t]) meets one that 32 bits do not
- * hold, the product is 0. The gradient is rounded once to the logits' type.
+ * hold, the product is 0 (a NaN stays one). The gradient is rounded once to the logits' type.
  *   d_tokens        device int32[B]
  *   d_old_logprobs, d_advantages  device float[B]
  *   d_ref_logprobs  device float[B] or NULL (no KL term, as for kl = 0)
@@ -676,7 +676,7 @@ int trie_sample(const void *d_logits, int dtype, int64_t stride, int32_t B, int3
  *                   sum the gradient is of
  *   d_temperature   device float[B] or NULL (1); as in trie_sample, not above 0 is 1
  *   clip_low        in [0, 1];  clip_high, kl >= 0
- *   d_losses, d_logprobs  device float[B]
+ *   d_losses, d_logprobs  device float[B], apart from each other and from the inputs
  *   d_grad          device [B] rows of V, grad_stride elements apart, of the
  *                   logits' type, or NULL (no gradient); may be d_logits itself
  *                   (with the same stride), else apart from it

@@ -210,7 +210,7 @@ __device__ __forceinline__ Slope finish(const PolicyArgs &a, int32_t b, const Ma
     if (lp != -INFINITY && v.weight != 0.0f) {
         const float rho = expf(lp - v.old);
         // no advantage, no surrogate, if the ratio is infinite too
-        const float free = v.advantage == 0.0f ? 0.0f : rho * v.advantage, held = fminf(fmaxf(rho, a.low), a.high) * v.advantage;
+        const float free = v.advantage == 0.0f && rho == INFINITY ? 0.0f : rho * v.advantage, held = fminf(fmaxf(rho, a.low), a.high) * v.advantage;
         loss = -(free > held ? held : free);  // a NaN stays one
         slope = free > held ? 0.0f : -free;
         if (a.ref) {
@@ -226,7 +226,7 @@ __device__ __forceinline__ Slope finish(const PolicyArgs &a, int32_t b, const Ma
         a.logprobs[b] = lp;
     }
     const float per = 1.0f / v.temperature, others = -expm1f(lp);
-    return {all.top, 1.44269504f / v.temperature, -slope / all.sum * per, others == 0.0f ? 0.0f : slope * others * per,
+    return {all.top, 1.44269504f / v.temperature, -slope / all.sum * per, others == 0.0f && slope == slope ? 0.0f : slope * others * per,
             slope == 0.0f ? -1 : v.token};
 }
 // Of a token that is not allowed 0, whatever f is, and of one whose probability is 0 in 32 bits, unless f is a NaN.
@@ -508,7 +508,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_policy_rows(const PolicyArgs
             __syncwarp();
             if (lane == 0) bar_arrive(full + 8 * slot);
         }
-        if (slot < rows) copies_end(full + 8 * slot, phase);  // the CTA does not before they do
+        if (slot < rows) copies_end(full + 8 * slot, phase);  // before the CTA does
         if (!ok) leave();
         return;
     }

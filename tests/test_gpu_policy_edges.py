@@ -96,3 +96,18 @@ def test_no_token_beside_nan(cuda, V, value, dtype):  # noqa: F811
         ok = torch.from_numpy(allowed[s]).to(cuda)
         assert bool(grad[b][ok].isnan().all()) and bool((grad[b][~ok] == 0).all())
     assert bool((losses[10:] == 0).all()) and bool((grad[10:] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", SIZES)
+def test_nan_beside_zero(cuda, V, dtype):  # noqa: F811
+    """A NaN is none of the values that 32 bits do not hold: beside an advantage of 0, or a probability of 1, it stays."""
+    import torch
+    x = torch.from_numpy(np.random.default_rng(V).normal(0, 1, (5, V)).astype(np.float32)).to(_type(dtype)).to(cuda)
+    x[0, V - 2] = math.nan          # a logit
+    x[2] = -300.0
+    x[2, 5] = 300.0                 # the token's probability is 1
+    losses, lp, grad = _run(cuda, x, [5] * 5, [-3.0, math.nan, 0.0, -3.0, -3.0], [0.0, 0.0, math.nan, math.nan, 0.0], clip=(0.2, 0.2))
+    assert bool(losses[:4].isnan().all()) and bool(grad[:4].isnan().all())
+    assert bool(lp[0].isnan()) and bool(lp[1:].isfinite().all())
+    assert losses[4] == 0 and bool((grad[4] == 0).all())
